@@ -232,6 +232,42 @@ int slimpipe_attn_fwd_ranges(const slimpipe_attn_params* p, const void* q_slice,
                              int32_t n_ranges, const int64_t* kv_begin, const int64_t* kv_end,
                              float* part_out, float* part_lse, void* out, float* lse, void* hip_stream);
 
+/* Sparse attention over key blocks that a cheap score selects for each query row.
+ * Keys come in blocks: block j holds positions [j * block_len, (j + 1) * block_len).  The three calls below make the blocks' means,
+ * pick the blocks of every query row and head, and attend to the keys of these blocks; slimpipe_attn_block_bwd is the gradient of the
+ * last with the picks held fixed (they are a choice and have none).  As with every call here the key range [kv_begin, kv_end) may be a
+ * part of the prefix, so that the (out, lse) of several ranges can be folded by slimpipe_attn_merge.
+ *   block_len : a multiple of 64, 64 .. 65536 (SLIMPIPE_EINVAL_SHAPE otherwise); with several chunks chunk_len is a multiple of it.
+ *   top_k     : 1 .. 64 slots per row (SLIMPIPE_EINVAL_SHAPE otherwise; also for more than 2^30 slots of one kv head and 2^34 in all,
+ *               or batch * n_kv_heads > 65535).
+ *   index     : int32 [batch, n_q_heads, s_q, top_k], contiguous.
+ *   means     : float32 [batch, n_kv_heads, ceil(kv_capacity / block_len), head_dim], contiguous. */
+
+/* Means of the blocks that hold a key of [kv_begin, kv_end): mean j = the average of the keys of block j before kv_end (summed in 64
+ * bits, rounded once).  kv_begin is a multiple of block_len (SLIMPIPE_EINVAL_RANGE otherwise); other blocks' means are untouched, so a
+ * cache that grows by slices has every slice's first and new blocks made as it comes.  Of p the query side (s_q, n_q_heads, strides,
+ * q_offset) is only validated; v is not needed. */
+int slimpipe_attn_block_means(const slimpipe_attn_params* p, const void* const* k_chunks, int32_t n_chunks, int64_t chunk_len, int32_t block_len,
+                              float* means, void* hip_stream);
+
+/* The blocks of every query row and head, as ascending indices, filled up with -1.  Blocks of the range compete by q . mean (in 64 bits,
+ * scale left out); the top_k largest are taken, of equal ones the lower index, NaN last.  causal: a row's own block, the one that
+ * holds position q_offset + row, is always taken (where the range has it) and counts as one of the top_k, only blocks before it
+ * compete, and its mean is not used. */
+int slimpipe_attn_block_select(const slimpipe_attn_params* p, const void* q_slice, const float* means, int32_t block_len, int32_t top_k, int32_t* index,
+                               void* hip_stream);
+
+/* Device workspace of slimpipe_attn_block_fwd (is_bwd = 0) or _bwd; both refuse less (SLIMPIPE_EWORKSPACE).  Mostly one float32 result row of
+ * head_dim per (row, head, slot): what the blocks of a row give before they are folded. */
+int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, int is_bwd, size_t* bytes);
+
+/* Forward: row r of head h attends to the keys that slimpipe_attn_fwd would let it see and that lie in one of its blocks.  Any index will
+ * do: entries outside the range's blocks are no block, a block named twice counts once, order is free.  out, lse, rows without a key and
+ * keys that no row sees: as in slimpipe_attn_fwd.  Results do not depend on the order in which workgroups run. */
+int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
+                            int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* hip_stream);
+
 const char* slimpipe_attn_strerror(int code);
 
 #ifdef __cplusplus

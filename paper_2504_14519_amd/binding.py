@@ -93,6 +93,15 @@ def _load():
     L.slimpipe_attn_merge.restype = ctypes.c_int
     L.slimpipe_attn_finalize_bf16.argtypes = [vp, vp, i64, vp]
     L.slimpipe_attn_finalize_bf16.restype = ctypes.c_int
+    szp = ctypes.POINTER(ctypes.c_size_t)
+    L.slimpipe_attn_block_means.argtypes = [P, pp, i32, i64, i32, vp, vp]
+    L.slimpipe_attn_block_means.restype = ctypes.c_int
+    L.slimpipe_attn_block_select.argtypes = [P, vp, vp, i32, i32, vp, vp]
+    L.slimpipe_attn_block_select.restype = ctypes.c_int
+    L.slimpipe_attn_block_workspace_bytes.argtypes = [P, i32, i32, ctypes.c_int, szp]
+    L.slimpipe_attn_block_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_block_fwd.argtypes = [P, vp, pp, pp, i32, i64, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_block_fwd.restype = ctypes.c_int
     L.slimpipe_attn_mfma_rate.argtypes = [ctypes.c_int, vp, ctypes.POINTER(ctypes.c_double), vp]
     L.slimpipe_attn_mfma_rate.restype = ctypes.c_int
     L.slimpipe_attn_dq_atomic_probe.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -343,6 +352,94 @@ def slimpipe_attn_finalize_bf16(acc, dst=None):
         dst = torch.empty(acc.shape, device=acc.device, dtype=torch.bfloat16)
     _check(lib.slimpipe_attn_finalize_bf16(acc.data_ptr(), dst.data_ptr(), acc.numel(), _stream()), "finalize_bf16")
     return dst
+
+
+def _as_chunks(x):
+    return x if isinstance(x, (list, tuple)) else [x]
+
+
+def _kv_like(chunks):
+    return chunks[0] if len(chunks) == 1 else _ChunkedKV(chunks)
+
+
+def _check_index(index, q_slice):
+    B, s, Hq, _ = q_slice.shape
+    if index.dtype != torch.int32 or index.dim() != 4 or index.shape[:3] != (B, Hq, s) or not index.is_contiguous():
+        raise SlimpipeError("index must be a contiguous int32 tensor [batch, query heads, rows, top_k]")
+    return index.shape[3]
+
+
+def _check_means(means, batch, kv_heads, blocks, head_dim):
+    if means.dtype != torch.float32 or tuple(means.shape) != (batch, kv_heads, blocks, head_dim) or not means.is_contiguous():
+        raise SlimpipeError("means must be a contiguous float32 tensor [batch, kv heads, ceil(keys / block_len), head_dim]")
+
+
+def slimpipe_attn_block_means(k_chunks, kv_begin, kv_end, block_len, means=None):
+    """-> means [B, Hkv, ceil(keys / block_len), D] fp32: those of the blocks that hold a key of [kv_begin, kv_end) are written (kv_begin a
+    multiple of block_len), the others left as they are (zero where the call allocates).  k_chunks: one tensor or a list of chunks."""
+    chunks = _as_chunks(k_chunks)
+    k = _kv_like(chunks)
+    B, N, Hkv, D = k.shape
+    blocks = -(-N // block_len) if block_len > 0 else 0
+    if means is None:
+        means = torch.zeros((B, Hkv, blocks, D), device=chunks[0].device, dtype=torch.float32)
+    _check_means(means, B, Hkv, blocks, D)
+    one = torch.Size((B, 1, Hkv, D))
+    p = AttnParams(B, 1, Hkv, Hkv, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *_contiguous_strides(one), *k.stride()[:3], *_contiguous_strides(one),
+                   *_contiguous_strides(one))
+    _check(lib.slimpipe_attn_block_means(ctypes.byref(p), _chunk_table(chunks), len(chunks), chunks[0].shape[1], block_len, means.data_ptr(),
+                                         _stream()), "slimpipe_attn_block_means")
+    return means
+
+
+def _contiguous_strides(shape):
+    return shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3]
+
+
+def slimpipe_attn_block_select(q_slice, means, q_offset, kv_begin, kv_end, block_len, top_k, causal=True, index=None):
+    """-> index [B, Hq, s, top_k] int32: the blocks of every query row, ascending, filled up with -1."""
+    B, s, Hq, D = q_slice.shape
+    Hkv, blocks = means.shape[1], means.shape[2]
+    _check_means(means, B, Hkv, blocks, D)
+    if index is None:
+        index = torch.empty((B, Hq, s, top_k), device=q_slice.device, dtype=torch.int32)
+    if _check_index(index, q_slice) != top_k:
+        raise SlimpipeError("index must have top_k entries a row")
+    sq = q_slice.stride()
+    p = AttnParams(B, s, Hq, Hkv, D, 1 if causal else 0, blocks * block_len, q_offset, kv_begin, kv_end, 1.0, BF16, sq[0], sq[1], sq[2],
+                   Hkv * D, Hkv * D, D, sq[0], sq[1], sq[2], sq[0], sq[1], sq[2])
+    _check(lib.slimpipe_attn_block_select(ctypes.byref(p), q_slice.data_ptr(), means.data_ptr(), block_len, top_k, index.data_ptr(), _stream()),
+           "slimpipe_attn_block_select")
+    return index
+
+
+def _block_ws(p, block_len, top_k, is_bwd):
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_block_workspace_bytes(ctypes.byref(p), block_len, top_k, 1 if is_bwd else 0, ctypes.byref(n)), "block_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_block_workspace_bytes(q_slice, k_chunks, index, q_offset, kv_begin, kv_end, block_len, causal=True, is_bwd=False):
+    """Bytes of workspace that slimpipe_attn_block_fwd (or _bwd) of these tensors needs."""
+    p = _params(q_slice, _kv_like(_as_chunks(k_chunks)), q_slice, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)
+    return _block_ws(p, block_len, _check_index(index, q_slice), is_bwd)
+
+
+def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_begin, kv_end, block_len, causal=True, scale=None, out_dtype=BF16,
+                            out=None, lse=None, workspace=None):
+    """-> (out, lse): slimpipe_attn_fwd restricted to the keys of the blocks that `index` names for each row.  k_chunks / v_chunks: one
+    tensor each or lists of chunks.  workspace: uint8 tensor, allocated where None."""
+    k_chunks, v_chunks = _as_chunks(k_chunks), _as_chunks(v_chunks)
+    top_k = _check_index(index, q_slice)
+    if out is None or lse is None:
+        out, lse = _outputs(q_slice, out_dtype, out, lse)
+    p = _params(q_slice, _kv_like(k_chunks), out, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    if workspace is None:
+        workspace = torch.empty(_block_ws(p, block_len, top_k, False), device=q_slice.device, dtype=torch.uint8)
+    _check(lib.slimpipe_attn_block_fwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
+                                       k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                       *_ws(workspace), _stream()), "slimpipe_attn_block_fwd")
+    return out, lse
 
 
 KERNEL_KINDS = ("fwd", "delta", "dq", "dkdv", "merge", "finalize", "dkdv_reduce", "dq_reduce",

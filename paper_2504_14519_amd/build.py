@@ -7,7 +7,8 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslimpipe_attn.so")
-SOURCES = ["api.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_small.hip", "attn_aux.hip"]
+SOURCES = ["api.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_small.hip", "attn_aux.hip",
+           "block_api.hip", "block_select.hip", "block_fwd.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffast-math", "-fno-finite-math-only",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
@@ -26,7 +27,7 @@ def _compile(src, verbose):
 
 
 def build(verbose=False):
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
     r = subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs],
                        capture_output=True, text=True)

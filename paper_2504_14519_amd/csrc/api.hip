@@ -8,6 +8,8 @@
 
 #include "../../include/slimpipe_attn.h"
 #include "../../include/slimpipe_attn_bench.h"
+#include "blocks.hpp"
+#include "host_common.hpp"
 #include "kernels.hpp"
 
 using namespace slimpipe;
@@ -21,9 +23,6 @@ constexpr size_t kScratchTicketBytes = 256;                // + the counters the
 static __device__ __align__(256) unsigned char scratch[kScratchBytes + kScratchTicketBytes];
 
 namespace {
-
-bool stride_ok(int64_t s) { return s > 0 && (s % 8) == 0; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // one float array per row statistic (delta, lse in log2 units), each rounded up to 256 bytes
 size_t stat_bytes(const slimpipe_attn_params* p) {
@@ -44,8 +43,9 @@ struct DeviceState {
 DeviceState g_device[kMaxDevices];
 std::atomic<int> g_compute_units[kMaxDevices];
 
-// Makes the current device ready for launches: SLIMPIPE_OK, or SLIMPIPE_ELAUNCH when the runtime refuses.
-int ensure_device_ready(void** scratch_ptr = nullptr) {
+}  // namespace
+
+int slimpipe::ensure_device_ready(void** scratch_ptr) {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return SLIMPIPE_ELAUNCH;
   DeviceState& d = g_device[dev];
@@ -53,6 +53,8 @@ int ensure_device_ready(void** scratch_ptr = nullptr) {
     d.status = opt_in_fwd_kernels();
     if (d.status == hipSuccess) d.status = opt_in_bwd_kernels();
     if (d.status == hipSuccess) d.status = opt_in_small_kernels();
+    if (d.status == hipSuccess) d.status = opt_in_block_select_kernels();
+    if (d.status == hipSuccess) d.status = opt_in_block_fwd_kernels();
     if (d.status == hipSuccess) d.status = hipGetSymbolAddress(&d.scratch, HIP_SYMBOL(scratch));
     if (d.status == hipSuccess && d.scratch == nullptr) d.status = hipErrorInvalidSymbol;
   });
@@ -60,9 +62,7 @@ int ensure_device_ready(void** scratch_ptr = nullptr) {
   return d.status == hipSuccess ? SLIMPIPE_OK : SLIMPIPE_ELAUNCH;
 }
 
-// Compute units of the current device (256 on MI355X, also assumed when no device can be asked, so that the
-// workspace query stays a pure host function).
-int compute_units() {
+int slimpipe::compute_units() {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 256;
   int cus = g_compute_units[dev].load(std::memory_order_relaxed);
@@ -71,6 +71,8 @@ int compute_units() {
   g_compute_units[dev].store(cus, std::memory_order_relaxed);
   return cus;
 }
+
+namespace {
 
 // The dk/dv kernel runs one workgroup per compute unit; a call with W key tiles takes ceil(W / CUs)
 // rounds of one tile's query stream each.  Cutting every stream into S chunks makes W*S workgroups of
@@ -230,11 +232,6 @@ double fwd_small_us(const slimpipe_attn_params* p, int64_t cus, int r) {
   const double steps = (double)((keys + r * per_step - 1) / (r * per_step)), rounds = (double)((wgs + cus - 1) / cus);
   return (d64 ? 7.0 : 8.7) + 2 * (rounds - 1) + rounds * steps * (d64 ? 1.4 : 1.3) +
          (r > 1 ? 4.5 + (double)(r + 1) * p->s_q * p->n_q_heads * p->batch * p->head_dim * 4 / 4e6 : 0.0);
-}
-// One past the last key before `end` that any row sees (`begin` when none does).
-int64_t seen_end(const slimpipe_attn_params* p, int64_t begin, int64_t end) {
-  if (p->causal && p->q_offset + p->s_q < end) end = p->q_offset + p->s_q;
-  return end > begin ? end : begin;
 }
 struct FwdPlan {
   int head_waves;    // of the query blocks
@@ -491,17 +488,6 @@ void equal_work_ranges(const slimpipe_attn_params* p, int ranges, int64_t* begin
     prev = cut;
   }
 }
-
-// A chunk list is legal when it covers kv_capacity rows; with more than one chunk the chunk length is a
-// multiple of the dk/dv key tile (256), so that no key tile of any kernel straddles two chunks.
-int check_chunks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_len) {
-  if (n_chunks < 1 || n_chunks > kMaxChunks || chunk_len < 1) return SLIMPIPE_EINVAL_SHAPE;
-  if (n_chunks * chunk_len < p->kv_capacity) return SLIMPIPE_EINVAL_RANGE;
-  if (n_chunks > 1 && chunk_len % dkdv_keys_per_workgroup() != 0) return SLIMPIPE_EINVAL_SHAPE;
-  return SLIMPIPE_OK;
-}
-
-
 
 // ---- optional per-kernel event timing (benchmark aid) ----------------------------------------------
 struct ProfRecord { int kind; hipEvent_t start, stop; };

@@ -1,0 +1,204 @@
+// C ABI of sparse attention over selected key blocks: argument checks, workspace layout, launches.
+#include <math.h>
+#include <string.h>
+
+#include "blocks.hpp"
+#include "host_common.hpp"
+
+using namespace slimpipe;
+
+namespace {
+
+constexpr int kMinBlockLen = 64, kMaxBlockLen = 1 << 16;
+
+// What every block call checks beyond slimpipe_attn_validate: the block length, and that a block lies in one chunk.
+int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_len, int32_t block_len) {
+  if (block_len < kMinBlockLen || block_len > kMaxBlockLen || block_len % 64 != 0) return SLIMPIPE_EINVAL_SHAPE;
+  if (p->kv_capacity > (int64_t)block_len * INT32_MAX) return SLIMPIPE_EINVAL_SHAPE;          // block indices are 32 bits
+  const int rc = check_chunks(p, n_chunks, chunk_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (n_chunks > 1 && chunk_len % block_len != 0) return SLIMPIPE_EINVAL_SHAPE;
+  if ((int64_t)p->batch * p->n_kv_heads > 65535) return SLIMPIPE_EINVAL_SHAPE;                 // planes are a grid dimension
+  return SLIMPIPE_OK;
+}
+int check_top_k(const slimpipe_attn_params* p, int32_t top_k) {
+  if (top_k < 1 || top_k > kMaxTopK) return SLIMPIPE_EINVAL_SHAPE;
+  const int64_t rows = (int64_t)p->n_q_heads / p->n_kv_heads * p->s_q;
+  // rows and slots of a plane, and all of them as workgroups, in 32 bits
+  if (rows * top_k > (int64_t)1 << 30 || rows * p->n_kv_heads * p->batch * top_k > (int64_t)1 << 34) return SLIMPIPE_EINVAL_SHAPE;
+  return SLIMPIPE_OK;
+}
+int set_chunks(KvChunks* kv, const slimpipe_attn_params* p, const void* const* k, const void* const* v, int32_t n_chunks, int64_t chunk_len) {
+  memset(kv, 0, sizeof(*kv));
+  for (int i = 0; i < n_chunks; ++i) {
+    if (p->kv_end > 0 && (!k[i] || (v && !v[i]))) return SLIMPIPE_EINVAL_NULL;
+    if (!aligned16(k[i]) || (v && !aligned16(v[i]))) return SLIMPIPE_EINVAL_ALIGN;
+    kv->k[i] = static_cast<const __bf16*>(k[i]);
+    if (v) kv->v[i] = static_cast<const __bf16*>(v[i]);
+  }
+  kv->len = chunk_len;
+  kv->n = n_chunks;
+  return SLIMPIPE_OK;
+}
+
+// Blocks that hold a key of [begin, end).
+int64_t blocks_of(int64_t begin, int64_t end, int64_t block_len) { return end > begin ? (end + block_len - 1) / block_len - begin / block_len : 0; }
+
+int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->batch * p->n_q_heads * p->s_q; }
+
+// Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot).
+bool few_rows(const slimpipe_attn_params* p, int32_t top_k) { return rows_of(p) * top_k <= 4 * (int64_t)compute_units(); }
+
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Where the parts of the workspace lie, and its size.
+struct BlockWorkspace {
+  size_t part_out, part_lse, counts, start, entries, items, n_items, bytes;
+  int32_t n_list_chunks, item_cap;
+};
+BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists) {
+  BlockWorkspace w;
+  memset(&w, 0, sizeof(w));
+  const size_t rows = (size_t)rows_of(p), planes = (size_t)p->batch * p->n_kv_heads, plane_rows = rows / planes;
+  const size_t blocks = (size_t)blocks_of(p->kv_begin, p->kv_end, block_len);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
+  w.part_out = take(rows * top_k * p->head_dim * 4);
+  w.part_lse = take(rows * top_k * 4);
+  if (lists) {
+    w.n_list_chunks = (int32_t)((plane_rows + kListRows - 1) / kListRows);
+    // every tile but a block's last is full
+    const size_t tiles = plane_rows * top_k / kBlockTileRows + blocks, slots = plane_rows * top_k;
+    w.item_cap = (int32_t)(tiles < 1 ? 1 : tiles < slots ? tiles : slots);
+    w.counts = take(planes * w.n_list_chunks * blocks * 4);
+    w.start = take(planes * blocks * 4);
+    w.entries = take(planes * slots * sizeof(BlockEntry));
+    w.items = take(planes * w.item_cap * sizeof(BlockItem));
+    w.n_items = take(planes * 4);
+  }
+  w.bytes = at;
+  return w;
+}
+
+// The argument block of a call, without outputs.
+void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int32_t* index, int32_t block_len, int32_t top_k, const BlockWorkspace& w, char* ws) {
+  a->q = static_cast<const __bf16*>(q);
+  a->index = index;
+  a->batch = p->batch; a->s_q = p->s_q; a->n_q_heads = p->n_q_heads; a->n_kv_heads = p->n_kv_heads;
+  a->group = p->n_q_heads / p->n_kv_heads; a->causal = p->causal; a->top_k = top_k; a->block_len = block_len;
+  a->q_offset = p->q_offset; a->kv_begin = p->kv_begin; a->kv_end = seen_end(p, p->kv_begin, p->kv_end); a->kv_end_range = p->kv_end;
+  a->first_block = (int32_t)(p->kv_begin / block_len);
+  a->n_blocks = (int32_t)blocks_of(a->kv_begin, a->kv_end, block_len);
+  a->scale = p->scale; a->scale_log2e = p->scale * 1.4426950408889634f;
+  a->q_stride_b = p->q_stride_b; a->q_stride_s = p->q_stride_s; a->q_stride_h = p->q_stride_h;
+  a->kv_stride_b = p->kv_stride_b; a->kv_stride_s = p->kv_stride_s; a->kv_stride_h = p->kv_stride_h;
+  a->o_stride_b = p->o_stride_b; a->o_stride_s = p->o_stride_s; a->o_stride_h = p->o_stride_h;
+  a->do_stride_b = p->do_stride_b; a->do_stride_s = p->do_stride_s; a->do_stride_h = p->do_stride_h;
+  a->part_out = reinterpret_cast<float*>(ws + w.part_out);
+  a->part_lse = reinterpret_cast<float*>(ws + w.part_lse);
+  a->n_list_chunks = w.n_list_chunks;
+  a->counts = reinterpret_cast<uint32_t*>(ws + w.counts);
+  a->start = reinterpret_cast<uint32_t*>(ws + w.start);
+  a->entries = reinterpret_cast<BlockEntry*>(ws + w.entries);
+  a->items = reinterpret_cast<BlockItem*>(ws + w.items);
+  a->n_items = reinterpret_cast<int32_t*>(ws + w.n_items);
+  a->item_cap = w.item_cap;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? SLIMPIPE_OK : SLIMPIPE_ELAUNCH; }
+
+}  // namespace
+
+extern "C" {
+
+int slimpipe_attn_block_means(const slimpipe_attn_params* p, const void* const* k_chunks, int32_t n_chunks, int64_t chunk_len, int32_t block_len,
+                              float* means, void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!k_chunks || !means) return SLIMPIPE_EINVAL_NULL;
+  rc = check_blocks(p, n_chunks, chunk_len, block_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (p->kv_begin % block_len != 0) return SLIMPIPE_EINVAL_RANGE;
+  if (!aligned16(means)) return SLIMPIPE_EINVAL_ALIGN;
+  BlockMeansArgs a;
+  rc = set_chunks(&a.kv, p, k_chunks, nullptr, n_chunks, chunk_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  a.means = means;
+  a.batch = p->batch; a.n_kv_heads = p->n_kv_heads; a.block_len = block_len;
+  a.first_block = (int32_t)(p->kv_begin / block_len);
+  a.n_blocks = (int32_t)blocks_of(p->kv_begin, p->kv_end, block_len);
+  a.blocks_total = blocks_of(0, p->kv_capacity, block_len);
+  a.kv_end = p->kv_end;
+  a.kv_stride_b = p->kv_stride_b; a.kv_stride_s = p->kv_stride_s; a.kv_stride_h = p->kv_stride_h;
+  if (a.n_blocks == 0) return SLIMPIPE_OK;
+  return status(launch_block_means(a, p->head_dim, static_cast<hipStream_t>(hip_stream)));
+}
+
+int slimpipe_attn_block_select(const slimpipe_attn_params* p, const void* q_slice, const float* means, int32_t block_len, int32_t top_k, int32_t* index,
+                               void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!q_slice || !means || !index) return SLIMPIPE_EINVAL_NULL;
+  rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  rc = check_top_k(p, top_k);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!aligned16(q_slice) || !aligned16(means) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
+  BlockSelectArgs a;
+  a.q = static_cast<const __bf16*>(q_slice);
+  a.means = means;
+  a.index = index;
+  a.batch = p->batch; a.s_q = p->s_q; a.n_q_heads = p->n_q_heads; a.n_kv_heads = p->n_kv_heads; a.group = p->n_q_heads / p->n_kv_heads;
+  a.causal = p->causal; a.top_k = top_k; a.block_len = block_len;
+  a.first_block = (int32_t)(p->kv_begin / block_len);
+  a.n_blocks = (int32_t)blocks_of(p->kv_begin, p->kv_end, block_len);
+  a.blocks_total = blocks_of(0, p->kv_capacity, block_len);
+  a.q_offset = p->q_offset;
+  a.q_stride_b = p->q_stride_b; a.q_stride_s = p->q_stride_s; a.q_stride_h = p->q_stride_h;
+  return status(launch_block_select(a, p->head_dim, static_cast<hipStream_t>(hip_stream)));
+}
+
+int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, int is_bwd, size_t* bytes) {
+  if (!bytes) return SLIMPIPE_EINVAL_NULL;
+  int rc = slimpipe_attn_validate(p, is_bwd);
+  if (rc != SLIMPIPE_OK) return rc;
+  rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc != SLIMPIPE_OK) return rc;
+  *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, top_k)).bytes;
+  return SLIMPIPE_OK;
+}
+
+int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
+                            int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!q_slice || !k_chunks || !v_chunks || !index || !out || !lse) return SLIMPIPE_EINVAL_NULL;
+  rc = check_blocks(p, n_chunks, chunk_len, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
+  const bool few = few_rows(p, top_k);
+  const BlockWorkspace w = layout(p, block_len, top_k, !few);
+  if (!workspace || workspace_bytes < w.bytes) return SLIMPIPE_EWORKSPACE;
+  if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
+  BlockArgs a;
+  memset(&a, 0, sizeof(a));
+  rc = set_chunks(&a.kv, p, k_chunks, v_chunks, n_chunks, chunk_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
+  a.out = out;
+  a.lse = lse;
+  a.out_f32 = p->out_dtype == SLIMPIPE_F32;
+  if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (few) {
+    if (launch_block_fwd_few(a, p->head_dim, st) != hipSuccess) return SLIMPIPE_ELAUNCH;
+  } else if (launch_block_lists(a, false, st) != hipSuccess || launch_block_fwd(a, p->head_dim, st) != hipSuccess) {
+    return SLIMPIPE_ELAUNCH;
+  }
+  return status(launch_block_merge(a, p->head_dim, st));
+}
+
+}  // extern "C"

@@ -1,0 +1,261 @@
+// Forward of sparse attention over selected key blocks.
+//
+// A tile is up to 128 rows that chose one block (block_select.hip): four waves of 32 rows each, the block's keys in tiles of 64 through
+// two LDS slots.  Every (row, slot) leaves out and lse of its block's keys in 32 bits; the merge kernel folds a row's slots.
+#include "block_tile.hpp"
+#include "row_tile.hpp"
+#include "tile_common.hpp"
+
+namespace slimpipe {
+
+constexpr int kBlockTileKeys = 64;
+
+template <int D>
+constexpr size_t block_fwd_lds_bytes() {       // two slots of K and V; the output rows on their way out take their place
+  constexpr size_t rings = (size_t)4 * kBlockTileKeys * D * 2, rows = (size_t)4 * 32 * kOutRow<D> * 4;
+  return rings > rows ? rings : rows;
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
+  constexpr int BN = kBlockTileKeys, TILE = BN * D * 2;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int tile = tile_of(blockIdx.x, a.n_items[plane]);
+  if (tile < 0) return;
+  const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
+  const int n_rows = it.count;
+  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
+  const int mine = wave_u * 32 + (lane & 31);
+  const BlockEntry e = list[mine < n_rows ? mine : n_rows - 1];
+  const int h = hk * a.group + (int)(e.head_slot >> 6);
+
+  const BlockKeys keys(a, it.block, b, hk);
+  // Last key that the row sees, relative to the first of the block (negative: none), and how many the tile's rows see: keys behind
+  // these are not read (they may hold anything, and a weight of 0 times a NaN is a NaN).
+  int64_t see = keys.hi - 1;
+  if (a.causal && a.q_offset + e.row < see) see = a.q_offset + e.row;
+  const int see_rel = (int)(see - keys.lo);
+  const int n_keys = rows_max(see_rel, reinterpret_cast<int*>(smem), wave_u, lane) + 1;
+  const int nt = n_keys > 0 ? (n_keys + BN - 1) / BN : 0;
+  const unsigned lds = lds_addr(smem);
+  const uint32_t row_bytes = (uint32_t)a.kv_stride_s * 2;
+  const bf16_t* const kp = a.kv.k[keys.chunk] + keys.off;
+  const bf16_t* const vp = a.kv.v[keys.chunk] + keys.off;
+  TileDma<D, BN, 256> dma;
+  dma.init(tid);
+  auto copy = [&](int t) {
+    const int64_t off = (int64_t)t * BN * a.kv_stride_s;
+    const int left = n_keys - t * BN, avail = left < BN ? left : BN;
+    const unsigned slot = lds + (t & 1) * 2 * TILE;
+#pragma unroll
+    for (int n = 0; n < TileDma<D, BN, 256>::PASSES; ++n) dma.issue(slot, kp + off, row_bytes, avail, wave_u, n);
+#pragma unroll
+    for (int n = 0; n < TileDma<D, BN, 256>::PASSES; ++n) dma.issue(slot + TILE, vp + off, row_bytes, avail, wave_u, n);
+  };
+
+  RowState<D> st;
+  st.init();
+  if (nt > 0) {
+    copy(0);
+    {
+      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)e.row * a.q_stride_s + (int64_t)h * a.q_stride_h + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) st.q[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+    }
+    RpOffsets<D> lo_k;
+    TrOffsets<D> lo_v;
+    lo_k.init(lane, (int)lds);
+    lo_v.init(lane, (int)lds + TILE);
+    wait_async();
+    __syncthreads();
+    for (int t = 0; t < nt; ++t) {
+      if (t + 1 < nt) copy(t + 1);
+      const int kmax = see_rel - t * BN;
+      const bool masked = __builtin_amdgcn_ballot_w64(kmax < BN - 1) != 0;
+      attend_tile<D, BN>(st, lo_k, lo_v, a.scale_log2e, masked, 0, kmax, g);
+      const int step = (t & 1) ? -2 * TILE : 2 * TILE;
+      lo_k.add(step);
+      lo_v.add(step);
+      wait_async();
+      __syncthreads();
+    }
+  }
+  float lse;
+  const float norm = st.finish(&lse);
+  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
+  put_rows<D>(part, st.o, norm, lane);
+  const int64_t row = ((int64_t)b * a.n_q_heads + h) * a.s_q + e.row;
+  const int64_t slot = row * a.top_k + (e.head_slot & 63u);
+  if (lane < 32 && mine < n_rows) a.part_lse[slot] = lse;
+  constexpr int PER = D / 4, RPP = 64 / PER;
+#pragma unroll
+  for (int j = 0; j < 32 / RPP; ++j) {
+    const int r = j * RPP + lane / PER;
+    const int64_t to = __shfl(slot, r, 64);
+    if (wave_u * 32 + r < n_rows)
+      *reinterpret_cast<f32x4*>(a.part_out + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
+  }
+}
+
+// Calls of few rows (tokens): lists and tiles of 128 rows would be mostly empty, so each (row, slot) has a workgroup of its own, whose four
+// waves share out the block's keys.  D / 8 lanes a key row: products summed over these lanes, then every lane weighs its 8 elements of V.
+template <int D>
+__global__ __launch_bounds__(256) void block_fwd_few_kernel(const BlockArgs a) {
+  constexpr int NC = D / 8, PER = 64 / NC, STEP = 8;           // lanes a key, keys a wave's load, loads in flight
+  __shared__ float acc_s[4][D], m_s[4], l_s[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane / NC, c = lane % NC;
+  const int64_t item = blockIdx.x;
+  const int slot = (int)(item % a.top_k);
+  const int64_t row = item / a.top_k;
+  const int64_t bh = row / a.s_q;
+  const int r = (int)(row - bh * a.s_q), b = (int)(bh / a.n_q_heads), h = (int)(bh - (int64_t)b * a.n_q_heads), hk = h / a.group;
+  const int32_t* idx = a.index + row * a.top_k;
+  const int64_t pos = a.q_offset + r;
+  if (!block_slot_valid(a, idx, slot, pos)) {
+    if (tid == 0) a.part_lse[item] = -INFINITY;
+    return;
+  }
+  const BlockKeys keys(a, idx[slot], b, hk);
+  const int64_t hi = a.causal && pos + 1 < keys.hi ? pos + 1 : keys.hi;
+  const int n = hi > keys.lo ? (int)(hi - keys.lo) : 0;
+  const bf16_t* const kp = a.kv.k[keys.chunk] + keys.off + c * 8;
+  const bf16_t* const vp = a.kv.v[keys.chunk] + keys.off + c * 8;
+  float q[8];
+  {
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(a.q + (int64_t)b * a.q_stride_b + (int64_t)r * a.q_stride_s + (int64_t)h * a.q_stride_h + c * 8);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = (float)x[e] * a.scale_log2e;
+  }
+  float m = -INFINITY, l = 0.f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int k0 = wave * PER * STEP; k0 < n; k0 += 4 * PER * STEP) {
+    bf16x8 kx[STEP], vx[STEP];
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const int key = k0 + u * PER + sub, kc = key < n ? key : n - 1;
+      kx[u] = *reinterpret_cast<const bf16x8*>(kp + (int64_t)kc * a.kv_stride_s);
+      vx[u] = *reinterpret_cast<const bf16x8*>(vp + (int64_t)kc * a.kv_stride_s);
+    }
+    float s[STEP], mx = m;
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      float d = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d += q[e] * (float)kx[u][e];
+#pragma unroll
+      for (int w = 1; w < NC; w <<= 1) d += __shfl_xor(d, w, 64);
+      s[u] = k0 + u * PER + sub < n ? d : -INFINITY;
+      mx = fmaxf(mx, s[u]);
+    }
+    const float m_eff = mx == -INFINITY ? 0.f : mx, alpha = exp2_fast(m - m_eff);
+    m = mx;
+    l *= alpha;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= alpha;
+#pragma unroll
+    for (int u = 0; u < STEP; ++u) {
+      const float p = exp2_fast(s[u] - m_eff);
+      l += p;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += p * (float)vx[u][e];
+    }
+  }
+  // the lane groups of a wave, then the waves
+#pragma unroll
+  for (int w = NC; w < 64; w <<= 1) {
+    const float mo = __shfl_xor(m, w, 64), mn = fmaxf(m, mo), me = mn == -INFINITY ? 0.f : mn;
+    const float f = exp2_fast(m - me), fo = exp2_fast(mo - me);
+    l = l * f + __shfl_xor(l, w, 64) * fo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * f + __shfl_xor(acc[e], w, 64) * fo;
+    m = mn;
+  }
+  if (lane < NC) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc_s[wave][c * 8 + e] = acc[e];
+    if (c == 0) { m_s[wave] = m; l_s[wave] = l; }
+  }
+  __syncthreads();
+  if (tid < D) {
+    const float mx = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3])), me = mx == -INFINITY ? 0.f : mx;
+    float sum = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(m_s[w] - me);
+      sum += l_s[w] * f;
+      o += acc_s[w][tid] * f;
+    }
+    const bool has = sum > 0.f;
+    a.part_out[item * D + tid] = has ? o / sum : 0.f;
+    if (tid == 0) a.part_lse[item] = has ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// lse = ln sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s over the slots of a row, in slot order; D / 8 lanes a row.
+template <int D>
+__global__ __launch_bounds__(256) void block_merge_kernel(const BlockArgs a) {
+  constexpr int NC = D / 8;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
+  const int c = (int)(gid - row * NC);
+  if (row >= (int64_t)a.batch * a.n_q_heads * a.s_q) return;
+  const float* lp = a.part_lse + row * a.top_k;
+  const float* op = a.part_out + row * a.top_k * D + c * 8;
+  float m = -INFINITY;
+  for (int s = 0; s < a.top_k; ++s) m = fmaxf(m, lp[s]);
+  f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
+  float sum = 0.f;
+  if (m != -INFINITY)
+#pragma unroll 4
+    for (int s = 0; s < a.top_k; ++s) {
+      const float ls = lp[s];
+      if (ls == -INFINITY) continue;                 // (its partial out was not written)
+      const float w = exp2_fast((ls - m) * kLog2e);
+      sum += w;
+      x0 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D);
+      x1 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D + 4);
+    }
+  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
+  const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
+  const int64_t to = b * a.o_stride_b + (row - bh * a.s_q) * a.o_stride_s + (bh - b * a.n_q_heads) * a.o_stride_h + c * 8;
+  x0 *= inv;
+  x1 *= inv;
+  if (a.out_f32) {
+    f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
+    dst[0] = x0;
+    dst[1] = x1;
+  } else {
+    const bf16x4 lo = __builtin_convertvector(x0, bf16x4), hi = __builtin_convertvector(x1, bf16x4);
+    *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  if (c == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(sum) * kLn2;
+}
+
+hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st) {
+  dim3 grid((unsigned)((a.item_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(block_fwd_kernel<128>, grid, block, block_fwd_lds_bytes<128>(), st, a);
+  else hipLaunchKernelGGL(block_fwd_kernel<64>, grid, block, block_fwd_lds_bytes<64>(), st, a);
+  return hipGetLastError();
+}
+hipError_t launch_block_fwd_few(const BlockArgs& a, int head_dim, hipStream_t st) {
+  dim3 grid((unsigned)((int64_t)a.batch * a.n_q_heads * a.s_q * a.top_k)), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(block_fwd_few_kernel<128>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(block_fwd_few_kernel<64>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_block_merge(const BlockArgs& a, int head_dim, hipStream_t st) {
+  const int64_t lanes = (int64_t)a.batch * a.n_q_heads * a.s_q * (head_dim / 8);
+  dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(block_merge_kernel<128>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(block_merge_kernel<64>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t opt_in_block_fwd_kernels() {
+  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_fwd_kernel<128>), attr, (int)block_fwd_lds_bytes<128>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_fwd_kernel<64>), attr, (int)block_fwd_lds_bytes<64>());
+  return e;
+}
+
+}  // namespace slimpipe
