@@ -268,6 +268,14 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
                             int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
                             size_t workspace_bytes, void* hip_stream);
 
+/* Backward of slimpipe_attn_block_fwd with the same index: gradients through the attention to the chosen keys.  out, lse, dq, dk / dv
+ * (a chunk list as k / v), accumulation, row and key order independence and shared memory are as in slimpipe_attn_bwd(_chunked); keys of the range that no
+ * row chose or sees get 0 (or nothing is added). */
+int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
+                            int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, const void* out, const void* d_out, const float* lse,
+                            void* dq, int32_t dq_dtype, int32_t dq_accumulate, float* const* dk_chunks, float* const* dv_chunks, int32_t dkv_accumulate,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* slimpipe_attn_strerror(int code);
 
 #ifdef __cplusplus

@@ -102,6 +102,8 @@ def _load():
     L.slimpipe_attn_block_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_block_fwd.argtypes = [P, vp, pp, pp, i32, i64, i32, i32, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_block_fwd.restype = ctypes.c_int
+    L.slimpipe_attn_block_bwd.argtypes = [P, vp, pp, pp, i32, i64, i32, i32, vp, vp, vp, vp, vp, i32, i32, pp, pp, i32, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_block_bwd.restype = ctypes.c_int
     L.slimpipe_attn_mfma_rate.argtypes = [ctypes.c_int, vp, ctypes.POINTER(ctypes.c_double), vp]
     L.slimpipe_attn_mfma_rate.restype = ctypes.c_int
     L.slimpipe_attn_dq_atomic_probe.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -431,6 +433,8 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
     tensor each or lists of chunks.  workspace: uint8 tensor, allocated where None."""
     k_chunks, v_chunks = _as_chunks(k_chunks), _as_chunks(v_chunks)
     top_k = _check_index(index, q_slice)
+    if len(k_chunks) != len(v_chunks) or not _same_strides(v_chunks[0], k_chunks[0]):
+        raise SlimpipeError("v must have as many chunks as k, of the same shape and strides")
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     p = _params(q_slice, _kv_like(k_chunks), out, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
@@ -440,6 +444,31 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
                                        k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                        *_ws(workspace), _stream()), "slimpipe_attn_block_fwd")
     return out, lse
+
+
+def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse, q_offset, kv_begin, kv_end, block_len, dk_chunks, dv_chunks,
+                            causal=True, scale=None, dq=None, dq_dtype=BF16, dq_accumulate=False, dkv_accumulate=True, workspace=None):
+    """-> dq: the gradients of slimpipe_attn_block_fwd with the same index.  dk_chunks / dv_chunks (fp32, one tensor each or lists, shaped like
+    the keys) get rows [kv_begin, kv_end) written or incremented."""
+    k_chunks, v_chunks, dk_chunks, dv_chunks = (list(_as_chunks(x)) for x in (k_chunks, v_chunks, dk_chunks, dv_chunks))
+    top_k = _check_index(index, q_slice)
+    if dq is None:
+        dq = torch.empty_like(q_slice, dtype=torch.float32 if dq_dtype == F32 else torch.bfloat16)
+    if not _same_strides(dq, q_slice):
+        raise SlimpipeError("dq must have the strides of q")
+    for c in v_chunks + dk_chunks + dv_chunks:
+        if not _same_strides(c, k_chunks[0]):
+            raise SlimpipeError("v, dk and dv must have the strides of k")
+    if not len(k_chunks) == len(v_chunks) == len(dk_chunks) == len(dv_chunks):
+        raise SlimpipeError("k, v, dk and dv must have the same number of chunks")
+    p = _params(q_slice, _kv_like(k_chunks), out, d_out, q_offset, kv_begin, kv_end, causal, scale, BF16)
+    if workspace is None:
+        workspace = torch.empty(_block_ws(p, block_len, top_k, True), device=q_slice.device, dtype=torch.uint8)
+    _check(lib.slimpipe_attn_block_bwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
+                                       k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), d_out.data_ptr(), lse.data_ptr(),
+                                       dq.data_ptr(), dq_dtype, 1 if dq_accumulate else 0, _chunk_table(dk_chunks), _chunk_table(dv_chunks),
+                                       1 if dkv_accumulate else 0, *_ws(workspace), _stream()), "slimpipe_attn_block_bwd")
+    return dq
 
 
 KERNEL_KINDS = ("fwd", "delta", "dq", "dkdv", "merge", "finalize", "dkdv_reduce", "dq_reduce",

@@ -55,6 +55,7 @@ int slimpipe::ensure_device_ready(void** scratch_ptr) {
     if (d.status == hipSuccess) d.status = opt_in_small_kernels();
     if (d.status == hipSuccess) d.status = opt_in_block_select_kernels();
     if (d.status == hipSuccess) d.status = opt_in_block_fwd_kernels();
+    if (d.status == hipSuccess) d.status = opt_in_block_bwd_kernels();
     if (d.status == hipSuccess) d.status = hipGetSymbolAddress(&d.scratch, HIP_SYMBOL(scratch));
     if (d.status == hipSuccess && d.scratch == nullptr) d.status = hipErrorInvalidSymbol;
   });

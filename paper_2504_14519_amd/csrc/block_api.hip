@@ -14,7 +14,7 @@ constexpr int kMinBlockLen = 64, kMaxBlockLen = 1 << 16;
 // What every block call checks beyond slimpipe_attn_validate: the block length, and that a block lies in one chunk.
 int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_len, int32_t block_len) {
   if (block_len < kMinBlockLen || block_len > kMaxBlockLen || block_len % 64 != 0) return SLIMPIPE_EINVAL_SHAPE;
-  if (p->kv_capacity > (int64_t)block_len * INT32_MAX) return SLIMPIPE_EINVAL_SHAPE;          // block indices are 32 bits
+  if (p->kv_capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;                         // block indices, in parts of 64 keys, are 32 bits
   const int rc = check_chunks(p, n_chunks, chunk_len);
   if (rc != SLIMPIPE_OK) return rc;
   if (n_chunks > 1 && chunk_len % block_len != 0) return SLIMPIPE_EINVAL_SHAPE;
@@ -53,10 +53,16 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where the parts of the workspace lie, and its size.
 struct BlockWorkspace {
-  size_t part_out, part_lse, counts, start, entries, items, n_items, bytes;
-  int32_t n_list_chunks, item_cap;
+  size_t part_out, part_lse, counts, start, entries, items, n_items, delta, lse2, dkdv_items, n_dkdv_items, sums, dkdv_part, bytes;
+  int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
-BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists) {
+// Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but 2048 at least, because every part of
+// a list writes its sums (128 KB for 128 keys of head_dim 128) and a reduce reads them again.
+int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub) {
+  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units());
+  return (int32_t)(rows < 2048 ? 2048 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
+}
+BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {
   BlockWorkspace w;
   memset(&w, 0, sizeof(w));
   const size_t rows = (size_t)rows_of(p), planes = (size_t)p->batch * p->n_kv_heads, plane_rows = rows / planes;
@@ -75,6 +81,22 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.entries = take(planes * slots * sizeof(BlockEntry));
     w.items = take(planes * w.item_cap * sizeof(BlockItem));
     w.n_items = take(planes * 4);
+  }
+  if (is_bwd) {
+    w.delta = take(rows * 4);
+    w.lse2 = take(rows * 4);
+    const size_t slots = plane_rows * top_k;
+    const int32_t keys = block_dkdv_keys(block_len);
+    w.n_sub = (block_len + keys - 1) / keys;
+    w.chunk_rows = dkdv_chunk_rows((int64_t)(rows * top_k), w.n_sub);
+    // a list of n rows has at most n / chunk_rows + 1 parts, and partial sums only when n > chunk_rows: then at most twice n / chunk_rows
+    w.dkdv_cap = (int32_t)((slots / w.chunk_rows + blocks) * w.n_sub);
+    if (w.dkdv_cap < 1) w.dkdv_cap = 1;
+    w.part_cap = (int32_t)(2 * slots / w.chunk_rows);
+    w.dkdv_items = take(planes * w.dkdv_cap * sizeof(BlockItem));
+    w.n_dkdv_items = take(planes * 4);
+    w.sums = take(planes * blocks * sizeof(BlockItem));
+    w.dkdv_part = take(planes * w.part_cap * 2 * (size_t)(w.n_sub * keys) * p->head_dim * 4);
   }
   w.bytes = at;
   return w;
@@ -103,6 +125,13 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->items = reinterpret_cast<BlockItem*>(ws + w.items);
   a->n_items = reinterpret_cast<int32_t*>(ws + w.n_items);
   a->item_cap = w.item_cap;
+  a->delta = reinterpret_cast<float*>(ws + w.delta);
+  a->lse2 = reinterpret_cast<float*>(ws + w.lse2);
+  a->chunk_rows = w.chunk_rows; a->n_sub = w.n_sub; a->dkdv_cap = w.dkdv_cap; a->part_cap = w.part_cap;
+  a->dkdv_items = reinterpret_cast<BlockItem*>(ws + w.dkdv_items);
+  a->n_dkdv_items = reinterpret_cast<int32_t*>(ws + w.n_dkdv_items);
+  a->sums = reinterpret_cast<BlockItem*>(ws + w.sums);
+  a->dkdv_part = reinterpret_cast<float*>(ws + w.dkdv_part);
 }
 
 int status(hipError_t e) { return e == hipSuccess ? SLIMPIPE_OK : SLIMPIPE_ELAUNCH; }
@@ -165,7 +194,7 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
   rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
   if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
   if (rc != SLIMPIPE_OK) return rc;
-  *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, top_k)).bytes;
+  *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, top_k), is_bwd != 0).bytes;
   return SLIMPIPE_OK;
 }
 
@@ -180,7 +209,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
   const bool few = few_rows(p, top_k);
-  const BlockWorkspace w = layout(p, block_len, top_k, !few);
+  const BlockWorkspace w = layout(p, block_len, top_k, !few, false);
   if (!workspace || workspace_bytes < w.bytes) return SLIMPIPE_EWORKSPACE;
   if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
   BlockArgs a;
@@ -199,6 +228,58 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
     return SLIMPIPE_ELAUNCH;
   }
   return status(launch_block_merge(a, p->head_dim, st));
+}
+
+int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
+                            int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, const void* out, const void* d_out, const float* lse,
+                            void* dq, int32_t dq_dtype, int32_t dq_accumulate, float* const* dk_chunks, float* const* dv_chunks, int32_t dkv_accumulate,
+                            void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 1);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!q_slice || !k_chunks || !v_chunks || !index || !out || !d_out || !lse || !dq || !dk_chunks || !dv_chunks) return SLIMPIPE_EINVAL_NULL;
+  rc = check_blocks(p, n_chunks, chunk_len, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (dq_dtype != SLIMPIPE_BF16 && dq_dtype != SLIMPIPE_F32) return SLIMPIPE_EINVAL_SHAPE;
+  if (dq_accumulate && dq_dtype != SLIMPIPE_F32) return SLIMPIPE_EINVAL_SHAPE;
+  if (!aligned16(q_slice) || !aligned16(out) || !aligned16(d_out) || !aligned16(dq) || !aligned4(lse) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
+  const BlockWorkspace w = layout(p, block_len, top_k, true, true);
+  if (!workspace || workspace_bytes < w.bytes) return SLIMPIPE_EWORKSPACE;
+  if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
+  BlockArgs a;
+  memset(&a, 0, sizeof(a));
+  rc = set_chunks(&a.kv, p, k_chunks, v_chunks, n_chunks, chunk_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  for (int i = 0; i < n_chunks; ++i) {
+    if (!dk_chunks[i] || !dv_chunks[i]) return SLIMPIPE_EINVAL_NULL;
+    if (!aligned16(dk_chunks[i]) || !aligned16(dv_chunks[i])) return SLIMPIPE_EINVAL_ALIGN;
+    a.dk_acc[i] = dk_chunks[i];
+    a.dv_acc[i] = dv_chunks[i];
+  }
+  fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
+  a.d_out = static_cast<const __bf16*>(d_out);
+  a.dq = dq;
+  a.dq_f32 = dq_dtype == SLIMPIPE_F32; a.dq_accumulate = dq_accumulate ? 1 : 0; a.dkv_accumulate = dkv_accumulate ? 1 : 0;
+  if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  // delta and lse in log2 units as for the dense backward, ahead of all that writes a gradient
+  BwdArgs d;
+  memset(&d, 0, sizeof(d));
+  d.out = static_cast<const __bf16*>(out);
+  d.d_out = a.d_out;
+  d.lse = lse;
+  d.delta = const_cast<float*>(a.delta);
+  d.lse2 = const_cast<float*>(a.lse2);
+  d.s_q = p->s_q; d.n_q_heads = p->n_q_heads;
+  d.o_stride_b = p->o_stride_b; d.o_stride_s = p->o_stride_s; d.o_stride_h = p->o_stride_h;
+  d.do_stride_b = p->do_stride_b; d.do_stride_s = p->do_stride_s; d.do_stride_h = p->do_stride_h;
+  hipError_t e = launch_delta(d, p->batch, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_lists(a, true, st);
+  if (e == hipSuccess) e = launch_block_bwd_dq(a, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_dq_reduce(a, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_bwd_dkdv(a, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_dkdv_reduce(a, p->head_dim, st);
+  return status(e);
 }
 
 }  // extern "C"

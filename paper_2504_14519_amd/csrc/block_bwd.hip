@@ -1,0 +1,431 @@
+// Backward of sparse attention over selected key blocks.
+//
+// With p_ij = exp(scale q_i.k_j - lse_i) on the visible pairs of the chosen blocks and delta_i = dO_i . O_i:
+//   dV_j = sum_i p_ij dO_i            dS_ij = p_ij (dO_i . v_j - delta_i)
+//   dQ_i = scale sum_j dS_ij k_j      dK_j  = scale sum_i dS_ij q_i
+// As in the dense backward dq and dk/dv have kernels of their own, both over the lists of block_select.hip:
+//   dq     tiles of 128 rows of one block, as in the forward; each (row, slot) leaves a partial dq that a last kernel adds in slot order
+//   dk/dv  a workgroup owns 128 (block length 64: 64) keys and walks the rows that chose their block, 32 at a time; long lists are
+//          cut into parts whose sums a last kernel adds in list order.
+// No sum depends on the order in which workgroups run.
+#include "block_tile.hpp"
+#include "row_tile.hpp"
+
+namespace slimpipe {
+
+constexpr int kDqKeys = 64;
+
+template <int D>
+constexpr size_t block_dq_lds_bytes() {
+  constexpr size_t rings = (size_t)4 * kDqKeys * D * 2, rows = (size_t)4 * 32 * kOutRow<D> * 4;
+  return rings > rows ? rings : rows;
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
+  constexpr int BN = kDqKeys, TILE = BN * D * 2, KS = D / 16, DB = D / 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int tile = tile_of(blockIdx.x, a.n_items[plane]);
+  if (tile < 0) return;
+  const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
+  const int n_rows = it.count;
+  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
+  const int mine = wave_u * 32 + (lane & 31);
+  const BlockEntry e = list[mine < n_rows ? mine : n_rows - 1];
+  const int h = hk * a.group + (int)(e.head_slot >> 6);
+  const int64_t row = ((int64_t)b * a.n_q_heads + h) * a.s_q + e.row;
+
+  const BlockKeys keys(a, it.block, b, hk);
+  int64_t see = keys.hi - 1;
+  if (a.causal && a.q_offset + e.row < see) see = a.q_offset + e.row;
+  const int see_rel = (int)(see - keys.lo);
+  const int n_keys = rows_max(see_rel, reinterpret_cast<int*>(smem), wave_u, lane) + 1;      // (keys behind are not read)
+  const int nt = n_keys > 0 ? (n_keys + BN - 1) / BN : 0;
+  const unsigned lds = lds_addr(smem);
+  const uint32_t row_bytes = (uint32_t)a.kv_stride_s * 2;
+  const bf16_t* const kp = a.kv.k[keys.chunk] + keys.off;
+  const bf16_t* const vp = a.kv.v[keys.chunk] + keys.off;
+  TileDma<D, BN, 256> dma;
+  dma.init(tid);
+  auto copy = [&](int t) {
+    const int64_t off = (int64_t)t * BN * a.kv_stride_s;
+    const int left = n_keys - t * BN, avail = left < BN ? left : BN;
+    const unsigned slot = lds + (t & 1) * 2 * TILE;
+#pragma unroll
+    for (int n = 0; n < TileDma<D, BN, 256>::PASSES; ++n) dma.issue(slot, kp + off, row_bytes, avail, wave_u, n);
+#pragma unroll
+    for (int n = 0; n < TileDma<D, BN, 256>::PASSES; ++n) dma.issue(slot + TILE, vp + off, row_bytes, avail, wave_u, n);
+  };
+
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dq[db][i] = 0.f;
+  if (nt > 0) {
+    copy(0);
+    bf16x8 q[KS], d_o[KS];
+    {
+      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)e.row * a.q_stride_s + (int64_t)h * a.q_stride_h + 8 * g;
+      const bf16_t* op = a.d_out + (int64_t)b * a.do_stride_b + (int64_t)e.row * a.do_stride_s + (int64_t)h * a.do_stride_h + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) d_o[ks] = *reinterpret_cast<const bf16x8*>(op + 16 * ks);
+    }
+    const float lse2 = a.lse2[row], ndelta = a.delta[row], c = a.scale_log2e;      // (lse2 +inf for a row without keys: p = 0)
+    RpOffsets<D> lo_k;
+    TrOffsets<D> lo_kt;
+    lo_k.init(lane, (int)lds);
+    lo_kt.init(lane, (int)lds);
+    wait_async();
+    __syncthreads();
+    for (int t = 0; t < nt; ++t) {
+      if (t + 1 < nt) copy(t + 1);
+      const int kmax = see_rel - t * BN;
+      const bool masked = __builtin_amdgcn_ballot_w64(kmax < BN - 1) != 0;
+#pragma unroll
+      for (int kb = 0; kb < BN / 32; ++kb) {
+        f32x16 s, dp;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s[i] = 0.f; dp[i] = ndelta; }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          s = mfma32(lds_rp<D>(lo_k, ks, kb * 32 * D * 2), q[ks], s);
+          dp = mfma32(lds_rp<D>(lo_k, ks, TILE + kb * 32 * D * 2), d_o[ks], dp);
+        }
+        if (masked) {
+          const int hi = kmax - kb * 32 - 4 * g;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) <= hi ? s[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], c, -lse2)) * dp[i];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const bf16x8 ds = pack8(s, 8 * half);      // (rounded to bf16 for the matrix unit, as in the dense backward)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) dq[db] = mfma32(lds_tr<D>(lo_kt, db, (2 * kb + half) * 16 * D * 2), ds, dq[db]);
+        }
+      }
+      const int step = (t & 1) ? -2 * TILE : 2 * TILE;
+      lo_k.add(step);
+      lo_kt.add(step);
+      wait_async();
+      __syncthreads();
+    }
+  }
+  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
+  put_rows<D>(part, dq, a.scale, lane);
+  const int64_t slot = row * a.top_k + (e.head_slot & 63u);
+  constexpr int PER = D / 4, RPP = 64 / PER;
+#pragma unroll
+  for (int j = 0; j < 32 / RPP; ++j) {
+    const int r = j * RPP + lane / PER;
+    const int64_t to = __shfl(slot, r, 64);
+    if (wave_u * 32 + r < n_rows)
+      *reinterpret_cast<f32x4*>(a.part_out + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
+  }
+}
+
+// dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.
+template <int D>
+__global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a) {
+  constexpr int NC = D / 4;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
+  const int c = (int)(gid - row * NC) * 4;
+  if (row >= (int64_t)a.batch * a.n_q_heads * a.s_q) return;
+  const float* lp = a.part_lse + row * a.top_k;
+  const float* src = a.part_out + row * a.top_k * D + c;
+  f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = 0; s < a.top_k; ++s)
+    if (lp[s] != -INFINITY) x += *reinterpret_cast<const f32x4*>(src + (int64_t)s * D);
+  const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
+  const int64_t to = b * a.q_stride_b + (row - bh * a.s_q) * a.q_stride_s + (bh - b * a.n_q_heads) * a.q_stride_h + c;
+  if (a.dq_f32) {
+    f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.dq) + to);
+    if (a.dq_accumulate) x += *dst;
+    *dst = x;
+  } else {
+    *reinterpret_cast<bf16x4*>(static_cast<bf16_t*>(a.dq) + to) = __builtin_convertvector(x, bf16x4);
+  }
+}
+
+// ------------------------------------------------------------------------------------ dk / dv
+int block_dkdv_keys(int block_len) { return block_len >= 128 ? 128 : 64; }
+
+template <int D, int NW>
+struct BlockDkdvLds {
+  static constexpr int TILE = 32 * D * 2;                  // 32 rows of Q or dO
+  static constexpr int V = 4 * TILE, STAT = V + NW * 32 * D * 2, STAT_BYTES = 3 * 32 * 4;      // {Q, dO} x 2, V, {lse2, -delta, position} x 2
+  static constexpr int RINGS = STAT + 2 * STAT_BYTES, OUT = NW * 32 * kOutRow<D> * 4;
+  static constexpr int TOTAL = RINGS > OUT ? RINGS : OUT;
+};
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs a) {
+  using L = BlockDkdvLds<D, NW>;
+  constexpr int KS = D / 16, DB = D / 32, NC = D / 8, T = NW * 64, RPP = T / NC, PASSES = 32 / RPP, KEYS = NW * 32;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int item = tile_of(blockIdx.x, a.n_dkdv_items[plane]);
+  if (item < 0) return;
+  const BlockItem it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
+  const int block = it.block / a.n_sub, sub = it.block - block * a.n_sub, n_rows = it.count;
+  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
+
+  // keys [lo, hi) of the block that exist, the workgroup's first one
+  const int64_t key0 = (int64_t)block * a.block_len + sub * KEYS;
+  const int64_t end = (int64_t)(block + 1) * a.block_len < a.kv_end ? (int64_t)(block + 1) * a.block_len : a.kv_end;
+  const int kmin = a.kv_begin > key0 ? (a.kv_begin - key0 < KEYS ? (int)(a.kv_begin - key0) : KEYS) : 0;
+  const int kmax = end - key0 < KEYS ? (int)(end - key0) : KEYS;          // keys [kmin, kmax) of the workgroup exist
+  if (kmax <= kmin) return;
+  const int chunk = kv_chunk_of(a.kv, key0);
+  const int64_t off = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + (key0 - (int64_t)chunk * a.kv.len) * a.kv_stride_s;
+  const unsigned lds = lds_addr(smem);
+
+  // K as B operand: column = my key (clamped to those that exist), k-slots = head_dim 16 ks + 8 g ..; V rows in LDS
+  const int key = wave_u * 32 + ql;
+  bf16x8 kreg[KS];
+  {
+    const int kc = key < kmin ? kmin : (key < kmax ? key : kmax - 1);
+    const bf16_t* kp = a.kv.k[chunk] + off + (int64_t)kc * a.kv_stride_s + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kreg[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
+  }
+  {
+    const bf16_t* vp = a.kv.v[chunk] + off;
+    WaveDma<D, 32> dma;
+    dma.init(lane, (uint32_t)a.kv_stride_s * 2);
+    const int w0 = wave_u * 32;
+    const int first = kmin > w0 ? (kmin - w0 < 32 ? kmin - w0 : 31) : 0, avail = kmax - w0 > 0 ? kmax - w0 : 0;
+    if (avail > 0 && kmin - w0 < 32) dma.copy(lds + L::V + w0 * D * 2, vp + (int64_t)w0 * a.kv_stride_s, (uint32_t)a.kv_stride_s * 2, first, avail, lane);
+  }
+  // This thread's part of a tile copy: rows tid / NC + n * RPP, the chunk that the swizzle puts at its place.
+  const int crow = tid / NC, cpos = tid % NC;
+  auto chunk_of = [&](int r) {
+    return D == 128 ? ((((cpos >> 2) ^ r) & 3) << 2) | (((cpos & 3) ^ (r >> 2)) & 3) : (cpos ^ r) & (NC - 1);
+  };
+  const bf16_t* const qb = a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h;
+  const bf16_t* const ob = a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h;
+  const int64_t stat0 = ((int64_t)b * a.n_q_heads + hk * a.group) * a.s_q;
+  auto entry = [&](int i) { return list[i < n_rows ? i : n_rows - 1]; };
+  BlockEntry ec[PASSES], es;                     // entries of the next tile to copy: the rows this thread copies, the row whose statistics it brings
+  auto fetch = [&](int u) {
+#pragma unroll
+    for (int n = 0; n < PASSES; ++n) ec[n] = entry(u * 32 + crow + n * RPP);
+    es = entry(u * 32 + (tid & 31));
+  };
+  auto copy = [&](int u) {
+    const unsigned slot = lds + (u & 1) * 2 * L::TILE + wave_u * 1024;
+#pragma unroll
+    for (int n = 0; n < PASSES; ++n) {
+      const int64_t hl = ec[n].head_slot >> 6, c8 = chunk_of(crow + n * RPP) * 8;
+      dma16_at(qb + hl * a.q_stride_h + (int64_t)ec[n].row * a.q_stride_s + c8, slot + n * T * 16);
+      dma16_at(ob + hl * a.do_stride_h + (int64_t)ec[n].row * a.do_stride_s + c8, slot + L::TILE + n * T * 16);
+    }
+  };
+  float s_lse2, s_ndelta;
+  int s_pos;
+  auto load_stats = [&](int u) {
+    const int64_t i = stat0 + (int64_t)(es.head_slot >> 6) * a.s_q + es.row;
+    s_lse2 = u * 32 + (tid & 31) < n_rows ? a.lse2[i] : INFINITY;      // (rows past the list's end: p = 0)
+    s_ndelta = a.delta[i];
+    const int64_t rel = a.q_offset + es.row - key0;                    // last key of the workgroup that the row sees
+    s_pos = !a.causal || rel > KEYS ? KEYS : (rel < -1 ? -1 : (int)rel);
+  };
+  auto put_stats = [&](int u) {
+    float* st = reinterpret_cast<float*>(smem + L::STAT + (u & 1) * L::STAT_BYTES);
+    if (tid < 32) { st[tid] = s_lse2; st[32 + tid] = s_ndelta; reinterpret_cast<int*>(st)[64 + tid] = s_pos; }
+  };
+
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { dk[db][i] = 0.f; dv[db][i] = 0.f; }
+  const int nt = (n_rows + 31) / 32;
+  fetch(0);
+  load_stats(0);
+  copy(0);
+  fetch(1);
+  put_stats(0);
+  RpOffsets<D> lo_q, lo_v;
+  TrOffsets<D> lo_t;
+  lo_q.init(lane, (int)lds);
+  lo_t.init(lane, (int)lds);
+  lo_v.init(lane, (int)lds + L::V + wave_u * 32 * D * 2);
+  wait_async();
+  __syncthreads();
+  const float c = a.scale_log2e;
+  for (int u = 0; u < nt; ++u) {
+    if (u + 1 < nt) {
+      load_stats(u + 1);
+      copy(u + 1);
+      fetch(u + 2);
+    }
+    const float* st = reinterpret_cast<const float*>(smem + L::STAT + (u & 1) * L::STAT_BYTES);
+    f32x16 s, dp;
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4 nd = *reinterpret_cast<const f32x4*>(st + 32 + 8 * i4 + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { s[4 * i4 + e] = 0.f; dp[4 * i4 + e] = nd[e]; }
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      s = mfma32(lds_rp<D>(lo_q, ks, 0), kreg[ks], s);
+      dp = mfma32(lds_rp<D>(lo_q, ks, L::TILE), lds_rp<D>(lo_v, ks, 0), dp);
+    }
+    const int pos_lane = reinterpret_cast<const int*>(st)[64 + ql];
+    if (__builtin_amdgcn_ballot_w64(pos_lane < wave_u * 32 + 31) != 0) {      // some row does not see all keys of the wave
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 ps = *reinterpret_cast<const i32x4*>(st + 64 + 8 * i4 + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key > ps[e]) { s[4 * i4 + e] = -INFINITY; dp[4 * i4 + e] = 0.f; }      // (what no row sees may be NaN)
+      }
+    }
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4 l2 = *reinterpret_cast<const f32x4*>(st + 8 * i4 + 4 * g);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[4 * i4 + e] = exp2_fast(__builtin_fmaf(s[4 * i4 + e], c, -l2[e]));
+        dp[4 * i4 + e] *= s[4 * i4 + e];
+      }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8 p = pack8(s, 8 * half), ds = pack8(dp, 8 * half);      // (bf16 for the matrix unit)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        dv[db] = mfma32(lds_tr<D>(lo_t, db, L::TILE + half * 16 * D * 2), p, dv[db]);
+        dk[db] = mfma32(lds_tr<D>(lo_t, db, half * 16 * D * 2), ds, dk[db]);
+      }
+    }
+    const int step = (u & 1) ? -2 * L::TILE : 2 * L::TILE;
+    lo_q.add(step);
+    lo_t.add(step);
+    wait_async();
+    if (u + 1 < nt) put_stats(u + 1);
+    __syncthreads();
+  }
+
+  // rows [kmin, kmax) of the workgroup: to the accumulators, or to the partial sums of this part of the list
+  const int keys_pad = a.n_sub * KEYS;
+  float *kdst, *vdst;
+  int64_t stride;
+  bool accumulate = false;
+  if (it.part >= 0) {
+    kdst = a.dkdv_part + (((int64_t)plane * a.part_cap + it.part) * 2 * keys_pad + sub * KEYS) * D;
+    vdst = kdst + (int64_t)keys_pad * D;
+    stride = D;
+  } else {
+    kdst = a.dk_acc[chunk] + off;
+    vdst = a.dv_acc[chunk] + off;
+    stride = a.kv_stride_s;
+    accumulate = a.dkv_accumulate != 0;
+  }
+  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
+  constexpr int PER = D / 4, OPP = 64 / PER;
+  const int d4 = lane % PER * 4;
+  auto flush = [&](const f32x16 (&acc)[DB], float factor, float* dst) {
+    put_rows<D>(part, acc, factor, lane);
+#pragma unroll
+    for (int j = 0; j < 32 / OPP; ++j) {
+      const int r = j * OPP + lane / PER, kr = wave_u * 32 + r;
+      if (kr < kmin || kr >= kmax) continue;
+      f32x4 v = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d4);
+      f32x4* to = reinterpret_cast<f32x4*>(dst + (int64_t)kr * stride + d4);
+      if (accumulate) v += *to;
+      *to = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  flush(dk, a.scale, kdst);
+  flush(dv, 1.0f, vdst);
+}
+
+// dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.
+template <int D>
+__global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs a, int keys_pad) {
+  constexpr int NC = D / 4;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.kv_end_range - a.kv_begin, kk = gid / NC;
+  const int c = (int)(gid - kk * NC) * 4, plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  if (kk >= n) return;
+  const int64_t key = a.kv_begin + kk;
+  const int64_t block = key / a.block_len, j = block - a.first_block;
+  BlockItem sums = {0, 0, 0, 0};
+  if (key < a.kv_end) sums = a.sums[(int64_t)plane * a.n_blocks + j];
+  const int len = sums.block, parts = sums.first;
+  if (len > 0 ? parts == 0 : a.dkv_accumulate != 0) return;
+  const int chunk = kv_chunk_of(a.kv, key);
+  const int64_t to = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + (key - (int64_t)chunk * a.kv.len) * a.kv_stride_s + c;
+  f32x4* kd = reinterpret_cast<f32x4*>(a.dk_acc[chunk] + to);
+  f32x4* vd = reinterpret_cast<f32x4*>(a.dv_acc[chunk] + to);
+  f32x4 k4 = {0, 0, 0, 0}, v4 = {0, 0, 0, 0};
+  const float* src = a.dkdv_part + (((int64_t)plane * a.part_cap + sums.count) * 2 * keys_pad + (key - block * a.block_len)) * D + c;
+#pragma unroll 4
+  for (int i = 0; i < parts; ++i) {
+    k4 += *reinterpret_cast<const f32x4*>(src + (int64_t)i * 2 * keys_pad * D);
+    v4 += *reinterpret_cast<const f32x4*>(src + (int64_t)(2 * i + 1) * keys_pad * D);
+  }
+  if (a.dkv_accumulate) { k4 += *kd; v4 += *vd; }
+  *kd = k4;
+  *vd = v4;
+}
+
+hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st) {
+  dim3 grid((unsigned)((a.item_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(block_dq_kernel<128>, grid, block, block_dq_lds_bytes<128>(), st, a);
+  else hipLaunchKernelGGL(block_dq_kernel<64>, grid, block, block_dq_lds_bytes<64>(), st, a);
+  return hipGetLastError();
+}
+hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
+  const int64_t lanes = (int64_t)a.batch * a.n_q_heads * a.s_q * (head_dim / 4);
+  dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(block_dq_reduce_kernel<128>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(block_dq_reduce_kernel<64>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+template <int D, int NW>
+static void launch_dkdv_t(const BlockArgs& a, hipStream_t st) {
+  dim3 grid((unsigned)((a.dkdv_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(NW * 64);
+  hipLaunchKernelGGL((block_dkdv_kernel<D, NW>), grid, block, (BlockDkdvLds<D, NW>::TOTAL), st, a);
+}
+hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st) {
+  const bool wide = block_dkdv_keys(a.block_len) == 128;
+  if (head_dim == 128) wide ? launch_dkdv_t<128, 4>(a, st) : launch_dkdv_t<128, 2>(a, st);
+  else wide ? launch_dkdv_t<64, 4>(a, st) : launch_dkdv_t<64, 2>(a, st);
+  return hipGetLastError();
+}
+hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
+  const int64_t lanes = (a.kv_end_range - a.kv_begin) * (head_dim / 4);
+  if (lanes <= 0) return hipSuccess;
+  dim3 grid((unsigned)((lanes + 255) / 256), (unsigned)(a.batch * a.n_kv_heads)), block(256);
+  const int keys_pad = a.n_sub * block_dkdv_keys(a.block_len);
+  if (head_dim == 128) hipLaunchKernelGGL(block_dkdv_reduce_kernel<128>, grid, block, 0, st, a, keys_pad);
+  else hipLaunchKernelGGL(block_dkdv_reduce_kernel<64>, grid, block, 0, st, a, keys_pad);
+  return hipGetLastError();
+}
+
+hipError_t opt_in_block_bwd_kernels() {
+  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<128>), attr, (int)block_dq_lds_bytes<128>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<64>), attr, (int)block_dq_lds_bytes<64>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 4>), attr, (int)BlockDkdvLds<128, 4>::TOTAL);
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 2>), attr, (int)BlockDkdvLds<128, 2>::TOTAL);
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<64, 4>), attr, (int)BlockDkdvLds<64, 4>::TOTAL);
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<64, 2>), attr, (int)BlockDkdvLds<64, 2>::TOTAL);
+  return e;
+}
+
+}  // namespace slimpipe

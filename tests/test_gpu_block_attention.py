@@ -192,3 +192,130 @@ def test_ranges_merge_to_the_whole(sp):
     r = bu.Reference(ref["q"], ref["k"], ref["v"], bu.visible(idx.cpu().numpy(), off, 0, N, L, True, N), 1 / math.sqrt(D))
     bu.check("out", host_f64(out), r.out, r.out_tol)
     bu.check("lse", host_f64(lse), r.lse, r.lse_tol)
+
+
+@pytest.mark.parametrize("wild", [False, True])
+@pytest.mark.parametrize("case", SHAPES)
+def test_backward(sp, case, wild):
+    import torch
+    B, s, off, Hq, Hkv, D, L, top_k, causal, rng_ = case
+    N = off + s
+    begin, end = rng_ or (0, N)
+    say("block backward %r wild=%s" % (case, wild))
+    dev, ref = tensors(B, s, N, Hq, Hkv, D, salt=top_k + 100)
+    index = random_index(np.random.default_rng(s + D), B, Hq, s, top_k, -(-N // L), wild)
+    idx = torch.from_numpy(index).cuda()
+    r = bu.Reference(ref["q"], ref["k"], ref["v"], bu.visible(index, off, begin, end, L, causal, N), 1 / math.sqrt(D))
+    out, lse = sp.slimpipe_attn_block_fwd(dev["q"], dev["k"], dev["v"], idx, off, begin, end, L, causal)
+    dk, dv = torch.full((2,) + dev["k"].shape, 3.0, device="cuda")
+    dq = sp.slimpipe_attn_block_bwd(dev["q"], dev["k"], dev["v"], idx, out, dev["do"], lse, off, begin, end, L, dk, dv, causal, dkv_accumulate=wild)
+    torch.cuda.synchronize()
+    want = r.backward(host_f64(out), ref["do"], host_f64(lse), True)
+    bu.check("dq", host_f64(dq), *want[0])
+    for name, x, (w, tol) in (("dk", dk, want[1]), ("dv", dv, want[2])):
+        got = host_f64(x)
+        assert (got[:, :begin] == 3.0).all() and (got[:, end:] == 3.0).all(), name      # rows outside the range stay
+        if wild:                                                                       # added to what was there: one float32 rounding more
+            got, tol = got - 3.0, tol + 2.0 ** -23 * (3.0 + np.abs(w))
+        bu.check(name, got[:, begin:end], w[:, begin:end], tol[:, begin:end])
+
+
+def test_backward_long_lists_layouts_and_repeats(sp):
+    """Lists longer than one workgroup's part, from chunk lists, dq in float32 added to what is there; the same bits again, and with NaN in
+    the keys that no row sees."""
+    import torch
+    B, s, off, Hq, Hkv, D, L, top_k = 1, 1500, 548, 6, 1, 64, 128, 3
+    N = off + s
+    dev, ref = tensors(B, s, N, Hq, Hkv, D, salt=8)
+    index = random_index(np.random.default_rng(3), B, Hq, s, top_k, 10, False)
+    index[..., 0] = 2                                       # 9000 rows on one block
+    idx = torch.from_numpy(index).cuda()
+    see = bu.visible(index, off, 0, N, L, True, N)
+    r = bu.Reference(ref["q"], ref["k"], ref["v"], see, 1 / math.sqrt(D))
+    out, lse = sp.slimpipe_attn_block_fwd(dev["q"], dev["k"], dev["v"], idx, off, 0, N, L)
+    want = r.backward(host_f64(out), ref["do"], host_f64(lse), False)
+    nan = torch.tensor(float("nan"), device="cuda", dtype=torch.bfloat16)
+    mask = torch.from_numpy(np.ascontiguousarray(see.any((1, 2)))).cuda()[:, :, None, None]
+    first = None
+    for k, v in ((dev["k"], dev["v"]), (dev["k"], dev["v"]), (torch.where(mask, dev["k"], nan), torch.where(mask, dev["v"], nan))):
+        kc, vc = ([x[:, i:i + 1024].contiguous() for i in (0, 1024)] for x in (k, v))
+        dkc, dvc = ([torch.full(x.shape, 9.0, device="cuda") for x in kc] for _ in range(2))
+        dq = torch.ones((B, s, Hq, D), device="cuda")
+        sp.slimpipe_attn_block_bwd(dev["q"], kc, vc, idx, out, dev["do"], lse, off, 0, N, L, dkc, dvc, dq=dq, dq_dtype=sp.F32, dq_accumulate=True,
+                                   dkv_accumulate=False)
+        got = dq, torch.cat(dkc, 1), torch.cat(dvc, 1)
+        if first is None:
+            first = got
+            bu.check("dq", host_f64(dq) - 1.0, want[0][0], want[0][1] + 2.0 ** -23 * (1.0 + np.abs(want[0][0])))
+            bu.check("dk", host_f64(got[1]), *want[1])
+            bu.check("dv", host_f64(got[2]), *want[2])
+        assert all(torch.equal(x, y) for x, y in zip(first, got))
+
+
+def test_gradients_against_differences(sp):
+    """dq, dk, dv against central differences of the 64-bit forward along random directions, as far as the call's roundings allow."""
+    import torch
+    B, s, off, Hq, Hkv, D, L, top_k = 1, 48, 160, 4, 2, 64, 64, 2
+    N = off + s
+    dev, ref = tensors(B, s, N, Hq, Hkv, D, salt=21)
+    index = random_index(np.random.default_rng(5), B, Hq, s, top_k, -(-N // L), False)
+    idx = torch.from_numpy(index).cuda()
+    see = bu.visible(index, off, 0, N, L, True, N)
+    scale = 1 / math.sqrt(D)
+    out, lse = sp.slimpipe_attn_block_fwd(dev["q"], dev["k"], dev["v"], idx, off, 0, N, L)
+    dk, dv = torch.zeros((2,) + dev["k"].shape, device="cuda")
+    dq = sp.slimpipe_attn_block_bwd(dev["q"], dev["k"], dev["v"], idx, out, dev["do"], lse, off, 0, N, L, dk, dv, dq_dtype=sp.F32)
+    r = bu.Reference(ref["q"], ref["k"], ref["v"], see, scale)
+    rng, eps = np.random.default_rng(6), 1e-5
+    want = r.backward(host_f64(out), ref["do"], host_f64(lse), False)
+    exact = r.backward(r.out, ref["do"], r.lse, False)
+    for i, (name, got) in enumerate((("q", dq), ("k", dk), ("v", dv))):
+        step = rng.standard_normal(ref[name].shape)
+        f = [(bu.Reference(*(ref[t] + (sign * eps * step if t == name else 0.0) for t in "qkv"), see, scale).out * ref["do"]).sum() for sign in (1, -1)]
+        slope = (f[0] - f[1]) / (2 * eps)
+        assert abs((exact[i][0] * step).sum() - slope) <= 1e-6 * (np.abs(exact[i][0] * step).sum() + 1.0), name      # the formula's own gradient
+        # the call's: its tolerance, and what the roundings of the saved out and lse change
+        allowed = ((want[i][1] + np.abs(want[i][0] - exact[i][0])) * np.abs(step)).sum()
+        assert abs((host_f64(got) * step).sum() - slope) <= allowed + 1e-6 * np.abs(exact[i][0] * step).sum(), name
+
+
+def test_streams_and_graph(sp):
+    """A forward and a backward on another stream, and both captured into a graph that is replayed with other inputs."""
+    import torch
+    B, s, off, Hq, Hkv, D, L, top_k = 1, 300, 468, 4, 2, 64, 64, 4
+    N = off + s
+    sets = [tensors(B, s, N, Hq, Hkv, D, salt=40 + i)[0] for i in range(3)]
+    idxs = [torch.from_numpy(random_index(np.random.default_rng(i), B, Hq, s, top_k, -(-N // L), False)).cuda() for i in range(3)]
+
+    def step(t, idx, ws):
+        means = sp.slimpipe_attn_block_means(t["k"], 0, N, L)
+        chosen = sp.slimpipe_attn_block_select(t["q"], means, off, 0, N, L, top_k)
+        o, l = sp.slimpipe_attn_block_fwd(t["q"], t["k"], t["v"], chosen, off, 0, N, L, workspace=ws[0])
+        o, l = sp.slimpipe_attn_block_fwd(t["q"], t["k"], t["v"], idx, off, 0, N, L, workspace=ws[0])
+        dk, dv = torch.zeros((2,) + t["k"].shape, device="cuda")
+        dq = sp.slimpipe_attn_block_bwd(t["q"], t["k"], t["v"], idx, o, t["do"], l, off, 0, N, L, dk, dv, workspace=ws[1])
+        return chosen, o, l, dq, dk, dv
+    ws = [torch.empty(sp.slimpipe_attn_block_workspace_bytes(sets[0]["q"], sets[0]["k"], idxs[0], off, 0, N, L, True, bwd), device="cuda", dtype=torch.uint8)
+          for bwd in (False, True)]
+    eager = [step(t, i, ws) for t, i in zip(sets, idxs)]
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        again = step(sets[1], idxs[1], ws)
+    other.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(again, eager[1]))
+    buf, ibuf = {k: v.clone() for k, v in sets[0].items()}, idxs[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    sp.slimpipe_attn_init()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = step(buf, ibuf, ws)
+    for i in (1, 2, 0, 2):
+        for k in buf:
+            buf[k].copy_(sets[i][k])
+        ibuf.copy_(idxs[i])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, eager[i])), i
+        step(sets[0], idxs[0], ws)
+        torch.cuda.synchronize()
