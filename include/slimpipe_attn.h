@@ -276,6 +276,31 @@ int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, 
                             void* dq, int32_t dq_dtype, int32_t dq_accumulate, float* const* dk_chunks, float* const* dv_chunks, int32_t dkv_accumulate,
                             void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* A key/value cache held in 4 bits, for long prefixes that are only read (answering from a prompt, evaluation): 4.25 bits an element
+ * instead of 16.  32 consecutive elements of a head share a scale 2^e, stored as the byte e + 127; e is the smallest integer, at least
+ * -125, with max |x| < 7 * 2^e.  An element is the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7, ties to the even code) times 2^e, a sign
+ * bit above the code; two to a byte, the first in the low half.  A group with an infinity or a NaN has scale byte 255 and reads as NaN.
+ *   codes, scales : [batch, kv_capacity, n_kv_heads, head_dim / 2] and [.., head_dim / 32] bytes, for keys and for values, at the kv
+ *              strides of p, which count ELEMENTS: byte strides are half and a 32nd of them.  They are multiples of 32
+ *              (SLIMPIPE_EINVAL_STRIDE otherwise), codes 16-byte aligned.
+ *   limits   : kv_capacity <= 2^36, batch * n_kv_heads <= 65535, 2^30 query rows per kv head, 2^34 rows of all heads a store or load. */
+
+/* Stores the rows of a slice at positions q_offset .. q_offset + s_q - 1.  k_slice, v_slice: bf16 [batch, s_q, n_kv_heads, head_dim] with the q
+ * strides.  Other rows of the cache are untouched.  (n_q_heads, causal, scale and the key range are only validated.) */
+int slimpipe_attn_kv4_store(const slimpipe_attn_params* p, const void* k_slice, const void* v_slice, void* k_codes, void* k_scales, void* v_codes,
+                            void* v_scales, void* hip_stream);
+/* Rows [kv_begin, kv_end) as the bf16 numbers they stand for (exactly): k_rows, v_rows [batch, kv_end - kv_begin, n_kv_heads, head_dim] with the
+ * o strides. */
+int slimpipe_attn_kv4_load(const slimpipe_attn_params* p, const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales, void* k_rows,
+                           void* v_rows, void* hip_stream);
+/* slimpipe_attn_fwd over such a cache, from one token to a slice: the same visibility, out, lse and rows without a key, and (out, lse) of key
+ * ranges fold with those of bf16 calls (an old prefix in 4 bits, the newest slices in bf16).  workspace: slimpipe_attn_kv4_workspace_bytes
+ * (0 for calls that fill the GPU by themselves: may be NULL then), for the float32 partial results of the key ranges that a call of few rows is
+ * cut into.  Results do not depend on the order in which workgroups run. */
+int slimpipe_attn_kv4_workspace_bytes(const slimpipe_attn_params* p, size_t* bytes);
+int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, const void* k_codes, const void* k_scales, const void* v_codes,
+                          const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* slimpipe_attn_strerror(int code);
 
 #ifdef __cplusplus

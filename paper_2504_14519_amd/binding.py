@@ -4,6 +4,7 @@ Same entry-point names as the C header.  Tensors are torch tensors on the GPU; t
 device memory and the current stream, every step of the computation runs in the library's kernels.
 There is no fallback: if the shared library is missing the import fails.
 """
+import collections
 import ctypes
 import math
 import os
@@ -104,6 +105,14 @@ def _load():
     L.slimpipe_attn_block_fwd.restype = ctypes.c_int
     L.slimpipe_attn_block_bwd.argtypes = [P, vp, pp, pp, i32, i64, i32, i32, vp, vp, vp, vp, vp, i32, i32, pp, pp, i32, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_block_bwd.restype = ctypes.c_int
+    L.slimpipe_attn_kv4_store.argtypes = [P, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv4_store.restype = ctypes.c_int
+    L.slimpipe_attn_kv4_load.argtypes = [P, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv4_load.restype = ctypes.c_int
+    L.slimpipe_attn_kv4_workspace_bytes.argtypes = [P, szp]
+    L.slimpipe_attn_kv4_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_fwd_kv4.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_fwd_kv4.restype = ctypes.c_int
     L.slimpipe_attn_mfma_rate.argtypes = [ctypes.c_int, vp, ctypes.POINTER(ctypes.c_double), vp]
     L.slimpipe_attn_mfma_rate.restype = ctypes.c_int
     L.slimpipe_attn_dq_atomic_probe.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -469,6 +478,94 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
                                        dq.data_ptr(), dq_dtype, 1 if dq_accumulate else 0, _chunk_table(dk_chunks), _chunk_table(dv_chunks),
                                        1 if dkv_accumulate else 0, *_ws(workspace), _stream()), "slimpipe_attn_block_bwd")
     return dq
+
+
+class KvCache4(collections.namedtuple("KvCache4", "k_codes k_scales v_codes v_scales")):
+    """A key/value cache held in 4 bits: uint8 tensors [B, capacity, Hkv, D / 2] (codes) and [B, capacity, Hkv, D / 32] (scales)."""
+    __slots__ = ()
+
+    @classmethod
+    def empty(cls, batch, capacity, kv_heads, head_dim, device="cuda"):
+        def new(n):
+            return torch.zeros((batch, capacity, kv_heads, n), device=device, dtype=torch.uint8)
+        return cls(new(head_dim // 2), new(head_dim // 32), new(head_dim // 2), new(head_dim // 32))
+
+    def layout(self):
+        """(batch, capacity, kv heads, head_dim) and the three strides in elements, after a check that the four tensors agree."""
+        kc, ks, vc, vs = self
+        B, N, H, half = kc.shape
+        ok = all(x.dtype == torch.uint8 and x.dim() == 4 and x.stride(3) == 1 for x in self)
+        ok = ok and vc.shape == kc.shape and ks.shape == vs.shape == torch.Size((B, N, H, half // 16))
+        # (a dimension of one element may have any stride)
+        ok = ok and all(n == 1 or kc.stride(i) == vc.stride(i) == 16 * ks.stride(i) == 16 * vs.stride(i) for i, n in ((0, B), (1, N), (2, H)))
+        if not ok:
+            raise SlimpipeError("codes and scales must be uint8 [batch, keys, heads, head_dim / 2] and [.., head_dim / 32] of the same layout")
+        D = 2 * half
+        full = N * H * D, H * D, D
+        return (B, N, H, D), tuple(2 * kc.stride(i) if n > 1 else full[i] for i, n in ((0, B), (1, N), (2, H)))
+
+
+def _cache_ptrs(cache):
+    return cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr()
+
+
+def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
+    """Store bf16 rows k_slice, v_slice [B, s, Hkv, D] in a KvCache4 from `position` on."""
+    (B, N, H, D), skv = cache.layout()
+    if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or not _same_strides(k_slice, v_slice):
+        raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
+    sx = k_slice.stride()[:3]
+    p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
+    _check(lib.slimpipe_attn_kv4_store(ctypes.byref(p), k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()), "slimpipe_attn_kv4_store")
+
+
+def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
+    """-> (k, v) bf16 [B, kv_end - kv_begin, Hkv, D]: the numbers that the rows of a KvCache4 stand for."""
+    (B, N, H, D), skv = cache.layout()
+    shape = (B, kv_end - kv_begin, H, D)
+    if k_rows is None:
+        k_rows = torch.empty(shape, device=cache.k_codes.device, dtype=torch.bfloat16)
+    if v_rows is None:
+        v_rows = torch.empty_like(k_rows)
+    if tuple(k_rows.shape) != shape or not _same_strides(k_rows, v_rows):
+        raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
+    sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
+    p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
+    _check(lib.slimpipe_attn_kv4_load(ctypes.byref(p), *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
+           if shape[1] > 0 else lib.slimpipe_attn_validate(ctypes.byref(p), 0), "slimpipe_attn_kv4_load")
+    return k_rows, v_rows
+
+
+def _kv4_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
+    (B, N, H, D), skv = cache.layout()
+    if q_slice.shape[0] != B or q_slice.shape[3] != D:
+        raise SlimpipeError("q_slice and the cache must have the same batch and head_dim")
+    sq, so = q_slice.stride(), out_like.stride()
+    return AttnParams(B, q_slice.shape[1], q_slice.shape[2], H, D, 1 if causal else 0, N, q_offset, kv_begin, kv_end,
+                      float(scale) if scale is not None else 1.0 / math.sqrt(D), out_dtype, *sq[:3], *skv, *so[:3], *so[:3])
+
+
+def _kv4_ws(p):
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_kv4_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "kv4_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
+    """Bytes of workspace that slimpipe_attn_fwd_kv4 of these tensors needs (may be 0)."""
+    return _kv4_ws(_kv4_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16))
+
+
+def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
+    """-> (out, lse): slimpipe_attn_fwd over a KvCache4.  workspace: uint8 tensor, allocated where None."""
+    if out is None or lse is None:
+        out, lse = _outputs(q_slice, out_dtype, out, lse)
+    p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    if workspace is None:
+        workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
+    _check(lib.slimpipe_attn_fwd_kv4(ctypes.byref(p), q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(), *_ws(workspace),
+                                     _stream()), "slimpipe_attn_fwd_kv4")
+    return out, lse
 
 
 KERNEL_KINDS = ("fwd", "delta", "dq", "dkdv", "merge", "finalize", "dkdv_reduce", "dq_reduce",

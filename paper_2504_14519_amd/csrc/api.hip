@@ -11,6 +11,7 @@
 #include "blocks.hpp"
 #include "host_common.hpp"
 #include "kernels.hpp"
+#include "kv4.hpp"
 
 using namespace slimpipe;
 
@@ -56,6 +57,7 @@ int slimpipe::ensure_device_ready(void** scratch_ptr) {
     if (d.status == hipSuccess) d.status = opt_in_block_select_kernels();
     if (d.status == hipSuccess) d.status = opt_in_block_fwd_kernels();
     if (d.status == hipSuccess) d.status = opt_in_block_bwd_kernels();
+    if (d.status == hipSuccess) d.status = opt_in_kv4_kernels();
     if (d.status == hipSuccess) d.status = hipGetSymbolAddress(&d.scratch, HIP_SYMBOL(scratch));
     if (d.status == hipSuccess && d.scratch == nullptr) d.status = hipErrorInvalidSymbol;
   });

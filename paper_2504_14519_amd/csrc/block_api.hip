@@ -4,6 +4,7 @@
 
 #include "blocks.hpp"
 #include "host_common.hpp"
+#include "kv4.hpp"
 
 using namespace slimpipe;
 
@@ -227,7 +228,12 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   } else if (launch_block_lists(a, false, st) != hipSuccess || launch_block_fwd(a, p->head_dim, st) != hipSuccess) {
     return SLIMPIPE_ELAUNCH;
   }
-  return status(launch_block_merge(a, p->head_dim, st));
+  PartMergeArgs m;
+  m.part_out = a.part_out; m.part_lse = a.part_lse; m.parts = top_k; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
+  m.rows = rows_of(p);
+  m.out = out; m.lse = lse;
+  m.o_stride_b = p->o_stride_b; m.o_stride_s = p->o_stride_s; m.o_stride_h = p->o_stride_h;
+  return status(launch_part_merge(m, p->head_dim, st));
 }
 
 int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,

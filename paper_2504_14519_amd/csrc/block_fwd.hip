@@ -1,7 +1,7 @@
 // Forward of sparse attention over selected key blocks.
 //
 // A tile is up to 128 rows that chose one block (block_select.hip): four waves of 32 rows each, the block's keys in tiles of 64 through
-// two LDS slots.  Every (row, slot) leaves out and lse of its block's keys in 32 bits; the merge kernel folds a row's slots.
+// two LDS slots.  Every (row, slot) leaves out and lse of its block's keys in 32 bits; part_merge.hip folds a row's slots.
 #include "block_tile.hpp"
 #include "row_tile.hpp"
 #include "tile_common.hpp"
@@ -192,45 +192,6 @@ __global__ __launch_bounds__(256) void block_fwd_few_kernel(const BlockArgs a) {
   }
 }
 
-// lse = ln sum_s exp(lse_s), out = sum_s exp(lse_s - lse) out_s over the slots of a row, in slot order; D / 8 lanes a row.
-template <int D>
-__global__ __launch_bounds__(256) void block_merge_kernel(const BlockArgs a) {
-  constexpr int NC = D / 8;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
-  const int c = (int)(gid - row * NC);
-  if (row >= (int64_t)a.batch * a.n_q_heads * a.s_q) return;
-  const float* lp = a.part_lse + row * a.top_k;
-  const float* op = a.part_out + row * a.top_k * D + c * 8;
-  float m = -INFINITY;
-  for (int s = 0; s < a.top_k; ++s) m = fmaxf(m, lp[s]);
-  f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
-  float sum = 0.f;
-  if (m != -INFINITY)
-#pragma unroll 4
-    for (int s = 0; s < a.top_k; ++s) {
-      const float ls = lp[s];
-      if (ls == -INFINITY) continue;                 // (its partial out was not written)
-      const float w = exp2_fast((ls - m) * kLog2e);
-      sum += w;
-      x0 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D);
-      x1 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D + 4);
-    }
-  const float inv = sum > 0.f ? 1.0f / sum : 0.f;
-  const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
-  const int64_t to = b * a.o_stride_b + (row - bh * a.s_q) * a.o_stride_s + (bh - b * a.n_q_heads) * a.o_stride_h + c * 8;
-  x0 *= inv;
-  x1 *= inv;
-  if (a.out_f32) {
-    f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
-    dst[0] = x0;
-    dst[1] = x1;
-  } else {
-    const bf16x4 lo = __builtin_convertvector(x0, bf16x4), hi = __builtin_convertvector(x1, bf16x4);
-    *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-  }
-  if (c == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(sum) * kLn2;
-}
-
 hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st) {
   dim3 grid((unsigned)((a.item_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(256);
   if (head_dim == 128) hipLaunchKernelGGL(block_fwd_kernel<128>, grid, block, block_fwd_lds_bytes<128>(), st, a);
@@ -243,14 +204,6 @@ hipError_t launch_block_fwd_few(const BlockArgs& a, int head_dim, hipStream_t st
   else hipLaunchKernelGGL(block_fwd_few_kernel<64>, grid, block, 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_block_merge(const BlockArgs& a, int head_dim, hipStream_t st) {
-  const int64_t lanes = (int64_t)a.batch * a.n_q_heads * a.s_q * (head_dim / 8);
-  dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
-  if (head_dim == 128) hipLaunchKernelGGL(block_merge_kernel<128>, grid, block, 0, st, a);
-  else hipLaunchKernelGGL(block_merge_kernel<64>, grid, block, 0, st, a);
-  return hipGetLastError();
-}
-
 hipError_t opt_in_block_fwd_kernels() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_fwd_kernel<128>), attr, (int)block_fwd_lds_bytes<128>());

@@ -100,7 +100,6 @@ hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream
 hipError_t launch_block_lists(const BlockArgs& a, bool dkdv, hipStream_t st);
 hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_fwd_few(const BlockArgs& a, int head_dim, hipStream_t st);
-hipError_t launch_block_merge(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st);

@@ -1,0 +1,397 @@
+// A key/value cache held in 4 bits: rows stored and read back, and attention of a query slice or of single tokens over it.
+//
+// 32 consecutive elements of a head share a scale 2^e; an element is a 4-bit float (sign, 2 exponent bits, 1 mantissa bit: 0, 0.5, 1, 1.5,
+// 2, 3, 4, 6).  gfx950 converts such numbers with their scale in one instruction, two at a time, exactly, to bf16, so that the attention
+// below is the bf16 one on converted tiles: 4.25 bits an element are read instead of 16.
+#include "kv4.hpp"
+#include "row_tile.hpp"
+
+namespace slimpipe {
+
+// Scale byte as the float whose exponent the conversions use (255, a group with an infinity or a NaN: NaN).
+SP_DEV float kv4_scale(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23); }
+
+// 8 elements (4 bytes of codes) -> bf16
+SP_DEV bf16x8 kv4_values(uint32_t codes, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  bf16x8 r;
+  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1]; r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
+  return r;
+}
+
+// ------------------------------------------------------------------------------------ store, load
+// Four lanes a group, 16 bytes of bf16 and 4 bytes of codes each: bound by the bytes.  blockIdx.y: keys or values.
+template <int D, bool LOAD>
+__global__ __launch_bounds__(256) void kv4_copy_kernel(const Kv4CopyArgs a) {
+  constexpr int NC = D / 8;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, rh = gid / NC;      // (batch index, row, head) flattened
+  const int c = (int)(gid - rh * NC);
+  const bool keys = blockIdx.y == 0;
+  if (rh >= a.batch * a.rows * a.n_kv_heads) return;             // (whole rows: the lanes of a group leave together)
+  const int64_t br = rh / a.n_kv_heads, h = rh - br * a.n_kv_heads, b = br / a.rows, r = br - b * a.rows;
+  const int64_t x = b * a.x_stride_b + r * a.x_stride_s + h * a.x_stride_h + c * 8;
+  const int64_t y = b * a.kv_stride_b + (a.position + r) * a.kv_stride_s + h * a.kv_stride_h + c * 8;
+  const Kv4Operand to = keys ? a.k : a.v;
+  uint32_t* const codes = reinterpret_cast<uint32_t*>(to.codes + y / 2);
+  uint8_t* const scale = to.scales + y / 32;
+  if constexpr (LOAD) {
+    const uint32_t s = *scale;
+    bf16x8 v = kv4_values(*codes, kv4_scale(s));
+    if (s == 255u) {
+      typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+      v = __builtin_bit_cast(bf16x8, (u16x8)(0x7fc0));
+    }
+    *reinterpret_cast<bf16x8*>((keys ? a.k_dst : a.v_dst) + x) = v;
+  } else {
+    const u32x4 w = *reinterpret_cast<const u32x4*>((keys ? a.k_src : a.v_src) + x);
+    uint32_t most = 0;                                            // largest magnitude, as bf16 bits
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
+      most = most > lo ? most : lo;
+      most = most > hi ? most : hi;
+    }
+#pragma unroll
+    for (int k = 1; k < 4; k <<= 1) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)most, k, 64);
+      most = most > o ? most : o;
+    }
+    // largest = 1.m 2^(E - 127): 2^e with e = E - 127 - 2, one more where 1.m >= 1.75, and at least -125
+    const bool finite = most < 0x7f80u;
+    int byte = (int)(most >> 7) - 2 + ((most & 0x7fu) >= 0x60u ? 1 : 0);
+    byte = byte < 2 ? 2 : byte;
+    const float s = __uint_as_float((uint32_t)byte << 23);
+    const bf16x8 x8 = __builtin_bit_cast(bf16x8, w);
+    uint32_t packed = 0;
+    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, __builtin_shufflevector(x8, x8, 0, 1), s, 0);
+    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, __builtin_shufflevector(x8, x8, 2, 3), s, 1);
+    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, __builtin_shufflevector(x8, x8, 4, 5), s, 2);
+    packed = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(packed, __builtin_shufflevector(x8, x8, 6, 7), s, 3);
+    *codes = finite ? packed : 0u;
+    if (c % 4 == 0) *scale = (uint8_t)(finite ? byte : 255);
+  }
+}
+
+template <bool LOAD>
+static hipError_t launch_copy(const Kv4CopyArgs& a, int head_dim, hipStream_t st) {
+  const int64_t lanes = a.batch * a.rows * a.n_kv_heads * (head_dim / 8);
+  dim3 grid((unsigned)((lanes + 255) / 256), 2), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL((kv4_copy_kernel<128, LOAD>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((kv4_copy_kernel<64, LOAD>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_kv4_store(const Kv4CopyArgs& a, int head_dim, hipStream_t st) { return launch_copy<false>(a, head_dim, st); }
+hipError_t launch_kv4_load(const Kv4CopyArgs& a, int head_dim, hipStream_t st) { return launch_copy<true>(a, head_dim, st); }
+
+// ------------------------------------------------------------------------------------ attention
+// Rows of a plane (batch index, kv head) are numbered head of the group major: row rh is row rh % s_q of head rh / s_q.
+struct Kv4Row { int r, h; };
+SP_DEV Kv4Row kv4_row(const Kv4Args& a, int hk, int rh) {
+  const int hl = rh / a.s_q;
+  return {rh - hl * a.s_q, hk * a.group + hl};
+}
+
+template <int D>
+constexpr size_t kv4_fwd_lds_bytes() {         // two slots of converted K and V tiles; then the output rows
+  constexpr size_t rings = (size_t)4 * 64 * D * 2, rows = (size_t)4 * 32 * kOutRow<D> * 4;
+  return rings > rows ? rings : rows;
+}
+
+// Slices: 128 rows a workgroup, 32 a wave (row_tile.hpp).  Codes of a tile of 64 keys are fetched one tile ahead into registers and
+// converted into LDS, a group of 32 elements a thread, for all four waves at once.
+template <int D>
+__global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
+  constexpr int BN = 64, TILE = BN * D * 2, NG = D / 32, GROUPS = 2 * BN * NG, PER = GROUPS / 256;      // groups of K and V; a thread's
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = a.group * a.s_q, blocks = (rows + 127) / 128;
+  const int part_i = blockIdx.x / blocks, blk = blocks - 1 - (blockIdx.x - part_i * blocks);
+  const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int rh = blk * 128 + wave_u * 32 + (lane & 31);
+  const Kv4Row my = kv4_row(a, hk, rh < rows ? rh : rows - 1);
+  const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
+  int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
+  // last row of the block: of its head, or of the head before where the block holds the end of one
+  if (a.causal) {
+    const int r0 = blk * 128, r1 = r0 + 127 < rows ? r0 + 127 : rows - 1;
+    const int64_t last = r0 / a.s_q == r1 / a.s_q ? r1 % a.s_q : a.s_q - 1;
+    if (a.q_offset + last + 1 < hi) hi = a.q_offset + last + 1;
+  }
+  const int n_keys = hi > lo ? (int)(hi - lo) : 0, nt = (n_keys + BN - 1) / BN;
+  const int64_t see = a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1;
+  const int64_t see_far = see - lo;
+  const int see_rel = see_far < -1 ? -1 : (int)see_far;
+  const unsigned lds = lds_addr(smem);
+
+  // this thread's groups: group i of the tile is key i / NG (of K, then of V), group i % NG of its row
+  const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s;
+  u32x4 codes[PER];
+  uint32_t scales[PER];
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      const int i = n * 256 + tid, kv = i / (BN * NG), key = i / NG % BN, grp = i % NG;
+      const int k = t * BN + key < n_keys ? t * BN + key : n_keys - 1;      // (keys behind the last are not read)
+      const int64_t at = base + (int64_t)k * a.kv_stride_s + grp * 32;
+      const Kv4Operand& op = kv ? a.v : a.k;
+      codes[n] = *reinterpret_cast<const u32x4*>(op.codes + at / 2);
+      scales[n] = op.scales[at / 32];
+    }
+  };
+  auto convert = [&](int t) {
+#pragma unroll
+    for (int n = 0; n < PER; ++n) {
+      const int i = n * 256 + tid, kv = i / (BN * NG), key = i / NG % BN, grp = i % NG;
+      const float s = kv4_scale(scales[n]);
+      char* tile = smem + (t & 1) * 2 * TILE + kv * TILE;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<bf16x8*>(tile + tile_off<D>(key, 4 * grp + j)) = kv4_values(codes[n][j], s);
+    }
+  };
+
+  RowState<D> st;
+  st.init();
+  if (nt > 0) {
+    fetch(0);
+    {
+      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) st.q[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
+    }
+    RpOffsets<D> lo_k;
+    TrOffsets<D> lo_v;
+    lo_k.init(lane, (int)lds);
+    lo_v.init(lane, (int)lds + TILE);
+    convert(0);
+    if (nt > 1) fetch(1);
+    __syncthreads();
+    for (int t = 0; t < nt; ++t) {
+      const int kmax = see_rel - t * BN;
+      const bool masked = __builtin_amdgcn_ballot_w64(kmax < BN - 1) != 0;
+      attend_tile<D, BN>(st, lo_k, lo_v, a.scale_log2e, masked, 0, kmax, g);
+      const int step = (t & 1) ? -2 * TILE : 2 * TILE;
+      lo_k.add(step);
+      lo_v.add(step);
+      if (t + 1 < nt) convert(t + 1);
+      if (t + 2 < nt) fetch(t + 2);
+      __syncthreads();
+    }
+  }
+  float lse;
+  const float norm = st.finish(&lse);
+  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
+  put_rows<D>(part, st.o, norm, lane);
+  const int64_t row = ((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r;
+  const int n_mine = rows - (blk * 128 + wave_u * 32);
+  if (a.n_parts > 1) {
+    const int64_t slot = row * a.n_parts + part_i;
+    if (lane < 32 && lane < n_mine) a.part_lse[slot] = lse;
+    constexpr int PERR = D / 4, RPP = 64 / PERR;
+#pragma unroll
+    for (int j = 0; j < 32 / RPP; ++j) {
+      const int r = j * RPP + lane / PERR;
+      const int64_t to = __shfl(slot, r, 64);
+      if (r < n_mine) *reinterpret_cast<f32x4*>(a.part_out + to * D + lane % PERR * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PERR * 4);
+    }
+    return;
+  }
+  if (lane < 32 && lane < n_mine) a.lse[row] = lse;
+  const int64_t at = (int64_t)b * a.o_stride_b + (int64_t)my.r * a.o_stride_s + (int64_t)my.h * a.o_stride_h;
+  constexpr int PERR = D / 8, RPP = 64 / PERR;
+#pragma unroll
+  for (int j = 0; j < 32 / RPP; ++j) {
+    const int r = j * RPP + lane / PERR, d = lane % PERR * 8;
+    const int64_t to = __shfl(at, r, 64) + d;
+    const f32x4 x0 = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d), x1 = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d + 4);
+    if (r >= n_mine) continue;
+    if (a.out_f32) {
+      f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
+      dst[0] = x0;
+      dst[1] = x1;
+    } else {
+      const bf16x4 y0 = __builtin_convertvector(x0, bf16x4), y1 = __builtin_convertvector(x1, bf16x4);
+      *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+}
+
+// Tokens: at most 32 rows of a plane (its query heads and a few tokens), all in every wave; the four waves of a workgroup share out the
+// 32-key tiles of its keys.  K goes from memory to the matrix unit without LDS: a lane's operand is 8 elements of its key in each step, and
+// since the contraction may take head_dim in any order, half-wave g takes elements D/2 g .. in order: 16 codes bytes after 16.  V
+// passes through 32 rows of LDS of the wave's own for the transposed read.
+template <int D>
+constexpr size_t kv4_few_lds_bytes(int rows) {
+  const size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * rows * kOutRow<D> * 4 + 4 * 2 * 32 * 4;
+  return tiles > out ? tiles : out;
+}
+template <int D>
+__global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
+  constexpr int KS = D / 16, DB = D / 32, W = D / 64, HALF = D / 2;      // W: 16-byte words of codes of half a row
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = a.group * a.s_q;
+  const int part_i = blockIdx.x, plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const Kv4Row my = kv4_row(a, hk, ql < rows ? ql : rows - 1);
+  const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
+  const int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
+  const int n_keys = hi > lo ? (int)(hi - lo) : 0, nt = (n_keys + 31) / 32;
+  const int64_t see = a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1;
+  const int64_t see_far = see - lo;
+  const int see_rel = see_far < -1 ? -1 : (int)see_far;
+  const unsigned tile = lds_addr(smem) + wave_u * 32 * D * 2;
+  char* const tile_p = smem + wave_u * 32 * D * 2;
+
+  RowState<D> st;
+  st.init();
+  {
+    const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + HALF * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) st.q[ks] = *reinterpret_cast<const bf16x8*>(qp + 8 * ks);
+  }
+  TrOffsets<D> lo_v;
+  lo_v.init(lane, (int)tile);
+  // K: lane = (key ql, half g).  V: the same half row, written to LDS.
+  const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s + HALF * g;
+  u32x4 kc[W], vc[W];
+  uint32_t ks_[W], vs_[W];                       // scale of each 32 elements
+  auto fetch = [&](int t) {
+    const int k = t * 32 + ql < n_keys ? t * 32 + ql : n_keys - 1;
+    const int64_t at = base + (int64_t)k * a.kv_stride_s;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      kc[w] = *reinterpret_cast<const u32x4*>(a.k.codes + at / 2 + 16 * w);
+      vc[w] = *reinterpret_cast<const u32x4*>(a.v.codes + at / 2 + 16 * w);
+      ks_[w] = a.k.scales[at / 32 + w];
+      vs_[w] = a.v.scales[at / 32 + w];
+    }
+  };
+  if (wave_u < nt) fetch(wave_u);
+  for (int t = wave_u; t < nt; t += 4) {
+    f32x16 s = {0};
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s = mfma32(kv4_values(kc[w][j], kv4_scale(ks_[w])), st.q[4 * w + j], s);
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<bf16x8*>(tile_p + tile_off<D>(ql, g * (D / 16) + 4 * w + j)) = kv4_values(vc[w][j], kv4_scale(vs_[w]));
+    if (t + 4 < nt) fetch(t + 4);
+    const int kmax = see_rel - t * 32;
+    if (__builtin_amdgcn_ballot_w64(kmax < 31) != 0) {
+      const int top = kmax - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) <= top ? s[i] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(s[i], mx);
+    mx = xhalf_max(mx);
+    const float m_new = fmaxf(st.m, mx * a.scale_log2e), m_eff = m_new == -INFINITY ? 0.f : m_new;
+    if (__builtin_amdgcn_ballot_w64(m_new != st.m) != 0) {
+      const float alpha = exp2_fast(st.m - m_eff);
+      st.l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st.o[db][i] *= alpha;
+    }
+    st.m = m_new;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = exp2_fast(__builtin_fmaf(s[i], a.scale_log2e, -m_eff));
+      sum += s[i];
+    }
+    st.l += sum;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bf16x8 p = pack8(s, 8 * half);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) st.o[db] = mfma32(lds_tr<D>(lo_v, db, half * 16 * D * 2), p, st.o[db]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  // the waves' results, unnormalised, and their (maximum, sum), folded in wave order
+  __syncthreads();
+  float* const acc = reinterpret_cast<float*>(smem);                         // [wave][rows][kOutRow]
+  float* const stat = acc + 4 * rows * kOutRow<D>;                           // [wave][2][32]
+  const float l_tot = xhalf_sum(st.l);
+  if (lane < 32) { stat[wave_u * 64 + ql] = st.m; stat[wave_u * 64 + 32 + ql] = l_tot; }
+  if (ql < rows)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 v = {st.o[db][4 * i4], st.o[db][4 * i4 + 1], st.o[db][4 * i4 + 2], st.o[db][4 * i4 + 3]};
+        *reinterpret_cast<f32x4*>(acc + (wave_u * rows + ql) * kOutRow<D> + 32 * db + 8 * i4 + 4 * g) = v;
+      }
+  __syncthreads();
+  constexpr int PER = D / 8;
+  for (int i = tid; i < rows * PER; i += 256) {
+    const int r = i / PER, d = i % PER * 8;
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, stat[w * 64 + r]);
+    f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
+    const float m_eff = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast(stat[w * 64 + r] - m_eff);
+      l += f * stat[w * 64 + 32 + r];
+      x0 += f * *reinterpret_cast<const f32x4*>(acc + (w * rows + r) * kOutRow<D> + d);
+      x1 += f * *reinterpret_cast<const f32x4*>(acc + (w * rows + r) * kOutRow<D> + d + 4);
+    }
+    const float norm = l > 0.f ? 1.0f / l : 0.f, lse = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+    x0 *= norm;
+    x1 *= norm;
+    const Kv4Row at = kv4_row(a, hk, r);
+    const int64_t row = ((int64_t)b * a.n_q_heads + at.h) * a.s_q + at.r;
+    if (a.n_parts > 1) {
+      f32x4* dst = reinterpret_cast<f32x4*>(a.part_out + (row * a.n_parts + part_i) * D + d);
+      dst[0] = x0;
+      dst[1] = x1;
+      if (d == 0) a.part_lse[row * a.n_parts + part_i] = lse;
+      continue;
+    }
+    const int64_t to = (int64_t)b * a.o_stride_b + (int64_t)at.r * a.o_stride_s + (int64_t)at.h * a.o_stride_h + d;
+    if (a.out_f32) {
+      f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
+      dst[0] = x0;
+      dst[1] = x1;
+    } else {
+      const bf16x4 y0 = __builtin_convertvector(x0, bf16x4), y1 = __builtin_convertvector(x1, bf16x4);
+      *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    if (d == 0) a.lse[row] = lse;
+  }
+}
+
+template <int D>
+static void launch_fwd_t(const Kv4Args& a, bool few, hipStream_t st) {
+  const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
+  const int rows = a.group * a.s_q;
+  if (few) hipLaunchKernelGGL(kv4_few_kernel<D>, dim3((unsigned)a.n_parts, planes), dim3(256), kv4_few_lds_bytes<D>(rows), st, a);
+  else hipLaunchKernelGGL(kv4_fwd_kernel<D>, dim3((unsigned)a.n_parts * (unsigned)((rows + 127) / 128), planes), dim3(256), kv4_fwd_lds_bytes<D>(), st, a);
+}
+hipError_t launch_kv4_fwd(const Kv4Args& a, int head_dim, bool few, hipStream_t st) {
+  if (head_dim == 128) launch_fwd_t<128>(a, few, st);
+  else launch_fwd_t<64>(a, few, st);
+  return hipGetLastError();
+}
+
+hipError_t opt_in_kv4_kernels() {
+  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<128>), attr, (int)kv4_fwd_lds_bytes<128>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<64>), attr, (int)kv4_fwd_lds_bytes<64>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128>), attr, (int)kv4_few_lds_bytes<128>(kKv4FewRows));
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<64>), attr, (int)kv4_few_lds_bytes<64>(kKv4FewRows));
+  return e;
+}
+
+}  // namespace slimpipe
