@@ -54,7 +54,7 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where the parts of the workspace lie, and its size.
 struct BlockWorkspace {
-  size_t part_out, part_lse, counts, start, entries, items, n_items, delta, lse2, dkdv_items, n_dkdv_items, sums, dkdv_part, bytes;
+  size_t part_out, part_lse, ranks, counts, lists, entries, items, n_items, delta, lse2, dkdv_items, n_dkdv_items, dkdv_part, bytes;
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
 // Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but 2048 at least, because every part of
@@ -77,8 +77,9 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     // every tile but a block's last is full
     const size_t tiles = plane_rows * top_k / kBlockTileRows + blocks, slots = plane_rows * top_k;
     w.item_cap = (int32_t)(tiles < 1 ? 1 : tiles < slots ? tiles : slots);
+    w.ranks = take(planes * slots * 2);
     w.counts = take(planes * w.n_list_chunks * blocks * 4);
-    w.start = take(planes * blocks * 4);
+    w.lists = take(planes * blocks * sizeof(BlockList));
     w.entries = take(planes * slots * sizeof(BlockEntry));
     w.items = take(planes * w.item_cap * sizeof(BlockItem));
     w.n_items = take(planes * 4);
@@ -96,7 +97,6 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.part_cap = (int32_t)(2 * slots / w.chunk_rows);
     w.dkdv_items = take(planes * w.dkdv_cap * sizeof(BlockItem));
     w.n_dkdv_items = take(planes * 4);
-    w.sums = take(planes * blocks * sizeof(BlockItem));
     w.dkdv_part = take(planes * w.part_cap * 2 * (size_t)(w.n_sub * keys) * p->head_dim * 4);
   }
   w.bytes = at;
@@ -120,8 +120,9 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->part_out = reinterpret_cast<float*>(ws + w.part_out);
   a->part_lse = reinterpret_cast<float*>(ws + w.part_lse);
   a->n_list_chunks = w.n_list_chunks;
+  a->ranks = reinterpret_cast<uint16_t*>(ws + w.ranks);
   a->counts = reinterpret_cast<uint32_t*>(ws + w.counts);
-  a->start = reinterpret_cast<uint32_t*>(ws + w.start);
+  a->lists = reinterpret_cast<BlockList*>(ws + w.lists);
   a->entries = reinterpret_cast<BlockEntry*>(ws + w.entries);
   a->items = reinterpret_cast<BlockItem*>(ws + w.items);
   a->n_items = reinterpret_cast<int32_t*>(ws + w.n_items);
@@ -131,7 +132,6 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->chunk_rows = w.chunk_rows; a->n_sub = w.n_sub; a->dkdv_cap = w.dkdv_cap; a->part_cap = w.part_cap;
   a->dkdv_items = reinterpret_cast<BlockItem*>(ws + w.dkdv_items);
   a->n_dkdv_items = reinterpret_cast<int32_t*>(ws + w.n_dkdv_items);
-  a->sums = reinterpret_cast<BlockItem*>(ws + w.sums);
   a->dkdv_part = reinterpret_cast<float*>(ws + w.dkdv_part);
 }
 
@@ -185,7 +185,8 @@ int slimpipe_attn_block_select(const slimpipe_attn_params* p, const void* q_slic
   a.blocks_total = blocks_of(0, p->kv_capacity, block_len);
   a.q_offset = p->q_offset;
   a.q_stride_b = p->q_stride_b; a.q_stride_s = p->q_stride_s; a.q_stride_h = p->q_stride_h;
-  return status(launch_block_select(a, p->head_dim, static_cast<hipStream_t>(hip_stream)));
+  if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
+  return status(launch_block_select(a, p->head_dim, compute_units(), static_cast<hipStream_t>(hip_stream)));
 }
 
 int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, int is_bwd, size_t* bytes) {

@@ -363,16 +363,19 @@ __global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs 
   if (kk >= n) return;
   const int64_t key = a.kv_begin + kk;
   const int64_t block = key / a.block_len, j = block - a.first_block;
-  BlockItem sums = {0, 0, 0, 0};
-  if (key < a.kv_end) sums = a.sums[(int64_t)plane * a.n_blocks + j];
-  const int len = sums.block, parts = sums.first;
+  uint32_t len = 0, part0 = 0;
+  int parts = 0;
+  if (key < a.kv_end) {
+    const BlockList& l = a.lists[(int64_t)plane * a.n_blocks + j];
+    len = l.len; parts = (int)l.parts; part0 = l.part0;
+  }
   if (len > 0 ? parts == 0 : a.dkv_accumulate != 0) return;
   const int chunk = kv_chunk_of(a.kv, key);
   const int64_t to = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + (key - (int64_t)chunk * a.kv.len) * a.kv_stride_s + c;
   f32x4* kd = reinterpret_cast<f32x4*>(a.dk_acc[chunk] + to);
   f32x4* vd = reinterpret_cast<f32x4*>(a.dv_acc[chunk] + to);
   f32x4 k4 = {0, 0, 0, 0}, v4 = {0, 0, 0, 0};
-  const float* src = a.dkdv_part + (((int64_t)plane * a.part_cap + sums.count) * 2 * keys_pad + (key - block * a.block_len)) * D + c;
+  const float* src = a.dkdv_part + (((int64_t)plane * a.part_cap + part0) * 2 * keys_pad + (key - block * a.block_len)) * D + c;
 #pragma unroll 4
   for (int i = 0; i < parts; ++i) {
     k4 += *reinterpret_cast<const f32x4*>(src + (int64_t)i * 2 * keys_pad * D);

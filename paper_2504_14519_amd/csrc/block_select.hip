@@ -57,269 +57,606 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 }
 
 // ------------------------------------------------------------------------------------ selection
-// score[r][j] = q_r . mean_j in 64 bits.  A workgroup takes 16 rows of a plane (they share the means); its four waves share out the
-// blocks, 16 at a time on the matrix unit (v_mfma_f64_16x16x4: a lane holds row or block lane & 15, contraction index lane >> 4;
-// result register i of a lane is row 4 i + (lane >> 4), column lane & 15), and leave the scores rounded to 32 bits in LDS.
-// Rounding keeps order, so only equal 32-bit scores at the border are looked at again, in 64 bits.  Then every wave picks the blocks of
-// four rows, the largest score first: scores in registers as unsigned numbers of the same order, a maximum over the wave,
-// and all that equal it are taken at once while there is room for them.  Blocks come in chunks of kSelBlocks; what is taken of one
-// competes with the next one's.
-constexpr int kSelRows = 16, kSelBlocks = 512, kSelRegs = kSelBlocks / 64;
+// score[r][j] = q_r . mean_j, compared in 64 bits, without computing most of it in 64 bits.  A float32 mean is exactly the sum of three bf16
+// numbers, each 2^-8 of the one before at most, so bf16 matrix instructions give every score with float32 additions alone as its error.
+// The smallest parts go first: only the D products of the largest are added at the size of the score, so that it is off by at most
+//   delta_r = (9/8) D 2^-23 |q_r| max_j |mean_j|.
+// If T is the n-th largest of the approximate scores of a row, the exact n-th largest lies within delta of T: what is above T + 2 delta is
+// taken for certain, what is below T - 2 delta is not, and only where more lies between than there are places are scores computed in
+// 64 bits (one row in a hundred).
+//
+// T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
+// goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
+// again (cheaper than keeping them: 24 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
+// 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: SELECT_US us; with sorted pieces of scores kept in LDS 204, with
+// every score in 64 bits on the matrix unit 550.
 
-// The order of floats as unsigned numbers: 0 stays free for "no candidate", NaN comes before all others.
-SP_DEV uint32_t score_key(float x) {
-  uint32_t u = __float_as_uint(x);
-  if ((u & 0x7fffffffu) > 0x7f800000u) return 1u;
-  if (u == 0x80000000u) u = 0u;                      // -0 = 0
-  return (u & 0x80000000u) ? ~u : u | 0x80000000u;   // (-inf: 0x007fffff)
-}
-SP_DEV uint32_t wave_max(uint32_t v) {
+// Places that a row's list of candidates has (what is certain and what is not): with more, which only many equal scores can bring, the row
+// is done in 64 bits throughout.
+constexpr int select_places(int k) { return k <= 16 ? 32 : kMaxTopK + 32; }
+constexpr uint32_t kUnsure = 0x80000000u;      // flag of a candidate within 2 delta of T
+
+// A tile of 32 blocks of means as three bf16 parts (largest first): upper halves of floats, rounded towards zero, so that what is left is exact.
+SP_DEV void split_means(const f32x4& x0, const f32x4& x1, bf16x8 (&part)[3], float& sq) {
+  float r[8];
 #pragma unroll
-  for (int w = 1; w < 64; w <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, w, 64);
-    v = v > o ? v : o;
+  for (int e = 0; e < 8; ++e) {
+    r[e] = e < 4 ? x0[e & 3] : x1[e & 3];
+    sq += r[e] * r[e];
   }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const uint32_t lo = __float_as_uint(r[e]), hi = __float_as_uint(r[e + 1]);
+      w[e / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+      r[e] -= __uint_as_float(lo & 0xffff0000u);
+      r[e + 1] -= __uint_as_float(hi & 0xffff0000u);
+    }
+    part[i] = __builtin_bit_cast(bf16x8, w);
+  }
+}
+template <int K>
+SP_DEV void keep_largest(float (&t)[K], float x) {
+#pragma unroll
+  for (int i = K - 1; i > 0; --i) t[i] = __builtin_amdgcn_fmed3f(t[i - 1], t[i], x);
+  t[0] = fmaxf(t[0], x);
+}
+// Two lists in order -> the K largest of both, in order: the larger ones of one and the other reversed, sorted by halves.
+template <int K>
+SP_DEV void merge_largest(float (&t)[K], const float (&o)[K]) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) t[i] = fmaxf(t[i], o[K - 1 - i]);
+#pragma unroll
+  for (int d = K / 2; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (!(i & d)) {
+        const float big = fmaxf(t[i], t[i + d]);
+        t[i + d] = fminf(t[i], t[i + d]);
+        t[i] = big;
+      }
+}
+template <int K>
+SP_DEV float place_of(const float (&t)[K], int n) {      // t[n - 1]
+  float v = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < K; ++i) v = i == n - 1 ? t[i] : v;
   return v;
 }
 
+// What a row wants: `need` of the blocks [first_block, own), and block `forced` (or -1) before all others.
+struct SelRow { int own, need, forced; };
+SP_DEV SelRow select_row_of(const BlockSelectArgs& a, int rh) {
+  const int end = a.first_block + a.n_blocks;
+  SelRow r = {end, a.top_k, -1};
+  if (a.causal) {
+    const int64_t own = (a.q_offset + rh % a.s_q) / a.block_len;
+    if (own < end) r.own = (int)own;
+    if (own >= a.first_block && own < end) { r.forced = (int)own; --r.need; }
+  }
+  if (r.need <= 0 || r.own < a.first_block) r.own = a.first_block;
+  return r;
+}
+SP_DEV const bf16_t* select_q(const BlockSelectArgs& a, int b, int hk, int rh) {
+  const int hl = rh / a.s_q, r = rh - hl * a.s_q;
+  return a.q + (int64_t)b * a.q_stride_b + (int64_t)r * a.q_stride_s + (int64_t)(hk * a.group + hl) * a.q_stride_h;
+}
+// What lies between and above: NaN bounds (a mean or a query that is not finite) leave everything open.
+SP_DEV void select_bounds(float t, float delta, float* lo, float* hi) {
+  const bool clear = delta < INFINITY && fabsf(t) < INFINITY;
+  *lo = clear ? t - 2.f * delta : -INFINITY;
+  *hi = clear ? t + 2.f * delta : INFINITY;
+}
+// Bit n of a lane's mask: block n of a tile whose 16 scores of the lane's half are s (NaN counts as open).
+SP_DEV uint32_t at_least(const f32x16& s, float lo, int g) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m |= !(s[i] < lo) ? 1u << (8 * (i >> 2) + (i & 3)) : 0u;
+  return m << (4 * g);
+}
+SP_DEV uint32_t above(const f32x16& s, float hi, int g) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m |= s[i] > hi ? 1u << (8 * (i >> 2) + (i & 3)) : 0u;
+  return m << (4 * g);
+}
+SP_DEV uint32_t both_halves(uint32_t m) {
+  auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return r[0] | r[1];
+}
+SP_DEV uint32_t blocks_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }      // bits of the tile's blocks before the n-th
+
 template <int D>
-__global__ __launch_bounds__(256) void block_select_kernel(const BlockSelectArgs a) {
-  typedef double f64x4 __attribute__((ext_vector_type(4)));
-  constexpr int ROW = kSelBlocks + 1;                // (padded: a column of the tile is 4 banks apart)
-  __shared__ uint32_t keys[kSelRows * ROW];
-  __shared__ uint32_t carry_key[kSelRows][kMaxTopK];
-  __shared__ int32_t carry_idx[kSelRows][kMaxTopK];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hk = blockIdx.y, b = blockIdx.z;
-  const int rows = a.group * a.s_q, row0 = blockIdx.x * kSelRows;
+SP_DEV double exact_score(const float* mean, const bf16_t* q) {
+  double sum = 0;
+#pragma unroll 8
+  for (int e = 0; e < D / 4; ++e) {
+    const f32x4 x = reinterpret_cast<const f32x4*>(mean)[e];
+    const bf16x4 y = reinterpret_cast<const bf16x4*>(q)[e];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sum += (double)(float)y[u] * (double)x[u];
+  }
+  return sum == sum ? sum : -INFINITY;               // (NaN counts as the lowest)
+}
+SP_DEV double wave_max(double v) {
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) {
+    const double o = __shfl_xor(v, w, 64);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+// A row with more candidates than places, by one wave: scores in 64 bits of those that are not certain, the largest first, of equal ones the
+// lower index.  The list (ascending) ends up with `need` entries.
+template <int D>
+SP_DEV void settle_row(uint32_t* list, int count, int places, int need, const bf16_t* q, const float* means, int first_block, int own, int lane) {
+  if (count <= places) {
+    constexpr int REGS = (kMaxTopK + 32 + 63) / 64;
+    uint32_t c[REGS];
+    double d[REGS];
+    uint32_t open = 0, taken = 0;
+    int room = need;
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      const int at = 64 * i + lane;
+      c[i] = at < count ? list[at] : 0u;
+      const bool unsure = at < count && (c[i] & kUnsure), sure = at < count && !(c[i] & kUnsure);
+      open |= unsure ? 1u << i : 0u;
+      taken |= sure ? 1u << i : 0u;
+      room -= __popcll(__builtin_amdgcn_ballot_w64(sure));
+      c[i] &= ~kUnsure;
+      d[i] = unsure ? exact_score<D>(means + (int64_t)c[i] * D, q) : -INFINITY;
+    }
+    for (; room > 0; --room) {
+      double best = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < REGS; ++i)
+        if (((open >> i) & 1u) && d[i] > best) best = d[i];
+      best = wave_max(best);
+      bool found = false;                            // (lanes ascend within a register, registers ascend)
+#pragma unroll
+      for (int i = 0; i < REGS; ++i) {
+        const uint64_t eq = __builtin_amdgcn_ballot_w64(((open >> i) & 1u) && d[i] == best);
+        if (!found && eq) {
+          found = true;
+          if (lane == __ffsll((unsigned long long)eq) - 1) { open &= ~(1u << i); taken |= 1u << i; }
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < REGS; ++i) {
+      const bool in = (taken >> i) & 1u;
+      const uint64_t mask = __builtin_amdgcn_ballot_w64(in);
+      if (in) list[at + __popcll(mask & ((1ull << lane) - 1ull))] = c[i];
+      at += __popcll(mask);
+    }
+  } else {
+    // the next one each time: the largest score behind the one before (lower, or equal with a higher index)
+    double last = INFINITY;
+    int last_j = 0x7fffffff, mine = 0x7fffffff;      // (the first: everything is behind +inf but +inf itself, which any index is behind)
+    bool first = true;
+    for (int n = 0; n < need; ++n) {
+      double best = -INFINITY;
+      int best_j = 0x7fffffff;
+      for (int j = first_block + lane; j < own; j += 64) {
+        const double s = exact_score<D>(means + (int64_t)j * D, q);
+        if ((first || s < last || (s == last && j > last_j)) && (best_j == 0x7fffffff || s > best)) { best = s; best_j = j; }
+      }
+      const double top = wave_max(best_j == 0x7fffffff ? -INFINITY : best);
+      int lowest = best_j != 0x7fffffff && best == top ? best_j : 0x7fffffff;
+#pragma unroll
+      for (int w = 1; w < 64; w <<= 1) {
+        const int o = __shfl_xor(lowest, w, 64);
+        lowest = o < lowest ? o : lowest;
+      }
+      last = top;
+      last_j = lowest;
+      first = false;
+      if (lane == n) mine = lowest;
+    }
+    int at = 0;                                      // ascending: each goes behind the smaller ones
+    for (int n = 0; n < need; ++n) at += __shfl(mine, n, 64) < mine ? 1 : 0;
+    __builtin_amdgcn_wave_barrier();
+    if (lane < need) list[at] = (uint32_t)mine;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Many rows: 128 a workgroup, 32 a wave; means are split once for all of them, into two LDS slots.
+template <int D, int K>
+constexpr size_t select_lds_bytes() { return (size_t)2 * 3 * 32 * D * 2 + (size_t)128 * select_places(K) * 4; }
+template <int D, int K>
+__global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectArgs a) {
+  constexpr int KS = D / 16, PART = 32 * D * 2, SLOT = 3 * PART, PLACES = select_places(K), PER = D / 8 / 8;      // 16-byte chunks of a part a thread writes
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ uint32_t most_s;                        // largest |mean|^2 (bits of a float; all are >= 0)
+  __shared__ int last_s;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.y, b = blockIdx.z, rows = a.group * a.s_q, row0 = blockIdx.x * 128 + wave * 32;
   const float* const means = a.means + ((int64_t)b * a.n_kv_heads + hk) * a.blocks_total * D;
-  const int end_block = a.first_block + a.n_blocks;
-
-  auto row_ptr = [&](int rh) {
-    const int hl = rh / a.s_q, r = rh - hl * a.s_q;
-    return a.q + (int64_t)b * a.q_stride_b + (int64_t)r * a.q_stride_s + (int64_t)(hk * a.group + hl) * a.q_stride_h;
-  };
-  // one past the last block that competes for a row, and whether the row's own block is taken before all others
-  auto own_block = [&](int rh) { return a.causal ? (a.q_offset + rh % a.s_q) / a.block_len : (int64_t)end_block; };
-
-  // this lane's row as A operand: contraction step (v, e) of group g is head_dim 16 v + 4 g + e
-  double q[D / 4];
+  const int rh = row0 + ql < rows ? row0 + ql : rows - 1;
+  const SelRow want = select_row_of(a, rh);
+  if (tid == 0) { most_s = 0u; last_s = a.first_block; }
+  bf16x8 q[KS];
+  float norm = 0.f;
   {
-    const int rh = row0 + (lane & 15);
-    const bf16_t* p = row_ptr(rh < rows ? rh : rows - 1) + 4 * (lane >> 4);
+    const bf16_t* p = select_q(a, b, hk, rh) + 8 * g;
 #pragma unroll
-    for (int v = 0; v < D / 16; ++v) {
-      const bf16x4 x = *reinterpret_cast<const bf16x4*>(p + 16 * v);
+    for (int ks = 0; ks < KS; ++ks) {
+      q[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q[4 * v + e] = (double)(float)x[e];
+      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
     }
+    norm = __builtin_sqrtf(xhalf_sum(norm));
   }
-  // blocks behind the last own block of the rows are nobody's candidates
-  int64_t last = 0;
-  for (int i = 0; i < kSelRows && row0 + i < rows; ++i) {
-    const int64_t o = own_block(row0 + i);
-    last = o > last ? o : last;
-  }
-  const int stop = last < end_block ? (int)last : end_block;
-  int carried[4] = {0, 0, 0, 0};                     // of the wave's four rows
+  __syncthreads();
+  atomicMax(&last_s, want.own);
+  __syncthreads();
+  const int stop = __builtin_amdgcn_readfirstlane(last_s), nt = (stop - a.first_block + 31) / 32;
+  uint32_t* const list = reinterpret_cast<uint32_t*>(smem + 2 * SLOT) + (wave * 32 + ql) * PLACES;
 
-  for (int c0 = a.first_block; c0 < stop; c0 += kSelBlocks) {
-    const int n = stop - c0 < kSelBlocks ? stop - c0 : kSelBlocks;
-    for (int t = wave; t * 16 < n; t += 4) {
-      const int j = c0 + t * 16 + (lane & 15);
-      const float* mp = means + (int64_t)(j < stop ? j : stop - 1) * D + 4 * (lane >> 4);
-      f32x4 m[D / 16];
+  f32x4 x[2 * PER];
+  float most = 0.f;
+  auto fetch = [&](int t) {
+    const int j = a.first_block + t * 32 + tid / 8;
+    const f32x4* mp = reinterpret_cast<const f32x4*>(means + (int64_t)(j < stop ? j : stop - 1) * D + tid % 8 * (D / 8));
 #pragma unroll
-      for (int v = 0; v < D / 16; ++v) m[v] = *reinterpret_cast<const f32x4*>(mp + 16 * v);
-      f64x4 s = {0, 0, 0, 0};
+    for (int i = 0; i < 2 * PER; ++i) x[i] = mp[i];
+  };
+  auto store = [&](int t) {
+    float sq = 0.f;
 #pragma unroll
-      for (int v = 0; v < D / 16; ++v)
+    for (int i = 0; i < PER; ++i) {
+      bf16x8 part[3];
+      split_means(x[2 * i], x[2 * i + 1], part, sq);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[4 * v + e], (double)m[v][e], s, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) keys[(4 * i + (lane >> 4)) * ROW + t * 16 + (lane & 15)] = score_key((float)s[i]);
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(smem + (t & 1) * SLOT + p * PART + tile_off<D>(tid / 8, tid % 8 * PER + i)) = part[p];
     }
+#pragma unroll
+    for (int w = 1; w < 8; w <<= 1) sq += __shfl_xor(sq, w, 64);
+    most = sq == sq ? fmaxf(most, sq) : INFINITY;    // (a NaN anywhere: nothing is certain)
+  };
+  RpOffsets<D> lo_m;
+  lo_m.init(lane, (int)lds_addr(smem));
+  // walks the tiles; use(t, s): scores of tile t
+  auto walk = [&](auto&& use) {
+    fetch(0);
+    store(0);
     __syncthreads();
+    for (int t = 0; t < nt; ++t) {
+      if (t + 1 < nt) fetch(t + 1);
+      f32x16 s = {0};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const int rl = wave * 4 + w, rh = row0 + rl;
-      if (rh >= rows) continue;
-      const int64_t own = own_block(rh);
-      const bool forced = a.causal && own >= a.first_block && own < end_block;
-      int need = a.top_k - (forced ? 1 : 0);
-      // register 0: what the chunks before left (their blocks come first); then the chunk's, 64 blocks a register
-      uint32_t k[kSelRegs + 1];
-      k[0] = lane < carried[w] ? carry_key[rl][lane] : 0u;
+      for (int p = 2; p >= 0; --p)
 #pragma unroll
-      for (int i = 0; i < kSelRegs; ++i) {
-        const int at = 64 * i + lane;
-        k[i + 1] = at < n && c0 + at < own ? keys[rl * ROW + at] : 0u;
-      }
-      uint32_t taken = 0;                            // bit i: this lane's candidate of register i
-      while (need > 0) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i <= kSelRegs; ++i) m = m > k[i] ? m : k[i];
-        m = wave_max(m);
-        if (m == 0) break;
-        int cnt = 0;
-#pragma unroll
-        for (int i = 0; i <= kSelRegs; ++i) cnt += __popcll(__builtin_amdgcn_ballot_w64(k[i] == m));
-        if (cnt <= need) {
-#pragma unroll
-          for (int i = 0; i <= kSelRegs; ++i)
-            if (k[i] == m) { k[i] = 0; taken |= 1u << i; }
-          need -= cnt;
-          continue;
-        }
-        // More equal 32-bit scores than room: their scores in 64 bits, each lane its own candidates; then the largest of them, the
-        // lowest index first (lanes ascend within a register, registers ascend).
-        const bf16_t* qp = row_ptr(rh);
-        double d[kSelRegs + 1];
-#pragma unroll
-        for (int i = 0; i <= kSelRegs; ++i) {
-          d[i] = -INFINITY;
-          if (k[i] == m) {
-            const int j = i == 0 ? carry_idx[rl][lane] : c0 + 64 * (i - 1) + lane;
-            const float* mp = means + (int64_t)j * D;
-            double s = 0;
-            for (int e = 0; e < D; ++e) s += (double)(float)qp[e] * (double)mp[e];
-            d[i] = s == s ? s : -INFINITY;           // (NaN: all alike, the lowest index first)
-          }
-        }
-        while (need > 0) {
-          double best = -INFINITY;
-#pragma unroll
-          for (int i = 0; i <= kSelRegs; ++i)
-            if (k[i] == m && d[i] > best) best = d[i];
-#pragma unroll
-          for (int w2 = 1; w2 < 64; w2 <<= 1) {
-            const double o = __shfl_xor(best, w2, 64);
-            best = o > best ? o : best;
-          }
-          bool found = false;
-#pragma unroll
-          for (int i = 0; i <= kSelRegs; ++i) {
-            const uint64_t eq = __builtin_amdgcn_ballot_w64(k[i] == m && d[i] == best);
-            if (!found && eq) {
-              found = true;
-              if (lane == __ffsll((unsigned long long)eq) - 1) { k[i] = 0; taken |= 1u << i; }
-            }
-          }
-          --need;
-        }
-      }
-      // what was taken, in ascending order
-      int at = 0;
-      uint32_t out_key[kSelRegs + 1];
-      int out_idx[kSelRegs + 1], out_at[kSelRegs + 1];
-#pragma unroll
-      for (int i = 0; i <= kSelRegs; ++i) {
-        const uint64_t mask = __builtin_amdgcn_ballot_w64((taken >> i) & 1u);
-        out_at[i] = (taken >> i) & 1u ? at + __popcll(mask & ((1ull << lane) - 1ull)) : -1;
-        at += __popcll(mask);
-        out_idx[i] = out_key[i] = 0;
-        if (out_at[i] >= 0) {
-          out_key[i] = i == 0 ? carry_key[rl][lane] : keys[rl * ROW + 64 * (i - 1) + lane];
-          out_idx[i] = i == 0 ? carry_idx[rl][lane] : c0 + 64 * (i - 1) + lane;
-        }
-      }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int i = 0; i <= kSelRegs; ++i)
-        if (out_at[i] >= 0) { carry_key[rl][out_at[i]] = out_key[i]; carry_idx[rl][out_at[i]] = out_idx[i]; }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      carried[w] = at;
+        for (int ks = 0; ks < KS; ++ks) s = mfma32(lds_rp<D>(lo_m, ks, p * PART), q[ks], s);
+      use(t, s);
+      lo_m.add((t & 1) ? -SLOT : SLOT);
+      if (t + 1 < nt) store(t + 1);
+      __syncthreads();
     }
+    if (nt & 1) lo_m.add(-SLOT);
+  };
+  int count = 0, sure = 0;
+  if (nt > 0) {
+    float top[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) top[i] = -INFINITY;
+    walk([&](int t, f32x16& s) {
+      const int left = want.own - a.first_block - t * 32;      // blocks of the tile that compete for the row
+      if (__builtin_amdgcn_ballot_w64(left < 32) != 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < left - 4 * g ? s[i] : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) keep_largest<K>(top, s[i]);
+    });
+    atomicMax(&most_s, __float_as_uint(most));
+    float other[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[i]), __float_as_uint(top[i]), false, false);
+      other[i] = __uint_as_float(g ? r[0] : r[1]);
+    }
+    merge_largest<K>(top, other);
     __syncthreads();
+    float lo, hi;
+    select_bounds(place_of<K>(top, want.need), 1.125f * D * 0x1p-23f * norm * __builtin_sqrtf(__uint_as_float(most_s)), &lo, &hi);
+    if (want.own - a.first_block <= want.need) { lo = -INFINITY; hi = INFINITY; }      // no more than are wanted: all
+    walk([&](int t, f32x16& s) {
+      const int left = want.own - a.first_block - t * 32;
+      const uint32_t in = blocks_below(left), open = both_halves(at_least(s, lo, g)) & in, certain = both_halves(above(s, hi, g));
+      sure += __popc(certain & in);
+      if (g == 0)
+        for (uint32_t m = open; m; m &= m - 1) {
+          const int n = __ffs(m) - 1;
+          if (count < PLACES) list[count] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
+          ++count;
+        }
+    });
   }
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const int rl = wave * 4 + w, rh = row0 + rl;
-    if (rh >= rows || lane >= a.top_k) continue;
-    const int64_t own = own_block(rh);
-    const bool forced = a.causal && own >= a.first_block && own < end_block;
-    const int hl = rh / a.s_q, r = rh - hl * a.s_q;
-    const int v = lane < carried[w] ? carry_idx[rl][lane] : (lane == carried[w] && forced ? (int)own : -1);
-    a.index[(((int64_t)b * a.n_q_heads + hk * a.group + hl) * a.s_q + r) * a.top_k + lane] = v;
+  // rows with more candidates than places
+  for (uint64_t m = __builtin_amdgcn_ballot_w64(g == 0 && count > want.need && row0 + ql < rows); m; m &= m - 1) {
+    const int from = __ffsll((unsigned long long)m) - 1;
+    const int n = __builtin_amdgcn_readlane(count, from), need = __builtin_amdgcn_readlane(want.need, from), own = __builtin_amdgcn_readlane(want.own, from);
+    settle_row<D>(reinterpret_cast<uint32_t*>(smem + 2 * SLOT) + (wave * 32 + from) * PLACES, n, PLACES, need, select_q(a, b, hk, row0 + from), means,
+                  a.first_block, own, lane);
+  }
+  count = count < want.need ? count : want.need;
+  // the wave's rows of the index, whole lines at a time
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int n_rows = rows - row0 < 32 ? rows - row0 : 32;
+  int32_t* const to = a.index + (((int64_t)b * a.n_kv_heads + hk) * rows + row0) * a.top_k;
+  for (int i0 = 0; i0 < n_rows * a.top_k; i0 += 64) {
+    const int i = i0 + lane, r = i / a.top_k, slot = i - r * a.top_k, rr = r < 32 ? r : 31;
+    const int n = __shfl(count, rr, 64), f = __shfl(want.forced, rr, 64);
+    const uint32_t v = reinterpret_cast<const uint32_t*>(smem + 2 * SLOT)[(wave * 32 + rr) * PLACES + (slot < PLACES ? slot : 0)];
+    if (i < n_rows * a.top_k) to[i] = slot < n ? (int)(v & ~kUnsure) : slot == n && f >= 0 ? f : -1;
   }
 }
 
-hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t st) {
-  dim3 grid((unsigned)((a.group * (int64_t)a.s_q + kSelRows - 1) / kSelRows), (unsigned)a.n_kv_heads, (unsigned)a.batch), block(256);
-  if (head_dim == 128) hipLaunchKernelGGL(block_select_kernel<128>, grid, block, 0, st, a);
-  else hipLaunchKernelGGL(block_select_kernel<64>, grid, block, 0, st, a);
+// Few rows (tokens): 32 a workgroup, whose eight waves share out the tiles; means go from memory through registers to the matrix unit.  The waves'
+// lists meet in LDS, and so do the second walk's masks, a bit a block.
+constexpr int kFewWaves = 8, kFewTiles = 512;
+template <int D, int K>
+constexpr size_t select_few_lds_bytes(int tiles) {
+  const size_t lists = (size_t)kFewWaves * 2 * 32 * (K + 1) * 4, masks = (size_t)tiles * 32 * 2 * 4 + 32 * select_places(K) * 4;
+  return lists > masks ? lists : masks;
+}
+template <int D, int K>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(const BlockSelectArgs a) {
+  constexpr int KS = D / 16, PLACES = select_places(K);
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  __shared__ uint32_t most_s;
+  __shared__ int last_s;
+  __shared__ float border_s[32], norm_s[32];
+  __shared__ int count_s[32];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hk = blockIdx.y, b = blockIdx.z, rows = a.group * a.s_q, row0 = blockIdx.x * 32;
+  const float* const means = a.means + ((int64_t)b * a.n_kv_heads + hk) * a.blocks_total * D;
+  const int rh = row0 + ql < rows ? row0 + ql : rows - 1;
+  const SelRow want = select_row_of(a, rh);
+  if (tid == 0) { most_s = 0u; last_s = a.first_block; }
+  bf16x8 q[KS];
+  {
+    float norm = 0.f;
+    const bf16_t* p = select_q(a, b, hk, rh) + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      q[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
+    }
+    norm = __builtin_sqrtf(xhalf_sum(norm));
+    if (tid < 32) norm_s[tid] = norm;
+  }
+  __syncthreads();
+  if (tid < 32) atomicMax(&last_s, want.own);
+  __syncthreads();
+  const int stop = __builtin_amdgcn_readfirstlane(last_s), nt = (stop - a.first_block + 31) / 32;
+  float most = 0.f;
+  auto scores = [&](int t) {
+    const int j = a.first_block + t * 32 + ql;
+    const float* mp = means + (int64_t)(j < stop ? j : stop - 1) * D + 8 * g;
+    bf16x8 part[KS][3];
+    float sq = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      split_means(*reinterpret_cast<const f32x4*>(mp + 16 * ks), *reinterpret_cast<const f32x4*>(mp + 16 * ks + 4), part[ks], sq);
+    f32x16 s = {0};
+#pragma unroll
+    for (int p = 2; p >= 0; --p)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s = mfma32(part[ks][p], q[ks], s);
+    sq = xhalf_sum(sq);
+    most = sq == sq ? fmaxf(most, sq) : INFINITY;
+    return s;
+  };
+  float top[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) top[i] = -INFINITY;
+  for (int t = wave; t < nt; t += kFewWaves) {
+    f32x16 s = scores(t);
+    const int left = want.own - a.first_block - t * 32 - 4 * g;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) keep_largest<K>(top, 8 * (i >> 2) + (i & 3) < left ? s[i] : -INFINITY);
+  }
+  atomicMax(&most_s, __float_as_uint(most));
+  float* const lists = reinterpret_cast<float*>(smem);      // [row][wave, half][K + 1]
+#pragma unroll
+  for (int i = 0; i < K; ++i) lists[((ql * kFewWaves + wave) * 2 + g) * (K + 1) + i] = top[i];
+  __syncthreads();
+  {
+    // sixteen lists a row, a lane each
+    static_assert(kFewWaves * 2 == 16 && kFewWaves * 4 == 32, "four rows a wave");
+    const int r = wave * 4 + lane / 16;
+#pragma unroll
+    for (int i = 0; i < K; ++i) top[i] = lists[(r * 16 + lane % 16) * (K + 1) + i];
+#pragma unroll
+    for (int w = 1; w < 16; w <<= 1) {
+      float other[K];
+#pragma unroll
+      for (int i = 0; i < K; ++i) other[i] = __shfl_xor(top[i], w, 64);
+      merge_largest<K>(top, other);
+    }
+    const float v = place_of<K>(top, __shfl(want.need, r, 64));
+    if (lane % 16 == 0) border_s[r] = v;
+  }
+  __syncthreads();
+  float lo, hi;
+  select_bounds(border_s[ql], 1.125f * D * 0x1p-23f * norm_s[ql] * __builtin_sqrtf(__uint_as_float(most_s)), &lo, &hi);
+  if (want.own - a.first_block <= want.need) { lo = -INFINITY; hi = INFINITY; }
+  uint32_t* const open_s = reinterpret_cast<uint32_t*>(smem);      // [tile][row]; certain ones behind them, then the rows' lists
+  uint32_t* const certain_s = open_s + nt * 32;
+  for (int t = wave; t < nt; t += kFewWaves) {
+    const f32x16 s = scores(t);
+    const uint32_t in = blocks_below(want.own - a.first_block - t * 32), open = both_halves(at_least(s, lo, g)) & in, certain = both_halves(above(s, hi, g)) & in;
+    if (g == 0) { open_s[t * 32 + ql] = open; certain_s[t * 32 + ql] = certain; }
+  }
+  __syncthreads();
+  uint32_t* const cand = certain_s + nt * 32;
+  if (tid < 32) {
+    int count = 0;
+    for (int t = 0; t < nt; ++t) {
+      const uint32_t certain = certain_s[t * 32 + tid];
+      for (uint32_t m = open_s[t * 32 + tid]; m; m &= m - 1) {
+        const int n = __ffs(m) - 1;
+        if (count < PLACES) cand[tid * PLACES + count] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
+        ++count;
+      }
+    }
+    count_s[tid] = count;
+  }
+  __syncthreads();
+  for (int r = wave; r < 32 && row0 + r < rows; r += kFewWaves) {
+    const int n = __builtin_amdgcn_readfirstlane(count_s[r]), need = __builtin_amdgcn_readlane(want.need, r), own = __builtin_amdgcn_readlane(want.own, r);
+    if (n > need) settle_row<D>(cand + r * PLACES, n, PLACES, need, select_q(a, b, hk, row0 + r), means, a.first_block, own, lane);
+    const int forced = __builtin_amdgcn_readlane(want.forced, r), have = n < need ? n : need;
+    if (lane < a.top_k)
+      a.index[(((int64_t)b * a.n_kv_heads + hk) * rows + row0 + r) * a.top_k + lane] =
+          lane < have ? (int)(cand[r * PLACES + lane] & ~kUnsure) : lane == have && forced >= 0 ? forced : -1;
+  }
+}
+
+template <int D, int K>
+static hipError_t launch_select_t(const BlockSelectArgs& a, bool few, hipStream_t st) {
+  const int64_t rows = a.group * (int64_t)a.s_q;
+  const unsigned heads = (unsigned)a.n_kv_heads, batch = (unsigned)a.batch;
+  if (few) hipLaunchKernelGGL((block_select_few_kernel<D, K>), dim3((unsigned)((rows + 31) / 32), heads, batch), dim3(kFewWaves * 64),
+                              (select_few_lds_bytes<D, K>((a.n_blocks + 31) / 32)), st, a);
+  else hipLaunchKernelGGL((block_select_kernel<D, K>), dim3((unsigned)((rows + 127) / 128), heads, batch), dim3(256), (select_lds_bytes<D, K>()), st, a);
   return hipGetLastError();
+}
+template <int D>
+static hipError_t launch_select_d(const BlockSelectArgs& a, bool few, hipStream_t st) {
+  if (a.top_k <= 8) return launch_select_t<D, 8>(a, few, st);
+  if (a.top_k <= 16) return launch_select_t<D, 16>(a, few, st);
+  if (a.top_k <= 32) return launch_select_t<D, 32>(a, few, st);
+  return launch_select_t<D, 64>(a, few, st);
+}
+// The few-row kernel has four times the workgroups, and a walk an eighth as long, for calls whose 128-row workgroups would not fill the
+// chip; its masks of a call's blocks have to fit LDS.
+hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, int compute_units, hipStream_t st) {
+  const int64_t wgs = (a.group * (int64_t)a.s_q + 127) / 128 * a.n_kv_heads * a.batch;
+  const bool few = wgs < compute_units && a.n_blocks <= kFewTiles * 32;
+  return head_dim == 128 ? launch_select_d<128>(a, few, st) : launch_select_d<64>(a, few, st);
+}
+
+template <int D, int K>
+static hipError_t opt_in_select() {
+  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_kernel<D, K>), attr, (int)select_lds_bytes<D, K>());
+  if (e == hipSuccess)
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_few_kernel<D, K>), attr, (int)select_few_lds_bytes<D, K>(kFewTiles));
+  return e;
+}
+template <int D>
+static hipError_t opt_in_select_d() {
+  hipError_t e = opt_in_select<D, 8>();
+  if (e == hipSuccess) e = opt_in_select<D, 16>();
+  if (e == hipSuccess) e = opt_in_select<D, 32>();
+  return e == hipSuccess ? opt_in_select<D, 64>() : e;
 }
 
 // ------------------------------------------------------------------------------------ lists
-// The rows of every block, in ascending order of (head of the group, row).  Count and fill go over chunks of kListRows rows with a bit
-// per (block, row) in LDS: setting bits commutes, and a row's place in the block's list is a count of the bits below its own, so the
-// lists are the same on every run.
-SP_DEV int64_t list_row_base(const BlockArgs& a, int b, int hk, int rh, int* hl, int* r) {
-  *hl = rh / a.s_q;
-  *r = rh - *hl * a.s_q;
-  return ((int64_t)b * a.n_q_heads + hk * a.group + *hl) * a.s_q + *r;
-}
-template <bool FILL>
-__global__ __launch_bounds__(kListRows) void block_list_kernel(const BlockArgs a) {
-  extern __shared__ uint32_t bits[];                 // [blocks of the window][kListRows / 32]
-  constexpr int W = kListRows / 32;
+// The rows of every block, in ascending order of (head of the group, row).  Three launches: places of the rows of a chunk within the
+// chunk, starts, entries.
+//
+// Chunks of kListRows rows have a bit per (block, row) in LDS: setting bits commutes, and a row's place among the chunk's rows of a block
+// is a count of the bits below its own, so the lists are the same on every run.  (The index rows of a plane follow each other, and so do the
+// slots of part_lse: entry i of the chunk is row i / top_k, slot i % top_k of both.)
+constexpr int kListThreads = 512, kListWords = kListRows / 32, kListStride = kListWords + 1;      // (odd: a column of words is spread over the banks)
+SP_HOST_DEV int list_lds_words(int n_blocks) { return (n_blocks < kListBlocks ? n_blocks : kListBlocks) * kListStride * 3 / 2 + 1; }
+__global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArgs a) {
+  extern __shared__ uint32_t bits[];                 // [blocks of the window][kListStride]; bits below each word behind them; the chunk's index
   const int tid = threadIdx.x, chunk = blockIdx.x, plane = blockIdx.y;
-  const int b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int rows = a.group * a.s_q, rh = chunk * kListRows + tid;
-  int hl = 0, r = 0;
-  const int64_t row = rh < rows ? list_row_base(a, b, hk, rh, &hl, &r) : 0;
-  const int32_t* idx = a.index + row * a.top_k;
-  uint64_t valid = 0;
-  if (rh < rows)
-    for (int s = 0; s < a.top_k; ++s)
-      if (block_slot_valid(a, idx, s, a.q_offset + r)) valid |= 1ull << s;
-  uint32_t* counts = a.counts + ((int64_t)plane * a.n_list_chunks + chunk) * a.n_blocks;
+  const int rows = a.group * a.s_q, row0 = chunk * kListRows, n_rows = rows - row0 < kListRows ? rows - row0 : kListRows;
+  const int64_t first = ((int64_t)plane * rows + row0) * a.top_k;      // (plane = batch index * kv heads + kv head)
+  int32_t* index = reinterpret_cast<int32_t*>(bits + list_lds_words(a.n_blocks));
+  float* valid = a.part_lse + first;                 // -inf: the slot has no block (and no result)
+  uint16_t* rank = a.ranks + first;
+  const int n_slots = n_rows * a.top_k;
+  uint32_t* counts = a.counts + (int64_t)plane * a.n_blocks * a.n_list_chunks + chunk;
+  for (int i = tid; i < n_slots; i += kListThreads) index[i] = a.index[first + i];
+  __syncthreads();
+  const float per_row = 1.0f / (float)a.top_k;
+  auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per_row); };      // i / top_k (i < 2^14: the half keeps it off the border)
+  static_assert(kListRows * kMaxTopK <= 1 << 14 && kListRows * kMaxTopK <= 32 * kListThreads, "slots of a chunk: exact quotients, a bit each");
+  uint32_t ok = 0;                                   // bit: this thread's slots
+  for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
+    const int row = row_of(i);
+    const bool v = block_slot_valid(a, index + row * a.top_k, i - row * a.top_k, a.q_offset + (row0 + row) % a.s_q);
+    valid[i] = v ? 0.f : -INFINITY;
+    ok |= v ? 1u << u : 0u;
+  }
   for (int w0 = 0; w0 < a.n_blocks; w0 += kListBlocks) {
     const int n = a.n_blocks - w0 < kListBlocks ? a.n_blocks - w0 : kListBlocks;
+    uint16_t* below = reinterpret_cast<uint16_t*>(bits + n * kListStride);
+    for (int i = tid; i < n * kListStride; i += kListThreads) bits[i] = 0u;
     __syncthreads();
-    for (int i = tid; i < n * W; i += kListRows) bits[i] = 0u;
-    __syncthreads();
-    for (uint64_t v = valid; v; v &= v - 1) {
-      const int j = idx[__ffsll((unsigned long long)v) - 1] - a.first_block - w0;
-      if (j >= 0 && j < n) atomicOr(&bits[j * W + (tid >> 5)], 1u << (tid & 31));
+    for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
+      const int j = index[i] - a.first_block - w0, row = row_of(i);
+      if (((ok >> u) & 1u) && j >= 0 && j < n) atomicOr(&bits[j * kListStride + (row >> 5)], 1u << (row & 31));
     }
     __syncthreads();
-    if constexpr (!FILL) {
-      for (int j = tid; j < n; j += kListRows) {
-        uint32_t c = 0;
-        for (int w = 0; w < W; ++w) c += __popc(bits[j * W + ((w + j) & (W - 1))]);
-        counts[w0 + j] = c;
+    for (int j = tid; j < n; j += kListThreads) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int w = 0; w < kListWords; ++w) {
+        below[j * kListStride + w] = (uint16_t)c;
+        c += __popc(bits[j * kListStride + w]);
       }
-    } else {
-      BlockEntry* entries = a.entries + (int64_t)plane * rows * a.top_k;
-      const uint32_t* start = a.start + (int64_t)plane * a.n_blocks;
-      for (uint64_t v = valid; v; v &= v - 1) {
-        const int s = __ffsll((unsigned long long)v) - 1, j = idx[s] - a.first_block - w0;
-        if (j < 0 || j >= n) continue;
-        uint32_t at = start[w0 + j] + counts[w0 + j];
-        for (int w = 0; w < (tid >> 5); ++w) at += __popc(bits[j * W + w]);
-        at += __popc(bits[j * W + (tid >> 5)] & ((1u << (tid & 31)) - 1u));
-        entries[at] = {(uint32_t)r, (uint32_t)(hl << 6 | s)};
-      }
+      counts[(int64_t)(w0 + j) * a.n_list_chunks] = c;
     }
+    __syncthreads();
+    for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
+      const int j = index[i] - a.first_block - w0, row = row_of(i);
+      if (((ok >> u) & 1u) && j >= 0 && j < n)
+        rank[i] = (uint16_t)(below[j * kListStride + (row >> 5)] + __popc(bits[j * kListStride + (row >> 5)] & ((1u << (row & 31)) - 1u)));
+    }
+    __syncthreads();
   }
-  if (FILL && rh < rows)                             // slots without a result: nothing else writes them
-    for (int s = 0; s < a.top_k; ++s) a.part_lse[row * a.top_k + s] = (valid >> s) & 1u ? 0.f : -INFINITY;
+}
+
+__global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int dkdv) {
+  const int plane = blockIdx.y, rows = a.group * a.s_q;
+  const int64_t n_slots = (int64_t)rows * a.top_k, i = (int64_t)blockIdx.x * 256 + threadIdx.x, at = plane * n_slots + i;
+  if (i >= n_slots || a.part_lse[at] != 0.f) return;
+  const int j = a.index[at] - a.first_block, rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
+  const BlockList list = a.lists[(int64_t)plane * a.n_blocks + j];
+  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * a.n_list_chunks + rh / kListRows] + a.ranks[at], to = list.first + pos;
+  a.entries[plane * n_slots + to] = {(uint32_t)(rh - hl * a.s_q), (uint32_t)(hl << 6 | slot)};
+  // the first row of a tile writes the tile down
+  const uint32_t left = list.len - pos, block = (uint32_t)(a.first_block + j);
+  if (pos % kBlockTileRows == 0)
+    a.items[(int64_t)plane * a.item_cap + list.tile0 + pos / kBlockTileRows] = {(int)block, (int)to, (int)(left < kBlockTileRows ? left : kBlockTileRows), 0};
+  if (dkdv && pos % (uint32_t)a.chunk_rows == 0) {
+    const uint32_t c = pos / (uint32_t)a.chunk_rows;
+    BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + list.item0 + c * (uint32_t)a.n_sub;
+    for (int s = 0; s < a.n_sub; ++s)
+      it[s] = {(int)block * a.n_sub + s, (int)to, (int)(left < (uint32_t)a.chunk_rows ? left : (uint32_t)a.chunk_rows), list.parts ? (int)(list.part0 + c) : -1};
+  }
 }
 
 // One workgroup a plane: counts of the chunks -> where each chunk's rows start in the block's list, list starts, tiles.
-constexpr int kScanThreads = 1024, kScanCols = 128, kScanSegs = kScanThreads / kScanCols;
+constexpr int kScanThreads = 1024;
+SP_DEV uint32_t wave_scan(uint32_t v) {      // inclusive sum over the lanes up to this one
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+  return v;
+}
 SP_DEV uint32_t scan_add(uint32_t* tmp, int tid, uint32_t v, uint32_t* total) {      // exclusive scan over the workgroup
   const int lane = tid & 63, wave = tid >> 6;
-  uint32_t x = v;
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_up((int)x, w, 64);
-    if (lane >= w) x += o;
-  }
+  const uint32_t x = wave_scan(v);
   __syncthreads();
   if (lane == 63) tmp[wave] = x;
   __syncthreads();
@@ -332,68 +669,57 @@ SP_DEV uint32_t scan_add(uint32_t* tmp, int tid, uint32_t v, uint32_t* total) { 
   return before + x - v;
 }
 __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
-  __shared__ uint32_t seg[kScanSegs][kScanCols], tmp[kScanThreads / 64];
-  const int tid = threadIdx.x, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
-  uint32_t* counts = a.counts + (int64_t)plane * nc * nb;
-  uint32_t* totals = a.start + (int64_t)plane * nb;              // (lengths first, starts in their place afterwards)
-  const int per = (nc + kScanSegs - 1) / kScanSegs;
-  for (int j0 = 0; j0 < nb; j0 += kScanCols) {
-    const int col = tid % kScanCols, s = tid / kScanCols, j = j0 + col;
-    const int c0 = s * per, c1 = c0 + per < nc ? c0 + per : nc;
-    uint32_t sum = 0;
-    if (j < nb)
-      for (int c = c0; c < c1; ++c) sum += counts[(int64_t)c * nb + j];
-    __syncthreads();
-    seg[s][col] = sum;
-    __syncthreads();
-    if (j < nb) {
-      uint32_t at = 0;
-      for (int i = 0; i < s; ++i) at += seg[i][col];
-      for (int c = c0; c < c1; ++c) {
-        const uint32_t x = counts[(int64_t)c * nb + j];
-        counts[(int64_t)c * nb + j] = at;
-        at += x;
+  __shared__ uint32_t tmp[kScanThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
+  BlockList* lists = a.lists + (int64_t)plane * nb;
+  // a wave four blocks at a time, four chunks a lane
+  constexpr int WAVES = kScanThreads / 64, PER = 4;
+  for (int j0 = tid >> 6; j0 < nb; j0 += PER * WAVES) {
+    uint32_t before[PER] = {0, 0, 0, 0};
+    for (int c0 = 4 * lane; c0 - 4 * lane < nc; c0 += 256) {
+      uint32_t v[PER][4];
+#pragma unroll
+      for (int p = 0; p < PER; ++p)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[p][u] = j0 + p * WAVES < nb && c0 + u < nc ? a.counts[((int64_t)plane * nb + j0 + p * WAVES) * nc + c0 + u] : 0u;
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        const uint32_t sum = v[p][0] + v[p][1] + v[p][2] + v[p][3], upto = wave_scan(sum);
+        uint32_t at = before[p] + upto - sum;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (j0 + p * WAVES < nb && c0 + u < nc) a.counts[((int64_t)plane * nb + j0 + p * WAVES) * nc + c0 + u] = at;
+          at += v[p][u];
+        }
+        before[p] += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
       }
-      if (s == kScanSegs - 1) totals[j] = at;
     }
+#pragma unroll
+    for (int p = 0; p < PER; ++p)
+      if (lane == 0 && j0 + p * WAVES < nb) lists[j0 + p * WAVES].len = before[p];
   }
   __threadfence_block();
   __syncthreads();
   uint32_t first = 0, tile = 0, item = 0, part = 0;              // running totals of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    const uint32_t len = j < nb ? totals[j] : 0u;
-    const uint32_t tiles = (len + kBlockTileRows - 1) / kBlockTileRows;
-    uint32_t sum_len, sum_tiles;
-    const uint32_t f = first + scan_add(tmp, tid, len, &sum_len);
-    const uint32_t t = tile + scan_add(tmp, tid, tiles, &sum_tiles);
+    BlockList l;
+    l.len = j < nb ? lists[j].len : 0u;
+    uint32_t sum_len, sum_tiles, sum_items = 0, sum_parts = 0;
+    l.first = first + scan_add(tmp, tid, l.len, &sum_len);
+    l.tile0 = tile + scan_add(tmp, tid, (l.len + kBlockTileRows - 1) / kBlockTileRows, &sum_tiles);
+    l.item0 = l.parts = l.part0 = 0;
+    if (dkdv) {
+      const uint32_t chunks = (l.len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows;
+      l.parts = chunks > 1 ? chunks : 0u;
+      l.item0 = item + scan_add(tmp, tid, chunks * (uint32_t)a.n_sub, &sum_items);
+      l.part0 = part + scan_add(tmp, tid, l.parts, &sum_parts);
+    }
     first += sum_len;
     tile += sum_tiles;
-    if (j < nb) {
-      totals[j] = f;
-      BlockItem* it = a.items + (int64_t)plane * a.item_cap + t;
-      for (uint32_t i = 0; i < tiles; ++i) {
-        const uint32_t left = len - i * kBlockTileRows;
-        it[i] = {a.first_block + j, (int)(f + i * kBlockTileRows), (int)(left < kBlockTileRows ? left : kBlockTileRows), 0};
-      }
-    }
-    if (dkdv) {
-      const uint32_t rows = (uint32_t)a.chunk_rows, chunks = (len + rows - 1) / rows, parts = chunks > 1 ? chunks : 0u;
-      uint32_t sum_items, sum_parts;
-      const uint32_t i0 = item + scan_add(tmp, tid, chunks * (uint32_t)a.n_sub, &sum_items);
-      const uint32_t p0 = part + scan_add(tmp, tid, parts, &sum_parts);
-      item += sum_items;
-      part += sum_parts;
-      if (j < nb) {
-        a.sums[(int64_t)plane * nb + j] = {(int)len, (int)parts, (int)p0, 0};
-        BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + i0;
-        for (uint32_t c = 0; c < chunks; ++c)
-          for (int s = 0; s < a.n_sub; ++s) {
-            const uint32_t left = len - c * rows;
-            *it++ = {(a.first_block + j) * a.n_sub + s, (int)(f + c * rows), (int)(left < rows ? left : rows), parts ? (int)(p0 + c) : -1};
-          }
-      }
-    }
+    item += sum_items;
+    part += sum_parts;
+    if (j < nb) lists[j] = l;
   }
   if (tid == 0) {
     a.n_items[plane] = (int)tile;
@@ -401,24 +727,21 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   }
 }
 
-static size_t list_lds_bytes(const BlockArgs& a) {
-  return (size_t)(a.n_blocks < kListBlocks ? a.n_blocks : kListBlocks) * (kListRows / 32) * 4;
-}
+static size_t list_lds_bytes(const BlockArgs& a) { return ((size_t)list_lds_words(a.n_blocks) + (size_t)kListRows * a.top_k) * 4; }
 hipError_t launch_block_lists(const BlockArgs& a, bool dkdv, hipStream_t st) {
-  const int planes = a.batch * a.n_kv_heads;
-  dim3 grid((unsigned)a.n_list_chunks, (unsigned)planes);
-  hipLaunchKernelGGL(block_list_kernel<false>, grid, dim3(kListRows), list_lds_bytes(a), st, a);
-  hipLaunchKernelGGL(block_scan_kernel, dim3((unsigned)planes), dim3(kScanThreads), 0, st, a, dkdv ? 1 : 0);
-  hipLaunchKernelGGL(block_list_kernel<true>, grid, dim3(kListRows), list_lds_bytes(a), st, a);
+  const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
+  const int64_t slots = (int64_t)a.group * a.s_q * a.top_k;
+  hipLaunchKernelGGL(block_rank_kernel, dim3((unsigned)a.n_list_chunks, planes), dim3(kListThreads), list_lds_bytes(a), st, a);
+  hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, dkdv ? 1 : 0);
+  hipLaunchKernelGGL(block_fill_kernel, dim3((unsigned)((slots + 255) / 256), planes), dim3(256), 0, st, a, dkdv ? 1 : 0);
   return hipGetLastError();
 }
 
 hipError_t opt_in_block_select_kernels() {
-  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
-  const int most = kListBlocks * (kListRows / 32) * 4;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_list_kernel<false>), attr, most);
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_list_kernel<true>), attr, most);
-  return e;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_rank_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     (list_lds_words(kListBlocks) + kListRows * kMaxTopK) * 4);
+  if (e == hipSuccess) e = opt_in_select_d<128>();
+  return e == hipSuccess ? opt_in_select_d<64>() : e;
 }
 
 }  // namespace slimpipe

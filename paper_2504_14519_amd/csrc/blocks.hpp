@@ -11,8 +11,8 @@ namespace slimpipe {
 
 constexpr int kMaxTopK = 64;
 // rows of a plane that one workgroup of the list kernels handles, and blocks it handles at a time (a bit per row and block in LDS)
-constexpr int kListRows = 512;
-constexpr int kListBlocks = 2048;
+constexpr int kListRows = 256;
+constexpr int kListBlocks = 1024;
 constexpr int kBlockTileRows = 128;      // rows of a tile of the forward and dq kernels
 
 // One row of a list: row of the slice and (head within the group << 6 | slot).
@@ -20,6 +20,10 @@ struct BlockEntry { uint32_t row, head_slot; };
 // A tile of a list: block (absolute index), first entry within the plane's list, entries; the dk/dv items also have the part of the
 // block's keys (in units of its workgroup's keys) and the plane's partial-sum slot, or -1 when the sums go straight to the accumulators
 struct BlockItem { int32_t block, first, count, part; };
+
+// The list of a block: first entry within the plane's, length, first tile, first dk/dv item; how many partial dk/dv sums it leaves (0: one
+// workgroup has all of it, or nobody) and the first of them
+struct BlockList { uint32_t first, len, tile0, item0, parts, part0, unused[2]; };
 
 struct BlockArgs {
   const __bf16* q;
@@ -36,8 +40,9 @@ struct BlockArgs {
   int64_t do_stride_b, do_stride_s, do_stride_h;
   // lists (workspace), plane by plane
   int32_t n_list_chunks;         // ceil(group * s_q / kListRows)
-  uint32_t* counts;              // [plane][chunk][n_blocks]: rows of the chunk that chose the block, then where they start in its list
-  uint32_t* start;               // [plane][n_blocks]: where the block's list starts
+  uint16_t* ranks;               // [plane][group * s_q * top_k]: place of a slot's row among the rows of its chunk that chose the block
+  uint32_t* counts;              // [plane][n_blocks][chunk]: rows of the chunk that chose the block, then where they start in its list
+  BlockList* lists;              // [plane][n_blocks]
   BlockEntry* entries;           // [plane][group * s_q * top_k]
   BlockItem* items;              // [plane][item_cap]
   int32_t* n_items;              // [plane]
@@ -61,7 +66,6 @@ struct BlockArgs {
   BlockItem* dkdv_items;         // [plane][dkdv_cap]
   int32_t* n_dkdv_items;         // [plane]
   int32_t dkdv_cap;
-  BlockItem* sums;               // [plane][n_blocks]: {list length, partial sums, first partial-sum slot, -}
   float* dkdv_part;              // [plane][part_cap][2][sub * sub keys][head_dim]
   int32_t part_cap;
   int64_t kv_end_range;          // end of the call's key range (rows behind the last seen key get gradients of 0)
@@ -95,7 +99,7 @@ struct BlockSelectArgs {
 };
 
 hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t st);
-hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, hipStream_t st);
+hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, int compute_units, hipStream_t st);
 // lists and tiles of the call's index; with `dkdv` the dk/dv items too
 hipError_t launch_block_lists(const BlockArgs& a, bool dkdv, hipStream_t st);
 hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st);
