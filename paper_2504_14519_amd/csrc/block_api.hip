@@ -183,7 +183,9 @@ int slimpipe_attn_block_select(const slimpipe_attn_params* p, const void* q_slic
   a.first_block = (int32_t)(p->kv_begin / block_len);
   a.n_blocks = (int32_t)blocks_of(p->kv_begin, p->kv_end, block_len);
   a.blocks_total = blocks_of(0, p->kv_capacity, block_len);
-  a.q_offset = p->q_offset;
+  const int64_t own0 = p->q_offset / block_len;
+  a.own0 = (int32_t)(own0 < (int64_t)1 << 30 ? own0 : (int64_t)1 << 30);      // (behind every block of a cache, see check_blocks)
+  a.own_rest = (int32_t)(p->q_offset % block_len);
   a.q_stride_b = p->q_stride_b; a.q_stride_s = p->q_stride_s; a.q_stride_h = p->q_stride_h;
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   return status(launch_block_select(a, p->head_dim, compute_units(), static_cast<hipStream_t>(hip_stream)));

@@ -73,7 +73,8 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 
 // Places that a row's list of candidates has (what is certain and what is not): with more, which only many equal scores can bring, the row
 // is done in 64 bits throughout.
-constexpr int select_places(int k) { return k <= 16 ? 32 : kMaxTopK + 32; }
+// (few enough of them that the LDS of two workgroups fits a compute unit)
+constexpr int select_places(int k) { return k <= 8 ? 16 : k <= 16 ? 28 : kMaxTopK + 32; }
 constexpr uint32_t kUnsure = 0x80000000u;      // flag of a candidate within 2 delta of T
 
 // A tile of 32 blocks of means as three bf16 parts (largest first): upper halves of floats, rounded towards zero, so that what is left is exact.
@@ -118,6 +119,17 @@ SP_DEV void merge_largest(float (&t)[K], const float (&o)[K]) {
         t[i] = big;
       }
 }
+// The K largest of both halves' lists of a row.
+template <int K>
+SP_DEV void merge_halves(float (&t)[K], int g) {
+  float other[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[i]), __float_as_uint(t[i]), false, false);
+    other[i] = __uint_as_float(g ? r[0] : r[1]);
+  }
+  merge_largest<K>(t, other);
+}
 template <int K>
 SP_DEV float place_of(const float (&t)[K], int n) {      // t[n - 1]
   float v = -INFINITY;
@@ -132,9 +144,9 @@ SP_DEV SelRow select_row_of(const BlockSelectArgs& a, int rh) {
   const int end = a.first_block + a.n_blocks;
   SelRow r = {end, a.top_k, -1};
   if (a.causal) {
-    const int64_t own = (a.q_offset + rh % a.s_q) / a.block_len;
-    if (own < end) r.own = (int)own;
-    if (own >= a.first_block && own < end) { r.forced = (int)own; --r.need; }
+    const int own = a.own0 + (int)((unsigned)(a.own_rest + rh % a.s_q) / (unsigned)a.block_len);
+    if (own < end) r.own = own;
+    if (own >= a.first_block && own < end) { r.forced = own; --r.need; }
   }
   if (r.need <= 0 || r.own < a.first_block) r.own = a.first_block;
   return r;
@@ -267,38 +279,47 @@ SP_DEV void settle_row(uint32_t* list, int count, int places, int need, const bf
   __builtin_amdgcn_wave_barrier();
 }
 
-// Many rows: 128 a workgroup, 32 a wave; means are split once for all of them, into two LDS slots.
+// Many rows: 32 R rows a wave, four waves; means are split once for all of them, into two LDS slots, and a matrix operand that is read
+// from there serves R rows sets (R = 2 where the lists are short: the LDS reads of R = 1 are half of a tile's time).
+constexpr int select_sets(int k) { return k <= 16 ? 2 : 1; }
 template <int D, int K>
-constexpr size_t select_lds_bytes() { return (size_t)2 * 3 * 32 * D * 2 + (size_t)128 * select_places(K) * 4; }
+constexpr size_t select_lds_bytes() { return (size_t)2 * 3 * 32 * D * 2 + (size_t)128 * select_sets(K) * select_places(K) * 4; }
 template <int D, int K>
 __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectArgs a) {
   constexpr int KS = D / 16, PART = 32 * D * 2, SLOT = 3 * PART, PLACES = select_places(K), PER = D / 8 / 8;      // 16-byte chunks of a part a thread writes
+  constexpr int R = select_sets(K), WROWS = 32 * R;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ uint32_t most_s;                        // largest |mean|^2 (bits of a float; all are >= 0)
   __shared__ int last_s;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int hk = blockIdx.y, b = blockIdx.z, rows = a.group * a.s_q, row0 = blockIdx.x * 128 + wave * 32;
+  const int hk = blockIdx.y, b = blockIdx.z, rows = a.group * a.s_q, row0 = blockIdx.x * 4 * WROWS + wave * WROWS;
   const float* const means = a.means + ((int64_t)b * a.n_kv_heads + hk) * a.blocks_total * D;
-  const int rh = row0 + ql < rows ? row0 + ql : rows - 1;
-  const SelRow want = select_row_of(a, rh);
   if (tid == 0) { most_s = 0u; last_s = a.first_block; }
-  bf16x8 q[KS];
-  float norm = 0.f;
-  {
+  SelRow want[R];
+  bf16x8 q[R][KS];
+  float norm[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int rh = row0 + 32 * r + ql < rows ? row0 + 32 * r + ql : rows - 1;
+    want[r] = select_row_of(a, rh);
     const bf16_t* p = select_q(a, b, hk, rh) + 8 * g;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      q[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
-    }
-    norm = __builtin_sqrtf(xhalf_sum(norm));
+    for (int ks = 0; ks < KS; ++ks) q[r][ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
   }
   __syncthreads();
-  atomicMax(&last_s, want.own);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    norm[r] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) norm[r] += (float)q[r][ks][e] * (float)q[r][ks][e];
+    norm[r] = __builtin_sqrtf(xhalf_sum(norm[r]));
+    atomicMax(&last_s, want[r].own);
+  }
   __syncthreads();
   const int stop = __builtin_amdgcn_readfirstlane(last_s), nt = (stop - a.first_block + 31) / 32;
-  uint32_t* const list = reinterpret_cast<uint32_t*>(smem + 2 * SLOT) + (wave * 32 + ql) * PLACES;
+  uint32_t* const wave_lists = reinterpret_cast<uint32_t*>(smem + 2 * SLOT) + wave * WROWS * PLACES;
 
   f32x4 x[2 * PER];
   float most = 0.f;
@@ -330,11 +351,15 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
     __syncthreads();
     for (int t = 0; t < nt; ++t) {
       if (t + 1 < nt) fetch(t + 1);
-      f32x16 s = {0};
+      f32x16 s[R] = {};
 #pragma unroll
       for (int p = 2; p >= 0; --p)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma32(lds_rp<D>(lo_m, ks, p * PART), q[ks], s);
+        for (int ks = 0; ks < KS; ++ks) {
+          const bf16x8 m = lds_rp<D>(lo_m, ks, p * PART);
+#pragma unroll
+          for (int r = 0; r < R; ++r) s[r] = mfma32(m, q[r][ks], s[r]);
+        }
       use(t, s);
       lo_m.add((t & 1) ? -SLOT : SLOT);
       if (t + 1 < nt) store(t + 1);
@@ -342,70 +367,82 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
     }
     if (nt & 1) lo_m.add(-SLOT);
   };
-  int count = 0, sure = 0;
+  int count[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) count[r] = 0;
   if (nt > 0) {
-    float top[K];
+    float top[R][K];
 #pragma unroll
-    for (int i = 0; i < K; ++i) top[i] = -INFINITY;
-    walk([&](int t, f32x16& s) {
-      const int left = want.own - a.first_block - t * 32;      // blocks of the tile that compete for the row
-      if (__builtin_amdgcn_ballot_w64(left < 32) != 0)
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < left - 4 * g ? s[i] : -INFINITY;
+      for (int i = 0; i < K; ++i) top[r][i] = -INFINITY;
+    walk([&](int t, f32x16 (&s)[R]) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) keep_largest<K>(top, s[i]);
+      for (int r = 0; r < R; ++r) {
+        const int left = want[r].own - a.first_block - t * 32;      // blocks of the tile that compete for the row
+        if (__builtin_amdgcn_ballot_w64(left < 32) != 0)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[r][i] = 8 * (i >> 2) + (i & 3) < left - 4 * g ? s[r][i] : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) keep_largest<K>(top[r], s[r][i]);
+      }
     });
     atomicMax(&most_s, __float_as_uint(most));
-    float other[K];
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[i]), __float_as_uint(top[i]), false, false);
-      other[i] = __uint_as_float(g ? r[0] : r[1]);
-    }
-    merge_largest<K>(top, other);
     __syncthreads();
-    float lo, hi;
-    select_bounds(place_of<K>(top, want.need), 1.125f * D * 0x1p-23f * norm * __builtin_sqrtf(__uint_as_float(most_s)), &lo, &hi);
-    if (want.own - a.first_block <= want.need) { lo = -INFINITY; hi = INFINITY; }      // no more than are wanted: all
-    walk([&](int t, f32x16& s) {
-      const int left = want.own - a.first_block - t * 32;
-      const uint32_t in = blocks_below(left), open = both_halves(at_least(s, lo, g)) & in, certain = both_halves(above(s, hi, g));
-      sure += __popc(certain & in);
-      if (g == 0)
-        for (uint32_t m = open; m; m &= m - 1) {
-          const int n = __ffs(m) - 1;
-          if (count < PLACES) list[count] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
-          ++count;
-        }
+    float lo[R], hi[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      merge_halves<K>(top[r], g);
+      select_bounds(place_of<K>(top[r], want[r].need), 1.125f * D * 0x1p-23f * norm[r] * __builtin_sqrtf(__uint_as_float(most_s)), &lo[r], &hi[r]);
+      if (want[r].own - a.first_block <= want[r].need) { lo[r] = -INFINITY; hi[r] = INFINITY; }      // no more than are wanted: all
+    }
+    walk([&](int t, f32x16 (&s)[R]) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const uint32_t open = both_halves(at_least(s[r], lo[r], g)) & blocks_below(want[r].own - a.first_block - t * 32);
+        const uint32_t certain = both_halves(above(s[r], hi[r], g));
+        if (g == 0)
+          for (uint32_t m = open; m; m &= m - 1) {
+            const int n = __ffs(m) - 1;
+            if (count[r] < PLACES) wave_lists[(32 * r + ql) * PLACES + count[r]] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
+            ++count[r];
+          }
+      }
     });
   }
-  // rows with more candidates than places
-  for (uint64_t m = __builtin_amdgcn_ballot_w64(g == 0 && count > want.need && row0 + ql < rows); m; m &= m - 1) {
-    const int from = __ffsll((unsigned long long)m) - 1;
-    const int n = __builtin_amdgcn_readlane(count, from), need = __builtin_amdgcn_readlane(want.need, from), own = __builtin_amdgcn_readlane(want.own, from);
-    settle_row<D>(reinterpret_cast<uint32_t*>(smem + 2 * SLOT) + (wave * 32 + from) * PLACES, n, PLACES, need, select_q(a, b, hk, row0 + from), means,
-                  a.first_block, own, lane);
-  }
-  count = count < want.need ? count : want.need;
-  // the wave's rows of the index, whole lines at a time
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  const int n_rows = rows - row0 < 32 ? rows - row0 : 32;
-  int32_t* const to = a.index + (((int64_t)b * a.n_kv_heads + hk) * rows + row0) * a.top_k;
-  for (int i0 = 0; i0 < n_rows * a.top_k; i0 += 64) {
-    const int i = i0 + lane, r = i / a.top_k, slot = i - r * a.top_k, rr = r < 32 ? r : 31;
-    const int n = __shfl(count, rr, 64), f = __shfl(want.forced, rr, 64);
-    const uint32_t v = reinterpret_cast<const uint32_t*>(smem + 2 * SLOT)[(wave * 32 + rr) * PLACES + (slot < PLACES ? slot : 0)];
-    if (i < n_rows * a.top_k) to[i] = slot < n ? (int)(v & ~kUnsure) : slot == n && f >= 0 ? f : -1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int first = row0 + 32 * r;
+    uint32_t* const lists = wave_lists + 32 * r * PLACES;
+    // rows with more candidates than places
+    for (uint64_t m = __builtin_amdgcn_ballot_w64(g == 0 && count[r] > want[r].need && first + ql < rows); m; m &= m - 1) {
+      const int from = __ffsll((unsigned long long)m) - 1;
+      const int n = __builtin_amdgcn_readlane(count[r], from), need = __builtin_amdgcn_readlane(want[r].need, from), own = __builtin_amdgcn_readlane(want[r].own, from);
+      settle_row<D>(lists + from * PLACES, n, PLACES, need, select_q(a, b, hk, first + from), means, a.first_block, own, lane);
+    }
+    const int have = count[r] < want[r].need ? count[r] : want[r].need;
+    // the rows of the index, whole lines at a time
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int n_rows = rows - first < 32 ? rows - first : 32;
+    int32_t* const to = a.index + (((int64_t)b * a.n_kv_heads + hk) * rows + first) * a.top_k;
+    for (int i0 = 0; i0 < n_rows * a.top_k; i0 += 64) {
+      const int i = i0 + lane, row = i / a.top_k, slot = i - row * a.top_k, rr = row < 32 ? row : 31;
+      const int n = __shfl(have, rr, 64), f = __shfl(want[r].forced, rr, 64);
+      const uint32_t v = lists[rr * PLACES + (slot < PLACES ? slot : 0)];
+      if (i < n_rows * a.top_k) to[i] = slot < n ? (int)(v & ~kUnsure) : slot == n && f >= 0 ? f : -1;
+    }
   }
 }
 
 // Few rows (tokens): 32 a workgroup, whose eight waves share out the tiles; means go from memory through registers to the matrix unit.  The waves'
 // lists meet in LDS, and so do the second walk's masks, a bit a block.
-constexpr int kFewWaves = 8, kFewTiles = 512;
+constexpr int kFewWaves = 8, kFewTiles = 512, kFewKept = 2;      // tiles of a wave whose scores stay in registers for the second walk
+template <int K>
+constexpr int few_list_stride() { return K * 32 + 8; }              // floats of a wave's lists (eight banks on, so that a row's lists are spread)
 template <int D, int K>
 constexpr size_t select_few_lds_bytes(int tiles) {
-  const size_t lists = (size_t)kFewWaves * 2 * 32 * (K + 1) * 4, masks = (size_t)tiles * 32 * 2 * 4 + 32 * select_places(K) * 4;
+  const size_t lists = (size_t)kFewWaves * few_list_stride<K>() * 4, masks = (size_t)tiles * 32 * 2 * 4 + 32 * select_places(K) * 4;
   return lists > masks ? lists : masks;
 }
 template <int D, int K>
@@ -420,21 +457,14 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   const int hk = blockIdx.y, b = blockIdx.z, rows = a.group * a.s_q, row0 = blockIdx.x * 32;
   const float* const means = a.means + ((int64_t)b * a.n_kv_heads + hk) * a.blocks_total * D;
   const int rh = row0 + ql < rows ? row0 + ql : rows - 1;
-  const SelRow want = select_row_of(a, rh);
   if (tid == 0) { most_s = 0u; last_s = a.first_block; }
   bf16x8 q[KS];
   {
-    float norm = 0.f;
     const bf16_t* p = select_q(a, b, hk, rh) + 8 * g;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      q[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
-    }
-    norm = __builtin_sqrtf(xhalf_sum(norm));
-    if (tid < 32) norm_s[tid] = norm;
+    for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(p + 16 * ks);
   }
+  const SelRow want = select_row_of(a, rh);
   __syncthreads();
   if (tid < 32) atomicMax(&last_s, want.own);
   __syncthreads();
@@ -460,32 +490,49 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   float top[K];
 #pragma unroll
   for (int i = 0; i < K; ++i) top[i] = -INFINITY;
-  for (int t = wave; t < nt; t += kFewWaves) {
-    f32x16 s = scores(t);
+  auto offer = [&](const f32x16& s, int t) {
     const int left = want.own - a.first_block - t * 32 - 4 * g;
 #pragma unroll
     for (int i = 0; i < 16; ++i) keep_largest<K>(top, 8 * (i >> 2) + (i & 3) < left ? s[i] : -INFINITY);
+  };
+  f32x16 kept[kFewKept] = {};
+#pragma unroll
+  for (int i = 0; i < kFewKept; ++i) {
+    const int t = wave + i * kFewWaves;
+    if (t < nt) { kept[i] = scores(t); offer(kept[i], t); }
+  }
+  for (int t = wave + kFewKept * kFewWaves; t < nt; t += kFewWaves) offer(scores(t), t);
+  {
+    float norm = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
+    norm = __builtin_sqrtf(xhalf_sum(norm));
+    if (tid < 32) norm_s[tid] = norm;
   }
   atomicMax(&most_s, __float_as_uint(most));
-  float* const lists = reinterpret_cast<float*>(smem);      // [row][wave, half][K + 1]
+  merge_halves<K>(top, g);
+  float* const lists = reinterpret_cast<float*>(smem);      // [wave][place][row]
+  if (g == 0)
 #pragma unroll
-  for (int i = 0; i < K; ++i) lists[((ql * kFewWaves + wave) * 2 + g) * (K + 1) + i] = top[i];
+    for (int i = 0; i < K; ++i) lists[wave * few_list_stride<K>() + i * 32 + ql] = top[i];
   __syncthreads();
   {
-    // sixteen lists a row, a lane each
-    static_assert(kFewWaves * 2 == 16 && kFewWaves * 4 == 32, "four rows a wave");
-    const int r = wave * 4 + lane / 16;
+    // eight lists a row, a lane each, four rows a wave (lanes 32 .. 63 do the same)
+    static_assert(kFewWaves == 8 && kFewWaves * 4 == 32, "four rows a wave");
+    const int r = wave * 4 + ql / 8;
 #pragma unroll
-    for (int i = 0; i < K; ++i) top[i] = lists[(r * 16 + lane % 16) * (K + 1) + i];
+    for (int i = 0; i < K; ++i) top[i] = lists[ql % 8 * few_list_stride<K>() + i * 32 + r];
 #pragma unroll
-    for (int w = 1; w < 16; w <<= 1) {
+    for (int w = 1; w < 8; w <<= 1) {
       float other[K];
 #pragma unroll
       for (int i = 0; i < K; ++i) other[i] = __shfl_xor(top[i], w, 64);
       merge_largest<K>(top, other);
     }
     const float v = place_of<K>(top, __shfl(want.need, r, 64));
-    if (lane % 16 == 0) border_s[r] = v;
+    if (lane < 32 && lane % 8 == 0) border_s[r] = v;
   }
   __syncthreads();
   float lo, hi;
@@ -493,24 +540,38 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   if (want.own - a.first_block <= want.need) { lo = -INFINITY; hi = INFINITY; }
   uint32_t* const open_s = reinterpret_cast<uint32_t*>(smem);      // [tile][row]; certain ones behind them, then the rows' lists
   uint32_t* const certain_s = open_s + nt * 32;
-  for (int t = wave; t < nt; t += kFewWaves) {
-    const f32x16 s = scores(t);
+  auto mark = [&](const f32x16& s, int t) {
     const uint32_t in = blocks_below(want.own - a.first_block - t * 32), open = both_halves(at_least(s, lo, g)) & in, certain = both_halves(above(s, hi, g)) & in;
     if (g == 0) { open_s[t * 32 + ql] = open; certain_s[t * 32 + ql] = certain; }
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kFewKept; ++i)
+    if (wave + i * kFewWaves < nt) mark(kept[i], wave + i * kFewWaves);
+  for (int t = wave + kFewKept * kFewWaves; t < nt; t += kFewWaves) mark(scores(t), t);
   __syncthreads();
   uint32_t* const cand = certain_s + nt * 32;
-  if (tid < 32) {
+  {
+    // sixteen tiles of a row at a time, a lane each
+    const int r = wave * 4 + lane / 16;
     int count = 0;
-    for (int t = 0; t < nt; ++t) {
-      const uint32_t certain = certain_s[t * 32 + tid];
-      for (uint32_t m = open_s[t * 32 + tid]; m; m &= m - 1) {
-        const int n = __ffs(m) - 1;
-        if (count < PLACES) cand[tid * PLACES + count] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
-        ++count;
+    for (int t0 = 0; t0 < nt; t0 += 16) {
+      const int t = t0 + lane % 16;
+      const uint32_t open = t < nt ? open_s[t * 32 + r] : 0u, certain = t < nt ? certain_s[t * 32 + r] : 0u;
+      int at = __popc(open);
+#pragma unroll
+      for (int w = 1; w < 16; w <<= 1) {
+        const int o = __shfl_up(at, w, 16);
+        if (lane % 16 >= w) at += o;
       }
+      const int all = __shfl(at, 15, 16);
+      at += count - __popc(open);
+      for (uint32_t m = open; m; m &= m - 1, ++at) {
+        const int n = __ffs(m) - 1;
+        if (at < PLACES) cand[r * PLACES + at] = (uint32_t)(a.first_block + t * 32 + n) | ((certain >> n) & 1u ? 0u : kUnsure);
+      }
+      count += all;
     }
-    count_s[tid] = count;
+    if (lane % 16 == 0) count_s[r] = count;
   }
   __syncthreads();
   for (int r = wave; r < 32 && row0 + r < rows; r += kFewWaves) {
@@ -529,7 +590,8 @@ static hipError_t launch_select_t(const BlockSelectArgs& a, bool few, hipStream_
   const unsigned heads = (unsigned)a.n_kv_heads, batch = (unsigned)a.batch;
   if (few) hipLaunchKernelGGL((block_select_few_kernel<D, K>), dim3((unsigned)((rows + 31) / 32), heads, batch), dim3(kFewWaves * 64),
                               (select_few_lds_bytes<D, K>((a.n_blocks + 31) / 32)), st, a);
-  else hipLaunchKernelGGL((block_select_kernel<D, K>), dim3((unsigned)((rows + 127) / 128), heads, batch), dim3(256), (select_lds_bytes<D, K>()), st, a);
+  else hipLaunchKernelGGL((block_select_kernel<D, K>), dim3((unsigned)((rows + 128 * select_sets(K) - 1) / (128 * select_sets(K))), heads, batch),
+                          dim3(256), (select_lds_bytes<D, K>()), st, a);
   return hipGetLastError();
 }
 template <int D>

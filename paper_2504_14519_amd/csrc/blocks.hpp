@@ -94,7 +94,8 @@ struct BlockSelectArgs {
   const float* means;
   int32_t* index;
   int32_t batch, s_q, n_q_heads, n_kv_heads, group, causal, top_k, block_len, first_block, n_blocks;
-  int64_t blocks_total, q_offset;
+  int64_t blocks_total;
+  int32_t own0, own_rest;        // causal: block of position q_offset (clamped to 2^30), and where in it that lies
   int64_t q_stride_b, q_stride_s, q_stride_h;
 };
 
