@@ -27,7 +27,7 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int tile = tile_of(blockIdx.x, a.n_items[plane]);
+  const int tile = xcd_run(blockIdx.x, a.n_items[plane]);
   if (tile < 0) return;
   const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
   const int n_rows = it.count;
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int item = tile_of(blockIdx.x, a.n_dkdv_items[plane]);
+  const int item = xcd_run(blockIdx.x, a.n_dkdv_items[plane]);
   if (item < 0) return;
   const BlockItem it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
   const int block = it.block / a.n_sub, sub = it.block - block * a.n_sub, n_rows = it.count;

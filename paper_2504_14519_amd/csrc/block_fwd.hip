@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int tile = tile_of(blockIdx.x, a.n_items[plane]);
+  const int tile = xcd_run(blockIdx.x, a.n_items[plane]);
   if (tile < 0) return;
   const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
   const int n_rows = it.count;

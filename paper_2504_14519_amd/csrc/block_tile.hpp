@@ -5,12 +5,6 @@
 
 namespace slimpipe {
 
-// Workgroup index -> tile: the tiles of an XCD (index mod 8) follow each other, so that those of one block share an L2.
-SP_DEV int tile_of(int index, int n) {
-  const int per = (n + 7) / 8, t = (index & 7) * per + (index >> 3);
-  return (index >> 3) < per && t < n ? t : -1;
-}
-
 // The keys of a block that exist, and where the first of them lies.
 struct BlockKeys {
   int64_t lo, hi;

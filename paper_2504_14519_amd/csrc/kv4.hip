@@ -216,138 +216,197 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   }
 }
 
-// Tokens: at most 32 rows of a plane (its query heads and a few tokens), all in every wave; the four waves of a workgroup share out the
-// 32-key tiles of its keys.  K goes from memory to the matrix unit without LDS: a lane's operand is 8 elements of its key in each step, and
-// since the contraction may take head_dim in any order, half-wave g takes elements D/2 g .. in order: 16 codes bytes after 16.  V
-// passes through 32 rows of LDS of the wave's own for the transposed read.
-template <int D>
-constexpr size_t kv4_few_lds_bytes(int rows) {
-  const size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * rows * kOutRow<D> * 4 + 4 * 2 * 32 * 4;
+// Tokens: at most 16 SETS rows of a plane (its query heads and a few tokens), all in every wave; the four waves of a workgroup share out the
+// 32-key steps of its keys.  v_mfma_f32_16x16x32_bf16: with lane = 16 h + r an operand's lane holds row or column r, contraction slots
+// 8 h .. 8 h + 7, a result's column r, register i row 4 h + i.
+//   S^T = K Q^T      K goes from memory to the matrix unit without LDS: since the contraction may take head_dim in any order, lane group h
+//                    takes the h-th quarter of a row, 8 elements a step, and a lane's codes of 16 keys are one load
+//   O^T += V^T P^T   V passes through 32 rows of LDS of the wave's own for the transposed read (lane group h: keys 4 h .. 4 h + 3 of either 16)
+// Codes of the next two steps are under way in registers.  Bound by the bytes of the cache.
+// Workgroups: the key ranges of all heads of a sequence that cover the same keys go to one XCD one after the other, because a
+// row's codes are 64 bytes and its scales 4, of lines of 128 that hold the next heads' too.
+template <int D, int SETS>
+constexpr size_t kv4_few_lds_bytes() {
+  constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * kOutRow<D> * 4 + 4 * 2 * 16 * SETS * 4;
   return tiles > out ? tiles : out;
 }
-template <int D>
+SP_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+SP_DEV float quarters_max(float v) {      // over the four lane groups
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return xhalf_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+SP_DEV float quarters_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+template <int D, int SETS>
 __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
-  constexpr int KS = D / 16, DB = D / 32, W = D / 64, HALF = D / 2;      // W: 16-byte words of codes of half a row
+  constexpr int W = D / 32, DB = D / 16, QUARTER = D / 4;      // dwords of codes of a quarter row (= matrix steps), output blocks
+  typedef uint32_t codes_t __attribute__((ext_vector_type(W)));
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = a.group * a.s_q;
-  const int part_i = blockIdx.x, plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const Kv4Row my = kv4_row(a, hk, ql < rows ? ql : rows - 1);
+  const int tid = threadIdx.x, lane = tid & 63, h4 = lane >> 4, ql = lane & 15, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = a.group * a.s_q, planes = a.batch * a.n_kv_heads;
+  int part_i = 0, plane = blockIdx.x;
+  if (a.n_parts > 1) {
+    const int per = 8 * planes, first = (int)blockIdx.x / per * 8, i = (int)blockIdx.x % per, n = a.n_parts - first < 8 ? a.n_parts - first : 8;
+    part_i = first + i % n;
+    plane = i / n;
+  } else {
+    plane = xcd_run(blockIdx.x, planes);
+  }
+  if (plane < 0 || plane >= planes) return;
+  const int b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
   const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
   const int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
   const int n_keys = hi > lo ? (int)(hi - lo) : 0, nt = (n_keys + 31) / 32;
-  const int64_t see = a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1;
-  const int64_t see_far = see - lo;
-  const int see_rel = see_far < -1 ? -1 : (int)see_far;
-  const unsigned tile = lds_addr(smem) + wave_u * 32 * D * 2;
   char* const tile_p = smem + wave_u * 32 * D * 2;
 
-  RowState<D> st;
-  st.init();
-  {
-    const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + HALF * g;
+  bf16x8 q[SETS][W];
+  f32x4 o[SETS][DB];
+  float m[SETS], l[SETS];
+  int see_rel[SETS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) st.q[ks] = *reinterpret_cast<const bf16x8*>(qp + 8 * ks);
+  for (int r = 0; r < SETS; ++r) {
+    const int rh = 16 * r + ql;
+    const Kv4Row my = kv4_row(a, hk, rh < rows ? rh : rows - 1);
+    const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + QUARTER * h4;
+#pragma unroll
+    for (int j = 0; j < W; ++j) q[r][j] = *reinterpret_cast<const bf16x8*>(qp + 8 * j);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[r][db] = f32x4{0, 0, 0, 0};
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+    const int64_t see = (a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1) - lo;
+    see_rel[r] = see < -1 ? -1 : (int)see;
   }
-  TrOffsets<D> lo_v;
-  lo_v.init(lane, (int)tile);
-  // K: lane = (key ql, half g).  V: the same half row, written to LDS.
-  const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s + HALF * g;
-  u32x4 kc[W], vc[W];
-  uint32_t ks_[W], vs_[W];                       // scale of each 32 elements
-  auto fetch = [&](int t) {
-    const int k = t * 32 + ql < n_keys ? t * 32 + ql : n_keys - 1;
-    const int64_t at = base + (int64_t)k * a.kv_stride_s;
+  int min_see = see_rel[0];                      // keys up to here: every row of the lane sees them
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      kc[w] = *reinterpret_cast<const u32x4*>(a.k.codes + at / 2 + 16 * w);
-      vc[w] = *reinterpret_cast<const u32x4*>(a.v.codes + at / 2 + 16 * w);
-      ks_[w] = a.k.scales[at / 32 + w];
-      vs_[w] = a.v.scales[at / 32 + w];
+  for (int r = 1; r < SETS; ++r) min_see = min_see < see_rel[r] ? min_see : see_rel[r];
+
+  // LDS addresses: where this lane writes its quarter of a key's row (of 16 keys), and where it reads
+  int to[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) to[j] = tile_off<D>(ql, h4 * W + j);
+  const int from = (int)lds_addr(smem) + wave_u * 32 * D * 2 + tile_off<D>(4 * h4 + ql / 4, (ql & 3) >> 1) + ((ql & 1) << 3);
+
+  const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s + QUARTER * h4;
+  struct Step { codes_t k[2], v[2]; uint32_t ks[2], vs[2]; };
+  auto fetch = [&](Step& s, int t) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int key = t * 32 + 16 * u + ql, kc = key < n_keys ? key : n_keys - 1;      // (keys behind the last are not read)
+      const int64_t at = base + (int64_t)kc * a.kv_stride_s;
+      s.k[u] = *reinterpret_cast<const codes_t*>(a.k.codes + at / 2);
+      s.v[u] = *reinterpret_cast<const codes_t*>(a.v.codes + at / 2);
+      s.ks[u] = a.k.scales[at / 32];
+      s.vs[u] = a.v.scales[at / 32];
     }
   };
-  if (wave_u < nt) fetch(wave_u);
-  for (int t = wave_u; t < nt; t += 4) {
-    f32x16 s = {0};
+  auto work = [&](Step& st, int t, int next) {
+    f32x4 s[SETS][2];
 #pragma unroll
-    for (int w = 0; w < W; ++w)
+    for (int u = 0; u < 2; ++u) {
+      const float ks = kv4_scale(st.ks[u]), vs = kv4_scale(st.vs[u]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s = mfma32(kv4_values(kc[w][j], kv4_scale(ks_[w])), st.q[4 * w + j], s);
+      for (int r = 0; r < SETS; ++r) s[r][u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < W; ++w)
+      for (int j = 0; j < W; ++j) {
+        const bf16x8 k8 = kv4_values(st.k[u][j], ks);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<bf16x8*>(tile_p + tile_off<D>(ql, g * (D / 16) + 4 * w + j)) = kv4_values(vc[w][j], kv4_scale(vs_[w]));
-    if (t + 4 < nt) fetch(t + 4);
-    const int kmax = see_rel - t * 32;
-    if (__builtin_amdgcn_ballot_w64(kmax < 31) != 0) {
-      const int top = kmax - 4 * g;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) <= top ? s[i] : -INFINITY;
+        for (int r = 0; r < SETS; ++r) s[r][u] = mfma16(k8, q[r][j], s[r][u]);
+        *reinterpret_cast<bf16x8*>(tile_p + 16 * u * D * 2 + to[j]) = kv4_values(st.v[u][j], vs);
+      }
     }
-    float mx = -INFINITY;
+    if (next < nt) fetch(st, next);
+    if (__builtin_amdgcn_ballot_w64(min_see < t * 32 + 31) != 0)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) mx = fmaxf(s[i], mx);
-    mx = xhalf_max(mx);
-    const float m_new = fmaxf(st.m, mx * a.scale_log2e), m_eff = m_new == -INFINITY ? 0.f : m_new;
-    if (__builtin_amdgcn_ballot_w64(m_new != st.m) != 0) {
-      const float alpha = exp2_fast(st.m - m_eff);
-      st.l *= alpha;
+      for (int r = 0; r < SETS; ++r)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st.o[db][i] *= alpha;
+          for (int i = 0; i < 4; ++i) s[r][u][i] = t * 32 + 16 * u + 4 * h4 + i <= see_rel[r] ? s[r][u][i] : -INFINITY;
+    bf16x8 p[SETS];
+#pragma unroll
+    for (int r = 0; r < SETS; ++r) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[r][u][i]);
+      mx = quarters_max(mx);
+      const float m_new = fmaxf(m[r], mx * a.scale_log2e), m_eff = m_new == -INFINITY ? 0.f : m_new;
+      if (__builtin_amdgcn_ballot_w64(m_new != m[r]) != 0) {
+        const float alpha = exp2_fast(m[r] - m_eff);
+        l[r] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[r][db] *= alpha;
+      }
+      m[r] = m_new;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[r][u][i] = exp2_fast(__builtin_fmaf(s[r][u][i], a.scale_log2e, -m_eff));
+          l[r] += s[r][u][i];
+        }
+      }
+      // (probabilities rounded to bf16 relative to the exact running maximum; their sum is not rounded)
+      const bf16x4 p0 = __builtin_convertvector(s[r][0], bf16x4), p1 = __builtin_convertvector(s[r][1], bf16x4);
+      p[r] = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    st.m = m_new;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = exp2_fast(__builtin_fmaf(s[i], a.scale_log2e, -m_eff));
-      sum += s[i];
-    }
-    st.l += sum;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const bf16x8 p = pack8(s, 8 * half);
+    for (int db = 0; db < DB; ++db) {
+      // (the swizzle makes block db's offset that of block 0 with db in bits 5 ..)
+      const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 0));
+      const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 16 * D * 2));
+      const bf16x8 v8 = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int db = 0; db < DB; ++db) st.o[db] = mfma32(lds_tr<D>(lo_v, db, half * 16 * D * 2), p, st.o[db]);
+      for (int r = 0; r < SETS; ++r) o[r][db] = mfma16(v8, p[r], o[r][db]);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+  };
+  if (wave_u < nt) {
+    Step s0, s1;
+    fetch(s0, wave_u);
+    if (wave_u + 4 < nt) fetch(s1, wave_u + 4);
+    for (int t = wave_u; t < nt; t += 8) {
+      work(s0, t, t + 8);
+      if (t + 4 < nt) work(s1, t + 4, t + 12);
+    }
   }
   // the waves' results, unnormalised, and their (maximum, sum), folded in wave order
   __syncthreads();
-  float* const acc = reinterpret_cast<float*>(smem);                         // [wave][rows][kOutRow]
-  float* const stat = acc + 4 * rows * kOutRow<D>;                           // [wave][2][32]
-  const float l_tot = xhalf_sum(st.l);
-  if (lane < 32) { stat[wave_u * 64 + ql] = st.m; stat[wave_u * 64 + 32 + ql] = l_tot; }
-  if (ql < rows)
+  constexpr int RW = 16 * SETS;
+  float* const acc = reinterpret_cast<float*>(smem);                         // [wave][row][kOutRow]
+  float* const stat = acc + 4 * RW * kOutRow<D>;                             // [wave][2][row]
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+  for (int r = 0; r < SETS; ++r) {
+    const float sum = quarters_sum(l[r]);
+    if (lane < 16) { stat[wave_u * 2 * RW + 16 * r + ql] = m[r]; stat[wave_u * 2 * RW + RW + 16 * r + ql] = sum; }
+    if (16 * r + ql < rows)
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 v = {st.o[db][4 * i4], st.o[db][4 * i4 + 1], st.o[db][4 * i4 + 2], st.o[db][4 * i4 + 3]};
-        *reinterpret_cast<f32x4*>(acc + (wave_u * rows + ql) * kOutRow<D> + 32 * db + 8 * i4 + 4 * g) = v;
-      }
+      for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(acc + (wave_u * RW + 16 * r + ql) * kOutRow<D> + 16 * db + 4 * h4) = o[r][db];
+  }
   __syncthreads();
   constexpr int PER = D / 8;
   for (int i = tid; i < rows * PER; i += 256) {
     const int r = i / PER, d = i % PER * 8;
-    float m = -INFINITY, l = 0.f;
+    float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) m = fmaxf(m, stat[w * 64 + r]);
+    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, stat[w * 2 * RW + r]);
     f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
-    const float m_eff = m == -INFINITY ? 0.f : m;
+    const float m_eff = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = exp2_fast(stat[w * 64 + r] - m_eff);
-      l += f * stat[w * 64 + 32 + r];
-      x0 += f * *reinterpret_cast<const f32x4*>(acc + (w * rows + r) * kOutRow<D> + d);
-      x1 += f * *reinterpret_cast<const f32x4*>(acc + (w * rows + r) * kOutRow<D> + d + 4);
+      const float f = exp2_fast(stat[w * 2 * RW + r] - m_eff);
+      sum += f * stat[w * 2 * RW + RW + r];
+      x0 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d);
+      x1 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d + 4);
     }
-    const float norm = l > 0.f ? 1.0f / l : 0.f, lse = l > 0.f ? (m + __builtin_log2f(l)) * kLn2 : -INFINITY;
+    const float norm = sum > 0.f ? 1.0f / sum : 0.f, lse = sum > 0.f ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
     x0 *= norm;
     x1 *= norm;
     const Kv4Row at = kv4_row(a, hk, r);
@@ -359,24 +418,30 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
       if (d == 0) a.part_lse[row * a.n_parts + part_i] = lse;
       continue;
     }
-    const int64_t to = (int64_t)b * a.o_stride_b + (int64_t)at.r * a.o_stride_s + (int64_t)at.h * a.o_stride_h + d;
+    const int64_t to_out = (int64_t)b * a.o_stride_b + (int64_t)at.r * a.o_stride_s + (int64_t)at.h * a.o_stride_h + d;
     if (a.out_f32) {
-      f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to);
+      f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + to_out);
       dst[0] = x0;
       dst[1] = x1;
     } else {
       const bf16x4 y0 = __builtin_convertvector(x0, bf16x4), y1 = __builtin_convertvector(x1, bf16x4);
-      *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
+      *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to_out) = __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     if (d == 0) a.lse[row] = lse;
   }
 }
 
+template <int D, int SETS>
+static void launch_few_t(const Kv4Args& a, hipStream_t st) {
+  const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
+  hipLaunchKernelGGL((kv4_few_kernel<D, SETS>), dim3(a.n_parts > 1 ? (unsigned)a.n_parts * planes : (planes + 7) / 8 * 8), dim3(256),
+                     (kv4_few_lds_bytes<D, SETS>()), st, a);
+}
 template <int D>
 static void launch_fwd_t(const Kv4Args& a, bool few, hipStream_t st) {
   const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
   const int rows = a.group * a.s_q;
-  if (few) hipLaunchKernelGGL(kv4_few_kernel<D>, dim3((unsigned)a.n_parts, planes), dim3(256), kv4_few_lds_bytes<D>(rows), st, a);
+  if (few) rows <= 16 ? launch_few_t<D, 1>(a, st) : launch_few_t<D, 2>(a, st);
   else hipLaunchKernelGGL(kv4_fwd_kernel<D>, dim3((unsigned)a.n_parts * (unsigned)((rows + 127) / 128), planes), dim3(256), kv4_fwd_lds_bytes<D>(), st, a);
 }
 hipError_t launch_kv4_fwd(const Kv4Args& a, int head_dim, bool few, hipStream_t st) {
@@ -389,8 +454,8 @@ hipError_t opt_in_kv4_kernels() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<128>), attr, (int)kv4_fwd_lds_bytes<128>());
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<64>), attr, (int)kv4_fwd_lds_bytes<64>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128>), attr, (int)kv4_few_lds_bytes<128>(kKv4FewRows));
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<64>), attr, (int)kv4_few_lds_bytes<64>(kKv4FewRows));
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128, 2>), attr, (int)kv4_few_lds_bytes<128, 2>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<64, 2>), attr, (int)kv4_few_lds_bytes<64, 2>());
   return e;
 }
 

@@ -41,6 +41,7 @@ Kv4Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t wgs = planes * (plan.few ? 1 : (rows + 127) / 128), want = (plan.few ? 4 : 2) * (int64_t)compute_units();
   const int64_t least = plan.few ? 256 : 1024;       // keys of a part
   int64_t parts = (want + wgs - 1) / wgs;
+  if (plan.few && parts > 4) parts = (parts + 7) / 8 * 8;      // (ranges of the same keys share an XCD: eight at a time)
   if (parts > keys / least) parts = keys / least;
   if (parts > 1) {
     plan.part_keys = ((keys + parts - 1) / parts + 127) / 128 * 128;

@@ -470,6 +470,13 @@ SP_DEV int next_item(unsigned* tickets, int n_items, int blocks, bool by_group) 
   return -1;
 }
 
+// Workgroup index -> item 0 .. n - 1, or -1: the hardware hands workgroups to the eight XCDs in turn, and here the items of one XCD follow
+// each other, so that neighbours share an L2.  Grid: n rounded up to a multiple of 8.
+SP_DEV int xcd_run(int index, int n) {
+  const int per = (n + 7) / 8, t = (index & 7) * per + (index >> 3);
+  return (index >> 3) < per && t < n ? t : -1;
+}
+
 // ---- scheduling helpers ------------------------------------------------------------------------
 #define SP_FENCE() __builtin_amdgcn_sched_barrier(0)
 // Issue priority of a wave while it is in a matrix phase.  Waves are served oldest first, so without
