@@ -216,18 +216,18 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   }
 }
 
-// Tokens: at most 16 SETS rows of a plane (its query heads and a few tokens), all in every wave; the four waves of a workgroup share out the
-// 32-key steps of its keys.  v_mfma_f32_16x16x32_bf16: with lane = 16 h + r an operand's lane holds row or column r, contraction slots
+// Tokens: at most 16 SETS rows of a plane (its query heads and a few tokens), all in every wave; the four waves of a workgroup have a head
+// each (or two, or all of them one) and share out the 32-key steps of its keys.  v_mfma_f32_16x16x32_bf16: with lane = 16 h + r an operand's lane holds row or column r, contraction slots
 // 8 h .. 8 h + 7, a result's column r, register i row 4 h + i.
 //   S^T = K Q^T      K goes from memory to the matrix unit without LDS: since the contraction may take head_dim in any order, lane group h
 //                    takes the h-th quarter of a row, 8 elements a step, and a lane's codes of 16 keys are one load
 //   O^T += V^T P^T   V passes through 32 rows of LDS of the wave's own for the transposed read (lane group h: keys 4 h .. 4 h + 3 of either 16)
 // Codes of the next two steps are under way in registers.  Bound by the bytes of the cache.
-// Workgroups: the key ranges of all heads of a sequence that cover the same keys go to one XCD one after the other, because a
-// row's codes are 64 bytes and its scales 4, of lines of 128 that hold the next heads' too.
-template <int D, int SETS>
+// A row's codes are 64 bytes and its scales 4, of lines of 128 that hold the next heads' too: hence neighbouring heads in a workgroup, and the
+// workgroups that cover the same keys of a sequence one after the other on one XCD.
+template <int D, int SETS, int HEADS>
 constexpr size_t kv4_few_lds_bytes() {
-  constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * kOutRow<D> * 4 + 4 * 2 * 16 * SETS * 4;
+  constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * HEADS * (kOutRow<D> + 2) * 4;
   return tiles > out ? tiles : out;
 }
 SP_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -239,13 +239,14 @@ SP_DEV float quarters_sum(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
-template <int D, int SETS>
-__global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
-  constexpr int W = D / 32, DB = D / 16, QUARTER = D / 4;      // dwords of codes of a quarter row (= matrix steps), output blocks
+template <int D, int SETS, int HEADS>
+__global__ __launch_bounds__(256, 2) void kv4_few_kernel(const Kv4Args a) {
+  constexpr int W = D / 32, N = SETS * HEADS, DEPTH = HEADS == 1 ? 2 : 1, DB = D / 16, QUARTER = D / 4;      // dwords of codes of a quarter row (= matrix steps), output blocks
   typedef uint32_t codes_t __attribute__((ext_vector_type(W)));
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, h4 = lane >> 4, ql = lane & 15, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = a.group * a.s_q, planes = a.batch * a.n_kv_heads;
+  const int hw = a.heads_wg, subs = 4 / hw, sub = wave_u / hw;      // sets of HEADS heads of the workgroup, waves of a set, which of them this is
+  const int rows = a.group * a.s_q, head_sets = a.n_kv_heads / (hw * HEADS), planes = a.batch * head_sets;
   int part_i = 0, plane = blockIdx.x;
   if (a.n_parts > 1) {
     const int per = 8 * planes, first = (int)blockIdx.x / per * 8, i = (int)blockIdx.x % per, n = a.n_parts - first < 8 ? a.n_parts - first : 8;
@@ -255,20 +256,21 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
     plane = xcd_run(blockIdx.x, planes);
   }
   if (plane < 0 || plane >= planes) return;
-  const int b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int b = plane / head_sets, hk0 = (plane - b * head_sets) * hw * HEADS, hk = hk0 + wave_u % hw * HEADS;
   const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
   const int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
   const int n_keys = hi > lo ? (int)(hi - lo) : 0, nt = (n_keys + 31) / 32;
   char* const tile_p = smem + wave_u * 32 * D * 2;
 
-  bf16x8 q[SETS][W];
-  f32x4 o[SETS][DB];
-  float m[SETS], l[SETS];
+  // element n: row set n % SETS of head n / SETS
+  bf16x8 q[N][W];
+  f32x4 o[N][DB];
+  float m[N], l[N];
   int see_rel[SETS];
 #pragma unroll
-  for (int r = 0; r < SETS; ++r) {
-    const int rh = 16 * r + ql;
-    const Kv4Row my = kv4_row(a, hk, rh < rows ? rh : rows - 1);
+  for (int r = 0; r < N; ++r) {
+    const int rh = 16 * (r % SETS) + ql;
+    const Kv4Row my = kv4_row(a, hk + r / SETS, rh < rows ? rh : rows - 1);
     const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + QUARTER * h4;
 #pragma unroll
     for (int j = 0; j < W; ++j) q[r][j] = *reinterpret_cast<const bf16x8*>(qp + 8 * j);
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
     m[r] = -INFINITY;
     l[r] = 0.f;
     const int64_t see = (a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1) - lo;
-    see_rel[r] = see < -1 ? -1 : (int)see;
+    see_rel[r % SETS] = see < -1 ? -1 : (int)see;
   }
   int min_see = see_rel[0];                      // keys up to here: every row of the lane sees them
 #pragma unroll
@@ -290,117 +292,126 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
   const int from = (int)lds_addr(smem) + wave_u * 32 * D * 2 + tile_off<D>(4 * h4 + ql / 4, (ql & 3) >> 1) + ((ql & 1) << 3);
 
   const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s + QUARTER * h4;
-  struct Step { codes_t k[2], v[2]; uint32_t ks[2], vs[2]; };
+  const int64_t lane_off = (int64_t)ql * a.kv_stride_s, step_off = 16 * a.kv_stride_s;
+  struct Step { codes_t k[HEADS][2], v[HEADS][2]; uint32_t ks[HEADS][2], vs[HEADS][2]; };
   auto fetch = [&](Step& s, int t) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int key = t * 32 + 16 * u + ql, kc = key < n_keys ? key : n_keys - 1;      // (keys behind the last are not read)
-      const int64_t at = base + (int64_t)kc * a.kv_stride_s;
-      s.k[u] = *reinterpret_cast<const codes_t*>(a.k.codes + at / 2);
-      s.v[u] = *reinterpret_cast<const codes_t*>(a.v.codes + at / 2);
-      s.ks[u] = a.k.scales[at / 32];
-      s.vs[u] = a.v.scales[at / 32];
+      int64_t at = base + (2 * t + u) * step_off + lane_off;
+      const int over = t * 32 + 16 * u + ql - (n_keys - 1);      // (keys behind the last are not read)
+      if (t * 32 + 32 > n_keys) at -= (over > 0 ? over : 0) * a.kv_stride_s;
+#pragma unroll
+      for (int hd = 0; hd < HEADS; ++hd, at += a.kv_stride_h) {
+        s.k[hd][u] = *reinterpret_cast<const codes_t*>(a.k.codes + at / 2);
+        s.v[hd][u] = *reinterpret_cast<const codes_t*>(a.v.codes + at / 2);
+        s.ks[hd][u] = a.k.scales[at / 32];
+        s.vs[hd][u] = a.v.scales[at / 32];
+      }
     }
   };
   auto work = [&](Step& st, int t, int next) {
-    f32x4 s[SETS][2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float ks = kv4_scale(st.ks[u]), vs = kv4_scale(st.vs[u]);
+    for (int hd = 0; hd < HEADS; ++hd) {
+      f32x4 s[SETS][2];
 #pragma unroll
-      for (int r = 0; r < SETS; ++r) s[r][u] = f32x4{0, 0, 0, 0};
+      for (int u = 0; u < 2; ++u) {
+        const float ks = kv4_scale(st.ks[hd][u]), vs = kv4_scale(st.vs[hd][u]);
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const bf16x8 k8 = kv4_values(st.k[u][j], ks);
+        for (int r = 0; r < SETS; ++r) s[r][u] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int r = 0; r < SETS; ++r) s[r][u] = mfma16(k8, q[r][j], s[r][u]);
-        *reinterpret_cast<bf16x8*>(tile_p + 16 * u * D * 2 + to[j]) = kv4_values(st.v[u][j], vs);
+        for (int j = 0; j < W; ++j) {
+          const bf16x8 k8 = kv4_values(st.k[hd][u][j], ks);
+#pragma unroll
+          for (int r = 0; r < SETS; ++r) s[r][u] = mfma16(k8, q[hd * SETS + r][j], s[r][u]);
+          *reinterpret_cast<bf16x8*>(tile_p + 16 * u * D * 2 + to[j]) = kv4_values(st.v[hd][u][j], vs);
+        }
       }
-    }
-    if (next < nt) fetch(st, next);
-    if (__builtin_amdgcn_ballot_w64(min_see < t * 32 + 31) != 0)
+      if (hd == HEADS - 1 && next < nt) fetch(st, next);
+      if (__builtin_amdgcn_ballot_w64(min_see < t * 32 + 31) != 0)
 #pragma unroll
-      for (int r = 0; r < SETS; ++r)
+        for (int r = 0; r < SETS; ++r)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[r][u][i] = t * 32 + 16 * u + 4 * h4 + i <= see_rel[r] ? s[r][u][i] : -INFINITY;
+      bf16x8 p[SETS];
+#pragma unroll
+      for (int r = 0; r < SETS; ++r) {
+        const int n = hd * SETS + r;
+        float mx = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[r][u][i] = t * 32 + 16 * u + 4 * h4 + i <= see_rel[r] ? s[r][u][i] : -INFINITY;
-    bf16x8 p[SETS];
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[r][u][i]);
+        mx = quarters_max(mx);
+        const float m_new = fmaxf(m[n], mx * a.scale_log2e), m_eff = m_new == -INFINITY ? 0.f : m_new;
+        if (__builtin_amdgcn_ballot_w64(m_new != m[n]) != 0) {
+          const float alpha = exp2_fast(m[n] - m_eff);
+          l[n] *= alpha;
 #pragma unroll
-    for (int r = 0; r < SETS; ++r) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[r][u][i]);
-      mx = quarters_max(mx);
-      const float m_new = fmaxf(m[r], mx * a.scale_log2e), m_eff = m_new == -INFINITY ? 0.f : m_new;
-      if (__builtin_amdgcn_ballot_w64(m_new != m[r]) != 0) {
-        const float alpha = exp2_fast(m[r] - m_eff);
-        l[r] *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[r][db] *= alpha;
-      }
-      m[r] = m_new;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[r][u][i] = exp2_fast(__builtin_fmaf(s[r][u][i], a.scale_log2e, -m_eff));
-          l[r] += s[r][u][i];
+          for (int db = 0; db < DB; ++db) o[n][db] *= alpha;
         }
+        m[n] = m_new;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[r][u][i] = exp2_fast(__builtin_fmaf(s[r][u][i], a.scale_log2e, -m_eff));
+            l[n] += s[r][u][i];
+          }
+        }
+        // (probabilities rounded to bf16 relative to the exact running maximum; their sum is not rounded)
+        const bf16x4 p0 = __builtin_convertvector(s[r][0], bf16x4), p1 = __builtin_convertvector(s[r][1], bf16x4);
+        p[r] = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
       }
-      // (probabilities rounded to bf16 relative to the exact running maximum; their sum is not rounded)
-      const bf16x4 p0 = __builtin_convertvector(s[r][0], bf16x4), p1 = __builtin_convertvector(s[r][1], bf16x4);
-      p[r] = __builtin_shufflevector(p0, p1, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int db = 0; db < DB; ++db) {
-      // (the swizzle makes block db's offset that of block 0 with db in bits 5 ..)
-      const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 0));
-      const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 16 * D * 2));
-      const bf16x8 v8 = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+      for (int db = 0; db < DB; ++db) {
+        // (the swizzle makes block db's offset that of block 0 with db in bits 5 ..)
+        const bf16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 0));
+        const bf16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_ptr<bf16x4>(from ^ (db << 5), 16 * D * 2));
+        const bf16x8 v8 = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-      for (int r = 0; r < SETS; ++r) o[r][db] = mfma16(v8, p[r], o[r][db]);
+        for (int r = 0; r < SETS; ++r) o[hd * SETS + r][db] = mfma16(v8, p[r], o[hd * SETS + r][db]);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
   };
-  if (wave_u < nt) {
-    Step s0, s1;
-    fetch(s0, wave_u);
-    if (wave_u + 4 < nt) fetch(s1, wave_u + 4);
-    for (int t = wave_u; t < nt; t += 8) {
-      work(s0, t, t + 8);
-      if (t + 4 < nt) work(s1, t + 4, t + 12);
-    }
+  if (sub < nt) {
+    Step s[DEPTH];
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+      if (sub + i * subs < nt) fetch(s[i], sub + i * subs);
+    for (int t = sub; t < nt; t += DEPTH * subs)
+#pragma unroll
+      for (int i = 0; i < DEPTH; ++i)
+        if (t + i * subs < nt) work(s[i], t + i * subs, t + (i + DEPTH) * subs);
   }
-  // the waves' results, unnormalised, and their (maximum, sum), folded in wave order
+  // the results of a head's waves, unnormalised, and their (maximum, sum), folded in wave order
   __syncthreads();
-  constexpr int RW = 16 * SETS;
+  constexpr int RW = 16 * N;
   float* const acc = reinterpret_cast<float*>(smem);                         // [wave][row][kOutRow]
   float* const stat = acc + 4 * RW * kOutRow<D>;                             // [wave][2][row]
 #pragma unroll
-  for (int r = 0; r < SETS; ++r) {
+  for (int r = 0; r < N; ++r) {
     const float sum = quarters_sum(l[r]);
     if (lane < 16) { stat[wave_u * 2 * RW + 16 * r + ql] = m[r]; stat[wave_u * 2 * RW + RW + 16 * r + ql] = sum; }
-    if (16 * r + ql < rows)
+    if (16 * (r % SETS) + ql < rows)
 #pragma unroll
       for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(acc + (wave_u * RW + 16 * r + ql) * kOutRow<D> + 16 * db + 4 * h4) = o[r][db];
   }
   __syncthreads();
   constexpr int PER = D / 8;
-  for (int i = tid; i < rows * PER; i += 256) {
-    const int r = i / PER, d = i % PER * 8;
+  for (int i = tid; i < hw * HEADS * rows * PER; i += 256) {
+    const int hh = i / (rows * PER), rr = (i - hh * rows * PER) / PER, d = i % PER * 8;
+    const int w0 = hh / HEADS, r = hh % HEADS * 16 * SETS + rr;      // first wave of the head, row among its wave's
     float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) mx = fmaxf(mx, stat[w * 2 * RW + r]);
+    for (int w = w0; w < 4; w += hw) mx = fmaxf(mx, stat[w * 2 * RW + r]);
     f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
     const float m_eff = mx == -INFINITY ? 0.f : mx;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = w0; w < 4; w += hw) {
       const float f = exp2_fast(stat[w * 2 * RW + r] - m_eff);
       sum += f * stat[w * 2 * RW + RW + r];
       x0 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d);
@@ -409,7 +420,7 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
     const float norm = sum > 0.f ? 1.0f / sum : 0.f, lse = sum > 0.f ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
     x0 *= norm;
     x1 *= norm;
-    const Kv4Row at = kv4_row(a, hk, r);
+    const Kv4Row at = kv4_row(a, hk0 + hh, rr);
     const int64_t row = ((int64_t)b * a.n_q_heads + at.h) * a.s_q + at.r;
     if (a.n_parts > 1) {
       f32x4* dst = reinterpret_cast<f32x4*>(a.part_out + (row * a.n_parts + part_i) * D + d);
@@ -431,17 +442,18 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(const Kv4Args a) {
   }
 }
 
-template <int D, int SETS>
+template <int D, int SETS, int HEADS>
 static void launch_few_t(const Kv4Args& a, hipStream_t st) {
-  const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
-  hipLaunchKernelGGL((kv4_few_kernel<D, SETS>), dim3(a.n_parts > 1 ? (unsigned)a.n_parts * planes : (planes + 7) / 8 * 8), dim3(256),
-                     (kv4_few_lds_bytes<D, SETS>()), st, a);
+  const unsigned planes = (unsigned)(a.batch * (a.n_kv_heads / (a.heads_wg * HEADS)));
+  hipLaunchKernelGGL((kv4_few_kernel<D, SETS, HEADS>), dim3(a.n_parts > 1 ? (unsigned)a.n_parts * planes : (planes + 7) / 8 * 8), dim3(256),
+                     (kv4_few_lds_bytes<D, SETS, HEADS>()), st, a);
 }
 template <int D>
 static void launch_fwd_t(const Kv4Args& a, bool few, hipStream_t st) {
   const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
   const int rows = a.group * a.s_q;
-  if (few) rows <= 16 ? launch_few_t<D, 1>(a, st) : launch_few_t<D, 2>(a, st);
+  if (few && a.wave_heads == 2) launch_few_t<D, 1, 2>(a, st);
+  else if (few) rows <= 16 ? launch_few_t<D, 1, 1>(a, st) : launch_few_t<D, 2, 1>(a, st);
   else hipLaunchKernelGGL(kv4_fwd_kernel<D>, dim3((unsigned)a.n_parts * (unsigned)((rows + 127) / 128), planes), dim3(256), kv4_fwd_lds_bytes<D>(), st, a);
 }
 hipError_t launch_kv4_fwd(const Kv4Args& a, int head_dim, bool few, hipStream_t st) {
@@ -454,8 +466,8 @@ hipError_t opt_in_kv4_kernels() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<128>), attr, (int)kv4_fwd_lds_bytes<128>());
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_fwd_kernel<64>), attr, (int)kv4_fwd_lds_bytes<64>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128, 2>), attr, (int)kv4_few_lds_bytes<128, 2>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<64, 2>), attr, (int)kv4_few_lds_bytes<64, 2>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128, 2, 1>), attr, (int)kv4_few_lds_bytes<128, 2, 1>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv4_few_kernel<128, 1, 2>), attr, (int)kv4_few_lds_bytes<128, 1, 2>());
   return e;
 }
 

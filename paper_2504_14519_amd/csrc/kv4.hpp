@@ -31,6 +31,7 @@ struct Kv4Args {
   int64_t o_stride_b, o_stride_s, o_stride_h;
   int32_t n_parts;               // key ranges of part_keys keys (the last one shorter), a workgroup each; 1: straight to out, lse
   int64_t part_keys;
+  int32_t wave_heads, heads_wg;  // few rows: kv heads of a wave (1 or 2), sets of them of a workgroup (1, 2 or 4); their product divides n_kv_heads
   float* part_out;               // [batch, n_q_heads, s_q][n_parts][head_dim], as in PartMergeArgs
   float* part_lse;
 };

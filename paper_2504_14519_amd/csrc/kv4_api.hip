@@ -32,19 +32,27 @@ int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->n_q_heads / 
 // Key ranges that a call is cut into, a workgroup for each and each block of rows, so that the chip is full.
 struct Kv4Plan {
   bool few;
-  int32_t parts;
+  int32_t wave_heads, heads_wg, parts;
   int64_t part_keys;
 };
 Kv4Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
-  Kv4Plan plan{rows <= kKv4FewRows, 1, keys};
-  const int64_t wgs = planes * (plan.few ? 1 : (rows + 127) / 128), want = (plan.few ? 4 : 2) * (int64_t)compute_units();
+  Kv4Plan plan{rows <= kKv4FewRows, 1, 1, 1, keys};
+  if (plan.few) {
+    // two heads a wave: in a cache with heads next to each other their codes share lines
+    plan.wave_heads = rows <= 16 && p->n_kv_heads % 2 == 0 ? 2 : 1;
+    const int32_t sets = p->n_kv_heads / plan.wave_heads;
+    plan.heads_wg = sets % 4 == 0 ? 4 : sets % 2 == 0 ? 2 : 1;
+  }
+  const int64_t wgs = plan.few ? planes / (plan.wave_heads * plan.heads_wg) : planes * ((rows + 127) / 128), want = 2 * (int64_t)compute_units();
   const int64_t least = plan.few ? 256 : 1024;       // keys of a part
-  int64_t parts = (want + wgs - 1) / wgs;
-  if (plan.few && parts > 4) parts = (parts + 7) / 8 * 8;      // (ranges of the same keys share an XCD: eight at a time)
+  // tokens: whole rounds of the workgroups that the chip holds, eight ranges at a time (ranges of the same keys share an XCD)
+  int64_t parts = plan.few ? want / wgs : (want + wgs - 1) / wgs;
+  if (plan.few && parts >= 8) parts = parts / 8 * 8;
   if (parts > keys / least) parts = keys / least;
   if (parts > 1) {
-    plan.part_keys = ((keys + parts - 1) / parts + 127) / 128 * 128;
+    const int64_t unit = plan.few ? 32 : 64;      // keys of a step
+    plan.part_keys = ((keys + parts - 1) / parts + unit - 1) / unit * unit;
     plan.parts = (int32_t)((keys + plan.part_keys - 1) / plan.part_keys);
   }
   return plan;
@@ -142,6 +150,7 @@ int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, co
   a.o_stride_b = p->o_stride_b; a.o_stride_s = p->o_stride_s; a.o_stride_h = p->o_stride_h;
   a.n_parts = plan.parts;
   a.part_keys = plan.part_keys;
+  a.wave_heads = plan.wave_heads; a.heads_wg = plan.heads_wg;
   if (plan.parts > 1) {
     a.part_out = static_cast<float*>(workspace);
     a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + out_bytes(p, plan));

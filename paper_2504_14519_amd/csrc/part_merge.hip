@@ -4,58 +4,11 @@
 
 namespace slimpipe {
 
-// D / 8 lanes hold a row; GROUPS such sets share out its parts (1: sixteen rows a workgroup for D = 128, many rows; 16: few rows of many
-// parts, where the chain of dependent loads of one set would be the time).  Sums in float32, parts in order, sets in order.
-template <int D, int GROUPS>
-__global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) {
-  constexpr int NC = D / 8, SETS = 256 / NC, ROWS = SETS / GROUPS, STRIDE = GROUPS;
-  __shared__ float acc_s[GROUPS > 1 ? SETS : 1][D + 4], m_s[SETS], l_s[SETS];
-  const int set = threadIdx.x / NC, c = threadIdx.x % NC, g = set / ROWS;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + set % ROWS;
-  const bool mine = row < a.rows;
-  const int64_t first = (mine ? row : 0) * a.parts;
-  const float* lp = a.part_lse + first;
-  const float* op = a.part_out + first * D + c * 8;
-  float m = -INFINITY, l = 0.f;
-  f32x4 x0 = {0, 0, 0, 0}, x1 = {0, 0, 0, 0};
-  if (mine) {
-    for (int s = g; s < a.parts; s += STRIDE) m = fmaxf(m, lp[s]);
-    if (m != -INFINITY)
-#pragma unroll 4
-      for (int s = g; s < a.parts; s += STRIDE) {
-        const float ls = lp[s];
-        if (ls == -INFINITY) continue;
-        const float w = exp2_fast((ls - m) * kLog2e);
-        l += w;
-        x0 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D);
-        x1 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D + 4);
-      }
-  }
-  if constexpr (GROUPS > 1) {
-    if (c == 0) { m_s[set] = m; l_s[set] = l; }
-    *reinterpret_cast<f32x4*>(&acc_s[set][c * 8]) = x0;
-    *reinterpret_cast<f32x4*>(&acc_s[set][c * 8 + 4]) = x1;
-    __syncthreads();
-    if (g != 0) return;
-    const int r = set;                               // (sets 0 .. ROWS - 1 are the rows)
-    float mx = -INFINITY;
-    for (int i = 0; i < GROUPS; ++i) mx = fmaxf(mx, m_s[r + i * ROWS]);
-    x0 = x1 = f32x4{0, 0, 0, 0};
-    l = 0.f;
-    m = mx;
-    if (mx != -INFINITY)
-      for (int i = 0; i < GROUPS; ++i) {
-        const int o = r + i * ROWS;
-        const float w = exp2_fast((m_s[o] - mx) * kLog2e);
-        l += w * l_s[o];
-        x0 += w * *reinterpret_cast<const f32x4*>(&acc_s[o][c * 8]);
-        x1 += w * *reinterpret_cast<const f32x4*>(&acc_s[o][c * 8 + 4]);
-      }
-  }
-  if (!mine) return;
+// Writes 8 elements of a row's result, and its lse.
+SP_DEV void put_result(const PartMergeArgs& a, int64_t row, int d, f32x4 x0, f32x4 x1, float m, float l) {
   const float inv = l > 0.f ? 1.0f / l : 0.f;
   const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
-  const int64_t to = b * a.o_stride_b + (row - bh * a.s_q) * a.o_stride_s + (bh - b * a.n_q_heads) * a.o_stride_h + c * 8;
+  const int64_t to = b * a.o_stride_b + (row - bh * a.s_q) * a.o_stride_s + (bh - b * a.n_q_heads) * a.o_stride_h + d;
   x0 *= inv;
   x1 *= inv;
   if (a.out_f32) {
@@ -66,18 +19,96 @@ __global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) 
     const bf16x4 lo = __builtin_convertvector(x0, bf16x4), hi = __builtin_convertvector(x1, bf16x4);
     *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  if (c == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(l) * kLn2;
+  if (d == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(l) * kLn2;
+}
+// Parts first, first + step, .. of 8 elements of a row: maximum of their lse, sum of weights, weighted sum.
+template <int D>
+SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, int step, f32x4& x0, f32x4& x1, float& m, float& l) {
+  const float* lp = a.part_lse + row * a.parts;
+  const float* op = a.part_out + row * a.parts * D + d;
+  m = -INFINITY;
+  l = 0.f;
+  x0 = x1 = f32x4{0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = first; s < a.parts; s += step) m = fmaxf(m, lp[s]);
+  if (m == -INFINITY) return;
+#pragma unroll 4
+  for (int s = first; s < a.parts; s += step) {
+    const float ls = lp[s];
+    if (ls == -INFINITY) continue;
+    const float w = exp2_fast((ls - m) * kLog2e);
+    l += w;
+    x0 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D);
+    x1 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D + 4);
+  }
 }
 
-template <int D, int GROUPS>
-static void launch_t(const PartMergeArgs& a, hipStream_t st) {
-  constexpr int ROWS = 256 / (D / 8) / GROUPS;
-  hipLaunchKernelGGL((part_merge_kernel<D, GROUPS>), dim3((unsigned)((a.rows + ROWS - 1) / ROWS)), dim3(256), 0, st, a);
+// Many rows: D / 8 lanes a row.  Bound by the bytes (65536 rows of 8 parts of head_dim 128: 285 MB in 56 us).
+template <int D>
+__global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) {
+  constexpr int NC = D / 8;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
+  const int d = (int)(gid - row * NC) * 8;
+  if (row >= a.rows) return;
+  f32x4 x0, x1;
+  float m, l;
+  fold_parts<D>(a, row, d, 0, 1, x0, x1, m, l);
+  put_result(a, row, d, x0, x1, m, l);
 }
+
+// Few rows: a workgroup has 32 elements of one row, and its 64 sets of four lanes share out the parts, where the chain of dependent loads of
+// one set would be the time.  Sets of a wave are folded by exchanges, the waves through LDS, always in the same order.
+template <int D>
+__global__ __launch_bounds__(256) void part_merge_few_kernel(const PartMergeArgs a) {
+  __shared__ float acc_s[4][32], m_s[4], l_s[4];
+  const int64_t row = blockIdx.x;
+  const int set = threadIdx.x / 4, c = threadIdx.x % 4, d = blockIdx.y * 32 + c * 8, wave = threadIdx.x >> 6;
+  f32x4 x0, x1;
+  float m, l;
+  fold_parts<D>(a, row, d, set, 64, x0, x1, m, l);
+#pragma unroll
+  for (int w = 4; w < 64; w <<= 1) {
+    const float mo = __shfl_xor(m, w, 64), lo = __shfl_xor(l, w, 64), mx = fmaxf(m, mo), me = mx == -INFINITY ? 0.f : mx;
+    const float f = exp2_fast((m - me) * kLog2e), fo = exp2_fast((mo - me) * kLog2e);
+    l = l * f + lo * fo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x0[e] = x0[e] * f + __shfl_xor(x0[e], w, 64) * fo;
+      x1[e] = x1[e] * f + __shfl_xor(x1[e], w, 64) * fo;
+    }
+    m = mx;
+  }
+  if ((threadIdx.x & 63) < 4) {
+    *reinterpret_cast<f32x4*>(&acc_s[wave][c * 8]) = x0;
+    *reinterpret_cast<f32x4*>(&acc_s[wave][c * 8 + 4]) = x1;
+    if (c == 0) { m_s[wave] = m; l_s[wave] = l; }
+  }
+  __syncthreads();
+  if (threadIdx.x >= 4) return;
+  m = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
+  l = 0.f;
+  x0 = x1 = f32x4{0, 0, 0, 0};
+  if (m != -INFINITY)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = exp2_fast((m_s[w] - m) * kLog2e);
+      l += f * l_s[w];
+      x0 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8]);
+      x1 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8 + 4]);
+    }
+  put_result(a, row, d, x0, x1, m, l);
+}
+
 hipError_t launch_part_merge(const PartMergeArgs& a, int head_dim, hipStream_t st) {
-  const bool spread = a.rows <= 4096 && a.parts > 2;
-  if (head_dim == 128) spread ? launch_t<128, 16>(a, st) : launch_t<128, 1>(a, st);
-  else spread ? launch_t<64, 16>(a, st) : launch_t<64, 1>(a, st);
+  if (a.rows <= 1024 && a.parts > 4) {
+    dim3 grid((unsigned)a.rows, (unsigned)(head_dim / 32));
+    if (head_dim == 128) hipLaunchKernelGGL(part_merge_few_kernel<128>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(part_merge_few_kernel<64>, grid, dim3(256), 0, st, a);
+  } else {
+    dim3 grid((unsigned)((a.rows * (head_dim / 8) + 255) / 256));
+    if (head_dim == 128) hipLaunchKernelGGL(part_merge_kernel<128>, grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(part_merge_kernel<64>, grid, dim3(256), 0, st, a);
+  }
   return hipGetLastError();
 }
 
