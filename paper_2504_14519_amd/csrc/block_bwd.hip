@@ -91,11 +91,14 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
         f32x16 s, dp;
 #pragma unroll
         for (int i = 0; i < 16; ++i) { s[i] = 0.f; dp[i] = ndelta; }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          s = mfma32(lds_rp<D>(lo_k, ks, kb * 32 * D * 2), q[ks], s);
-          dp = mfma32(lds_rp<D>(lo_k, ks, TILE + kb * 32 * D * 2), d_o[ks], dp);
-        }
+        constexpr int LOOK = 3;
+        bf16x8 buf[LOOK + 1];
+        matrix_run<2 * KS, LOOK>(
+            [&](auto m) { buf[m % (LOOK + 1)] = lds_rp<D>(lo_k, m / 2, m % 2 * TILE + kb * 32 * D * 2); },
+            [&](auto m) {
+              if constexpr (m % 2 == 0) s = mfma32(buf[m % (LOOK + 1)], q[m / 2], s);
+              else dp = mfma32(buf[m % (LOOK + 1)], d_o[m / 2], dp);
+            });
         if (masked) {
           const int hi = kmax - kb * 32 - 4 * g;
 #pragma unroll
@@ -103,12 +106,10 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = exp2_fast(__builtin_fmaf(s[i], c, -lse2)) * dp[i];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const bf16x8 ds = pack8(s, 8 * half);      // (rounded to bf16 for the matrix unit, as in the dense backward)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) dq[db] = mfma32(lds_tr<D>(lo_kt, db, (2 * kb + half) * 16 * D * 2), ds, dq[db]);
-        }
+        const bf16x8 ds[2] = {pack8(s, 0), pack8(s, 8)};      // (rounded to bf16 for the matrix unit, as in the dense backward)
+        matrix_run<2 * DB, LOOK>(
+            [&](auto m) { buf[m % (LOOK + 1)] = lds_tr<D>(lo_kt, m % DB, (2 * kb + m / DB) * 16 * D * 2); },
+            [&](auto m) { dq[m % DB] = mfma32(buf[m % (LOOK + 1)], ds[m / DB], dq[m % DB]); });
       }
       const int step = (t & 1) ? -2 * TILE : 2 * TILE;
       lo_k.add(step);
@@ -254,8 +255,8 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   copy(0);
   fetch(1);
   put_stats(0);
-  RpOffsets<D> lo_q, lo_v;
-  TrOffsets<D> lo_t;
+  RpBase<D> lo_q, lo_v;          // (one register each: they are short here)
+  TrBase<D> lo_t;
   lo_q.init(lane, (int)lds);
   lo_t.init(lane, (int)lds);
   lo_v.init(lane, (int)lds + L::V + wave_u * 32 * D * 2);
@@ -276,11 +277,17 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
 #pragma unroll
       for (int e = 0; e < 4; ++e) { s[4 * i4 + e] = 0.f; dp[4 * i4 + e] = nd[e]; }
     }
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      s = mfma32(lds_rp<D>(lo_q, ks, 0), kreg[ks], s);
-      dp = mfma32(lds_rp<D>(lo_q, ks, L::TILE), lds_rp<D>(lo_v, ks, 0), dp);
-    }
+    constexpr int LOOK = 3;
+    bf16x8 buf[LOOK + 1], vbuf[2];
+    matrix_run<2 * KS, LOOK>(
+        [&](auto m) {
+          buf[m % (LOOK + 1)] = lds_rp<D>(lo_q, m / 2, m % 2 * L::TILE);
+          if constexpr (m % 2 == 1) vbuf[m / 2 % 2] = lds_rp<D>(lo_v, m / 2, 0);
+        },
+        [&](auto m) {
+          if constexpr (m % 2 == 0) s = mfma32(buf[m % (LOOK + 1)], kreg[m / 2], s);
+          else dp = mfma32(buf[m % (LOOK + 1)], vbuf[m / 2 % 2], dp);
+        });
     const int pos_lane = reinterpret_cast<const int*>(st)[64 + ql];
     if (__builtin_amdgcn_ballot_w64(pos_lane < wave_u * 32 + 31) != 0) {      // some row does not see all keys of the wave
 #pragma unroll
@@ -301,15 +308,14 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
         dp[4 * i4 + e] *= s[4 * i4 + e];
       }
     }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const bf16x8 p = pack8(s, 8 * half), ds = pack8(dp, 8 * half);      // (bf16 for the matrix unit)
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        dv[db] = mfma32(lds_tr<D>(lo_t, db, L::TILE + half * 16 * D * 2), p, dv[db]);
-        dk[db] = mfma32(lds_tr<D>(lo_t, db, half * 16 * D * 2), ds, dk[db]);
-      }
-    }
+    const bf16x8 p[2] = {pack8(s, 0), pack8(s, 8)}, ds[2] = {pack8(dp, 0), pack8(dp, 8)};      // (bf16 for the matrix unit)
+    matrix_run<4 * DB, LOOK>(
+        [&](auto m) { buf[m % (LOOK + 1)] = lds_tr<D>(lo_t, m % (2 * DB) / 2, (m % 2 == 0 ? L::TILE : 0) + m / (2 * DB) * 16 * D * 2); },
+        [&](auto m) {
+          constexpr int half = m / (2 * DB), db = m % (2 * DB) / 2;
+          if constexpr (m % 2 == 0) dv[db] = mfma32(buf[m % (LOOK + 1)], p[half], dv[db]);
+          else dk[db] = mfma32(buf[m % (LOOK + 1)], ds[half], dk[db]);
+        });
     const int step = (u & 1) ? -2 * L::TILE : 2 * L::TILE;
     lo_q.add(step);
     lo_t.add(step);

@@ -37,10 +37,11 @@ SP_DEV void attend_tile(RowState<D>& st, const LoK& lo_k, const LoV& lo_v, float
   constexpr int KB = KEYS / 32, KS = D / 16, DB = D / 32;
   f32x16 s[KB];
   const f32x16 zero = {0};
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) s[kb] = mfma32(lds_rp<D>(lo_k, ks, kb * 32 * D * 2), st.q[ks], ks == 0 ? zero : s[kb]);
+  constexpr int LOOK = 3;
+  bf16x8 buf[LOOK + 1];
+  matrix_run<KS * KB, LOOK>(
+      [&](auto m) { buf[m % (LOOK + 1)] = lds_rp<D>(lo_k, m / KB, m % KB * 32 * D * 2); },
+      [&](auto m) { s[m % KB] = mfma32(buf[m % (LOOK + 1)], st.q[m / KB], m < KB ? zero : s[m % KB]); });
   if (masked) {
     const int lo = kmin - 4 * g, hi = kmax - 4 * g;
 #pragma unroll
@@ -82,10 +83,9 @@ SP_DEV void attend_tile(RowState<D>& st, const LoK& lo_k, const LoV& lo_v, float
     p[kb][1] = pack8(s[kb], 8);
   }
   st.l += sum;
-#pragma unroll
-  for (int blk = 0; blk < 2 * KB; ++blk)
-#pragma unroll
-    for (int db = 0; db < DB; ++db) st.o[db] = mfma32(lds_tr<D>(lo_v, db, blk * 16 * D * 2), p[blk / 2][blk % 2], st.o[db]);
+  matrix_run<2 * KB * DB, LOOK>(
+      [&](auto m) { buf[m % (LOOK + 1)] = lds_tr<D>(lo_v, m % DB, m / DB * 16 * D * 2); },
+      [&](auto m) { st.o[m % DB] = mfma32(buf[m % (LOOK + 1)], p[m / DB / 2][m / DB % 2], st.o[m % DB]); });
 }
 
 }  // namespace slimpipe

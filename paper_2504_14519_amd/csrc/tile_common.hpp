@@ -7,6 +7,8 @@
 #include "kernels.hpp"
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace slimpipe {
 
 typedef __bf16 bf16_t;
@@ -485,6 +487,37 @@ SP_DEV int xcd_run(int index, int n) {
 // go first costs the vector phase little.
 SP_DEV void matrix_phase_begin() { __builtin_amdgcn_s_setprio(3); }
 SP_DEV void matrix_phase_end() { __builtin_amdgcn_s_setprio(0); }
+
+// N matrix instructions as an explicit software pipeline: read(m) fetches the operands of instruction m from LDS, LOOK instructions ahead of
+// mul(m), and scheduling fences keep that order (left to the scheduler, reads end up right in front of their instruction whenever registers
+// are short).  m comes as std::integral_constant.
+template <int M, int N, int LOOK, class R, class F>
+SP_DEV void matrix_step(R& read, F& mul) {
+  if constexpr (M < N) {
+    if constexpr (M + LOOK < N) read(std::integral_constant<int, M + LOOK>{});
+    SP_FENCE();
+    mul(std::integral_constant<int, M>{});
+    SP_FENCE();
+    matrix_step<M + 1, N, LOOK>(read, mul);
+  }
+}
+template <int M, int LOOK, class R>
+SP_DEV void matrix_ahead(R& read) {
+  if constexpr (M < LOOK) {
+    read(std::integral_constant<int, M>{});
+    matrix_ahead<M + 1, LOOK>(read);
+  }
+}
+template <int N, int LOOK, class R, class F>
+SP_DEV void matrix_run(R&& read, F&& mul) {
+  SP_FENCE();
+  matrix_phase_begin();
+  matrix_ahead<0, LOOK>(read);
+  SP_FENCE();
+  matrix_step<0, N, LOOK>(read, mul);
+  matrix_phase_end();
+  SP_FENCE();
+}
 
 // End of a phase of the two-group schedules: nothing may be scheduled across the barrier.
 SP_DEV void phase_end() {
