@@ -22,11 +22,14 @@ int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_
   if ((int64_t)p->batch * p->n_kv_heads > 65535) return SLIMPIPE_EINVAL_SHAPE;                 // planes are a grid dimension
   return SLIMPIPE_OK;
 }
-int check_top_k(const slimpipe_attn_params* p, int32_t top_k) {
+int check_top_k(const slimpipe_attn_params* p, int32_t top_k, int is_bwd) {
   if (top_k < 1 || top_k > kMaxTopK) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t rows = (int64_t)p->n_q_heads / p->n_kv_heads * p->s_q;
-  // rows and slots of a plane, and all of them as workgroups, in 32 bits
+  // rows and slots of a plane, all of them as workgroups, and offsets of a plane's rows in units of 8 elements, in 32 bits
   if (rows * top_k > (int64_t)1 << 30 || rows * p->n_kv_heads * p->batch * top_k > (int64_t)1 << 34) return SLIMPIPE_EINVAL_SHAPE;
+  const int64_t heads = p->n_q_heads / p->n_kv_heads - 1, last = p->s_q - 1, most = (int64_t)1 << 35;
+  if (p->q_stride_h > most / (heads + 1) || p->q_stride_h * heads + p->q_stride_s * last >= most) return SLIMPIPE_EINVAL_STRIDE;
+  if (is_bwd && (p->do_stride_h > most / (heads + 1) || p->do_stride_h * heads + p->do_stride_s * last >= most)) return SLIMPIPE_EINVAL_STRIDE;
   return SLIMPIPE_OK;
 }
 int set_chunks(KvChunks* kv, const slimpipe_attn_params* p, const void* const* k, const void* const* v, int32_t n_chunks, int64_t chunk_len) {
@@ -50,6 +53,9 @@ int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->batch * p->n
 // Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot).
 bool few_rows(const slimpipe_attn_params* p, int32_t top_k) { return rows_of(p) * top_k <= 4 * (int64_t)compute_units(); }
 
+// Items of a table, and workgroups of its launch: whole rounds of runs (xcd_item), one at least.
+int32_t whole_rounds(size_t n) { return (int32_t)((n + 8 * kXcdRun - 1) / (8 * kXcdRun) * (8 * kXcdRun)) + (n == 0 ? 8 * kXcdRun : 0); }
+
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where the parts of the workspace lie, and its size.
@@ -63,7 +69,7 @@ int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub) {
   const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units());
   return (int32_t)(rows < 2048 ? 2048 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
 }
-BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {
+BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)
   BlockWorkspace w;
   memset(&w, 0, sizeof(w));
   const size_t rows = (size_t)rows_of(p), planes = (size_t)p->batch * p->n_kv_heads, plane_rows = rows / planes;
@@ -76,11 +82,11 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.n_list_chunks = (int32_t)((plane_rows + kListRows - 1) / kListRows);
     // every tile but a block's last is full
     const size_t tiles = plane_rows * top_k / kBlockTileRows + blocks, slots = plane_rows * top_k;
-    w.item_cap = (int32_t)(tiles < 1 ? 1 : tiles < slots ? tiles : slots);
+    w.item_cap = whole_rounds(tiles < slots ? tiles : slots);
     w.ranks = take(planes * slots * 2);
     w.counts = take(planes * w.n_list_chunks * blocks * 4);
     w.lists = take(planes * blocks * sizeof(BlockList));
-    w.entries = take(planes * slots * sizeof(BlockEntry));
+    w.entries = take(planes * w.item_cap * kBlockTileRows * sizeof(BlockEntry));
     w.items = take(planes * w.item_cap * sizeof(BlockItem));
     w.n_items = take(planes * 4);
   }
@@ -92,8 +98,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.n_sub = (block_len + keys - 1) / keys;
     w.chunk_rows = dkdv_chunk_rows((int64_t)(rows * top_k), w.n_sub);
     // a list of n rows has at most n / chunk_rows + 1 parts, and partial sums only when n > chunk_rows: then at most twice n / chunk_rows
-    w.dkdv_cap = (int32_t)((slots / w.chunk_rows + blocks) * w.n_sub);
-    if (w.dkdv_cap < 1) w.dkdv_cap = 1;
+    w.dkdv_cap = whole_rounds((slots / w.chunk_rows + blocks) * w.n_sub);
     w.part_cap = (int32_t)(2 * slots / w.chunk_rows);
     w.dkdv_items = take(planes * w.dkdv_cap * sizeof(BlockItem));
     w.n_dkdv_items = take(planes * 4);
@@ -117,7 +122,7 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->kv_stride_b = p->kv_stride_b; a->kv_stride_s = p->kv_stride_s; a->kv_stride_h = p->kv_stride_h;
   a->o_stride_b = p->o_stride_b; a->o_stride_s = p->o_stride_s; a->o_stride_h = p->o_stride_h;
   a->do_stride_b = p->do_stride_b; a->do_stride_s = p->do_stride_s; a->do_stride_h = p->do_stride_h;
-  a->part_out = reinterpret_cast<float*>(ws + w.part_out);
+  a->part_out = ws + w.part_out;
   a->part_lse = reinterpret_cast<float*>(ws + w.part_lse);
   a->n_list_chunks = w.n_list_chunks;
   a->ranks = reinterpret_cast<uint16_t*>(ws + w.ranks);
@@ -171,7 +176,7 @@ int slimpipe_attn_block_select(const slimpipe_attn_params* p, const void* q_slic
   if (!q_slice || !means || !index) return SLIMPIPE_EINVAL_NULL;
   rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
   if (rc != SLIMPIPE_OK) return rc;
-  rc = check_top_k(p, top_k);
+  rc = check_top_k(p, top_k, 0);
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned16(q_slice) || !aligned16(means) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
   BlockSelectArgs a;
@@ -196,7 +201,7 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
   int rc = slimpipe_attn_validate(p, is_bwd);
   if (rc != SLIMPIPE_OK) return rc;
   rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
-  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k, is_bwd);
   if (rc != SLIMPIPE_OK) return rc;
   *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, top_k), is_bwd != 0).bytes;
   return SLIMPIPE_OK;
@@ -209,7 +214,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   if (rc != SLIMPIPE_OK) return rc;
   if (!q_slice || !k_chunks || !v_chunks || !index || !out || !lse) return SLIMPIPE_EINVAL_NULL;
   rc = check_blocks(p, n_chunks, chunk_len, block_len);
-  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k, 0);
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
   const bool few = few_rows(p, top_k);
@@ -223,7 +228,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
   a.out = out;
   a.lse = lse;
-  a.out_f32 = p->out_dtype == SLIMPIPE_F32;
+  a.out_f32 = a.part_f32 = p->out_dtype == SLIMPIPE_F32;
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (few) {
@@ -232,7 +237,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
     return SLIMPIPE_ELAUNCH;
   }
   PartMergeArgs m;
-  m.part_out = a.part_out; m.part_lse = a.part_lse; m.parts = top_k; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
+  m.part_out = a.part_out; m.part_f32 = a.part_f32; m.part_lse = a.part_lse; m.parts = top_k; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
   m.rows = rows_of(p);
   m.out = out; m.lse = lse;
   m.o_stride_b = p->o_stride_b; m.o_stride_s = p->o_stride_s; m.o_stride_h = p->o_stride_h;
@@ -247,7 +252,7 @@ int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, 
   if (rc != SLIMPIPE_OK) return rc;
   if (!q_slice || !k_chunks || !v_chunks || !index || !out || !d_out || !lse || !dq || !dk_chunks || !dv_chunks) return SLIMPIPE_EINVAL_NULL;
   rc = check_blocks(p, n_chunks, chunk_len, block_len);
-  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k);
+  if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k, 1);
   if (rc != SLIMPIPE_OK) return rc;
   if (dq_dtype != SLIMPIPE_BF16 && dq_dtype != SLIMPIPE_F32) return SLIMPIPE_EINVAL_SHAPE;
   if (dq_accumulate && dq_dtype != SLIMPIPE_F32) return SLIMPIPE_EINVAL_SHAPE;
@@ -268,7 +273,7 @@ int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, 
   fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
   a.d_out = static_cast<const __bf16*>(d_out);
   a.dq = dq;
-  a.dq_f32 = dq_dtype == SLIMPIPE_F32; a.dq_accumulate = dq_accumulate ? 1 : 0; a.dkv_accumulate = dkv_accumulate ? 1 : 0;
+  a.dq_f32 = a.part_f32 = dq_dtype == SLIMPIPE_F32; a.dq_accumulate = dq_accumulate ? 1 : 0; a.dkv_accumulate = dkv_accumulate ? 1 : 0;
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   // delta and lse in log2 units as for the dense backward, ahead of all that writes a gradient

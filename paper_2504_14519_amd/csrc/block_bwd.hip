@@ -27,13 +27,11 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int tile = xcd_run(blockIdx.x, a.n_items[plane]);
-  if (tile < 0) return;
-  const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
-  const int n_rows = it.count;
-  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
-  const int mine = wave_u * 32 + (lane & 31);
-  const BlockEntry e = list[mine < n_rows ? mine : n_rows - 1];
+  const TileRows rows(a, plane, wave_u, lane);
+  if (rows.none) return;
+  const BlockItem it = rows.item;
+  const BlockEntry e = rows.e;
+  const int n_rows = it.count, mine = rows.mine;
   const int h = hk * a.group + (int)(e.head_slot >> 6);
   const int64_t row = ((int64_t)b * a.n_q_heads + h) * a.s_q + e.row;
 
@@ -68,8 +66,8 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
     copy(0);
     bf16x8 q[KS], d_o[KS];
     {
-      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)e.row * a.q_stride_s + (int64_t)h * a.q_stride_h + 8 * g;
-      const bf16_t* op = a.d_out + (int64_t)b * a.do_stride_b + (int64_t)e.row * a.do_stride_s + (int64_t)h * a.do_stride_h + 8 * g;
+      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h + (int64_t)e.q_off * 8 + 8 * g;
+      const bf16_t* op = a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h + (int64_t)e.do_off * 8 + 8 * g;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) q[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
 #pragma unroll
@@ -118,32 +116,30 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
       __syncthreads();
     }
   }
-  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
-  put_rows<D>(part, dq, a.scale, lane);
-  const int64_t slot = row * a.top_k + (e.head_slot & 63u);
-  constexpr int PER = D / 4, RPP = 64 / PER;
-#pragma unroll
-  for (int j = 0; j < 32 / RPP; ++j) {
-    const int r = j * RPP + lane / PER;
-    const int64_t to = __shfl(slot, r, 64);
-    if (wave_u * 32 + r < n_rows)
-      *reinterpret_cast<f32x4*>(a.part_out + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
-  }
+  store_parts<D>(a, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dq, a.scale, row * a.top_k + (e.head_slot & 63u), n_rows, wave_u, lane);
 }
 
 // dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.
-template <int D>
+template <int D, bool F32>
 __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a) {
   constexpr int NC = D / 4;
   const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
   const int c = (int)(gid - row * NC) * 4;
   if (row >= (int64_t)a.batch * a.n_q_heads * a.s_q) return;
   const float* lp = a.part_lse + row * a.top_k;
-  const float* src = a.part_out + row * a.top_k * D + c;
   f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
   for (int s = 0; s < a.top_k; ++s)
-    if (lp[s] != -INFINITY) x += *reinterpret_cast<const f32x4*>(src + (int64_t)s * D);
+    if (lp[s] != -INFINITY) {
+      const int64_t at = (row * a.top_k + s) * D + c;
+      if constexpr (F32) {
+        x += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
+      } else {
+        const bf16x4 y = *reinterpret_cast<const bf16x4*>(static_cast<const bf16_t*>(a.part_out) + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += (float)y[e];
+      }
+    }
   const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
   const int64_t to = b * a.q_stride_b + (row - bh * a.s_q) * a.q_stride_s + (bh - b * a.n_q_heads) * a.q_stride_h + c;
   if (a.dq_f32) {
@@ -156,6 +152,8 @@ __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a)
 }
 
 // ------------------------------------------------------------------------------------ dk / dv
+// Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.
+SP_DEV int dkdv_run(int n_sub) { return n_sub > 1 ? 8 : 2; }
 int block_dkdv_keys(int block_len) { return block_len >= 128 ? 128 : 64; }
 
 template <int D, int NW>
@@ -173,11 +171,11 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int item = xcd_run(blockIdx.x, a.n_dkdv_items[plane]);
-  if (item < 0) return;
+  const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, dkdv_run(a.n_sub), plane));
+  if (item >= a.n_dkdv_items[plane]) return;
   const BlockItem it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
   const int block = it.block / a.n_sub, sub = it.block - block * a.n_sub, n_rows = it.count;
-  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
+  const BlockEntry* list = a.entries + (int64_t)plane * a.item_cap * kBlockTileRows + it.first;
 
   // keys [lo, hi) of the block that exist, the workgroup's first one
   const int64_t key0 = (int64_t)block * a.block_len + sub * KEYS;
@@ -214,20 +212,25 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   const bf16_t* const qb = a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h;
   const bf16_t* const ob = a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h;
   const int64_t stat0 = ((int64_t)b * a.n_q_heads + hk * a.group) * a.s_q;
-  auto entry = [&](int i) { return list[i < n_rows ? i : n_rows - 1]; };
-  BlockEntry ec[PASSES], es;                     // entries of the next tile to copy: the rows this thread copies, the row whose statistics it brings
+  auto entry = [&](int i) { return list + (i < n_rows ? i : n_rows - 1); };
+  struct { uint32_t q_off, do_off; } ec[PASSES];
+  struct { uint32_t row, head_slot; } es;        // entries of the next tile to copy: the rows this thread copies, the row whose statistics it brings
   auto fetch = [&](int u) {
 #pragma unroll
-    for (int n = 0; n < PASSES; ++n) ec[n] = entry(u * 32 + crow + n * RPP);
-    es = entry(u * 32 + (tid & 31));
+    for (int n = 0; n < PASSES; ++n) {
+      const BlockEntry* x = entry(u * 32 + crow + n * RPP);
+      ec[n] = {x->q_off, x->do_off};
+    }
+    const BlockEntry* x = entry(u * 32 + (tid & 31));
+    es = {x->row, x->head_slot};
   };
   auto copy = [&](int u) {
     const unsigned slot = lds + (u & 1) * 2 * L::TILE + wave_u * 1024;
 #pragma unroll
     for (int n = 0; n < PASSES; ++n) {
-      const int64_t hl = ec[n].head_slot >> 6, c8 = chunk_of(crow + n * RPP) * 8;
-      dma16_at(qb + hl * a.q_stride_h + (int64_t)ec[n].row * a.q_stride_s + c8, slot + n * T * 16);
-      dma16_at(ob + hl * a.do_stride_h + (int64_t)ec[n].row * a.do_stride_s + c8, slot + L::TILE + n * T * 16);
+      const int c8 = chunk_of(crow + n * RPP) * 8;
+      dma16_at(qb + (int64_t)ec[n].q_off * 8 + c8, slot + n * T * 16);
+      dma16_at(ob + (int64_t)ec[n].do_off * 8 + c8, slot + L::TILE + n * T * 16);
     }
   };
   float s_lse2, s_ndelta;
@@ -393,7 +396,7 @@ __global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs 
 }
 
 hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st) {
-  dim3 grid((unsigned)((a.item_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(256);
+  dim3 grid((unsigned)a.item_cap, (unsigned)(a.batch * a.n_kv_heads)), block(256);
   if (head_dim == 128) hipLaunchKernelGGL(block_dq_kernel<128>, grid, block, block_dq_lds_bytes<128>(), st, a);
   else hipLaunchKernelGGL(block_dq_kernel<64>, grid, block, block_dq_lds_bytes<64>(), st, a);
   return hipGetLastError();
@@ -401,13 +404,14 @@ hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st)
 hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
   const int64_t lanes = (int64_t)a.batch * a.n_q_heads * a.s_q * (head_dim / 4);
   dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
-  if (head_dim == 128) hipLaunchKernelGGL(block_dq_reduce_kernel<128>, grid, block, 0, st, a);
-  else hipLaunchKernelGGL(block_dq_reduce_kernel<64>, grid, block, 0, st, a);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
+  if (head_dim == 128) a.part_f32 ? go(block_dq_reduce_kernel<128, true>) : go(block_dq_reduce_kernel<128, false>);
+  else a.part_f32 ? go(block_dq_reduce_kernel<64, true>) : go(block_dq_reduce_kernel<64, false>);
   return hipGetLastError();
 }
 template <int D, int NW>
 static void launch_dkdv_t(const BlockArgs& a, hipStream_t st) {
-  dim3 grid((unsigned)((a.dkdv_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(NW * 64);
+  dim3 grid((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), block(NW * 64);
   hipLaunchKernelGGL((block_dkdv_kernel<D, NW>), grid, block, (BlockDkdvLds<D, NW>::TOTAL), st, a);
 }
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st) {

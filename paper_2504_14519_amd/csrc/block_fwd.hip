@@ -1,7 +1,10 @@
 // Forward of sparse attention over selected key blocks.
 //
 // A tile is up to 128 rows that chose one block (block_select.hip): four waves of 32 rows each, the block's keys in tiles of 64 through
-// two LDS slots.  Every (row, slot) leaves out and lse of its block's keys in 32 bits; part_merge.hip folds a row's slots.
+// two LDS slots.  Every (row, slot) leaves out and lse of its block's keys; part_merge.hip folds a row's slots in 32 bits.  Where the result is
+// bf16 so are the partial outs (lse is float32 always): their roundings, each half a step of a value whose weight is its share of the row,
+// add at most half a step of the weighted mean of |v|, no more than the rounding of the probabilities does, and the bytes of the partial
+// outs, which every one of them costs twice, are what the fold and a third of the tiles' epilogue take.
 #include "block_tile.hpp"
 #include "row_tile.hpp"
 #include "tile_common.hpp"
@@ -22,13 +25,11 @@ __global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int tile = xcd_run(blockIdx.x, a.n_items[plane]);
-  if (tile < 0) return;
-  const BlockItem it = a.items[(int64_t)plane * a.item_cap + tile];
-  const int n_rows = it.count;
-  const BlockEntry* list = a.entries + (int64_t)plane * a.group * a.s_q * a.top_k + it.first;
-  const int mine = wave_u * 32 + (lane & 31);
-  const BlockEntry e = list[mine < n_rows ? mine : n_rows - 1];
+  const TileRows rows(a, plane, wave_u, lane);
+  if (rows.none) return;
+  const BlockItem it = rows.item;
+  const BlockEntry e = rows.e;
+  const int n_rows = it.count, mine = rows.mine;
   const int h = hk * a.group + (int)(e.head_slot >> 6);
 
   const BlockKeys keys(a, it.block, b, hk);
@@ -60,7 +61,7 @@ __global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
   if (nt > 0) {
     copy(0);
     {
-      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)e.row * a.q_stride_s + (int64_t)h * a.q_stride_h + 8 * g;
+      const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h + (int64_t)e.q_off * 8 + 8 * g;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) st.q[ks] = *reinterpret_cast<const bf16x8*>(qp + 16 * ks);
     }
@@ -84,19 +85,9 @@ __global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
   }
   float lse;
   const float norm = st.finish(&lse);
-  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
-  put_rows<D>(part, st.o, norm, lane);
-  const int64_t row = ((int64_t)b * a.n_q_heads + h) * a.s_q + e.row;
-  const int64_t slot = row * a.top_k + (e.head_slot & 63u);
+  const int64_t slot = (((int64_t)b * a.n_q_heads + h) * a.s_q + e.row) * a.top_k + (e.head_slot & 63u);
   if (lane < 32 && mine < n_rows) a.part_lse[slot] = lse;
-  constexpr int PER = D / 4, RPP = 64 / PER;
-#pragma unroll
-  for (int j = 0; j < 32 / RPP; ++j) {
-    const int r = j * RPP + lane / PER;
-    const int64_t to = __shfl(slot, r, 64);
-    if (wave_u * 32 + r < n_rows)
-      *reinterpret_cast<f32x4*>(a.part_out + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
-  }
+  store_parts<D>(a, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, st.o, norm, slot, n_rows, wave_u, lane);
 }
 
 // Calls of few rows (tokens): lists and tiles of 128 rows would be mostly empty, so each (row, slot) has a workgroup of its own, whose four
@@ -187,13 +178,15 @@ __global__ __launch_bounds__(256) void block_fwd_few_kernel(const BlockArgs a) {
       o += acc_s[w][tid] * f;
     }
     const bool has = sum > 0.f;
-    a.part_out[item * D + tid] = has ? o / sum : 0.f;
+    const float r = has ? o / sum : 0.f;
+    if (a.part_f32) static_cast<float*>(a.part_out)[item * D + tid] = r;
+    else static_cast<bf16_t*>(a.part_out)[item * D + tid] = (bf16_t)r;
     if (tid == 0) a.part_lse[item] = has ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
   }
 }
 
 hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st) {
-  dim3 grid((unsigned)((a.item_cap + 7) / 8 * 8), (unsigned)(a.batch * a.n_kv_heads)), block(256);
+  dim3 grid((unsigned)a.item_cap, (unsigned)(a.batch * a.n_kv_heads)), block(256);
   if (head_dim == 128) hipLaunchKernelGGL(block_fwd_kernel<128>, grid, block, block_fwd_lds_bytes<128>(), st, a);
   else hipLaunchKernelGGL(block_fwd_kernel<64>, grid, block, block_fwd_lds_bytes<64>(), st, a);
   return hipGetLastError();

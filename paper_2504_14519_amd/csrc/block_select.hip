@@ -691,8 +691,9 @@ __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int 
   if (i >= n_slots || a.part_lse[at] != 0.f) return;
   const int j = a.index[at] - a.first_block, rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
   const BlockList list = a.lists[(int64_t)plane * a.n_blocks + j];
-  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * a.n_list_chunks + rh / kListRows] + a.ranks[at], to = list.first + pos;
-  a.entries[plane * n_slots + to] = {(uint32_t)(rh - hl * a.s_q), (uint32_t)(hl << 6 | slot)};
+  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * a.n_list_chunks + rh / kListRows] + a.ranks[at], to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
+  a.entries[(int64_t)plane * a.item_cap * kBlockTileRows + to] = {r, (uint32_t)(hl << 6 | slot), r * (uint32_t)(a.q_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.q_stride_h / 8),
+                                                                   r * (uint32_t)(a.do_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.do_stride_h / 8)};
   // the first row of a tile writes the tile down
   const uint32_t left = list.len - pos, block = (uint32_t)(a.first_block + j);
   if (pos % kBlockTileRows == 0)
@@ -716,28 +717,33 @@ SP_DEV uint32_t wave_scan(uint32_t v) {      // inclusive sum over the lanes up 
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
   return v;
 }
-SP_DEV uint32_t scan_add(uint32_t* tmp, int tid, uint32_t v, uint32_t* total) {      // exclusive scan over the workgroup
-  const int lane = tid & 63, wave = tid >> 6;
-  const uint32_t x = wave_scan(v);
+// Exclusive sums of four numbers a thread over the workgroup, and the totals.
+SP_DEV void scan_add(uint32_t (*tmp)[4], int tid, uint32_t (&v)[4], uint32_t (&total)[4]) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  uint32_t x[4];
   __syncthreads();
-  if (lane == 63) tmp[wave] = x;
-  __syncthreads();
-  uint32_t before = 0, all = 0;
-  for (int w = 0; w < kScanThreads / 64; ++w) {
-    if (w < wave) before += tmp[w];
-    all += tmp[w];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = wave_scan(v[i]);
+    if (lane == 63) tmp[wave][i] = x[i];
   }
-  *total = all;
-  return before + x - v;
+  __syncthreads();
+  static_assert(kScanThreads / 64 == 16, "the waves' sums along the lanes");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t upto = wave_scan(lane < 16 ? tmp[lane][i] : 0u);
+    total[i] = (uint32_t)__builtin_amdgcn_readlane((int)upto, 15);
+    v[i] = x[i] - v[i] + (wave > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, wave - 1) : 0u);
+  }
 }
 __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
-  __shared__ uint32_t tmp[kScanThreads / 64];
+  __shared__ uint32_t tmp[kScanThreads / 64][4];
   const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
   BlockList* lists = a.lists + (int64_t)plane * nb;
-  // a wave four blocks at a time, four chunks a lane
-  constexpr int WAVES = kScanThreads / 64, PER = 4;
+  // a wave eight blocks at a time, four chunks a lane
+  constexpr int WAVES = kScanThreads / 64, PER = 8;
   for (int j0 = tid >> 6; j0 < nb; j0 += PER * WAVES) {
-    uint32_t before[PER] = {0, 0, 0, 0};
+    uint32_t before[PER] = {};
     for (int c0 = 4 * lane; c0 - 4 * lane < nc; c0 += 256) {
       uint32_t v[PER][4];
 #pragma unroll
@@ -762,30 +768,20 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   }
   __threadfence_block();
   __syncthreads();
-  uint32_t first = 0, tile = 0, item = 0, part = 0;              // running totals of the blocks before
+  uint32_t before[4] = {0, 0, 0, 0};                             // entries, tiles, dk/dv items, partial sums of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    BlockList l;
-    l.len = j < nb ? lists[j].len : 0u;
-    uint32_t sum_len, sum_tiles, sum_items = 0, sum_parts = 0;
-    l.first = first + scan_add(tmp, tid, l.len, &sum_len);
-    l.tile0 = tile + scan_add(tmp, tid, (l.len + kBlockTileRows - 1) / kBlockTileRows, &sum_tiles);
-    l.item0 = l.parts = l.part0 = 0;
-    if (dkdv) {
-      const uint32_t chunks = (l.len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows;
-      l.parts = chunks > 1 ? chunks : 0u;
-      l.item0 = item + scan_add(tmp, tid, chunks * (uint32_t)a.n_sub, &sum_items);
-      l.part0 = part + scan_add(tmp, tid, l.parts, &sum_parts);
-    }
-    first += sum_len;
-    tile += sum_tiles;
-    item += sum_items;
-    part += sum_parts;
-    if (j < nb) lists[j] = l;
+    const uint32_t len = j < nb ? lists[j].len : 0u, chunks = dkdv ? (len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows : 0u;
+    const uint32_t parts = chunks > 1 ? chunks : 0u;
+    uint32_t v[4] = {len, (len + kBlockTileRows - 1) / kBlockTileRows, chunks * (uint32_t)a.n_sub, parts}, total[4];
+    scan_add(tmp, tid, v, total);
+    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], parts, before[3] + v[3]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) before[i] += total[i];
   }
   if (tid == 0) {
-    a.n_items[plane] = (int)tile;
-    if (dkdv) a.n_dkdv_items[plane] = (int)item;
+    a.n_items[plane] = (int)before[1];
+    if (dkdv) a.n_dkdv_items[plane] = (int)before[2];
   }
 }
 

@@ -19,6 +19,50 @@ struct BlockKeys {
   }
 };
 
+// This workgroup's tile of a plane and its lane's row of it.  What is read does not wait for each other: the number of tiles, the tile
+// and its rows.
+struct TileRows {
+  BlockItem item;
+  BlockEntry e;              // of the lane's row (lanes l and l + 32 have the same; rows past the tile's last: some row of the plane)
+  int mine;                  // its place in the tile; item.count or more: none
+  bool none;                 // no such tile
+  SP_DEV TileRows(const BlockArgs& a, int plane, int wave, int lane) {
+    const int tile = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, kXcdRun, plane));
+    mine = wave * 32 + (lane & 31);
+    const int n = a.n_items[plane];
+    item = a.items[(int64_t)plane * a.item_cap + tile];
+    e = a.entries[((int64_t)plane * a.item_cap + tile) * kBlockTileRows + mine];
+    none = tile >= n;
+    if (mine >= item.count) e = {0, 0, 0, 0};
+  }
+};
+// A wave's 32 rows in C layout, times `factor`, to the partial results at `slot` (of the lane's row), through `part` (kOutRow<D> * 32 floats of
+// LDS of the wave's own).
+template <int D>
+SP_DEV void store_parts(const BlockArgs& a, float* part, const f32x16 (&acc)[D / 32], float factor, int64_t slot, int n_rows, int wave, int lane) {
+  put_rows<D>(part, acc, factor, lane);
+  if (a.part_f32) {
+    constexpr int PER = D / 4, RPP = 64 / PER;
+#pragma unroll
+    for (int j = 0; j < 32 / RPP; ++j) {
+      const int r = j * RPP + lane / PER;
+      const int64_t to = __shfl(slot, r, 64);
+      if (wave * 32 + r < n_rows)
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.part_out) + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
+    }
+  } else {
+    constexpr int PER = D / 8, RPP = 64 / PER;
+#pragma unroll
+    for (int j = 0; j < 32 / RPP; ++j) {
+      const int r = j * RPP + lane / PER, d = lane % PER * 8;
+      const int64_t to = __shfl(slot, r, 64);
+      const bf16x4 lo = __builtin_convertvector(*reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d), bf16x4);
+      const bf16x4 hi = __builtin_convertvector(*reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d + 4), bf16x4);
+      if (wave * 32 + r < n_rows) *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.part_out) + to * D + d) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+}
+
 // Maximum of v over four waves (its lanes 32 .. 63 hold what 0 .. 31 do), through `tmp` in LDS, which is free again afterwards.
 SP_DEV int rows_max(int v, int* tmp, int wave, int lane) {
 #pragma unroll

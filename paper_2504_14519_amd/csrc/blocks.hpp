@@ -14,16 +14,18 @@ constexpr int kMaxTopK = 64;
 constexpr int kListRows = 256;
 constexpr int kListBlocks = 1024;
 constexpr int kBlockTileRows = 128;      // rows of a tile of the forward and dq kernels
+constexpr int kXcdRun = 16;              // tiles that follow each other on one XCD (xcd_item); the tables of items are whole rounds of eight runs
 
-// One row of a list: row of the slice and (head within the group << 6 | slot).
-struct BlockEntry { uint32_t row, head_slot; };
-// A tile of a list: block (absolute index), first entry within the plane's list, entries; the dk/dv items also have the part of the
+// One row of a list: row of the slice, (head within the group << 6 | slot), and where its q and d_out lie behind those of the plane's first
+// row, in units of 8 elements.  A block's list starts on a multiple of kBlockTileRows entries, so that tile t's are known without its item.
+struct BlockEntry { uint32_t row, head_slot, q_off, do_off; };
+// A tile of a list: block (absolute index), first entry within the plane's, entries; the dk/dv items also have the part of the
 // block's keys (in units of its workgroup's keys) and the plane's partial-sum slot, or -1 when the sums go straight to the accumulators
 struct BlockItem { int32_t block, first, count, part; };
 
-// The list of a block: first entry within the plane's, length, first tile, first dk/dv item; how many partial dk/dv sums it leaves (0: one
-// workgroup has all of it, or nobody) and the first of them
-struct BlockList { uint32_t first, len, tile0, item0, parts, part0, unused[2]; };
+// The list of a block: length, first tile, first dk/dv item; how many partial dk/dv sums it leaves (0: one workgroup has all of it, or
+// nobody) and the first of them
+struct BlockList { uint32_t len, tile0, item0, parts, part0, unused[3]; };
 
 struct BlockArgs {
   const __bf16* q;
@@ -43,12 +45,13 @@ struct BlockArgs {
   uint16_t* ranks;               // [plane][group * s_q * top_k]: place of a slot's row among the rows of its chunk that chose the block
   uint32_t* counts;              // [plane][n_blocks][chunk]: rows of the chunk that chose the block, then where they start in its list
   BlockList* lists;              // [plane][n_blocks]
-  BlockEntry* entries;           // [plane][group * s_q * top_k]
+  BlockEntry* entries;           // [plane][item_cap * kBlockTileRows]
   BlockItem* items;              // [plane][item_cap]
   int32_t* n_items;              // [plane]
   int32_t item_cap;
   // partial results (workspace), rows in the order (batch index, query head, row of the slice)
-  float* part_out;               // [row][top_k][head_dim]
+  void* part_out;                // [row][top_k][head_dim], float32 or bf16
+  int32_t part_f32;
   float* part_lse;               // [row][top_k]; -inf: the slot has no result
   void* out;
   float* lse;                    // forward: written.  backward: the saved one

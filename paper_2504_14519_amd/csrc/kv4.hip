@@ -124,14 +124,19 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   const int see_rel = see_far < -1 ? -1 : (int)see_far;
   const unsigned lds = lds_addr(smem);
 
-  // this thread's groups: group i of the tile is key i / NG (of K, then of V), group i % NG of its row
+  // This thread's groups: a wave takes 64 / NG keys of K or V at a time, 16 keys along its lanes (sixteen rows in a column of chunks: no bank
+  // twice in the LDS writes)
+  constexpr int KEYS = 64 / NG, RUNS = BN / KEYS;
+  const int grp = (lane >> 4) % NG;
+  auto group_kv = [&](int n) { return (n * 4 + wave_u) / RUNS; };
+  auto group_key = [&](int n) { return (n * 4 + wave_u) % RUNS * KEYS + (lane >> 4) / NG * 16 + (lane & 15); };
   const int64_t base = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + lo * a.kv_stride_s;
   u32x4 codes[PER];
   uint32_t scales[PER];
   auto fetch = [&](int t) {
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
-      const int i = n * 256 + tid, kv = i / (BN * NG), key = i / NG % BN, grp = i % NG;
+      const int kv = group_kv(n), key = group_key(n);
       const int k = t * BN + key < n_keys ? t * BN + key : n_keys - 1;      // (keys behind the last are not read)
       const int64_t at = base + (int64_t)k * a.kv_stride_s + grp * 32;
       const Kv4Operand& op = kv ? a.v : a.k;
@@ -142,7 +147,7 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   auto convert = [&](int t) {
 #pragma unroll
     for (int n = 0; n < PER; ++n) {
-      const int i = n * 256 + tid, kv = i / (BN * NG), key = i / NG % BN, grp = i % NG;
+      const int kv = group_kv(n), key = group_key(n);
       const float s = kv4_scale(scales[n]);
       char* tile = smem + (t & 1) * 2 * TILE + kv * TILE;
 #pragma unroll

@@ -22,10 +22,9 @@ SP_DEV void put_result(const PartMergeArgs& a, int64_t row, int d, f32x4 x0, f32
   if (d == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(l) * kLn2;
 }
 // Parts first, first + step, .. of 8 elements of a row: maximum of their lse, sum of weights, weighted sum.
-template <int D>
+template <int D, bool F32>
 SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, int step, f32x4& x0, f32x4& x1, float& m, float& l) {
   const float* lp = a.part_lse + row * a.parts;
-  const float* op = a.part_out + row * a.parts * D + d;
   m = -INFINITY;
   l = 0.f;
   x0 = x1 = f32x4{0, 0, 0, 0};
@@ -38,13 +37,21 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
     if (ls == -INFINITY) continue;
     const float w = exp2_fast((ls - m) * kLog2e);
     l += w;
-    x0 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D);
-    x1 += w * *reinterpret_cast<const f32x4*>(op + (int64_t)s * D + 4);
+    const int64_t at = (row * a.parts + s) * D + d;
+    if constexpr (F32) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
+      x0 += w * src[0];
+      x1 += w * src[1];
+    } else {
+      const bf16x8 x = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.part_out) + at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { x0[e] += w * (float)x[e]; x1[e] += w * (float)x[4 + e]; }
+    }
   }
 }
 
-// Many rows: D / 8 lanes a row.  Bound by the bytes (65536 rows of 8 parts of head_dim 128: 285 MB in 56 us).
-template <int D>
+// Many rows: D / 8 lanes a row.  Bound by the bytes.
+template <int D, bool F32>
 __global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) {
   constexpr int NC = D / 8;
   const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
@@ -52,20 +59,20 @@ __global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) 
   if (row >= a.rows) return;
   f32x4 x0, x1;
   float m, l;
-  fold_parts<D>(a, row, d, 0, 1, x0, x1, m, l);
+  fold_parts<D, F32>(a, row, d, 0, 1, x0, x1, m, l);
   put_result(a, row, d, x0, x1, m, l);
 }
 
 // Few rows: a workgroup has 32 elements of one row, and its 64 sets of four lanes share out the parts, where the chain of dependent loads of
 // one set would be the time.  Sets of a wave are folded by exchanges, the waves through LDS, always in the same order.
-template <int D>
+template <int D, bool F32>
 __global__ __launch_bounds__(256) void part_merge_few_kernel(const PartMergeArgs a) {
   __shared__ float acc_s[4][32], m_s[4], l_s[4];
   const int64_t row = blockIdx.x;
   const int set = threadIdx.x / 4, c = threadIdx.x % 4, d = blockIdx.y * 32 + c * 8, wave = threadIdx.x >> 6;
   f32x4 x0, x1;
   float m, l;
-  fold_parts<D>(a, row, d, set, 64, x0, x1, m, l);
+  fold_parts<D, F32>(a, row, d, set, 64, x0, x1, m, l);
 #pragma unroll
   for (int w = 4; w < 64; w <<= 1) {
     const float mo = __shfl_xor(m, w, 64), lo = __shfl_xor(l, w, 64), mx = fmaxf(m, mo), me = mx == -INFINITY ? 0.f : mx;
@@ -99,16 +106,14 @@ __global__ __launch_bounds__(256) void part_merge_few_kernel(const PartMergeArgs
   put_result(a, row, d, x0, x1, m, l);
 }
 
+template <int D, bool F32>
+static void launch_merge_t(const PartMergeArgs& a, hipStream_t st) {
+  if (a.rows <= 1024 && a.parts > 4) hipLaunchKernelGGL((part_merge_few_kernel<D, F32>), dim3((unsigned)a.rows, D / 32), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((part_merge_kernel<D, F32>), dim3((unsigned)((a.rows * (D / 8) + 255) / 256)), dim3(256), 0, st, a);
+}
 hipError_t launch_part_merge(const PartMergeArgs& a, int head_dim, hipStream_t st) {
-  if (a.rows <= 1024 && a.parts > 4) {
-    dim3 grid((unsigned)a.rows, (unsigned)(head_dim / 32));
-    if (head_dim == 128) hipLaunchKernelGGL(part_merge_few_kernel<128>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(part_merge_few_kernel<64>, grid, dim3(256), 0, st, a);
-  } else {
-    dim3 grid((unsigned)((a.rows * (head_dim / 8) + 255) / 256));
-    if (head_dim == 128) hipLaunchKernelGGL(part_merge_kernel<128>, grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(part_merge_kernel<64>, grid, dim3(256), 0, st, a);
-  }
+  if (head_dim == 128) a.part_f32 ? launch_merge_t<128, true>(a, st) : launch_merge_t<128, false>(a, st);
+  else a.part_f32 ? launch_merge_t<64, true>(a, st) : launch_merge_t<64, false>(a, st);
   return hipGetLastError();
 }
 

@@ -479,6 +479,12 @@ SP_DEV int xcd_run(int index, int n) {
   return (index >> 3) < per && t < n ? t : -1;
 }
 
+// The same without the number of items: runs of `run` items, run r on XCD (r + first) mod 8.  Grid: a multiple of 8 * run.
+SP_DEV int xcd_item(int index, int run, int first) {
+  const int slot = index >> 3;
+  return ((slot / run) * 8 + ((index - first) & 7)) * run + slot % run;
+}
+
 // ---- scheduling helpers ------------------------------------------------------------------------
 #define SP_FENCE() __builtin_amdgcn_sched_barrier(0)
 // Issue priority of a wave while it is in a matrix phase.  Waves are served oldest first, so without
