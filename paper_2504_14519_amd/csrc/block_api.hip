@@ -60,11 +60,11 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where the parts of the workspace lie, and its size.
 struct BlockWorkspace {
-  size_t part_out, part_lse, ranks, counts, lists, entries, items, n_items, delta, lse2, dkdv_items, n_dkdv_items, dkdv_part, bytes;
+  size_t part_out, part_lse, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
 // Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but 2048 at least, because every part of
-// a list writes its sums (128 KB for 128 keys of head_dim 128) and a reduce reads them again.
+// a list writes its sums (256 KB for 256 keys of head_dim 128) and a reduce reads them again.
 int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub) {
   const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units());
   return (int32_t)(rows < 2048 ? 2048 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
@@ -84,7 +84,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     const size_t tiles = plane_rows * top_k / kBlockTileRows + blocks, slots = plane_rows * top_k;
     w.item_cap = whole_rounds(tiles < slots ? tiles : slots);
     w.ranks = take(planes * slots * 2);
-    w.counts = take(planes * w.n_list_chunks * blocks * 4);
+    w.counts = take(planes * count_stride(w.n_list_chunks) * blocks * 4);
     w.lists = take(planes * blocks * sizeof(BlockList));
     w.entries = take(planes * w.item_cap * kBlockTileRows * sizeof(BlockEntry));
     w.items = take(planes * w.item_cap * sizeof(BlockItem));
@@ -93,6 +93,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
   if (is_bwd) {
     w.delta = take(rows * 4);
     w.lse2 = take(rows * 4);
+    w.inf = take(4);
     const size_t slots = plane_rows * top_k;
     const int32_t keys = block_dkdv_keys(block_len);
     w.n_sub = (block_len + keys - 1) / keys;
@@ -134,6 +135,7 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->item_cap = w.item_cap;
   a->delta = reinterpret_cast<float*>(ws + w.delta);
   a->lse2 = reinterpret_cast<float*>(ws + w.lse2);
+  a->inf = reinterpret_cast<float*>(ws + w.inf);
   a->chunk_rows = w.chunk_rows; a->n_sub = w.n_sub; a->dkdv_cap = w.dkdv_cap; a->part_cap = w.part_cap;
   a->dkdv_items = reinterpret_cast<BlockItem*>(ws + w.dkdv_items);
   a->n_dkdv_items = reinterpret_cast<int32_t*>(ws + w.n_dkdv_items);

@@ -5,10 +5,11 @@
 //   dQ_i = scale sum_j dS_ij k_j      dK_j  = scale sum_i dS_ij q_i
 // As in the dense backward dq and dk/dv have kernels of their own, both over the lists of block_select.hip:
 //   dq     tiles of 128 rows of one block, as in the forward; each (row, slot) leaves a partial dq that a last kernel adds in slot order
-//   dk/dv  a workgroup owns 128 (block length 64: 64) keys and walks the rows that chose their block, 32 at a time; long lists are
+//   dk/dv  a workgroup owns 256 keys (128 or 64 in small blocks) and walks the rows that chose their block, 32 at a time; long lists are
 //          cut into parts whose sums a last kernel adds in list order.
 // No sum depends on the order in which workgroups run.
 #include "block_tile.hpp"
+#include "dkdv_tile.hpp"
 #include "row_tile.hpp"
 
 namespace slimpipe {
@@ -154,7 +155,85 @@ __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a)
 // ------------------------------------------------------------------------------------ dk / dv
 // Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.
 SP_DEV int dkdv_run(int n_sub) { return n_sub > 1 ? 8 : 2; }
-int block_dkdv_keys(int block_len) { return block_len >= 128 ? 128 : 64; }
+// Keys of a workgroup: 256 where whole blocks are made of them but for a part too small to matter, else 128, or 64 in the smallest blocks.
+static bool wide_dkdv(int block_len) { return block_len % 256 == 0 || block_len % 256 > 128 || block_len >= 1024; }
+int block_dkdv_keys(int block_len) { return wide_dkdv(block_len) ? 256 : block_len >= 128 ? 128 : 64; }
+
+// What a dk/dv item has: keys [kmin, kmax) of the workgroup's KEYS exist, the first of them all lies at element `off` of chunk `chunk`.
+template <int D, int KEYS>
+struct DkdvItem {
+  BlockItem it;
+  const BlockEntry* list;
+  int sub, kmin, kmax, chunk;
+  int64_t key0, off;
+  bool none;
+  SP_DEV DkdvItem(const BlockArgs& a, int plane, int b, int hk) {
+    const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, dkdv_run(a.n_sub), plane));
+    none = item >= a.n_dkdv_items[plane];
+    if (none) return;
+    it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
+    const int block = it.block / a.n_sub;
+    sub = it.block - block * a.n_sub;
+    list = a.entries + (int64_t)plane * a.item_cap * kBlockTileRows + it.first;
+    key0 = (int64_t)block * a.block_len + sub * KEYS;
+    const int64_t end = (int64_t)(block + 1) * a.block_len < a.kv_end ? (int64_t)(block + 1) * a.block_len : a.kv_end;
+    kmin = a.kv_begin > key0 ? (a.kv_begin - key0 < KEYS ? (int)(a.kv_begin - key0) : KEYS) : 0;
+    kmax = end - key0 < KEYS ? (int)(end - key0) : KEYS;
+    none = kmax <= kmin;
+    chunk = kv_chunk_of(a.kv, key0);
+    off = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + (key0 - (int64_t)chunk * a.kv.len) * a.kv_stride_s;
+  }
+  // K rows of the lane's key (clamped to those that exist) as B operand: k-slots = head_dim 16 ks + 8 g ..
+  SP_DEV void load_k(const BlockArgs& a, int key, int g, bf16x8 (&kreg)[D / 16]) const {
+    const int kc = key < kmin ? kmin : (key < kmax ? key : kmax - 1);
+    const bf16_t* kp = a.kv.k[chunk] + off + (int64_t)kc * a.kv_stride_s + 8 * g;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) kreg[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
+  }
+  // the wave's 32 V rows to LDS (a wave without keys copies nothing; what its columns come to is not stored)
+  SP_DEV void copy_v(const BlockArgs& a, unsigned lds, int w0, int lane) const {
+    WaveDma<D, 32> dma;
+    dma.init(lane, (uint32_t)a.kv_stride_s * 2);
+    if (kmax > w0 && kmin - w0 < 32)
+      dma.copy(lds, a.kv.v[chunk] + off + (int64_t)w0 * a.kv_stride_s, (uint32_t)a.kv_stride_s * 2, kmin > w0 ? kmin - w0 : 0, kmax - w0, lane);
+  }
+  // rows [kmin, kmax) of dk and dv of the wave: to the accumulators, or to the partial sums of this part of the list; `part`: kOutRow<D> * 32
+  // floats of LDS of the wave's own
+  SP_DEV void flush(const BlockArgs& a, int plane, float* part, const f32x16 (&dk)[D / 32], const f32x16 (&dv)[D / 32], int w0, int lane) const {
+    const int keys_pad = a.n_sub * KEYS;
+    float *kdst, *vdst;
+    int64_t stride;
+    bool accumulate = false;
+    if (it.part >= 0) {
+      kdst = a.dkdv_part + (((int64_t)plane * a.part_cap + it.part) * 2 * keys_pad + sub * KEYS) * D;
+      vdst = kdst + (int64_t)keys_pad * D;
+      stride = D;
+    } else {
+      kdst = a.dk_acc[chunk] + off;
+      vdst = a.dv_acc[chunk] + off;
+      stride = a.kv_stride_s;
+      accumulate = a.dkv_accumulate != 0;
+    }
+    constexpr int PER = D / 4, RPP = 64 / PER;
+    const int d4 = lane % PER * 4;
+    auto put = [&](const f32x16 (&acc)[D / 32], float factor, float* dst) {
+      put_rows<D>(part, acc, factor, lane);
+#pragma unroll
+      for (int j = 0; j < 32 / RPP; ++j) {
+        const int r = j * RPP + lane / PER, kr = w0 + r;
+        if (kr < kmin || kr >= kmax) continue;
+        f32x4 v = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d4);
+        f32x4* to = reinterpret_cast<f32x4*>(dst + (int64_t)kr * stride + d4);
+        if (accumulate) v += *to;
+        *to = v;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    };
+    put(dk, a.scale, kdst);
+    put(dv, 1.0f, vdst);
+  }
+};
 
 template <int D, int NW>
 struct BlockDkdvLds {
@@ -171,39 +250,16 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, dkdv_run(a.n_sub), plane));
-  if (item >= a.n_dkdv_items[plane]) return;
-  const BlockItem it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
-  const int block = it.block / a.n_sub, sub = it.block - block * a.n_sub, n_rows = it.count;
-  const BlockEntry* list = a.entries + (int64_t)plane * a.item_cap * kBlockTileRows + it.first;
-
-  // keys [lo, hi) of the block that exist, the workgroup's first one
-  const int64_t key0 = (int64_t)block * a.block_len + sub * KEYS;
-  const int64_t end = (int64_t)(block + 1) * a.block_len < a.kv_end ? (int64_t)(block + 1) * a.block_len : a.kv_end;
-  const int kmin = a.kv_begin > key0 ? (a.kv_begin - key0 < KEYS ? (int)(a.kv_begin - key0) : KEYS) : 0;
-  const int kmax = end - key0 < KEYS ? (int)(end - key0) : KEYS;          // keys [kmin, kmax) of the workgroup exist
-  if (kmax <= kmin) return;
-  const int chunk = kv_chunk_of(a.kv, key0);
-  const int64_t off = (int64_t)b * a.kv_stride_b + (int64_t)hk * a.kv_stride_h + (key0 - (int64_t)chunk * a.kv.len) * a.kv_stride_s;
+  const DkdvItem<D, KEYS> item(a, plane, b, hk);
+  if (item.none) return;
+  const int n_rows = item.it.count;
+  const BlockEntry* const list = item.list;
+  const int64_t key0 = item.key0;
   const unsigned lds = lds_addr(smem);
-
-  // K as B operand: column = my key (clamped to those that exist), k-slots = head_dim 16 ks + 8 g ..; V rows in LDS
   const int key = wave_u * 32 + ql;
   bf16x8 kreg[KS];
-  {
-    const int kc = key < kmin ? kmin : (key < kmax ? key : kmax - 1);
-    const bf16_t* kp = a.kv.k[chunk] + off + (int64_t)kc * a.kv_stride_s + 8 * g;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) kreg[ks] = *reinterpret_cast<const bf16x8*>(kp + 16 * ks);
-  }
-  {
-    const bf16_t* vp = a.kv.v[chunk] + off;
-    WaveDma<D, 32> dma;
-    dma.init(lane, (uint32_t)a.kv_stride_s * 2);
-    const int w0 = wave_u * 32;
-    const int first = kmin > w0 ? (kmin - w0 < 32 ? kmin - w0 : 31) : 0, avail = kmax - w0 > 0 ? kmax - w0 : 0;
-    if (avail > 0 && kmin - w0 < 32) dma.copy(lds + L::V + w0 * D * 2, vp + (int64_t)w0 * a.kv_stride_s, (uint32_t)a.kv_stride_s * 2, first, avail, lane);
-  }
+  item.load_k(a, key, g, kreg);
+  item.copy_v(a, lds + L::V + wave_u * 32 * D * 2, wave_u * 32, lane);
   // This thread's part of a tile copy: rows tid / NC + n * RPP, the chunk that the swizzle puts at its place.
   const int crow = tid / NC, cpos = tid % NC;
   auto chunk_of = [&](int r) {
@@ -327,40 +383,147 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
     __syncthreads();
   }
 
-  // rows [kmin, kmax) of the workgroup: to the accumulators, or to the partial sums of this part of the list
-  const int keys_pad = a.n_sub * KEYS;
-  float *kdst, *vdst;
-  int64_t stride;
-  bool accumulate = false;
-  if (it.part >= 0) {
-    kdst = a.dkdv_part + (((int64_t)plane * a.part_cap + it.part) * 2 * keys_pad + sub * KEYS) * D;
-    vdst = kdst + (int64_t)keys_pad * D;
-    stride = D;
-  } else {
-    kdst = a.dk_acc[chunk] + off;
-    vdst = a.dv_acc[chunk] + off;
-    stride = a.kv_stride_s;
-    accumulate = a.dkv_accumulate != 0;
-  }
-  float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
-  constexpr int PER = D / 4, OPP = 64 / PER;
-  const int d4 = lane % PER * 4;
-  auto flush = [&](const f32x16 (&acc)[DB], float factor, float* dst) {
-    put_rows<D>(part, acc, factor, lane);
+  item.flush(a, plane, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dk, dv, wave_u * 32, lane);
+}
+
+// Blocks of 256 keys and more: the phases of the dense dk/dv kernel (dkdv_tile.hpp, attn_bwd.hip) on gathered rows.  Eight waves of 32 keys; waves
+// 0-3 and 4-7 alternate matrix and vector phases one phase apart; rings of four slots; the group that is in a vector phase copies tile u + 2:
+// group A rows of Q, their statistics and row numbers, group B rows of dO, each lane from the address that its row's entry gives (fetched
+// one phase earlier).  8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: WIDE_US us; four waves of 32 keys, two workgroups a compute unit and
+// no phases 332.
+template <int D>
+struct WideLds {
+  using L = DkdvLds<D, 8, 32>;
+  static constexpr int STAT_BYTES = 512;                   // lse2, -delta, row of the slice of the tile's 32 rows; 32 unused
+  static constexpr int RINGS = L::STAT_BASE + L::SLOTS * STAT_BYTES, TOTAL = RINGS > L::OUT_BYTES ? RINGS : L::OUT_BYTES;
+};
+template <int D>
+__global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a) {
+  using L = DkdvLds<D, 8, 32>;
+  using W = WideLds<D>;
+  constexpr int KS = D / 16, DB = D / 32, NC = D / 8, GT = 256, RPP = GT / NC, PASSES = 32 / RPP, SLOTS = L::SLOTS, TILE = L::TILE_BYTES;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool group_b = wave_u >= 4;
+  const int plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const DkdvItem<D, 256> item(a, plane, b, hk);
+  if (item.none) return;
+  const int n_rows = item.it.count, cnt = (n_rows + 31) / 32;
+  const BlockEntry* const list = item.list;
+  const unsigned lds = lds_addr(smem);
+
+  DkdvState<D, 32> st;
 #pragma unroll
-    for (int j = 0; j < 32 / OPP; ++j) {
-      const int r = j * OPP + lane / PER, kr = wave_u * 32 + r;
-      if (kr < kmin || kr >= kmax) continue;
-      f32x4 v = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d4);
-      f32x4* to = reinterpret_cast<f32x4*>(dst + (int64_t)kr * stride + d4);
-      if (accumulate) v += *to;
-      *to = v;
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { st.dk[db][i] = 0.f; st.dv[db][i] = 0.f; }
+  item.load_k(a, wave_u * 32 + ql, g, st.kreg);
+  item.copy_v(a, lds + L::V_BASE + wave_u * 32 * D * 2, wave_u * 32, lane);
+
+  // this group's operand, and its thread's part of a tile copy: rows crow + n * RPP, the chunk that the swizzle puts at its place
+  const int gtid = tid & (GT - 1), crow = gtid / NC, cpos = gtid % NC;
+  const int c8 = (D == 128 ? ((((cpos >> 2) ^ crow) & 3) << 2) | (((cpos & 3) ^ (crow >> 2)) & 3) : (cpos ^ crow) & (NC - 1)) * 8;
+  static_assert(RPP % 16 == 0, "the rows of a thread have one swizzle phase");
+  const bf16_t* const src = (group_b ? a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h
+                                     : a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h) + c8;
+  const uint32_t* const offs = group_b ? &list->do_off : &list->q_off;
+  const int64_t stat0 = ((int64_t)b * a.n_q_heads + hk * a.group) * a.s_q;
+  struct Next { uint32_t off[PASSES], row, head_slot; } nx;      // of the next tile to copy
+  auto fetch = [&](int u) {
+    const int first = (u < cnt ? u : cnt - 1) * 32;
+#pragma unroll
+    for (int n = 0; n < PASSES; ++n) {
+      const int i = first + crow + n * RPP;
+      nx.off[n] = offs[(i < n_rows ? i : n_rows - 1) * (int)(sizeof(BlockEntry) / 4)];
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    if (!group_b) {
+      const int i = first + (lane & 31);
+      const BlockEntry* e = list + (i < n_rows ? i : n_rows - 1);
+      nx.row = e->row;
+      nx.head_slot = e->head_slot;
+    }
   };
-  flush(dk, a.scale, kdst);
-  flush(dv, 1.0f, vdst);
+  auto copy_part = [&](int u, int part) {
+    const unsigned slot = (unsigned)(u & (SLOTS - 1));
+    if (part < PASSES)
+      dma16_at(src + (int64_t)nx.off[part] * 8, lds + (group_b ? L::DO_BASE : L::Q_BASE) + slot * TILE + part * GT * 16 + (wave_u & 3) * 1024);
+    if (part == 2 && !group_b) {                           // (all four waves: the same data, no branch)
+      const int i = (u < cnt ? u : cnt - 1) * 32 + (lane & 31);
+      const int64_t at = stat0 + (int64_t)(nx.head_slot >> 6) * a.s_q + nx.row;
+      const float* from = lane < 32 ? (i < n_rows ? a.lse2 + at : a.inf) : a.delta + at;      // (rows past the list's end: p = 0)
+      dma4_at(from, lds + L::STAT_BASE + slot * W::STAT_BYTES);
+      dma4_at(&list[i < n_rows ? i : n_rows - 1].row, lds + L::STAT_BASE + slot * W::STAT_BYTES + 256);
+    }
+  };
+  auto copy_all = [&](int u) {
+#pragma unroll
+    for (int part = 0; part < 3; ++part) copy_part(u, part);
+  };
+  fetch(0);
+  copy_all(0);
+  fetch(1);
+  copy_all(1);
+  fetch(2);
+  wait_async();
+  TrBase<D> lo_qt;         // Q(u-1), transposed
+  RpBase<D> lo_q, lo_v;    // Q(u) and this wave's V rows, row-packed
+  lo_qt.init(lane, (int)lds + L::Q_BASE + (SLOTS - 1) * TILE);     // "Q(-1)": never read
+  lo_q.init(lane, (int)lds + L::Q_BASE);
+  lo_v.init(lane, (int)lds + L::V_BASE + wave_u * 32 * D * 2);
+  __syncthreads();
+
+  int slot = 0;            // ring slot of tile u
+  auto advance = [&]() {
+    lo_q.add(slot == SLOTS - 1 ? -(SLOTS - 1) * TILE : TILE);
+    lo_qt.add(slot == 0 ? -(SLOTS - 1) * TILE : TILE);      // Q(u-1) sits in slot - 1
+    slot = (slot == SLOTS - 1) ? 0 : slot + 1;
+  };
+  auto stat_of = [&](int u) { return reinterpret_cast<const float*>(smem + L::STAT_BASE + (u & (SLOTS - 1)) * W::STAT_BYTES) + 4 * ((fresh(tid) >> 5) & 1); };
+  // Rows of the slice from here on see the lane's key (at most s_q; without a mask: all), and whether some row of the call sees only a part
+  // of the workgroup's keys
+  const int64_t see = a.causal ? item.key0 + wave_u * 32 + ql - a.q_offset : 0;
+  const int first_row = see < 0 ? 0 : see < a.s_q ? (int)see : a.s_q;
+  const bool diagonal = a.causal && item.key0 + item.kmax - 1 > a.q_offset;
+  const float c = a.scale_log2e;
+  auto vector_phase = [&](int u) {
+    if (diagonal) {
+      const int* rows = reinterpret_cast<const int*>(stat_of(u)) + 64;
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4 r = *reinterpret_cast<const i32x4*>(rows + 8 * i4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (r[e] < first_row) { st.s[0][4 * i4 + e] = -INFINITY; st.dp[0][4 * i4 + e] = 0.f; }      // (what no row sees may be NaN)
+      }
+    }
+    dkdv_vector_phase<D, 32>(st, c, false, 0, 32, 0, [&](int part) {
+      if (part < 3) copy_part(u + 2, part);
+      else fetch(u + 3);
+    });
+  };
+  // Both groups run the same code; group B starts one phase (one barrier) later and group A idles one phase at the end.
+  if (group_b) phase_end();
+  { DkdvMatrixPhase<D, 8, 32, false, true, 2> ph{lo_qt, lo_q, lo_v, st, stat_of(0)}; ph.run(); }     // scores of tile 0
+  advance();
+  wait_async();
+  phase_end();
+  for (int u = 0; u + 1 < cnt; ++u) {
+    vector_phase(u);
+    phase_end();
+    asm volatile("" : "+v"(lo_v.off0));      // (V never moves: without this the offsets of its blocks are kept in registers across the loop)
+    { DkdvMatrixPhase<D, 8, 32, true, true, 2> ph{lo_qt, lo_q, lo_v, st, stat_of(u + 1)}; ph.run(); }    // sums of tile u, scores of tile u+1
+    advance();
+    wait_async();                            // the copies of the vector phase before have landed
+    phase_end();
+  }
+  vector_phase(cnt - 1);
+  phase_end();
+  { DkdvMatrixPhase<D, 8, 32, true, false, 2> ph{lo_qt, lo_q, lo_v, st, nullptr}; ph.run(); }     // sums of the last tile
+  wait_async();
+  phase_end();
+  if (!group_b) phase_end();
+  item.flush(a, plane, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, st.dk, st.dv, wave_u * 32, fresh(tid) & 63);
 }
 
 // dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.
@@ -414,10 +577,16 @@ static void launch_dkdv_t(const BlockArgs& a, hipStream_t st) {
   dim3 grid((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), block(NW * 64);
   hipLaunchKernelGGL((block_dkdv_kernel<D, NW>), grid, block, (BlockDkdvLds<D, NW>::TOTAL), st, a);
 }
+template <int D>
+static void launch_dkdv_d(const BlockArgs& a, hipStream_t st) {
+  const int keys = block_dkdv_keys(a.block_len);
+  if (keys == 256) hipLaunchKernelGGL(block_dkdv_wide_kernel<D>, dim3((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), dim3(512), WideLds<D>::TOTAL, st, a);
+  else if (keys == 128) launch_dkdv_t<D, 4>(a, st);
+  else launch_dkdv_t<D, 2>(a, st);
+}
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st) {
-  const bool wide = block_dkdv_keys(a.block_len) == 128;
-  if (head_dim == 128) wide ? launch_dkdv_t<128, 4>(a, st) : launch_dkdv_t<128, 2>(a, st);
-  else wide ? launch_dkdv_t<64, 4>(a, st) : launch_dkdv_t<64, 2>(a, st);
+  if (head_dim == 128) launch_dkdv_d<128>(a, st);
+  else launch_dkdv_d<64>(a, st);
   return hipGetLastError();
 }
 hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
@@ -434,6 +603,8 @@ hipError_t opt_in_block_bwd_kernels() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<128>), attr, (int)block_dq_lds_bytes<128>());
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<64>), attr, (int)block_dq_lds_bytes<64>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_wide_kernel<128>), attr, WideLds<128>::TOTAL);
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_wide_kernel<64>), attr, WideLds<64>::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 4>), attr, (int)BlockDkdvLds<128, 4>::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 2>), attr, (int)BlockDkdvLds<128, 2>::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<64, 4>), attr, (int)BlockDkdvLds<64, 4>::TOTAL);

@@ -643,9 +643,9 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
   float* valid = a.part_lse + first;                 // -inf: the slot has no block (and no result)
   uint16_t* rank = a.ranks + first;
   const int n_slots = n_rows * a.top_k;
-  uint32_t* counts = a.counts + (int64_t)plane * a.n_blocks * a.n_list_chunks + chunk;
+  uint32_t* counts = a.counts + (int64_t)plane * a.n_blocks * count_stride(a.n_list_chunks) + chunk;
   for (int i = tid; i < n_slots; i += kListThreads) index[i] = a.index[first + i];
-  __syncthreads();
+  lds_barrier();
   const float per_row = 1.0f / (float)a.top_k;
   auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per_row); };      // i / top_k (i < 2^14: the half keeps it off the border)
   static_assert(kListRows * kMaxTopK <= 1 << 14 && kListRows * kMaxTopK <= 32 * kListThreads, "slots of a chunk: exact quotients, a bit each");
@@ -660,12 +660,12 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
     const int n = a.n_blocks - w0 < kListBlocks ? a.n_blocks - w0 : kListBlocks;
     uint16_t* below = reinterpret_cast<uint16_t*>(bits + n * kListStride);
     for (int i = tid; i < n * kListStride; i += kListThreads) bits[i] = 0u;
-    __syncthreads();
+    lds_barrier();
     for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
       const int j = index[i] - a.first_block - w0, row = row_of(i);
       if (((ok >> u) & 1u) && j >= 0 && j < n) atomicOr(&bits[j * kListStride + (row >> 5)], 1u << (row & 31));
     }
-    __syncthreads();
+    lds_barrier();
     for (int j = tid; j < n; j += kListThreads) {
       uint32_t c = 0;
 #pragma unroll
@@ -673,15 +673,15 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
         below[j * kListStride + w] = (uint16_t)c;
         c += __popc(bits[j * kListStride + w]);
       }
-      counts[(int64_t)(w0 + j) * a.n_list_chunks] = c;
+      counts[(int64_t)(w0 + j) * count_stride(a.n_list_chunks)] = c;
     }
-    __syncthreads();
+    lds_barrier();
     for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
       const int j = index[i] - a.first_block - w0, row = row_of(i);
       if (((ok >> u) & 1u) && j >= 0 && j < n)
         rank[i] = (uint16_t)(below[j * kListStride + (row >> 5)] + __popc(bits[j * kListStride + (row >> 5)] & ((1u << (row & 31)) - 1u)));
     }
-    __syncthreads();
+    lds_barrier();
   }
 }
 
@@ -691,7 +691,7 @@ __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int 
   if (i >= n_slots || a.part_lse[at] != 0.f) return;
   const int j = a.index[at] - a.first_block, rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
   const BlockList list = a.lists[(int64_t)plane * a.n_blocks + j];
-  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * a.n_list_chunks + rh / kListRows] + a.ranks[at], to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
+  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * count_stride(a.n_list_chunks) + rh / kListRows] + a.ranks[at], to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
   a.entries[(int64_t)plane * a.item_cap * kBlockTileRows + to] = {r, (uint32_t)(hl << 6 | slot), r * (uint32_t)(a.q_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.q_stride_h / 8),
                                                                    r * (uint32_t)(a.do_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.do_stride_h / 8)};
   // the first row of a tile writes the tile down
@@ -721,13 +721,13 @@ SP_DEV uint32_t wave_scan(uint32_t v) {      // inclusive sum over the lanes up 
 SP_DEV void scan_add(uint32_t (*tmp)[4], int tid, uint32_t (&v)[4], uint32_t (&total)[4]) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t x[4];
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[i] = wave_scan(v[i]);
     if (lane == 63) tmp[wave][i] = x[i];
   }
-  __syncthreads();
+  lds_barrier();
   static_assert(kScanThreads / 64 == 16, "the waves' sums along the lanes");
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -737,41 +737,55 @@ SP_DEV void scan_add(uint32_t (*tmp)[4], int tid, uint32_t (&v)[4], uint32_t (&t
   }
 }
 __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
-  __shared__ uint32_t tmp[kScanThreads / 64][4];
+  constexpr int kLens = 8192;                                    // lengths that pass through LDS (more: through memory)
+  __shared__ uint32_t tmp[kScanThreads / 64][4], len_s[kLens];
   const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
+  const bool in_lds = nb <= kLens;
   BlockList* lists = a.lists + (int64_t)plane * nb;
   // a wave eight blocks at a time, four chunks a lane
   constexpr int WAVES = kScanThreads / 64, PER = 8;
   for (int j0 = tid >> 6; j0 < nb; j0 += PER * WAVES) {
     uint32_t before[PER] = {};
     for (int c0 = 4 * lane; c0 - 4 * lane < nc; c0 += 256) {
-      uint32_t v[PER][4];
-#pragma unroll
-      for (int p = 0; p < PER; ++p)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) v[p][u] = j0 + p * WAVES < nb && c0 + u < nc ? a.counts[((int64_t)plane * nb + j0 + p * WAVES) * nc + c0 + u] : 0u;
+      u32x4 v[PER];
 #pragma unroll
       for (int p = 0; p < PER; ++p) {
+        v[p] = u32x4{0, 0, 0, 0};
+        if (j0 + p * WAVES < nb && c0 < nc) v[p] = *reinterpret_cast<const u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * WAVES) * count_stride(nc) + c0);
+      }
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[p][u] = c0 + u < nc ? v[p][u] : 0u;
         const uint32_t sum = v[p][0] + v[p][1] + v[p][2] + v[p][3], upto = wave_scan(sum);
         uint32_t at = before[p] + upto - sum;
+        u32x4 starts;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          if (j0 + p * WAVES < nb && c0 + u < nc) a.counts[((int64_t)plane * nb + j0 + p * WAVES) * nc + c0 + u] = at;
+          starts[u] = at;
           at += v[p][u];
         }
+        if (j0 + p * WAVES < nb && c0 < nc) *reinterpret_cast<u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * WAVES) * count_stride(nc) + c0) = starts;
         before[p] += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
       }
     }
 #pragma unroll
     for (int p = 0; p < PER; ++p)
-      if (lane == 0 && j0 + p * WAVES < nb) lists[j0 + p * WAVES].len = before[p];
+      if (lane == 0 && j0 + p * WAVES < nb) {
+        if (in_lds) len_s[j0 + p * WAVES] = before[p];
+        else lists[j0 + p * WAVES].len = before[p];
+      }
   }
-  __threadfence_block();
-  __syncthreads();
+  if (in_lds) {
+    lds_barrier();
+  } else {
+    __threadfence_block();
+    __syncthreads();
+  }
   uint32_t before[4] = {0, 0, 0, 0};                             // entries, tiles, dk/dv items, partial sums of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    const uint32_t len = j < nb ? lists[j].len : 0u, chunks = dkdv ? (len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows : 0u;
+    const uint32_t len = j < nb ? (in_lds ? len_s[j] : lists[j].len) : 0u, chunks = dkdv ? (len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows : 0u;
     const uint32_t parts = chunks > 1 ? chunks : 0u;
     uint32_t v[4] = {len, (len + kBlockTileRows - 1) / kBlockTileRows, chunks * (uint32_t)a.n_sub, parts}, total[4];
     scan_add(tmp, tid, v, total);
@@ -781,6 +795,7 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   }
   if (tid == 0) {
     a.n_items[plane] = (int)before[1];
+    if (dkdv && plane == 0) *a.inf = INFINITY;
     if (dkdv) a.n_dkdv_items[plane] = (int)before[2];
   }
 }

@@ -10,6 +10,7 @@
 namespace slimpipe {
 
 constexpr int kMaxTopK = 64;
+inline __host__ __device__ int count_stride(int n_list_chunks) { return (n_list_chunks + 3) & ~3; }      // of BlockArgs::counts: 16 bytes a lane
 // rows of a plane that one workgroup of the list kernels handles, and blocks it handles at a time (a bit per row and block in LDS)
 constexpr int kListRows = 256;
 constexpr int kListBlocks = 1024;
@@ -43,7 +44,7 @@ struct BlockArgs {
   // lists (workspace), plane by plane
   int32_t n_list_chunks;         // ceil(group * s_q / kListRows)
   uint16_t* ranks;               // [plane][group * s_q * top_k]: place of a slot's row among the rows of its chunk that chose the block
-  uint32_t* counts;              // [plane][n_blocks][chunk]: rows of the chunk that chose the block, then where they start in its list
+  uint32_t* counts;              // [plane][n_blocks][count_stride]: rows of the chunk that chose the block, then where they start in its list
   BlockList* lists;              // [plane][n_blocks]
   BlockEntry* entries;           // [plane][item_cap * kBlockTileRows]
   BlockItem* items;              // [plane][item_cap]
@@ -60,6 +61,7 @@ struct BlockArgs {
   const __bf16* d_out;
   const float* delta;            // negated, and lse in log2 units, as the dense backward's
   const float* lse2;
+  float* inf;                    // a cell that holds +infinity: the lse2 of rows past a list's end
   void* dq;
   int32_t dq_f32, dq_accumulate, dkv_accumulate;
   float* dk_acc[kMaxChunks];

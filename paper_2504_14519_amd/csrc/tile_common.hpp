@@ -229,6 +229,10 @@ SP_DEV void dma16(const void* base, uint32_t lane_off, unsigned lds_base) {     
 SP_DEV void dma16_at(const void* lane_ptr, unsigned lds_base) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(lane_ptr), "s"(lds_base) : "memory", "m0");
 }
+// one dword per lane from an address of the lane's own: lane i lands at lds_base + 4*i
+SP_DEV void dma4_at(const void* lane_ptr, unsigned lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(lane_ptr), "s"(lds_base) : "memory", "m0");
+}
 // A tile copy with nothing but two per-lane constants (packed into one register): THREADS/NC rows per pass with THREADS a
 // multiple of 16*NC (THREADS = 256, NC = 16: 16 rows per pass), so pass n handles row
 // r0 + (THREADS/NC)*n of the tile and, the row step being a multiple of 16, the SAME swizzled chunk.
@@ -483,6 +487,13 @@ SP_DEV int xcd_run(int index, int n) {
 SP_DEV int xcd_item(int index, int run, int first) {
   const int slot = index >> 3;
   return ((slot / run) * 8 + ((index - first) & 7)) * run + slot % run;
+}
+
+// A barrier for what passes through LDS alone: stores to memory under way are not waited for.
+SP_DEV void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 // ---- scheduling helpers ------------------------------------------------------------------------
