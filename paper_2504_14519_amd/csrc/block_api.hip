@@ -67,7 +67,7 @@ struct BlockWorkspace {
 // a list writes its sums (256 KB for 256 keys of head_dim 128) and a reduce reads them again.
 int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub) {
   const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units());
-  return (int32_t)(rows < 2048 ? 2048 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
+  return (int32_t)(rows < 1536 ? 1536 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
 }
 BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)
   BlockWorkspace w;
@@ -102,7 +102,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.dkdv_cap = whole_rounds((slots / w.chunk_rows + blocks) * w.n_sub);
     w.part_cap = (int32_t)(2 * slots / w.chunk_rows);
     w.dkdv_items = take(planes * w.dkdv_cap * sizeof(BlockItem));
-    w.n_dkdv_items = take(planes * 4);
+    w.n_dkdv_items = take(planes * 8);
     w.dkdv_part = take(planes * w.part_cap * 2 * (size_t)(w.n_sub * keys) * p->head_dim * 4);
   }
   w.bytes = at;

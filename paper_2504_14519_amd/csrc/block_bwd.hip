@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a)
 
 // ------------------------------------------------------------------------------------ dk / dv
 // Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.
-SP_DEV int dkdv_run(int n_sub) { return n_sub > 1 ? 8 : 2; }
+SP_DEV int dkdv_run(int n_sub) { return n_sub > 2 ? 4 : 2; }
 // Keys of a workgroup: 256 where whole blocks are made of them but for a part too small to matter, else 128, or 64 in the smallest blocks.
 static bool wide_dkdv(int block_len) { return block_len % 256 == 0 || block_len % 256 > 128 || block_len >= 1024; }
 int block_dkdv_keys(int block_len) { return wide_dkdv(block_len) ? 256 : block_len >= 128 ? 128 : 64; }
@@ -169,7 +169,7 @@ struct DkdvItem {
   bool none;
   SP_DEV DkdvItem(const BlockArgs& a, int plane, int b, int hk) {
     const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, dkdv_run(a.n_sub), plane));
-    none = item >= a.n_dkdv_items[plane];
+    none = item >= a.n_dkdv_items[2 * plane];
     if (none) return;
     it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
     const int block = it.block / a.n_sub;
@@ -387,21 +387,26 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
 }
 
 // Blocks of 256 keys and more: the phases of the dense dk/dv kernel (dkdv_tile.hpp, attn_bwd.hip) on gathered rows.  Eight waves of 32 keys; waves
-// 0-3 and 4-7 alternate matrix and vector phases one phase apart; rings of four slots; the group that is in a vector phase copies tile u + 2:
-// group A rows of Q, their statistics and row numbers, group B rows of dO, each lane from the address that its row's entry gives (fetched
-// one phase earlier).  8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: WIDE_US us; four waves of 32 keys, two workgroups a compute unit and
-// no phases 332.
+// 0-3 and 4-7 alternate matrix and vector phases one phase apart.  The group that is in a vector phase VV(u) copies tile u + 3 (group A
+// rows of Q, their statistics and row numbers, group B rows of dO, each lane from the address that its row's entry gives) and the entries of
+// tile u + 6.  Gathered rows come from beyond the L2, 1700 cycles and more away, longer than a phase: a group waits at the end of
+// MM(u) for what it copied in VV(u - 2) and before, and leaves the copies of VV(u - 1) under way.  Tile t is so in LDS at the end of MM(t - 1),
+// where it is needed, entries at the end of MM(t - 4), and they are read in MM(t - 3) for VV(t - 3).
+// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: WIDE_US us; with copies of tile u + 2 that are waited for in the next phase 335, with four
+// waves of 32 keys, two workgroups a compute unit and no phases 332.
 template <int D>
 struct WideLds {
-  using L = DkdvLds<D, 8, 32>;
-  static constexpr int STAT_BYTES = 512;                   // lse2, -delta, row of the slice of the tile's 32 rows; 32 unused
-  static constexpr int RINGS = L::STAT_BASE + L::SLOTS * STAT_BYTES, TOTAL = RINGS > L::OUT_BYTES ? RINGS : L::OUT_BYTES;
+  static constexpr int BMQ = 32, SLOTS = 5, TILE = BMQ * D * 2, DO_BASE = SLOTS * TILE;      // rings of Q, dO
+  static constexpr int V = 2 * SLOTS * TILE, V_BYTES = 8 * 32 * D * 2;
+  static constexpr int STAT = V + V_BYTES, STAT_BYTES = 512;                   // lse2, -delta, row of the slice of a tile's 32 rows; 32 unused
+  static constexpr int ENTRY = STAT + SLOTS * STAT_BYTES, ENTRY_SLOTS = 8, ENTRY_BYTES = 32 * (int)sizeof(BlockEntry);      // of either group
+  static constexpr int ENTRY_RING = (ENTRY_SLOTS + 1) * ENTRY_BYTES;           // (a copy brings 64 entries: the last slot's second half is nobody's)
+  static constexpr int RINGS = ENTRY + 2 * ENTRY_RING, OUT = 8 * 32 * kOutRow<D> * 4, TOTAL = RINGS > OUT ? RINGS : OUT;
 };
 template <int D>
 __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a) {
-  using L = DkdvLds<D, 8, 32>;
-  using W = WideLds<D>;
-  constexpr int KS = D / 16, DB = D / 32, NC = D / 8, GT = 256, RPP = GT / NC, PASSES = 32 / RPP, SLOTS = L::SLOTS, TILE = L::TILE_BYTES;
+  using L = WideLds<D>;
+  constexpr int KS = D / 16, DB = D / 32, NC = D / 8, GT = 256, RPP = GT / NC, PASSES = 32 / RPP, SLOTS = L::SLOTS, TILE = L::TILE;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool group_b = wave_u >= 4;
@@ -417,59 +422,56 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) { st.dk[db][i] = 0.f; st.dv[db][i] = 0.f; }
-  item.load_k(a, wave_u * 32 + ql, g, st.kreg);
-  item.copy_v(a, lds + L::V_BASE + wave_u * 32 * D * 2, wave_u * 32, lane);
-
   // this group's operand, and its thread's part of a tile copy: rows crow + n * RPP, the chunk that the swizzle puts at its place
   const int gtid = tid & (GT - 1), crow = gtid / NC, cpos = gtid % NC;
   const int c8 = (D == 128 ? ((((cpos >> 2) ^ crow) & 3) << 2) | (((cpos & 3) ^ (crow >> 2)) & 3) : (cpos ^ crow) & (NC - 1)) * 8;
   static_assert(RPP % 16 == 0, "the rows of a thread have one swizzle phase");
   const bf16_t* const src = (group_b ? a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h
                                      : a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h) + c8;
-  const uint32_t* const offs = group_b ? &list->do_off : &list->q_off;
   const int64_t stat0 = ((int64_t)b * a.n_q_heads + hk * a.group) * a.s_q;
+  const unsigned ring = lds + L::ENTRY + (group_b ? L::ENTRY_RING : 0);
   struct Next { uint32_t off[PASSES], row, head_slot; } nx;      // of the next tile to copy
-  auto fetch = [&](int u) {
-    const int first = (u < cnt ? u : cnt - 1) * 32;
+  auto last_row = [&](int i) { return i < n_rows ? i : n_rows - 1; };
+  auto copy_entries = [&](int u) { dma16_at(list + last_row(u * 32 + lane), ring + (u & (L::ENTRY_SLOTS - 1)) * L::ENTRY_BYTES); };
+  auto read_entries = [&](int u) {
+    const char* p = smem + L::ENTRY + (group_b ? L::ENTRY_RING : 0) + (u & (L::ENTRY_SLOTS - 1)) * L::ENTRY_BYTES;
+    const int field = group_b ? (int)offsetof(BlockEntry, do_off) : (int)offsetof(BlockEntry, q_off);
 #pragma unroll
-    for (int n = 0; n < PASSES; ++n) {
-      const int i = first + crow + n * RPP;
-      nx.off[n] = offs[(i < n_rows ? i : n_rows - 1) * (int)(sizeof(BlockEntry) / 4)];
-    }
-    if (!group_b) {
-      const int i = first + (lane & 31);
-      const BlockEntry* e = list + (i < n_rows ? i : n_rows - 1);
-      nx.row = e->row;
-      nx.head_slot = e->head_slot;
-    }
+    for (int n = 0; n < PASSES; ++n) nx.off[n] = *reinterpret_cast<const uint32_t*>(p + (crow + n * RPP) * sizeof(BlockEntry) + field);
+    const BlockEntry* e = reinterpret_cast<const BlockEntry*>(p) + (lane & 31);
+    nx.row = e->row;
+    nx.head_slot = e->head_slot;
   };
-  auto copy_part = [&](int u, int part) {
-    const unsigned slot = (unsigned)(u & (SLOTS - 1));
+  // Copy instructions of a vector phase, the same number in every one: group B two of them less (and PASSES is 1 at head_dim 64).
+  constexpr int COPIES_B = PASSES + 1, COPIES_A = COPIES_B + 2;
+  auto copy_part = [&](int u, unsigned slot, int part) {
     if (part < PASSES)
-      dma16_at(src + (int64_t)nx.off[part] * 8, lds + (group_b ? L::DO_BASE : L::Q_BASE) + slot * TILE + part * GT * 16 + (wave_u & 3) * 1024);
+      dma16_at(src + (int64_t)nx.off[part] * 8, lds + (group_b ? L::DO_BASE : 0) + slot * TILE + part * GT * 16 + (wave_u & 3) * 1024);
     if (part == 2 && !group_b) {                           // (all four waves: the same data, no branch)
-      const int i = (u < cnt ? u : cnt - 1) * 32 + (lane & 31);
+      const int i = u * 32 + (lane & 31);
       const int64_t at = stat0 + (int64_t)(nx.head_slot >> 6) * a.s_q + nx.row;
       const float* from = lane < 32 ? (i < n_rows ? a.lse2 + at : a.inf) : a.delta + at;      // (rows past the list's end: p = 0)
-      dma4_at(from, lds + L::STAT_BASE + slot * W::STAT_BYTES);
-      dma4_at(&list[i < n_rows ? i : n_rows - 1].row, lds + L::STAT_BASE + slot * W::STAT_BYTES + 256);
+      dma4_at(from, lds + L::STAT + slot * L::STAT_BYTES);
+      dma4_at(&list[last_row(i)].row, lds + L::STAT + slot * L::STAT_BYTES + 256);
     }
   };
-  auto copy_all = [&](int u) {
-#pragma unroll
-    for (int part = 0; part < 3; ++part) copy_part(u, part);
-  };
-  fetch(0);
-  copy_all(0);
-  fetch(1);
-  copy_all(1);
-  fetch(2);
+  // prologue: entries of tiles 0 .. 5, then K, V and tiles 0, 1, 2
+  for (int u = 0; u < 6; u += 2) copy_entries(u);
+  item.load_k(a, wave_u * 32 + ql, g, st.kreg);
+  item.copy_v(a, lds + L::V + wave_u * 32 * D * 2, wave_u * 32, lane);
   wait_async();
-  TrBase<D> lo_qt;         // Q(u-1), transposed
+  __syncthreads();
+  for (int u = 0; u < 3; ++u) {
+    read_entries(u);
+#pragma unroll
+    for (int part = 0; part < 3; ++part) copy_part(u, u, part);
+  }
+  wait_async();
+  TrBase<D> lo_qt;         // Q(u-1), transposed; dO(u-1) sits DO_BASE further
   RpBase<D> lo_q, lo_v;    // Q(u) and this wave's V rows, row-packed
-  lo_qt.init(lane, (int)lds + L::Q_BASE + (SLOTS - 1) * TILE);     // "Q(-1)": never read
-  lo_q.init(lane, (int)lds + L::Q_BASE);
-  lo_v.init(lane, (int)lds + L::V_BASE + wave_u * 32 * D * 2);
+  lo_qt.init(lane, (int)lds + (SLOTS - 1) * TILE);     // "Q(-1)": never read
+  lo_q.init(lane, (int)lds);
+  lo_v.init(lane, (int)lds + L::V + wave_u * 32 * D * 2);
   __syncthreads();
 
   int slot = 0;            // ring slot of tile u
@@ -478,16 +480,16 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
     lo_qt.add(slot == 0 ? -(SLOTS - 1) * TILE : TILE);      // Q(u-1) sits in slot - 1
     slot = (slot == SLOTS - 1) ? 0 : slot + 1;
   };
-  auto stat_of = [&](int u) { return reinterpret_cast<const float*>(smem + L::STAT_BASE + (u & (SLOTS - 1)) * W::STAT_BYTES) + 4 * ((fresh(tid) >> 5) & 1); };
+  auto stat_of = [&](int at) { return reinterpret_cast<const float*>(smem + L::STAT + at * L::STAT_BYTES) + 4 * ((fresh(tid) >> 5) & 1); };
   // Rows of the slice from here on see the lane's key (at most s_q; without a mask: all), and whether some row of the call sees only a part
   // of the workgroup's keys
   const int64_t see = a.causal ? item.key0 + wave_u * 32 + ql - a.q_offset : 0;
   const int first_row = see < 0 ? 0 : see < a.s_q ? (int)see : a.s_q;
   const bool diagonal = a.causal && item.key0 + item.kmax - 1 > a.q_offset;
   const float c = a.scale_log2e;
-  auto vector_phase = [&](int u) {
+  auto vector_phase = [&](int u, int at) {                 // at: ring slot of tile u
     if (diagonal) {
-      const int* rows = reinterpret_cast<const int*>(stat_of(u)) + 64;
+      const int* rows = reinterpret_cast<const int*>(stat_of(at)) + 64;
 #pragma unroll
       for (int i4 = 0; i4 < 4; ++i4) {
         typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -497,29 +499,36 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
           if (r[e] < first_row) { st.s[0][4 * i4 + e] = -INFINITY; st.dp[0][4 * i4 + e] = 0.f; }      // (what no row sees may be NaN)
       }
     }
+    const int to = at + 3 < SLOTS ? at + 3 : at + 3 - SLOTS;
     dkdv_vector_phase<D, 32>(st, c, false, 0, 32, 0, [&](int part) {
-      if (part < 3) copy_part(u + 2, part);
-      else fetch(u + 3);
+      if (part < 3) copy_part(u + 3, to, part);
+      else copy_entries(u + 6);
     });
+  };
+  auto wait_old = [&]() {      // the copies of the vector phase before the last
+    if (group_b) wait_copies<COPIES_B>();
+    else wait_copies<COPIES_A>();
   };
   // Both groups run the same code; group B starts one phase (one barrier) later and group A idles one phase at the end.
   if (group_b) phase_end();
-  { DkdvMatrixPhase<D, 8, 32, false, true, 2> ph{lo_qt, lo_q, lo_v, st, stat_of(0)}; ph.run(); }     // scores of tile 0
+  read_entries(3);
+  { DkdvMatrixPhase<D, 8, 32, false, true, 2, L> ph{lo_qt, lo_q, lo_v, st, stat_of(0)}; ph.run(); }     // scores of tile 0
   advance();
-  wait_async();
   phase_end();
   for (int u = 0; u + 1 < cnt; ++u) {
-    vector_phase(u);
+    const int at = slot == 0 ? SLOTS - 1 : slot - 1;
+    vector_phase(u, at);
     phase_end();
     asm volatile("" : "+v"(lo_v.off0));      // (V never moves: without this the offsets of its blocks are kept in registers across the loop)
-    { DkdvMatrixPhase<D, 8, 32, true, true, 2> ph{lo_qt, lo_q, lo_v, st, stat_of(u + 1)}; ph.run(); }    // sums of tile u, scores of tile u+1
+    read_entries(u + 4);
+    { DkdvMatrixPhase<D, 8, 32, true, true, 2, L> ph{lo_qt, lo_q, lo_v, st, stat_of(slot)}; ph.run(); }    // sums of tile u, scores of tile u+1
     advance();
-    wait_async();                            // the copies of the vector phase before have landed
+    wait_old();
     phase_end();
   }
-  vector_phase(cnt - 1);
+  vector_phase(cnt - 1, slot == 0 ? SLOTS - 1 : slot - 1);
   phase_end();
-  { DkdvMatrixPhase<D, 8, 32, true, false, 2> ph{lo_qt, lo_q, lo_v, st, nullptr}; ph.run(); }     // sums of the last tile
+  { DkdvMatrixPhase<D, 8, 32, true, false, 2, L> ph{lo_qt, lo_q, lo_v, st, nullptr}; ph.run(); }     // sums of the last tile
   wait_async();
   phase_end();
   if (!group_b) phase_end();

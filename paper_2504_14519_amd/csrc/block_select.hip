@@ -700,7 +700,8 @@ __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int 
     a.items[(int64_t)plane * a.item_cap + list.tile0 + pos / kBlockTileRows] = {(int)block, (int)to, (int)(left < kBlockTileRows ? left : kBlockTileRows), 0};
   if (dkdv && pos % (uint32_t)a.chunk_rows == 0) {
     const uint32_t c = pos / (uint32_t)a.chunk_rows;
-    BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + list.item0 + c * (uint32_t)a.n_sub;
+    const uint32_t first = left >= (uint32_t)a.chunk_rows ? list.item0 + c * (uint32_t)a.n_sub : (uint32_t)a.n_dkdv_items[2 * plane + 1] + list.rest0;
+    BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + first;
     for (int s = 0; s < a.n_sub; ++s)
       it[s] = {(int)block * a.n_sub + s, (int)to, (int)(left < (uint32_t)a.chunk_rows ? left : (uint32_t)a.chunk_rows), list.parts ? (int)(list.part0 + c) : -1};
   }
@@ -782,21 +783,21 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
     __threadfence_block();
     __syncthreads();
   }
-  uint32_t before[4] = {0, 0, 0, 0};                             // entries, tiles, dk/dv items, partial sums of the blocks before
+  uint32_t before[4] = {0, 0, 0, 0};                             // short dk/dv items, tiles, dk/dv items of full length, partial sums of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    const uint32_t len = j < nb ? (in_lds ? len_s[j] : lists[j].len) : 0u, chunks = dkdv ? (len + (uint32_t)a.chunk_rows - 1) / (uint32_t)a.chunk_rows : 0u;
-    const uint32_t parts = chunks > 1 ? chunks : 0u;
-    uint32_t v[4] = {len, (len + kBlockTileRows - 1) / kBlockTileRows, chunks * (uint32_t)a.n_sub, parts}, total[4];
+    const uint32_t len = j < nb ? (in_lds ? len_s[j] : lists[j].len) : 0u, full = dkdv ? len / (uint32_t)a.chunk_rows : 0u;
+    const uint32_t rest = dkdv && len > full * (uint32_t)a.chunk_rows ? 1u : 0u, parts = full + rest > 1 ? full + rest : 0u;
+    uint32_t v[4] = {rest * (uint32_t)a.n_sub, (len + kBlockTileRows - 1) / kBlockTileRows, full * (uint32_t)a.n_sub, parts}, total[4];
     scan_add(tmp, tid, v, total);
-    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], parts, before[3] + v[3]};
+    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], before[0] + v[0], parts, before[3] + v[3]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) before[i] += total[i];
   }
   if (tid == 0) {
     a.n_items[plane] = (int)before[1];
     if (dkdv && plane == 0) *a.inf = INFINITY;
-    if (dkdv) a.n_dkdv_items[plane] = (int)before[2];
+    if (dkdv) { a.n_dkdv_items[2 * plane] = (int)(before[2] + before[0]); a.n_dkdv_items[2 * plane + 1] = (int)before[2]; }
   }
 }
 

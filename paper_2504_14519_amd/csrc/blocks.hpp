@@ -24,9 +24,10 @@ struct BlockEntry { uint32_t row, head_slot, q_off, do_off; };
 // block's keys (in units of its workgroup's keys) and the plane's partial-sum slot, or -1 when the sums go straight to the accumulators
 struct BlockItem { int32_t block, first, count, part; };
 
-// The list of a block: length, first tile, first dk/dv item; how many partial dk/dv sums it leaves (0: one workgroup has all of it, or
+// The list of a block: length, first tile; first dk/dv item of its parts of full length, and of its last part where that is shorter (these come
+// behind all of full length, so that no long item starts late); how many partial dk/dv sums it leaves (0: one workgroup has all of it, or
 // nobody) and the first of them
-struct BlockList { uint32_t len, tile0, item0, parts, part0, unused[3]; };
+struct BlockList { uint32_t len, tile0, item0, rest0, parts, part0, unused[2]; };
 
 struct BlockArgs {
   const __bf16* q;
@@ -69,7 +70,7 @@ struct BlockArgs {
   int32_t chunk_rows;            // rows of a list that one dk/dv workgroup sums (a multiple of 32)
   int32_t n_sub;                 // parts of a block's keys that have a dk/dv workgroup each
   BlockItem* dkdv_items;         // [plane][dkdv_cap]
-  int32_t* n_dkdv_items;         // [plane]
+  int32_t* n_dkdv_items;         // [plane][2]: all of them, those of full length
   int32_t dkdv_cap;
   float* dkdv_part;              // [plane][part_cap][2][sub * sub keys][head_dim]
   int32_t part_cap;

@@ -30,9 +30,8 @@ struct DkdvLds {
   static constexpr int TOTAL = RINGS > OUT_BYTES ? RINGS : OUT_BYTES;
 };
 
-template <int D, int NW, int BMQ, bool WITH_ACC, bool WITH_SCORES, int LOOK>
+template <int D, int NW, int BMQ, bool WITH_ACC, bool WITH_SCORES, int LOOK, class L = DkdvLds<D, NW, BMQ>>
 struct DkdvMatrixPhase {
-  using L = DkdvLds<D, NW, BMQ>;
   static constexpr int KS = D / 16, DB = D / 32, QB = BMQ / 32;
   static constexpr int N_AC = WITH_ACC ? 4 * DB * QB : 0, N_SC = WITH_SCORES ? 2 * KS * QB : 0, N = N_AC + N_SC;
   static constexpr int NBUF = LOOK + 1, HALF = 16 * D * 2;
