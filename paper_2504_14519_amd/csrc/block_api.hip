@@ -63,11 +63,13 @@ struct BlockWorkspace {
   size_t part_out, part_lse, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
-// Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but 2048 at least, because every part of
-// a list writes its sums (256 KB for 256 keys of head_dim 128) and a reduce reads them again.
-int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub) {
-  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units());
-  return (int32_t)(rows < 1536 ? 1536 : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
+// Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but no fewer than make the start of a
+// workgroup and its sums, which go to memory and back, a small part of it: 1536 where it owns 256 keys and has a compute unit to itself
+// (8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row, dk/dv and the sums' reduce: 1024 410 us, 1536 355, 2048 365), 512 for the smaller ones, of
+// which several share one (3 x 1337 rows of 12 heads of 64 on 64 blocks of 64 keys, 12 a row: 512 NARROW_US us, 1024 70, 1536 77, 2048 91).
+int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub, int32_t keys) {
+  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units()), least = keys == 256 ? 1536 : 512;
+  return (int32_t)(rows < least ? least : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
 }
 BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)
   BlockWorkspace w;
@@ -97,7 +99,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     const size_t slots = plane_rows * top_k;
     const int32_t keys = block_dkdv_keys(block_len);
     w.n_sub = (block_len + keys - 1) / keys;
-    w.chunk_rows = dkdv_chunk_rows((int64_t)(rows * top_k), w.n_sub);
+    w.chunk_rows = dkdv_chunk_rows((int64_t)(rows * top_k), w.n_sub, keys);
     // a list of n rows has at most n / chunk_rows + 1 parts, and partial sums only when n > chunk_rows: then at most twice n / chunk_rows
     w.dkdv_cap = whole_rounds((slots / w.chunk_rows + blocks) * w.n_sub);
     w.part_cap = (int32_t)(2 * slots / w.chunk_rows);

@@ -227,11 +227,11 @@ SP_DEV void dma16(const void* base, uint32_t lane_off, unsigned lds_base) {     
 }
 // 16 bytes per lane from an address of the lane's own: lane i lands at lds_base + 16*i
 SP_DEV void dma16_at(const void* lane_ptr, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(lane_ptr), "s"(lds_base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(lane_ptr), "s"(__builtin_amdgcn_readfirstlane(lds_base)) : "memory", "m0");
 }
 // one dword per lane from an address of the lane's own: lane i lands at lds_base + 4*i
 SP_DEV void dma4_at(const void* lane_ptr, unsigned lds_base) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(lane_ptr), "s"(lds_base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(lane_ptr), "s"(__builtin_amdgcn_readfirstlane(lds_base)) : "memory", "m0");
 }
 // A tile copy with nothing but two per-lane constants (packed into one register): THREADS/NC rows per pass with THREADS a
 // multiple of 16*NC (THREADS = 256, NC = 16: 16 rows per pass), so pass n handles row
