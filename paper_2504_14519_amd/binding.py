@@ -493,16 +493,16 @@ class KvCache4(collections.namedtuple("KvCache4", "k_codes k_scales v_codes v_sc
     def layout(self):
         """(batch, capacity, kv heads, head_dim) and the three strides in elements, after a check that the four tensors agree."""
         kc, ks, vc, vs = self
-        B, N, H, half = kc.shape
-        ok = all(x.dtype == torch.uint8 and x.dim() == 4 and x.stride(3) == 1 for x in self)
-        ok = ok and vc.shape == kc.shape and ks.shape == vs.shape == torch.Size((B, N, H, half // 16))
+        shape, codes, scales, v_codes, v_scales = kc.shape, kc.stride(), ks.stride(), vc.stride(), vs.stride()
+        ok = len(shape) == 4 and codes[3:] == scales[3:] == v_codes[3:] == v_scales[3:] == (1,) and kc.dtype == ks.dtype == vc.dtype == vs.dtype == torch.uint8
+        if ok:
+            B, N, H, half = shape
+            ok = vc.shape == shape and ks.shape == vs.shape == (B, N, H, half // 16)
         # (a dimension of one element may have any stride)
-        ok = ok and all(n == 1 or kc.stride(i) == vc.stride(i) == 16 * ks.stride(i) == 16 * vs.stride(i) for i, n in ((0, B), (1, N), (2, H)))
-        if not ok:
+        if not ok or not all(n == 1 or a == b == 16 * c == 16 * d for n, a, b, c, d in zip(shape[:3], codes, v_codes, scales, v_scales)):
             raise SlimpipeError("codes and scales must be uint8 [batch, keys, heads, head_dim / 2] and [.., head_dim / 32] of the same layout")
         D = 2 * half
-        full = N * H * D, H * D, D
-        return (B, N, H, D), tuple(2 * kc.stride(i) if n > 1 else full[i] for i, n in ((0, B), (1, N), (2, H)))
+        return (B, N, H, D), (2 * codes[0] if B > 1 else N * H * D, 2 * codes[1] if N > 1 else H * D, 2 * codes[2] if H > 1 else D)
 
 
 def _cache_ptrs(cache):
