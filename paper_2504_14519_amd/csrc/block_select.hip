@@ -63,7 +63,9 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 //   delta_r = (9/8) D 2^-23 |q_r| max_j |mean_j|.
 // If T is the n-th largest of the approximate scores of a row, the exact n-th largest lies within delta of T: what is above T + 2 delta is
 // taken for certain, what is below T - 2 delta is not, and only where more lies between than there are places are scores computed in
-// 64 bits (one row in a hundred).
+// 64 bits (one row in a hundred).  Where products might run into the smallest float32 numbers (|q| or max |mean| below 2^-40: the bound has
+// 2^-103 to spare then) nothing is certain.  A row of zeros, as padding has them, or means that are all zero have equal scores
+// throughout, which needs no computing.
 //
 // T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
 // goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
@@ -155,9 +157,43 @@ SP_DEV const bf16_t* select_q(const BlockSelectArgs& a, int b, int hk, int rh) {
   const int hl = rh / a.s_q, r = rh - hl * a.s_q;
   return a.q + (int64_t)b * a.q_stride_b + (int64_t)r * a.q_stride_s + (int64_t)(hk * a.group + hl) * a.q_stride_h;
 }
-// What lies between and above: NaN bounds (a mean or a query that is not finite) leave everything open.
-SP_DEV void select_bounds(float t, float delta, float* lo, float* hi) {
-  const bool clear = delta < INFINITY && fabsf(t) < INFINITY;
+SP_DEV uint32_t both_halves(uint32_t m) {
+  auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return r[0] | r[1];
+}
+// |q| of the lane's row (both halves of a wave have it); -1: all zeros.
+template <int KS>
+SP_DEV float row_norm(const bf16x8 (&q)[KS]) {
+  float norm = 0.f;
+  uint32_t any = 0;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const u32x4 w = __builtin_bit_cast(u32x4, q[ks]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) any |= w[i] & 0x7fff7fffu;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
+  }
+  norm = __builtin_sqrtf(xhalf_sum(norm));
+  return both_halves(any) == 0u ? -1.f : norm;
+}
+// Whether all scores of a row are equal: a row of zeros on finite means (`most`: largest |mean|^2, infinite where one is not), means of zeros.
+SP_DEV bool all_equal(float norm, uint32_t most, bool no_mean) { return (norm < 0.f && __uint_as_float(most) < INFINITY) || no_mean; }
+// Whether n floats (a multiple of 4) are zeros; for all threads of a workgroup at once, and only where their squares vanish: not kept up in the walk,
+// which has no registers to spare.
+SP_DEV bool means_are_zero(const float* means, int64_t n, int tid, int threads) {
+  uint32_t any = 0;
+  for (int64_t i = 4 * tid; i < n; i += 4 * threads) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(means + i);
+    any |= (w[0] | w[1] | w[2] | w[3]) << 1;
+  }
+  return __syncthreads_or((int)(any != 0u)) == 0;
+}
+// What lies between and above: bounds that are not finite (a mean or a query that is not) or too small leave everything open.
+template <int D>
+SP_DEV void select_bounds(float t, float norm, uint32_t most, float* lo, float* hi) {
+  const float mean = __builtin_sqrtf(__uint_as_float(most)), delta = 1.125f * D * 0x1p-23f * norm * mean;
+  const bool clear = norm >= 0x1p-40f && mean >= 0x1p-40f && delta < INFINITY && fabsf(t) < INFINITY;
   *lo = clear ? t - 2.f * delta : -INFINITY;
   *hi = clear ? t + 2.f * delta : INFINITY;
 }
@@ -173,10 +209,6 @@ SP_DEV uint32_t above(const f32x16& s, float hi, int g) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) m |= s[i] > hi ? 1u << (8 * (i >> 2) + (i & 3)) : 0u;
   return m << (4 * g);
-}
-SP_DEV uint32_t both_halves(uint32_t m) {
-  auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-  return r[0] | r[1];
 }
 SP_DEV uint32_t blocks_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }      // bits of the tile's blocks before the n-th
 
@@ -309,12 +341,7 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    norm[r] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) norm[r] += (float)q[r][ks][e] * (float)q[r][ks][e];
-    norm[r] = __builtin_sqrtf(xhalf_sum(norm[r]));
+    norm[r] = row_norm<KS>(q[r]);
     atomicMax(&last_s, want[r].own);
   }
   __syncthreads();
@@ -389,11 +416,12 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
     });
     atomicMax(&most_s, __float_as_uint(most));
     __syncthreads();
+    const bool no_mean = most_s == 0u && means_are_zero(means + (int64_t)a.first_block * D, (int64_t)(stop - a.first_block) * D, tid, 256);
     float lo[R], hi[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       merge_halves<K>(top[r], g);
-      select_bounds(place_of<K>(top[r], want[r].need), 1.125f * D * 0x1p-23f * norm[r] * __builtin_sqrtf(__uint_as_float(most_s)), &lo[r], &hi[r]);
+      select_bounds<D>(place_of<K>(top[r], want[r].need), norm[r], most_s, &lo[r], &hi[r]);
       if (want[r].own - a.first_block <= want[r].need) { lo[r] = -INFINITY; hi[r] = INFINITY; }      // no more than are wanted: all
     }
     walk([&](int t, f32x16 (&s)[R]) {
@@ -409,6 +437,9 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
           }
       }
     });
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (all_equal(norm[r], most_s, no_mean) && count[r] > want[r].need) count[r] = want[r].need;      // the first ones
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -473,16 +504,17 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   auto scores = [&](int t) {
     const int j = a.first_block + t * 32 + ql;
     const float* mp = means + (int64_t)(j < stop ? j : stop - 1) * D + 8 * g;
-    bf16x8 part[KS][3];
     float sq = 0.f;
+    // (a sum for each of the parts, added up smallest first: the parts of a step are used at once and need few registers)
+    f32x16 x[3] = {};
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      split_means(*reinterpret_cast<const f32x4*>(mp + 16 * ks), *reinterpret_cast<const f32x4*>(mp + 16 * ks + 4), part[ks], sq);
-    f32x16 s = {0};
+    for (int ks = 0; ks < KS; ++ks) {
+      bf16x8 part[3];
+      split_means(*reinterpret_cast<const f32x4*>(mp + 16 * ks), *reinterpret_cast<const f32x4*>(mp + 16 * ks + 4), part, sq);
 #pragma unroll
-    for (int p = 2; p >= 0; --p)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma32(part[ks][p], q[ks], s);
+      for (int p = 0; p < 3; ++p) x[p] = mfma32(part[p], q[ks], x[p]);
+    }
+    const f32x16 s = (x[2] + x[1]) + x[0];
     sq = xhalf_sum(sq);
     most = sq == sq ? fmaxf(most, sq) : INFINITY;
     return s;
@@ -503,12 +535,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   }
   for (int t = wave + kFewKept * kFewWaves; t < nt; t += kFewWaves) offer(scores(t), t);
   {
-    float norm = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) norm += (float)q[ks][e] * (float)q[ks][e];
-    norm = __builtin_sqrtf(xhalf_sum(norm));
+    const float norm = row_norm<KS>(q);
     if (tid < 32) norm_s[tid] = norm;
   }
   atomicMax(&most_s, __float_as_uint(most));
@@ -535,8 +562,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
     if (lane < 32 && lane % 8 == 0) border_s[r] = v;
   }
   __syncthreads();
+  const bool no_mean = most_s == 0u && stop > a.first_block && means_are_zero(means + (int64_t)a.first_block * D, (int64_t)(stop - a.first_block) * D, tid, kFewWaves * 64);
   float lo, hi;
-  select_bounds(border_s[ql], 1.125f * D * 0x1p-23f * norm_s[ql] * __builtin_sqrtf(__uint_as_float(most_s)), &lo, &hi);
+  select_bounds<D>(border_s[ql], norm_s[ql], most_s, &lo, &hi);
   if (want.own - a.first_block <= want.need) { lo = -INFINITY; hi = INFINITY; }
   uint32_t* const open_s = reinterpret_cast<uint32_t*>(smem);      // [tile][row]; certain ones behind them, then the rows' lists
   uint32_t* const certain_s = open_s + nt * 32;
@@ -576,7 +604,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
   __syncthreads();
   for (int r = wave; r < 32 && row0 + r < rows; r += kFewWaves) {
     const int n = __builtin_amdgcn_readfirstlane(count_s[r]), need = __builtin_amdgcn_readlane(want.need, r), own = __builtin_amdgcn_readlane(want.own, r);
-    if (n > need) settle_row<D>(cand + r * PLACES, n, PLACES, need, select_q(a, b, hk, row0 + r), means, a.first_block, own, lane);
+    if (n > need && !all_equal(norm_s[r], most_s, no_mean)) settle_row<D>(cand + r * PLACES, n, PLACES, need, select_q(a, b, hk, row0 + r), means, a.first_block, own, lane);
     const int forced = __builtin_amdgcn_readlane(want.forced, r), have = n < need ? n : need;
     if (lane < a.top_k)
       a.index[(((int64_t)b * a.n_kv_heads + hk) * rows + row0 + r) * a.top_k + lane] =
