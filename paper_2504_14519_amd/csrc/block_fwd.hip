@@ -177,11 +177,11 @@ __global__ __launch_bounds__(256) void block_fwd_few_kernel(const BlockArgs a) {
       sum += l_s[w] * f;
       o += acc_s[w][tid] * f;
     }
-    const bool has = sum > 0.f;
-    const float r = has ? o / sum : 0.f;
+    const bool none = sum == 0.f;                    // (a NaN is not that)
+    const float r = none ? 0.f : o / sum;
     if (a.part_f32) static_cast<float*>(a.part_out)[item * D + tid] = r;
     else static_cast<bf16_t*>(a.part_out)[item * D + tid] = (bf16_t)r;
-    if (tid == 0) a.part_lse[item] = has ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+    if (tid == 0) a.part_lse[item] = none ? -INFINITY : (mx + __builtin_log2f(sum)) * kLn2;
   }
 }
 

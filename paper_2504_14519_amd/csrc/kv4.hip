@@ -422,7 +422,7 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(const Kv4Args a) {
       x0 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d);
       x1 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d + 4);
     }
-    const float norm = sum > 0.f ? 1.0f / sum : 0.f, lse = sum > 0.f ? (mx + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+    const float norm = sum == 0.f ? 0.f : 1.0f / sum, lse = sum == 0.f ? -INFINITY : (mx + __builtin_log2f(sum)) * kLn2;      // (a NaN is not 0)
     x0 *= norm;
     x1 *= norm;
     const Kv4Row at = kv4_row(a, hk0 + hh, rr);

@@ -6,7 +6,7 @@ namespace slimpipe {
 
 // Writes 8 elements of a row's result, and its lse.
 SP_DEV void put_result(const PartMergeArgs& a, int64_t row, int d, f32x4 x0, f32x4 x1, float m, float l) {
-  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;      // (NaN, from a NaN among what the row saw: stays)
   const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
   const int64_t to = b * a.o_stride_b + (row - bh * a.s_q) * a.o_stride_s + (bh - b * a.n_q_heads) * a.o_stride_h + d;
   x0 *= inv;
@@ -19,7 +19,7 @@ SP_DEV void put_result(const PartMergeArgs& a, int64_t row, int d, f32x4 x0, f32
     const bf16x4 lo = __builtin_convertvector(x0, bf16x4), hi = __builtin_convertvector(x1, bf16x4);
     *reinterpret_cast<bf16x8*>(static_cast<bf16_t*>(a.out) + to) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
-  if (d == 0) a.lse[row] = m == -INFINITY ? -INFINITY : m + __builtin_log2f(l) * kLn2;
+  if (d == 0) a.lse[row] = l == 0.f ? -INFINITY : m + __builtin_log2f(l) * kLn2;
 }
 // Parts first, first + step, .. of 8 elements of a row: maximum of their lse, sum of weights, weighted sum.
 template <int D, bool F32>
@@ -30,12 +30,11 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
   x0 = x1 = f32x4{0, 0, 0, 0};
 #pragma unroll 4
   for (int s = first; s < a.parts; s += step) m = fmaxf(m, lp[s]);
-  if (m == -INFINITY) return;
 #pragma unroll 4
   for (int s = first; s < a.parts; s += step) {
     const float ls = lp[s];
     if (ls == -INFINITY) continue;
-    const float w = exp2_fast((ls - m) * kLog2e);
+    const float w = exp2_fast((ls - m) * kLog2e);      // (m is -inf only where all are that or NaN, which gives NaN)
     l += w;
     const int64_t at = (row * a.parts + s) * D + d;
     if constexpr (F32) {
@@ -95,14 +94,14 @@ __global__ __launch_bounds__(256) void part_merge_few_kernel(const PartMergeArgs
   m = fmaxf(fmaxf(m_s[0], m_s[1]), fmaxf(m_s[2], m_s[3]));
   l = 0.f;
   x0 = x1 = f32x4{0, 0, 0, 0};
-  if (m != -INFINITY)
+  const float me = m == -INFINITY ? 0.f : m;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = exp2_fast((m_s[w] - m) * kLog2e);
-      l += f * l_s[w];
-      x0 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8]);
-      x1 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8 + 4]);
-    }
+  for (int w = 0; w < 4; ++w) {
+    const float f = exp2_fast((m_s[w] - me) * kLog2e);
+    l += f * l_s[w];
+    x0 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8]);
+    x1 += f * *reinterpret_cast<const f32x4*>(&acc_s[w][c * 8 + 4]);
+  }
   put_result(a, row, d, x0, x1, m, l);
 }
 

@@ -22,12 +22,12 @@ struct RowState {
     m = -INFINITY;
     l = 0.f;
   }
-  // 1 / sum and lse of the lane's row; (0, -inf) when it saw no key
+  // 1 / sum and lse of the lane's row; (0, -inf) when it saw no key (a sum that is NaN is not that)
   SP_DEV float finish(float* lse) const {
     const float total = xhalf_sum(l);
-    const bool has = total > 0.f;
-    *lse = has ? (m + __builtin_log2f(total)) * kLn2 : -INFINITY;
-    return has ? 1.0f / total : 0.f;
+    const bool none = total == 0.f;
+    *lse = none ? -INFINITY : (m + __builtin_log2f(total)) * kLn2;
+    return none ? 0.f : 1.0f / total;
   }
 };
 
