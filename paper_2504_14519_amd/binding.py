@@ -462,7 +462,8 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
     k_chunks, v_chunks, dk_chunks, dv_chunks = (list(_as_chunks(x)) for x in (k_chunks, v_chunks, dk_chunks, dv_chunks))
     top_k = _check_index(index, q_slice)
     if dq is None:
-        dq = torch.empty_like(q_slice, dtype=torch.float32 if dq_dtype == F32 else torch.bfloat16)
+        # (the strides of q also where those leave gaps: a slice of a sequence, a part of packed rows)
+        dq = torch.empty_strided(q_slice.shape, q_slice.stride(), device=q_slice.device, dtype=torch.float32 if dq_dtype == F32 else torch.bfloat16)
     if not _same_strides(dq, q_slice):
         raise SlimpipeError("dq must have the strides of q")
     for c in v_chunks + dk_chunks + dv_chunks:
