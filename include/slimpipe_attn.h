@@ -238,8 +238,10 @@ int slimpipe_attn_fwd_ranges(const slimpipe_attn_params* p, const void* q_slice,
  * last with the picks held fixed (they are a choice and have none).  As with every call here the key range [kv_begin, kv_end) may be a
  * part of the prefix, so that the (out, lse) of several ranges can be folded by slimpipe_attn_merge.
  *   block_len : a multiple of 64, 64 .. 65536 (SLIMPIPE_EINVAL_SHAPE otherwise); with several chunks chunk_len is a multiple of it.
- *   top_k     : 1 .. 64 slots per row (SLIMPIPE_EINVAL_SHAPE otherwise; also for more than 2^30 slots of one kv head and 2^34 in all,
- *               or batch * n_kv_heads > 65535).
+ *   top_k     : 1 .. 64 slots per row (SLIMPIPE_EINVAL_SHAPE otherwise).
+ *   limits    : batch * n_kv_heads <= 65535, less than 2^27 rows of all heads, 2^30 slots of one kv head, less than 2^22 - 1 blocks in the key range, in the
+ *               backward less than 2^27 keys there, kv_capacity <= 2^36 (SLIMPIPE_EINVAL_SHAPE otherwise); the rows of the query heads of
+ *               one kv head, of q and in the backward of d_out, lie within 2^35 elements (SLIMPIPE_EINVAL_STRIDE otherwise).
  *   index     : int32 [batch, n_q_heads, s_q, top_k], contiguous.
  *   means     : float32 [batch, n_kv_heads, ceil(kv_capacity / block_len), head_dim], contiguous. */
 
@@ -263,7 +265,8 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
 
 /* Forward: row r of head h attends to the keys that slimpipe_attn_fwd would let it see and that lie in one of its blocks.  Any index will
  * do: entries outside the range's blocks are no block, a block named twice counts once, order is free.  out, lse, rows without a key and
- * keys that no row sees: as in slimpipe_attn_fwd.  Results do not depend on the order in which workgroups run. */
+ * keys that no row sees: as in slimpipe_attn_fwd.  A bf16 out is folded from bf16 results of a row's blocks (weights and sums in
+ * float32), a float32 one from float32 results; likewise dq in the backward.  Results do not depend on the order in which workgroups run. */
 int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
                             int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
                             size_t workspace_bytes, void* hip_stream);
@@ -283,7 +286,9 @@ int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, 
  *   codes, scales : [batch, kv_capacity, n_kv_heads, head_dim / 2] and [.., head_dim / 32] bytes, for keys and for values, at the kv
  *              strides of p, which count ELEMENTS: byte strides are half and a 32nd of them.  They are multiples of 32
  *              (SLIMPIPE_EINVAL_STRIDE otherwise), codes 16-byte aligned.
- *   limits   : kv_capacity <= 2^36, batch * n_kv_heads <= 65535, 2^30 query rows per kv head, 2^34 rows of all heads a store or load. */
+ *              Magnitudes from 1.75 * 2^127 on read as infinities.
+ *   limits   : kv_capacity <= 2^36, batch * n_kv_heads <= 65535, 2^30 keys in a range, less than 2^27 rows of all heads in a slice, a store or a
+ *              load (SLIMPIPE_EINVAL_SHAPE otherwise). */
 
 /* Stores the rows of a slice at positions q_offset .. q_offset + s_q - 1.  k_slice, v_slice: bf16 [batch, s_q, n_kv_heads, head_dim] with the q
  * strides.  Other rows of the cache are untouched.  (n_q_heads, causal, scale and the key range are only validated.) */

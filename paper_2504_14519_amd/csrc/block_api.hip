@@ -16,6 +16,8 @@ constexpr int kMinBlockLen = 64, kMaxBlockLen = 1 << 16;
 int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_len, int32_t block_len) {
   if (block_len < kMinBlockLen || block_len > kMaxBlockLen || block_len % 64 != 0) return SLIMPIPE_EINVAL_SHAPE;
   if (p->kv_capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;                         // block indices, in parts of 64 keys, are 32 bits
+  // a launch has less than 2^32 threads: 1024 a block where the means are made
+  if (p->kv_end / block_len - p->kv_begin / block_len >= (1 << 22) - 1) return SLIMPIPE_EINVAL_SHAPE;
   const int rc = check_chunks(p, n_chunks, chunk_len);
   if (rc != SLIMPIPE_OK) return rc;
   if (n_chunks > 1 && chunk_len % block_len != 0) return SLIMPIPE_EINVAL_SHAPE;
@@ -25,8 +27,9 @@ int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_
 int check_top_k(const slimpipe_attn_params* p, int32_t top_k, int is_bwd) {
   if (top_k < 1 || top_k > kMaxTopK) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t rows = (int64_t)p->n_q_heads / p->n_kv_heads * p->s_q;
-  // rows and slots of a plane, all of them as workgroups, and offsets of a plane's rows in units of 8 elements, in 32 bits
-  if (rows * top_k > (int64_t)1 << 30 || rows * p->n_kv_heads * p->batch * top_k > (int64_t)1 << 34) return SLIMPIPE_EINVAL_SHAPE;
+  // slots of a plane, and offsets of its rows in units of 8 elements, in 32 bits; less than 2^32 threads, 32 a row and in the backward 32 a key
+  if (rows * top_k > (int64_t)1 << 30 || rows * p->n_kv_heads * p->batch >= 1 << 27) return SLIMPIPE_EINVAL_SHAPE;
+  if (is_bwd && p->kv_end - p->kv_begin >= 1 << 27) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t heads = p->n_q_heads / p->n_kv_heads - 1, last = p->s_q - 1, most = (int64_t)1 << 35;
   if (p->q_stride_h > most / (heads + 1) || p->q_stride_h * heads + p->q_stride_s * last >= most) return SLIMPIPE_EINVAL_STRIDE;
   if (is_bwd && (p->do_stride_h > most / (heads + 1) || p->do_stride_h * heads + p->do_stride_s * last >= most)) return SLIMPIPE_EINVAL_STRIDE;

@@ -8,11 +8,12 @@ using namespace slimpipe;
 
 namespace {
 
-// What every call on the cache checks beyond slimpipe_attn_validate: whole groups of 32 elements, and counts that fit a launch.
+// What every call on the cache checks beyond slimpipe_attn_validate: whole groups of 32 elements, counts that fit a launch (less than 2^32
+// threads) and 32 bits.
 int check_cache(const slimpipe_attn_params* p) {
   if (p->kv_stride_b % 32 != 0 || p->kv_stride_s % 32 != 0 || p->kv_stride_h % 32 != 0) return SLIMPIPE_EINVAL_STRIDE;
   if (p->kv_capacity > (int64_t)1 << 36 || (int64_t)p->batch * p->n_kv_heads > 65535) return SLIMPIPE_EINVAL_SHAPE;
-  if ((int64_t)p->n_q_heads / p->n_kv_heads * p->s_q > (int64_t)1 << 30) return SLIMPIPE_EINVAL_SHAPE;
+  if ((int64_t)p->batch * p->n_q_heads * p->s_q >= 1 << 27 || p->kv_end - p->kv_begin > 1 << 30) return SLIMPIPE_EINVAL_SHAPE;
   return SLIMPIPE_OK;
 }
 int check_operands(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales) {
@@ -20,7 +21,7 @@ int check_operands(const void* k_codes, const void* k_scales, const void* v_code
   return aligned16(k_codes) && aligned16(v_codes) ? SLIMPIPE_OK : SLIMPIPE_EINVAL_ALIGN;
 }
 int copy_args(Kv4CopyArgs* a, const slimpipe_attn_params* p, int64_t rows) {
-  if ((int64_t)p->batch * p->n_kv_heads * rows > (int64_t)1 << 34) return SLIMPIPE_EINVAL_SHAPE;
+  if (rows > 1 << 30 || (int64_t)p->batch * p->n_kv_heads * rows >= 1 << 27) return SLIMPIPE_EINVAL_SHAPE;
   memset(a, 0, sizeof(*a));
   a->n_kv_heads = p->n_kv_heads; a->batch = p->batch; a->rows = rows;
   a->kv_stride_b = p->kv_stride_b; a->kv_stride_s = p->kv_stride_s; a->kv_stride_h = p->kv_stride_h;

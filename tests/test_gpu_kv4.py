@@ -80,7 +80,7 @@ def test_extreme_groups(sp):
     k, _ = sp.slimpipe_attn_kv4_load(cache, 0, 6)
     got = host_f64(k)
     assert (got[0, 0] == 0).all() and (got[0, 1] == 0).all()
-    assert (got[0, 2] == 2.0 ** 128).all() or (got[0, 2] == 4 * 2.0 ** 126).all() or np.isinf(got[0, 2]).all()
+    assert np.isinf(got[0, 2]).all()                     # the nearest code is 4 times 2^126
     assert np.isnan(got[0, 3, 0, :32]).all() and (got[0, 3, 0, 32:] == 0).all()
     assert np.isnan(got[0, 4, 0, 32:]).all() and (got[0, 4, 0, :32] == 0).all()
     assert (got[0, 5] == 2.0 ** -125).all()              # 0.75 is as near to 0.5 as to 1: the even code
@@ -188,7 +188,7 @@ def test_old_prefix_in_4_bits_new_keys_in_bf16(sp):
 
 
 def test_tokens_as_they_come_streams_and_graph(sp):
-    """Tokens stored and attended to one by one, eagerly, on another stream and from a replayed graph whose position moves by its inputs."""
+    """Tokens stored and attended to one by one, eagerly, on another stream and from a graph that is replayed with other rows."""
     import torch
     B, Hq, Hkv, D, N = 2, 8, 2, 64, 400
     rows = [dev_bf16(normal_bf16((B, N, H, D), 36, t)) for t, H in (("q", Hq), ("k", Hkv), ("v", Hkv))]
