@@ -767,7 +767,7 @@ SP_DEV void scan_add(uint32_t (*tmp)[4], int tid, uint32_t (&v)[4], uint32_t (&t
 }
 __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
   constexpr int kLens = 8192;                                    // lengths that pass through LDS (more: through memory)
-  __shared__ uint32_t tmp[kScanThreads / 64][4], len_s[kLens];
+  __shared__ uint32_t tmp[kScanThreads / 64][4], len_s[kLens], bin_s[64];
   const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
   const bool in_lds = nb <= kLens;
   BlockList* lists = a.lists + (int64_t)plane * nb;
@@ -811,14 +811,33 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
     __threadfence_block();
     __syncthreads();
   }
+  // The short dk/dv items in descending order of length, to a 64th of the full one: the last ones to start are the shortest, and runs dealt out to
+  // the XCDs in turn give all of them as much.  (Which of two of one bin goes first is left open: it changes no sum.)
+  auto length_of = [&](int j) { return in_lds ? len_s[j] : lists[j].len; };
+  auto bin_of = [&](uint32_t rest) { return 63u - (uint32_t)(((uint64_t)rest * 64 - 1) / (uint32_t)a.chunk_rows); };      // 0 < rest < chunk_rows
+  if (dkdv) {
+    if (tid < 64) bin_s[tid] = 0u;
+    lds_barrier();
+    for (int j = tid; j < nb; j += kScanThreads) {
+      const uint32_t rest = length_of(j) % (uint32_t)a.chunk_rows;
+      if (rest) atomicAdd(&bin_s[bin_of(rest)], 1u);
+    }
+    lds_barrier();
+    if (tid < 64) {
+      const uint32_t n = bin_s[tid];
+      bin_s[tid] = wave_scan(n) - n;
+    }
+    lds_barrier();
+  }
   uint32_t before[4] = {0, 0, 0, 0};                             // short dk/dv items, tiles, dk/dv items of full length, partial sums of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    const uint32_t len = j < nb ? (in_lds ? len_s[j] : lists[j].len) : 0u, full = dkdv ? len / (uint32_t)a.chunk_rows : 0u;
+    const uint32_t len = j < nb ? length_of(j) : 0u, full = dkdv ? len / (uint32_t)a.chunk_rows : 0u;
     const uint32_t rest = dkdv && len > full * (uint32_t)a.chunk_rows ? 1u : 0u, parts = full + rest > 1 ? full + rest : 0u;
     uint32_t v[4] = {rest * (uint32_t)a.n_sub, (len + kBlockTileRows - 1) / kBlockTileRows, full * (uint32_t)a.n_sub, parts}, total[4];
     scan_add(tmp, tid, v, total);
-    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], before[0] + v[0], parts, before[3] + v[3]};
+    const uint32_t rest0 = rest ? atomicAdd(&bin_s[bin_of(len - full * (uint32_t)a.chunk_rows)], 1u) * (uint32_t)a.n_sub : 0u;
+    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], rest0, parts, before[3] + v[3]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) before[i] += total[i];
   }
