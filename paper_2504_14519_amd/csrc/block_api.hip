@@ -67,11 +67,11 @@ struct BlockWorkspace {
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
 // Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but no fewer than make the start of a
-// workgroup and its sums, which go to memory and back, a small part of it: 1536 where it owns 256 keys and has a compute unit to itself
-// (8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row, dk/dv and the sums' reduce: 1024 410 us, 1536 355, 2048 365), 512 for the smaller ones, of
-// which several share one (3 x 1337 rows of 12 heads of 64 on 64 blocks of 64 keys, 12 a row: 512 NARROW_US us, 1024 70, 1536 77, 2048 91).
+// workgroup and its sums, which go to memory and back, a small part of it: 2048 where it owns 256 keys and has a compute unit to itself
+// (8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row, the whole backward: 1024 660 us, 1536 608, 2048 589, 2560 596), 512 for the smaller
+// ones, of which several share one (3 x 1337 rows of 12 heads of 64 on 64 blocks of 64 keys, 12 a row, kernel and reduce: 512 66 us, 1024 70, 1536 77).
 int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub, int32_t keys) {
-  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units()), least = keys == 256 ? 1536 : 512;
+  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units()), least = keys == 256 ? 2048 : 512;
   return (int32_t)(rows < least ? least : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
 }
 BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)

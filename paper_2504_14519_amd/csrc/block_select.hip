@@ -672,15 +672,28 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
   uint16_t* rank = a.ranks + first;
   const int n_slots = n_rows * a.top_k;
   uint32_t* counts = a.counts + (int64_t)plane * a.n_blocks * count_stride(a.n_list_chunks) + chunk;
-  for (int i = tid; i < n_slots; i += kListThreads) index[i] = a.index[first + i];
-  lds_barrier();
   const float per_row = 1.0f / (float)a.top_k;
   auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per_row); };      // i / top_k (i < 2^14: the half keeps it off the border)
   static_assert(kListRows * kMaxTopK <= 1 << 14 && kListRows * kMaxTopK <= 32 * kListThreads, "slots of a chunk: exact quotients, a bit each");
+  // A row whose entries ascend up to its fill-up names no block twice; where all of the chunk's do (the selection's do) no slot has to look at the ones
+  // before it.
+  __shared__ uint32_t disorder[kListThreads / 64];
+  bool unordered = false;
+  for (int i = tid; i < n_slots; i += kListThreads) {
+    const int j = a.index[first + i], before = a.index[first + (i > 0 ? i - 1 : 0)];
+    index[i] = j;
+    unordered |= j >= a.first_block && i != row_of(i) * a.top_k && (before < a.first_block || before >= j);
+  }
+  const uint64_t some = __builtin_amdgcn_ballot_w64(unordered);
+  if ((tid & 63) == 0) disorder[tid >> 6] = some != 0;
+  lds_barrier();
+  uint32_t repeats = 0;                              // may there be any?
+#pragma unroll
+  for (int w = 0; w < kListThreads / 64; ++w) repeats |= disorder[w];
   uint32_t ok = 0;                                   // bit: this thread's slots
   for (int i = tid, u = 0; i < n_slots; i += kListThreads, ++u) {
     const int row = row_of(i);
-    const bool v = block_slot_valid(a, index + row * a.top_k, i - row * a.top_k, a.q_offset + (row0 + row) % a.s_q);
+    const bool v = block_slot_valid(a, index + row * a.top_k, i - row * a.top_k, a.q_offset + (row0 + row) % a.s_q, repeats != 0);
     valid[i] = v ? 0.f : -INFINITY;
     ok |= v ? 1u << u : 0u;
   }
@@ -716,10 +729,13 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
 __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int dkdv) {
   const int plane = blockIdx.y, rows = a.group * a.s_q;
   const int64_t n_slots = (int64_t)rows * a.top_k, i = (int64_t)blockIdx.x * 256 + threadIdx.x, at = plane * n_slots + i;
-  if (i >= n_slots || a.part_lse[at] != 0.f) return;
-  const int j = a.index[at] - a.first_block, rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
+  if (i >= n_slots) return;
+  const int j = a.index[at] - a.first_block;
+  const uint32_t rank = a.ranks[at];                 // (read beside what says whether the slot counts, not behind it)
+  if (a.part_lse[at] != 0.f) return;
+  const int rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
   const BlockList list = a.lists[(int64_t)plane * a.n_blocks + j];
-  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * count_stride(a.n_list_chunks) + rh / kListRows] + a.ranks[at], to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
+  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * count_stride(a.n_list_chunks) + rh / kListRows] + rank, to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
   a.entries[(int64_t)plane * a.item_cap * kBlockTileRows + to] = {r, (uint32_t)(hl << 6 | slot), r * (uint32_t)(a.q_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.q_stride_h / 8),
                                                                    r * (uint32_t)(a.do_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.do_stride_h / 8)};
   // the first row of a tile writes the tile down

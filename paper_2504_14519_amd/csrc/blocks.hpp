@@ -78,12 +78,12 @@ struct BlockArgs {
 };
 
 // Whether a slot of a row holds a block that the call computes: a block of the range that the row does not lie before,
-// and not one that an earlier slot of the row has named already.
-inline __host__ __device__ bool block_slot_valid(const BlockArgs& a, const int32_t* row_index, int slot, int64_t pos) {
+// and not one that an earlier slot of the row has named already (not looked for without `repeats`).
+inline __host__ __device__ bool block_slot_valid(const BlockArgs& a, const int32_t* row_index, int slot, int64_t pos, bool repeats = true) {
   const int32_t j = row_index[slot];
   if (j < a.first_block || j - a.first_block >= a.n_blocks) return false;
   if (a.causal && (int64_t)j * a.block_len > pos) return false;
-  for (int i = 0; i < slot; ++i)
+  for (int i = 0; repeats && i < slot; ++i)
     if (row_index[i] == j) return false;
   return true;
 }
