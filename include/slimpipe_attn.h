@@ -265,8 +265,8 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
 
 /* Forward: row r of head h attends to the keys that slimpipe_attn_fwd would let it see and that lie in one of its blocks.  Any index will
  * do: entries outside the range's blocks are no block, a block named twice counts once, order is free.  out, lse, rows without a key and
- * keys that no row sees: as in slimpipe_attn_fwd.  A bf16 out is folded from bf16 results of a row's blocks (weights and sums in
- * float32), a float32 one from float32 results; likewise dq in the backward.  Results do not depend on the order in which workgroups run. */
+ * keys that no row sees: as in slimpipe_attn_fwd.  A bf16 out is folded from results of a row's blocks in float16 with a float32
+ * scale (weights and sums in float32), a float32 one from float32 results; likewise dq in the backward.  Results do not depend on the order in which workgroups run. */
 int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
                             int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
                             size_t workspace_bytes, void* hip_stream);

@@ -63,7 +63,7 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where the parts of the workspace lie, and its size.
 struct BlockWorkspace {
-  size_t part_out, part_lse, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
+  size_t part_out, part_lse, part_scale, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
 };
 // Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but no fewer than make the start of a
@@ -83,6 +83,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
   auto take = [&](size_t bytes) { const size_t o = at; at += up(bytes); return o; };
   w.part_out = take(rows * top_k * p->head_dim * 4);
   w.part_lse = take(rows * top_k * 4);
+  w.part_scale = take(rows * top_k * 4);
   if (lists) {
     w.n_list_chunks = (int32_t)((plane_rows + kListRows - 1) / kListRows);
     // every tile but a block's last is full
@@ -130,6 +131,7 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->do_stride_b = p->do_stride_b; a->do_stride_s = p->do_stride_s; a->do_stride_h = p->do_stride_h;
   a->part_out = ws + w.part_out;
   a->part_lse = reinterpret_cast<float*>(ws + w.part_lse);
+  a->part_scale = reinterpret_cast<float*>(ws + w.part_scale);
   a->n_list_chunks = w.n_list_chunks;
   a->ranks = reinterpret_cast<uint16_t*>(ws + w.ranks);
   a->counts = reinterpret_cast<uint32_t*>(ws + w.counts);
@@ -235,7 +237,8 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
   a.out = out;
   a.lse = lse;
-  a.out_f32 = a.part_f32 = p->out_dtype == SLIMPIPE_F32;
+  a.out_f32 = p->out_dtype == SLIMPIPE_F32;
+  a.part_f32 = a.out_f32 || few;
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (few) {
@@ -244,7 +247,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
     return SLIMPIPE_ELAUNCH;
   }
   PartMergeArgs m;
-  m.part_out = a.part_out; m.part_f32 = a.part_f32; m.part_lse = a.part_lse; m.parts = top_k; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
+  m.part_out = a.part_out; m.part_f32 = a.part_f32; m.part_scale = a.part_scale; m.part_lse = a.part_lse; m.parts = top_k; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
   m.rows = rows_of(p);
   m.out = out; m.lse = lse;
   m.o_stride_b = p->o_stride_b; m.o_stride_s = p->o_stride_s; m.o_stride_h = p->o_stride_h;

@@ -136,9 +136,10 @@ __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a)
       if constexpr (F32) {
         x += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
       } else {
-        const bf16x4 y = *reinterpret_cast<const bf16x4*>(static_cast<const bf16_t*>(a.part_out) + at);
+        const f16x4 y = *reinterpret_cast<const f16x4*>(static_cast<const _Float16*>(a.part_out) + at);
+        const float w = a.part_scale[row * a.top_k + s];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += (float)y[e];
+        for (int e = 0; e < 4; ++e) x[e] += w * (float)y[e];
       }
     }
   const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;

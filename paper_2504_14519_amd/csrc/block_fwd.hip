@@ -2,9 +2,9 @@
 //
 // A tile is up to 128 rows that chose one block (block_select.hip): four waves of 32 rows each, the block's keys in tiles of 64 through
 // two LDS slots.  Every (row, slot) leaves out and lse of its block's keys; part_merge.hip folds a row's slots in 32 bits.  Where the result is
-// bf16 so are the partial outs (lse is float32 always): their roundings, each half a step of a value whose weight is its share of the row,
-// add at most half a step of the weighted mean of |v|, no more than the rounding of the probabilities does, and the bytes of the partial
-// outs, which every one of them costs twice, are what the fold and a third of the tiles' epilogue take.
+// bf16 the partial outs have 16 bits (float16 with a float32 scale a row; lse is float32 always): rounded to 2^-11 of themselves they add an
+// eighth of what one rounding to bf16 does, and the bytes of the partial outs, which every one of them costs twice, are what the fold and a
+// third of the tiles' epilogue take.
 #include "block_tile.hpp"
 #include "row_tile.hpp"
 #include "tile_common.hpp"
@@ -179,8 +179,7 @@ __global__ __launch_bounds__(256) void block_fwd_few_kernel(const BlockArgs a) {
     }
     const bool none = sum == 0.f;                    // (a NaN is not that)
     const float r = none ? 0.f : o / sum;
-    if (a.part_f32) static_cast<float*>(a.part_out)[item * D + tid] = r;
-    else static_cast<bf16_t*>(a.part_out)[item * D + tid] = (bf16_t)r;
+    static_cast<float*>(a.part_out)[item * D + tid] = r;
     if (tid == 0) a.part_lse[item] = none ? -INFINITY : (mx + __builtin_log2f(sum)) * kLn2;
   }
 }

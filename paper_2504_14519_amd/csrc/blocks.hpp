@@ -52,8 +52,9 @@ struct BlockArgs {
   int32_t* n_items;              // [plane]
   int32_t item_cap;
   // partial results (workspace), rows in the order (batch index, query head, row of the slice)
-  void* part_out;                // [row][top_k][head_dim], float32 or bf16
+  void* part_out;                // [row][top_k][head_dim], float32, or float16 to be multiplied by part_scale
   int32_t part_f32;
+  float* part_scale;             // [row][top_k]
   float* part_lse;               // [row][top_k]; -inf: the slot has no result
   void* out;
   float* lse;                    // forward: written.  backward: the saved one

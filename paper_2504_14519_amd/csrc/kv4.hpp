@@ -38,7 +38,8 @@ struct Kv4Args {
 
 // Folds the partial results of every row: lse = ln sum_i exp(lse_i), out = sum_i exp(lse_i - lse) out_i, in the order of the parts.
 struct PartMergeArgs {
-  const void* part_out;          // [row][parts][head_dim], rows in the order (batch index, query head, row of the slice); float32 or bf16
+  const void* part_out;          // [row][parts][head_dim], rows in the order (batch index, query head, row of the slice); float32, or float16
+  const float* part_scale;       // [row][parts]: what float16 ones are to be multiplied by
   const float* part_lse;         // [row][parts]; -inf: no result, its part_out is not read
   int32_t part_f32, parts, s_q, n_q_heads, out_f32;
   int64_t rows;

@@ -161,7 +161,7 @@ int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, co
   if (launch_kv4_fwd(a, p->head_dim, plan.few, st) != hipSuccess) return SLIMPIPE_ELAUNCH;
   if (plan.parts <= 1) return SLIMPIPE_OK;
   PartMergeArgs m;
-  m.part_out = a.part_out; m.part_f32 = 1; m.part_lse = a.part_lse; m.parts = plan.parts; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
+  m.part_out = a.part_out; m.part_f32 = 1; m.part_scale = nullptr; m.part_lse = a.part_lse; m.parts = plan.parts; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;
   m.rows = (int64_t)p->batch * p->n_q_heads * p->s_q;
   m.out = out; m.lse = lse;
   m.o_stride_b = p->o_stride_b; m.o_stride_s = p->o_stride_s; m.o_stride_h = p->o_stride_h;

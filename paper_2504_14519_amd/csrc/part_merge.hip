@@ -34,7 +34,7 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
   for (int s = first; s < a.parts; s += step) {
     const float ls = lp[s];
     if (ls == -INFINITY) continue;
-    const float w = exp2_fast((ls - m) * kLog2e);      // (m is -inf only where all are that or NaN, which gives NaN)
+    float w = exp2_fast((ls - m) * kLog2e);      // (m is -inf only where all are that or NaN, which gives NaN)
     l += w;
     const int64_t at = (row * a.parts + s) * D + d;
     if constexpr (F32) {
@@ -42,7 +42,8 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
       x0 += w * src[0];
       x1 += w * src[1];
     } else {
-      const bf16x8 x = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.part_out) + at);
+      const f16x8 x = *reinterpret_cast<const f16x8*>(static_cast<const _Float16*>(a.part_out) + at);
+      w *= a.part_scale[row * a.parts + s];
 #pragma unroll
       for (int e = 0; e < 4; ++e) { x0[e] += w * (float)x[e]; x1[e] += w * (float)x[4 + e]; }
     }

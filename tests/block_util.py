@@ -47,7 +47,7 @@ def visible(index, offset, begin, end, block, causal, N):
 class Reference:
     """Forward (and, given d_out, backward) in 64 bits; *_tol: how far a right result may be off, element by element."""
 
-    def __init__(self, q, k, v, see, scale, out_bf16=True, parts_bf16=False):
+    def __init__(self, q, k, v, see, scale, out_bf16=True, parts_16=False):
         self.q, self.k, self.v, self.see, self.scale = q, k, v, see, scale
         B, s, Hq, D = q.shape
         g = Hq // k.shape[2]
@@ -66,10 +66,11 @@ class Reference:
         out = self.p @ V
         mag = self.p @ np.abs(V)
         tol = mag * (HALF_BF16 + 2.0 * self.f32) + (np.abs(out) * HALF_BF16 if out_bf16 else 0.0)
-        # A row folded from bf16 results of its blocks: part b of weight w_b (their sum is 1) is off by 2^-8 |o_b|, and
+        # A row folded from 16-bit results of its blocks: part b of weight w_b (their sum is 1) is float16 times a scale that brings its row's
+        # largest element to 2^14, so off by 2^-11 |o_b|, or by 2^-25 2^-14 of the largest where float16 is subnormal, and
         # sum_b w_b |o_b| <= sum_j p_j |v_j|.
-        self.parts_bf16 = parts_bf16
-        tol = tol + (mag * HALF_BF16 if parts_bf16 else 0.0)
+        self.parts_16 = parts_16
+        tol = tol + (mag * 2.0 ** -11 + mag.max(-1, keepdims=True) * 2.0 ** -38 if parts_16 else 0.0)
         self.lse_tol = 2.0 * self.f32[..., 0]
         self.lse = self.lse[..., 0]
         self.out, self.out_tol = out.transpose(0, 2, 1, 3), tol.transpose(0, 2, 1, 3) * 1.01 + 1e-30
@@ -93,8 +94,9 @@ class Reference:
         t = np.swapaxes
         dq = (self.scale * ds @ self.K).transpose(0, 2, 1, 3)
         dq_tol = (self.scale * ds_tol @ np.abs(self.K)).transpose(0, 2, 1, 3) * 1.01 + (np.abs(dq) * HALF_BF16 if dq_bf16 else 0.0)
-        if self.parts_bf16 and dq_bf16:      # added up from bf16 parts of its blocks: 2^-8 sum_b |dq_b| <= 2^-8 scale sum_j |dS_j| |k_j|
-            dq_tol = dq_tol + HALF_BF16 * (self.scale * np.abs(ds) @ np.abs(self.K)).transpose(0, 2, 1, 3) * 1.01
+        if self.parts_16 and dq_bf16:      # added up from 16-bit parts of its blocks: sum_b |dq_b| <= scale sum_j |dS_j| |k_j|
+            dq_mag = (self.scale * np.abs(ds) @ np.abs(self.K)).transpose(0, 2, 1, 3) * 1.01
+            dq_tol = dq_tol + 2.0 ** -11 * dq_mag + 2.0 ** -38 * dq_mag.max(-1, keepdims=True)
         # (float32 sums over rows: n 2^-24 of the summed magnitudes, below 2^-12 of what one bf16 rounding of each term may give)
         dk, dv = fold(self.scale * t(ds, -1, -2) @ self.Q), fold(t(p, -1, -2) @ G)
         dk_tol, dv_tol = fold(self.scale * t(ds_tol, -1, -2) @ np.abs(self.Q)) * 1.01, fold(t(p_tol, -1, -2) @ np.abs(G)) * 1.01

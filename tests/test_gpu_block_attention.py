@@ -148,7 +148,7 @@ def test_all_blocks_chosen_is_dense(sp):
     out, lse = sp.slimpipe_attn_block_fwd(dev["q"], dev["k"], dev["v"], index, off, 0, off + s, L)
     dense, dense_lse = sp.slimpipe_attn_fwd(dev["q"], dev["k"], dev["v"], off, 0, off + s)
     see = np.broadcast_to(np.arange(off + s) <= (off + np.arange(s))[:, None], (B, Hq, s, off + s))
-    r = bu.Reference(ref["q"], ref["k"], ref["v"], see, 1 / math.sqrt(D), parts_bf16=True)
+    r = bu.Reference(ref["q"], ref["k"], ref["v"], see, 1 / math.sqrt(D), parts_16=True)
     bu.check("out", host_f64(out), r.out, r.out_tol)
     bu.check("out against dense", host_f64(out), host_f64(dense), 2 * r.out_tol)
     bu.check("lse against dense", host_f64(lse), host_f64(dense_lse), 2 * r.lse_tol)
@@ -205,7 +205,7 @@ def test_backward(sp, case, wild):
     dev, ref = tensors(B, s, N, Hq, Hkv, D, salt=top_k + 100)
     index = random_index(np.random.default_rng(s + D), B, Hq, s, top_k, -(-N // L), wild)
     idx = torch.from_numpy(index).cuda()
-    r = bu.Reference(ref["q"], ref["k"], ref["v"], bu.visible(index, off, begin, end, L, causal, N), 1 / math.sqrt(D), parts_bf16=True)
+    r = bu.Reference(ref["q"], ref["k"], ref["v"], bu.visible(index, off, begin, end, L, causal, N), 1 / math.sqrt(D), parts_16=True)
     out, lse = sp.slimpipe_attn_block_fwd(dev["q"], dev["k"], dev["v"], idx, off, begin, end, L, causal)
     dk, dv = torch.full((2,) + dev["k"].shape, 3.0, device="cuda")
     dq = sp.slimpipe_attn_block_bwd(dev["q"], dev["k"], dev["v"], idx, out, dev["do"], lse, off, begin, end, L, dk, dv, causal, dkv_accumulate=wild)

@@ -137,7 +137,7 @@ def test_lists_of_many_blocks(sp):
         nan = ~see.any((1, 2))                              # keys that no row sees stay NaN
         k[:, at[torch.from_numpy(nan[0]).cuda()]] = float("nan")
         v[:, at[torch.from_numpy(nan[0]).cuda()]] = float("nan")
-        r = bu.Reference(q64, k64, v64, see, 1 / math.sqrt(D), parts_bf16=True)
+        r = bu.Reference(q64, k64, v64, see, 1 / math.sqrt(D), parts_16=True)
         idx = torch.from_numpy(index).cuda()
         out, lse = sp.slimpipe_attn_block_fwd(q, k, v, idx, off, 0, N, L)
         bu.check("out", host_f64(out), r.out, r.out_tol)
@@ -179,7 +179,7 @@ def test_backward_of_long_blocks(sp, case):
     index = np.stack([rng.permutation(blocks)[:top_k] if top_k <= blocks else np.resize(np.arange(blocks), top_k) for _ in range(Hq * s)])
     index[rng.random(len(index)) < 0.8, 0] = begin // L       # most rows on one block (and then maybe twice)
     index = index.reshape(1, Hq, s, top_k).astype(np.int32)
-    r = bu.Reference(q64, k64, v64, bu.visible(index, off, begin, end, L, causal, N), 1 / math.sqrt(D), parts_bf16=True)
+    r = bu.Reference(q64, k64, v64, bu.visible(index, off, begin, end, L, causal, N), 1 / math.sqrt(D), parts_16=True)
     idx = torch.from_numpy(index).cuda()
     out, lse = sp.slimpipe_attn_block_fwd(q, k, v, idx, off, begin, end, L, causal)
     bu.check("out", host_f64(out), r.out, r.out_tol)
@@ -352,7 +352,7 @@ def test_training_step_over_slices(sp):
     for i in reversed(range(n)):
         qi, index, out, lse = saved[i]
         end = (i + 1) * s
-        r = bu.Reference(host_f64(qi), k64, v64, bu.visible(index.cpu().numpy(), i * s, 0, end, L, True, N), 1 / math.sqrt(D), parts_bf16=True)
+        r = bu.Reference(host_f64(qi), k64, v64, bu.visible(index.cpu().numpy(), i * s, 0, end, L, True, N), 1 / math.sqrt(D), parts_16=True)
         bu.check("out %d" % i, host_f64(out), r.out, r.out_tol)
         bu.check("lse %d" % i, host_f64(lse), r.lse, r.lse_tol)
         dq = sp.slimpipe_attn_block_bwd(qi, kc, vc, index, out, do[:, i * s:end], lse, i * s, 0, end, L, dkc, dvc)
@@ -364,3 +364,37 @@ def test_training_step_over_slices(sp):
         # one float32 addition a slice, one rounding to bf16
         got = torch.cat([sp.slimpipe_attn_finalize_bf16(x) for x in acc], 1)
         bu.check(name, host_f64(got), w, tol * (1 + 2.0 ** -7) + (bu.HALF_BF16 + n * 2.0 ** -23) * np.abs(w))
+
+
+@pytest.mark.parametrize("power", [100, -60])
+def test_values_of_any_magnitude(sp, power):
+    """Values and upstream gradients far from 1: 16-bit partial results keep their bits.  An infinite value leaves the other columns alone."""
+    import torch
+    s, off, Hq, Hkv, D, L, top_k = 300, 468, 4, 2, 128, 64, 4
+    N = off + s
+    say("magnitude 2^%d" % power)
+    q, q64 = rows((1, s, Hq, D), "q")
+    k, k64 = rows((1, N, Hkv, D), "k")
+    v, v64 = rows((1, N, Hkv, D), "v")
+    do, do64 = rows((1, s, Hq, D), "do")
+    v, v64 = v * 2.0 ** power, v64 * 2.0 ** power
+    do, do64 = do * 2.0 ** -power, do64 * 2.0 ** -power
+    index = np.random.default_rng(9).integers(0, N // L, (1, Hq, s, top_k), dtype=np.int32)
+    idx = torch.from_numpy(index).cuda()
+    r = bu.Reference(q64, k64, v64, bu.visible(index, off, 0, N, L, True, N), 1 / math.sqrt(D), parts_16=True)
+    out, lse = sp.slimpipe_attn_block_fwd(q, k, v, idx, off, 0, N, L)
+    bu.check("out", host_f64(out), r.out, r.out_tol)
+    dk, dv = torch.zeros((2,) + k.shape, device="cuda")
+    # (the gradients: with v and d_out both scaled dP keeps its size; then d_out alone, and dq is as small or large as it)
+    for scaled, scaled64 in ((do, do64), (do * 2.0 ** -20, do64 * 2.0 ** -20)):
+        dq = sp.slimpipe_attn_block_bwd(q, k, v, idx, out, scaled, lse, off, 0, N, L, dk, dv)
+        want = r.backward(host_f64(out), scaled64, host_f64(lse), True)
+        bu.check("dq", host_f64(dq), *want[0])
+    v[0, 5, :, 40] = float("inf")
+    index[..., 0] = 0                                         # every row sees key 5
+    idx = torch.from_numpy(index).cuda()
+    r = bu.Reference(q64, k64, v64, bu.visible(index, off, 0, N, L, True, N), 1 / math.sqrt(D), parts_16=True)
+    out, _ = sp.slimpipe_attn_block_fwd(q, k, v, idx, off, 0, N, L)
+    got, rest = host_f64(out), np.arange(D) != 40
+    assert np.isinf(got[..., 40]).all()
+    bu.check("the other columns", got[..., rest], r.out[..., rest], r.out_tol[..., rest])
