@@ -38,26 +38,11 @@ struct TileRows {
 };
 // A wave's 32 rows in C layout, times `factor`, to the partial results at `slot` (of the lane's row), through `part` (kOutRow<D> * 32 floats of
 // LDS of the wave's own).  In 16 bits they are float16 numbers with a power of two of the row's own in front, which brings the largest
-// finite one to 2^14 .. 2^15, and `factor` stays outside (part_scale).
+// finite one to 2^14 .. 2^15 (2^-97 and less are taken for that), and `factor` stays outside (part_scale).
 template <int D>
 SP_DEV void store_parts(const BlockArgs& a, float* part, const f32x16 (&acc)[D / 32], float factor, int64_t slot, int n_rows, int wave, int lane) {
-  if (!a.part_f32) {
-    auto largest = [&](auto&& of) {
-      float mx = 0.f;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, of(fabsf(acc[db][i])));
-      return xhalf_max(mx);
-    };
-    float mx = largest([](float x) { return x; });
-    if (__builtin_amdgcn_ballot_w64(mx == INFINITY) != 0) mx = largest([](float x) { return x < INFINITY ? x : 0.f; });
-    const uint32_t bits = __float_as_uint(mx) >> 23, e = bits < 30u ? 30u : bits;      // (its exponent + 127; smaller ones need no bits below 2^-97)
-    if (lane < 32 && wave * 32 + lane < n_rows) a.part_scale[slot] = factor * __uint_as_float((e - 14u) << 23);
-    factor = __uint_as_float((268u - e) << 23);
-  }
-  put_rows<D>(part, acc, factor, lane);
   if (a.part_f32) {
+    put_rows<D>(part, acc, factor, lane);
     constexpr int PER = D / 4, RPP = 64 / PER;
 #pragma unroll
     for (int j = 0; j < 32 / RPP; ++j) {
@@ -66,16 +51,38 @@ SP_DEV void store_parts(const BlockArgs& a, float* part, const f32x16 (&acc)[D /
       if (wave * 32 + r < n_rows)
         *reinterpret_cast<f32x4*>(static_cast<float*>(a.part_out) + to * D + lane % PER * 4) = *reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + lane % PER * 4);
     }
-  } else {
-    constexpr int PER = D / 8, RPP = 64 / PER;
+    return;
+  }
+  auto largest = [&](auto&& of) {
+    float mx = 0.f;
 #pragma unroll
-    for (int j = 0; j < 32 / RPP; ++j) {
-      const int r = j * RPP + lane / PER, d = lane % PER * 8;
-      const int64_t to = __shfl(slot, r, 64);
-      const f16x4 lo = __builtin_convertvector(*reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d), f16x4);
-      const f16x4 hi = __builtin_convertvector(*reinterpret_cast<const f32x4*>(part + r * kOutRow<D> + d + 4), f16x4);
-      if (wave * 32 + r < n_rows) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(a.part_out) + to * D + d) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, of(fabsf(acc[db][i])));
+    return xhalf_max(mx);
+  };
+  float mx = largest([](float x) { return x; });
+  if (__builtin_amdgcn_ballot_w64(mx == INFINITY) != 0) mx = largest([](float x) { return x < INFINITY ? x : 0.f; });
+  const uint32_t bits = __float_as_uint(mx) >> 23, e = bits < 30u ? 30u : bits;
+  if (lane < 32 && wave * 32 + lane < n_rows) a.part_scale[slot] = factor * __uint_as_float((e - 14u) << 23);
+  const float up = __uint_as_float((268u - e) << 23);
+  constexpr int ROW = D + 4, PER = D / 8, RPP = 64 / PER;      // (rows of two banks more than all: 32 rows' 8 bytes meet no bank twice)
+  _Float16* const h = reinterpret_cast<_Float16*>(part);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const f32x4 v = {acc[db][4 * i4] * up, acc[db][4 * i4 + 1] * up, acc[db][4 * i4 + 2] * up, acc[db][4 * i4 + 3] * up};
+      *reinterpret_cast<f16x4*>(h + (lane & 31) * ROW + 32 * db + 8 * i4 + 4 * (lane >> 5)) = __builtin_convertvector(v, f16x4);
     }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int j = 0; j < 32 / RPP; ++j) {
+    const int r = j * RPP + lane / PER, d = lane % PER * 8;
+    const int64_t to = __shfl(slot, r, 64);
+    const f16x4 lo = *reinterpret_cast<const f16x4*>(h + r * ROW + d), hi = *reinterpret_cast<const f16x4*>(h + r * ROW + d + 4);
+    if (wave * 32 + r < n_rows) *reinterpret_cast<f16x8*>(static_cast<_Float16*>(a.part_out) + to * D + d) = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 }
 
