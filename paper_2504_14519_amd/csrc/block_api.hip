@@ -53,8 +53,10 @@ int64_t blocks_of(int64_t begin, int64_t end, int64_t block_len) { return end > 
 
 int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->batch * p->n_q_heads * p->s_q; }
 
-// Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot).
-bool few_rows(const slimpipe_attn_params* p, int32_t top_k) { return rows_of(p) * top_k <= 4 * (int64_t)compute_units(); }
+// Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot): up to 8 of these a compute unit.  8 heads, 16 slots, us with
+// a workgroup each and with lists: 4 rows on blocks of 256 (512 slots) 18 and 38, 16 rows (2048) 38 and 55, 32 rows (4096) 65 and 62; 16 rows on
+// blocks of 64 at head_dim 64 (2048) 42 and 41.
+bool few_rows(const slimpipe_attn_params* p, int32_t top_k) { return rows_of(p) * top_k <= 8 * (int64_t)compute_units(); }
 
 // Items of a table, and workgroups of its launch: whole rounds of runs (xcd_item), one at least.
 int32_t whole_rounds(size_t n) { return (int32_t)((n + 8 * kXcdRun - 1) / (8 * kXcdRun) * (8 * kXcdRun)) + (n == 0 ? 8 * kXcdRun : 0); }
@@ -64,15 +66,27 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 // Where the parts of the workspace lie, and its size.
 struct BlockWorkspace {
   size_t part_out, part_lse, part_scale, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
-  int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_cap, part_cap;
+  int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_keys, dkdv_cap, part_cap;
 };
-// Rows of a list that one dk/dv workgroup walks: as many as leave a dozen workgroups a compute unit, but no fewer than make the start of a
-// workgroup and its sums, which go to memory and back, a small part of it: 2048 where it owns 256 keys and has a compute unit to itself
-// (8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row, the whole backward: 1024 660 us, 1536 608, 2048 589, 2560 596), 512 for the smaller
-// ones, of which several share one (3 x 1337 rows of 12 heads of 64 on 64 blocks of 64 keys, 12 a row, kernel and reduce: 512 66 us, 1024 70, 1536 77).
+// Keys of a dk/dv workgroup: 256 at head_dim 128 where the parts of a block are whole but for a quarter of the last, or there are many; else 128,
+// or 64 in the smallest blocks.  Whole backwards, 8192 rows of 8 heads, 8 blocks a row, us with 256 and with 128 keys: blocks of 256 406 and
+// 427, 384 560 and 526, 512 609 and 642, 1024 1065 and 1143; 4096 rows, 4 blocks a row: 192 146 and 152, 320 187 and 180, 448 197 and 204, 576 240 and
+// 232, 704 247 and 254.  At head_dim 64 256 keys were never faster (blocks of 256 251 and 238, 1024 646 and 643) and have no kernel.
+int32_t dkdv_keys(int32_t block_len, int32_t head_dim) {
+  if (head_dim == 128 && (block_len % 256 == 0 || block_len % 256 > 128 || block_len >= 1024)) return 256;
+  return block_len >= 128 ? 128 : 64;
+}
+// Rows of a list that one of them walks: few enough that there are three full parts for four compute units (256 keys, one workgroup a unit),
+// two for each (128) or four (64), within what keeps a workgroup's start and its sums, which go to memory and back, a small part of it, and
+// workspaces small (no more than a dozen a unit).  Whole backwards of 8 heads at head_dim 128, us: 8192 rows, 8 blocks of 512 a row (2048 by
+// the rule): 1024 660, 1536 608, 2048 589, 2560 596; 1500 rows, 4 of 512 (512): 384 121, 512 109, 1024 123, 2048 164; 4096 rows, 4 of 256, 128 keys
+// (512): 256 190, 512 163, 768 155, 1024 162, 2048 200; 500 rows, 4 of 64 at head_dim 64 (256): 256 56, 512 63, 1024 78.
 int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub, int32_t keys) {
-  const int64_t rows = slots * n_sub / (12 * (int64_t)compute_units()), least = keys == 256 ? 2048 : 512;
-  return (int32_t)(rows < least ? least : rows > 1 << 20 ? 1 << 20 : rows / 32 * 32);
+  const int64_t cus = compute_units(), work = slots * n_sub, least = keys == 256 ? 512 : 256, most = keys == 256 ? 2048 : 1536;
+  int64_t rows = work / (keys == 256 ? 3 * cus / 4 : keys == 128 ? 2 * cus : 4 * cus);
+  rows = rows < least ? least : rows > most ? most : rows;
+  if (rows < work / (12 * cus)) rows = work / (12 * cus);
+  return (int32_t)(rows > 1 << 20 ? 1 << 20 : (rows + 31) / 32 * 32);
 }
 BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)
   BlockWorkspace w;
@@ -101,7 +115,7 @@ BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t 
     w.lse2 = take(rows * 4);
     w.inf = take(4);
     const size_t slots = plane_rows * top_k;
-    const int32_t keys = block_dkdv_keys(block_len);
+    const int32_t keys = w.dkdv_keys = dkdv_keys(block_len, p->head_dim);
     w.n_sub = (block_len + keys - 1) / keys;
     w.chunk_rows = dkdv_chunk_rows((int64_t)(rows * top_k), w.n_sub, keys);
     // a list of n rows has at most n / chunk_rows + 1 parts, and partial sums only when n > chunk_rows: then at most twice n / chunk_rows
@@ -143,7 +157,7 @@ void fill(BlockArgs* a, const slimpipe_attn_params* p, const void* q, const int3
   a->delta = reinterpret_cast<float*>(ws + w.delta);
   a->lse2 = reinterpret_cast<float*>(ws + w.lse2);
   a->inf = reinterpret_cast<float*>(ws + w.inf);
-  a->chunk_rows = w.chunk_rows; a->n_sub = w.n_sub; a->dkdv_cap = w.dkdv_cap; a->part_cap = w.part_cap;
+  a->chunk_rows = w.chunk_rows; a->n_sub = w.n_sub; a->dkdv_keys = w.dkdv_keys; a->dkdv_cap = w.dkdv_cap; a->part_cap = w.part_cap;
   a->dkdv_items = reinterpret_cast<BlockItem*>(ws + w.dkdv_items);
   a->n_dkdv_items = reinterpret_cast<int32_t*>(ws + w.n_dkdv_items);
   a->dkdv_part = reinterpret_cast<float*>(ws + w.dkdv_part);

@@ -154,12 +154,9 @@ __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a)
 }
 
 // ------------------------------------------------------------------------------------ dk / dv
-// Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.
-SP_DEV int dkdv_run(int n_sub) { return n_sub > 2 ? 4 : 2; }
-// Keys of a workgroup: 256 where whole blocks are made of them but for a part too small to matter, else 128, or 64 in the smallest blocks.
-static bool wide_dkdv(int block_len) { return block_len % 256 == 0 || block_len % 256 > 128 || block_len >= 1024; }
-int block_dkdv_keys(int block_len) { return wide_dkdv(block_len) ? 256 : block_len >= 128 ? 128 : 64; }
-
+// Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.  (Runs of 1
+// and 4 come within 1 % on blocks of 256, 512 and 1024 keys; with long ones the XCDs have unequal work.)
+constexpr int kDkdvRun = 2;
 // What a dk/dv item has: keys [kmin, kmax) of the workgroup's KEYS exist, the first of them all lies at element `off` of chunk `chunk`.
 template <int D, int KEYS>
 struct DkdvItem {
@@ -169,7 +166,7 @@ struct DkdvItem {
   int64_t key0, off;
   bool none;
   SP_DEV DkdvItem(const BlockArgs& a, int plane, int b, int hk) {
-    const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, dkdv_run(a.n_sub), plane));
+    const int item = __builtin_amdgcn_readfirstlane(xcd_item(blockIdx.x, kDkdvRun, plane));
     none = item >= a.n_dkdv_items[2 * plane];
     if (none) return;
     it = a.dkdv_items[(int64_t)plane * a.dkdv_cap + item];
@@ -393,21 +390,20 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
 // tile u + 6.  Gathered rows come from beyond the L2, 1700 cycles and more away, longer than a phase: a group waits at the end of
 // MM(u) for what it copied in VV(u - 2) and before, and leaves the copies of VV(u - 1) under way.  Tile t is so in LDS at the end of MM(t - 1),
 // where it is needed, entries at the end of MM(t - 4), and they are read in MM(t - 3) for VV(t - 3).
-// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: WIDE_US us; with copies of tile u + 2 that are waited for in the next phase 335, with four
-// waves of 32 keys, two workgroups a compute unit and no phases 332.
-template <int D>
+// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: 277 us (a tile of 32 rows in 1.8 us, 1180 TFLOP/s while the loop runs; a workgroup's
+// start is 7.6 us, its way out 3.8).  In parts of 1536 rows, before short parts went in order of length, it was 314, with copies of tile u + 2
+// that are waited for in the next phase 335, with four waves of 32 keys, two workgroups a compute unit and no phases 332.
 struct WideLds {
-  static constexpr int BMQ = 32, SLOTS = 5, TILE = BMQ * D * 2, DO_BASE = SLOTS * TILE;      // rings of Q, dO
+  static constexpr int D = 128, BMQ = 32, SLOTS = 5, TILE = BMQ * D * 2, DO_BASE = SLOTS * TILE;      // rings of Q, dO
   static constexpr int V = 2 * SLOTS * TILE, V_BYTES = 8 * 32 * D * 2;
   static constexpr int STAT = V + V_BYTES, STAT_BYTES = 512;                   // lse2, -delta, row of the slice of a tile's 32 rows; 32 unused
   static constexpr int ENTRY = STAT + SLOTS * STAT_BYTES, ENTRY_SLOTS = 8, ENTRY_BYTES = 32 * (int)sizeof(BlockEntry);      // of either group
   static constexpr int ENTRY_RING = (ENTRY_SLOTS + 1) * ENTRY_BYTES;           // (a copy brings 64 entries: the last slot's second half is nobody's)
   static constexpr int RINGS = ENTRY + 2 * ENTRY_RING, OUT = 8 * 32 * kOutRow<D> * 4, TOTAL = RINGS > OUT ? RINGS : OUT;
 };
-template <int D>
 __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a) {
-  using L = WideLds<D>;
-  constexpr int KS = D / 16, DB = D / 32, NC = D / 8, GT = 256, RPP = GT / NC, PASSES = 32 / RPP, SLOTS = L::SLOTS, TILE = L::TILE;
+  using L = WideLds;
+  constexpr int D = L::D, DB = D / 32, NC = D / 8, GT = 256, RPP = GT / NC, PASSES = 32 / RPP, SLOTS = L::SLOTS, TILE = L::TILE;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, ql = lane & 31, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
   const bool group_b = wave_u >= 4;
@@ -425,7 +421,7 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
     for (int i = 0; i < 16; ++i) { st.dk[db][i] = 0.f; st.dv[db][i] = 0.f; }
   // this group's operand, and its thread's part of a tile copy: rows crow + n * RPP, the chunk that the swizzle puts at its place
   const int gtid = tid & (GT - 1), crow = gtid / NC, cpos = gtid % NC;
-  const int c8 = (D == 128 ? ((((cpos >> 2) ^ crow) & 3) << 2) | (((cpos & 3) ^ (crow >> 2)) & 3) : (cpos ^ crow) & (NC - 1)) * 8;
+  const int c8 = (((((cpos >> 2) ^ crow) & 3) << 2) | (((cpos & 3) ^ (crow >> 2)) & 3)) * 8;
   static_assert(RPP % 16 == 0, "the rows of a thread have one swizzle phase");
   const bf16_t* const src = (group_b ? a.d_out + (int64_t)b * a.do_stride_b + (int64_t)hk * a.group * a.do_stride_h
                                      : a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h) + c8;
@@ -443,7 +439,7 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
     nx.row = e->row;
     nx.head_slot = e->head_slot;
   };
-  // Copy instructions of a vector phase, the same number in every one: group B two of them less (and PASSES is 1 at head_dim 64).
+  // Copy instructions of a vector phase, the same number in every one: group B two of them less.
   constexpr int COPIES_B = PASSES + 1, COPIES_A = COPIES_B + 2;
   auto copy_part = [&](int u, unsigned slot, int part) {
     if (part < PASSES)
@@ -587,23 +583,17 @@ static void launch_dkdv_t(const BlockArgs& a, hipStream_t st) {
   dim3 grid((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), block(NW * 64);
   hipLaunchKernelGGL((block_dkdv_kernel<D, NW>), grid, block, (BlockDkdvLds<D, NW>::TOTAL), st, a);
 }
-template <int D>
-static void launch_dkdv_d(const BlockArgs& a, hipStream_t st) {
-  const int keys = block_dkdv_keys(a.block_len);
-  if (keys == 256) hipLaunchKernelGGL(block_dkdv_wide_kernel<D>, dim3((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), dim3(512), WideLds<D>::TOTAL, st, a);
-  else if (keys == 128) launch_dkdv_t<D, 4>(a, st);
-  else launch_dkdv_t<D, 2>(a, st);
-}
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st) {
-  if (head_dim == 128) launch_dkdv_d<128>(a, st);
-  else launch_dkdv_d<64>(a, st);
+  if (a.dkdv_keys == 256) hipLaunchKernelGGL(block_dkdv_wide_kernel, dim3((unsigned)a.dkdv_cap, (unsigned)(a.batch * a.n_kv_heads)), dim3(512), WideLds::TOTAL, st, a);
+  else if (head_dim == 128) a.dkdv_keys == 128 ? launch_dkdv_t<128, 4>(a, st) : launch_dkdv_t<128, 2>(a, st);
+  else a.dkdv_keys == 128 ? launch_dkdv_t<64, 4>(a, st) : launch_dkdv_t<64, 2>(a, st);
   return hipGetLastError();
 }
 hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
   const int64_t lanes = (a.kv_end_range - a.kv_begin) * (head_dim / 4);
   if (lanes <= 0) return hipSuccess;
   dim3 grid((unsigned)((lanes + 255) / 256), (unsigned)(a.batch * a.n_kv_heads)), block(256);
-  const int keys_pad = a.n_sub * block_dkdv_keys(a.block_len);
+  const int keys_pad = a.n_sub * a.dkdv_keys;
   if (head_dim == 128) hipLaunchKernelGGL(block_dkdv_reduce_kernel<128>, grid, block, 0, st, a, keys_pad);
   else hipLaunchKernelGGL(block_dkdv_reduce_kernel<64>, grid, block, 0, st, a, keys_pad);
   return hipGetLastError();
@@ -613,8 +603,7 @@ hipError_t opt_in_block_bwd_kernels() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<128>), attr, (int)block_dq_lds_bytes<128>());
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dq_kernel<64>), attr, (int)block_dq_lds_bytes<64>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_wide_kernel<128>), attr, WideLds<128>::TOTAL);
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_wide_kernel<64>), attr, WideLds<64>::TOTAL);
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_wide_kernel), attr, WideLds::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 4>), attr, (int)BlockDkdvLds<128, 4>::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<128, 2>), attr, (int)BlockDkdvLds<128, 2>::TOTAL);
   if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_dkdv_kernel<64, 4>), attr, (int)BlockDkdvLds<64, 4>::TOTAL);

@@ -70,7 +70,7 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 // T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
 // goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
 // again (cheaper than keeping them: 24 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
-// 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: SELECT_US us; with sorted pieces of scores kept in LDS 204, with
+// 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: 76 us; with sorted pieces of scores kept in LDS 204, with
 // every score in 64 bits on the matrix unit 550.
 
 // Places that a row's list of candidates has (what is certain and what is not): with more, which only many equal scores can bring, the row
@@ -630,10 +630,12 @@ static hipError_t launch_select_d(const BlockSelectArgs& a, bool few, hipStream_
   return launch_select_t<D, 64>(a, few, st);
 }
 // The few-row kernel has four times the workgroups, and a walk an eighth as long, for calls whose 128-row workgroups would not fill the
-// chip; its masks of a call's blocks have to fit LDS.
+// chip; its masks of a call's blocks have to fit LDS.  Means and selection, us with it and without, by 128-row workgroups: 8 of blocks of 512 at
+// head_dim 128, 64 workgroups 23 and 57, 128 36 and 58, 255 60 and 59; where lists are long its joins cost more, 24 of blocks of 64 at head_dim 64:
+// 64 26 and 50, 128 44 and 50, 255 80 and 54.
 hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, int compute_units, hipStream_t st) {
   const int64_t wgs = (a.group * (int64_t)a.s_q + 127) / 128 * a.n_kv_heads * a.batch;
-  const bool few = wgs < compute_units && a.n_blocks <= kFewTiles * 32;
+  const bool few = wgs < (a.top_k <= 16 ? compute_units : compute_units / 2) && a.n_blocks <= kFewTiles * 32;
   return head_dim == 128 ? launch_select_d<128>(a, few, st) : launch_select_d<64>(a, few, st);
 }
 

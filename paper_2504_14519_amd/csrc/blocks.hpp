@@ -15,7 +15,9 @@ inline __host__ __device__ int count_stride(int n_list_chunks) { return (n_list_
 constexpr int kListRows = 256;
 constexpr int kListBlocks = 1024;
 constexpr int kBlockTileRows = 128;      // rows of a tile of the forward and dq kernels
-constexpr int kXcdRun = 16;              // tiles that follow each other on one XCD (xcd_item); the tables of items are whole rounds of eight runs
+// Tiles that follow each other on one XCD (xcd_item); the tables of items are whole rounds of eight runs.  (8192 rows of 8 heads on 128 blocks of
+// 512 keys, 8 a row, forward: runs of 16 213 us, 1 221, 4 224, 64 220.)
+constexpr int kXcdRun = 16;
 
 // One row of a list: row of the slice, (head within the group << 6 | slot), and where its q and d_out lie behind those of the plane's first
 // row, in units of 8 elements.  A block's list starts on a multiple of kBlockTileRows entries, so that tile t's are known without its item.
@@ -69,6 +71,7 @@ struct BlockArgs {
   float* dk_acc[kMaxChunks];
   float* dv_acc[kMaxChunks];
   int32_t chunk_rows;            // rows of a list that one dk/dv workgroup sums (a multiple of 32)
+  int32_t dkdv_keys;             // keys of a dk/dv workgroup: 256, 128 or 64
   int32_t n_sub;                 // parts of a block's keys that have a dk/dv workgroup each
   BlockItem* dkdv_items;         // [plane][dkdv_cap]
   int32_t* n_dkdv_items;         // [plane][2]: all of them, those of full length
@@ -116,7 +119,6 @@ hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st)
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st);
-int block_dkdv_keys(int block_len);      // keys of a dk/dv workgroup
 hipError_t opt_in_block_select_kernels();
 hipError_t opt_in_block_fwd_kernels();
 hipError_t opt_in_block_bwd_kernels();

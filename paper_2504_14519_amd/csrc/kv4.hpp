@@ -52,7 +52,7 @@ hipError_t launch_part_merge(const PartMergeArgs& a, int head_dim, hipStream_t s
 hipError_t launch_kv4_store(const Kv4CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv4_load(const Kv4CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv4_fwd(const Kv4Args& a, int head_dim, bool few, hipStream_t st);      // few: group * s_q <= kKv4FewRows
-constexpr int kKv4FewRows = 32;
+constexpr int kKv4FewRows = 32;      // (8 heads on 100000 keys, us with the kernel of few rows and the other: 2 tokens 17 and 31, 4 tokens 22 and 33)
 hipError_t opt_in_kv4_kernels();
 
 }  // namespace slimpipe

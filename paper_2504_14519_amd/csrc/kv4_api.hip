@@ -40,14 +40,17 @@ Kv4Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
   Kv4Plan plan{rows <= kKv4FewRows, 1, 1, 1, keys};
   if (plan.few) {
-    // two heads a wave: in a cache with heads next to each other their codes share lines
+    // two heads a wave: in a cache with heads next to each other their codes share lines (tokens of 4 sequences of 32K keys, us with two and with one:
+    // 40 heads 204 and 328, 8 heads 41 and 40)
     plan.wave_heads = rows <= 16 && p->n_kv_heads % 2 == 0 ? 2 : 1;
     const int32_t sets = p->n_kv_heads / plan.wave_heads;
     plan.heads_wg = sets % 4 == 0 ? 4 : sets % 2 == 0 ? 2 : 1;
   }
   const int64_t wgs = plan.few ? planes / (plan.wave_heads * plan.heads_wg) : planes * ((rows + 127) / 128), want = 2 * (int64_t)compute_units();
-  const int64_t least = plan.few ? 256 : 1024;       // keys of a part
-  // tokens: whole rounds of the workgroups that the chip holds, eight ranges at a time (ranges of the same keys share an XCD)
+  // keys of a part (a token of 8 heads on 8000 keys: 256 11.9 us, 512 12.3, 1024 15.7; 256 rows on 8000 keys: 512 34.5 us, 1024 37.3, 2048 53.9)
+  const int64_t least = plan.few ? 256 : 512;
+  // tokens: whole rounds of the workgroups that the chip holds, two a unit (a token behind 1M keys: one a unit 43 us, two 35, four 42), eight ranges
+  // at a time (ranges of the same keys share an XCD)
   int64_t parts = plan.few ? want / wgs : (want + wgs - 1) / wgs;
   if (plan.few && parts >= 8) parts = parts / 8 * 8;
   if (parts > keys / least) parts = keys / least;
