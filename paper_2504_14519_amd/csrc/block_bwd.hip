@@ -37,10 +37,8 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
   const int64_t row = ((int64_t)b * a.n_q_heads + h) * a.s_q + e.row;
 
   const BlockKeys keys(a, it.block, b, hk);
-  int64_t see = keys.hi - 1;
-  if (a.causal && a.q_offset + e.row < see) see = a.q_offset + e.row;
-  const int see_rel = (int)(see - keys.lo);
-  const int n_keys = rows_max(see_rel, reinterpret_cast<int*>(smem), wave_u, lane) + 1;      // (keys behind are not read)
+  const TileSight sight(a, keys, e.row, reinterpret_cast<int*>(smem), wave_u, lane);
+  const int see_rel = sight.see_rel, n_keys = sight.n_keys;
   const int nt = n_keys > 0 ? (n_keys + BN - 1) / BN : 0;
   const unsigned lds = lds_addr(smem);
   const uint32_t row_bytes = (uint32_t)a.kv_stride_s * 2;

@@ -33,12 +33,8 @@ __global__ __launch_bounds__(256, 2) void block_fwd_kernel(const BlockArgs a) {
   const int h = hk * a.group + (int)(e.head_slot >> 6);
 
   const BlockKeys keys(a, it.block, b, hk);
-  // Last key that the row sees, relative to the first of the block (negative: none), and how many the tile's rows see: keys behind
-  // these are not read (they may hold anything, and a weight of 0 times a NaN is a NaN).
-  int64_t see = keys.hi - 1;
-  if (a.causal && a.q_offset + e.row < see) see = a.q_offset + e.row;
-  const int see_rel = (int)(see - keys.lo);
-  const int n_keys = rows_max(see_rel, reinterpret_cast<int*>(smem), wave_u, lane) + 1;
+  const TileSight sight(a, keys, e.row, reinterpret_cast<int*>(smem), wave_u, lane);
+  const int see_rel = sight.see_rel, n_keys = sight.n_keys;
   const int nt = n_keys > 0 ? (n_keys + BN - 1) / BN : 0;
   const unsigned lds = lds_addr(smem);
   const uint32_t row_bytes = (uint32_t)a.kv_stride_s * 2;

@@ -86,20 +86,31 @@ SP_DEV void store_parts(const BlockArgs& a, float* part, const f32x16 (&acc)[D /
   }
 }
 
-// Maximum of v over four waves (its lanes 32 .. 63 hold what 0 .. 31 do), through `tmp` in LDS, which is free again afterwards.
-SP_DEV int rows_max(int v, int* tmp, int wave, int lane) {
+// What the rows of a tile see of its block: the last key that the lane's row does, relative to the first (negative: none), and how many some row
+// does: keys behind these are not read (they may hold anything, and a weight of 0 times a NaN is a NaN).  `tmp`: LDS for four numbers, free
+// again afterwards.
+struct TileSight {
+  int see_rel, n_keys;
+  SP_DEV TileSight(const BlockArgs& a, const BlockKeys& keys, uint32_t row, int* tmp, int wave, int lane) {
+    see_rel = (int)(keys.hi - 1 - keys.lo);
+    n_keys = see_rel + 1;
+    if (!a.causal || a.q_offset >= keys.hi - 1) return;      // every row of the call sees the whole block
+    const int64_t see = a.q_offset + row - keys.lo;
+    see_rel = see < see_rel ? (int)see : see_rel;
+    int v = see_rel;
 #pragma unroll
-  for (int w = 1; w < 32; w <<= 1) {
-    const int o = __shfl_xor(v, w, 64);
-    v = v > o ? v : o;
+    for (int w = 1; w < 32; w <<= 1) {                       // (lanes 32 .. 63 hold what 0 .. 31 do)
+      const int o = __shfl_xor(v, w, 64);
+      v = v > o ? v : o;
+    }
+    if (lane == 0) tmp[wave] = v;
+    __syncthreads();
+    int m = tmp[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = m > tmp[w] ? m : tmp[w];
+    __syncthreads();
+    n_keys = __builtin_amdgcn_readfirstlane(m) + 1;
   }
-  if (lane == 0) tmp[wave] = v;
-  __syncthreads();
-  int m = tmp[0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) m = m > tmp[w] ? m : tmp[w];
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(m);
-}
+};
 
 }  // namespace slimpipe
