@@ -57,19 +57,19 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 }
 
 // ------------------------------------------------------------------------------------ selection
-// score[r][j] = q_r . mean_j, compared in 64 bits, without computing most of it in 64 bits.  A float32 mean is exactly the sum of three bf16
-// numbers, each 2^-8 of the one before at most, so bf16 matrix instructions give every score with float32 additions alone as its error.
-// The smallest parts go first: only the D products of the largest are added at the size of the score, so that it is off by at most
-//   delta_r = (9/8) D 2^-23 |q_r| max_j |mean_j|.
+// score[r][j] = q_r . mean_j, compared in 64 bits, without computing most of it in 64 bits.  A float32 mean is the sum of two bf16 numbers to 2^-16
+// of itself (each rounded to 2^-8), so bf16 matrix instructions give every score with that and float32 additions as its error.  The
+// smaller parts go first: only the D products of the larger ones are added at the size of the score, so that it is off by at most
+//   delta_r = ((9/8) D 2^-23 + 2^-16) |q_r| max_j |mean_j|.
 // If T is the n-th largest of the approximate scores of a row, the exact n-th largest lies within delta of T: what is above T + 2 delta is
 // taken for certain, what is below T - 2 delta is not, and only where more lies between than there are places are scores computed in
-// 64 bits (one row in a hundred).  Where products might run into the smallest float32 numbers (|q| or max |mean| below 2^-40: the bound has
+// 64 bits (one row in fifty).  Where products might run into the smallest float32 numbers (|q| or max |mean| below 2^-40: the bound has
 // 2^-103 to spare then) nothing is certain.  A row of zeros, as padding has them, or means that are all zero have equal scores
 // throughout, which needs no computing.
 //
 // T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
 // goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
-// again (cheaper than keeping them: 24 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
+// again (cheaper than keeping them: 16 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
 // 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: 76 us; with sorted pieces of scores kept in LDS 204, with
 // every score in 64 bits on the matrix unit 550.
 
@@ -79,26 +79,15 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 constexpr int select_places(int k) { return k <= 8 ? 16 : k <= 16 ? 28 : kMaxTopK + 32; }
 constexpr uint32_t kUnsure = 0x80000000u;      // flag of a candidate within 2 delta of T
 
-// A tile of 32 blocks of means as three bf16 parts (largest first): upper halves of floats, rounded towards zero, so that what is left is exact.
-SP_DEV void split_means(const f32x4& x0, const f32x4& x1, bf16x8 (&part)[3], float& sq) {
-  float r[8];
+// Eight elements of a mean as two bf16 parts (larger first), and their squares.
+SP_DEV void split_means(const f32x4& x0, const f32x4& x1, bf16x8 (&part)[2], float& sq) {
+  const bf16x4 a0 = __builtin_convertvector(x0, bf16x4), a1 = __builtin_convertvector(x1, bf16x4);
+  const f32x4 r0 = x0 - __builtin_convertvector(a0, f32x4), r1 = x1 - __builtin_convertvector(a1, f32x4);      // (exact)
+  const bf16x4 b0 = __builtin_convertvector(r0, bf16x4), b1 = __builtin_convertvector(r1, bf16x4);
+  part[0] = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+  part[1] = __builtin_shufflevector(b0, b1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    r[e] = e < 4 ? x0[e & 3] : x1[e & 3];
-    sq += r[e] * r[e];
-  }
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    u32x4 w;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const uint32_t lo = __float_as_uint(r[e]), hi = __float_as_uint(r[e + 1]);
-      w[e / 2] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
-      r[e] -= __uint_as_float(lo & 0xffff0000u);
-      r[e + 1] -= __uint_as_float(hi & 0xffff0000u);
-    }
-    part[i] = __builtin_bit_cast(bf16x8, w);
-  }
+  for (int e = 0; e < 4; ++e) sq += x0[e] * x0[e] + x1[e] * x1[e];
 }
 template <int K>
 SP_DEV void keep_largest(float (&t)[K], float x) {
@@ -192,7 +181,7 @@ SP_DEV bool means_are_zero(const float* means, int64_t n, int tid, int threads) 
 // What lies between and above: bounds that are not finite (a mean or a query that is not) or too small leave everything open.
 template <int D>
 SP_DEV void select_bounds(float t, float norm, uint32_t most, float* lo, float* hi) {
-  const float mean = __builtin_sqrtf(__uint_as_float(most)), delta = 1.125f * D * 0x1p-23f * norm * mean;
+  const float mean = __builtin_sqrtf(__uint_as_float(most)), delta = (1.125f * D * 0x1p-23f + 0x1p-16f) * norm * mean;
   const bool clear = norm >= 0x1p-40f && mean >= 0x1p-40f && delta < INFINITY && fabsf(t) < INFINITY;
   *lo = clear ? t - 2.f * delta : -INFINITY;
   *hi = clear ? t + 2.f * delta : INFINITY;
@@ -315,10 +304,10 @@ SP_DEV void settle_row(uint32_t* list, int count, int places, int need, const bf
 // from there serves R rows sets (R = 2 where the lists are short: the LDS reads of R = 1 are half of a tile's time).
 constexpr int select_sets(int k) { return k <= 16 ? 2 : 1; }
 template <int D, int K>
-constexpr size_t select_lds_bytes() { return (size_t)2 * 3 * 32 * D * 2 + (size_t)128 * select_sets(K) * select_places(K) * 4; }
+constexpr size_t select_lds_bytes() { return (size_t)2 * 2 * 32 * D * 2 + (size_t)128 * select_sets(K) * select_places(K) * 4; }
 template <int D, int K>
 __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectArgs a) {
-  constexpr int KS = D / 16, PART = 32 * D * 2, SLOT = 3 * PART, PLACES = select_places(K), PER = D / 8 / 8;      // 16-byte chunks of a part a thread writes
+  constexpr int KS = D / 16, PART = 32 * D * 2, SLOT = 2 * PART, PLACES = select_places(K), PER = D / 8 / 8;      // 16-byte chunks of a part a thread writes
   constexpr int R = select_sets(K), WROWS = 32 * R;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   __shared__ uint32_t most_s;                        // largest |mean|^2 (bits of a float; all are >= 0)
@@ -360,10 +349,10 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
     float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      bf16x8 part[3];
+      bf16x8 part[2];
       split_means(x[2 * i], x[2 * i + 1], part, sq);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) *reinterpret_cast<bf16x8*>(smem + (t & 1) * SLOT + p * PART + tile_off<D>(tid / 8, tid % 8 * PER + i)) = part[p];
+      for (int p = 0; p < 2; ++p) *reinterpret_cast<bf16x8*>(smem + (t & 1) * SLOT + p * PART + tile_off<D>(tid / 8, tid % 8 * PER + i)) = part[p];
     }
 #pragma unroll
     for (int w = 1; w < 8; w <<= 1) sq += __shfl_xor(sq, w, 64);
@@ -380,7 +369,7 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
       if (t + 1 < nt) fetch(t + 1);
       f32x16 s[R] = {};
 #pragma unroll
-      for (int p = 2; p >= 0; --p)
+      for (int p = 1; p >= 0; --p)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           const bf16x8 m = lds_rp<D>(lo_m, ks, p * PART);
@@ -505,16 +494,16 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
     const int j = a.first_block + t * 32 + ql;
     const float* mp = means + (int64_t)(j < stop ? j : stop - 1) * D + 8 * g;
     float sq = 0.f;
-    // (a sum for each of the parts, added up smallest first: the parts of a step are used at once and need few registers)
-    f32x16 x[3] = {};
+    // (a sum for each of the parts: the parts of a step are used at once and need few registers)
+    f32x16 x[2] = {};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      bf16x8 part[3];
+      bf16x8 part[2];
       split_means(*reinterpret_cast<const f32x4*>(mp + 16 * ks), *reinterpret_cast<const f32x4*>(mp + 16 * ks + 4), part, sq);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) x[p] = mfma32(part[p], q[ks], x[p]);
+      for (int p = 0; p < 2; ++p) x[p] = mfma32(part[p], q[ks], x[p]);
     }
-    const f32x16 s = (x[2] + x[1]) + x[0];
+    const f32x16 s = x[1] + x[0];
     sq = xhalf_sum(sq);
     most = sq == sq ? fmaxf(most, sq) : INFINITY;
     return s;
