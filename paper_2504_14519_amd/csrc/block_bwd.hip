@@ -16,6 +16,7 @@ namespace slimpipe {
 
 constexpr int kDqKeys = 64;
 
+// 8192 rows of 8 heads of 128 on 128 blocks of 512 keys, 8 a row: 212 us (910 TFLOP/s); as in the forward a workgroup's start and way out are hidden in part.
 template <int D>
 constexpr size_t block_dq_lds_bytes() {
   constexpr size_t rings = (size_t)4 * kDqKeys * D * 2, rows = (size_t)4 * 32 * kOutRow<D> * 4;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
   store_parts<D>(a, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dq, a.scale, row * a.top_k + (e.head_slot & 63u), n_rows, wave_u, lane);
 }
 
-// dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.
+// dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.  Bound by the bytes: 65536 rows of 8 slots of 128 in 35 us (4.3 TB/s).
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a) {
   constexpr int NC = D / 4;
@@ -239,6 +240,9 @@ struct BlockDkdvLds {
   static constexpr int TOTAL = RINGS > OUT ? RINGS : OUT;
 };
 
+// The other ones: a wave owns 32 keys, rows in tiles of 32 through two LDS slots, two barriers a tile; two workgroups or more share a compute unit, so that
+// one's vector work and waits are behind another's matrix work.  3 x 1337 rows of 12 heads of 64 on 64 blocks of 64 keys, 12 a row: 57 us; 8192 rows of 8
+// heads of 128 on blocks of 512, in 128 keys each: 332.
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs a) {
   using L = BlockDkdvLds<D, NW>;
@@ -388,7 +392,7 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
 // tile u + 6.  Gathered rows come from beyond the L2, 1700 cycles and more away, longer than a phase: a group waits at the end of
 // MM(u) for what it copied in VV(u - 2) and before, and leaves the copies of VV(u - 1) under way.  Tile t is so in LDS at the end of MM(t - 1),
 // where it is needed, entries at the end of MM(t - 4), and they are read in MM(t - 3) for VV(t - 3).
-// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: 277 us (a tile of 32 rows in 1.8 us, 1180 TFLOP/s while the loop runs; a workgroup's
+// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: 280 us (920 TFLOP/s; a tile of 32 rows in 1.8 us, 1180 TFLOP/s while the loop runs; a workgroup's
 // start is 7.6 us, its way out 3.8).  In parts of 1536 rows, before short parts went in order of length, it was 314, with copies of tile u + 2
 // that are waited for in the next phase 335, with four waves of 32 keys, two workgroups a compute unit and no phases 332.
 struct WideLds {
@@ -530,7 +534,8 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
   item.flush(a, plane, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, st.dk, st.dv, wave_u * 32, fresh(tid) & 63);
 }
 
-// dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.
+// dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.  Bound by the bytes (31 us
+// behind the kernel above).
 template <int D>
 __global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs a, int keys_pad) {
   constexpr int NC = D / 4;

@@ -8,7 +8,8 @@ namespace slimpipe {
 // ------------------------------------------------------------------------------------ block means
 // mean[j] = (1 / n_j) sum of the n_j keys that block j holds before kv_end.  One workgroup a block and kv head, D / 8 lanes a row
 // (16 bytes each); sums in 64 bits, in which sums of bf16 numbers of like size are exact, so that the mean is rounded once (to 32
-// bits) and does not depend on the order.  Bound by reading the keys once.
+// bits) and does not depend on the order.  Bound by reading the keys once (32 blocks of 512
+// keys of 128: 6 us, a third of it the launch).
 template <int D>
 __global__ __launch_bounds__(1024) void block_means_kernel(const BlockMeansArgs a) {
   constexpr int NC = D / 8, ROWS = 1024 / NC, WROWS = 64 / NC;
@@ -70,8 +71,8 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 // T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
 // goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
 // again (cheaper than keeping them: 16 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
-// 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: 76 us; with sorted pieces of scores kept in LDS 204, with
-// every score in 64 bits on the matrix unit 550.
+// 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: 70 us, 18 a walk (7 for Q, 4 at the end, most of it rows settled in 64 bits); with three parts of a mean 77, with sorted pieces of scores kept in LDS 204,
+// with every score in 64 bits on the matrix unit 550.
 
 // Places that a row's list of candidates has (what is certain and what is not): with more, which only many equal scores can bring, the row
 // is done in 64 bits throughout.
@@ -456,7 +457,8 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
 }
 
 // Few rows (tokens): 32 a workgroup, whose eight waves share out the tiles; means go from memory through registers to the matrix unit.  The waves'
-// lists meet in LDS, and so do the second walk's masks, a bit a block.
+// lists meet in LDS, and so do the second walk's masks, a bit a block.  8 heads of each of 4 sequences on 511 blocks of means of 128, top_k 16: 21 us, of
+// which the two tiles of scores of a wave take 8 (vector work of one compute unit), the joins 6.
 constexpr int kFewWaves = 8, kFewTiles = 512, kFewKept = 2;      // tiles of a wave whose scores stay in registers for the second walk
 template <int K>
 constexpr int few_list_stride() { return K * 32 + 8; }              // floats of a wave's lists (eight banks on, so that a row's lists are spread)
@@ -646,7 +648,7 @@ static hipError_t opt_in_select_d() {
 
 // ------------------------------------------------------------------------------------ lists
 // The rows of every block, in ascending order of (head of the group, row).  Three launches: places of the rows of a chunk within the
-// chunk, starts, entries.
+// chunk, starts, entries.  Bound by a few trips to memory each: 8192 rows of 8 heads, 8 slots, 128 blocks: 7.5, 6.5 and 8 us.
 //
 // Chunks of kListRows rows have a bit per (block, row) in LDS: setting bits commutes, and a row's place among the chunk's rows of a block
 // is a count of the bits below its own, so the lists are the same on every run.  (The index rows of a plane follow each other, and so do the

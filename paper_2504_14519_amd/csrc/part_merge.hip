@@ -50,7 +50,7 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
   }
 }
 
-// Many rows: D / 8 lanes a row.  Bound by the bytes.
+// Many rows: D / 8 lanes a row.  Bound by the bytes: 65536 rows of 8 parts of 128 in 24 us (6.3 TB/s: they have just been written).
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void part_merge_kernel(const PartMergeArgs a) {
   constexpr int NC = D / 8;
