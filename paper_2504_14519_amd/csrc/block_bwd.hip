@@ -536,13 +536,15 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
 
 // dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.  Bound by the bytes (31 us
 // behind the kernel above).
+// (From a multiple of four keys on: the keys of a wave then lie in one chunk, whose length is a multiple of 256, as kv_chunk_of has it.)
+SP_HOST_DEV int64_t dkdv_reduce_first(const BlockArgs& a) { return a.kv_begin & ~(int64_t)3; }
 template <int D>
 __global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs a, int keys_pad) {
   constexpr int NC = D / 4;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.kv_end_range - a.kv_begin, kk = gid / NC;
+  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, kk = gid / NC;
   const int c = (int)(gid - kk * NC) * 4, plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
-  if (kk >= n) return;
-  const int64_t key = a.kv_begin + kk;
+  const int64_t key = dkdv_reduce_first(a) + kk;
+  if (key < a.kv_begin || key >= a.kv_end_range) return;
   const int64_t block = key / a.block_len, j = block - a.first_block;
   uint32_t len = 0, part0 = 0;
   int parts = 0;
@@ -593,7 +595,7 @@ hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t s
   return hipGetLastError();
 }
 hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
-  const int64_t lanes = (a.kv_end_range - a.kv_begin) * (head_dim / 4);
+  const int64_t lanes = (a.kv_end_range - dkdv_reduce_first(a)) * (head_dim / 4);
   if (lanes <= 0) return hipSuccess;
   dim3 grid((unsigned)((lanes + 255) / 256), (unsigned)(a.batch * a.n_kv_heads)), block(256);
   const int keys_pad = a.n_sub * a.dkdv_keys;

@@ -194,6 +194,38 @@ def test_backward_of_long_blocks(sp, case):
         bu.check(name, got[:, begin:end], w[:, begin:end], tol[:, begin:end])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("begin", [371, 510, 253])
+def test_backward_of_chunks_behind_an_odd_first_key(sp, D, begin):
+    """Lists in several parts on either side of a chunk's end, in a range that starts at any key: each key's sums go to its own chunk, and what
+    lies behind the chunks stays as it was."""
+    import torch
+    s, off, Hq, L, C = 520, 400, 8, 64, 256
+    N = off + s
+    say("chunked reduce D=%d begin=%d" % (D, begin))
+    q, q64 = rows((1, s, Hq, D), "q")
+    do, do64 = rows((1, s, Hq, D), "do")
+    k, k64 = rows((1, N, 1, D), "k")
+    v, v64 = rows((1, N, 1, D), "v")
+    index = np.tile(np.array([3, 4, 7, 8, 11, 12], dtype=np.int32), (1, Hq, s, 1))
+    idx = torch.from_numpy(index).cuda()
+    kc, vc = ([torch.nn.functional.pad(x[:, i:i + C], (0, 0, 0, 0, 0, max(0, i + C - N))).contiguous() for i in range(0, N, C)] for x in (k, v))
+    out, lse = sp.slimpipe_attn_block_fwd(q, kc, vc, idx, off, begin, N, L)
+    r = bu.Reference(q64, k64, v64, bu.visible(index, off, begin, N, L, True, N), 1 / math.sqrt(D), parts_16=True)
+    bu.check("out", host_f64(out), r.out, r.out_tol)
+    # every chunk's accumulator with a margin of 64 rows on either side
+    room = [torch.full((1, C + 128, 1, D), 2.0, device="cuda") for _ in range(2 * len(kc))]
+    acc = [x[:, 64:64 + C] for x in room]
+    dkc, dvc = acc[:len(kc)], acc[len(kc):]
+    sp.slimpipe_attn_block_bwd(q, kc, vc, idx, out, do, lse, off, begin, N, L, dkc, dvc)
+    assert all((x[:, :64] == 2.0).all() and (x[:, 64 + C:] == 2.0).all() for x in room)
+    want = r.backward(host_f64(out), do64, host_f64(lse), True)
+    for name, chunks, (w, tol) in (("dk", dkc, want[1]), ("dv", dvc, want[2])):
+        got = host_f64(torch.cat(chunks, 1))
+        assert (got[:, :begin] == 2.0).all() and (got[:, N:] == 2.0).all()
+        bu.check(name, got[:, begin:N] - 2.0, w[:, begin:], tol[:, begin:] + 2.0 ** -22 * (2.0 + np.abs(w[:, begin:])))
+
+
 @pytest.mark.parametrize("s", [3, 300])
 def test_nan_is_not_dropped(sp, s):
     """A NaN among what a row sees makes its out and lse NaN, in either form of both attentions, and leaves rows alone that do not see it."""
