@@ -240,7 +240,7 @@ int slimpipe_attn_fwd_ranges(const slimpipe_attn_params* p, const void* q_slice,
  *   block_len : a multiple of 64, 64 .. 65536 (SLIMPIPE_EINVAL_SHAPE otherwise); with several chunks chunk_len is a multiple of it.
  *   top_k     : 1 .. 64 slots per row (SLIMPIPE_EINVAL_SHAPE otherwise).
  *   limits    : batch * n_kv_heads <= 65535, less than 2^27 rows of all heads, 2^30 slots of one kv head, less than 2^22 - 1 blocks in the key range, in the
- *               backward less than 2^27 keys there, kv_capacity <= 2^36 (SLIMPIPE_EINVAL_SHAPE otherwise); the rows of the query heads of
+ *               backward less than 2^27 - 64 keys there and rows of one kv head together, kv_capacity <= 2^36 (SLIMPIPE_EINVAL_SHAPE otherwise); the rows of the query heads of
  *               one kv head, of q and in the backward of d_out, lie within 2^35 elements (SLIMPIPE_EINVAL_STRIDE otherwise).
  *   index     : int32 [batch, n_q_heads, s_q, top_k], contiguous.
  *   means     : float32 [batch, n_kv_heads, ceil(kv_capacity / block_len), head_dim], contiguous. */

@@ -27,9 +27,9 @@ int check_blocks(const slimpipe_attn_params* p, int32_t n_chunks, int64_t chunk_
 int check_top_k(const slimpipe_attn_params* p, int32_t top_k, int is_bwd) {
   if (top_k < 1 || top_k > kMaxTopK) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t rows = (int64_t)p->n_q_heads / p->n_kv_heads * p->s_q;
-  // slots of a plane, and offsets of its rows in units of 8 elements, in 32 bits; less than 2^32 threads, 32 a row and in the backward 32 a key
+  // slots of a plane, and offsets of its rows in units of 8 elements, in 32 bits; less than 2^32 threads, 32 a row and in the backward 32 a key, too
   if (rows * top_k > (int64_t)1 << 30 || rows * p->n_kv_heads * p->batch >= 1 << 27) return SLIMPIPE_EINVAL_SHAPE;
-  if (is_bwd && p->kv_end - p->kv_begin >= 1 << 27) return SLIMPIPE_EINVAL_SHAPE;
+  if (is_bwd && rows + p->kv_end - p->kv_begin >= (1 << 27) - 64) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t heads = p->n_q_heads / p->n_kv_heads - 1, last = p->s_q - 1, most = (int64_t)1 << 35;
   if (p->q_stride_h > most / (heads + 1) || p->q_stride_h * heads + p->q_stride_s * last >= most) return SLIMPIPE_EINVAL_STRIDE;
   if (is_bwd && (p->do_stride_h > most / (heads + 1) || p->do_stride_h * heads + p->do_stride_s * last >= most)) return SLIMPIPE_EINVAL_STRIDE;
@@ -257,7 +257,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   if (few) {
     if (launch_block_fwd_few(a, p->head_dim, st) != hipSuccess) return SLIMPIPE_ELAUNCH;
-  } else if (launch_block_lists(a, false, st) != hipSuccess || launch_block_fwd(a, p->head_dim, st) != hipSuccess) {
+  } else if (launch_block_lists(a, p->head_dim, false, st) != hipSuccess || launch_block_fwd(a, p->head_dim, st) != hipSuccess) {
     return SLIMPIPE_ELAUNCH;
   }
   PartMergeArgs m;
@@ -295,28 +295,17 @@ int slimpipe_attn_block_bwd(const slimpipe_attn_params* p, const void* q_slice, 
     a.dv_acc[i] = dv_chunks[i];
   }
   fill(&a, p, q_slice, index, block_len, top_k, w, static_cast<char*>(workspace));
+  a.out = const_cast<void*>(out);
+  a.lse = const_cast<float*>(lse);
   a.d_out = static_cast<const __bf16*>(d_out);
   a.dq = dq;
   a.dq_f32 = a.part_f32 = dq_dtype == SLIMPIPE_F32; a.dq_accumulate = dq_accumulate ? 1 : 0; a.dkv_accumulate = dkv_accumulate ? 1 : 0;
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  // delta and lse in log2 units as for the dense backward, ahead of all that writes a gradient
-  BwdArgs d;
-  memset(&d, 0, sizeof(d));
-  d.out = static_cast<const __bf16*>(out);
-  d.d_out = a.d_out;
-  d.lse = lse;
-  d.delta = const_cast<float*>(a.delta);
-  d.lse2 = const_cast<float*>(a.lse2);
-  d.s_q = p->s_q; d.n_q_heads = p->n_q_heads;
-  d.o_stride_b = p->o_stride_b; d.o_stride_s = p->o_stride_s; d.o_stride_h = p->o_stride_h;
-  d.do_stride_b = p->do_stride_b; d.do_stride_s = p->do_stride_s; d.do_stride_h = p->do_stride_h;
-  hipError_t e = launch_delta(d, p->batch, p->head_dim, st);
-  if (e == hipSuccess) e = launch_block_lists(a, true, st);
-  if (e == hipSuccess) e = launch_block_bwd_dq(a, p->head_dim, st);
-  if (e == hipSuccess) e = launch_block_dq_reduce(a, p->head_dim, st);
+  hipError_t e = launch_block_lists(a, p->head_dim, true, st);
   if (e == hipSuccess) e = launch_block_bwd_dkdv(a, p->head_dim, st);
-  if (e == hipSuccess) e = launch_block_dkdv_reduce(a, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_bwd_dq(a, p->head_dim, st);
+  if (e == hipSuccess) e = launch_block_reduce(a, p->head_dim, st);
   return status(e);
 }
 

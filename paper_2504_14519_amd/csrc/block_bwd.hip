@@ -119,39 +119,6 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
   store_parts<D>(a, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dq, a.scale, row * a.top_k + (e.head_slot & 63u), n_rows, wave_u, lane);
 }
 
-// dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.  Bound by the bytes: 65536 rows of 8 slots of 128 in 35 us (4.3 TB/s).
-template <int D, bool F32>
-__global__ __launch_bounds__(256) void block_dq_reduce_kernel(const BlockArgs a) {
-  constexpr int NC = D / 4;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, row = gid / NC;
-  const int c = (int)(gid - row * NC) * 4;
-  if (row >= (int64_t)a.batch * a.n_q_heads * a.s_q) return;
-  const float* lp = a.part_lse + row * a.top_k;
-  f32x4 x = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int s = 0; s < a.top_k; ++s)
-    if (lp[s] != -INFINITY) {
-      const int64_t at = (row * a.top_k + s) * D + c;
-      if constexpr (F32) {
-        x += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
-      } else {
-        const f16x4 y = *reinterpret_cast<const f16x4*>(static_cast<const _Float16*>(a.part_out) + at);
-        const float w = a.part_scale[row * a.top_k + s];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += w * (float)y[e];
-      }
-    }
-  const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
-  const int64_t to = b * a.q_stride_b + (row - bh * a.s_q) * a.q_stride_s + (bh - b * a.n_q_heads) * a.q_stride_h + c;
-  if (a.dq_f32) {
-    f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.dq) + to);
-    if (a.dq_accumulate) x += *dst;
-    *dst = x;
-  } else {
-    *reinterpret_cast<bf16x4*>(static_cast<bf16_t*>(a.dq) + to) = __builtin_convertvector(x, bf16x4);
-  }
-}
-
 // ------------------------------------------------------------------------------------ dk / dv
 // Items that follow each other on one XCD: the parts of a block's keys share the rows of the list, and the parts of its list its keys.  (Runs of 1
 // and 4 come within 1 % on blocks of 256, 512 and 1024 keys; with long ones the XCDs have unequal work.)
@@ -534,15 +501,49 @@ __global__ __launch_bounds__(512) void block_dkdv_wide_kernel(const BlockArgs a)
   item.flush(a, plane, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, st.dk, st.dv, wave_u * 32, fresh(tid) & 63);
 }
 
-// dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.  Bound by the bytes (31 us
-// behind the kernel above).
+// ------------------------------------------------------------------------------------ reduce
+// dq (+)= the partial dq of the slots that have one, in slot order; D / 4 lanes a row.
+template <int D, bool F32>
+SP_DEV void reduce_dq(const BlockArgs& a, int plane, int64_t gid) {
+  constexpr int NC = D / 4;
+  const int64_t rows = (int64_t)a.group * a.s_q, rh = gid / NC, row = plane * rows + rh;      // (plane = batch index * kv heads + kv head)
+  const int c = (int)(gid - rh * NC) * 4;
+  if (rh >= rows) return;
+  const float* lp = a.part_lse + row * a.top_k;
+  f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = 0; s < a.top_k; ++s)
+    if (lp[s] != -INFINITY) {
+      const int64_t at = (row * a.top_k + s) * D + c;
+      if constexpr (F32) {
+        x += *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
+      } else {
+        const f16x4 y = *reinterpret_cast<const f16x4*>(static_cast<const _Float16*>(a.part_out) + at);
+        const float w = a.part_scale[row * a.top_k + s];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += w * (float)y[e];
+      }
+    }
+  const int64_t bh = row / a.s_q, b = bh / a.n_q_heads;
+  const int64_t to = b * a.q_stride_b + (row - bh * a.s_q) * a.q_stride_s + (bh - b * a.n_q_heads) * a.q_stride_h + c;
+  if (a.dq_f32) {
+    f32x4* dst = reinterpret_cast<f32x4*>(static_cast<float*>(a.dq) + to);
+    if (a.dq_accumulate) x += *dst;
+    *dst = x;
+  } else {
+    *reinterpret_cast<bf16x4*>(static_cast<bf16_t*>(a.dq) + to) = __builtin_convertvector(x, bf16x4);
+  }
+}
+
+// dk, dv of the keys whose workgroups left partial sums (in list order) and of those that nobody chose; D / 4 lanes a key.
 // (From a multiple of four keys on: the keys of a wave then lie in one chunk, whose length is a multiple of 256, as kv_chunk_of has it.)
 SP_HOST_DEV int64_t dkdv_reduce_first(const BlockArgs& a) { return a.kv_begin & ~(int64_t)3; }
 template <int D>
-__global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs a, int keys_pad) {
+SP_DEV void reduce_dkdv(const BlockArgs& a, int plane, int64_t gid) {
   constexpr int NC = D / 4;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, kk = gid / NC;
-  const int c = (int)(gid - kk * NC) * 4, plane = blockIdx.y, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  const int keys_pad = a.n_sub * a.dkdv_keys;
+  const int64_t kk = gid / NC;
+  const int c = (int)(gid - kk * NC) * 4, b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
   const int64_t key = dkdv_reduce_first(a) + kk;
   if (key < a.kv_begin || key >= a.kv_end_range) return;
   const int64_t block = key / a.block_len, j = block - a.first_block;
@@ -569,18 +570,18 @@ __global__ __launch_bounds__(256) void block_dkdv_reduce_kernel(const BlockArgs 
   *vd = v4;
 }
 
+// Both in one launch: dq_wgs workgroups for the rows of the plane (blockIdx.y), the others for its keys.  Bound by the bytes: 65536 rows of 8 slots of
+// 128, 65536 keys with 2 to 3 parts each 70 us (two launches took 67, and 5 us more where there is little to add up).
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void block_reduce_kernel(const BlockArgs a, int dq_wgs) {
+  if ((int)blockIdx.x < dq_wgs) reduce_dq<D, F32>(a, blockIdx.y, (int64_t)blockIdx.x * 256 + threadIdx.x);
+  else reduce_dkdv<D>(a, blockIdx.y, (int64_t)((int)blockIdx.x - dq_wgs) * 256 + threadIdx.x);
+}
+
 hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st) {
   dim3 grid((unsigned)a.item_cap, (unsigned)(a.batch * a.n_kv_heads)), block(256);
   if (head_dim == 128) hipLaunchKernelGGL(block_dq_kernel<128>, grid, block, block_dq_lds_bytes<128>(), st, a);
   else hipLaunchKernelGGL(block_dq_kernel<64>, grid, block, block_dq_lds_bytes<64>(), st, a);
-  return hipGetLastError();
-}
-hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
-  const int64_t lanes = (int64_t)a.batch * a.n_q_heads * a.s_q * (head_dim / 4);
-  dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, st, a); };
-  if (head_dim == 128) a.part_f32 ? go(block_dq_reduce_kernel<128, true>) : go(block_dq_reduce_kernel<128, false>);
-  else a.part_f32 ? go(block_dq_reduce_kernel<64, true>) : go(block_dq_reduce_kernel<64, false>);
   return hipGetLastError();
 }
 template <int D, int NW>
@@ -594,13 +595,14 @@ hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t s
   else a.dkdv_keys == 128 ? launch_dkdv_t<64, 4>(a, st) : launch_dkdv_t<64, 2>(a, st);
   return hipGetLastError();
 }
-hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
-  const int64_t lanes = (a.kv_end_range - dkdv_reduce_first(a)) * (head_dim / 4);
-  if (lanes <= 0) return hipSuccess;
-  dim3 grid((unsigned)((lanes + 255) / 256), (unsigned)(a.batch * a.n_kv_heads)), block(256);
-  const int keys_pad = a.n_sub * a.dkdv_keys;
-  if (head_dim == 128) hipLaunchKernelGGL(block_dkdv_reduce_kernel<128>, grid, block, 0, st, a, keys_pad);
-  else hipLaunchKernelGGL(block_dkdv_reduce_kernel<64>, grid, block, 0, st, a, keys_pad);
+hipError_t launch_block_reduce(const BlockArgs& a, int head_dim, hipStream_t st) {
+  const int64_t per = head_dim / 4, keys = a.kv_end_range - dkdv_reduce_first(a);
+  const int64_t dq_wgs = ((int64_t)a.group * a.s_q * per + 255) / 256, dkdv_wgs = (keys * per + 255) / 256;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(dq_wgs + dkdv_wgs), (unsigned)(a.batch * a.n_kv_heads)), dim3(256), 0, st, a, (int)dq_wgs);
+  };
+  if (head_dim == 128) a.part_f32 ? go(block_reduce_kernel<128, true>) : go(block_reduce_kernel<128, false>);
+  else a.part_f32 ? go(block_reduce_kernel<64, true>) : go(block_reduce_kernel<64, false>);
   return hipGetLastError();
 }
 

@@ -719,8 +719,35 @@ __global__ __launch_bounds__(kListThreads) void block_rank_kernel(const BlockArg
   }
 }
 
-__global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int dkdv) {
+// delta = -sum_d dO O and lse2 = lse log2(e) (+inf: no key) of the rows of a plane, as the dense backward has them; D / 8 lanes a row.
+template <int D>
+SP_DEV void block_delta(const BlockArgs& a, int plane, int64_t gid) {
+  constexpr int NC = D / 8;
+  const int64_t rows = (int64_t)a.group * a.s_q, rh = gid / NC;
+  const int c = (int)(gid - rh * NC), b = plane / a.n_kv_heads, hk = plane - b * a.n_kv_heads;
+  if (rh >= rows) return;                            // (whole rows: the lanes of one leave together)
+  const int hl = (int)(rh / a.s_q), h = hk * a.group + hl, r = (int)(rh - (int64_t)hl * a.s_q);
+  const bf16x8 o = *reinterpret_cast<const bf16x8*>(static_cast<const bf16_t*>(a.out) + (int64_t)b * a.o_stride_b + (int64_t)r * a.o_stride_s + (int64_t)h * a.o_stride_h + c * 8);
+  const bf16x8 g = *reinterpret_cast<const bf16x8*>(a.d_out + (int64_t)b * a.do_stride_b + (int64_t)r * a.do_stride_s + (int64_t)h * a.do_stride_h + c * 8);
+  float acc = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc += (float)o[e] * (float)g[e];
+#pragma unroll
+  for (int w = NC / 2; w >= 1; w >>= 1) acc += __shfl_xor(acc, w, 64);
+  if (c != 0) return;
+  const int64_t at = plane * rows + rh;
+  const float l = a.lse[at];
+  a.delta[at] = -acc;
+  a.lse2[at] = l == -INFINITY ? INFINITY : l * kLog2e;
+}
+// A slot a thread.  D > 0: behind fill_wgs workgroups those that make delta and lse2, which wait for nothing (a launch of their own was 5 to 10 us).
+template <int D>
+__global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int fill_wgs) {
+  constexpr bool dkdv = D > 0;
   const int plane = blockIdx.y, rows = a.group * a.s_q;
+  if constexpr (D > 0) {
+    if ((int)blockIdx.x >= fill_wgs) return block_delta<D>(a, plane, (int64_t)((int)blockIdx.x - fill_wgs) * 256 + threadIdx.x);
+  }
   const int64_t n_slots = (int64_t)rows * a.top_k, i = (int64_t)blockIdx.x * 256 + threadIdx.x, at = plane * n_slots + i;
   if (i >= n_slots) return;
   const int j = a.index[at] - a.first_block;
@@ -858,12 +885,15 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
 }
 
 static size_t list_lds_bytes(const BlockArgs& a) { return ((size_t)list_lds_words(a.n_blocks) + (size_t)kListRows * a.top_k) * 4; }
-hipError_t launch_block_lists(const BlockArgs& a, bool dkdv, hipStream_t st) {
+hipError_t launch_block_lists(const BlockArgs& a, int head_dim, bool is_bwd, hipStream_t st) {
   const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
-  const int64_t slots = (int64_t)a.group * a.s_q * a.top_k;
+  const int64_t rows = (int64_t)a.group * a.s_q, fill = (rows * a.top_k + 255) / 256, delta = is_bwd ? (rows * (head_dim / 8) + 255) / 256 : 0;
   hipLaunchKernelGGL(block_rank_kernel, dim3((unsigned)a.n_list_chunks, planes), dim3(kListThreads), list_lds_bytes(a), st, a);
-  hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, dkdv ? 1 : 0);
-  hipLaunchKernelGGL(block_fill_kernel, dim3((unsigned)((slots + 255) / 256), planes), dim3(256), 0, st, a, dkdv ? 1 : 0);
+  hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, is_bwd ? 1 : 0);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(fill + delta), planes), dim3(256), 0, st, a, (int)fill); };
+  if (!is_bwd) go(block_fill_kernel<0>);
+  else if (head_dim == 128) go(block_fill_kernel<128>);
+  else go(block_fill_kernel<64>);
   return hipGetLastError();
 }
 

@@ -63,8 +63,8 @@ struct BlockArgs {
   int32_t out_f32;
   // backward
   const __bf16* d_out;
-  const float* delta;            // negated, and lse in log2 units, as the dense backward's
-  const float* lse2;
+  float* delta;                  // negated, and lse in log2 units, as the dense backward's
+  float* lse2;
   float* inf;                    // a cell that holds +infinity: the lse2 of rows past a list's end
   void* dq;
   int32_t dq_f32, dq_accumulate, dkv_accumulate;
@@ -111,14 +111,13 @@ struct BlockSelectArgs {
 
 hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_select(const BlockSelectArgs& a, int head_dim, int compute_units, hipStream_t st);
-// lists and tiles of the call's index; with `dkdv` the dk/dv items too
-hipError_t launch_block_lists(const BlockArgs& a, bool dkdv, hipStream_t st);
+// lists and tiles of the call's index; for a backward (is_bwd) the dk/dv items too, and delta and lse2 of out, d_out and lse
+hipError_t launch_block_lists(const BlockArgs& a, int head_dim, bool is_bwd, hipStream_t st);
 hipError_t launch_block_fwd(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_fwd_few(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_bwd_dq(const BlockArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_block_bwd_dkdv(const BlockArgs& a, int head_dim, hipStream_t st);
-hipError_t launch_block_dq_reduce(const BlockArgs& a, int head_dim, hipStream_t st);
-hipError_t launch_block_dkdv_reduce(const BlockArgs& a, int head_dim, hipStream_t st);
+hipError_t launch_block_reduce(const BlockArgs& a, int head_dim, hipStream_t st);      // dq, dk, dv from what the two above left
 hipError_t opt_in_block_select_kernels();
 hipError_t opt_in_block_fwd_kernels();
 hipError_t opt_in_block_bwd_kernels();
