@@ -647,8 +647,8 @@ static hipError_t opt_in_select_d() {
 }
 
 // ------------------------------------------------------------------------------------ lists
-// The rows of every block, in ascending order of (head of the group, row).  Three launches: places of the rows of a chunk within the
-// chunk, starts, entries.  Bound by a few trips to memory each: 8192 rows of 8 heads, 8 slots, 128 blocks: 7.5, 6.5 and 8 us.
+// The rows of every block, in ascending order of (head of the group, row).  Three launches (one where rows are few): places of the rows of a chunk
+// within the chunk, starts, entries.  Bound by a few trips to memory each: 8192 rows of 8 heads, 8 slots, 128 blocks: 7.5, 6.5 and 8 us.
 //
 // Chunks of kListRows rows have a bit per (block, row) in LDS: setting bits commutes, and a row's place among the chunk's rows of a block
 // is a count of the bits below its own, so the lists are the same on every run.  (The index rows of a plane follow each other, and so do the
@@ -740,6 +740,25 @@ SP_DEV void block_delta(const BlockArgs& a, int plane, int64_t gid) {
   a.delta[at] = -acc;
   a.lse2[at] = l == -INFINITY ? INFINITY : l * kLog2e;
 }
+// Row rh of a plane at place `pos` of block j's list: its entry, and with the first row of a tile or of a dk/dv part that too.  n_full: dk/dv items of
+// full length of the plane.
+template <bool DKDV>
+SP_DEV void put_entry(const BlockArgs& a, int plane, int j, int rh, int slot, const BlockList& list, uint32_t pos, uint32_t n_full) {
+  const int hl = rh / a.s_q;
+  const uint32_t to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
+  a.entries[(int64_t)plane * a.item_cap * kBlockTileRows + to] = {r, (uint32_t)(hl << 6 | slot), r * (uint32_t)(a.q_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.q_stride_h / 8),
+                                                                   r * (uint32_t)(a.do_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.do_stride_h / 8)};
+  const uint32_t left = list.len - pos, block = (uint32_t)(a.first_block + j);
+  if (pos % kBlockTileRows == 0)
+    a.items[(int64_t)plane * a.item_cap + list.tile0 + pos / kBlockTileRows] = {(int)block, (int)to, (int)(left < kBlockTileRows ? left : kBlockTileRows), 0};
+  if (DKDV && pos % (uint32_t)a.chunk_rows == 0) {
+    const uint32_t c = pos / (uint32_t)a.chunk_rows;
+    const uint32_t first = left >= (uint32_t)a.chunk_rows ? list.item0 + c * (uint32_t)a.n_sub : n_full + list.rest0;
+    BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + first;
+    for (int s = 0; s < a.n_sub; ++s)
+      it[s] = {(int)block * a.n_sub + s, (int)to, (int)(left < (uint32_t)a.chunk_rows ? left : (uint32_t)a.chunk_rows), list.parts ? (int)(list.part0 + c) : -1};
+  }
+}
 // A slot a thread.  D > 0: behind fill_wgs workgroups those that make delta and lse2, which wait for nothing (a launch of their own was 5 to 10 us).
 template <int D>
 __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int fill_wgs) {
@@ -753,22 +772,9 @@ __global__ __launch_bounds__(256) void block_fill_kernel(const BlockArgs a, int 
   const int j = a.index[at] - a.first_block;
   const uint32_t rank = a.ranks[at];                 // (read beside what says whether the slot counts, not behind it)
   if (a.part_lse[at] != 0.f) return;
-  const int rh = (int)(i / a.top_k), slot = (int)(i - (int64_t)rh * a.top_k), hl = rh / a.s_q;
-  const BlockList list = a.lists[(int64_t)plane * a.n_blocks + j];
-  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * count_stride(a.n_list_chunks) + rh / kListRows] + rank, to = list.tile0 * kBlockTileRows + pos, r = (uint32_t)(rh - hl * a.s_q);
-  a.entries[(int64_t)plane * a.item_cap * kBlockTileRows + to] = {r, (uint32_t)(hl << 6 | slot), r * (uint32_t)(a.q_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.q_stride_h / 8),
-                                                                   r * (uint32_t)(a.do_stride_s / 8) + (uint32_t)hl * (uint32_t)(a.do_stride_h / 8)};
-  // the first row of a tile writes the tile down
-  const uint32_t left = list.len - pos, block = (uint32_t)(a.first_block + j);
-  if (pos % kBlockTileRows == 0)
-    a.items[(int64_t)plane * a.item_cap + list.tile0 + pos / kBlockTileRows] = {(int)block, (int)to, (int)(left < kBlockTileRows ? left : kBlockTileRows), 0};
-  if (dkdv && pos % (uint32_t)a.chunk_rows == 0) {
-    const uint32_t c = pos / (uint32_t)a.chunk_rows;
-    const uint32_t first = left >= (uint32_t)a.chunk_rows ? list.item0 + c * (uint32_t)a.n_sub : (uint32_t)a.n_dkdv_items[2 * plane + 1] + list.rest0;
-    BlockItem* it = a.dkdv_items + (int64_t)plane * a.dkdv_cap + first;
-    for (int s = 0; s < a.n_sub; ++s)
-      it[s] = {(int)block * a.n_sub + s, (int)to, (int)(left < (uint32_t)a.chunk_rows ? left : (uint32_t)a.chunk_rows), list.parts ? (int)(list.part0 + c) : -1};
-  }
+  const int rh = (int)(i / a.top_k);
+  const uint32_t pos = a.counts[((int64_t)plane * a.n_blocks + j) * count_stride(a.n_list_chunks) + rh / kListRows] + rank;
+  put_entry<dkdv>(a, plane, j, rh, (int)(i - (int64_t)rh * a.top_k), a.lists[(int64_t)plane * a.n_blocks + j], pos, dkdv ? (uint32_t)a.n_dkdv_items[2 * plane + 1] : 0u);
 }
 
 // One workgroup a plane: counts of the chunks -> where each chunk's rows start in the block's list, list starts, tiles.
@@ -800,6 +806,17 @@ SP_DEV void scan_add(uint32_t (*tmp)[4], int tid, uint32_t (&v)[4], uint32_t (&t
     total[i] = (uint32_t)__builtin_amdgcn_readlane((int)upto, 15);
     v[i] = x[i] - v[i] + (wave > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, wave - 1) : 0u);
   }
+}
+// Bin of a short dk/dv item of 0 < rest < chunk_rows rows, the longest first.
+SP_DEV uint32_t bin_of(const BlockArgs& a, uint32_t rest) { return 63u - (uint32_t)(((uint64_t)rest * 64 - 1) / (uint32_t)a.chunk_rows); }
+// The list of length `len` of every thread's block, behind those of the threads before it and `before` (short dk/dv items, tiles, dk/dv items of full
+// length, partial sums); total: what all threads have of these.  bin_s: where the next short item of a bin goes.
+SP_DEV BlockList place_list(const BlockArgs& a, bool dkdv, int tid, uint32_t len, const uint32_t (&before)[4], uint32_t (&total)[4], uint32_t (*tmp)[4], uint32_t* bin_s) {
+  const uint32_t full = dkdv ? len / (uint32_t)a.chunk_rows : 0u, rest = dkdv && len > full * (uint32_t)a.chunk_rows ? 1u : 0u, parts = full + rest > 1 ? full + rest : 0u;
+  uint32_t v[4] = {rest * (uint32_t)a.n_sub, (len + kBlockTileRows - 1) / kBlockTileRows, full * (uint32_t)a.n_sub, parts};
+  scan_add(tmp, tid, v, total);
+  const uint32_t rest0 = rest ? atomicAdd(&bin_s[bin_of(a, len - full * (uint32_t)a.chunk_rows)], 1u) * (uint32_t)a.n_sub : 0u;
+  return {len, before[1] + v[1], before[2] + v[2], rest0, parts, before[3] + v[3]};
 }
 __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
   constexpr int kLens = 8192;                                    // lengths that pass through LDS (more: through memory)
@@ -850,13 +867,12 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   // The short dk/dv items in descending order of length, to a 64th of the full one: the last ones to start are the shortest, and runs dealt out to
   // the XCDs in turn give all of them as much.  (Which of two of one bin goes first is left open: it changes no sum.)
   auto length_of = [&](int j) { return in_lds ? len_s[j] : lists[j].len; };
-  auto bin_of = [&](uint32_t rest) { return 63u - (uint32_t)(((uint64_t)rest * 64 - 1) / (uint32_t)a.chunk_rows); };      // 0 < rest < chunk_rows
   if (dkdv) {
     if (tid < 64) bin_s[tid] = 0u;
     lds_barrier();
     for (int j = tid; j < nb; j += kScanThreads) {
       const uint32_t rest = length_of(j) % (uint32_t)a.chunk_rows;
-      if (rest) atomicAdd(&bin_s[bin_of(rest)], 1u);
+      if (rest) atomicAdd(&bin_s[bin_of(a, rest)], 1u);
     }
     lds_barrier();
     if (tid < 64) {
@@ -868,12 +884,9 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   uint32_t before[4] = {0, 0, 0, 0};                             // short dk/dv items, tiles, dk/dv items of full length, partial sums of the blocks before
   for (int j0 = 0; j0 < nb; j0 += kScanThreads) {
     const int j = j0 + tid;
-    const uint32_t len = j < nb ? length_of(j) : 0u, full = dkdv ? len / (uint32_t)a.chunk_rows : 0u;
-    const uint32_t rest = dkdv && len > full * (uint32_t)a.chunk_rows ? 1u : 0u, parts = full + rest > 1 ? full + rest : 0u;
-    uint32_t v[4] = {rest * (uint32_t)a.n_sub, (len + kBlockTileRows - 1) / kBlockTileRows, full * (uint32_t)a.n_sub, parts}, total[4];
-    scan_add(tmp, tid, v, total);
-    const uint32_t rest0 = rest ? atomicAdd(&bin_s[bin_of(len - full * (uint32_t)a.chunk_rows)], 1u) * (uint32_t)a.n_sub : 0u;
-    if (j < nb) lists[j] = {len, before[1] + v[1], before[2] + v[2], rest0, parts, before[3] + v[3]};
+    uint32_t total[4];
+    const BlockList list = place_list(a, dkdv != 0, tid, j < nb ? length_of(j) : 0u, before, total, tmp, bin_s);
+    if (j < nb) lists[j] = list;
 #pragma unroll
     for (int i = 0; i < 4; ++i) before[i] += total[i];
   }
@@ -884,10 +897,112 @@ __global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArg
   }
 }
 
+// The three in one workgroup a plane, with what passes between them in LDS: for planes of so few rows that launches cost more than it does.  Calls of
+// 8 heads on one, us with it and with three launches, forward and backward: 64 rows, 8 of 63 blocks of 64 24 and 30, 51 and 56; 64 rows, 16 of 234 blocks
+// of 256 34 and 40, 93 and 97; 200 rows, 2 of 128 blocks of 64 20 and 26, 43 and 48; 128 rows, 8 of 64 blocks of 64 32 and 34, 57 both; 256 rows, 4 of 59 blocks of 512 35 both, 88 and 84; 250 rows, 8 of 126
+// blocks of 128 39 and 33, 78 and 66.
+// D > 0 as in block_fill_kernel, behind the first workgroup of a plane.
+constexpr int kOneListSlots = 8, kOneListRows = 2048;      // slots a thread; rows of a plane
+constexpr int64_t kOneListWork = 1 << 23;                   // rows times slots: a thread's slots, and the words of a block's bits behind each other
+SP_HOST_DEV int one_list_stride(int rows) { return ((rows + 31) / 32) | 1; }
+SP_HOST_DEV size_t one_list_lds_bytes(int rows, int n_blocks) { return (size_t)n_blocks * ((size_t)one_list_stride(rows) * 6 + sizeof(BlockList)) + 16; }
+constexpr size_t kOneListLds = 128 * 1024;
+template <int D>
+__global__ __launch_bounds__(kScanThreads) void block_lists_kernel(const BlockArgs a) {
+  constexpr bool dkdv = D > 0;
+  const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.y, rows = a.group * a.s_q, nb = a.n_blocks;
+  if constexpr (D > 0) {
+    if (blockIdx.x > 0) return block_delta<D>(a, plane, (int64_t)((int)blockIdx.x - 1) * kScanThreads + tid);
+  }
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ uint32_t tmp[kScanThreads / 64][4], bin_s[64], disorder[kScanThreads / 64];
+  const int stride = one_list_stride(rows), words = (rows + 31) / 32, n_slots = rows * a.top_k;
+  BlockList* const list_s = reinterpret_cast<BlockList*>(smem);
+  uint32_t* const bits = reinterpret_cast<uint32_t*>(list_s + nb);
+  uint16_t* const below = reinterpret_cast<uint16_t*>(bits + nb * stride);
+  const int32_t* const index = a.index + (int64_t)plane * n_slots;
+  float* const valid = a.part_lse + (int64_t)plane * n_slots;
+  const float per_row = 1.0f / (float)a.top_k;
+  auto row_of = [&](int i) { return (int)(((float)i + 0.5f) * per_row); };      // (as in block_rank_kernel)
+  static_assert(kOneListSlots * kScanThreads <= 1 << 14, "exact quotients");
+  int j[kOneListSlots];                              // blocks of this thread's slots, from the range's first on; -1: none
+  bool unordered = false;
+#pragma unroll
+  for (int u = 0; u < kOneListSlots; ++u) {
+    const int i = tid + u * kScanThreads;
+    j[u] = -1;
+    if (i >= n_slots) continue;
+    const int x = index[i], before = index[i > 0 ? i - 1 : 0];
+    unordered |= x >= a.first_block && i != row_of(i) * a.top_k && (before < a.first_block || before >= x);
+    j[u] = x < a.first_block || x - a.first_block >= nb ? -1 : x - a.first_block;
+  }
+  for (int i = tid; i < nb * stride; i += kScanThreads) bits[i] = 0u;
+  if (tid < 64) bin_s[tid] = 0u;
+  const uint64_t some = __builtin_amdgcn_ballot_w64(unordered);
+  if (lane == 0) disorder[tid >> 6] = some != 0;
+  lds_barrier();
+  uint32_t repeats = 0;
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 64; ++w) repeats |= disorder[w];
+#pragma unroll
+  for (int u = 0; u < kOneListSlots; ++u) {
+    const int i = tid + u * kScanThreads, row = row_of(i);
+    if (i >= n_slots) continue;
+    if (j[u] >= 0 && !block_slot_valid(a, index + row * a.top_k, i - row * a.top_k, a.q_offset + row % a.s_q, repeats != 0)) j[u] = -1;
+    valid[i] = j[u] >= 0 ? 0.f : -INFINITY;
+    if (j[u] >= 0) atomicOr(&bits[j[u] * stride + (row >> 5)], 1u << (row & 31));
+  }
+  lds_barrier();
+  uint32_t len = 0;                                  // of block tid
+  if (tid < nb)
+    for (int w = 0; w < words; ++w) {
+      below[tid * stride + w] = (uint16_t)len;
+      len += __popc(bits[tid * stride + w]);
+    }
+  if (dkdv) {
+    const uint32_t rest = len % (uint32_t)a.chunk_rows;
+    if (rest) atomicAdd(&bin_s[bin_of(a, rest)], 1u);
+    lds_barrier();
+    if (tid < 64) {
+      const uint32_t n = bin_s[tid];
+      bin_s[tid] = wave_scan(n) - n;
+    }
+    lds_barrier();
+  }
+  uint32_t total[4];
+  const uint32_t before[4] = {0, 0, 0, 0};
+  const BlockList list = place_list(a, dkdv, tid, len, before, total, tmp, bin_s);
+  if (tid < nb) {
+    list_s[tid] = list;
+    a.lists[(int64_t)plane * nb + tid] = list;
+  }
+  if (tid == 0) {
+    a.n_items[plane] = (int)total[1];
+    if (dkdv && plane == 0) *a.inf = INFINITY;
+    if (dkdv) { a.n_dkdv_items[2 * plane] = (int)(total[2] + total[0]); a.n_dkdv_items[2 * plane + 1] = (int)total[2]; }
+  }
+  lds_barrier();
+#pragma unroll
+  for (int u = 0; u < kOneListSlots; ++u) {
+    const int i = tid + u * kScanThreads, row = row_of(i);
+    if (j[u] < 0) continue;
+    const int at = j[u] * stride + (row >> 5);
+    put_entry<dkdv>(a, plane, j[u], row, i - row * a.top_k, list_s[j[u]], below[at] + __popc(bits[at] & ((1u << (row & 31)) - 1u)), total[2]);
+  }
+}
+
 static size_t list_lds_bytes(const BlockArgs& a) { return ((size_t)list_lds_words(a.n_blocks) + (size_t)kListRows * a.top_k) * 4; }
 hipError_t launch_block_lists(const BlockArgs& a, int head_dim, bool is_bwd, hipStream_t st) {
   const unsigned planes = (unsigned)(a.batch * a.n_kv_heads);
   const int64_t rows = (int64_t)a.group * a.s_q, fill = (rows * a.top_k + 255) / 256, delta = is_bwd ? (rows * (head_dim / 8) + 255) / 256 : 0;
+  if (rows <= kOneListRows && rows * a.top_k <= kOneListSlots * kScanThreads && rows * rows * a.top_k <= kOneListWork && a.n_blocks <= kScanThreads && one_list_lds_bytes((int)rows, a.n_blocks) <= kOneListLds) {
+    const size_t lds = one_list_lds_bytes((int)rows, a.n_blocks);
+    const dim3 grid((unsigned)(1 + (delta * 256 + kScanThreads - 1) / kScanThreads), planes), block(kScanThreads);
+    if (!is_bwd) hipLaunchKernelGGL(block_lists_kernel<0>, grid, block, lds, st, a);
+    else if (head_dim == 128) hipLaunchKernelGGL(block_lists_kernel<128>, grid, block, lds, st, a);
+    else hipLaunchKernelGGL(block_lists_kernel<64>, grid, block, lds, st, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(block_rank_kernel, dim3((unsigned)a.n_list_chunks, planes), dim3(kListThreads), list_lds_bytes(a), st, a);
   hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, is_bwd ? 1 : 0);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(fill + delta), planes), dim3(256), 0, st, a, (int)fill); };
@@ -900,6 +1015,10 @@ hipError_t launch_block_lists(const BlockArgs& a, int head_dim, bool is_bwd, hip
 hipError_t opt_in_block_select_kernels() {
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_rank_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      (list_lds_words(kListBlocks) + kListRows * kMaxTopK) * 4);
+  const auto lists = [](const void* kernel) { return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kOneListLds); };
+  if (e == hipSuccess) e = lists(reinterpret_cast<const void*>(&block_lists_kernel<0>));
+  if (e == hipSuccess) e = lists(reinterpret_cast<const void*>(&block_lists_kernel<64>));
+  if (e == hipSuccess) e = lists(reinterpret_cast<const void*>(&block_lists_kernel<128>));
   if (e == hipSuccess) e = opt_in_select_d<128>();
   return e == hipSuccess ? opt_in_select_d<64>() : e;
 }
