@@ -53,10 +53,14 @@ int64_t blocks_of(int64_t begin, int64_t end, int64_t block_len) { return end > 
 
 int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->batch * p->n_q_heads * p->s_q; }
 
-// Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot): up to 8 of these a compute unit.  8 heads, 16 slots, us with
-// a workgroup each and with lists: 4 rows on blocks of 256 (512 slots) 18 and 38, 16 rows (2048) 38 and 55, 32 rows (4096) 65 and 62; 16 rows on
-// blocks of 64 at head_dim 64 (2048) 42 and 41.
-bool few_rows(const slimpipe_attn_params* p, int32_t top_k) { return rows_of(p) * top_k <= 8 * (int64_t)compute_units(); }
+// Rows so few that lists and 128-row tiles cost more than a workgroup for each (row, slot), which reads its block for itself: up to 8 of these a
+// compute unit, and 2^25 elements of keys in all.  8 heads on one, us with a workgroup each and with lists: 16 slots of blocks of 64 at head_dim 128,
+// 16 rows (2048 of them) 18 and 20; 8 slots of 128, 32 rows (2048, 2^25 elements) 20 and 21; 16 slots of 256, 16 rows (2048, 2^26) 27 and 21; 4 slots of 512, 32
+// rows (1024, 2^26) 25 both.
+bool few_rows(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k) {
+  const int64_t slots = rows_of(p) * top_k;
+  return slots <= 8 * (int64_t)compute_units() && slots * block_len * p->head_dim <= 1 << 25;
+}
 
 // Items of a table, and workgroups of its launch: whole rounds of runs (xcd_item), one at least.
 int32_t whole_rounds(size_t n) { return (int32_t)((n + 8 * kXcdRun - 1) / (8 * kXcdRun) * (8 * kXcdRun)) + (n == 0 ? 8 * kXcdRun : 0); }
@@ -226,7 +230,7 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
   rc = check_blocks(p, 1, p->kv_capacity > 0 ? p->kv_capacity : 1, block_len);
   if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k, is_bwd);
   if (rc != SLIMPIPE_OK) return rc;
-  *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, top_k), is_bwd != 0).bytes;
+  *bytes = layout(p, block_len, top_k, is_bwd || !few_rows(p, block_len, top_k), is_bwd != 0).bytes;
   return SLIMPIPE_OK;
 }
 
@@ -240,7 +244,7 @@ int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, 
   if (rc == SLIMPIPE_OK) rc = check_top_k(p, top_k, 0);
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
-  const bool few = few_rows(p, top_k);
+  const bool few = few_rows(p, block_len, top_k);
   const BlockWorkspace w = layout(p, block_len, top_k, !few, false);
   if (!workspace || workspace_bytes < w.bytes) return SLIMPIPE_EWORKSPACE;
   if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
