@@ -648,7 +648,8 @@ static hipError_t opt_in_select_d() {
 
 // ------------------------------------------------------------------------------------ lists
 // The rows of every block, in ascending order of (head of the group, row).  Three launches (one where rows are few): places of the rows of a chunk
-// within the chunk, starts, entries.  Bound by a few trips to memory each: 8192 rows of 8 heads, 8 slots, 128 blocks: 7.5, 6.5 and 8 us.
+// within the chunk, starts, entries.  Bound by a few trips to memory each: 8192 rows of 8 heads, 8 slots, 128 blocks: 7, 6 and 7 us
+// (15 with delta).
 //
 // Chunks of kListRows rows have a bit per (block, row) in LDS: setting bits commutes, and a row's place among the chunk's rows of a block
 // is a count of the bits below its own, so the lists are the same on every run.  (The index rows of a plane follow each other, and so do the
