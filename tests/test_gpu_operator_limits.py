@@ -113,15 +113,17 @@ def test_selection_of_degenerate_scores(sp, s, D):
 
 
 def test_lists_of_many_blocks(sp):
-    """More blocks than one window of the lists (1024) and than the lengths that pass through LDS (8192): forward and backward."""
+    """As many blocks as fit the lists of one launch, more than one window of the lists (1024) and than the lengths that pass through LDS (8192): forward and
+    backward."""
     import torch
     B, s, Hq, Hkv, D, L, top_k = 1, 150, 2, 1, 64, 64, 8
-    for blocks in (1500, 8300):
+    for blocks in (900, 1500, 8300):
         N = blocks * L - 17
         off = N - s
         say("many blocks %d" % blocks)
         rng = np.random.default_rng(blocks)
         used = np.unique(np.concatenate([[0, 1023, 1024, blocks - 1, blocks - 2, blocks - 3], rng.integers(0, blocks, 6)]))
+        used = used[used < blocks]
         index = np.full((B, Hq, s, top_k), -1, dtype=np.int32)
         for at in np.ndindex(B, Hq, s):
             index[at] = rng.permutation(used)[:top_k]
@@ -430,3 +432,65 @@ def test_values_of_any_magnitude(sp, power):
     got, rest = host_f64(out), np.arange(D) != 40
     assert np.isinf(got[..., 40]).all()
     bu.check("the other columns", got[..., rest], r.out[..., rest], r.out_tol[..., rest])
+
+
+@pytest.mark.parametrize("s,L,D", [(60, 64, 64), (700, 64, 64), (700, 256, 128)])
+def test_gradients_over_out_and_lse(sp, s, L, D):
+    """dq in place of out and dv over lse: both are read before any gradient is written."""
+    import torch
+    Hq, Hkv, top_k, off = 4, 1, 4, 900
+    N = off + s
+    q, _ = rows((1, s, Hq, D), "q")
+    do, _ = rows((1, s, Hq, D), "do")
+    k, _ = rows((1, N, Hkv, D), "k")
+    v, _ = rows((1, N, Hkv, D), "v")
+    index = torch.from_numpy(np.random.default_rng(s).integers(0, -(-N // L), (1, Hq, s, top_k), dtype=np.int32)).cuda()
+    out, lse = sp.slimpipe_attn_block_fwd(q, k, v, index, off, 0, N, L)
+    dk, dv = torch.zeros((2,) + k.shape, device="cuda")
+    dq = sp.slimpipe_attn_block_bwd(q, k, v, index, out, do, lse, off, 0, N, L, dk, dv)
+    dv2 = torch.zeros_like(dv)
+    lse2 = dv2.view(-1)[:lse.numel()].view(lse.shape)
+    lse2.copy_(lse)
+    dk2, out2 = torch.zeros_like(dk), out.clone()
+    sp.slimpipe_attn_block_bwd(q, k, v, index, out2, do, lse2, off, 0, N, L, dk2, dv2, dq=out2, dkv_accumulate=False)
+    assert torch.equal(out2, dq) and torch.equal(dk2, dk) and torch.equal(dv2, dv)
+
+
+def test_calls_from_two_threads(sp):
+    """Two host threads, a stream and a workspace each: the results of each call on its own."""
+    import threading
+    import torch
+    s, off, Hq, Hkv, D, L, top_k = 300, 700, 8, 2, 128, 64, 5
+    N = off + s
+    sets = []
+    for i in range(2):
+        t = [rows((1, n, h, D), tag, 70 + i)[0] for tag, n, h in (("q", s, Hq), ("k", N, Hkv), ("v", N, Hkv), ("do", s, Hq))]
+        cache = sp.KvCache4.empty(1, N, Hkv, D)
+        sp.slimpipe_attn_kv4_store(t[1], t[2], cache, 0)
+        sets.append(t + [cache])
+
+    def work(q, k, v, do, cache):
+        means = sp.slimpipe_attn_block_means(k, 0, N, L)
+        index = sp.slimpipe_attn_block_select(q, means, off, 0, N, L, top_k)
+        out, lse = sp.slimpipe_attn_block_fwd(q, k, v, index, off, 0, N, L)
+        dk, dv = torch.zeros((2,) + k.shape, device="cuda")
+        dq = sp.slimpipe_attn_block_bwd(q, k, v, index, out, do, lse, off, 0, N, L, dk, dv)
+        return index, out, lse, dq, dk, dv, *sp.slimpipe_attn_fwd_kv4(q, cache, off, 0, N)
+    want = [work(*t) for t in sets]
+    torch.cuda.synchronize()
+    bad = []
+
+    def run(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = work(*sets[i])
+                stream.synchronize()
+                if not all(torch.equal(x, y) for x, y in zip(got, want[i])):
+                    bad.append(i)
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
