@@ -495,15 +495,16 @@ class KvCache4(collections.namedtuple("KvCache4", "k_codes k_scales v_codes v_sc
         """(batch, capacity, kv heads, head_dim) and the three strides in elements, after a check that the four tensors agree."""
         kc, ks, vc, vs = self
         shape, codes, scales, v_codes, v_scales = kc.shape, kc.stride(), ks.stride(), vc.stride(), vs.stride()
-        ok = len(shape) == 4 and codes[3:] == scales[3:] == v_codes[3:] == v_scales[3:] == (1,) and kc.dtype == ks.dtype == vc.dtype == vs.dtype == torch.uint8
-        if ok:
+        u8 = torch.uint8
+        if codes[3:] == scales[3:] == v_codes[3:] == v_scales[3:] == (1,) and kc.dtype is ks.dtype is vc.dtype is vs.dtype is u8 and vc.shape == shape:
             B, N, H, half = shape
-            ok = vc.shape == shape and ks.shape == vs.shape == (B, N, H, half // 16)
-        # (a dimension of one element may have any stride)
-        if not ok or not all(n == 1 or a == b == 16 * c == 16 * d for n, a, b, c, d in zip(shape[:3], codes, v_codes, scales, v_scales)):
-            raise SlimpipeError("codes and scales must be uint8 [batch, keys, heads, head_dim / 2] and [.., head_dim / 32] of the same layout")
-        D = 2 * half
-        return (B, N, H, D), (2 * codes[0] if B > 1 else N * H * D, 2 * codes[1] if N > 1 else H * D, 2 * codes[2] if H > 1 else D)
+            b, n, h = codes[:3]
+            # (a dimension of one element may have any stride)
+            if (ks.shape == vs.shape == (B, N, H, half // 16) and (B == 1 or b == v_codes[0] == 16 * scales[0] == 16 * v_scales[0])
+                    and (N == 1 or n == v_codes[1] == 16 * scales[1] == 16 * v_scales[1]) and (H == 1 or h == v_codes[2] == 16 * scales[2] == 16 * v_scales[2])):
+                D = 2 * half
+                return (B, N, H, D), (2 * b if B > 1 else N * H * D, 2 * n if N > 1 else H * D, 2 * h if H > 1 else D)
+        raise SlimpipeError("codes and scales must be uint8 [batch, keys, heads, head_dim / 2] and [.., head_dim / 32] of the same layout")
 
 
 def _cache_ptrs(cache):
@@ -524,9 +525,11 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     """-> (k, v) bf16 [B, kv_end - kv_begin, Hkv, D]: the numbers that the rows of a KvCache4 stand for."""
     (B, N, H, D), skv = cache.layout()
     shape = (B, kv_end - kv_begin, H, D)
-    if k_rows is None:
-        k_rows = torch.empty(shape, device=cache.k_codes.device, dtype=torch.bfloat16)
-    if v_rows is None:
+    if k_rows is None and v_rows is None:
+        k_rows, v_rows = torch.empty((2,) + shape, device=cache.k_codes.device, dtype=torch.bfloat16).unbind(0)
+    elif k_rows is None:
+        k_rows = torch.empty_like(v_rows)
+    elif v_rows is None:
         v_rows = torch.empty_like(k_rows)
     if tuple(k_rows.shape) != shape or not _same_strides(k_rows, v_rows):
         raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")

@@ -269,28 +269,25 @@ SP_DEV void settle_row(uint32_t* list, int count, int places, int need, const bf
       at += __popcll(mask);
     }
   } else {
-    // the next one each time: the largest score behind the one before (lower, or equal with a higher index)
-    double last = INFINITY;
-    int last_j = 0x7fffffff, mine = 0x7fffffff;      // (the first: everything is behind +inf but +inf itself, which any index is behind)
-    bool first = true;
-    for (int n = 0; n < need; ++n) {
-      double best = -INFINITY;
-      int best_j = 0x7fffffff;
-      for (int j = first_block + lane; j < own; j += 64) {
-        const double s = exact_score<D>(means + (int64_t)j * D, q);
-        if ((first || s < last || (s == last && j > last_j)) && (best_j == 0x7fffffff || s > best)) { best = s; best_j = j; }
+    // Every score once, 64 blocks at a time; lane n keeps the n-th of the `need` best so far (of equal ones the first stays ahead, so that equal
+    // scores throughout cost no more than the first ones of them).
+    double kept = -INFINITY, border = -INFINITY;     // border: of the last one
+    int mine = 0x7fffffff, have = 0;
+    for (int j0 = first_block; j0 < own; j0 += 64) {
+      const int j = j0 + lane;
+      const double s = j < own ? exact_score<D>(means + (int64_t)j * D, q) : -INFINITY;
+      for (uint64_t m = __builtin_amdgcn_ballot_w64(j < own && (have < need || s > border)); m; m &= m - 1) {
+        const int from = __ffsll((unsigned long long)m) - 1;
+        const double x = __shfl(s, from, 64);
+        if (have == need && !(x > border)) continue;
+        const int pos = __popcll(__builtin_amdgcn_ballot_w64(lane < have && kept >= x));
+        const double up = __shfl_up(kept, 1, 64);
+        const int up_j = __shfl_up(mine, 1, 64);
+        kept = lane > pos ? up : lane == pos ? x : kept;
+        mine = lane > pos ? up_j : lane == pos ? j0 + from : mine;
+        have = have < need ? have + 1 : need;
+        border = __shfl(kept, need - 1, 64);
       }
-      const double top = wave_max(best_j == 0x7fffffff ? -INFINITY : best);
-      int lowest = best_j != 0x7fffffff && best == top ? best_j : 0x7fffffff;
-#pragma unroll
-      for (int w = 1; w < 64; w <<= 1) {
-        const int o = __shfl_xor(lowest, w, 64);
-        lowest = o < lowest ? o : lowest;
-      }
-      last = top;
-      last_j = lowest;
-      first = false;
-      if (lane == n) mine = lowest;
     }
     int at = 0;                                      // ascending: each goes behind the smaller ones
     for (int n = 0; n < need; ++n) at += __shfl(mine, n, 64) < mine ? 1 : 0;
