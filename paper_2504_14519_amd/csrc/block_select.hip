@@ -816,46 +816,63 @@ SP_DEV BlockList place_list(const BlockArgs& a, bool dkdv, int tid, uint32_t len
   const uint32_t rest0 = rest ? atomicAdd(&bin_s[bin_of(a, len - full * (uint32_t)a.chunk_rows)], 1u) * (uint32_t)a.n_sub : 0u;
   return {len, before[1] + v[1], before[2] + v[2], rest0, parts, before[3] + v[3]};
 }
-__global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv) {
-  constexpr int kLens = 8192;                                    // lengths that pass through LDS (more: through memory)
-  __shared__ uint32_t tmp[kScanThreads / 64][4], len_s[kLens], bin_s[64];
-  const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks, nc = a.n_list_chunks;
-  const bool in_lds = nb <= kLens;
-  BlockList* lists = a.lists + (int64_t)plane * nb;
-  // a wave eight blocks at a time, four chunks a lane
-  constexpr int WAVES = kScanThreads / 64, PER = 8;
-  for (int j0 = tid >> 6; j0 < nb; j0 += PER * WAVES) {
-    uint32_t before[PER] = {};
-    for (int c0 = 4 * lane; c0 - 4 * lane < nc; c0 += 256) {
-      u32x4 v[PER];
+// Counts of the chunks of eight blocks -> where each chunk's rows start in its block's list, four chunks a lane, by one wave: blocks j0,
+// j0 + step, .., whose lengths go to put_len.
+template <class Len>
+SP_DEV void chunk_starts(const BlockArgs& a, int plane, int j0, int step, int lane, Len&& put_len) {
+  constexpr int PER = 8;
+  const int nb = a.n_blocks, nc = a.n_list_chunks;
+  uint32_t before[PER] = {};
+  for (int c0 = 4 * lane; c0 - 4 * lane < nc; c0 += 256) {
+    u32x4 v[PER];
 #pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        v[p] = u32x4{0, 0, 0, 0};
-        if (j0 + p * WAVES < nb && c0 < nc) v[p] = *reinterpret_cast<const u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * WAVES) * count_stride(nc) + c0);
-      }
-#pragma unroll
-      for (int p = 0; p < PER; ++p) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) v[p][u] = c0 + u < nc ? v[p][u] : 0u;
-        const uint32_t sum = v[p][0] + v[p][1] + v[p][2] + v[p][3], upto = wave_scan(sum);
-        uint32_t at = before[p] + upto - sum;
-        u32x4 starts;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          starts[u] = at;
-          at += v[p][u];
-        }
-        if (j0 + p * WAVES < nb && c0 < nc) *reinterpret_cast<u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * WAVES) * count_stride(nc) + c0) = starts;
-        before[p] += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-      }
+    for (int p = 0; p < PER; ++p) {
+      v[p] = u32x4{0, 0, 0, 0};
+      if (j0 + p * step < nb && c0 < nc) v[p] = *reinterpret_cast<const u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * step) * count_stride(nc) + c0);
     }
 #pragma unroll
-    for (int p = 0; p < PER; ++p)
-      if (lane == 0 && j0 + p * WAVES < nb) {
-        if (in_lds) len_s[j0 + p * WAVES] = before[p];
-        else lists[j0 + p * WAVES].len = before[p];
+    for (int p = 0; p < PER; ++p) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[p][u] = c0 + u < nc ? v[p][u] : 0u;
+      const uint32_t sum = v[p][0] + v[p][1] + v[p][2] + v[p][3], upto = wave_scan(sum);
+      uint32_t at = before[p] + upto - sum;
+      u32x4 starts;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        starts[u] = at;
+        at += v[p][u];
       }
+      if (j0 + p * step < nb && c0 < nc) *reinterpret_cast<u32x4*>(a.counts + ((int64_t)plane * nb + j0 + p * step) * count_stride(nc) + c0) = starts;
+      before[p] += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
   }
+#pragma unroll
+  for (int p = 0; p < PER; ++p)
+    if (lane == 0 && j0 + p * step < nb) put_len(j0 + p * step, before[p]);
+}
+// A launch of its own for them, 128 blocks a workgroup, where they are many: 4096 rows of 8 heads, this and the next kernel and the next alone, 2048
+// blocks (2^18 counts) 10 and 40 us, 16384 blocks 39 and 333; 128 blocks of 65536 rows (2^15) 10 and 6.
+__global__ __launch_bounds__(kScanThreads) void block_starts_kernel(const BlockArgs a) {
+  constexpr int WAVES = kScanThreads / 64;
+  BlockList* const lists = a.lists + (int64_t)blockIdx.y * a.n_blocks;
+  chunk_starts(a, blockIdx.y, (int)blockIdx.x * 8 * WAVES + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), WAVES, threadIdx.x & 63,
+               [&](int j, uint32_t n) { lists[j].len = n; });
+}
+constexpr int64_t kScanCounts = 1 << 16;         // counts that the one workgroup of the next kernel goes through by itself
+// started: block_starts_kernel has run.
+__global__ __launch_bounds__(kScanThreads) void block_scan_kernel(const BlockArgs a, int dkdv, int started) {
+  constexpr int kLens = 8192;                                    // lengths that pass through LDS (more: through memory)
+  __shared__ uint32_t tmp[kScanThreads / 64][4], len_s[kLens], bin_s[64];
+  const int tid = threadIdx.x, lane = tid & 63, plane = blockIdx.x, nb = a.n_blocks;
+  const bool in_lds = nb <= kLens && !started;
+  BlockList* lists = a.lists + (int64_t)plane * nb;
+  constexpr int WAVES = kScanThreads / 64;
+  if (!started)
+    for (int j0 = __builtin_amdgcn_readfirstlane(tid >> 6); j0 < nb; j0 += 8 * WAVES)
+      chunk_starts(a, plane, j0, WAVES, lane, [&](int j, uint32_t n) {
+        if (in_lds) len_s[j] = n;
+        else lists[j].len = n;
+      });
   if (in_lds) {
     lds_barrier();
   } else {
@@ -1002,7 +1019,9 @@ hipError_t launch_block_lists(const BlockArgs& a, int head_dim, bool is_bwd, hip
     return hipGetLastError();
   }
   hipLaunchKernelGGL(block_rank_kernel, dim3((unsigned)a.n_list_chunks, planes), dim3(kListThreads), list_lds_bytes(a), st, a);
-  hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, is_bwd ? 1 : 0);
+  const bool starts = (int64_t)a.n_blocks * a.n_list_chunks > kScanCounts;
+  if (starts) hipLaunchKernelGGL(block_starts_kernel, dim3((unsigned)((a.n_blocks + kScanThreads / 8 - 1) / (kScanThreads / 8)), planes), dim3(kScanThreads), 0, st, a);
+  hipLaunchKernelGGL(block_scan_kernel, dim3(planes), dim3(kScanThreads), 0, st, a, is_bwd ? 1 : 0, starts ? 1 : 0);
   auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(fill + delta), planes), dim3(256), 0, st, a, (int)fill); };
   if (!is_bwd) go(block_fill_kernel<0>);
   else if (head_dim == 128) go(block_fill_kernel<128>);

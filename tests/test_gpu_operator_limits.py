@@ -116,8 +116,8 @@ def test_lists_of_many_blocks(sp):
     """As many blocks as fit the lists of one launch, more than one window of the lists (1024) and than the lengths that pass through LDS (8192): forward and
     backward."""
     import torch
-    B, s, Hq, Hkv, D, L, top_k = 1, 150, 2, 1, 64, 64, 8
-    for blocks in (900, 1500, 8300):
+    B, Hkv, D, L, top_k = 1, 1, 64, 64, 8
+    for blocks, s, Hq in ((900, 150, 2), (1500, 150, 2), (8300, 150, 2), (4200, 1024, 4)):      # (the last: with a launch for the chunks' starts)
         N = blocks * L - 17
         off = N - s
         say("many blocks %d" % blocks)
