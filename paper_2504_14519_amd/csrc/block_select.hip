@@ -851,7 +851,7 @@ SP_DEV void chunk_starts(const BlockArgs& a, int plane, int j0, int step, int la
     if (lane == 0 && j0 + p * step < nb) put_len(j0 + p * step, before[p]);
 }
 // A launch of its own for them, 128 blocks a workgroup, where they are many: 4096 rows of 8 heads, this and the next kernel and the next alone, 2048
-// blocks (2^18 counts) 10 and 40 us, 16384 blocks 39 and 333; 128 blocks of 65536 rows (2^15) 10 and 6.
+// blocks (2^18 counts) 10 and 40 us, 16384 blocks 39 and 333; the launch costs 4 to 6, and with 2^15 counts the next alone takes 6.
 __global__ __launch_bounds__(kScanThreads) void block_starts_kernel(const BlockArgs a) {
   constexpr int WAVES = kScanThreads / 64;
   BlockList* const lists = a.lists + (int64_t)blockIdx.y * a.n_blocks;
