@@ -456,7 +456,10 @@ __global__ __launch_bounds__(256, 2) void block_select_kernel(const BlockSelectA
 // Few rows (tokens): 32 a workgroup, whose eight waves share out the tiles; means go from memory through registers to the matrix unit.  The waves'
 // lists meet in LDS, and so do the second walk's masks, a bit a block.  8 heads of each of 4 sequences on 511 blocks of means of 128, top_k 16: 21 us, of
 // which the two tiles of scores of a wave take 8 (vector work of one compute unit), the joins 6.
-constexpr int kFewWaves = 8, kFewTiles = 512, kFewKept = 2;      // tiles of a wave whose scores stay in registers for the second walk
+constexpr int kFewWaves = 8, kFewTiles = 512;
+// Tiles of a wave whose scores stay in registers for the second walk: two, or six where there are more and lists leave the registers (8 rows on 2048
+// blocks, top_k 16: two 67 us, six 52; 2048 rows of 8 heads on 256 blocks, two tiles a wave: two 34 us, six 39).
+constexpr int few_kept(int k, bool many) { return many && k <= 32 ? 6 : 2; }
 template <int K>
 constexpr int few_list_stride() { return K * 32 + 8; }              // floats of a wave's lists (eight banks on, so that a row's lists are spread)
 template <int D, int K>
@@ -464,7 +467,7 @@ constexpr size_t select_few_lds_bytes(int tiles) {
   const size_t lists = (size_t)kFewWaves * few_list_stride<K>() * 4, masks = (size_t)tiles * 32 * 2 * 4 + 32 * select_places(K) * 4;
   return lists > masks ? lists : masks;
 }
-template <int D, int K>
+template <int D, int K, int KEPT>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(const BlockSelectArgs a) {
   constexpr int KS = D / 16, PLACES = select_places(K);
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -515,13 +518,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
 #pragma unroll
     for (int i = 0; i < 16; ++i) keep_largest<K>(top, 8 * (i >> 2) + (i & 3) < left ? s[i] : -INFINITY);
   };
-  f32x16 kept[kFewKept] = {};
+  f32x16 kept[KEPT] = {};
 #pragma unroll
-  for (int i = 0; i < kFewKept; ++i) {
+  for (int i = 0; i < KEPT; ++i) {
     const int t = wave + i * kFewWaves;
     if (t < nt) { kept[i] = scores(t); offer(kept[i], t); }
   }
-  for (int t = wave + kFewKept * kFewWaves; t < nt; t += kFewWaves) offer(scores(t), t);
+  for (int t = wave + KEPT * kFewWaves; t < nt; t += kFewWaves) offer(scores(t), t);
   {
     const float norm = row_norm<KS>(q);
     if (tid < 32) norm_s[tid] = norm;
@@ -561,9 +564,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void block_select_few_kernel(con
     if (g == 0) { open_s[t * 32 + ql] = open; certain_s[t * 32 + ql] = certain; }
   };
 #pragma unroll
-  for (int i = 0; i < kFewKept; ++i)
+  for (int i = 0; i < KEPT; ++i)
     if (wave + i * kFewWaves < nt) mark(kept[i], wave + i * kFewWaves);
-  for (int t = wave + kFewKept * kFewWaves; t < nt; t += kFewWaves) mark(scores(t), t);
+  for (int t = wave + KEPT * kFewWaves; t < nt; t += kFewWaves) mark(scores(t), t);
   __syncthreads();
   uint32_t* const cand = certain_s + nt * 32;
   {
@@ -604,8 +607,11 @@ template <int D, int K>
 static hipError_t launch_select_t(const BlockSelectArgs& a, bool few, hipStream_t st) {
   const int64_t rows = a.group * (int64_t)a.s_q;
   const unsigned heads = (unsigned)a.n_kv_heads, batch = (unsigned)a.batch;
-  if (few) hipLaunchKernelGGL((block_select_few_kernel<D, K>), dim3((unsigned)((rows + 31) / 32), heads, batch), dim3(kFewWaves * 64),
-                              (select_few_lds_bytes<D, K>((a.n_blocks + 31) / 32)), st, a);
+  const int tiles = (a.n_blocks + 31) / 32;
+  auto go_few = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 31) / 32), heads, batch), dim3(kFewWaves * 64), (select_few_lds_bytes<D, K>(tiles)), st, a);
+  };
+  if (few) tiles > 2 * kFewWaves ? go_few(block_select_few_kernel<D, K, few_kept(K, true)>) : go_few(block_select_few_kernel<D, K, few_kept(K, false)>);
   else hipLaunchKernelGGL((block_select_kernel<D, K>), dim3((unsigned)((rows + 128 * select_sets(K) - 1) / (128 * select_sets(K))), heads, batch),
                           dim3(256), (select_lds_bytes<D, K>()), st, a);
   return hipGetLastError();
@@ -632,7 +638,9 @@ static hipError_t opt_in_select() {
   const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
   hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_kernel<D, K>), attr, (int)select_lds_bytes<D, K>());
   if (e == hipSuccess)
-    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_few_kernel<D, K>), attr, (int)select_few_lds_bytes<D, K>(kFewTiles));
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_few_kernel<D, K, few_kept(K, false)>), attr, (int)select_few_lds_bytes<D, K>(kFewTiles));
+  if (e == hipSuccess)
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&block_select_few_kernel<D, K, few_kept(K, true)>), attr, (int)select_few_lds_bytes<D, K>(kFewTiles));
   return e;
 }
 template <int D>

@@ -79,6 +79,8 @@ def test_forward(sp, case, wild):
     (1, 90, 500, 4, 1, 128, 64, 3, True, (128, 530)),
     (1, 20, 100, 2, 1, 64, 64, 3, True, (64, 64)),
     (1, 5, 40000, 4, 1, 64, 64, 64, True, None),        # more blocks than one chunk of the selection
+    (1, 3, 60000, 4, 1, 128, 64, 24, True, None),       # scores of more tiles a wave than two, all of them kept
+    (1, 2, 140000, 8, 1, 64, 64, 8, True, None),        # and more than are kept
 ])
 def test_means_and_selection(sp, case):
     import torch
