@@ -5,8 +5,8 @@
 //   dQ_i = scale sum_j dS_ij k_j      dK_j  = scale sum_i dS_ij q_i
 // As in the dense backward dq and dk/dv have kernels of their own, both over the lists of block_select.hip:
 //   dq     tiles of 128 rows of one block, as in the forward; each (row, slot) leaves a partial dq that a last kernel adds in slot order
-//   dk/dv  a workgroup owns 256 keys (128 or 64 in small blocks) and walks the rows that chose their block, 32 at a time; long lists are
-//          cut into parts whose sums a last kernel adds in list order.
+//   dk/dv  a workgroup owns 256 keys (128 or 64 at head_dim 64 and in small blocks) and walks the rows that chose their block, 32 at a time; long
+//          lists are cut into parts whose sums the last kernel adds in list order.
 // No sum depends on the order in which workgroups run.
 #include "block_tile.hpp"
 #include "dkdv_tile.hpp"
