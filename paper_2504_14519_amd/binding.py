@@ -373,6 +373,22 @@ def _kv_like(chunks):
     return chunks[0] if len(chunks) == 1 else _ChunkedKV(chunks)
 
 
+# The library takes element widths from its entry points and dtype codes: a tensor of another dtype would be read or written as what it is
+# not, a narrower one past its end.
+_TORCH_DTYPE = {BF16: torch.bfloat16, F32: torch.float32}
+
+
+def _check_dtype(dtype, names, *tensors):
+    for x in tensors:
+        if x.dtype is not dtype:
+            raise SlimpipeError("%s must be %s (not %s)" % (names, dtype, x.dtype))
+
+
+def _check_result_dtype(code, name, flag, x):
+    if x.dtype is not _TORCH_DTYPE.get(code):
+        raise SlimpipeError("%s is %s: %s must name that dtype" % (name, x.dtype, flag))
+
+
 def _check_index(index, q_slice):
     B, s, Hq, _ = q_slice.shape
     if index.dtype != torch.int32 or index.dim() != 4 or index.shape[:3] != (B, Hq, s) or not index.is_contiguous():
@@ -389,6 +405,7 @@ def slimpipe_attn_block_means(k_chunks, kv_begin, kv_end, block_len, means=None)
     """-> means [B, Hkv, ceil(keys / block_len), D] fp32: those of the blocks that hold a key of [kv_begin, kv_end) are written (kv_begin a
     multiple of block_len), the others left as they are (zero where the call allocates).  k_chunks: one tensor or a list of chunks."""
     chunks = _as_chunks(k_chunks)
+    _check_dtype(torch.bfloat16, "keys", *chunks)
     k = _kv_like(chunks)
     B, N, Hkv, D = k.shape
     blocks = -(-N // block_len) if block_len > 0 else 0
@@ -409,6 +426,7 @@ def _contiguous_strides(shape):
 
 def slimpipe_attn_block_select(q_slice, means, q_offset, kv_begin, kv_end, block_len, top_k, causal=True, index=None):
     """-> index [B, Hq, s, top_k] int32: the blocks of every query row, ascending, filled up with -1."""
+    _check_dtype(torch.bfloat16, "q_slice", q_slice)
     B, s, Hq, D = q_slice.shape
     Hkv, blocks = means.shape[1], means.shape[2]
     _check_means(means, B, Hkv, blocks, D)
@@ -444,8 +462,11 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
     top_k = _check_index(index, q_slice)
     if len(k_chunks) != len(v_chunks) or not _same_strides(v_chunks[0], k_chunks[0]):
         raise SlimpipeError("v must have as many chunks as k, of the same shape and strides")
+    _check_dtype(torch.bfloat16, "q, k and v", q_slice, *k_chunks, *v_chunks)
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
+    _check_result_dtype(out_dtype, "out", "out_dtype", out)
+    _check_dtype(torch.float32, "lse", lse)
     p = _params(q_slice, _kv_like(k_chunks), out, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, False), device=q_slice.device, dtype=torch.uint8)
@@ -471,6 +492,9 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
             raise SlimpipeError("v, dk and dv must have the strides of k")
     if not len(k_chunks) == len(v_chunks) == len(dk_chunks) == len(dv_chunks):
         raise SlimpipeError("k, v, dk and dv must have the same number of chunks")
+    _check_dtype(torch.bfloat16, "q, k, v, out and d_out", q_slice, out, d_out, *k_chunks, *v_chunks)
+    _check_dtype(torch.float32, "lse, dk and dv", lse, *dk_chunks, *dv_chunks)
+    _check_result_dtype(dq_dtype, "dq", "dq_dtype", dq)
     p = _params(q_slice, _kv_like(k_chunks), out, d_out, q_offset, kv_begin, kv_end, causal, scale, BF16)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, True), device=q_slice.device, dtype=torch.uint8)
@@ -516,6 +540,7 @@ def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
     (B, N, H, D), skv = cache.layout()
     if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or not _same_strides(k_slice, v_slice):
         raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
+    _check_dtype(torch.bfloat16, "k_slice and v_slice", k_slice, v_slice)
     sx = k_slice.stride()[:3]
     p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
     _check(lib.slimpipe_attn_kv4_store(ctypes.byref(p), k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()), "slimpipe_attn_kv4_store")
@@ -533,6 +558,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
         v_rows = torch.empty_like(k_rows)
     if tuple(k_rows.shape) != shape or not _same_strides(k_rows, v_rows):
         raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
+    _check_dtype(torch.bfloat16, "k_rows and v_rows", k_rows, v_rows)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
     p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
     _check(lib.slimpipe_attn_kv4_load(ctypes.byref(p), *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
@@ -562,8 +588,11 @@ def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end
 
 def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
     """-> (out, lse): slimpipe_attn_fwd over a KvCache4.  workspace: uint8 tensor, allocated where None."""
+    _check_dtype(torch.bfloat16, "q_slice", q_slice)
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
+    _check_result_dtype(out_dtype, "out", "out_dtype", out)
+    _check_dtype(torch.float32, "lse", lse)
     p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
