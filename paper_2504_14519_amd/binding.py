@@ -389,6 +389,31 @@ def _check_result_dtype(code, name, flag, x):
         raise SlimpipeError("%s is %s: %s must name that dtype" % (name, x.dtype, flag))
 
 
+# Extents come from q_slice, the keys and the key range alone: what else a call is given has to have them, or is read and written past its end.
+def _check_rows(name, x, shape):
+    if x.shape != shape or len(shape) != 4 or x.stride(3) != 1:
+        raise SlimpipeError("%s must be [batch, rows, heads, head_dim] of the call's sizes, head_dim contiguous" % name)
+
+
+def _check_keys(q_slice, chunks):
+    """The chunks among themselves: _chunk_table."""
+    if not chunks or chunks[0].dim() != 4 or chunks[0].stride(3) != 1:
+        raise SlimpipeError("keys must be [batch, keys, kv heads, head_dim], head_dim contiguous, or a list of such chunks")
+    if q_slice is not None and (chunks[0].shape[0] != q_slice.shape[0] or chunks[0].shape[3] != q_slice.shape[3]):
+        raise SlimpipeError("q_slice and the keys must have the same batch and head_dim")
+
+
+def _check_lse(lse, q_slice):
+    B, s, Hq, _ = q_slice.shape
+    if lse.shape != (B, Hq, s) or not lse.is_contiguous():
+        raise SlimpipeError("lse must be a contiguous tensor [batch, query heads, rows]")
+
+
+def _check_workspace(workspace):
+    if not workspace.is_contiguous():
+        raise SlimpipeError("a workspace must be contiguous")
+
+
 def _check_index(index, q_slice):
     B, s, Hq, _ = q_slice.shape
     if index.dtype != torch.int32 or index.dim() != 4 or index.shape[:3] != (B, Hq, s) or not index.is_contiguous():
@@ -406,6 +431,7 @@ def slimpipe_attn_block_means(k_chunks, kv_begin, kv_end, block_len, means=None)
     multiple of block_len), the others left as they are (zero where the call allocates).  k_chunks: one tensor or a list of chunks."""
     chunks = _as_chunks(k_chunks)
     _check_dtype(torch.bfloat16, "keys", *chunks)
+    _check_keys(None, chunks)
     k = _kv_like(chunks)
     B, N, Hkv, D = k.shape
     blocks = -(-N // block_len) if block_len > 0 else 0
@@ -427,6 +453,9 @@ def _contiguous_strides(shape):
 def slimpipe_attn_block_select(q_slice, means, q_offset, kv_begin, kv_end, block_len, top_k, causal=True, index=None):
     """-> index [B, Hq, s, top_k] int32: the blocks of every query row, ascending, filled up with -1."""
     _check_dtype(torch.bfloat16, "q_slice", q_slice)
+    _check_rows("q_slice", q_slice, q_slice.shape)
+    if means.dim() != 4:
+        raise SlimpipeError("means must have four dimensions")
     B, s, Hq, D = q_slice.shape
     Hkv, blocks = means.shape[1], means.shape[2]
     _check_means(means, B, Hkv, blocks, D)
@@ -450,7 +479,10 @@ def _block_ws(p, block_len, top_k, is_bwd):
 
 def slimpipe_attn_block_workspace_bytes(q_slice, k_chunks, index, q_offset, kv_begin, kv_end, block_len, causal=True, is_bwd=False):
     """Bytes of workspace that slimpipe_attn_block_fwd (or _bwd) of these tensors needs."""
-    p = _params(q_slice, _kv_like(_as_chunks(k_chunks)), q_slice, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)
+    k_chunks = _as_chunks(k_chunks)
+    _check_rows("q_slice", q_slice, q_slice.shape)
+    _check_keys(q_slice, k_chunks)
+    p = _params(q_slice, _kv_like(k_chunks), q_slice, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)
     return _block_ws(p, block_len, _check_index(index, q_slice), is_bwd)
 
 
@@ -459,6 +491,8 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
     """-> (out, lse): slimpipe_attn_fwd restricted to the keys of the blocks that `index` names for each row.  k_chunks / v_chunks: one
     tensor each or lists of chunks.  workspace: uint8 tensor, allocated where None."""
     k_chunks, v_chunks = _as_chunks(k_chunks), _as_chunks(v_chunks)
+    _check_rows("q_slice", q_slice, q_slice.shape)
+    _check_keys(q_slice, k_chunks)
     top_k = _check_index(index, q_slice)
     if len(k_chunks) != len(v_chunks) or not _same_strides(v_chunks[0], k_chunks[0]):
         raise SlimpipeError("v must have as many chunks as k, of the same shape and strides")
@@ -467,9 +501,12 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     _check_result_dtype(out_dtype, "out", "out_dtype", out)
     _check_dtype(torch.float32, "lse", lse)
+    _check_rows("out", out, q_slice.shape)
+    _check_lse(lse, q_slice)
     p = _params(q_slice, _kv_like(k_chunks), out, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, False), device=q_slice.device, dtype=torch.uint8)
+    _check_workspace(workspace)
     _check(lib.slimpipe_attn_block_fwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
                                        k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                        *_ws(workspace), _stream()), "slimpipe_attn_block_fwd")
@@ -481,6 +518,8 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
     """-> dq: the gradients of slimpipe_attn_block_fwd with the same index.  dk_chunks / dv_chunks (fp32, one tensor each or lists, shaped like
     the keys) get rows [kv_begin, kv_end) written or incremented."""
     k_chunks, v_chunks, dk_chunks, dv_chunks = (list(_as_chunks(x)) for x in (k_chunks, v_chunks, dk_chunks, dv_chunks))
+    _check_rows("q_slice", q_slice, q_slice.shape)
+    _check_keys(q_slice, k_chunks)
     top_k = _check_index(index, q_slice)
     if dq is None:
         # (the strides of q also where those leave gaps: a slice of a sequence, a part of packed rows)
@@ -495,9 +534,13 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
     _check_dtype(torch.bfloat16, "q, k, v, out and d_out", q_slice, out, d_out, *k_chunks, *v_chunks)
     _check_dtype(torch.float32, "lse, dk and dv", lse, *dk_chunks, *dv_chunks)
     _check_result_dtype(dq_dtype, "dq", "dq_dtype", dq)
+    _check_rows("out", out, q_slice.shape)
+    _check_rows("d_out", d_out, q_slice.shape)
+    _check_lse(lse, q_slice)
     p = _params(q_slice, _kv_like(k_chunks), out, d_out, q_offset, kv_begin, kv_end, causal, scale, BF16)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, True), device=q_slice.device, dtype=torch.uint8)
+    _check_workspace(workspace)
     _check(lib.slimpipe_attn_block_bwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
                                        k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), d_out.data_ptr(), lse.data_ptr(),
                                        dq.data_ptr(), dq_dtype, 1 if dq_accumulate else 0, _chunk_table(dk_chunks), _chunk_table(dv_chunks),
@@ -538,7 +581,7 @@ def _cache_ptrs(cache):
 def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
     """Store bf16 rows k_slice, v_slice [B, s, Hkv, D] in a KvCache4 from `position` on."""
     (B, N, H, D), skv = cache.layout()
-    if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or not _same_strides(k_slice, v_slice):
+    if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or k_slice.stride(3) != 1 or not _same_strides(k_slice, v_slice):
         raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
     _check_dtype(torch.bfloat16, "k_slice and v_slice", k_slice, v_slice)
     sx = k_slice.stride()[:3]
@@ -549,6 +592,8 @@ def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
 def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     """-> (k, v) bf16 [B, kv_end - kv_begin, Hkv, D]: the numbers that the rows of a KvCache4 stand for."""
     (B, N, H, D), skv = cache.layout()
+    if kv_end < kv_begin:
+        raise SlimpipeError("kv_end lies before kv_begin")
     shape = (B, kv_end - kv_begin, H, D)
     if k_rows is None and v_rows is None:
         k_rows, v_rows = torch.empty((2,) + shape, device=cache.k_codes.device, dtype=torch.bfloat16).unbind(0)
@@ -556,7 +601,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
         k_rows = torch.empty_like(v_rows)
     elif v_rows is None:
         v_rows = torch.empty_like(k_rows)
-    if tuple(k_rows.shape) != shape or not _same_strides(k_rows, v_rows):
+    if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
         raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
     _check_dtype(torch.bfloat16, "k_rows and v_rows", k_rows, v_rows)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
@@ -568,6 +613,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
 
 def _kv4_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
     (B, N, H, D), skv = cache.layout()
+    _check_rows("q_slice", q_slice, q_slice.shape)
     if q_slice.shape[0] != B or q_slice.shape[3] != D:
         raise SlimpipeError("q_slice and the cache must have the same batch and head_dim")
     sq, so = q_slice.stride(), out_like.stride()
@@ -589,13 +635,17 @@ def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end
 def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
     """-> (out, lse): slimpipe_attn_fwd over a KvCache4.  workspace: uint8 tensor, allocated where None."""
     _check_dtype(torch.bfloat16, "q_slice", q_slice)
+    _check_rows("q_slice", q_slice, q_slice.shape)
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     _check_result_dtype(out_dtype, "out", "out_dtype", out)
     _check_dtype(torch.float32, "lse", lse)
+    _check_rows("out", out, q_slice.shape)
+    _check_lse(lse, q_slice)
     p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
+    _check_workspace(workspace)
     _check(lib.slimpipe_attn_fwd_kv4(ctypes.byref(p), q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(), *_ws(workspace),
                                      _stream()), "slimpipe_attn_fwd_kv4")
     return out, lse

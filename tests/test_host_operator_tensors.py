@@ -104,3 +104,92 @@ def test_a_result_has_the_dtype_that_the_call_names(sp, call, name):
     refuses(sp, call, dtype=sp.F32, **{name: t(*shape)})                # float32 stores would run past its end
     refuses(sp, call, dtype=sp.BF16, **{name: t(*shape, dtype=f32)})
     refuses(sp, call, dtype=sp.BF16, **{name: t(*shape, dtype=torch.float16)})
+
+
+# A right tensor's place may be taken by one of these: another batch, fewer rows, other heads, another head_dim, one dimension less, elements that
+# do not follow each other.
+def misfits(x):
+    wide = torch.zeros(x.shape[:-1] + (2 * x.shape[-1],), dtype=x.dtype)
+    return [x[:1].clone(), x[:, :x.shape[1] - 1].clone(), x[:, :, :1].clone(), wide, wide[..., ::2], x[0]]
+
+
+@pytest.mark.parametrize("call,names", [("means", "means"), ("select", "q means index"), ("fwd", "q index out"), ("bwd", "q index out d_out dq"),
+                                        ("load", "k_rows v_rows"), ("fwd_kv4", "out")])
+def test_shapes(sp, call, names):
+    for name in names.split():
+        for i, x in enumerate(misfits(right(sp)[name])):
+            # (an index of more slots, and means of fewer heads or blocks, are those of another call)
+            if not (name == "index" and call != "select" and i == 3) and not (name == "means" and call == "select" and i in (1, 2)):
+                refuses(sp, call, **{name: x})
+
+
+@pytest.mark.parametrize("call,names", [("fwd", "k v"), ("bwd", "k v dk dv")])
+def test_shapes_of_keys(sp, call, names):
+    for name in names.split():
+        for x in misfits(right(sp)[name]):
+            refuses(sp, call, **{name: x})
+    for x in misfits(right(sp)["k"])[:1] + misfits(right(sp)["k"])[3:]:      # all of them alike, and none fits q
+        refuses(sp, call, k=x, v=x, dk=x.float(), dv=x.float())
+
+
+@pytest.mark.parametrize("call", ["means", "fwd", "bwd"])
+def test_chunk_lists(sp, call):
+    a = right(sp)
+    change = {n: [a[n], a[n]] for n in ("k", "v", "dk", "dv")}
+    change["means"] = t(B, H, 2 * N // L, D, dtype=f32)
+    accepts(sp, call, **change)
+    for name in {"means": "k", "fwd": "k v", "bwd": "k v dk dv"}[call].split():
+        for x in misfits(a[name]):
+            refuses(sp, call, **{**change, name: [a[name], x]})
+        refuses(sp, call, **{**change, name: []})
+    refuses(sp, call, **{**change, "k": [], "v": [], "dk": [], "dv": []})
+
+
+@pytest.mark.parametrize("call", ["means", "select", "fwd_kv4"])
+def test_shapes_without_a_partner(sp, call):
+    """What has nothing of its own size beside it: elements that do not follow each other, dimensions that are missing."""
+    name = "k" if call == "means" else "q"
+    x = right(sp)[name]
+    for wrong in (torch.zeros(x.shape[:-1] + (2 * D,), dtype=bf16)[..., ::2], x[0]):
+        refuses(sp, call, **{name: wrong})
+    refuses(sp, call, **{name: t(*x.shape[:-1], 2 * D)})
+    if call == "fwd_kv4":
+        refuses(sp, call, q=x[:1].clone(), out=x[:1].clone(), lse=t(1, HQ, S, dtype=f32))
+
+
+@pytest.mark.parametrize("call", ["fwd", "bwd", "fwd_kv4"])
+def test_lse_is_contiguous_and_has_the_rows(sp, call):
+    for x in (t(B, S, HQ, dtype=f32).transpose(1, 2), t(B, HQ, S - 1, dtype=f32), t(B, HQ - 1, S, dtype=f32), t(1, HQ, S, dtype=f32), t(B, HQ * S, dtype=f32),
+              t(B, HQ, 2 * S, dtype=f32)[..., ::2], t(B, HQ, 1, dtype=f32).expand(B, HQ, S)):
+        refuses(sp, call, lse=x)
+    accepts(sp, call, lse=t(2 * B * HQ * S, dtype=f32)[B * HQ * S:].view(B, HQ, S))      # a part of a larger one
+
+
+@pytest.mark.parametrize("call", ["store", "load"])
+def test_cache_rows(sp, call):
+    wide = torch.zeros((B, S, H, 2 * D), dtype=bf16)[..., ::2]
+    refuses(sp, call, k_rows=wide, v_rows=wide)
+    for x in misfits(right(sp)["k_rows"]):
+        if call == "load" or x.shape[1:] != (S - 1, H, D):
+            refuses(sp, call, k_rows=x, v_rows=x)
+    packed = t(B, S, 3 * H, D)
+    accepts(sp, call, k_rows=packed[:, :, :H], v_rows=packed[:, :, H:2 * H])             # heads of a packed projection
+
+
+def test_load_of_a_range_that_ends_before_it_begins(sp):
+    with pytest.raises(sp.SlimpipeError):
+        sp.slimpipe_attn_kv4_load(right(sp)["cache"], 5, 4)
+
+
+@pytest.mark.parametrize("call", ["fwd", "bwd", "fwd_kv4"])
+def test_a_workspace_is_one_piece(sp, call):
+    refuses(sp, call, ws=t(1, dtype=torch.uint8).expand(1 << 22))
+
+
+def test_workspace_queries(sp):
+    a = right(sp)
+    for x in (t(1, N, H, D), t(B, N, H, 2 * D), t(N, H, D)):
+        with pytest.raises(sp.SlimpipeError):
+            sp.slimpipe_attn_block_workspace_bytes(a["q"], x, a["index"], 0, 0, N, L)
+    with pytest.raises(sp.SlimpipeError):
+        sp.slimpipe_attn_kv4_workspace_bytes(a["q"][0], a["cache"], 0, 0, N)
