@@ -409,6 +409,25 @@ def _check_lse(lse, q_slice):
         raise SlimpipeError("lse must be a contiguous tensor [batch, query heads, rows]")
 
 
+_gpus = None
+
+
+def _current_device():
+    """Index of the current GPU; -1, the index of tensors in host memory, where there is none (a call then ends in the library's own checks)."""
+    global _gpus
+    if _gpus is None:
+        _gpus = torch.cuda.device_count()
+    return torch._C._cuda_getDevice() if _gpus else -1
+
+
+def _check_device(*tensors):
+    """The kernels run on the current device's current stream: every tensor has to be there."""
+    here = _current_device()
+    for x in tensors:
+        if x.get_device() != here:
+            raise SlimpipeError("every tensor of a call must be on the current device")
+
+
 def _check_workspace(workspace):
     if not workspace.is_contiguous():
         raise SlimpipeError("a workspace must be contiguous")
@@ -438,6 +457,7 @@ def slimpipe_attn_block_means(k_chunks, kv_begin, kv_end, block_len, means=None)
     if means is None:
         means = torch.zeros((B, Hkv, blocks, D), device=chunks[0].device, dtype=torch.float32)
     _check_means(means, B, Hkv, blocks, D)
+    _check_device(means, *chunks)
     one = torch.Size((B, 1, Hkv, D))
     p = AttnParams(B, 1, Hkv, Hkv, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *_contiguous_strides(one), *k.stride()[:3], *_contiguous_strides(one),
                    *_contiguous_strides(one))
@@ -463,6 +483,7 @@ def slimpipe_attn_block_select(q_slice, means, q_offset, kv_begin, kv_end, block
         index = torch.empty((B, Hq, s, top_k), device=q_slice.device, dtype=torch.int32)
     if _check_index(index, q_slice) != top_k:
         raise SlimpipeError("index must have top_k entries a row")
+    _check_device(q_slice, means, index)
     sq = q_slice.stride()
     p = AttnParams(B, s, Hq, Hkv, D, 1 if causal else 0, blocks * block_len, q_offset, kv_begin, kv_end, 1.0, BF16, sq[0], sq[1], sq[2],
                    Hkv * D, Hkv * D, D, sq[0], sq[1], sq[2], sq[0], sq[1], sq[2])
@@ -507,6 +528,7 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, False), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
+    _check_device(q_slice, index, out, lse, workspace, *k_chunks, *v_chunks)
     _check(lib.slimpipe_attn_block_fwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
                                        k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                        *_ws(workspace), _stream()), "slimpipe_attn_block_fwd")
@@ -541,6 +563,7 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, True), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
+    _check_device(q_slice, index, out, d_out, lse, dq, workspace, *k_chunks, *v_chunks, *dk_chunks, *dv_chunks)
     _check(lib.slimpipe_attn_block_bwd(ctypes.byref(p), q_slice.data_ptr(), _chunk_table(k_chunks), _chunk_table(v_chunks), len(k_chunks),
                                        k_chunks[0].shape[1], block_len, top_k, index.data_ptr(), out.data_ptr(), d_out.data_ptr(), lse.data_ptr(),
                                        dq.data_ptr(), dq_dtype, 1 if dq_accumulate else 0, _chunk_table(dk_chunks), _chunk_table(dv_chunks),
@@ -584,6 +607,7 @@ def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
     if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or k_slice.stride(3) != 1 or not _same_strides(k_slice, v_slice):
         raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
     _check_dtype(torch.bfloat16, "k_slice and v_slice", k_slice, v_slice)
+    _check_device(k_slice, v_slice, *cache)
     sx = k_slice.stride()[:3]
     p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
     _check(lib.slimpipe_attn_kv4_store(ctypes.byref(p), k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()), "slimpipe_attn_kv4_store")
@@ -604,6 +628,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
         raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
     _check_dtype(torch.bfloat16, "k_rows and v_rows", k_rows, v_rows)
+    _check_device(k_rows, v_rows, *cache)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
     p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
     _check(lib.slimpipe_attn_kv4_load(ctypes.byref(p), *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
@@ -646,6 +671,7 @@ def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
+    _check_device(q_slice, out, lse, workspace, *cache)
     _check(lib.slimpipe_attn_fwd_kv4(ctypes.byref(p), q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(), *_ws(workspace),
                                      _stream()), "slimpipe_attn_fwd_kv4")
     return out, lse

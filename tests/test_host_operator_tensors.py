@@ -193,3 +193,17 @@ def test_workspace_queries(sp):
             sp.slimpipe_attn_block_workspace_bytes(a["q"], x, a["index"], 0, 0, N, L)
     with pytest.raises(sp.SlimpipeError):
         sp.slimpipe_attn_kv4_workspace_bytes(a["q"][0], a["cache"], 0, 0, N)
+
+
+@pytest.mark.parametrize("call", list(CALLS))
+def test_tensors_of_another_device(sp, monkeypatch, call):
+    """Every tensor has to be on the current device, whose stream the kernels run on; here that is said to be a GPU, and the tensors are not there."""
+    import paper_2504_14519_amd.binding as binding
+    monkeypatch.setattr(binding, "_current_device", lambda: 0, raising=False)
+    refuses(sp, call)
+
+
+def test_current_device_of_this_host(sp):
+    import paper_2504_14519_amd.binding as binding
+    if torch.cuda.device_count() == 0:
+        assert binding._current_device() == -1 == t(1).get_device()
