@@ -212,7 +212,8 @@ SP_DEV double exact_score(const float* mean, const bf16_t* q) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) sum += (double)(float)y[u] * (double)x[u];
   }
-  return sum == sum ? sum : -INFINITY;               // (NaN counts as the lowest)
+  // NaN comes last: it counts as -infinity, and that as the lowest finite number (no finite score comes near it: at most D 2^128 2^128)
+  return sum == sum ? __builtin_fmax(sum, -__DBL_MAX__) : -INFINITY;
 }
 SP_DEV double wave_max(double v) {
 #pragma unroll
