@@ -263,8 +263,8 @@ def slimpipe_attn_bwd_noalloc(q_slice, k_prefix, v_prefix, out, d_out, lse, q_of
 def _chunk_table(chunks):
     """list of tensors -> ctypes array of device pointers (all chunks share shape and strides)."""
     c0 = chunks[0]
-    for c in chunks:
-        if c.shape != c0.shape or not _same_strides(c, c0):
+    for c in chunks[1:]:
+        if not _same_strides(c, c0):
             raise SlimpipeError("chunks must share shape and strides")
     return (ctypes.c_void_p * len(chunks))(*[c.data_ptr() for c in chunks])
 
@@ -373,40 +373,32 @@ def _kv_like(chunks):
     return chunks[0] if len(chunks) == 1 else _ChunkedKV(chunks)
 
 
-# The library takes element widths from its entry points and dtype codes: a tensor of another dtype would be read or written as what it is
-# not, a narrower one past its end.
+# The library takes element widths from its entry points and dtype codes, and extents from q_slice, the keys and the key range alone.  A tensor
+# of another dtype would be read or written as what it is not, a narrower or smaller one past its end.  (Few questions to a tensor, each
+# asked once: these checks take 0.5 to 2 us of a call.)
 _TORCH_DTYPE = {BF16: torch.bfloat16, F32: torch.float32}
 
 
-def _check_dtype(dtype, names, *tensors):
-    for x in tensors:
-        if x.dtype is not dtype:
-            raise SlimpipeError("%s must be %s (not %s)" % (names, dtype, x.dtype))
+def _check_rows(name, x, shape, dtype=torch.bfloat16):
+    if x.dtype is not dtype or x.shape != shape or len(shape) != 4 or x.stride(3) != 1:
+        raise SlimpipeError("%s must be %s, [batch, rows, heads, head_dim] of the call's sizes, head_dim contiguous" % (name, dtype))
 
 
-def _check_result_dtype(code, name, flag, x):
-    if x.dtype is not _TORCH_DTYPE.get(code):
-        raise SlimpipeError("%s is %s: %s must name that dtype" % (name, x.dtype, flag))
+def _check_lse(lse, shape):
+    if lse.dtype is not torch.float32 or lse.shape != (shape[0], shape[2], shape[1]) or not lse.is_contiguous():
+        raise SlimpipeError("lse must be contiguous and float32, [batch, query heads, rows]")
 
 
-# Extents come from q_slice, the keys and the key range alone: what else a call is given has to have them, or is read and written past its end.
-def _check_rows(name, x, shape):
-    if x.shape != shape or len(shape) != 4 or x.stride(3) != 1:
-        raise SlimpipeError("%s must be [batch, rows, heads, head_dim] of the call's sizes, head_dim contiguous" % name)
-
-
-def _check_keys(q_slice, chunks):
-    """The chunks among themselves: _chunk_table."""
-    if not chunks or chunks[0].dim() != 4 or chunks[0].stride(3) != 1:
+def _check_keys(chunks, q_shape=None, dtype=torch.bfloat16):
+    """One tensor or a list of chunks, whose shapes and strides _chunk_table compares."""
+    for c in chunks:
+        if c.dtype is not dtype:
+            raise SlimpipeError("keys and values must be torch.bfloat16, their gradients torch.float32")
+    shape = chunks[0].shape if chunks else ()
+    if len(shape) != 4 or chunks[0].stride(3) != 1:
         raise SlimpipeError("keys must be [batch, keys, kv heads, head_dim], head_dim contiguous, or a list of such chunks")
-    if q_slice is not None and (chunks[0].shape[0] != q_slice.shape[0] or chunks[0].shape[3] != q_slice.shape[3]):
+    if q_shape is not None and (shape[0] != q_shape[0] or shape[3] != q_shape[3]):
         raise SlimpipeError("q_slice and the keys must have the same batch and head_dim")
-
-
-def _check_lse(lse, q_slice):
-    B, s, Hq, _ = q_slice.shape
-    if lse.shape != (B, Hq, s) or not lse.is_contiguous():
-        raise SlimpipeError("lse must be a contiguous tensor [batch, query heads, rows]")
 
 
 _gpus = None
@@ -433,11 +425,12 @@ def _check_workspace(workspace):
         raise SlimpipeError("a workspace must be contiguous")
 
 
-def _check_index(index, q_slice):
-    B, s, Hq, _ = q_slice.shape
-    if index.dtype != torch.int32 or index.dim() != 4 or index.shape[:3] != (B, Hq, s) or not index.is_contiguous():
+def _check_index(index, q_shape):
+    shape = index.shape
+    if (index.dtype is not torch.int32 or len(shape) != 4 or shape[0] != q_shape[0] or shape[1] != q_shape[2] or shape[2] != q_shape[1]
+            or not index.is_contiguous()):
         raise SlimpipeError("index must be a contiguous int32 tensor [batch, query heads, rows, top_k]")
-    return index.shape[3]
+    return shape[3]
 
 
 def _check_means(means, batch, kv_heads, blocks, head_dim):
@@ -449,8 +442,7 @@ def slimpipe_attn_block_means(k_chunks, kv_begin, kv_end, block_len, means=None)
     """-> means [B, Hkv, ceil(keys / block_len), D] fp32: those of the blocks that hold a key of [kv_begin, kv_end) are written (kv_begin a
     multiple of block_len), the others left as they are (zero where the call allocates).  k_chunks: one tensor or a list of chunks."""
     chunks = _as_chunks(k_chunks)
-    _check_dtype(torch.bfloat16, "keys", *chunks)
-    _check_keys(None, chunks)
+    _check_keys(chunks)
     k = _kv_like(chunks)
     B, N, Hkv, D = k.shape
     blocks = -(-N // block_len) if block_len > 0 else 0
@@ -472,16 +464,16 @@ def _contiguous_strides(shape):
 
 def slimpipe_attn_block_select(q_slice, means, q_offset, kv_begin, kv_end, block_len, top_k, causal=True, index=None):
     """-> index [B, Hq, s, top_k] int32: the blocks of every query row, ascending, filled up with -1."""
-    _check_dtype(torch.bfloat16, "q_slice", q_slice)
-    _check_rows("q_slice", q_slice, q_slice.shape)
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
     if means.dim() != 4:
         raise SlimpipeError("means must have four dimensions")
-    B, s, Hq, D = q_slice.shape
+    B, s, Hq, D = shape
     Hkv, blocks = means.shape[1], means.shape[2]
     _check_means(means, B, Hkv, blocks, D)
     if index is None:
         index = torch.empty((B, Hq, s, top_k), device=q_slice.device, dtype=torch.int32)
-    if _check_index(index, q_slice) != top_k:
+    if _check_index(index, shape) != top_k:
         raise SlimpipeError("index must have top_k entries a row")
     _check_device(q_slice, means, index)
     sq = q_slice.stride()
@@ -501,10 +493,11 @@ def _block_ws(p, block_len, top_k, is_bwd):
 def slimpipe_attn_block_workspace_bytes(q_slice, k_chunks, index, q_offset, kv_begin, kv_end, block_len, causal=True, is_bwd=False):
     """Bytes of workspace that slimpipe_attn_block_fwd (or _bwd) of these tensors needs."""
     k_chunks = _as_chunks(k_chunks)
-    _check_rows("q_slice", q_slice, q_slice.shape)
-    _check_keys(q_slice, k_chunks)
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
+    _check_keys(k_chunks, shape)
     p = _params(q_slice, _kv_like(k_chunks), q_slice, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)
-    return _block_ws(p, block_len, _check_index(index, q_slice), is_bwd)
+    return _block_ws(p, block_len, _check_index(index, shape), is_bwd)
 
 
 def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_begin, kv_end, block_len, causal=True, scale=None, out_dtype=BF16,
@@ -512,18 +505,17 @@ def slimpipe_attn_block_fwd(q_slice, k_chunks, v_chunks, index, q_offset, kv_beg
     """-> (out, lse): slimpipe_attn_fwd restricted to the keys of the blocks that `index` names for each row.  k_chunks / v_chunks: one
     tensor each or lists of chunks.  workspace: uint8 tensor, allocated where None."""
     k_chunks, v_chunks = _as_chunks(k_chunks), _as_chunks(v_chunks)
-    _check_rows("q_slice", q_slice, q_slice.shape)
-    _check_keys(q_slice, k_chunks)
-    top_k = _check_index(index, q_slice)
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
+    _check_keys(k_chunks, shape)
+    _check_keys(v_chunks)
+    top_k = _check_index(index, shape)
     if len(k_chunks) != len(v_chunks) or not _same_strides(v_chunks[0], k_chunks[0]):
         raise SlimpipeError("v must have as many chunks as k, of the same shape and strides")
-    _check_dtype(torch.bfloat16, "q, k and v", q_slice, *k_chunks, *v_chunks)
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
-    _check_result_dtype(out_dtype, "out", "out_dtype", out)
-    _check_dtype(torch.float32, "lse", lse)
-    _check_rows("out", out, q_slice.shape)
-    _check_lse(lse, q_slice)
+    _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
+    _check_lse(lse, shape)
     p = _params(q_slice, _kv_like(k_chunks), out, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, False), device=q_slice.device, dtype=torch.uint8)
@@ -540,9 +532,10 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
     """-> dq: the gradients of slimpipe_attn_block_fwd with the same index.  dk_chunks / dv_chunks (fp32, one tensor each or lists, shaped like
     the keys) get rows [kv_begin, kv_end) written or incremented."""
     k_chunks, v_chunks, dk_chunks, dv_chunks = (list(_as_chunks(x)) for x in (k_chunks, v_chunks, dk_chunks, dv_chunks))
-    _check_rows("q_slice", q_slice, q_slice.shape)
-    _check_keys(q_slice, k_chunks)
-    top_k = _check_index(index, q_slice)
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
+    _check_keys(k_chunks, shape)
+    top_k = _check_index(index, shape)
     if dq is None:
         # (the strides of q also where those leave gaps: a slice of a sequence, a part of packed rows)
         dq = torch.empty_strided(q_slice.shape, q_slice.stride(), device=q_slice.device, dtype=torch.float32 if dq_dtype == F32 else torch.bfloat16)
@@ -553,12 +546,12 @@ def slimpipe_attn_block_bwd(q_slice, k_chunks, v_chunks, index, out, d_out, lse,
             raise SlimpipeError("v, dk and dv must have the strides of k")
     if not len(k_chunks) == len(v_chunks) == len(dk_chunks) == len(dv_chunks):
         raise SlimpipeError("k, v, dk and dv must have the same number of chunks")
-    _check_dtype(torch.bfloat16, "q, k, v, out and d_out", q_slice, out, d_out, *k_chunks, *v_chunks)
-    _check_dtype(torch.float32, "lse, dk and dv", lse, *dk_chunks, *dv_chunks)
-    _check_result_dtype(dq_dtype, "dq", "dq_dtype", dq)
-    _check_rows("out", out, q_slice.shape)
-    _check_rows("d_out", d_out, q_slice.shape)
-    _check_lse(lse, q_slice)
+    _check_keys(v_chunks)
+    _check_keys(dk_chunks + dv_chunks, None, torch.float32)
+    _check_rows("dq (its dtype is dq_dtype's)", dq, shape, _TORCH_DTYPE.get(dq_dtype))
+    _check_rows("out", out, shape)
+    _check_rows("d_out", d_out, shape)
+    _check_lse(lse, shape)
     p = _params(q_slice, _kv_like(k_chunks), out, d_out, q_offset, kv_begin, kv_end, causal, scale, BF16)
     if workspace is None:
         workspace = torch.empty(_block_ws(p, block_len, top_k, True), device=q_slice.device, dtype=torch.uint8)
@@ -606,7 +599,8 @@ def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
     (B, N, H, D), skv = cache.layout()
     if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or k_slice.stride(3) != 1 or not _same_strides(k_slice, v_slice):
         raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
-    _check_dtype(torch.bfloat16, "k_slice and v_slice", k_slice, v_slice)
+    if not k_slice.dtype is v_slice.dtype is torch.bfloat16:
+        raise SlimpipeError("k_slice and v_slice must be torch.bfloat16")
     _check_device(k_slice, v_slice, *cache)
     sx = k_slice.stride()[:3]
     p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
@@ -627,7 +621,8 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
         v_rows = torch.empty_like(k_rows)
     if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
         raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
-    _check_dtype(torch.bfloat16, "k_rows and v_rows", k_rows, v_rows)
+    if not k_rows.dtype is v_rows.dtype is torch.bfloat16:
+        raise SlimpipeError("k_rows and v_rows must be torch.bfloat16")
     _check_device(k_rows, v_rows, *cache)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
     p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
@@ -638,11 +633,11 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
 
 def _kv4_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
     (B, N, H, D), skv = cache.layout()
-    _check_rows("q_slice", q_slice, q_slice.shape)
-    if q_slice.shape[0] != B or q_slice.shape[3] != D:
+    shape = q_slice.shape
+    if len(shape) != 4 or shape[0] != B or shape[3] != D:
         raise SlimpipeError("q_slice and the cache must have the same batch and head_dim")
     sq, so = q_slice.stride(), out_like.stride()
-    return AttnParams(B, q_slice.shape[1], q_slice.shape[2], H, D, 1 if causal else 0, N, q_offset, kv_begin, kv_end,
+    return AttnParams(B, shape[1], shape[2], H, D, 1 if causal else 0, N, q_offset, kv_begin, kv_end,
                       float(scale) if scale is not None else 1.0 / math.sqrt(D), out_dtype, *sq[:3], *skv, *so[:3], *so[:3])
 
 
@@ -659,14 +654,12 @@ def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end
 
 def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
     """-> (out, lse): slimpipe_attn_fwd over a KvCache4.  workspace: uint8 tensor, allocated where None."""
-    _check_dtype(torch.bfloat16, "q_slice", q_slice)
-    _check_rows("q_slice", q_slice, q_slice.shape)
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
     if out is None or lse is None:
         out, lse = _outputs(q_slice, out_dtype, out, lse)
-    _check_result_dtype(out_dtype, "out", "out_dtype", out)
-    _check_dtype(torch.float32, "lse", lse)
-    _check_rows("out", out, q_slice.shape)
-    _check_lse(lse, q_slice)
+    _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
+    _check_lse(lse, shape)
     p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
