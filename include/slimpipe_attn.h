@@ -235,8 +235,9 @@ int slimpipe_attn_fwd_ranges(const slimpipe_attn_params* p, const void* q_slice,
 /* Sparse attention over key blocks that a cheap score selects for each query row.
  * Keys come in blocks: block j holds positions [j * block_len, (j + 1) * block_len).  The three calls below make the blocks' means,
  * pick the blocks of every query row and head, and attend to the keys of these blocks; slimpipe_attn_block_bwd is the gradient of the
- * last with the picks held fixed (they are a choice and have none).  As with every call here the key range [kv_begin, kv_end) may be a
- * part of the prefix, so that the (out, lse) of several ranges can be folded by slimpipe_attn_merge.
+ * last with the picks held fixed (they are a choice and have none).  They pay where a row's blocks are a small share of the keys it sees: beyond
+ * a quarter of them (blocks of 64 at head_dim 64) to a half (512 at 128) slimpipe_attn_fwd and slimpipe_attn_bwd are as fast.
+ * As with every call here the key range [kv_begin, kv_end) may be a part of the prefix, so that the (out, lse) of several ranges can be folded by slimpipe_attn_merge.
  *   block_len : a multiple of 64, 64 .. 65536 (SLIMPIPE_EINVAL_SHAPE otherwise); with several chunks chunk_len is a multiple of it.
  *   top_k     : 1 .. 64 slots per row (SLIMPIPE_EINVAL_SHAPE otherwise).
  *   limits    : batch * n_kv_heads <= 65535, less than 2^27 rows of all heads, 2^30 slots of one kv head, less than 2^22 - 1 blocks in the key range, in the
@@ -266,7 +267,10 @@ int slimpipe_attn_block_workspace_bytes(const slimpipe_attn_params* p, int32_t b
 /* Forward: row r of head h attends to the keys that slimpipe_attn_fwd would let it see and that lie in one of its blocks.  Any index will
  * do: entries outside the range's blocks are no block, a block named twice counts once, order is free.  out, lse, rows without a key and
  * keys that no row sees: as in slimpipe_attn_fwd.  A bf16 out is folded from results of a row's blocks in float16 with a float32
- * scale (weights and sums in float32), a float32 one from float32 results; likewise dq in the backward.  Results do not depend on the order in which workgroups run. */
+ * scale (weights and sums in float32), a float32 one from float32 results; likewise dq in the backward.  Under results of either dtype, as in
+ * slimpipe_attn_fwd and _bwd, the probabilities, and in the backward dS too, are rounded to bf16 once for the matrix units (the forward
+ * of a few tokens keeps them in float32); scores, softmax statistics and sums are float32.  Against 64 bits out is off by 0.0020 to 0.0023
+ * of its size and the gradients by 0.0024 (root mean square), of which one rounding to bf16 is 0.0017.  Results do not depend on the order in which workgroups run. */
 int slimpipe_attn_block_fwd(const slimpipe_attn_params* p, const void* q_slice, const void* const* k_chunks, const void* const* v_chunks, int32_t n_chunks,
                             int64_t chunk_len, int32_t block_len, int32_t top_k, const int32_t* index, void* out, float* lse, void* workspace,
                             size_t workspace_bytes, void* hip_stream);
@@ -301,7 +305,8 @@ int slimpipe_attn_kv4_load(const slimpipe_attn_params* p, const void* k_codes, c
 /* slimpipe_attn_fwd over such a cache, from one token to a slice: the same visibility, out, lse and rows without a key, and (out, lse) of key
  * ranges fold with those of bf16 calls (an old prefix in 4 bits, the newest slices in bf16).  workspace: slimpipe_attn_kv4_workspace_bytes
  * (0 for calls that fill the GPU by themselves: may be NULL then), for the float32 partial results of the key ranges that a call of few rows is
- * cut into.  Results do not depend on the order in which workgroups run. */
+ * cut into.  Results do not depend on the order in which workgroups run.  Codes are converted
+ * to bf16 exactly; roundings are otherwise those of slimpipe_attn_block_fwd with float32 results of the key ranges. */
 int slimpipe_attn_kv4_workspace_bytes(const slimpipe_attn_params* p, size_t* bytes);
 int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, const void* k_codes, const void* k_scales, const void* v_codes,
                           const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -67,7 +67,8 @@ int32_t whole_rounds(size_t n) { return (int32_t)((n + 8 * kXcdRun - 1) / (8 * k
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Where the parts of the workspace lie, and its size.
+// Where the parts of the workspace lie, and its size.  Partial results have room for float32 whatever the result's dtype: a workspace serves calls of either,
+// and the query of a backward does not know dq's.
 struct BlockWorkspace {
   size_t part_out, part_lse, part_scale, ranks, counts, lists, entries, items, n_items, delta, lse2, inf, dkdv_items, n_dkdv_items, dkdv_part, bytes;
   int32_t n_list_chunks, item_cap, chunk_rows, n_sub, dkdv_keys, dkdv_cap, part_cap;
@@ -92,7 +93,7 @@ int32_t dkdv_chunk_rows(int64_t slots, int32_t n_sub, int32_t keys) {
   if (rows < work / (12 * cus)) rows = work / (12 * cus);
   return (int32_t)(rows > 1 << 20 ? 1 << 20 : (rows + 31) / 32 * 32);
 }
-BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {      // (part_out: room for float32)
+BlockWorkspace layout(const slimpipe_attn_params* p, int32_t block_len, int32_t top_k, bool lists, bool is_bwd) {
   BlockWorkspace w;
   memset(&w, 0, sizeof(w));
   const size_t rows = (size_t)rows_of(p), planes = (size_t)p->batch * p->n_kv_heads, plane_rows = rows / planes;

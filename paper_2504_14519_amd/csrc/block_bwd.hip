@@ -353,14 +353,14 @@ __global__ __launch_bounds__(NW * 64, 2) void block_dkdv_kernel(const BlockArgs 
   item.flush(a, plane, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dk, dv, wave_u * 32, lane);
 }
 
-// Blocks of 256 keys and more: the phases of the dense dk/dv kernel (dkdv_tile.hpp, attn_bwd.hip) on gathered rows.  Eight waves of 32 keys; waves
+// 256 keys a workgroup (which block lengths take it: dkdv_keys() in block_api.hip): the phases of the dense dk/dv kernel (dkdv_tile.hpp, attn_bwd.hip) on gathered rows.  Eight waves of 32 keys; waves
 // 0-3 and 4-7 alternate matrix and vector phases one phase apart.  The group that is in a vector phase VV(u) copies tile u + 3 (group A
 // rows of Q, their statistics and row numbers, group B rows of dO, each lane from the address that its row's entry gives) and the entries of
 // tile u + 6.  Gathered rows come from beyond the L2, 1700 cycles and more away, longer than a phase: a group waits at the end of
 // MM(u) for what it copied in VV(u - 2) and before, and leaves the copies of VV(u - 1) under way.  Tile t is so in LDS at the end of MM(t - 1),
 // where it is needed, entries at the end of MM(t - 4), and they are read in MM(t - 3) for VV(t - 3).
-// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: 280 us (920 TFLOP/s; a tile of 32 rows in 1.8 us, 1180 TFLOP/s while the loop runs; a workgroup's
-// start is 7.6 us, its way out 3.8).  In parts of 1536 rows, before short parts went in order of length, it was 314, with copies of tile u + 2
+// 8192 rows of 8 heads on 128 blocks of 512 keys, 8 a row: 280 us (920 TFLOP/s; matrix units busy 56 % of it.  By clock reads in a copy of the kernel a tile of
+// 32 rows takes 1.9 us, 1140 TFLOP/s while the loop runs, a workgroup's start 7.5 us, its way out 4.3).  In parts of 1536 rows, before short parts went in order of length, it was 314, with copies of tile u + 2
 // that are waited for in the next phase 335, with four waves of 32 keys, two workgroups a compute unit and no phases 332.
 struct WideLds {
   static constexpr int D = 128, BMQ = 32, SLOTS = 5, TILE = BMQ * D * 2, DO_BASE = SLOTS * TILE;      // rings of Q, dO

@@ -5,8 +5,9 @@
 // bf16 the partial outs have 16 bits (float16 with a float32 scale a row; lse is float32 always): rounded to 2^-11 of themselves they add an
 // eighth of what one rounding to bf16 does, and the bytes of the partial outs, which every one of them costs twice, are what the fold and a
 // third of the tiles' epilogue take.
-// 8192 rows of 8 heads of 128 on 128 blocks of 512 keys, 8 a row: 179 us (720 TFLOP/s): a workgroup starts for 3.6 us, is 14 in its 8 tiles of keys (1210
-// TFLOP/s over the chip) and 2 to 3 on its way out, behind the other one of its compute unit in part.  3 x 1337 rows of 12 heads of 64 on 64 blocks of
+// 8192 rows of 8 heads of 128 on 128 blocks of 512 keys, 8 a row: 179 us (720 TFLOP/s; matrix units busy 41 % of it).  By clock reads in a copy of the
+// kernel a workgroup starts for 3.2 us, is 14 in its 8 tiles of keys (1210 TFLOP/s over the chip) and 2.2 on its way out, behind the other one of its
+// compute unit in part.  3 x 1337 rows of 12 heads of 64 on 64 blocks of
 // 64 keys, 12 a row: 37 us.
 #include "block_tile.hpp"
 #include "row_tile.hpp"

@@ -71,6 +71,8 @@ hipError_t launch_block_means(const BlockMeansArgs& a, int head_dim, hipStream_t
 // T comes from a first walk over the blocks: a lane keeps the K largest scores of its row that it has seen in order in registers; a score x
 // goes into the list t_0 >= t_1 .. by t_i = median(t_(i-1), t_i, x), one instruction a place and no branch.  A second walk computes the scores
 // again (cheaper than keeping them: 16 matrix instructions for 32 rows and 32 blocks) and writes down what is not below T - 2 delta.
+// The bound goes by the largest mean, so what all means have in common widens it without changing any order, and more rows are settled in 64 bits: the
+// case below with a common part of 3, 10 and 30 times the spread of the means takes 72, 98 and 151 us.
 // 16384 rows of 8 heads on 256 blocks of means of head_dim 128, top_k 8: 70 us, 18 a walk (7 for Q, 4 at the end, most of it rows settled in 64 bits); with three parts of a mean 77, with sorted pieces of scores kept in LDS 204,
 // with every score in 64 bits on the matrix unit 550.
 

@@ -76,7 +76,7 @@ struct BlockArgs {
   BlockItem* dkdv_items;         // [plane][dkdv_cap]
   int32_t* n_dkdv_items;         // [plane][2]: all of them, those of full length
   int32_t dkdv_cap;
-  float* dkdv_part;              // [plane][part_cap][2][sub * sub keys][head_dim]
+  float* dkdv_part;              // [plane][part_cap][2][n_sub * dkdv_keys][head_dim]
   int32_t part_cap;
   int64_t kv_end_range;          // end of the call's key range (rows behind the last seen key get gradients of 0)
 };

@@ -100,8 +100,9 @@ constexpr size_t kv4_fwd_lds_bytes() {         // two slots of converted K and V
 }
 
 // Slices: 128 rows a workgroup, 32 a wave (row_tile.hpp).  Codes of a tile of 64 keys are fetched one tile ahead into registers and
-// converted into LDS, a group of 32 elements a thread, for all four waves at once.  Bound by the matrix and vector work of the attention: 4096 rows of 8
-// heads on 32768 keys of one 530 us (970 TFLOP/s, the fold of two ranges included), the bf16 call 505.
+// converted into LDS, a group of 32 elements a thread, for all four waves at once.  4096 rows of 8 heads on 32768 keys of one: 530 us (970
+// TFLOP/s, the fold of two ranges included), and the bf16 call 455: this form saves memory, not time.  Matrix units are busy 47 % of it, vector units 15 %,
+// and 42 MB come from memory: none of them is full.
 template <int D>
 __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   constexpr int BN = 64, TILE = BN * D * 2, NG = D / 32, GROUPS = 2 * BN * NG, PER = GROUPS / 256;      // groups of K and V; a thread's
@@ -229,10 +230,11 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
 //   S^T = K Q^T      K goes from memory to the matrix unit without LDS: since the contraction may take head_dim in any order, lane group h
 //                    takes the h-th quarter of a row, 8 elements a step, and a lane's codes of 16 keys are one load
 //   O^T += V^T P^T   V passes through 32 rows of LDS of the wave's own for the transposed read (lane group h: keys 4 h .. 4 h + 3 of either 16)
-// Codes of the next two steps are under way in registers.  Bound by the bytes of the cache.
+// Codes of the next two steps are under way in registers (one with two heads a wave, whose loads start in the middle of the step before).
 // A row's codes are 64 bytes and its scales 4, of lines of 128 that hold the next heads' too: hence neighbouring heads in a workgroup, and the
-// workgroups that cover the same keys of a sequence one after the other on one XCD.  4 tokens of 40 heads on 32768 keys of 128: 200 us (3.6 TB/s, of
-// 3.8 to 4.0 that a sum over a large tensor reads).
+// workgroups that cover the same keys of a sequence one after the other on one XCD.  4 tokens of 40 heads on 32768 keys of 128: 200 us (720 MB,
+// 3.6 TB/s; the bf16 call 455).  Neither the memory, which gives a copy 4.8, nor the matrix units (busy 10 %), nor the vector units (8 %) are full: what is
+// left is the wait for codes.
 template <int D, int SETS, int HEADS>
 constexpr size_t kv4_few_lds_bytes() {
   constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * HEADS * (kOutRow<D> + 2) * 4;

@@ -106,8 +106,8 @@ __global__ __launch_bounds__(256) void part_merge_few_kernel(const PartMergeArgs
   put_result(a, row, d, x0, x1, m, l);
 }
 
-// Few rows: us of a call with the few-row kernel and without, 8 rows of 504 parts 35 and 226; 256 rows of 16 37 and 43, 1024 44 and 44, 2048 57 and 50;
-// of four parts no gain at 256 rows (13.4 both), 38 and 32 at 1024.
+// Few rows: us of a call with the few-row kernel and without, 8 rows of 512 parts 36 and 228; 256 rows of 128 29 and 84, 1024 of 64 40 and 59; of 16 parts
+// 256 rows 37 and 43, 1024 44 and 44, 2048 57 and 50; of four parts no gain at 256 rows (13.4 both), 38 and 32 at 1024.
 template <int D, bool F32>
 static void launch_merge_t(const PartMergeArgs& a, hipStream_t st) {
   if (a.rows <= 1024 && a.parts > 4) hipLaunchKernelGGL((part_merge_few_kernel<D, F32>), dim3((unsigned)a.rows, D / 32), dim3(256), 0, st, a);
