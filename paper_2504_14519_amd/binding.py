@@ -615,14 +615,15 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     shape = (B, kv_end - kv_begin, H, D)
     if k_rows is None and v_rows is None:
         k_rows, v_rows = torch.empty((2,) + shape, device=cache.k_codes.device, dtype=torch.bfloat16).unbind(0)
-    elif k_rows is None:
-        k_rows = torch.empty_like(v_rows)
-    elif v_rows is None:
-        v_rows = torch.empty_like(k_rows)
-    if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
-        raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
-    if not k_rows.dtype is v_rows.dtype is torch.bfloat16:
-        raise SlimpipeError("k_rows and v_rows must be torch.bfloat16")
+    else:
+        if k_rows is None:
+            k_rows = torch.empty_like(v_rows)
+        elif v_rows is None:
+            v_rows = torch.empty_like(k_rows)
+        if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
+            raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
+        if not k_rows.dtype is v_rows.dtype is torch.bfloat16:
+            raise SlimpipeError("k_rows and v_rows must be torch.bfloat16")
     _check_device(k_rows, v_rows, *cache)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
     p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
