@@ -617,9 +617,9 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
         k_rows, v_rows = torch.empty((2,) + shape, device=cache.k_codes.device, dtype=torch.bfloat16).unbind(0)
     else:
         if k_rows is None:
-            k_rows = torch.empty_like(v_rows)
+            k_rows = torch.empty_strided(v_rows.shape, v_rows.stride(), device=v_rows.device, dtype=v_rows.dtype)      # (gaps and all)
         elif v_rows is None:
-            v_rows = torch.empty_like(k_rows)
+            v_rows = torch.empty_strided(k_rows.shape, k_rows.stride(), device=k_rows.device, dtype=k_rows.dtype)
         if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
             raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
         if not k_rows.dtype is v_rows.dtype is torch.bfloat16:

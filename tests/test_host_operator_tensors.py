@@ -207,3 +207,11 @@ def test_current_device_of_this_host(sp):
     import paper_2504_14519_amd.binding as binding
     if torch.cuda.device_count() == 0:
         assert binding._current_device() == -1 == t(1).get_device()
+
+
+@pytest.mark.parametrize("name", ["k_rows", "v_rows"])
+def test_load_allocates_one_of_two(sp, name):
+    """The other one has gaps: a part of a packed tensor."""
+    for given in (t(B, S, H, D), t(B, S, 3 * H, D)[:, :, H:2 * H], t(B, H, S, D).transpose(1, 2), t(B, S + 3, H, D)[:, :S]):
+        accepts(sp, "load", k_rows=None, v_rows=None)
+        accepts(sp, "load", **{"k_rows": None, "v_rows": None, name: given})
