@@ -494,8 +494,9 @@ def slimpipe_attn_block_workspace_bytes(q_slice, k_chunks, index, q_offset, kv_b
     """Bytes of workspace that slimpipe_attn_block_fwd (or _bwd) of these tensors needs."""
     k_chunks = _as_chunks(k_chunks)
     shape = q_slice.shape
-    _check_rows("q_slice", q_slice, shape)
-    _check_keys(k_chunks, shape)
+    # (sizes alone: nothing is read, so stand-ins of any dtype will do)
+    _check_rows("q_slice", q_slice, shape, q_slice.dtype)
+    _check_keys(k_chunks, shape, k_chunks[0].dtype if k_chunks else None)
     p = _params(q_slice, _kv_like(k_chunks), q_slice, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)
     return _block_ws(p, block_len, _check_index(index, shape), is_bwd)
 

@@ -215,3 +215,15 @@ def test_load_allocates_one_of_two(sp, name):
     for given in (t(B, S, H, D), t(B, S, 3 * H, D)[:, :, H:2 * H], t(B, H, S, D).transpose(1, 2), t(B, S + 3, H, D)[:, :S]):
         accepts(sp, "load", k_rows=None, v_rows=None)
         accepts(sp, "load", **{"k_rows": None, "v_rows": None, name: given})
+
+
+def test_workspace_queries_look_at_sizes_alone(sp):
+    """Nothing is read: stand-ins of another dtype, or without memory, will do."""
+    a = right(sp)
+    want = sp.slimpipe_attn_block_workspace_bytes(a["q"], a["k"], a["index"], 0, 0, N, L)
+    for how in (dict(dtype=f32), dict(device="meta")):
+        q, k = (torch.empty(a[n].shape, **{"dtype": bf16, **how}) for n in "qk")
+        index = torch.empty(a["index"].shape, dtype=torch.int32, device=q.device)
+        assert sp.slimpipe_attn_block_workspace_bytes(q, k, index, 0, 0, N, L) == want
+        assert sp.slimpipe_attn_block_workspace_bytes(q, [k, k], index, 0, 0, N, L, True, True) > 0
+        assert sp.slimpipe_attn_kv4_workspace_bytes(q, a["cache"], 0, 0, N) == sp.slimpipe_attn_kv4_workspace_bytes(a["q"], a["cache"], 0, 0, N)
