@@ -188,6 +188,7 @@ __global__ __launch_bounds__(256, 2) void kv4_fwd_kernel(const Kv4Args a) {
   }
   float lse;
   const float norm = st.finish(&lse);
+  if (norm == 0.f) st.clear();                   // (weights of 0 times what other rows see, which may not be finite)
   float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
   put_rows<D>(part, st.o, norm, lane);
   const int64_t row = ((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r;
@@ -428,8 +429,8 @@ __global__ __launch_bounds__(256, 2) void kv4_few_kernel(const Kv4Args a) {
       x1 += f * *reinterpret_cast<const f32x4*>(acc + (w * RW + r) * kOutRow<D> + d + 4);
     }
     const float norm = sum == 0.f ? 0.f : 1.0f / sum, lse = sum == 0.f ? -INFINITY : (mx + __builtin_log2f(sum)) * kLn2;      // (a NaN is not 0)
-    x0 *= norm;
-    x1 *= norm;
+    x0 = sum == 0.f ? f32x4{0, 0, 0, 0} : x0 * norm;      // (as above)
+    x1 = sum == 0.f ? f32x4{0, 0, 0, 0} : x1 * norm;
     const Kv4Row at = kv4_row(a, hk0 + hh, rr);
     const int64_t row = ((int64_t)b * a.n_q_heads + at.h) * a.s_q + at.r;
     if (a.n_parts > 1) {

@@ -14,11 +14,14 @@ struct RowState {
   bf16x8 q[D / 16];
   f32x16 o[D / 32];
   float m, l;                // running maximum of the scaled scores (log2 units), sum of exp2(score - m), of this half-wave's keys
-  SP_DEV void init() {
+  SP_DEV void clear() {
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  }
+  SP_DEV void init() {
+    clear();
     m = -INFINITY;
     l = 0.f;
   }
