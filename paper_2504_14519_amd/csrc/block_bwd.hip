@@ -116,6 +116,12 @@ __global__ __launch_bounds__(256, 2) void block_dq_kernel(const BlockArgs a) {
       __syncthreads();
     }
   }
+  if (see_rel < 0) {                             // sees no key of the block (weights of 0 times what other rows see, which may not be finite)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) dq[db][i] = 0.f;
+  }
   store_parts<D>(a, reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>, dq, a.scale, row * a.top_k + (e.head_slot & 63u), n_rows, wave_u, lane);
 }
 
