@@ -313,6 +313,48 @@ int slimpipe_attn_kv4_workspace_bytes(const slimpipe_attn_params* p, size_t* byt
 int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, const void* k_codes, const void* k_scales, const void* v_codes,
                           const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Norm of every head of queries and keys, and the rotation of pairs of its elements by the row's position, in one pass: what a slice's projections
+ * go through before the attention calls.  For a head x of a row at position t
+ *     y = x / sqrt(mean(x^2) + eps) * weight;  of the first rotate_dim elements the pairs (i, i + rotate_dim / 2), or (2 i, 2 i + 1) when
+ *     interleaved, become (y_a cos - y_b sin, y_b cos + y_a sin) at the angle t * frequencies[i]; the others stay.
+ * Angles are computed in 64 bits, norms and products in 32, results rounded to bf16 once.
+ *   q, k            : bf16 [batch, rows, heads, head_dim] with the q and k strides (parts of one projected row, for instance); a side with 0 heads is not part
+ *                     of the call, its pointers may be NULL.
+ *   q_weight, k_weight : float32 [head_dim], NULL for ones.
+ *   frequencies     : float64 [rotate_dim / 2], radians a position (NULL when rotate_dim is 0).
+ *   positions       : int64 [batch, rows] contiguous, 0 .. 2^52, or NULL: row r is at p->position + r.
+ *   q_out, k_out    : bf16 with the qo and ko strides (k_out may be the slice's rows of a prefix).  A result may take the place of its operand (same pointer, same
+ *                     strides); tensors that overlap in other ways must not be passed.
+ * The backward takes the gradients of q_out and k_out (qo and ko strides, bf16 or float32 each: dk as the accumulators hold it) and gives those of q
+ * and k (bf16, the q and k strides; dq may take the place of q or, with equal strides and bf16, of dq_out) and of the weights (float32 [head_dim],
+ * overwritten, or added to when weight_accumulate; NULL: not wanted; only for weights that are given).  Sums run in a fixed order.
+ *   workspace : slimpipe_attn_norm_rotate_workspace_bytes, needed when a weight's gradient is wanted (SLIMPIPE_EWORKSPACE).
+ *   limits    : rotate_dim a multiple of 16, 0 .. head_dim; eps finite and > 0; heads 0 .. 65535, less than 2^31 rows of all heads
+ *               (SLIMPIPE_EINVAL_SHAPE); position + rows <= 2^52 (SLIMPIPE_EINVAL_RANGE). */
+typedef struct slimpipe_rotate_params {
+  int32_t batch;
+  int32_t rows;
+  int32_t n_q_heads;    /* any two numbers, not both 0                                    */
+  int32_t n_kv_heads;
+  int32_t head_dim;     /* 64 or 128                                                      */
+  int32_t rotate_dim;
+  int32_t interleaved;  /* 0 or 1                                                         */
+  float   eps;
+  int64_t position;
+  int64_t q_stride_b, q_stride_s, q_stride_h;     /* q and dq                              */
+  int64_t k_stride_b, k_stride_s, k_stride_h;     /* k and dk                              */
+  int64_t qo_stride_b, qo_stride_s, qo_stride_h;  /* q_out and dq_out                      */
+  int64_t ko_stride_b, ko_stride_s, ko_stride_h;  /* k_out and dk_out                      */
+} slimpipe_rotate_params;
+
+int slimpipe_attn_norm_rotate(const slimpipe_rotate_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                              const double* frequencies, const int64_t* positions, void* q_out, void* k_out, void* hip_stream);
+int slimpipe_attn_norm_rotate_workspace_bytes(const slimpipe_rotate_params* p, size_t* bytes);
+int slimpipe_attn_norm_rotate_bwd(const slimpipe_rotate_params* p, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                                  const double* frequencies, const int64_t* positions, const void* dq_out, int32_t dq_out_dtype, const void* dk_out,
+                                  int32_t dk_out_dtype, void* dq, void* dk, float* dq_weight, float* dk_weight, int32_t weight_accumulate,
+                                  void* workspace, size_t workspace_bytes, void* hip_stream);
+
 const char* slimpipe_attn_strerror(int code);
 
 #ifdef __cplusplus

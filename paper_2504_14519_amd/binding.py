@@ -37,6 +37,18 @@ class AttnParams(ctypes.Structure):
     ]
 
 
+class RotateParams(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("rows", ctypes.c_int32), ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("rotate_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+        ("position", ctypes.c_int64),
+        ("q_stride_b", ctypes.c_int64), ("q_stride_s", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+        ("k_stride_b", ctypes.c_int64), ("k_stride_s", ctypes.c_int64), ("k_stride_h", ctypes.c_int64),
+        ("qo_stride_b", ctypes.c_int64), ("qo_stride_s", ctypes.c_int64), ("qo_stride_h", ctypes.c_int64),
+        ("ko_stride_b", ctypes.c_int64), ("ko_stride_s", ctypes.c_int64), ("ko_stride_h", ctypes.c_int64),
+    ]
+
+
 class BwdPlan(ctypes.Structure):
     _fields_ = [
         ("one_launch", ctypes.c_int32), ("dq_first", ctypes.c_int32), ("dkdv_split", ctypes.c_int32), ("dq_ranges", ctypes.c_int32),
@@ -113,6 +125,13 @@ def _load():
     L.slimpipe_attn_kv4_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_fwd_kv4.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_fwd_kv4.restype = ctypes.c_int
+    R = ctypes.POINTER(RotateParams)
+    L.slimpipe_attn_norm_rotate.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_norm_rotate.restype = ctypes.c_int
+    L.slimpipe_attn_norm_rotate_workspace_bytes.argtypes = [R, szp]
+    L.slimpipe_attn_norm_rotate_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_norm_rotate_bwd.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_norm_rotate_bwd.restype = ctypes.c_int
     L.slimpipe_attn_mfma_rate.argtypes = [ctypes.c_int, vp, ctypes.POINTER(ctypes.c_double), vp]
     L.slimpipe_attn_mfma_rate.restype = ctypes.c_int
     L.slimpipe_attn_dq_atomic_probe.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, i32, vp, ctypes.POINTER(ctypes.c_double), vp]
@@ -670,6 +689,96 @@ def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
     _check(lib.slimpipe_attn_fwd_kv4(ctypes.byref(p), q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(), *_ws(workspace),
                                      _stream()), "slimpipe_attn_fwd_kv4")
     return out, lse
+
+
+def _rotate_params(q, k, weights, frequencies, position, eps, interleaved, q_out, k_out, q_out_dtype=torch.bfloat16, k_out_dtype=torch.bfloat16):
+    """Checks of what the two directions share -> (parameters, device pointer of the positions or None)."""
+    shape, k_shape = q.shape, k.shape
+    _check_rows("q", q, shape)
+    _check_rows("k", k, (shape[0], shape[1], k_shape[2] if len(k_shape) == 4 else -1, shape[3]))
+    _check_rows("q_out", q_out, shape, q_out_dtype)
+    _check_rows("k_out", k_out, k_shape, k_out_dtype)
+    B, s, Hq, D = shape
+    for w in weights:
+        if w is not None and (w.dtype is not torch.float32 or w.shape != (D,) or not w.is_contiguous()):
+            raise SlimpipeError("weights and their gradients must be contiguous float32 tensors [head_dim]")
+    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
+        raise SlimpipeError("frequencies must be a contiguous float64 tensor [rotate_dim / 2]")
+    at = None
+    if isinstance(position, torch.Tensor):
+        if position.dtype is not torch.int64 or position.shape != (B, s) or not position.is_contiguous():
+            raise SlimpipeError("positions must be a contiguous int64 tensor [batch, rows], or one number: that of row 0")
+        at, position = position, 0
+    _check_device(q, k, q_out, k_out, frequencies, *[w for w in weights if w is not None], *([at] if at is not None else []))
+    p = RotateParams(B, s, Hq, k_shape[2], D, 2 * frequencies.shape[0], 1 if interleaved else 0, eps, position,
+                     *q.stride()[:3], *k.stride()[:3], *q_out.stride()[:3], *k_out.stride()[:3])
+    return p, at.data_ptr() if at is not None else None
+
+
+def _ptr(x):
+    return x.data_ptr() if x is not None else None
+
+
+def slimpipe_attn_norm_rotate(q, k, q_weight, k_weight, frequencies, position, eps=1e-6, interleaved=False, q_out=None, k_out=None):
+    """-> (q_out, k_out): every head of q [B, s, Hq, D] and k [B, s, Hkv, D] divided by its root mean square and multiplied by the weight (fp32 [D],
+    None for ones), then rotated.  frequencies: fp64 [rotate_dim / 2], radians a position (empty: no rotation).  position: that of row 0, or an
+    int64 tensor [B, s].  The results may be q and k themselves, or rows of a key prefix."""
+    if q_out is None:
+        q_out = torch.empty(q.shape, device=q.device, dtype=torch.bfloat16)
+    if k_out is None:
+        k_out = torch.empty(k.shape, device=k.device, dtype=torch.bfloat16)
+    p, at = _rotate_params(q, k, (q_weight, k_weight), frequencies, position, eps, interleaved, q_out, k_out)
+    _check(lib.slimpipe_attn_norm_rotate(ctypes.byref(p), q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
+                                         q_out.data_ptr(), k_out.data_ptr(), _stream()), "slimpipe_attn_norm_rotate")
+    return q_out, k_out
+
+
+def _rotate_ws(p):
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_norm_rotate_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "norm_rotate_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_norm_rotate_workspace_bytes(q, k):
+    """Bytes of workspace that slimpipe_attn_norm_rotate_bwd of q and k needs for the gradients of the weights."""
+    _check_rows("q", q, q.shape, q.dtype)
+    _check_rows("k", k, k.shape, k.dtype)
+    B, s, Hq, D = q.shape
+    strides = (D,) * 3
+    return _rotate_ws(RotateParams(B, s, Hq, k.shape[2], D, 0, 0, 1.0, 0, *strides, *strides, *strides, *strides))
+
+
+def slimpipe_attn_norm_rotate_bwd(q, k, q_weight, k_weight, frequencies, position, dq_out, dk_out, eps=1e-6, interleaved=False, dq=None, dk=None,
+                                  dq_weight=None, dk_weight=None, weight_accumulate=False, workspace=None):
+    """-> (dq, dk, dq_weight, dk_weight): gradients of slimpipe_attn_norm_rotate from those of its results, bf16 or fp32 each (dk_out may be a slice's rows
+    of the fp32 accumulators).  dq, dk: bf16 with the strides of q and k.  Gradients of the weights (fp32 [D]) are written, or added to where
+    weight_accumulate; None for a weight that is None."""
+    if dq is None:
+        dq = torch.empty_strided(q.shape, q.stride(), device=q.device, dtype=torch.bfloat16)
+    if dk is None:
+        dk = torch.empty_strided(k.shape, k.stride(), device=k.device, dtype=torch.bfloat16)
+    if dq_weight is None and q_weight is not None:
+        dq_weight = torch.zeros_like(q_weight)
+    if dk_weight is None and k_weight is not None:
+        dk_weight = torch.zeros_like(k_weight)
+    dtypes = [x.dtype for x in (dq_out, dk_out)]
+    for t in dtypes:
+        if t is not torch.bfloat16 and t is not torch.float32:
+            raise SlimpipeError("gradients of the results must be torch.bfloat16 or torch.float32")
+    p, at = _rotate_params(q, k, (q_weight, k_weight, dq_weight, dk_weight), frequencies, position, eps, interleaved, dq_out, dk_out, *dtypes)
+    if not _same_strides(dq, q) or not _same_strides(dk, k):
+        raise SlimpipeError("dq and dk must have the strides of q and k")
+    if not dq.dtype is dk.dtype is torch.bfloat16:
+        raise SlimpipeError("dq and dk must be torch.bfloat16")
+    if workspace is None:
+        workspace = torch.empty(_rotate_ws(p), device=q.device, dtype=torch.uint8)
+    _check_workspace(workspace)
+    _check_device(dq, dk, workspace)
+    codes = [F32 if t is torch.float32 else BF16 for t in dtypes]
+    _check(lib.slimpipe_attn_norm_rotate_bwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
+                                             dq_out.data_ptr(), codes[0], dk_out.data_ptr(), codes[1], dq.data_ptr(), dk.data_ptr(), _ptr(dq_weight),
+                                             _ptr(dk_weight), 1 if weight_accumulate else 0, *_ws(workspace), _stream()), "slimpipe_attn_norm_rotate_bwd")
+    return dq, dk, dq_weight, dk_weight
 
 
 KERNEL_KINDS = ("fwd", "delta", "dq", "dkdv", "merge", "finalize", "dkdv_reduce", "dq_reduce",
