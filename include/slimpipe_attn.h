@@ -313,6 +313,35 @@ int slimpipe_attn_kv4_workspace_bytes(const slimpipe_attn_params* p, size_t* byt
 int slimpipe_attn_fwd_kv4(const slimpipe_attn_params* p, const void* q_slice, const void* k_codes, const void* k_scales, const void* v_codes,
                           const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* A key/value cache held in 8 bits with a scale for each block of rows and head, for prefixes that are kept for reading (answering from a prompt, token
+ * after token).  Rows [j * block_len, (j + 1) * block_len) of a kv head share a scale 2^e, stored as the byte e + 127; e is the smallest integer, at
+ * least -110, with max |x| <= 448 * 2^e over the finite elements of the block.  An element is x / 2^e rounded to an 8-bit float: sign, 4 exponent bits (bias 7), 3 mantissa
+ * bits, subnormal below 2^-6, ties to the even code, largest 448, 0x7f and 0xff NaN.  Infinities and NaN are stored as NaN; magnitudes
+ * that round to 2^128 (from 1.9375 * 2^127 on) read as infinities.
+ *   block_len     : a power of two, 16 .. 256 (SLIMPIPE_EINVAL_SHAPE otherwise).
+ *   codes         : bytes [batch, kv_capacity, n_kv_heads, head_dim] for keys and for values, at the kv strides of p, multiples of 16
+ *              (SLIMPIPE_EINVAL_STRIDE otherwise), 16-byte aligned.
+ *   scales        : bytes [batch, ceil(kv_capacity / block_len), n_kv_heads], contiguous.
+ *   limits   : kv_capacity <= 2^36, batch * n_kv_heads <= 65535, 2^30 keys in a range, less than 2^27 rows of all heads in a slice, a store or a
+ *              load (SLIMPIPE_EINVAL_SHAPE otherwise). */
+
+/* Appends the rows of a slice at positions q_offset .. q_offset + s_q - 1, behind the q_offset rows that the cache holds.  k_slice, v_slice: bf16
+ * [batch, s_q, n_kv_heads, head_dim] with the q strides.  A block that holds rows already keeps its scale, or takes the larger one that the new rows need; its rows are
+ * then rounded once more (without an error but for elements that fall below 2^-6 of the new scale).  What rows behind the last one of the slice stood for is lost in
+ * blocks that the slice touches (their codes stay, the scale may change).  (n_q_heads, causal, scale and the key range are only validated.) */
+int slimpipe_attn_kv8_store(const slimpipe_attn_params* p, int32_t block_len, const void* k_slice, const void* v_slice, void* k_codes, void* k_scales,
+                            void* v_codes, void* v_scales, void* hip_stream);
+/* Rows [kv_begin, kv_end) as the bf16 numbers they stand for (exactly): k_rows, v_rows [batch, kv_end - kv_begin, n_kv_heads, head_dim] with the
+ * o strides. */
+int slimpipe_attn_kv8_load(const slimpipe_attn_params* p, int32_t block_len, const void* k_codes, const void* k_scales, const void* v_codes,
+                           const void* v_scales, void* k_rows, void* v_rows, void* hip_stream);
+/* slimpipe_attn_fwd over such a cache, from one token to a slice: the same visibility, out, lse and rows without a key, and (out, lse) of key
+ * ranges fold with those of bf16 and 4-bit calls.  workspace: slimpipe_attn_kv8_workspace_bytes (may be 0: NULL then).  Results do not
+ * depend on the order in which workgroups run.  Codes are converted to bf16 exactly; roundings are otherwise those of slimpipe_attn_fwd. */
+int slimpipe_attn_kv8_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);
+int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
+                          const void* v_codes, const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Norm of every head of queries and keys, and the rotation of pairs of its elements by the row's position, in one pass: what a slice's projections
  * go through before the attention calls.  For a head x of a row at position t
  *     y = x / sqrt(mean(x^2) + eps) * weight;  of the first rotate_dim elements the pairs (i, i + rotate_dim / 2), or (2 i, 2 i + 1) when

@@ -7,5 +7,6 @@ from .binding import (  # noqa: F401
     slimpipe_attn_bwd_noalloc, slimpipe_attn_dq_atomic_probe, slimpipe_attn_xcd_rate, slimpipe_attn_small_bwd_plan,
     slimpipe_attn_block_means, slimpipe_attn_block_select, slimpipe_attn_block_workspace_bytes, slimpipe_attn_block_fwd, slimpipe_attn_block_bwd,
     KvCache4, slimpipe_attn_kv4_store, slimpipe_attn_kv4_load, slimpipe_attn_kv4_workspace_bytes, slimpipe_attn_fwd_kv4,
+    KvCache8, slimpipe_attn_kv8_store, slimpipe_attn_kv8_load, slimpipe_attn_kv8_workspace_bytes, slimpipe_attn_fwd_kv8,
     RotateParams, slimpipe_attn_norm_rotate, slimpipe_attn_norm_rotate_bwd, slimpipe_attn_norm_rotate_workspace_bytes,
 )

@@ -125,6 +125,14 @@ def _load():
     L.slimpipe_attn_kv4_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_fwd_kv4.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_fwd_kv4.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_store.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_store.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_load.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_load.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_workspace_bytes.argtypes = [P, i32, szp]
+    L.slimpipe_attn_kv8_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_fwd_kv8.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_fwd_kv8.restype = ctypes.c_int
     R = ctypes.POINTER(RotateParams)
     L.slimpipe_attn_norm_rotate.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_norm_rotate.restype = ctypes.c_int
@@ -627,23 +635,28 @@ def slimpipe_attn_kv4_store(k_slice, v_slice, cache, position):
     _check(lib.slimpipe_attn_kv4_store(ctypes.byref(p), k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()), "slimpipe_attn_kv4_store")
 
 
+def _loaded_rows(shape, device, k_rows, v_rows):
+    """The rows that a cache's load writes: those given, checked, or new ones."""
+    if shape[1] < 0:
+        raise SlimpipeError("kv_end lies before kv_begin")
+    if k_rows is None and v_rows is None:
+        return torch.empty((2,) + shape, device=device, dtype=torch.bfloat16).unbind(0)
+    if k_rows is None:
+        k_rows = torch.empty_strided(v_rows.shape, v_rows.stride(), device=v_rows.device, dtype=v_rows.dtype)      # (gaps and all)
+    elif v_rows is None:
+        v_rows = torch.empty_strided(k_rows.shape, k_rows.stride(), device=k_rows.device, dtype=k_rows.dtype)
+    if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
+        raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
+    if not k_rows.dtype is v_rows.dtype is torch.bfloat16:
+        raise SlimpipeError("k_rows and v_rows must be torch.bfloat16")
+    return k_rows, v_rows
+
+
 def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     """-> (k, v) bf16 [B, kv_end - kv_begin, Hkv, D]: the numbers that the rows of a KvCache4 stand for."""
     (B, N, H, D), skv = cache.layout()
-    if kv_end < kv_begin:
-        raise SlimpipeError("kv_end lies before kv_begin")
     shape = (B, kv_end - kv_begin, H, D)
-    if k_rows is None and v_rows is None:
-        k_rows, v_rows = torch.empty((2,) + shape, device=cache.k_codes.device, dtype=torch.bfloat16).unbind(0)
-    else:
-        if k_rows is None:
-            k_rows = torch.empty_strided(v_rows.shape, v_rows.stride(), device=v_rows.device, dtype=v_rows.dtype)      # (gaps and all)
-        elif v_rows is None:
-            v_rows = torch.empty_strided(k_rows.shape, k_rows.stride(), device=k_rows.device, dtype=k_rows.dtype)
-        if tuple(k_rows.shape) != shape or k_rows.stride(3) != 1 or not _same_strides(k_rows, v_rows):
-            raise SlimpipeError("k_rows and v_rows must be [batch, kv_end - kv_begin, kv heads, head_dim] with the same strides")
-        if not k_rows.dtype is v_rows.dtype is torch.bfloat16:
-            raise SlimpipeError("k_rows and v_rows must be torch.bfloat16")
+    k_rows, v_rows = _loaded_rows(shape, cache.k_codes.device, k_rows, v_rows)
     _check_device(k_rows, v_rows, *cache)
     sx = k_rows.stride()[:3] if shape[1] > 0 else (H * D, H * D, D)
     p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
@@ -652,7 +665,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     return k_rows, v_rows
 
 
-def _kv4_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
+def _cache_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
     (B, N, H, D), skv = cache.layout()
     shape = q_slice.shape
     if len(shape) != 4 or shape[0] != B or shape[3] != D:
@@ -670,7 +683,7 @@ def _kv4_ws(p):
 
 def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
     """Bytes of workspace that slimpipe_attn_fwd_kv4 of these tensors needs (may be 0)."""
-    return _kv4_ws(_kv4_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16))
+    return _kv4_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16))
 
 
 def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
@@ -681,13 +694,96 @@ def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
     _check_lse(lse, shape)
-    p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    p = _cache_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
     _check_device(q_slice, out, lse, workspace, *cache)
     _check(lib.slimpipe_attn_fwd_kv4(ctypes.byref(p), q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(), *_ws(workspace),
                                      _stream()), "slimpipe_attn_fwd_kv4")
+    return out, lse
+
+
+class KvCache8(collections.namedtuple("KvCache8", "k_codes k_scales v_codes v_scales block_len")):
+    """A key/value cache held in 8 bits: uint8 tensors [B, capacity, Hkv, D] (codes) and [B, ceil(capacity / block_len), Hkv] (scales, contiguous), where
+    block_len rows of a head share a scale."""
+    __slots__ = ()
+
+    @classmethod
+    def empty(cls, batch, capacity, kv_heads, head_dim, block_len=64, device="cuda"):
+        def codes():
+            return torch.zeros((batch, capacity, kv_heads, head_dim), device=device, dtype=torch.uint8)
+
+        def scales():
+            return torch.zeros((batch, -(-capacity // block_len), kv_heads), device=device, dtype=torch.uint8)
+        return cls(codes(), scales(), codes(), scales(), block_len)
+
+    def layout(self):
+        """(batch, capacity, kv heads, head_dim) and the three strides, after a check that the four tensors agree."""
+        kc, ks, vc, vs, block = self
+        shape, codes, v_codes, u8 = kc.shape, kc.stride(), vc.stride(), torch.uint8
+        if len(shape) == 4 and kc.dtype is ks.dtype is vc.dtype is vs.dtype is u8 and vc.shape == shape and codes[3] == v_codes[3] == 1 and block > 0:
+            B, N, H, D = shape
+            b, n, h = codes[:3]
+            # (a dimension of one element may have any stride)
+            if (ks.shape == vs.shape == (B, -(-N // block), H) and ks.is_contiguous() and vs.is_contiguous()
+                    and (codes == v_codes or ((B == 1 or b == v_codes[0]) and (N == 1 or n == v_codes[1]) and (H == 1 or h == v_codes[2])))):
+                return (B, N, H, D), (b if B > 1 else N * H * D, n if N > 1 else H * D, h if H > 1 else D)
+        raise SlimpipeError("codes must be uint8 [batch, keys, heads, head_dim] of the same layout, scales contiguous uint8 [batch, ceil(keys / block_len), heads]")
+
+
+def slimpipe_attn_kv8_store(k_slice, v_slice, cache, position):
+    """Append bf16 rows k_slice, v_slice [B, s, Hkv, D] to a KvCache8 that holds `position` rows."""
+    (B, N, H, D), skv = cache.layout()
+    if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or k_slice.stride(3) != 1 or not _same_strides(k_slice, v_slice):
+        raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
+    if not k_slice.dtype is v_slice.dtype is torch.bfloat16:
+        raise SlimpipeError("k_slice and v_slice must be torch.bfloat16")
+    _check_device(k_slice, v_slice, *cache[:4])
+    sx = k_slice.stride()[:3]
+    p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
+    _check(lib.slimpipe_attn_kv8_store(ctypes.byref(p), cache.block_len, k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()),
+           "slimpipe_attn_kv8_store")
+
+
+def slimpipe_attn_kv8_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
+    """-> (k, v) bf16 [B, kv_end - kv_begin, Hkv, D]: the numbers that the rows of a KvCache8 stand for."""
+    (B, N, H, D), skv = cache.layout()
+    k_rows, v_rows = _loaded_rows((B, kv_end - kv_begin, H, D), cache.k_codes.device, k_rows, v_rows)
+    _check_device(k_rows, v_rows, *cache[:4])
+    sx = k_rows.stride()[:3] if kv_end > kv_begin else (H * D, H * D, D)
+    p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
+    _check(lib.slimpipe_attn_kv8_load(ctypes.byref(p), cache.block_len, *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
+           if kv_end > kv_begin else lib.slimpipe_attn_validate(ctypes.byref(p), 0), "slimpipe_attn_kv8_load")
+    return k_rows, v_rows
+
+
+def _kv8_ws(p, block_len):
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_kv8_workspace_bytes(ctypes.byref(p), block_len, ctypes.byref(n)), "kv8_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_kv8_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
+    """Bytes of workspace that slimpipe_attn_fwd_kv8 of these tensors needs (may be 0)."""
+    return _kv8_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16), cache.block_len)
+
+
+def slimpipe_attn_fwd_kv8(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
+    """-> (out, lse): slimpipe_attn_fwd over a KvCache8.  workspace: uint8 tensor, allocated where None."""
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
+    if out is None or lse is None:
+        out, lse = _outputs(q_slice, out_dtype, out, lse)
+    _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
+    _check_lse(lse, shape)
+    p = _cache_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    if workspace is None:
+        workspace = torch.empty(_kv8_ws(p, cache.block_len), device=q_slice.device, dtype=torch.uint8)
+    _check_workspace(workspace)
+    _check_device(q_slice, out, lse, workspace, *cache[:4])
+    _check(lib.slimpipe_attn_fwd_kv8(ctypes.byref(p), cache.block_len, q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(),
+                                     *_ws(workspace), _stream()), "slimpipe_attn_fwd_kv8")
     return out, lse
 
 

@@ -241,15 +241,6 @@ constexpr size_t kv4_few_lds_bytes() {
   constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * HEADS * (kOutRow<D> + 2) * 4;
   return tiles > out ? tiles : out;
 }
-SP_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-SP_DEV float quarters_max(float v) {      // over the four lane groups
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return xhalf_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
-}
-SP_DEV float quarters_sum(float v) {
-  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
-}
 template <int D, int SETS, int HEADS>
 __global__ __launch_bounds__(256, 2) void kv4_few_kernel(const Kv4Args a) {
   constexpr int W = D / 32, N = SETS * HEADS, DEPTH = HEADS == 1 ? 2 : 1, DB = D / 16, QUARTER = D / 4;      // dwords of codes of a quarter row (= matrix steps), output blocks

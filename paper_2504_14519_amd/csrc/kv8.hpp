@@ -1,0 +1,79 @@
+// Argument blocks and launchers of the kernels of a key/value cache held in 8 bits (internal to the library).
+#pragma once
+#include "kv4.hpp"
+
+namespace slimpipe {
+
+// A cache operand: codes (a byte an element, at the element strides), scales ([batch, blocks, heads] bytes, contiguous)
+struct Kv8Operand { uint8_t* codes; uint8_t* scales; };
+
+struct Kv8Cache {
+  Kv8Operand k, v;
+  int32_t n_kv_heads, shift;     // a block has 1 << shift rows
+  int64_t stride_b, stride_s, stride_h, blocks;      // blocks of a sequence: ceil(capacity / block_len)
+};
+
+struct Kv8CopyArgs {
+  Kv8Cache cache;
+  const __bf16 *k_src, *v_src;   // store: [batch, rows, n_kv_heads, head_dim]
+  __bf16 *k_dst, *v_dst;         // load: the same
+  int64_t batch, rows, position; // rows of the slice, position of its first one in the cache
+  int64_t x_stride_b, x_stride_s, x_stride_h;          // of the bf16 rows
+};
+
+struct Kv8Args {
+  const __bf16* q;
+  Kv8Cache cache;
+  void* out;
+  float* lse;
+  int32_t batch, s_q, n_q_heads, group, causal, out_f32;
+  int64_t q_offset, kv_begin, kv_end;      // kv_end: one past the last key that any row sees
+  float scale_log2e;
+  int64_t q_stride_b, q_stride_s, q_stride_h;
+  int64_t o_stride_b, o_stride_s, o_stride_h;
+  int32_t n_parts;               // key ranges of part_keys keys (the last one shorter), a workgroup each; 1: straight to out, lse
+  int64_t part_keys;
+  float* part_out;               // [batch, n_q_heads, s_q][n_parts][head_dim], as in PartMergeArgs
+  float* part_lse;
+};
+
+struct Kv8WeightArgs {
+  const __bf16* q;
+  Kv8Cache cache;                // (of its values nothing is read)
+  const float* lse;              // [batch, n_q_heads, s_q]
+  const float* previous;         // [batch, n_kv_heads, capacity], or nullptr
+  float* weights;                // the same
+  float decay;
+  int32_t batch, s_q, n_q_heads, group, causal;
+  int64_t capacity, q_offset, kv_begin, kv_end, seen_end;      // keys of [seen_end, kv_end) are seen by no row
+  float scale_log2e;
+  int64_t q_stride_b, q_stride_s, q_stride_h;
+  int32_t n_parts;               // row ranges of part_rows rows of a plane, a workgroup each
+  int32_t part_rows;
+  float* part;                   // [n_parts][batch, n_kv_heads][keys], n_parts > 1
+};
+
+struct Kv8KeepArgs {
+  const float* weights;          // [planes][capacity]
+  int32_t* index;                // [planes][keep]
+  int64_t capacity;
+  int32_t planes, rows, keep, recent;
+  uint32_t* work;                // several workgroups a plane: histograms and counts (keep_work_words a plane)
+};
+
+struct Kv8GatherArgs {
+  Kv8Cache from, to;
+  const int32_t* index;          // [batch, n_kv_heads, keep]
+  const float* weights;          // [batch, n_kv_heads, capacity of from], or nullptr
+  float* kept_weights;           // [batch, n_kv_heads, weights_to_stride]
+  int64_t weights_stride, kept_weights_stride, from_rows;
+  int32_t batch, keep;
+};
+
+hipError_t launch_kv8_store(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
+hipError_t launch_kv8_load(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
+hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, bool few, hipStream_t st);      // few: group * s_q <= kKv8FewRows
+constexpr int kKv8FewRows = 32;
+hipError_t opt_in_kv8_kernels();
+
+}  // namespace slimpipe

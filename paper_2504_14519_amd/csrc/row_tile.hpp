@@ -9,6 +9,25 @@
 
 namespace slimpipe {
 
+// v_mfma_f32_16x16x32_bf16: with lane = 16 h + r an operand's lane holds row or column r, contraction slots 8 h .. 8 h + 7, a result's column r, register i
+// row 4 h + i.
+SP_DEV f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+SP_DEV float quarters_max(float v) {      // over the four lane groups
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return xhalf_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+SP_DEV float quarters_sum(float v) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Rows of a plane (batch index, kv head) are numbered head of the group major: row rh is row rh % s_q of head rh / s_q.
+struct PlaneRow { int r, h; };
+SP_DEV PlaneRow plane_row(int s_q, int group, int hk, int rh) {
+  const int hl = rh / s_q;
+  return {rh - hl * s_q, hk * group + hl};
+}
+
 template <int D>
 struct RowState {
   bf16x8 q[D / 16];
