@@ -342,6 +342,34 @@ int slimpipe_attn_kv8_workspace_bytes(const slimpipe_attn_params* p, int32_t blo
 int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
                           const void* v_codes, const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* Eviction: a cache in 8 bits made smaller by the attention weight that its rows have gathered.  The three calls below sum the weights up, choose the rows
+ * that stay, and move them, kv head by kv head, to another cache, where they lie one after the other in their old order: attention over it goes by rows
+ * (q_offset = rows of the cache), while the positions of queries and keys in slimpipe_attn_norm_rotate go on. */
+
+/* weights[b, h, j] = decay * previous[b, h, j] + sum of exp(scale * q.k_j - lse) over the rows of the slice that see key j and the query heads of kv head h, for
+ * the keys of [kv_begin, kv_end); others are untouched.  weights, previous: float32 [batch, n_kv_heads, kv_capacity], contiguous; previous may be NULL (for 0) or
+ * weights itself.  lse: what the attention of these rows over all their keys returned; a row whose lse is -inf adds nothing.  Values are not read.
+ * workspace: slimpipe_attn_kv8_weights_workspace_bytes (may be 0: NULL then).  Sums run in a fixed order, in 32 bits.
+ *   limits : as for the cache's other calls; decay finite; ceil(keys / 256) * batch * n_kv_heads < 2^25 (SLIMPIPE_EINVAL_SHAPE otherwise). */
+int slimpipe_attn_kv8_weights_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);
+int slimpipe_attn_kv8_weights(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
+                              const float* lse, const float* previous, float decay, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Of the first `rows` entries of each plane (batch index, kv head) of weights [planes, capacity] the `recent` last ones and the keep - recent largest of the
+ * others (equal ones, both zeros alike, the lower index first; NaN behind everything): their indices, ascending, in index, int32 [planes, keep], contiguous.
+ *   workspace : slimpipe_attn_kv8_keep_workspace_bytes (may be 0: NULL then).
+ *   limits    : planes 1 .. 65535, rows 1 .. 2^30 (SLIMPIPE_EINVAL_SHAPE), 0 <= recent <= keep, 1 <= keep <= rows <= capacity (SLIMPIPE_EINVAL_RANGE). */
+int slimpipe_attn_kv8_keep_workspace_bytes(int32_t planes, int64_t rows, int64_t keep, size_t* bytes);
+int slimpipe_attn_kv8_keep(const float* weights, int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int64_t recent, int32_t* index,
+                           void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Rows index[b, h, 0 .. keep - 1] of every kv head of a cache (p) as rows 0 .. keep - 1 of another one (to: its kv_capacity and kv strides, the same batch, kv
+ * heads and head_dim; the same block_len).  A block's scale is the largest that its rows had; rows of smaller scales are rounded to it (without an error
+ * but for elements that fall below 2^-6 of it).  Rows of `to` behind them keep their codes.  index: int32 [batch, n_kv_heads, keep]; any will do: a row may come
+ * twice, an entry outside [0, kv_capacity) gives a row of zeros.  weights, kept_weights: the sums move along, [batch, n_kv_heads, kv_capacity] of either
+ * cache; both or neither NULL.  The two caches, and the two sums, may not share memory (SLIMPIPE_EINVAL_RANGE). */
+int slimpipe_attn_kv8_gather(const slimpipe_attn_params* p, int32_t block_len, const int32_t* index, int64_t keep, const void* k_codes,
+                             const void* k_scales, const void* v_codes, const void* v_scales, const float* weights, const slimpipe_attn_params* to,
+                             void* to_k_codes, void* to_k_scales, void* to_v_codes, void* to_v_scales, float* kept_weights, void* hip_stream);
+
 /* Norm of every head of queries and keys, and the rotation of pairs of its elements by the row's position, in one pass: what a slice's projections
  * go through before the attention calls.  For a head x of a row at position t
  *     y = x / sqrt(mean(x^2) + eps) * weight;  of the first rotate_dim elements the pairs (i, i + rotate_dim / 2), or (2 i, 2 i + 1) when

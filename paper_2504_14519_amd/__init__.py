@@ -8,5 +8,7 @@ from .binding import (  # noqa: F401
     slimpipe_attn_block_means, slimpipe_attn_block_select, slimpipe_attn_block_workspace_bytes, slimpipe_attn_block_fwd, slimpipe_attn_block_bwd,
     KvCache4, slimpipe_attn_kv4_store, slimpipe_attn_kv4_load, slimpipe_attn_kv4_workspace_bytes, slimpipe_attn_fwd_kv4,
     KvCache8, slimpipe_attn_kv8_store, slimpipe_attn_kv8_load, slimpipe_attn_kv8_workspace_bytes, slimpipe_attn_fwd_kv8,
+    slimpipe_attn_kv8_weights, slimpipe_attn_kv8_weights_workspace_bytes, slimpipe_attn_kv8_keep, slimpipe_attn_kv8_keep_workspace_bytes,
+    slimpipe_attn_kv8_gather,
     RotateParams, slimpipe_attn_norm_rotate, slimpipe_attn_norm_rotate_bwd, slimpipe_attn_norm_rotate_workspace_bytes,
 )

@@ -133,6 +133,16 @@ def _load():
     L.slimpipe_attn_kv8_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_fwd_kv8.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_fwd_kv8.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_weights_workspace_bytes.argtypes = [P, i32, szp]
+    L.slimpipe_attn_kv8_weights_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_weights.argtypes = [P, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_kv8_weights.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_keep_workspace_bytes.argtypes = [i32, i64, i64, szp]
+    L.slimpipe_attn_kv8_keep_workspace_bytes.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_keep.argtypes = [vp, i32, i64, i64, i64, i64, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_kv8_keep.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_gather.argtypes = [P, i32, vp, i64, vp, vp, vp, vp, vp, P, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_gather.restype = ctypes.c_int
     R = ctypes.POINTER(RotateParams)
     L.slimpipe_attn_norm_rotate.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_norm_rotate.restype = ctypes.c_int
@@ -785,6 +795,97 @@ def slimpipe_attn_fwd_kv8(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
     _check(lib.slimpipe_attn_fwd_kv8(ctypes.byref(p), cache.block_len, q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(),
                                      *_ws(workspace), _stream()), "slimpipe_attn_fwd_kv8")
     return out, lse
+
+
+def _check_weights(name, x, shape):
+    if x.dtype is not torch.float32 or x.shape != shape or not x.is_contiguous():
+        raise SlimpipeError("%s must be contiguous float32 [batch, kv heads, capacity of the cache]" % name)
+
+
+def _weights_ws(p, block_len):
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_kv8_weights_workspace_bytes(ctypes.byref(p), block_len, ctypes.byref(n)), "kv8_weights_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_kv8_weights_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
+    """Bytes of workspace that slimpipe_attn_kv8_weights of these tensors needs (may be 0)."""
+    return _weights_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16), cache.block_len)
+
+
+def slimpipe_attn_kv8_weights(q_slice, cache, lse, q_offset, kv_begin, kv_end, causal=True, scale=None, weights=None, previous=None, decay=1.0,
+                              workspace=None):
+    """-> weights [B, Hkv, capacity] fp32: for the keys of [kv_begin, kv_end) decay * previous (None: 0; may be weights itself) and the attention weights of the
+    slice's rows and their heads, by the lse that their attention returned; other entries stay as they are (zero where the call allocates)."""
+    shape = q_slice.shape
+    _check_rows("q_slice", q_slice, shape)
+    _check_lse(lse, shape)
+    p = _cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, scale, BF16)
+    sums = (p.batch, p.n_kv_heads, p.kv_capacity)
+    if weights is None:
+        weights = torch.zeros(sums, device=q_slice.device, dtype=torch.float32)
+    _check_weights("weights", weights, sums)
+    if previous is not None:
+        _check_weights("previous", previous, sums)
+    if workspace is None:
+        workspace = torch.empty(_weights_ws(p, cache.block_len), device=q_slice.device, dtype=torch.uint8)
+    _check_workspace(workspace)
+    _check_device(q_slice, lse, weights, weights if previous is None else previous, workspace, cache.k_codes, cache.k_scales)
+    _check(lib.slimpipe_attn_kv8_weights(ctypes.byref(p), cache.block_len, q_slice.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(),
+                                         lse.data_ptr(), _ptr(previous), decay, weights.data_ptr(), *_ws(workspace), _stream()), "slimpipe_attn_kv8_weights")
+    return weights
+
+
+def slimpipe_attn_kv8_keep_workspace_bytes(weights, rows, keep):
+    """Bytes of workspace that slimpipe_attn_kv8_keep needs (may be 0)."""
+    n = ctypes.c_size_t(0)
+    _check(lib.slimpipe_attn_kv8_keep_workspace_bytes(weights.shape[0] * weights.shape[1], rows, keep, ctypes.byref(n)), "kv8_keep_workspace_bytes")
+    return n.value
+
+
+def slimpipe_attn_kv8_keep(weights, rows, keep, recent=0, index=None, workspace=None):
+    """-> index [B, Hkv, keep] int32, ascending: of the first `rows` rows of every kv head the `recent` last ones and the others with the largest weights [B,
+    Hkv, capacity], equal ones the lower index first."""
+    if weights.dim() != 3 or weights.dtype is not torch.float32 or not weights.is_contiguous():
+        raise SlimpipeError("weights must be contiguous float32 [batch, kv heads, capacity of the cache]")
+    B, H, N = weights.shape
+    if index is None:
+        index = torch.empty((B, H, max(keep, 0)), device=weights.device, dtype=torch.int32)
+    if index.dtype is not torch.int32 or index.shape != (B, H, keep) or not index.is_contiguous():
+        raise SlimpipeError("index must be contiguous int32 [batch, kv heads, keep]")
+    if workspace is None:
+        workspace = torch.empty(slimpipe_attn_kv8_keep_workspace_bytes(weights, rows, keep), device=weights.device, dtype=torch.uint8)
+    _check_workspace(workspace)
+    _check_device(weights, index, workspace)
+    _check(lib.slimpipe_attn_kv8_keep(weights.data_ptr(), B * H, N, rows, keep, recent, index.data_ptr(), *_ws(workspace), _stream()),
+           "slimpipe_attn_kv8_keep")
+    return index
+
+
+def slimpipe_attn_kv8_gather(cache, index, kept, weights=None, kept_weights=None):
+    """Rows index [B, Hkv, keep] (int32) of every kv head of a KvCache8 become rows 0 .. keep - 1 of the KvCache8 `kept`; with them the sums weights [B, Hkv,
+    capacity of cache], where given, those of kept_weights [B, Hkv, capacity of kept].  -> kept"""
+    (B, N, H, D), s_from = cache.layout()
+    (B2, N2, H2, D2), s_to = kept.layout()
+    if (B2, H2, D2, kept.block_len) != (B, H, D, cache.block_len):
+        raise SlimpipeError("the two caches must have the same batch, kv heads, head_dim and block_len")
+    if index.dtype is not torch.int32 or index.dim() != 3 or index.shape[:2] != (B, H) or not index.is_contiguous():
+        raise SlimpipeError("index must be contiguous int32 [batch, kv heads, keep]")
+    sums = []
+    if (weights is None) != (kept_weights is None):
+        raise SlimpipeError("weights and kept_weights: both or neither")
+    if weights is not None:
+        _check_weights("weights", weights, (B, H, N))
+        _check_weights("kept_weights", kept_weights, (B, H, N2))
+        sums = [weights, kept_weights]
+    _check_device(index, *sums, *cache[:4], *kept[:4])
+    one = (H * D, H * D, D)
+    p = AttnParams(B, 1, H, H, D, 1, N, 0, 0, 0, 1.0, BF16, *one, *s_from, *one, *one)
+    to = AttnParams(B, 1, H, H, D, 1, N2, 0, 0, 0, 1.0, BF16, *one, *s_to, *one, *one)
+    _check(lib.slimpipe_attn_kv8_gather(ctypes.byref(p), cache.block_len, index.data_ptr() or None, index.shape[2], *_cache_ptrs(cache), _ptr(weights),
+                                        ctypes.byref(to), *_cache_ptrs(kept), _ptr(kept_weights), _stream())
+           if index.shape[2] > 0 else 0, "slimpipe_attn_kv8_gather")
+    return kept
 
 
 def _rotate_params(q, k, weights, frequencies, position, eps, interleaved, q_out, k_out, q_out_dtype=torch.bfloat16, k_out_dtype=torch.bfloat16):

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslimpipe_attn.so")
 SOURCES = ["api.hip", "attn_fwd.hip", "attn_bwd.hip", "attn_small.hip", "attn_aux.hip",
            "block_api.hip", "block_select.hip", "block_fwd.hip", "block_bwd.hip", "part_merge.hip",
-           "kv4_api.hip", "kv4.hip", "rotate_api.hip", "rotate.hip", "kv8_api.hip", "kv8.hip"]
+           "kv4_api.hip", "kv4.hip", "rotate_api.hip", "rotate.hip", "kv8_api.hip", "kv8.hip",
+           "kv8_evict.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffast-math", "-fno-finite-math-only",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]

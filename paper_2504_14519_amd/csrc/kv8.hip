@@ -4,34 +4,10 @@
 // converts such numbers with their scale in one instruction, two at a time, exactly, to bf16, so that the attention below is the bf16 one on
 // converted tiles.  The scale is a power of two because the rows of a block come one after the other: when a larger one comes, those that are there
 // move to the larger scale without an error (but for elements below 2^-6 of it), which another factor would not allow.
-#include "kv8.hpp"
+#include "kv8_values.hpp"
 #include "row_tile.hpp"
 
 namespace slimpipe {
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-
-SP_DEV float kv8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
-SP_DEV int64_t kv8_scale_at(const Kv8Cache& c, int64_t b, int64_t row, int h) { return (b * c.blocks + (row >> c.shift)) * c.n_kv_heads + h; }
-
-// 8 elements (8 bytes of codes) -> bf16, and back
-SP_DEV bf16x8 kv8_values(uint32_t lo, uint32_t hi, float scale) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  bf16x8 r;
-  r[0] = a[0]; r[1] = a[1]; r[2] = b[0]; r[3] = b[1]; r[4] = c[0]; r[5] = c[1]; r[6] = d[0]; r[7] = d[1];
-  return r;
-}
-SP_DEV u32x2 kv8_codes(bf16x8 x, float scale) {
-  typedef short s16x2 __attribute__((ext_vector_type(2)));
-  s16x2 lo = {0, 0}, hi = {0, 0};
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_shufflevector(x, x, 0, 1), scale, false);
-  lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_shufflevector(x, x, 2, 3), scale, true);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_shufflevector(x, x, 4, 5), scale, false);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_shufflevector(x, x, 6, 7), scale, true);
-  return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
-}
 
 // ------------------------------------------------------------------------------------ store, load
 // Largest magnitude (bf16 bits) of 8 elements, two at a time; FINITE_ONLY: among those that are neither infinite nor NaN.
@@ -311,7 +287,6 @@ constexpr size_t kv8_few_lds_bytes() {
   constexpr size_t tiles = (size_t)4 * 32 * D * 2, out = (size_t)4 * 16 * SETS * (kOutRow<D> + 2) * 4;
   return tiles > out ? tiles : out;
 }
-constexpr int kv8_heads_wg(int n_kv_heads) { return n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 ? 2 : 1; }
 template <int D, int SETS>
 __global__ __launch_bounds__(256, 2) void kv8_few_kernel(const Kv8Args a) {
   constexpr int NP = D / 64, W = 2 * NP, DEPTH = 2, DB = D / 16;      // pieces of 16 bytes of a lane's row (two matrix steps each), output blocks

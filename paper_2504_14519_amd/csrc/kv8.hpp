@@ -45,12 +45,12 @@ struct Kv8WeightArgs {
   float* weights;                // the same
   float decay;
   int32_t batch, s_q, n_q_heads, group, causal;
-  int64_t capacity, q_offset, kv_begin, kv_end, seen_end;      // keys of [seen_end, kv_end) are seen by no row
+  int64_t capacity, q_offset, kv_begin, kv_end;
   float scale_log2e;
   int64_t q_stride_b, q_stride_s, q_stride_h;
-  int32_t n_parts;               // row ranges of part_rows rows of a plane, a workgroup each
-  int32_t part_rows;
-  float* part;                   // [n_parts][batch, n_kv_heads][keys], n_parts > 1
+  int32_t n_parts;               // few rows: key ranges of part_keys keys; else: parts of a plane's rows, a workgroup each for every 256 keys
+  int64_t part_keys;
+  float* part;                   // [n_parts][batch, n_kv_heads][keys], slices with n_parts > 1
 };
 
 struct Kv8KeepArgs {
@@ -58,14 +58,13 @@ struct Kv8KeepArgs {
   int32_t* index;                // [planes][keep]
   int64_t capacity;
   int32_t planes, rows, keep, recent;
-  uint32_t* work;                // several workgroups a plane: histograms and counts (keep_work_words a plane)
 };
 
 struct Kv8GatherArgs {
   Kv8Cache from, to;
   const int32_t* index;          // [batch, n_kv_heads, keep]
   const float* weights;          // [batch, n_kv_heads, capacity of from], or nullptr
-  float* kept_weights;           // [batch, n_kv_heads, weights_to_stride]
+  float* kept_weights;           // [batch, n_kv_heads, capacity of to]
   int64_t weights_stride, kept_weights_stride, from_rows;
   int32_t batch, keep;
 };
@@ -74,6 +73,12 @@ hipError_t launch_kv8_store(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv8_load(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, bool few, hipStream_t st);      // few: group * s_q <= kKv8FewRows
 constexpr int kKv8FewRows = 32;
+hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hipStream_t st);
+hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st);
+hipError_t launch_kv8_gather(const Kv8GatherArgs& a, int head_dim, hipStream_t st);
+// kv heads of a workgroup of the kernels of few rows, a wave (or two, or all four) each
+inline __host__ __device__ constexpr int kv8_heads_wg(int n_kv_heads) { return n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 ? 2 : 1; }
+constexpr int kv8_weight_keys() { return 256; }      // keys of a workgroup of the sums over a slice's rows
 hipError_t opt_in_kv8_kernels();
 
 }  // namespace slimpipe

@@ -1,4 +1,5 @@
 // C ABI of the key/value cache held in 8 bits: argument checks, workspace layout, launches.
+#include <math.h>
 #include <string.h>
 
 #include "host_common.hpp"
@@ -45,8 +46,7 @@ struct Kv8Plan {
 Kv8Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
   Kv8Plan plan{rows <= kKv8FewRows, 1, keys};
-  const int32_t heads_wg = p->n_kv_heads % 4 == 0 ? 4 : p->n_kv_heads % 2 == 0 ? 2 : 1;
-  const int64_t wgs = plan.few ? planes / heads_wg : planes * ((rows + 127) / 128), want = 2 * (int64_t)compute_units();
+  const int64_t wgs = plan.few ? planes / kv8_heads_wg(p->n_kv_heads) : planes * ((rows + 127) / 128), want = 2 * (int64_t)compute_units();
   const int64_t least = plan.few ? 256 : 512;      // keys of a part
   int64_t parts = plan.few ? want / wgs : (want + wgs - 1) / wgs;
   if (plan.few && parts >= 8) parts = parts / 8 * 8;      // (eight ranges at a time: ranges of the same keys share an XCD)
@@ -58,10 +58,63 @@ Kv8Plan plan_of(const slimpipe_attn_params* p) {
   }
   return plan;
 }
+// Sums of weights: key ranges of the kernel of few rows, or parts of a plane's rows, whose sums a second launch adds up.
+struct Kv8WeightPlan {
+  bool few;
+  int32_t parts;
+  int64_t part_keys;
+};
+Kv8WeightPlan weight_plan_of(const slimpipe_attn_params* p) {
+  const int64_t keys = p->kv_end - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
+  Kv8WeightPlan plan{rows <= kKv8FewRows, 1, keys};
+  if (plan.few) {
+    const int64_t want = 4 * (int64_t)compute_units(), wgs = planes / kv8_heads_wg(p->n_kv_heads);
+    int64_t parts = want / wgs;
+    if (parts >= 8) parts = parts / 8 * 8;                // (as in plan_of)
+    if (parts > keys / 256) parts = keys / 256;
+    if (parts > 1) {
+      plan.part_keys = ((keys + parts - 1) / parts + 31) / 32 * 32;
+      plan.parts = (int32_t)((keys + plan.part_keys - 1) / plan.part_keys);
+    }
+    return plan;
+  }
+  const int64_t wgs = planes * ((keys + kv8_weight_keys() - 1) / kv8_weight_keys()), want = 4 * (int64_t)compute_units();
+  int64_t parts = wgs > 0 ? (want + wgs - 1) / wgs : 1;
+  if (parts > rows / 256) parts = rows / 256;
+  if (parts > 64) parts = 64;
+  plan.parts = parts > 1 ? (int32_t)parts : 1;
+  return plan;
+}
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t out_bytes(const slimpipe_attn_params* p, const Kv8Plan& plan) { return up((size_t)p->batch * p->n_q_heads * p->s_q * plan.parts * p->head_dim * 4); }
 size_t bytes_of(const slimpipe_attn_params* p, const Kv8Plan& plan) {
   return plan.parts <= 1 ? 0 : out_bytes(p, plan) + up((size_t)p->batch * p->n_q_heads * p->s_q * plan.parts * 4);
+}
+size_t weight_bytes_of(const slimpipe_attn_params* p, const Kv8WeightPlan& plan) {
+  return plan.few || plan.parts <= 1 ? 0 : up((size_t)plan.parts * p->batch * p->n_kv_heads * (size_t)(p->kv_end - p->kv_begin) * 4);
+}
+// What the sums check beyond check_cache: workgroups that a launch numbers in 31 bits.
+int check_weights(const slimpipe_attn_params* p) {
+  const int64_t blocks = (p->kv_end - p->kv_begin + kv8_weight_keys() - 1) / kv8_weight_keys();
+  return blocks * p->batch * p->n_kv_heads * 64 < (int64_t)1 << 31 ? SLIMPIPE_OK : SLIMPIPE_EINVAL_SHAPE;
+}
+int check_keep(int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int64_t recent) {
+  if (planes < 1 || planes > 65535 || rows < 1 || rows > (int64_t)1 << 30 || capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;
+  return rows <= capacity && keep >= 1 && keep <= rows && recent >= 0 && recent <= keep ? SLIMPIPE_OK : SLIMPIPE_EINVAL_RANGE;
+}
+// A move writes its rows while others are still to be read: the two caches, and the two sums, may not share memory.
+bool overlap(const Kv8GatherArgs& a, int head_dim) {
+  const int64_t heads = a.to.n_kv_heads;
+  auto codes = [&](const uint8_t* x, const Kv8Cache& c, int64_t rows) { return span_of(x, 1, a.batch, rows, heads, head_dim, c.stride_b, c.stride_s, c.stride_h); };
+  auto bytes = [](const void* x, int64_t n) { return span_of(x, 1, 1, 1, 1, n, 1, 1, 1); };
+  const Span from[] = {codes(a.from.k.codes, a.from, a.from_rows), codes(a.from.v.codes, a.from, a.from_rows), bytes(a.from.k.scales, a.batch * a.from.blocks * heads),
+                       bytes(a.from.v.scales, a.batch * a.from.blocks * heads), bytes(a.weights, a.weights ? 4 * a.batch * heads * a.weights_stride : 0)};
+  const Span to[] = {codes(a.to.k.codes, a.to, a.keep), codes(a.to.v.codes, a.to, a.keep), bytes(a.to.k.scales, a.batch * a.to.blocks * heads),
+                     bytes(a.to.v.scales, a.batch * a.to.blocks * heads), bytes(a.kept_weights, a.kept_weights ? 4 * a.batch * heads * a.kept_weights_stride : 0)};
+  for (const Span& x : from)
+    for (const Span& y : to)
+      if (share_memory(x, y)) return true;
+  return false;
 }
 
 int status(hipError_t e) { return e == hipSuccess ? SLIMPIPE_OK : SLIMPIPE_ELAUNCH; }
@@ -161,6 +214,96 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
   m.out = out; m.lse = lse;
   m.o_stride_b = p->o_stride_b; m.o_stride_s = p->o_stride_s; m.o_stride_h = p->o_stride_h;
   return status(launch_part_merge(m, p->head_dim, st));
+}
+
+int slimpipe_attn_kv8_weights_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes) {
+  if (!bytes) return SLIMPIPE_EINVAL_NULL;
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_weights(p);
+  if (rc != SLIMPIPE_OK) return rc;
+  *bytes = weight_bytes_of(p, weight_plan_of(p));
+  return SLIMPIPE_OK;
+}
+
+int slimpipe_attn_kv8_weights(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales, const float* lse,
+                              const float* previous, float decay, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!q_slice || !lse || !weights) return SLIMPIPE_EINVAL_NULL;
+  rc = check_operands(k_codes, k_scales, k_codes, k_scales);
+  if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_weights(p);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!isfinite(decay)) return SLIMPIPE_EINVAL_SHAPE;
+  if (!aligned16(q_slice) || !aligned4(lse) || !aligned4(previous) || !aligned4(weights)) return SLIMPIPE_EINVAL_ALIGN;
+  const Kv8WeightPlan plan = weight_plan_of(p);
+  const size_t need = weight_bytes_of(p, plan);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return SLIMPIPE_EWORKSPACE;
+  if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
+  if (p->kv_begin == p->kv_end) return SLIMPIPE_OK;
+  Kv8WeightArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = static_cast<const __bf16*>(q_slice);
+  a.cache = cache_of(p, block_len, k_codes, k_scales, nullptr, nullptr);
+  a.lse = lse; a.previous = previous; a.weights = weights; a.decay = decay;
+  a.batch = p->batch; a.s_q = p->s_q; a.n_q_heads = p->n_q_heads; a.group = p->n_q_heads / p->n_kv_heads; a.causal = p->causal;
+  a.capacity = p->kv_capacity; a.q_offset = p->q_offset; a.kv_begin = p->kv_begin; a.kv_end = p->kv_end;
+  a.scale_log2e = p->scale * 1.4426950408889634f;
+  a.q_stride_b = p->q_stride_b; a.q_stride_s = p->q_stride_s; a.q_stride_h = p->q_stride_h;
+  a.n_parts = plan.parts; a.part_keys = plan.part_keys;
+  a.part = static_cast<float*>(workspace);
+  if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
+  return status(launch_kv8_weights(a, p->head_dim, plan.few, static_cast<hipStream_t>(hip_stream)));
+}
+
+int slimpipe_attn_kv8_keep_workspace_bytes(int32_t planes, int64_t rows, int64_t keep, size_t* bytes) {
+  if (!bytes) return SLIMPIPE_EINVAL_NULL;
+  const int rc = check_keep(planes, rows, rows, keep, 0);
+  if (rc == SLIMPIPE_OK) *bytes = 0;
+  return rc;
+}
+
+int slimpipe_attn_kv8_keep(const float* weights, int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int64_t recent, int32_t* index,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!weights || !index) return SLIMPIPE_EINVAL_NULL;
+  const int rc = check_keep(planes, capacity, rows, keep, recent);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!aligned4(weights) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
+  (void)workspace; (void)workspace_bytes;
+  Kv8KeepArgs a;
+  a.weights = weights; a.index = index; a.capacity = capacity;
+  a.planes = planes; a.rows = (int32_t)rows; a.keep = (int32_t)keep; a.recent = (int32_t)recent;
+  return status(launch_kv8_keep(a, static_cast<hipStream_t>(hip_stream)));
+}
+
+int slimpipe_attn_kv8_gather(const slimpipe_attn_params* p, int32_t block_len, const int32_t* index, int64_t keep, const void* k_codes, const void* k_scales,
+                             const void* v_codes, const void* v_scales, const float* weights, const slimpipe_attn_params* to, void* to_k_codes,
+                             void* to_k_scales, void* to_v_codes, void* to_v_scales, float* kept_weights, void* hip_stream) {
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc == SLIMPIPE_OK) rc = slimpipe_attn_validate(to, 0);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (!index || (weights == nullptr) != (kept_weights == nullptr)) return SLIMPIPE_EINVAL_NULL;
+  rc = check_operands(k_codes, k_scales, v_codes, v_scales);
+  if (rc == SLIMPIPE_OK) rc = check_operands(to_k_codes, to_k_scales, to_v_codes, to_v_scales);
+  if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
+  if (rc == SLIMPIPE_OK) rc = check_cache(to, block_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  if (p->batch != to->batch || p->n_kv_heads != to->n_kv_heads || p->head_dim != to->head_dim) return SLIMPIPE_EINVAL_SHAPE;
+  if (keep < 0 || keep > to->kv_capacity) return SLIMPIPE_EINVAL_RANGE;
+  if (!rows_fit(p, keep)) return SLIMPIPE_EINVAL_SHAPE;
+  if (!aligned4(index) || !aligned4(weights) || !aligned4(kept_weights)) return SLIMPIPE_EINVAL_ALIGN;
+  if (keep == 0) return SLIMPIPE_OK;
+  Kv8GatherArgs a;
+  memset(&a, 0, sizeof(a));
+  a.from = cache_of(p, block_len, k_codes, k_scales, v_codes, v_scales);
+  a.to = cache_of(to, block_len, to_k_codes, to_k_scales, to_v_codes, to_v_scales);
+  a.index = index; a.weights = weights; a.kept_weights = kept_weights;
+  a.weights_stride = p->kv_capacity; a.kept_weights_stride = to->kv_capacity;
+  a.from_rows = p->kv_capacity;
+  a.batch = p->batch; a.keep = (int32_t)keep;
+  if (overlap(a, p->head_dim)) return SLIMPIPE_EINVAL_RANGE;
+  return status(launch_kv8_gather(a, p->head_dim, static_cast<hipStream_t>(hip_stream)));
 }
 
 }  // extern "C"

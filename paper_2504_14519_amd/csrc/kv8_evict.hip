@@ -1,0 +1,463 @@
+// Eviction from a key/value cache in 8 bits: the attention weight that every key gathers, the choice of the rows to keep, and the move of these rows to another
+// cache.
+#include "kv8_values.hpp"
+#include "row_tile.hpp"
+
+namespace slimpipe {
+
+// ------------------------------------------------------------------------------------ weights
+// weight_j = decay * previous_j + sum over the rows r of the kv head's query heads that see j of exp(scale q_r . k_j - lse_r): the scores once more, an exponential
+// and a sum, no second product.
+SP_DEV void put_weight(const Kv8WeightArgs& a, int64_t plane, int64_t key, float sum) {
+  const int64_t at = plane * a.capacity + key;
+  a.weights[at] = a.previous ? __builtin_fmaf(a.decay, a.previous[at], sum) : sum;
+}
+// lse of a row in log2 units, where exp2(score - that) is 0 for rows that saw nothing
+SP_DEV float row_norm(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// Tokens: at most 16 SETS rows of a plane.  S^T = K Q^T as in the attention of tokens (kv8.hip): codes go from memory to the matrix unit, a lane holds one row's
+// scores with four keys of 16, and the sum over the rows is one over 16 lanes.  A wave takes every fourth (second) step of 32 keys of its head, codes of the next DEPTH
+// steps under way.
+template <int D, int SETS>
+__global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8WeightArgs a) {
+  constexpr int NP = D / 64, W = 2 * NP, DEPTH = 4;
+  const Kv8Cache& kv = a.cache;
+  const int lane = threadIdx.x & 63, h4 = lane >> 4, ql = lane & 15, wave_u = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hw = kv8_heads_wg(kv.n_kv_heads), subs = 4 / hw, sub = wave_u / hw;
+  const int rows = a.group * a.s_q, head_sets = kv.n_kv_heads / hw, planes = a.batch * head_sets;
+  const int per = 8 * planes, first = (int)blockIdx.x / per * 8, i0 = (int)blockIdx.x % per, n = a.n_parts - first < 8 ? a.n_parts - first : 8;
+  const int part_i = first + i0 % n, plane = i0 / n;
+  if (plane >= planes) return;
+  const int b = plane / head_sets, hk = (plane - b * head_sets) * hw + wave_u % hw;
+  const int64_t plane_out = (int64_t)b * kv.n_kv_heads + hk;
+  const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
+  const int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
+  const int n_keys = hi > lo ? (int)(hi - lo) : 0, nt = (n_keys + 31) / 32;
+
+  bf16x8 q[SETS][W];
+  float norm[SETS];
+  int see_rel[SETS];
+#pragma unroll
+  for (int r = 0; r < SETS; ++r) {
+    const int rh = 16 * r + ql;
+    const PlaneRow my = plane_row(a.s_q, a.group, hk, rh < rows ? rh : rows - 1);
+    const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + 16 * h4;
+#pragma unroll
+    for (int j = 0; j < W; ++j) q[r][j] = *reinterpret_cast<const bf16x8*>(qp + 64 * (j / 2) + 8 * (j % 2));
+    norm[r] = rh < rows ? row_norm(a.lse[((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r]) : INFINITY;
+    const int64_t see = (a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1) - lo;
+    see_rel[r] = see < -1 ? -1 : (int)see;
+  }
+  int min_see = see_rel[0];
+#pragma unroll
+  for (int r = 1; r < SETS; ++r) min_see = min_see < see_rel[r] ? min_see : see_rel[r];
+
+  const int64_t base = (int64_t)b * kv.stride_b + (int64_t)hk * kv.stride_h + lo * kv.stride_s + 16 * h4;
+  struct Step { u32x4 k[2][NP]; uint32_t ks[2]; };
+  auto fetch = [&](Step& s, int t) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      int key = t * 32 + 16 * u + ql;
+      key = key < n_keys ? key : n_keys - 1;                     // (keys behind the last are not read)
+      const int64_t at = base + (int64_t)key * kv.stride_s;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) s.k[u][p] = *reinterpret_cast<const u32x4*>(kv.k.codes + at + 64 * p);
+      s.ks[u] = kv.k.scales[kv8_scale_at(kv, b, lo + key, hk)];
+    }
+  };
+  auto work = [&](Step& st, int t, int next) {
+    f32x4 s[SETS][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float ks = kv8_scale(st.ks[u]);
+#pragma unroll
+      for (int r = 0; r < SETS; ++r) s[r][u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const bf16x8 k8 = kv8_values(st.k[u][j / 2][j % 2 * 2], st.k[u][j / 2][j % 2 * 2 + 1], ks);
+#pragma unroll
+        for (int r = 0; r < SETS; ++r) s[r][u] = mfma16(k8, q[r][j], s[r][u]);
+      }
+    }
+    if (next < nt) fetch(st, next);
+    const bool masked = __builtin_amdgcn_ballot_w64(min_see < t * 32 + 31) != 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float sum[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int r = 0; r < SETS; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = exp2_fast(__builtin_fmaf(s[r][u][i], a.scale_log2e, -norm[r]));
+          sum[i] += masked && t * 32 + 16 * u + 4 * h4 + i > see_rel[r] ? 0.f : p;
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int w = 1; w < 16; w <<= 1) sum[i] += __shfl_xor(sum[i], w, 64);
+      const float mine = ql == 0 ? sum[0] : ql == 1 ? sum[1] : ql == 2 ? sum[2] : sum[3];
+      const int key = t * 32 + 16 * u + 4 * h4 + ql;
+      if (ql < 4 && key < n_keys) put_weight(a, plane_out, lo + key, mine);
+    }
+  };
+  if (sub >= nt) return;
+  Step s[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i)
+    if (sub + i * subs < nt) fetch(s[i], sub + i * subs);
+  for (int t = sub; t < nt; t += DEPTH * subs)
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i)
+      if (t + i * subs < nt) work(s[i], t + i * subs, t + (i + DEPTH) * subs);
+}
+
+// Slices: a workgroup has 256 keys, 64 a wave, converted once and kept in registers, and walks the rows that see any of them (head by head, without the
+// rows before its first key), or one part of them, in tiles of 64 through a ring of three in LDS.
+//   S^T = K Q^T        A = K in registers, B = rows of Q from LDS: a lane has one row and 32 keys of a block of 32 rows
+//   sums               p = exp2(c s - norm) added in place: the lane's sums over its rows, over the lanes at the end
+// The scores of a block of 32 rows are computed while the exponentials of the block before are taken, instruction by instruction.
+constexpr int kWeightKeys = kv8_weight_keys(), kWeightRows = 64;
+template <int D>
+constexpr size_t kv8_weights_lds_bytes() { return (size_t)3 * kWeightRows * (D * 2 + 4); }
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs a) {
+  constexpr int KS = D / 16, TILE = kWeightRows * D * 2, NC = D / 8, PASSES = kWeightRows / (4 * (64 / NC));      // copies of a wave a tile
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const Kv8Cache& kv = a.cache;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int key_blocks = (int)((a.kv_end - a.kv_begin + kWeightKeys - 1) / kWeightKeys);
+  const int planes = a.batch * kv.n_kv_heads;
+  const int item = xcd_run(blockIdx.x, key_blocks * planes * a.n_parts);      // (plane, part, key block): an XCD's workgroups read the same rows
+  if (item < 0) return;
+  const int pp = item / key_blocks, kb_i = item - pp * key_blocks, plane = pp / a.n_parts, part_i = pp - plane * a.n_parts;
+  const int b = plane / kv.n_kv_heads, hk = plane - b * kv.n_kv_heads;
+  const int64_t key0 = a.kv_begin + (int64_t)kb_i * kWeightKeys, wave_key0 = key0 + 64 * wave_u;
+
+  // rows r_min .. s_q - 1 of every head of the group see a key of the workgroup; this part's tiles of them
+  int64_t r_first = a.causal ? key0 - a.q_offset : 0;
+  r_first = r_first < 0 ? 0 : r_first;
+  const int r_min = r_first < a.s_q ? (int)r_first : a.s_q, vis = a.s_q - r_min;
+  const int rows = vis * a.group, tiles = (rows + kWeightRows - 1) / kWeightRows;
+  const int t0 = (int)((int64_t)tiles * part_i / a.n_parts), t1 = (int)((int64_t)tiles * (part_i + 1) / a.n_parts);
+
+  f32x16 acc[2];
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[kb][i] = 0.f;
+
+  if (t0 < t1) {
+    const unsigned lds = lds_addr(smem);
+    const bf16_t* const q_base = a.q + (int64_t)b * a.q_stride_b + (int64_t)hk * a.group * a.q_stride_h;
+    const float* const lse = a.lse + ((int64_t)b * a.n_q_heads + (int64_t)hk * a.group) * a.s_q;
+    const uint32_t row_bytes = (uint32_t)a.q_stride_s * 2;
+    // Row rh of those that the workgroup walks is row r_min + rh % vis of head rh / vis.  A tile of one head, most of them, is copied from a uniform base.
+    // The rows' lse come along, behind the ring.
+    constexpr int RPP = 64 / NC;                                      // rows of a copy instruction
+    auto copy_tile = [&](int t) {
+      const unsigned to = lds + (t % 3) * TILE, to_lse = lds + 3 * TILE + (t % 3) * kWeightRows * 4;
+      const int rh0 = t * kWeightRows, h0 = __builtin_amdgcn_readfirstlane((int)((unsigned)rh0 / (unsigned)vis)), r0 = rh0 - h0 * vis;
+      if (r0 + kWeightRows <= vis) {
+        const bf16_t* src = q_base + (int64_t)h0 * a.q_stride_h + (int64_t)(r_min + r0) * a.q_stride_s;
+        dma4(uniform_ptr(lse + (int64_t)h0 * a.s_q + r_min + r0), (uint32_t)lane * 4, __builtin_amdgcn_readfirstlane(to_lse));
+#pragma unroll
+        for (int n = 0; n < PASSES; ++n) WaveDma<D, kWeightRows>::copy_pass(to, uniform_ptr(src), row_bytes, kWeightRows, lane, wave_u * PASSES + n);
+        return;
+      }
+      auto at = [&](int rh, int& hl) {
+        rh = rh < rows ? rh : rows - 1;
+        hl = (int)((unsigned)rh / (unsigned)vis);
+        return rh - hl * vis + r_min;
+      };
+      int hl;
+      const int rl = at(rh0 + lane, hl);
+      dma4_at(lse + (int64_t)hl * a.s_q + rl, to_lse);
+#pragma unroll
+      for (int n = 0; n < PASSES; ++n) {
+        const int pass = wave_u * PASSES + n, r = at(rh0 + pass * RPP + lane / NC, hl);
+        dma16_at(q_base + (int64_t)hl * a.q_stride_h + (int64_t)r * a.q_stride_s + WaveDma<D, kWeightRows>::chunk_off(lane, pass) / 2, to + pass * 1024);
+      }
+    };
+    copy_tile(t0);
+    if (t0 + 1 < t1) copy_tile(t0 + 1);
+    bf16x8 k[2][KS];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+      int64_t key = wave_key0 + 32 * kb + (lane & 31);
+      key = key < a.kv_end ? key : a.kv_end - 1;                  // (keys behind the last are not read)
+      const float unit = kv8_scale(kv.k.scales[kv8_scale_at(kv, b, key, hk)]);
+      const uint8_t* p = kv.k.codes + (int64_t)b * kv.stride_b + key * kv.stride_s + (int64_t)hk * kv.stride_h + 8 * g;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x2 c = *reinterpret_cast<const u32x2*>(p + 16 * ks);
+        k[kb][ks] = kv8_values(c[0], c[1], unit);
+      }
+    }
+    RpBase<D> lo_q;
+    lo_q.init(lane, (int)lds);
+    // norm and last visible key (relative to the wave's first, less the lane's 4 g) of the lane's row in a block of 32
+    const int64_t rel = a.q_offset - wave_key0 + r_min;
+    auto row_of = [&](int block, float& norm, int& see) {
+      const int rh = block * 32 + (lane & 31), rc = rh < rows ? rh : rows - 1;
+      const float x = *lds_ptr<float>((int)lds + 3 * TILE + (block / 2 % 3) * kWeightRows * 4 + (block & 1) * 128 + (lane & 31) * 4, 0);
+      norm = rh < rows ? row_norm(x) : INFINITY;
+      const int64_t far = rel + (int)((unsigned)rc % (unsigned)vis);
+      see = (!a.causal || far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
+    };
+    f32x16 s[2][2];
+    float norm[2];
+    int see[2];
+    // exponential and sum of element e (of 32) of the scores of block x
+    auto take = [&](int x, int e, bool masked) {
+      const int kb = e / 16, i = e % 16;
+      float p = exp2_fast(__builtin_fmaf(s[x][kb][i], a.scale_log2e, -norm[x]));
+      if (masked) p = 32 * kb + 8 * (i >> 2) + (i & 3) <= see[x] ? p : 0.f;
+      acc[kb][i] += p;
+    };
+    auto is_masked = [&](int x) { return __builtin_amdgcn_ballot_w64(see[x] < 63 - 4 * g) != 0; };
+    // scores of block x from the rows at lo_q in LDS; those of the other block taken meanwhile
+    auto block = [&](auto x_, bool with_other) {
+      constexpr int x = decltype(x_)::value;
+      const f32x16 zero = {0};
+      const bool masked = with_other && is_masked(1 - x);
+      constexpr int LOOK = 3;
+      bf16x8 buf[LOOK + 1];
+      if (!with_other || masked) {
+        matrix_run<2 * KS, LOOK>([&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % (LOOK + 1)] = lds_rp<D>(lo_q, m / 2, 0); },
+                                 [&](auto m) { s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % (LOOK + 1)], m < 2 ? zero : s[x][m % 2]); });
+        if (masked)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) take(1 - x, e, true);
+      } else {
+        matrix_run<2 * KS, LOOK>([&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % (LOOK + 1)] = lds_rp<D>(lo_q, m / 2, 0); },
+                                 [&](auto m) {
+                                   s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % (LOOK + 1)], m < 2 ? zero : s[x][m % 2]);
+                                   constexpr int E = 32 / (2 * KS);
+#pragma unroll
+                                   for (int e = 0; e < E; ++e) take(1 - x, m * E + e, false);
+                                 });
+      }
+    };
+    for (int t = t0; t < t1; ++t) {
+      // this wave's copies of tile t have landed when at most those of tile t + 1 are under way
+      if (t + 1 < t1) wait_copies<PASSES + 1>();
+      else wait_async();
+      __syncthreads();
+      if (t + 2 < t1) copy_tile(t + 2);
+      lo_q.off0 += ((t % 3) * TILE);
+      block(std::integral_constant<int, 0>{}, t > t0);
+      row_of(2 * t, norm[0], see[0]);
+      lo_q.off0 += 32 * D * 2;
+      block(std::integral_constant<int, 1>{}, true);
+      row_of(2 * t + 1, norm[1], see[1]);
+      lo_q.off0 -= 32 * D * 2 + ((t % 3) * TILE);
+    }
+    const bool masked = is_masked(1);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) take(1, e, masked);
+  }
+  // over the 32 rows of a half-wave
+  __syncthreads();
+  float* const out = reinterpret_cast<float*>(smem) + 64 * wave_u;
+#pragma unroll
+  for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = acc[kb][i];
+#pragma unroll
+      for (int w = 1; w < 32; w <<= 1) v += __shfl_xor(v, w, 64);
+      if ((lane & 31) == 0) out[32 * kb + 8 * (i >> 2) + 4 * g + (i & 3)] = v;
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int64_t key = wave_key0 + lane;
+  if (key >= a.kv_end) return;
+  if (a.n_parts > 1) a.part[((int64_t)part_i * planes + plane) * (a.kv_end - a.kv_begin) + key - a.kv_begin] = out[lane];
+  else put_weight(a, plane, key, out[lane]);
+}
+
+// Parts in their order.
+__global__ __launch_bounds__(256) void kv8_weights_sum_kernel(const Kv8WeightArgs a) {
+  const int64_t keys = a.kv_end - a.kv_begin, planes = (int64_t)a.batch * a.cache.n_kv_heads, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= keys * planes) return;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < a.n_parts; ++p) sum += a.part[p * planes * keys + i];
+  put_weight(a, i / keys, a.kv_begin + i % keys, sum);
+}
+
+template <int D>
+static hipError_t launch_weights_t(const Kv8WeightArgs& a, bool few, hipStream_t st) {
+  const int64_t keys = a.kv_end - a.kv_begin, planes = (int64_t)a.batch * a.cache.n_kv_heads;
+  if (few) {
+    const dim3 grid((unsigned)(a.n_parts * (planes / kv8_heads_wg(a.cache.n_kv_heads)))), block(256);
+    if (a.group * a.s_q <= 16) hipLaunchKernelGGL((kv8_weights_few_kernel<D, 1>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv8_weights_few_kernel<D, 2>), grid, block, 0, st, a);
+    return hipGetLastError();
+  }
+  const int64_t items = (keys + kWeightKeys - 1) / kWeightKeys * planes * a.n_parts;
+  hipLaunchKernelGGL(kv8_weights_kernel<D>, dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), kv8_weights_lds_bytes<D>(), st, a);
+  if (a.n_parts > 1) hipLaunchKernelGGL(kv8_weights_sum_kernel, dim3((unsigned)((keys * planes + 255) / 256)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hipStream_t st) {
+  return head_dim == 128 ? launch_weights_t<128>(a, few, st) : launch_weights_t<64>(a, few, st);
+}
+
+// ------------------------------------------------------------------------------------ keep
+// The rows of a plane that are kept: the `recent` last ones and those of the others with the largest weights.  A radix selection finds the smallest weight that is
+// taken and how many rows of exactly that weight are; a last walk writes the indices in order.
+constexpr int kKeepThreads = 1024;
+
+// A number that orders as the weight does: NaN behind everything, both zeros alike
+SP_DEV uint32_t weight_order(float w) {
+  uint32_t u = __float_as_uint(w);
+  if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
+  if (u == 0x80000000u) u = 0u;
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// Inclusive sum over the workgroup's threads; `total` of all.  Uses `wave_sums` (16 words) and two barriers.
+SP_DEV uint32_t keep_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_up((int)v, w, 64);
+    v += lane >= w ? o : 0u;
+  }
+  __syncthreads();
+  if (lane == 63) wave_sums[wave] = v;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kKeepThreads / 64; ++w) {
+    before += w < wave ? wave_sums[w] : 0u;
+    total += wave_sums[w];
+  }
+  return v + before;
+}
+
+__global__ __launch_bounds__(kKeepThreads) void kv8_keep_kernel(const Kv8KeepArgs a) {
+  __shared__ uint32_t hist[2048], wave_sums[kKeepThreads / 64], found[2];
+  const int tid = threadIdx.x;
+  const float* const w = a.weights + (int64_t)blockIdx.x * a.capacity;
+  int32_t* const out = a.index + (int64_t)blockIdx.x * a.keep;
+  const int others = a.rows - a.recent;
+  uint32_t need = (uint32_t)(a.keep - a.recent);      // of the others; then: of those with the leading bits found so far
+  uint32_t prefix = 0;                                // leading bits of the smallest weight that is taken
+  const bool all = need >= (uint32_t)others;
+  if (need > 0 && !all) {
+    constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = kShift[pass], bins = 1 << kBits[pass], above = shift + kBits[pass];
+      for (int i = tid; i < bins; i += kKeepThreads) hist[i] = 0;
+      __syncthreads();
+      for (int i = tid; i < others; i += kKeepThreads) {
+        const uint32_t u = weight_order(w[i]);
+        if (pass == 0 || (u >> above) == (prefix >> above)) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1u);
+      }
+      __syncthreads();
+      // the bin in which the need-th largest lies: thread t has bins from the top on
+      const int per = bins / kKeepThreads;            // 2, 2, 1
+      uint32_t mine[2] = {0, 0}, total;
+      for (int i = 0; i < per; ++i) mine[i] = hist[bins - 1 - (tid * per + i)];
+      const uint32_t upto = keep_scan(mine[0] + mine[1], wave_sums, total), ahead = upto - mine[0] - mine[1];
+      if (ahead < need && need <= upto) {
+        const int second = ahead + mine[0] < need;
+        found[0] = (uint32_t)(bins - 1 - (tid * per + second));
+        found[1] = need - ahead - (second ? mine[0] : 0u);
+      }
+      __syncthreads();
+      prefix |= found[0] << shift;
+      need = found[1];
+      __syncthreads();
+    }
+  }
+  // rows above `prefix`, and the first `need` ones equal to it, in order
+  const bool none = a.keep == a.recent;
+  uint32_t taken = 0, equal = 0;                      // so far
+  for (int base = 0; base < others; base += kKeepThreads) {
+    const int i = base + tid;
+    uint32_t above = 0, same = 0, total;
+    if (i < others && !none) {
+      const uint32_t u = all ? 1u : weight_order(w[i]);
+      above = all || u > prefix;
+      same = !all && u == prefix;
+    }
+    const uint32_t sums = keep_scan(above | same << 16, wave_sums, total);
+    // (rows equal to it that come before this one: those beyond `need` are not taken)
+    const uint32_t eq_before = equal + (sums >> 16) - same, eq_taken = eq_before < need ? eq_before : need;
+    const uint32_t eq_start = equal < need ? equal : need;
+    const bool take = above || (same && eq_before < need);
+    if (take) out[taken + (sums & 0xffffu) - above + eq_taken - eq_start] = i;
+    const uint32_t eq_all = equal + (total >> 16), eq_end = eq_all < need ? eq_all : need;
+    taken += (total & 0xffffu) + eq_end - eq_start;
+    equal = eq_all;
+  }
+  for (int i = tid; i < a.recent; i += kKeepThreads) out[a.keep - a.recent + i] = others + i;
+}
+hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(kv8_keep_kernel, dim3((unsigned)a.planes), dim3(kKeepThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------ gather
+// A block of kept rows of a head, keys (blockIdx.y = 0) or values: its scale is the largest that its rows had, rows of smaller scales are rounded to it.
+template <int D>
+__global__ __launch_bounds__(256) void kv8_gather_kernel(const Kv8GatherArgs a) {
+  constexpr int NP = D / 16;
+  __shared__ int32_t row[256];
+  __shared__ uint8_t was[256];
+  __shared__ uint32_t most[4];
+  const Kv8Cache &from = a.from, &to = a.to;
+  const int L = 1 << to.shift, tid = threadIdx.x;
+  const int64_t blocks = (a.keep + L - 1) / L, plane = blockIdx.x / blocks, blk = blockIdx.x - plane * blocks;
+  const int64_t b = plane / from.n_kv_heads;
+  const int h = (int)(plane - b * from.n_kv_heads), first = (int)blk * L, n = a.keep - first < L ? a.keep - first : L;
+  const bool keys = blockIdx.y == 0;
+  const Kv8Operand src = keys ? from.k : from.v, dst = keys ? to.k : to.v;
+  uint32_t byte = 0;
+  if (tid < n) {
+    const int32_t r = a.index[plane * a.keep + first + tid];
+    const bool there = r >= 0 && r < a.from_rows;      // (another entry is no row: zeros)
+    row[tid] = there ? r : -1;
+    byte = there ? src.scales[kv8_scale_at(from, b, r, h)] : 0u;
+    was[tid] = (uint8_t)byte;
+    if (keys && a.kept_weights) a.kept_weights[plane * a.kept_weights_stride + first + tid] = there ? a.weights[plane * a.weights_stride + r] : 0.f;
+  }
+#pragma unroll
+  for (int w = 1; w < 64; w <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)byte, w, 64);
+    byte = byte > o ? byte : o;
+  }
+  if ((tid & 63) == 0) most[tid >> 6] = byte;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) byte = byte > most[w] ? byte : most[w];
+  const float unit = kv8_scale(byte);
+  for (int i = tid; i < n * NP; i += 256) {
+    const int r = i / NP, c = i % NP;
+    u32x4 x = {0, 0, 0, 0};
+    if (row[r] >= 0) {
+      x = *reinterpret_cast<const u32x4*>(src.codes + b * from.stride_b + (int64_t)row[r] * from.stride_s + h * from.stride_h + 16 * c);
+      if (was[r] != byte) {
+        const float s = kv8_scale(was[r]);
+        const u32x2 lo = kv8_codes(kv8_values(x[0], x[1], s), unit), hi = kv8_codes(kv8_values(x[2], x[3], s), unit);
+        x = u32x4{lo[0], lo[1], hi[0], hi[1]};
+      }
+    }
+    *reinterpret_cast<u32x4*>(dst.codes + b * to.stride_b + (int64_t)(first + r) * to.stride_s + h * to.stride_h + 16 * c) = x;
+  }
+  if (tid == 0) dst.scales[(b * to.blocks + blk) * to.n_kv_heads + h] = (uint8_t)byte;
+}
+hipError_t launch_kv8_gather(const Kv8GatherArgs& a, int head_dim, hipStream_t st) {
+  const int64_t blocks = (a.keep + (1 << a.to.shift) - 1) >> a.to.shift;
+  const dim3 grid((unsigned)(blocks * a.batch * a.to.n_kv_heads), 2), block(256);
+  if (head_dim == 128) hipLaunchKernelGGL(kv8_gather_kernel<128>, grid, block, 0, st, a);
+  else hipLaunchKernelGGL(kv8_gather_kernel<64>, grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace slimpipe

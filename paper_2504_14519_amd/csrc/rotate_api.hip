@@ -20,10 +20,10 @@ int check(const slimpipe_rotate_params* p) {
   const int64_t far = (int64_t)1 << 52;      // (a position is a double on its way to an angle)
   if (p->position < 0 || p->position > far - p->rows) return SLIMPIPE_EINVAL_RANGE;
   if (p->n_q_heads > 0 && !(stride_ok(p->q_stride_b) && stride_ok(p->q_stride_s) && stride_ok(p->q_stride_h) && stride_ok(p->qo_stride_b) &&
-                            stride_ok(p->qo_stride_s) && stride_ok(p->qo_stride_h)))
+                            stride_ok(p->qo_stride_s) && stride_ok(p->qo_stride_h) && p->q_stride_h >= p->head_dim && p->qo_stride_h >= p->head_dim))
     return SLIMPIPE_EINVAL_STRIDE;
   if (p->n_kv_heads > 0 && !(stride_ok(p->k_stride_b) && stride_ok(p->k_stride_s) && stride_ok(p->k_stride_h) && stride_ok(p->ko_stride_b) &&
-                             stride_ok(p->ko_stride_s) && stride_ok(p->ko_stride_h)))
+                             stride_ok(p->ko_stride_s) && stride_ok(p->ko_stride_h) && p->k_stride_h >= p->head_dim && p->ko_stride_h >= p->head_dim))
     return SLIMPIPE_EINVAL_STRIDE;
   return SLIMPIPE_OK;
 }
