@@ -58,7 +58,13 @@ struct Kv8KeepArgs {
   int32_t* index;                // [planes][keep]
   int64_t capacity;
   int32_t planes, rows, keep, recent;
+  int32_t chunks;                // 0: a workgroup a plane; else one for every `chunk` rows, which leave their counts in `work`
+  int64_t chunk;
+  uint32_t* work;                // [planes][chunks * kKeepChunkWords + kKeepPlaneWords]
 };
+
+constexpr int kKeepChunkWords = 2048 + 2048 + 1024 + 1, kKeepPlaneWords = 4;
+constexpr int kKeepOneRows = 32 * 1024;      // most rows of a plane for one workgroup
 
 struct Kv8GatherArgs {
   Kv8Cache from, to;

@@ -102,6 +102,17 @@ int check_keep(int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int
   if (planes < 1 || planes > 65535 || rows < 1 || rows > (int64_t)1 << 30 || capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;
   return rows <= capacity && keep >= 1 && keep <= rows && recent >= 0 && recent <= keep ? SLIMPIPE_OK : SLIMPIPE_EINVAL_RANGE;
 }
+// Workgroups of 8192 rows, more where there would be more than 64 of them (each adds up the counts of all of its plane).
+struct KeepPlan {
+  int32_t chunks;
+  int64_t chunk;
+};
+KeepPlan keep_plan_of(int64_t rows) {
+  if (rows <= kKeepOneRows) return {0, 0};
+  const int64_t span = 8192, chunk = (rows + 64 * span - 1) / (64 * span) * span;
+  return {(int32_t)((rows + chunk - 1) / chunk), chunk};
+}
+size_t keep_bytes_of(int32_t planes, const KeepPlan& plan) { return plan.chunks ? (size_t)planes * ((size_t)plan.chunks * kKeepChunkWords + kKeepPlaneWords) * 4 : 0; }
 // A move writes its rows while others are still to be read: the two caches, and the two sums, may not share memory.
 bool overlap(const Kv8GatherArgs& a, int head_dim) {
   const int64_t heads = a.to.n_kv_heads;
@@ -260,7 +271,7 @@ int slimpipe_attn_kv8_weights(const slimpipe_attn_params* p, int32_t block_len, 
 int slimpipe_attn_kv8_keep_workspace_bytes(int32_t planes, int64_t rows, int64_t keep, size_t* bytes) {
   if (!bytes) return SLIMPIPE_EINVAL_NULL;
   const int rc = check_keep(planes, rows, rows, keep, 0);
-  if (rc == SLIMPIPE_OK) *bytes = 0;
+  if (rc == SLIMPIPE_OK) *bytes = keep_bytes_of(planes, keep_plan_of(rows));
   return rc;
 }
 
@@ -270,8 +281,12 @@ int slimpipe_attn_kv8_keep(const float* weights, int32_t planes, int64_t capacit
   const int rc = check_keep(planes, capacity, rows, keep, recent);
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned4(weights) || !aligned4(index)) return SLIMPIPE_EINVAL_ALIGN;
-  (void)workspace; (void)workspace_bytes;
+  const KeepPlan plan = keep_plan_of(rows);
+  const size_t need = keep_bytes_of(planes, plan);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return SLIMPIPE_EWORKSPACE;
+  if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
   Kv8KeepArgs a;
+  a.chunks = plan.chunks; a.chunk = plan.chunk; a.work = static_cast<uint32_t*>(workspace);
   a.weights = weights; a.index = index; a.capacity = capacity;
   a.planes = planes; a.rows = (int32_t)rows; a.keep = (int32_t)keep; a.recent = (int32_t)recent;
   return status(launch_kv8_keep(a, static_cast<hipStream_t>(hip_stream)));

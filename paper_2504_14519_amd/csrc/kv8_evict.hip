@@ -306,9 +306,11 @@ hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hi
 }
 
 // ------------------------------------------------------------------------------------ keep
-// The rows of a plane that are kept: the `recent` last ones and those of the others with the largest weights.  A radix selection finds the smallest weight that is
-// taken and how many rows of exactly that weight are; a last walk writes the indices in order.
-constexpr int kKeepThreads = 1024;
+// The rows of a plane that are kept: the `recent` last ones and those of the others with the largest weights.  A radix selection (11, 11 and 10 bits) finds the
+// smallest weight that is taken and how many rows of exactly that weight are; a last walk writes the indices in order.  Counts alone cross threads, so
+// that the order in which they run shows nowhere.
+constexpr int kKeepThreads = 1024, kKeepWaves = kKeepThreads / 64;
+constexpr int kKeepShift[3] = {21, 10, 0}, kKeepBins[3] = {2048, 2048, 1024};
 
 // A number that orders as the weight does: NaN behind everything, both zeros alike
 SP_DEV uint32_t weight_order(float w) {
@@ -317,8 +319,9 @@ SP_DEV uint32_t weight_order(float w) {
   if (u == 0x80000000u) u = 0u;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-// Inclusive sum over the workgroup's threads; `total` of all.  Uses `wave_sums` (16 words) and two barriers.
-SP_DEV uint32_t keep_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
+// Inclusive sum over the workgroup's threads, and the sum of all.  Two barriers.
+struct KeepScan { uint32_t upto, total; };
+SP_DEV KeepScan keep_scan(uint32_t v, uint32_t (&wave_sums)[kKeepWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int w = 1; w < 64; w <<= 1) {
@@ -328,78 +331,206 @@ SP_DEV uint32_t keep_scan(uint32_t v, uint32_t* wave_sums, uint32_t& total) {
   __syncthreads();
   if (lane == 63) wave_sums[wave] = v;
   __syncthreads();
-  uint32_t before = 0;
-  total = 0;
+  KeepScan s{v, 0};
 #pragma unroll
-  for (int w = 0; w < kKeepThreads / 64; ++w) {
-    before += w < wave ? wave_sums[w] : 0u;
-    total += wave_sums[w];
+  for (int w = 0; w < kKeepWaves; ++w) {
+    s.upto += w < wave ? wave_sums[w] : 0u;
+    s.total += wave_sums[w];
   }
-  return v + before;
+  return s;
+}
+struct KeepShared { uint32_t hist[2048], wave_sums[kKeepWaves], found[2], entry[32 * kKeepWaves]; };
+
+// What is known of the smallest weight that is taken: its leading bits, and how many rows that begin with them are wanted.
+struct KeepFound { uint32_t prefix, need; };
+// The bin of pass `pass` in which the need-th largest lies; thread t brings the counts of the bins from the top on: `mine` (one bin in the last pass).
+SP_DEV KeepFound keep_find(KeepShared& sh, int pass, uint32_t first, uint32_t second, KeepFound so_far) {
+  const int per = kKeepBins[pass] / kKeepThreads, top = kKeepBins[pass] - 1 - (int)threadIdx.x * per;
+  const uint32_t upto = keep_scan(first + second, sh.wave_sums).upto, ahead = upto - first - second;
+  if (ahead < so_far.need && so_far.need <= upto) {
+    const bool lower = ahead + first < so_far.need;
+    sh.found[0] = (uint32_t)(top - lower);
+    sh.found[1] = so_far.need - ahead - (lower ? first : 0u);
+  }
+  __syncthreads();
+  const KeepFound f{so_far.prefix | sh.found[0] << kKeepShift[pass], sh.found[1]};
+  __syncthreads();
+  return f;
+}
+SP_DEV void keep_count(KeepShared& sh, int pass, uint32_t u, uint32_t prefix) {
+  const int above = kKeepShift[pass] + (pass == 2 ? 10 : 11);
+  if (pass == 0 || (u >> above) == (prefix >> above)) atomicAdd(&sh.hist[(u >> kKeepShift[pass]) & (kKeepBins[pass] - 1)], 1u);
+}
+SP_DEV void keep_clear(KeepShared& sh, int pass) {
+  for (int i = threadIdx.x; i < kKeepBins[pass]; i += kKeepThreads) sh.hist[i] = 0;
+  __syncthreads();
+}
+// Writes those of the rows first + v * 1024 + thread (v < V, only rows below `others`) that are taken: weights above f.prefix, and of those equal to it the
+// first f.need of the plane.  `above`, `same`: how many rows before `first` are above and equal; both move on.
+template <int V>
+SP_DEV void keep_write(KeepShared& sh, const uint32_t (&u)[V], int64_t first, int64_t others, KeepFound f, uint32_t& above, uint32_t& same, int32_t* out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t more[V], equal[V];
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const bool there = first + v * kKeepThreads + threadIdx.x < others;
+    more[v] = __builtin_amdgcn_ballot_w64(there && u[v] > f.prefix);
+    equal[v] = __builtin_amdgcn_ballot_w64(there && u[v] == f.prefix);
+    if (lane == 0) sh.entry[v * kKeepWaves + wave] = (uint32_t)__popcll(more[v]) | (uint32_t)__popcll(equal[v]) << 16;
+  }
+  __syncthreads();
+  const uint32_t mine = threadIdx.x < V * kKeepWaves ? sh.entry[threadIdx.x] : 0u;
+  const KeepScan s = keep_scan(mine, sh.wave_sums);
+  if (threadIdx.x < V * kKeepWaves) sh.entry[threadIdx.x] = s.upto - mine;
+  __syncthreads();
+  const uint64_t before = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const uint32_t e = sh.entry[v * kKeepWaves + wave];
+    const uint32_t a = above + (e & 0xffffu) + (uint32_t)__popcll(more[v] & before), q = same + (e >> 16) + (uint32_t)__popcll(equal[v] & before);
+    const bool is_equal = equal[v] >> lane & 1;
+    if ((more[v] >> lane & 1) || (is_equal && q < f.need)) out[a + (q < f.need ? q : f.need)] = (int32_t)(first + v * kKeepThreads + threadIdx.x);
+  }
+  above += s.total & 0xffffu;
+  same += s.total >> 16;
 }
 
+// Up to 1024 V rows of a plane: a workgroup, which keeps them in registers.
+template <int V>
 __global__ __launch_bounds__(kKeepThreads) void kv8_keep_kernel(const Kv8KeepArgs a) {
-  __shared__ uint32_t hist[2048], wave_sums[kKeepThreads / 64], found[2];
-  const int tid = threadIdx.x;
+  __shared__ KeepShared sh;
+  const int tid = threadIdx.x, others = a.rows - a.recent;
   const float* const w = a.weights + (int64_t)blockIdx.x * a.capacity;
   int32_t* const out = a.index + (int64_t)blockIdx.x * a.keep;
-  const int others = a.rows - a.recent;
-  uint32_t need = (uint32_t)(a.keep - a.recent);      // of the others; then: of those with the leading bits found so far
-  uint32_t prefix = 0;                                // leading bits of the smallest weight that is taken
-  const bool all = need >= (uint32_t)others;
-  if (need > 0 && !all) {
-    constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
+  uint32_t u[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) u[v] = v * kKeepThreads + tid < others ? weight_order(w[v * kKeepThreads + tid]) : 0u;
+  KeepFound f{0u, (uint32_t)(a.keep - a.recent)};
+  if (f.need >= (uint32_t)others) {            // all of them
+    for (int i = tid; i < others; i += kKeepThreads) out[i] = i;
+  } else if (f.need > 0) {
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-      const int shift = kShift[pass], bins = 1 << kBits[pass], above = shift + kBits[pass];
-      for (int i = tid; i < bins; i += kKeepThreads) hist[i] = 0;
+      keep_clear(sh, pass);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v * kKeepThreads + tid < others) keep_count(sh, pass, u[v], f.prefix);
       __syncthreads();
-      for (int i = tid; i < others; i += kKeepThreads) {
-        const uint32_t u = weight_order(w[i]);
-        if (pass == 0 || (u >> above) == (prefix >> above)) atomicAdd(&hist[(u >> shift) & (bins - 1)], 1u);
-      }
-      __syncthreads();
-      // the bin in which the need-th largest lies: thread t has bins from the top on
-      const int per = bins / kKeepThreads;            // 2, 2, 1
-      uint32_t mine[2] = {0, 0}, total;
-      for (int i = 0; i < per; ++i) mine[i] = hist[bins - 1 - (tid * per + i)];
-      const uint32_t upto = keep_scan(mine[0] + mine[1], wave_sums, total), ahead = upto - mine[0] - mine[1];
-      if (ahead < need && need <= upto) {
-        const int second = ahead + mine[0] < need;
-        found[0] = (uint32_t)(bins - 1 - (tid * per + second));
-        found[1] = need - ahead - (second ? mine[0] : 0u);
-      }
-      __syncthreads();
-      prefix |= found[0] << shift;
-      need = found[1];
-      __syncthreads();
+      const int per = kKeepBins[pass] / kKeepThreads, top = kKeepBins[pass] - 1 - tid * per;
+      const uint32_t first = sh.hist[top], second = per > 1 ? sh.hist[top - 1] : 0u;
+      f = keep_find(sh, pass, first, second, f);
     }
-  }
-  // rows above `prefix`, and the first `need` ones equal to it, in order
-  const bool none = a.keep == a.recent;
-  uint32_t taken = 0, equal = 0;                      // so far
-  for (int base = 0; base < others; base += kKeepThreads) {
-    const int i = base + tid;
-    uint32_t above = 0, same = 0, total;
-    if (i < others && !none) {
-      const uint32_t u = all ? 1u : weight_order(w[i]);
-      above = all || u > prefix;
-      same = !all && u == prefix;
-    }
-    const uint32_t sums = keep_scan(above | same << 16, wave_sums, total);
-    // (rows equal to it that come before this one: those beyond `need` are not taken)
-    const uint32_t eq_before = equal + (sums >> 16) - same, eq_taken = eq_before < need ? eq_before : need;
-    const uint32_t eq_start = equal < need ? equal : need;
-    const bool take = above || (same && eq_before < need);
-    if (take) out[taken + (sums & 0xffffu) - above + eq_taken - eq_start] = i;
-    const uint32_t eq_all = equal + (total >> 16), eq_end = eq_all < need ? eq_all : need;
-    taken += (total & 0xffffu) + eq_end - eq_start;
-    equal = eq_all;
+    uint32_t above = 0, same = 0;
+    keep_write<V>(sh, u, 0, others, f, above, same, out);
   }
   for (int i = tid; i < a.recent; i += kKeepThreads) out[a.keep - a.recent + i] = others + i;
 }
+
+// More rows: a workgroup for every a.chunk of them (a multiple of kKeepSpan), a launch a pass.  The counts of a pass stay in the workspace, [plane][chunk]
+// [2048]; every workgroup of the next pass adds its plane's up.  Behind them, for each chunk, how many of its rows are known to be above; and for each
+// plane what the passes found.
+constexpr int kKeepSpan = 8 * kKeepThreads;
+struct KeepWork {
+  uint32_t *hist[3], *above, *found;
+  SP_DEV KeepWork(const Kv8KeepArgs& a, int plane) {
+    uint32_t* p = a.work + (int64_t)plane * (a.chunks * (int64_t)kKeepChunkWords + kKeepPlaneWords);
+    for (int i = 0; i < 3; p += (int64_t)a.chunks * kKeepBins[i], ++i) hist[i] = p;
+    above = p;
+    found = p + a.chunks;
+  }
+};
+static_assert(kKeepChunkWords == 2048 + 2048 + 1024 + 1, "words of a chunk");
+
+// PASS 0 .. 2: counts of a chunk; PASS 3: the indices.
+template <int PASS>
+__global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8KeepArgs a) {
+  __shared__ KeepShared sh;
+  const int tid = threadIdx.x, chunk = blockIdx.x, plane = blockIdx.y;
+  const int64_t others = a.rows - a.recent, first = (int64_t)chunk * a.chunk, last = first + a.chunk < others ? first + a.chunk : others;
+  const float* const w = a.weights + plane * a.capacity;
+  const KeepWork work(a, plane);
+  KeepFound f{0u, (uint32_t)(a.keep - a.recent)};
+  uint32_t above = 0, same = 0;                // PASS 3: rows before the chunk; else: those of it that the passes so far have put above
+  const bool all = f.need >= (uint32_t)others, search = f.need > 0 && !all;
+  if (PASS > 0 && search) {
+    constexpr int P = PASS > 0 ? PASS - 1 : 0, PER = kKeepBins[P] / kKeepThreads;
+    if (PASS > 1) f = KeepFound{work.found[2 * PASS - 4], work.found[2 * PASS - 3]};
+    const int top = kKeepBins[P] - 1 - tid * PER;
+    uint32_t total[2] = {0, 0}, before[2] = {0, 0}, mine[2] = {0, 0};
+#pragma unroll 8
+    for (int c = 0; c < a.chunks; ++c)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const uint32_t n = work.hist[P][(int64_t)c * kKeepBins[P] + top - i];
+        total[i] += n;
+        before[i] += c < chunk ? n : 0u;
+        mine[i] += c == chunk ? n : 0u;
+      }
+    const KeepFound was = f;
+    f = keep_find(sh, P, total[0], total[1], f);
+    // of the bins above the one found: rows of this chunk, or (the last time) of the chunks before
+    const int bin = (int)((f.prefix ^ was.prefix) >> kKeepShift[P]);
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n += top - i > bin ? (PASS == 3 ? before[i] : mine[i]) : 0u;
+    above = keep_scan(n, sh.wave_sums).total;
+    if (PASS == 3) {
+      __syncthreads();
+      if (top == bin) sh.found[0] = before[0];
+      uint32_t known = 0;
+      for (int c = tid; c < chunk; c += kKeepThreads) known += work.above[c];
+      above += keep_scan(known, sh.wave_sums).total;
+      same = sh.found[0];
+    } else if (tid == 0) {
+      if (PASS > 1) above += work.above[chunk];
+      work.above[chunk] = above;
+    }
+  }
+  if constexpr (PASS < 3) {
+    // (the first workgroup of a plane writes down what all of them have found, for the next launch)
+    if (PASS > 0 && chunk == 0 && tid == 0) { work.found[2 * PASS - 2] = f.prefix; work.found[2 * PASS - 1] = f.need; }
+    keep_clear(sh, PASS);
+    for (int64_t at = first; at < last; at += kKeepSpan) {
+      float x[8];
+#pragma unroll
+      for (int v = 0; v < 8; ++v) x[v] = at + v * kKeepThreads + tid < last ? w[at + v * kKeepThreads + tid] : 0.f;
+#pragma unroll
+      for (int v = 0; v < 8; ++v)
+        if (at + v * kKeepThreads + tid < last) keep_count(sh, PASS, weight_order(x[v]), f.prefix);
+    }
+    __syncthreads();
+    for (int i = tid; i < kKeepBins[PASS]; i += kKeepThreads) work.hist[PASS][(int64_t)chunk * kKeepBins[PASS] + i] = sh.hist[i];
+  } else {
+    int32_t* const out = a.index + (int64_t)plane * a.keep;
+    for (int64_t at = first; search && at < last; at += kKeepSpan) {
+      uint32_t u[8];
+#pragma unroll
+      for (int v = 0; v < 8; ++v) u[v] = at + v * kKeepThreads + tid < last ? weight_order(w[at + v * kKeepThreads + tid]) : 0u;
+      keep_write<8>(sh, u, at, last, f, above, same, out);
+    }
+    if (all)
+      for (int64_t i = first + tid; i < last; i += kKeepThreads) out[i] = (int32_t)i;
+    for (int64_t i = (int64_t)chunk * kKeepThreads + tid; i < a.recent; i += (int64_t)a.chunks * kKeepThreads) out[a.keep - a.recent + i] = (int32_t)(others + i);
+  }
+}
+
 hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(kv8_keep_kernel, dim3((unsigned)a.planes), dim3(kKeepThreads), 0, st, a);
+  const dim3 block(kKeepThreads);
+  if (a.chunks == 0) {
+    const dim3 grid((unsigned)a.planes);
+    if (a.rows <= 4 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<4>, grid, block, 0, st, a);
+    else if (a.rows <= 16 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<16>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(kv8_keep_kernel<32>, grid, block, 0, st, a);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)a.chunks, (unsigned)a.planes);
+  if (a.keep > a.recent && a.keep < a.rows) {
+    hipLaunchKernelGGL(kv8_keep_pass_kernel<0>, grid, block, 0, st, a);
+    hipLaunchKernelGGL(kv8_keep_pass_kernel<1>, grid, block, 0, st, a);
+    hipLaunchKernelGGL(kv8_keep_pass_kernel<2>, grid, block, 0, st, a);
+  }
+  hipLaunchKernelGGL(kv8_keep_pass_kernel<3>, grid, block, 0, st, a);
   return hipGetLastError();
 }
 
