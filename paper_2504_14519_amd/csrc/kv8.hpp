@@ -79,6 +79,9 @@ hipError_t launch_kv8_store(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv8_load(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, bool few, hipStream_t st);      // few: group * s_q <= kKv8FewRows
 constexpr int kKv8FewRows = 32;
+// Rows of a plane from which a bf16 copy of the keys and slimpipe_attn_fwd are faster than tiles converted in the kernel (us with the copy and without, 32K keys: 512
+// rows of 8 heads on one 39 and 29, 1024 43 and 41, 4096 77 and 92, 32768 444 and 572; 40 heads on 17K keys: 512 rows 254 and 250, 1024 423 and 490)
+constexpr int kKv8CopyRows = 1024;
 hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hipStream_t st);
 hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st);
 hipError_t launch_kv8_gather(const Kv8GatherArgs& a, int head_dim, hipStream_t st);

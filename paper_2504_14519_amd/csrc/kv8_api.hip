@@ -37,6 +37,24 @@ bool rows_fit(const slimpipe_attn_params* p, int64_t rows) { return rows <= 1 <<
 
 int64_t rows_of(const slimpipe_attn_params* p) { return (int64_t)p->n_q_heads / p->n_kv_heads * p->s_q; }      // of a plane
 
+// Key ranges of a call of few rows: `least_rounds` workgroups for every compute unit, then as many more (up to `most_rounds`) as the last round needs to be nearly
+// full, from 8 on in eights (ranges of the same keys share an XCD).  Attention, 2 to 6: tokens of 4 sequences of 32K keys, 40 heads, us: 8 ranges, 320
+// workgroups, 337; 24, 960, 255; 32, 1280, 246; beyond what evens the rounds out the fold of the results costs more than it gives (a token of 8 heads on one behind 1M
+// keys: 512 ranges 67, 1024 73, 1536 78).  Sums of weights have no fold, 8 to 12: the same token 42.6 with 2 to 6, 34.9 with 8 to 12; 8 heads of 64 in 8
+// sequences of 32K 67 and 42.
+int64_t few_parts(int64_t wgs, int64_t most, int64_t least_rounds, int64_t most_rounds) {
+  const int64_t units = compute_units();
+  if (most * wgs <= least_rounds * units) return most;
+  int64_t best = 1;
+  double best_full = 0.;
+  for (int64_t parts = 1; parts <= most && (parts == 1 || parts * wgs <= most_rounds * units); parts += parts < 8 ? 1 : 8) {
+    const int64_t n = parts * wgs;
+    const double full = n < least_rounds * units ? 0.5 * (double)n / (double)(least_rounds * units) : (double)n / (double)((n + units - 1) / units * units);
+    if (full > best_full) { best = parts; best_full = full; }
+    if (full >= 0.95) break;
+  }
+  return best;
+}
 // Key ranges that a call is cut into, a workgroup for each and each block of rows, so that the chip is full.
 struct Kv8Plan {
   bool few;
@@ -46,11 +64,15 @@ struct Kv8Plan {
 Kv8Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
   Kv8Plan plan{rows <= kKv8FewRows, 1, keys};
-  const int64_t wgs = plan.few ? planes / kv8_heads_wg(p->n_kv_heads) : planes * ((rows + 127) / 128), want = 2 * (int64_t)compute_units();
   const int64_t least = plan.few ? 256 : 512;      // keys of a part
-  int64_t parts = plan.few ? want / wgs : (want + wgs - 1) / wgs;
-  if (plan.few && parts >= 8) parts = parts / 8 * 8;      // (eight ranges at a time: ranges of the same keys share an XCD)
-  if (parts > keys / least) parts = keys / least;
+  int64_t parts;
+  if (plan.few) {
+    parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / least, 2, 6);
+  } else {
+    const int64_t wgs = planes * ((rows + 127) / 128);
+    parts = (2 * (int64_t)compute_units() + wgs - 1) / wgs;
+    if (parts > keys / least) parts = keys / least;
+  }
   if (parts > 1) {
     const int64_t unit = plan.few ? 32 : 64;      // keys of a step
     plan.part_keys = ((keys + parts - 1) / parts + unit - 1) / unit * unit;
@@ -68,10 +90,7 @@ Kv8WeightPlan weight_plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = p->kv_end - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
   Kv8WeightPlan plan{rows <= kKv8FewRows, 1, keys};
   if (plan.few) {
-    const int64_t want = 4 * (int64_t)compute_units(), wgs = planes / kv8_heads_wg(p->n_kv_heads);
-    int64_t parts = want / wgs;
-    if (parts >= 8) parts = parts / 8 * 8;                // (as in plan_of)
-    if (parts > keys / 256) parts = keys / 256;
+    const int64_t parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / 256, 8, 12);
     if (parts > 1) {
       plan.part_keys = ((keys + parts - 1) / parts + 31) / 32 * 32;
       plan.parts = (int32_t)((keys + plan.part_keys - 1) / plan.part_keys);
@@ -89,6 +108,39 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t out_bytes(const slimpipe_attn_params* p, const Kv8Plan& plan) { return up((size_t)p->batch * p->n_q_heads * p->s_q * plan.parts * p->head_dim * 4); }
 size_t bytes_of(const slimpipe_attn_params* p, const Kv8Plan& plan) {
   return plan.parts <= 1 ? 0 : out_bytes(p, plan) + up((size_t)p->batch * p->n_q_heads * p->s_q * plan.parts * 4);
+}
+// Long slices go to slimpipe_attn_fwd over a bf16 copy of the keys that they see, in the workspace.  (Not where early rows see no key: that call does not
+// keep them from keys that are not finite.)
+bool copies(const slimpipe_attn_params* p) {
+  return rows_of(p) >= kKv8CopyRows && seen_end(p, p->kv_begin, p->kv_end) > p->kv_begin && !(p->causal && p->kv_begin > p->q_offset) &&
+         rows_fit(p, p->kv_end - p->kv_begin);
+}
+size_t copy_bytes(const slimpipe_attn_params* p) {      // keys or values
+  return up((size_t)p->batch * (size_t)(seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin) * p->n_kv_heads * p->head_dim * 2);
+}
+slimpipe_attn_params copy_params(const slimpipe_attn_params* p) {
+  slimpipe_attn_params c = *p;
+  c.kv_end = seen_end(p, p->kv_begin, p->kv_end);
+  c.kv_stride_h = p->head_dim;
+  c.kv_stride_s = (int64_t)p->n_kv_heads * p->head_dim;
+  c.kv_stride_b = (c.kv_end - c.kv_begin) * c.kv_stride_s;
+  return c;
+}
+int fwd_by_copy(const slimpipe_attn_params* p, const Kv8Cache& cache, const void* q, void* out, float* lse, char* ws, size_t bytes, void* stream) {
+  const slimpipe_attn_params c = copy_params(p);
+  const size_t each = copy_bytes(p);
+  Kv8CopyArgs a;
+  memset(&a, 0, sizeof(a));
+  a.cache = cache;
+  a.k_dst = reinterpret_cast<__bf16*>(ws);
+  a.v_dst = reinterpret_cast<__bf16*>(ws + each);
+  a.batch = p->batch; a.rows = c.kv_end - c.kv_begin; a.position = c.kv_begin;
+  a.x_stride_b = c.kv_stride_b; a.x_stride_s = c.kv_stride_s; a.x_stride_h = c.kv_stride_h;
+  if (launch_kv8_load(a, p->head_dim, static_cast<hipStream_t>(stream)) != hipSuccess) return SLIMPIPE_ELAUNCH;
+  // (where row 0 of the copies would be; rows before kv_begin are not read)
+  const uintptr_t back = (uintptr_t)(c.kv_begin * c.kv_stride_s * 2);
+  return slimpipe_attn_fwd(&c, q, reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(ws) - back), reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(ws + each) - back),
+                           out, lse, ws + 2 * each, bytes - 2 * each, stream);
 }
 size_t weight_bytes_of(const slimpipe_attn_params* p, const Kv8WeightPlan& plan) {
   return plan.few || plan.parts <= 1 ? 0 : up((size_t)plan.parts * p->batch * p->n_kv_heads * (size_t)(p->kv_end - p->kv_begin) * 4);
@@ -182,7 +234,13 @@ int slimpipe_attn_kv8_workspace_bytes(const slimpipe_attn_params* p, int32_t blo
   if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
   if (rc != SLIMPIPE_OK) return rc;
   *bytes = bytes_of(p, plan_of(p));
-  return SLIMPIPE_OK;
+  if (copies(p)) {
+    const slimpipe_attn_params c = copy_params(p);
+    size_t attention = 0;
+    rc = slimpipe_attn_workspace_bytes(&c, 0, &attention);
+    if (rc == SLIMPIPE_OK && *bytes < 2 * copy_bytes(p) + attention) *bytes = 2 * copy_bytes(p) + attention;
+  }
+  return rc;
 }
 
 int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
@@ -197,10 +255,15 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
   const Kv8Plan plan = plan_of(p);
   if (workspace_bytes < bytes_of(p, plan) || (plan.parts > 1 && !workspace)) return SLIMPIPE_EWORKSPACE;
   if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
+  const Kv8Cache cache = cache_of(p, block_len, k_codes, k_scales, v_codes, v_scales);
+  if (workspace && copies(p) && workspace_bytes >= 2 * copy_bytes(p)) {
+    if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
+    return fwd_by_copy(p, cache, q_slice, out, lse, static_cast<char*>(workspace), workspace_bytes, hip_stream);
+  }
   Kv8Args a;
   memset(&a, 0, sizeof(a));
   a.q = static_cast<const __bf16*>(q_slice);
-  a.cache = cache_of(p, block_len, k_codes, k_scales, v_codes, v_scales);
+  a.cache = cache;
   a.out = out;
   a.lse = lse;
   a.batch = p->batch; a.s_q = p->s_q; a.n_q_heads = p->n_q_heads; a.group = p->n_q_heads / p->n_kv_heads;

@@ -20,7 +20,7 @@ SP_DEV float row_norm(float lse) { return lse == -INFINITY ? INFINITY : lse * kL
 // steps under way.
 template <int D, int SETS>
 __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8WeightArgs a) {
-  constexpr int NP = D / 64, W = 2 * NP, DEPTH = 4;
+  constexpr int NP = D / 64, W = 2 * NP, DEPTH = 2;
   const Kv8Cache& kv = a.cache;
   const int lane = threadIdx.x & 63, h4 = lane >> 4, ql = lane & 15, wave_u = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int hw = kv8_heads_wg(kv.n_kv_heads), subs = 4 / hw, sub = wave_u / hw;
@@ -53,10 +53,14 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
   for (int r = 1; r < SETS; ++r) min_see = min_see < see_rel[r] ? min_see : see_rel[r];
 
   const int64_t base = (int64_t)b * kv.stride_b + (int64_t)hk * kv.stride_h + lo * kv.stride_s + 16 * h4;
-  struct Step { u32x4 k[2][NP]; uint32_t ks[2]; };
+  // (the sums of earlier calls come along with the codes: a load of its own at the end of a step would wait for all that is under way)
+  const int64_t out0 = plane_out * a.capacity + lo + 4 * h4 + ql;      // entry of the key whose sum the lane writes, ql < 4
+  struct Step { u32x4 k[2][NP]; uint32_t ks[2]; float before[2]; };
   auto fetch = [&](Step& s, int t) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
+      s.before[u] = 0.f;
+      if (a.previous && ql < 4 && t * 32 + 16 * u + 4 * h4 + ql < n_keys) s.before[u] = a.previous[out0 + t * 32 + 16 * u];
       int key = t * 32 + 16 * u + ql;
       key = key < n_keys ? key : n_keys - 1;                     // (keys behind the last are not read)
       const int64_t at = base + (int64_t)key * kv.stride_s;
@@ -79,6 +83,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
         for (int r = 0; r < SETS; ++r) s[r][u] = mfma16(k8, q[r][j], s[r][u]);
       }
     }
+    const float before[2] = {st.before[0], st.before[1]};
     if (next < nt) fetch(st, next);
     const bool masked = __builtin_amdgcn_ballot_w64(min_see < t * 32 + 31) != 0;
 #pragma unroll
@@ -97,7 +102,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
         for (int w = 1; w < 16; w <<= 1) sum[i] += __shfl_xor(sum[i], w, 64);
       const float mine = ql == 0 ? sum[0] : ql == 1 ? sum[1] : ql == 2 ? sum[2] : sum[3];
       const int key = t * 32 + 16 * u + 4 * h4 + ql;
-      if (ql < 4 && key < n_keys) put_weight(a, plane_out, lo + key, mine);
+      if (ql < 4 && key < n_keys) a.weights[out0 + t * 32 + 16 * u] = __builtin_fmaf(a.decay, before[u], mine);
     }
   };
   if (sub >= nt) return;

@@ -163,6 +163,27 @@ def test_forward(sp, case):
         bu.check("lse", host_f64(lse), r.lse, r.lse_tol)
 
 
+def test_long_slice_with_and_without_room_for_a_copy(sp):
+    """1200 rows of a kv head, the whole range and a piece of it: by a bf16 copy of the keys, and tile by tile where the workspace has no room for one."""
+    import torch
+    B, s, off, Hq, Hkv, D, L = 2, 600, 333, 4, 2, 64, 32
+    N = off + s
+    cache, k, v = random_cache(sp, B, N, Hkv, D, L)
+    bits = normal_bf16((B, s, Hq, D), 43, "q", 1)
+    for begin, end in ((0, N), (301, 800)):
+        key = np.arange(N)
+        see = np.broadcast_to((key >= begin) & (key < end) & (key <= (off + np.arange(s))[:, None]), (B, Hq, s, N))
+        r = bu.Reference(bf16_bits_to_f64(bits), k, v, see, 1 / math.sqrt(D))
+        need = sp.slimpipe_attn_kv8_workspace_bytes(dev_bf16(bits), cache, off, begin, end)
+        copy = 2 * B * (end - begin) * Hkv * D * 2
+        assert need >= copy
+        for room in (need, copy - 256):
+            ws = torch.empty(room, device="cuda", dtype=torch.uint8)
+            out, lse = sp.slimpipe_attn_fwd_kv8(dev_bf16(bits), cache, off, begin, end, workspace=ws)
+            bu.check("out", host_f64(out), r.out, r.out_tol)
+            bu.check("lse", host_f64(lse), r.lse, r.lse_tol)
+
+
 @pytest.mark.parametrize("s", [2, 140, 520])
 def test_layouts_and_unseen_keys(sp, s):
     """Strided heads, a cache of another layout with NaN codes and scales behind the last seen key and before the first: the same bits."""
