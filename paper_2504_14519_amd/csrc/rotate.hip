@@ -4,21 +4,28 @@
 //   backward: dy = the result's gradient turned back;  dw = sum over rows and heads of dy n;  g = dy w;  dx = r (g - n mean(g n))
 //
 // Bound by the bytes: x in, result out.  A lane has two chunks of 8 elements that hold whole pairs, so that nothing but the two sums over a head
-// crosses lanes, head_dim / 16 lanes have a head of a row, and they walk heads of that row: the angles are made once a row.  An angle is made in 64 bits as a
-// fraction of a turn (position * frequency passes 2^20, where 32 bits leave an error of a sixteenth), its sine and cosine in 32.
+// crosses lanes, head_dim / 16 lanes have a head of a row, and a wave has a few heads of its 8 (head_dim 64: 16) rows: all of its loads are under way
+// before the angles are made, which serve all of its heads.  An angle is made in 64 bits as a fraction of a turn (position * frequency passes 2^20, where 32
+// bits leave an error of a sixteenth), its sine and cosine in 32.
 #include "rotate.hpp"
-#include "tile_common.hpp"
+#include "row_tile.hpp"
 
 namespace slimpipe {
 
+template <int CTRL>
+SP_DEV float add_lane(float v) { return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true)); }
 // Sum over the lanes of a head, in all of them: 4 or 8 consecutive lanes.
 template <int LANES>
 SP_DEV float head_sum(float v) {
-  auto add = [&](auto ctrl) { v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true)); };
-  add(std::integral_constant<int, 0xb1>{});                            // lane ^ 1
-  add(std::integral_constant<int, 0x4e>{});                            // lane ^ 2
-  if constexpr (LANES == 8) add(std::integral_constant<int, 0x141>{});  // 7 - lane of eight: the other four, whose sums are equal by now
-  return v;
+  v = add_lane<0xb1>(v);                                 // lane ^ 1
+  v = add_lane<0x4e>(v);                                 // lane ^ 2
+  return LANES == 8 ? add_lane<0x141>(v) : v;            // 7 - lane of eight: the other four, whose sums are equal by now
+}
+// Sum over the heads of a wave: the lanes with the same place in a head.
+template <int LANES>
+SP_DEV float rows_sum(float v) {
+  if constexpr (LANES == 4) v = add_lane<0x124>(v);      // lane + 4 of sixteen
+  return quarters_sum(add_lane<0x128>(v));               // lane + 8, then over the sixteens
 }
 
 // position * frequency / 2 pi less the whole turns, in [-1/2, 1/2].  Products keep what their rounding leaves behind: one 64-bit product alone
@@ -90,93 +97,90 @@ SP_DEV void load_weight(const RotateSide& s, const Turn<D, I>& t, float (&w)[16]
   }
 }
 
-constexpr int kRotateAhead = 4;      // heads whose loads are under way together
+// Which side, heads and rows a wave has.  Sets of heads are numbered through, those of the queries first, fastest over the workgroups: neighbours read
+// the same rows.
+struct RotateWave { int side, first, heads; int64_t block; };
+SP_DEV RotateWave rotate_wave(const RotateArgs& a, int wave_u) {
+  const int sets = a.sets[0] + a.sets[1], set = __builtin_amdgcn_readfirstlane((int)(blockIdx.x % (unsigned)sets));
+  const int side = set >= a.sets[0], first = (side ? set - a.sets[0] : set) * a.heads_wave, left = a.side[side].heads - first;
+  return {side, first, left < a.heads_wave ? left : a.heads_wave, (int64_t)(blockIdx.x / (unsigned)sets) * 4 + wave_u};
+}
 
 template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
-  constexpr int LANES = D / 16, ROWS = 64 / LANES;
+  constexpr int LANES = D / 16, ROWS = 64 / LANES, N = kRotateFwdHeads;
   const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int set = __builtin_amdgcn_readfirstlane((int)(w / a.row_blocks));
-  if (set >= a.head_sets) return;
-  const int64_t row = (w - (int64_t)set * a.row_blocks) * ROWS + lane / LANES;
+  const RotateWave w = rotate_wave(a, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  const int64_t row = w.block * ROWS + lane / LANES;
   if (row >= a.total_rows) return;                                    // (whole heads' lanes leave together)
+  const RotateSide& s = a.side[w.side];
   const int64_t b = row / a.rows, r = row - b * a.rows;
   Turn<D, INTERLEAVED> t;
   t.init(a, lane);
+  const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;
+  bf16x8 lo[N], hi[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const bf16_t* p = x + (int64_t)(u < w.heads ? u : 0) * s.stride_h;
+    lo[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.ca);
+    hi[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.cb);
+  }
+  float wt[16];
+  load_weight(s, t, wt);
   t.angles(a, lane, a.positions ? a.positions[row] : a.position + r);
-  const int first = set * a.heads_wave, last = first + a.heads_wave;
+  bf16_t* out = s.out + b * s.out_stride_b + r * s.out_stride_s + w.first * s.out_stride_h;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const RotateSide& s = a.side[i];
-    const int base = i == 0 ? 0 : a.side[0].heads;
-    int h = first > base ? first - base : 0;
-    const int end = last - base < s.heads ? last - base : s.heads;
-    if (h >= end) continue;
-    float wt[16];
-    load_weight(s, t, wt);
-    const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s;
-    bf16_t* out = s.out + b * s.out_stride_b + r * s.out_stride_s;
-    for (; h < end; h += kRotateAhead) {
-      bf16x8 lo[kRotateAhead], hi[kRotateAhead];
+  for (int u = 0; u < N; ++u) {
+    if (u >= w.heads) break;
+    float v[16], sum = 0.f;
+    widen(lo[u], hi[u], v);
 #pragma unroll
-      for (int u = 0; u < kRotateAhead; ++u) {
-        const bf16_t* p = x + (int64_t)(h + u < end ? h + u : end - 1) * s.stride_h;
-        lo[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.ca);
-        hi[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.cb);
-      }
+    for (int j = 0; j < 16; ++j) sum = __builtin_fmaf(v[j], v[j], sum);
+    const float inv = __builtin_amdgcn_rsqf(head_sum<LANES>(sum) * (1.0f / D) + a.eps);
 #pragma unroll
-      for (int u = 0; u < kRotateAhead; ++u) {
-        float v[16], sum = 0.f;
-        widen(lo[u], hi[u], v);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) sum = __builtin_fmaf(v[j], v[j], sum);
-        const float inv = __builtin_amdgcn_rsqf(head_sum<LANES>(sum) * (1.0f / D) + a.eps);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] *= inv * wt[j];
-        t.template apply<false>(v);
-        if (h + u < end) {
-          bf16_t* p = out + (int64_t)(h + u) * s.out_stride_h;
-          *reinterpret_cast<bf16x8*>(p + 8 * t.ca) = narrow(v);
-          *reinterpret_cast<bf16x8*>(p + 8 * t.cb) = narrow(v + 8);
-        }
-      }
-    }
+    for (int j = 0; j < 16; ++j) v[j] *= inv * wt[j];
+    t.template apply<false>(v);
+    bf16_t* p = out + (int64_t)u * s.out_stride_h;
+    *reinterpret_cast<bf16x8*>(p + 8 * t.ca) = narrow(v);
+    *reinterpret_cast<bf16x8*>(p + 8 * t.cb) = narrow(v + 8);
   }
 }
 
 // The gradient.  The weights' gradients are summed in the lanes over the rows and heads of a wave, over the waves of a workgroup in LDS, and over the
 // workgroups by rotate_weights_kernel, all in a fixed order.
 template <int D, bool INTERLEAVED, bool DOUT_F32>
-SP_DEV void rotate_back_heads(const RotateArgs& a, const RotateSide& s, const Turn<D, INTERLEAVED>& t, int64_t b, int64_t r, int h, int end, float (&dw)[16]) {
-  constexpr int LANES = D / 16, AHEAD = DOUT_F32 ? 2 : kRotateAhead;
+SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, INTERLEAVED>& t, int lane, float (&dw)[16]) {
+  constexpr int LANES = D / 16, ROWS = 64 / LANES, N = kRotateBwdHeads;
   typedef std::conditional_t<DOUT_F32, float, bf16_t> dout_t;
   typedef dout_t dout8 __attribute__((ext_vector_type(8)));
+  const RotateSide& s = a.side[w.side];
   float wt[16];
   load_weight(s, t, wt);
-  const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s;
-  bf16_t* dx = s.out + b * s.stride_b + r * s.stride_s;
-  const dout_t* d = static_cast<const dout_t*>(s.d_out) + b * s.out_stride_b + r * s.out_stride_s;
-  for (; h < end; h += AHEAD) {
-    bf16x8 lo[AHEAD], hi[AHEAD];
-    dout8 dlo[AHEAD], dhi[AHEAD];
+  for (int64_t block = w.block; block < a.row_blocks; block += a.wave_blocks) {
+    const int64_t row = block * ROWS + lane / LANES;
+    if (row >= a.total_rows) break;
+    const int64_t b = row / a.rows, r = row - b * a.rows;
+    const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;
+    const dout_t* d = static_cast<const dout_t*>(s.d_out) + b * s.out_stride_b + r * s.out_stride_s + w.first * s.out_stride_h;
+    bf16x8 lo[N], hi[N];
+    dout8 dlo[N], dhi[N];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int64_t hh = h + u < end ? h + u : end - 1;
-      const bf16_t* p = x + hh * s.stride_h;
-      const dout_t* e = d + hh * s.out_stride_h;
+    for (int u = 0; u < N; ++u) {
+      const bf16_t* p = x + (int64_t)(u < w.heads ? u : 0) * s.stride_h;
+      const dout_t* e = d + (int64_t)(u < w.heads ? u : 0) * s.out_stride_h;
       lo[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.ca);
       hi[u] = *reinterpret_cast<const bf16x8*>(p + 8 * t.cb);
       dlo[u] = *reinterpret_cast<const dout8*>(e + 8 * t.ca);
       dhi[u] = *reinterpret_cast<const dout8*>(e + 8 * t.cb);
     }
+    t.angles(a, lane, a.positions ? a.positions[row] : a.position + r);
+    bf16_t* dx = s.out + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (h + u >= end) break;
-      float y[16];
+    for (int u = 0; u < N; ++u) {
+      if (u >= w.heads) break;
+      float y[16], v[16], sum = 0.f, dot = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) { y[j] = (float)dlo[u][j]; y[8 + j] = (float)dhi[u][j]; }
-      float v[16], sum = 0.f, dot = 0.f;
       widen(lo[u], hi[u], v);
       t.template apply<true>(y);
 #pragma unroll
@@ -191,7 +195,7 @@ SP_DEV void rotate_back_heads(const RotateArgs& a, const RotateSide& s, const Tu
         dw[j] = __builtin_fmaf(y[j], v[j] * inv, dw[j]);
         v[j] = (y[j] * wt[j] - v[j] * back) * inv;
       }
-      bf16_t* p = dx + (int64_t)(h + u) * s.stride_h;
+      bf16_t* p = dx + (int64_t)u * s.stride_h;
       *reinterpret_cast<bf16x8*>(p + 8 * t.ca) = narrow(v);
       *reinterpret_cast<bf16x8*>(p + 8 * t.cb) = narrow(v + 8);
     }
@@ -200,75 +204,55 @@ SP_DEV void rotate_back_heads(const RotateArgs& a, const RotateSide& s, const Tu
 
 template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_bwd_kernel(const RotateArgs a) {
-  constexpr int LANES = D / 16, ROWS = 64 / LANES;
-  __shared__ float sums[2][4][D];
+  constexpr int LANES = D / 16;
+  __shared__ float sums[4][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
-  const int set = __builtin_amdgcn_readfirstlane((int)(w / a.wave_blocks));
+  const RotateWave w = rotate_wave(a, wave);
   Turn<D, INTERLEAVED> t;
   t.init(a, lane);
-  float dw[2][16];
+  float dw[16];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) dw[i][j] = 0.f;
-  if (set < a.head_sets) {
-    const int first = set * a.heads_wave, last = first + a.heads_wave;
-    for (int64_t blk = w - (int64_t)set * a.wave_blocks; blk < a.row_blocks; blk += a.wave_blocks) {
-      const int64_t row = blk * ROWS + lane / LANES;
-      if (row >= a.total_rows) continue;
-      const int64_t b = row / a.rows, r = row - b * a.rows;
-      t.angles(a, lane, a.positions ? a.positions[row] : a.position + r);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const RotateSide& s = a.side[i];
-        const int base = i == 0 ? 0 : a.side[0].heads;
-        const int h = first > base ? first - base : 0, end = last - base < s.heads ? last - base : s.heads;
-        if (h >= end) continue;
-        if (s.d_out_f32) rotate_back_heads<D, INTERLEAVED, true>(a, s, t, b, r, h, end, dw[i]);
-        else rotate_back_heads<D, INTERLEAVED, false>(a, s, t, b, r, h, end, dw[i]);
-      }
-    }
-  }
+  for (int j = 0; j < 16; ++j) dw[j] = 0.f;
+  if (a.side[w.side].d_out_f32) rotate_back_rows<D, INTERLEAVED, true>(a, w, t, lane, dw);
+  else rotate_back_rows<D, INTERLEAVED, false>(a, w, t, lane, dw);
   if (!a.part) return;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      float v = dw[i][j];
-#pragma unroll
-      for (int k = LANES; k < 64; k <<= 1) v += __shfl_xor(v, k, 64);
-      if (lane < LANES) sums[i][wave][8 * (j < 8 ? t.ca : t.cb) + j % 8] = v;
-    }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += 256) {
-    const int e = i % D, side = i / D;
-    a.part[((int64_t)side * a.workgroups + blockIdx.x) * D + e] = (sums[side][0][e] + sums[side][1][e]) + (sums[side][2][e] + sums[side][3][e]);
+  for (int j = 0; j < 16; ++j) {
+    const float v = rows_sum<LANES>(dw[j]);
+    if (lane < LANES) sums[wave][8 * (j < 8 ? t.ca : t.cb) + j % 8] = v;
   }
+  __syncthreads();
+  // (sums of the queries' workgroups, then those of the keys')
+  const int sets = a.sets[0] + a.sets[1], set = blockIdx.x % sets, group = blockIdx.x / sets, groups = gridDim.x / sets;
+  const int64_t at = w.side ? (int64_t)groups * a.sets[0] + (int64_t)group * a.sets[1] + set - a.sets[0] : (int64_t)group * a.sets[0] + set;
+  if (threadIdx.x < D) a.part[at * D + threadIdx.x] = (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
-// Sums of the workgroups: 16 elements of one side a workgroup, 16 threads an element.
+// Sums of the workgroups: 16 elements of one side a workgroup, 64 threads an element.
 template <int D>
-__global__ __launch_bounds__(256) void rotate_weights_kernel(const RotateArgs a) {
-  __shared__ float sums[16][16];
-  const int side = blockIdx.y, e = blockIdx.x * 16 + threadIdx.x % 16, k = threadIdx.x / 16;
+__global__ __launch_bounds__(1024) void rotate_weights_kernel(const RotateArgs a) {
+  __shared__ float sums[64][17];
+  const int side = blockIdx.y, c = threadIdx.x % 16, e = blockIdx.x * 16 + c, k = threadIdx.x / 16;
   if (!a.d_weight[side]) return;
-  const float* p = a.part + (int64_t)side * a.workgroups * D + e;
+  const int groups = a.workgroups / (a.sets[0] + a.sets[1]), n = groups * a.sets[side];
+  const float* p = a.part + (side ? (int64_t)groups * a.sets[0] * D : 0) + e;
   float v = 0.f;
-#pragma unroll 8
-  for (int i = k; i < a.workgroups; i += 16) v += p[(int64_t)i * D];
-  sums[k][threadIdx.x % 16] = v;
+#pragma unroll 16
+  for (int i = k; i < n; i += 64) v += p[(int64_t)i * D];
+  sums[k][c] = v;
   __syncthreads();
-  if (k) return;
-  v = a.weight_accumulate ? a.d_weight[side][e] : 0.f;
+  if (k >= 4) return;                                     // (the first wave: 4 threads an element)
+  v = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v += sums[i][threadIdx.x];
-  a.d_weight[side][e] = v;
+  for (int i = 0; i < 16; ++i) v += sums[k * 16 + i][c];
+  v += __shfl_xor(v, 16, 64);
+  v += __shfl_xor(v, 32, 64);
+  if (k == 0) a.d_weight[side][e] = a.weight_accumulate ? a.d_weight[side][e] + v : v;
 }
 
 template <int D>
 static hipError_t launch_fwd_t(const RotateArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((a.row_blocks * a.head_sets + 3) / 4)), block(256);
+  const dim3 grid((unsigned)a.workgroups), block(256);
   if (a.interleaved) hipLaunchKernelGGL((rotate_fwd_kernel<D, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((rotate_fwd_kernel<D, false>), grid, block, 0, st, a);
   return hipGetLastError();
@@ -280,7 +264,7 @@ static hipError_t launch_bwd_t(const RotateArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)a.workgroups), block(256);
   if (a.interleaved) hipLaunchKernelGGL((rotate_bwd_kernel<D, true>), grid, block, 0, st, a);
   else hipLaunchKernelGGL((rotate_bwd_kernel<D, false>), grid, block, 0, st, a);
-  if (a.part) hipLaunchKernelGGL((rotate_weights_kernel<D>), dim3(D / 16, 2), block, 0, st, a);
+  if (a.part) hipLaunchKernelGGL((rotate_weights_kernel<D>), dim3(D / 16, 2), dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 hipError_t launch_rotate_bwd(const RotateArgs& a, int head_dim, hipStream_t st) { return head_dim == 128 ? launch_bwd_t<128>(a, st) : launch_bwd_t<64>(a, st); }

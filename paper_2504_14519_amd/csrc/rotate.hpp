@@ -22,16 +22,19 @@ struct RotateArgs {
   int32_t rows, interleaved, rotate_dim;
   float eps;
   int64_t total_rows;            // batch * rows
-  // A wave takes a row block (64 / (head_dim / 16) rows) and `heads_wave` heads, those of the queries and of the keys numbered through;
-  // backward: one row block after the other, `wave_blocks` waves sharing them out, with the same heads
-  int32_t heads_wave, head_sets;
+  // A wave takes a block of rows (64 / (head_dim / 16)) and heads_wave heads of one side, a workgroup four such blocks; backward: every wave_blocks-th
+  // block from its first one on
+  int32_t heads_wave, sets[2];   // sets of heads of the queries, of the keys
   int64_t row_blocks, wave_blocks;
-  float* part;                   // backward: sums of the weights' gradients, [side][workgroup][head_dim]; nullptr: not wanted
+  int32_t workgroups;            // a multiple of the sets of both
+  float* part;                   // backward: sums of the weights' gradients, [workgroup][head_dim]; nullptr: not wanted
   float* d_weight[2];
-  int32_t weight_accumulate, workgroups;
+  int32_t weight_accumulate;
 };
 
 constexpr int rotate_rows_per_wave(int head_dim) { return 64 / (head_dim / 16); }
+// most heads of a wave: what its registers hold of loads under way
+constexpr int kRotateFwdHeads = 4, kRotateBwdHeads = 3;
 hipError_t launch_rotate_fwd(const RotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_rotate_bwd(const RotateArgs& a, int head_dim, hipStream_t st);
 

@@ -49,23 +49,28 @@ int common_args(RotateArgs* a, const slimpipe_rotate_params* p, const void* q, c
   a->row_blocks = (a->total_rows + per - 1) / per;
   return SLIMPIPE_OK;
 }
-// Cuts the heads into sets so that about `waves` waves have work.
-void cut_heads(RotateArgs* a, int64_t blocks, int64_t waves) {
-  const int heads = a->side[0].heads + a->side[1].heads;
-  int64_t sets = (waves + blocks - 1) / blocks;
-  if (sets > heads) sets = heads;
-  a->heads_wave = (int32_t)((heads + sets - 1) / sets);
-  a->head_sets = (heads + a->heads_wave - 1) / a->heads_wave;
+// Cuts the heads of either side into sets of at most `most` and the rows into blocks; `waves` of them at least, where there are heads enough, so that small calls
+// fill the chip.
+void plan(RotateArgs* a, int most, int64_t waves) {
+  a->heads_wave = most;
+  auto sets = [&](int i) { return (a->side[i].heads + a->heads_wave - 1) / a->heads_wave; };
+  while (a->heads_wave > 1 && a->row_blocks * (sets(0) + sets(1)) < waves) --a->heads_wave;
+  a->sets[0] = sets(0);
+  a->sets[1] = sets(1);
 }
-// Backward: the waves stay and take row blocks in turn, so that there are few sums of the weights' gradients to add up.
+void plan_fwd(RotateArgs* a) {
+  plan(a, kRotateFwdHeads, (int64_t)compute_units() * 4);
+  a->workgroups = (int32_t)((a->row_blocks + 3) / 4 * (a->sets[0] + a->sets[1]));
+}
+// Backward: beyond 8 workgroups a compute unit the waves take several blocks of rows, so that there are few sums of the weights' gradients to add up.
 void plan_bwd(RotateArgs* a) {
-  const int64_t most = (int64_t)compute_units() * 16;
-  cut_heads(a, a->row_blocks, most);
-  a->wave_blocks = most / a->head_sets < a->row_blocks ? most / a->head_sets : a->row_blocks;
-  if (a->wave_blocks < 1) a->wave_blocks = 1;
-  a->workgroups = (int32_t)((a->wave_blocks * a->head_sets + 3) / 4);
+  plan(a, kRotateBwdHeads, (int64_t)compute_units() * 4);
+  const int64_t sets = a->sets[0] + a->sets[1], groups = (a->row_blocks + 3) / 4, fit = (int64_t)compute_units() * 8 / sets;
+  const int64_t taken = groups < fit ? groups : fit > 1 ? fit : 1;
+  a->wave_blocks = 4 * taken;
+  a->workgroups = (int32_t)(taken * sets);
 }
-size_t bytes_of(const RotateArgs& a, int head_dim) { return (size_t)2 * a.workgroups * head_dim * 4; }
+size_t bytes_of(const RotateArgs& a, int head_dim) { return (size_t)a.workgroups * head_dim * 4; }
 
 int status(hipError_t e) { return e == hipSuccess ? SLIMPIPE_OK : SLIMPIPE_ELAUNCH; }
 
@@ -84,7 +89,7 @@ int slimpipe_attn_norm_rotate(const slimpipe_rotate_params* p, const void* q, co
   if (!aligned16(q_out) || !aligned16(k_out)) return SLIMPIPE_EINVAL_ALIGN;
   a.side[0].out = static_cast<__bf16*>(q_out);
   a.side[1].out = static_cast<__bf16*>(k_out);
-  cut_heads(&a, a.row_blocks, (int64_t)compute_units() * 16);
+  plan_fwd(&a);
   return status(launch_rotate_fwd(a, p->head_dim, static_cast<hipStream_t>(hip_stream)));
 }
 
