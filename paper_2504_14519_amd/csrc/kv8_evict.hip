@@ -97,9 +97,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
           sum[i] += masked && t * 32 + 16 * u + 4 * h4 + i > see_rel[r] ? 0.f : p;
         }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int w = 1; w < 16; w <<= 1) sum[i] += __shfl_xor(sum[i], w, 64);
+      for (int i = 0; i < 4; ++i) sum[i] = sixteen_sum(sum[i]);
       const float mine = ql == 0 ? sum[0] : ql == 1 ? sum[1] : ql == 2 ? sum[2] : sum[3];
       const int key = t * 32 + 16 * u + 4 * h4 + ql;
       if (ql < 4 && key < n_keys) a.weights[out0 + t * 32 + 16 * u] = __builtin_fmaf(a.decay, before[u], mine);
@@ -186,81 +184,101 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
     };
     copy_tile(t0);
     if (t0 + 1 < t1) copy_tile(t0 + 1);
+    // K in registers.  The contraction may take head_dim in any order: lane group g has elements 32 j + 16 g .. + 15 in steps 2 j and 2 j + 1, one load.
     bf16x8 k[2][KS];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
       int64_t key = wave_key0 + 32 * kb + (lane & 31);
       key = key < a.kv_end ? key : a.kv_end - 1;                  // (keys behind the last are not read)
       const float unit = kv8_scale(kv.k.scales[kv8_scale_at(kv, b, key, hk)]);
-      const uint8_t* p = kv.k.codes + (int64_t)b * kv.stride_b + key * kv.stride_s + (int64_t)hk * kv.stride_h + 8 * g;
+      const uint8_t* p = kv.k.codes + (int64_t)b * kv.stride_b + key * kv.stride_s + (int64_t)hk * kv.stride_h + 16 * g;
+      u32x4 c[KS / 2];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x2 c = *reinterpret_cast<const u32x2*>(p + 16 * ks);
-        k[kb][ks] = kv8_values(c[0], c[1], unit);
+      for (int j = 0; j < KS / 2; ++j) c[j] = *reinterpret_cast<const u32x4*>(p + 32 * j);
+#pragma unroll
+      for (int j = 0; j < KS / 2; ++j) {
+        k[kb][2 * j] = kv8_values(c[j][0], c[j][1], unit);
+        k[kb][2 * j + 1] = kv8_values(c[j][2], c[j][3], unit);
       }
     }
-    RpBase<D> lo_q;
-    lo_q.init(lane, (int)lds);
-    // norm and last visible key (relative to the wave's first, less the lane's 4 g) of the lane's row in a block of 32
+    // the rows of Q to go with it: step 2 j + e reads chunk 4 j + 2 g + e, which the swizzle puts at that of chunk 2 g with 4 j + e in bits 4 ..
+    int lo_q = (int)lds + tile_off<D>(lane & 31, 2 * g);
+    auto q_rows = [&](int ks) { return *lds_ptr<bf16x8>(lo_q ^ ((ks / 2 * 4 + ks % 2) << 4), 0); };
+    // Norm and last visible key (relative to the wave's first, less the lane's 4 g) of the lane's row in a block of 32.  Of most tiles every row sees every
+    // key of the wave.
     const int64_t rel = a.q_offset - wave_key0 + r_min;
+    auto norm_of = [&](int block) { return row_norm(*lds_ptr<float>((int)lds + 3 * TILE + (block / 2 % 3) * kWeightRows * 4 + (block & 1) * 128 + (lane & 31) * 4, 0)); };
+    auto whole = [&](int t) {
+      const int rh0 = t * kWeightRows, r0 = rh0 - __builtin_amdgcn_readfirstlane((int)((unsigned)rh0 / (unsigned)vis)) * vis;
+      return r0 + kWeightRows <= vis && (!a.causal || rel + r0 >= 63);
+    };
     auto row_of = [&](int block, float& norm, int& see) {
       const int rh = block * 32 + (lane & 31), rc = rh < rows ? rh : rows - 1;
-      const float x = *lds_ptr<float>((int)lds + 3 * TILE + (block / 2 % 3) * kWeightRows * 4 + (block & 1) * 128 + (lane & 31) * 4, 0);
-      norm = rh < rows ? row_norm(x) : INFINITY;
+      if (rh >= rows) norm = INFINITY;
       const int64_t far = rel + (int)((unsigned)rc % (unsigned)vis);
       see = (!a.causal || far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
     };
+    // Scores of block 0 or 1 of a tile, and of the block before (`Rows`: what its exponentials need), which are taken meanwhile.
+    struct Rows { float norm; int see; bool masked; };
     f32x16 s[2][2];
-    float norm[2];
-    int see[2];
-    // exponential and sum of element e (of 32) of the scores of block x
-    auto take = [&](int x, int e, bool masked) {
-      const int kb = e / 16, i = e % 16;
-      float p = exp2_fast(__builtin_fmaf(s[x][kb][i], a.scale_log2e, -norm[x]));
-      if (masked) p = 32 * kb + 8 * (i >> 2) + (i & 3) <= see[x] ? p : 0.f;
-      acc[kb][i] += p;
-    };
-    auto is_masked = [&](int x) { return __builtin_amdgcn_ballot_w64(see[x] < 63 - 4 * g) != 0; };
-    // scores of block x from the rows at lo_q in LDS; those of the other block taken meanwhile
-    auto block = [&](auto x_, bool with_other) {
-      constexpr int x = decltype(x_)::value;
+    auto scores = [&](auto x_, const Rows& other, bool with_other) {
+      constexpr int x = decltype(x_)::value, LOOK = 6, NBUF = LOOK / 2 + 1, E = 32 / (2 * KS);      // two instructions a read
       const f32x16 zero = {0};
-      const bool masked = with_other && is_masked(1 - x);
-      constexpr int LOOK = 3;
-      bf16x8 buf[LOOK + 1];
-      if (!with_other || masked) {
-        matrix_run<2 * KS, LOOK>([&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % (LOOK + 1)] = lds_rp<D>(lo_q, m / 2, 0); },
-                                 [&](auto m) { s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % (LOOK + 1)], m < 2 ? zero : s[x][m % 2]); });
-        if (masked)
+      bf16x8 buf[NBUF];
+      auto read = [&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % NBUF] = q_rows(m / 2); };
+      if (with_other && !other.masked) {
+        // (an opaque norm: or the arithmetic that this way and the one below share would be done ahead of both)
+        float norm = other.norm, p[E];
+        asm volatile("" : "+v"(norm));
+        matrix_run<2 * KS, LOOK>(read, [&](auto m) {
+          s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]);
+          // an exponential is added one instruction later, when it is there
 #pragma unroll
-          for (int e = 0; e < 32; ++e) take(1 - x, e, true);
-      } else {
-        matrix_run<2 * KS, LOOK>([&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % (LOOK + 1)] = lds_rp<D>(lo_q, m / 2, 0); },
-                                 [&](auto m) {
-                                   s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % (LOOK + 1)], m < 2 ? zero : s[x][m % 2]);
-                                   constexpr int E = 32 / (2 * KS);
+          for (int e = 0; e < E; ++e) {
+            constexpr int at = m * E;
+            if constexpr (m > 0) acc[(at - E) / 16][(at - E) % 16 + e] += p[e];
+            p[e] = exp2_fast(__builtin_fmaf(s[1 - x][at / 16][at % 16 + e], a.scale_log2e, -norm));
+          }
+        });
 #pragma unroll
-                                   for (int e = 0; e < E; ++e) take(1 - x, m * E + e, false);
-                                 });
+        for (int e = 0; e < E; ++e) acc[1][16 - E + e] += p[e];
+        return;
+      }
+      matrix_run<2 * KS, LOOK>(read, [&](auto m) { s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]); });
+      if (!with_other) return;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const float p = exp2_fast(__builtin_fmaf(s[1 - x][e / 16][e % 16], a.scale_log2e, -other.norm));
+        acc[e / 16][e % 16] += 32 * (e / 16) + 8 * (e % 16 >> 2) + (e & 3) <= other.see ? p : 0.f;
       }
     };
+    Rows r[2] = {{INFINITY, 63, false}, {INFINITY, 63, false}};
     for (int t = t0; t < t1; ++t) {
       // this wave's copies of tile t have landed when at most those of tile t + 1 are under way
       if (t + 1 < t1) wait_copies<PASSES + 1>();
       else wait_async();
       __syncthreads();
       if (t + 2 < t1) copy_tile(t + 2);
-      lo_q.off0 += ((t % 3) * TILE);
-      block(std::integral_constant<int, 0>{}, t > t0);
-      row_of(2 * t, norm[0], see[0]);
-      lo_q.off0 += 32 * D * 2;
-      block(std::integral_constant<int, 1>{}, true);
-      row_of(2 * t + 1, norm[1], see[1]);
-      lo_q.off0 -= 32 * D * 2 + ((t % 3) * TILE);
-    }
-    const bool masked = is_masked(1);
+      Rows now[2] = {{norm_of(2 * t), 63, false}, {norm_of(2 * t + 1), 63, false}};
+      if (!whole(t)) {
 #pragma unroll
-    for (int e = 0; e < 32; ++e) take(1, e, masked);
+        for (int x = 0; x < 2; ++x) {
+          row_of(2 * t + x, now[x].norm, now[x].see);
+          now[x].masked = __builtin_amdgcn_ballot_w64(now[x].see < 63 - 4 * g) != 0;
+        }
+      }
+      lo_q += (t % 3) * TILE;
+      scores(std::integral_constant<int, 0>{}, r[1], t > t0);
+      lo_q += 32 * D * 2;
+      scores(std::integral_constant<int, 1>{}, now[0], true);
+      lo_q -= 32 * D * 2 + (t % 3) * TILE;
+      r[1] = now[1];
+    }
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float p = exp2_fast(__builtin_fmaf(s[1][e / 16][e % 16], a.scale_log2e, -r[1].norm));
+      acc[e / 16][e % 16] += 32 * (e / 16) + 8 * (e % 16 >> 2) + (e & 3) <= r[1].see ? p : 0.f;
+    }
   }
   // over the 32 rows of a half-wave
   __syncthreads();
@@ -269,9 +287,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
   for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float v = acc[kb][i];
-#pragma unroll
-      for (int w = 1; w < 32; w <<= 1) v += __shfl_xor(v, w, 64);
+      const float v = half_sum(acc[kb][i]);
       if ((lane & 31) == 0) out[32 * kb + 8 * (i >> 2) + 4 * g + (i & 3)] = v;
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");

@@ -12,8 +12,6 @@
 
 namespace slimpipe {
 
-template <int CTRL>
-SP_DEV float add_lane(float v) { return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true)); }
 // Sum over the lanes of a head, in all of them: 4 or 8 consecutive lanes.
 template <int LANES>
 SP_DEV float head_sum(float v) {

@@ -34,7 +34,7 @@ struct RotateArgs {
 
 constexpr int rotate_rows_per_wave(int head_dim) { return 64 / (head_dim / 16); }
 // most heads of a wave: what its registers hold of loads under way
-constexpr int kRotateFwdHeads = 4, kRotateBwdHeads = 3;
+constexpr int kRotateFwdHeads = 4, kRotateBwdHeads = 4;
 hipError_t launch_rotate_fwd(const RotateArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_rotate_bwd(const RotateArgs& a, int head_dim, hipStream_t st);
 

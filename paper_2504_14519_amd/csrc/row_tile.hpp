@@ -20,6 +20,16 @@ SP_DEV float quarters_sum(float v) {
   auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return xhalf_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
+// A lane's value and that of another lane of the same sixteen, which CTRL (a DPP control) names
+template <int CTRL>
+SP_DEV float add_lane(float v) { return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true)); }
+// over sixteen lanes, over a half-wave; in all of them
+SP_DEV float sixteen_sum(float v) { return add_lane<0x140>(add_lane<0x141>(add_lane<0x4e>(add_lane<0xb1>(v)))); }      // lane ^ 1, ^ 2, 7 - lane, 15 - lane
+SP_DEV float half_sum(float v) {
+  v = sixteen_sum(v);
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 // Rows of a plane (batch index, kv head) are numbered head of the group major: row rh is row rh % s_q of head rh / s_q.
 struct PlaneRow { int r, h; };
