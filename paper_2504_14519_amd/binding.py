@@ -8,6 +8,7 @@ import collections
 import ctypes
 import math
 import os
+import struct
 
 # torch before the library: the tensors and streams handed to the library come from torch's HIP runtime, so that runtime has
 # to be the one already in the process when the library's dependency on libamdhip64 is resolved (loaded the other
@@ -47,6 +48,13 @@ class RotateParams(ctypes.Structure):
         ("qo_stride_b", ctypes.c_int64), ("qo_stride_s", ctypes.c_int64), ("qo_stride_h", ctypes.c_int64),
         ("ko_stride_b", ctypes.c_int64), ("ko_stride_s", ctypes.c_int64), ("ko_stride_h", ctypes.c_int64),
     ]
+
+
+# The parameter blocks as bytes, which the calls on the 8-bit cache and the norm and rotation pass (a Structure of as many fields takes twice as long to fill:
+# 0.5 us of a call)
+_pack_attn = struct.Struct("=6i4qfi12q").pack
+_pack_rotate = struct.Struct("=7if13q").pack
+assert len(_pack_attn(*[0] * 24)) == ctypes.sizeof(AttnParams) and len(_pack_rotate(*[0] * 21)) == ctypes.sizeof(RotateParams)
 
 
 class BwdPlan(ctypes.Structure):
@@ -125,30 +133,29 @@ def _load():
     L.slimpipe_attn_kv4_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_fwd_kv4.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_fwd_kv4.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_store.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_store.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_kv8_store.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_load.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_load.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_kv8_load.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_workspace_bytes.argtypes = [P, i32, szp]
+    L.slimpipe_attn_kv8_workspace_bytes.argtypes = [vp, i32, szp]
     L.slimpipe_attn_kv8_workspace_bytes.restype = ctypes.c_int
-    L.slimpipe_attn_fwd_kv8.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_fwd_kv8.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_fwd_kv8.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_weights_workspace_bytes.argtypes = [P, i32, szp]
+    L.slimpipe_attn_kv8_weights_workspace_bytes.argtypes = [vp, i32, szp]
     L.slimpipe_attn_kv8_weights_workspace_bytes.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_weights.argtypes = [P, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_kv8_weights.argtypes = [vp, i32, vp, vp, vp, vp, vp, ctypes.c_float, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_kv8_weights.restype = ctypes.c_int
     L.slimpipe_attn_kv8_keep_workspace_bytes.argtypes = [i32, i64, i64, szp]
     L.slimpipe_attn_kv8_keep_workspace_bytes.restype = ctypes.c_int
     L.slimpipe_attn_kv8_keep.argtypes = [vp, i32, i64, i64, i64, i64, vp, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_kv8_keep.restype = ctypes.c_int
-    L.slimpipe_attn_kv8_gather.argtypes = [P, i32, vp, i64, vp, vp, vp, vp, vp, P, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_kv8_gather.argtypes = [vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_kv8_gather.restype = ctypes.c_int
-    R = ctypes.POINTER(RotateParams)
-    L.slimpipe_attn_norm_rotate.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.slimpipe_attn_norm_rotate.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.slimpipe_attn_norm_rotate.restype = ctypes.c_int
-    L.slimpipe_attn_norm_rotate_workspace_bytes.argtypes = [R, szp]
+    L.slimpipe_attn_norm_rotate_workspace_bytes.argtypes = [vp, szp]
     L.slimpipe_attn_norm_rotate_workspace_bytes.restype = ctypes.c_int
-    L.slimpipe_attn_norm_rotate_bwd.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    L.slimpipe_attn_norm_rotate_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     L.slimpipe_attn_norm_rotate_bwd.restype = ctypes.c_int
     L.slimpipe_attn_mfma_rate.argtypes = [ctypes.c_int, vp, ctypes.POINTER(ctypes.c_double), vp]
     L.slimpipe_attn_mfma_rate.restype = ctypes.c_int
@@ -650,7 +657,8 @@ def _loaded_rows(shape, device, k_rows, v_rows):
     if shape[1] < 0:
         raise SlimpipeError("kv_end lies before kv_begin")
     if k_rows is None and v_rows is None:
-        return torch.empty((2,) + shape, device=device, dtype=torch.bfloat16).unbind(0)
+        k_rows = torch.empty(shape, device=device, dtype=torch.bfloat16)
+        return k_rows, torch.empty_like(k_rows)
     if k_rows is None:
         k_rows = torch.empty_strided(v_rows.shape, v_rows.stride(), device=v_rows.device, dtype=v_rows.dtype)      # (gaps and all)
     elif v_rows is None:
@@ -675,7 +683,7 @@ def slimpipe_attn_kv4_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     return k_rows, v_rows
 
 
-def _cache_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
+def _kv4_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
     (B, N, H, D), skv = cache.layout()
     shape = q_slice.shape
     if len(shape) != 4 or shape[0] != B or shape[3] != D:
@@ -693,7 +701,7 @@ def _kv4_ws(p):
 
 def slimpipe_attn_kv4_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
     """Bytes of workspace that slimpipe_attn_fwd_kv4 of these tensors needs (may be 0)."""
-    return _kv4_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16))
+    return _kv4_ws(_kv4_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16))
 
 
 def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
@@ -704,7 +712,7 @@ def slimpipe_attn_fwd_kv4(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
     _check_lse(lse, shape)
-    p = _cache_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    p = _kv4_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv4_ws(p), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
@@ -745,15 +753,15 @@ class KvCache8(collections.namedtuple("KvCache8", "k_codes k_scales v_codes v_sc
 def slimpipe_attn_kv8_store(k_slice, v_slice, cache, position):
     """Append bf16 rows k_slice, v_slice [B, s, Hkv, D] to a KvCache8 that holds `position` rows."""
     (B, N, H, D), skv = cache.layout()
-    if tuple(k_slice.shape) != (B, k_slice.shape[1], H, D) or k_slice.stride(3) != 1 or not _same_strides(k_slice, v_slice):
+    shape, sx = k_slice.shape, k_slice.stride()
+    if len(shape) != 4 or shape[0] != B or shape[2] != H or shape[3] != D or sx[3] != 1 or not _same_strides(k_slice, v_slice):
         raise SlimpipeError("k_slice and v_slice must be [batch, rows, kv heads, head_dim] of the cache, with the same strides")
     if not k_slice.dtype is v_slice.dtype is torch.bfloat16:
         raise SlimpipeError("k_slice and v_slice must be torch.bfloat16")
     _check_device(k_slice, v_slice, *cache[:4])
-    sx = k_slice.stride()[:3]
-    p = AttnParams(B, k_slice.shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx)
-    _check(lib.slimpipe_attn_kv8_store(ctypes.byref(p), cache.block_len, k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()),
-           "slimpipe_attn_kv8_store")
+    sx = sx[:3]
+    _check(lib.slimpipe_attn_kv8_store(_pack_attn(B, shape[1], H, H, D, 1, N, position, 0, 0, 1.0, BF16, *sx, *skv, *sx, *sx), cache.block_len,
+                                       k_slice.data_ptr(), v_slice.data_ptr(), *_cache_ptrs(cache), _stream()), "slimpipe_attn_kv8_store")
 
 
 def slimpipe_attn_kv8_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
@@ -762,21 +770,32 @@ def slimpipe_attn_kv8_load(cache, kv_begin, kv_end, k_rows=None, v_rows=None):
     k_rows, v_rows = _loaded_rows((B, kv_end - kv_begin, H, D), cache.k_codes.device, k_rows, v_rows)
     _check_device(k_rows, v_rows, *cache[:4])
     sx = k_rows.stride()[:3] if kv_end > kv_begin else (H * D, H * D, D)
-    p = AttnParams(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
-    _check(lib.slimpipe_attn_kv8_load(ctypes.byref(p), cache.block_len, *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
-           if kv_end > kv_begin else lib.slimpipe_attn_validate(ctypes.byref(p), 0), "slimpipe_attn_kv8_load")
+    p = _pack_attn(B, 1, H, H, D, 1, N, 0, kv_begin, kv_end, 1.0, BF16, *sx, *skv, *sx, *sx)
+    _check(lib.slimpipe_attn_kv8_load(p, cache.block_len, *_cache_ptrs(cache), k_rows.data_ptr() or None, v_rows.data_ptr() or None, _stream())
+           if kv_end > kv_begin else lib.slimpipe_attn_validate(ctypes.byref(AttnParams.from_buffer_copy(p)), 0), "slimpipe_attn_kv8_load")
     return k_rows, v_rows
+
+
+def _kv8_params(q_slice, cache, out_like, q_offset, kv_begin, kv_end, causal, scale, out_dtype):
+    """-> parameters, and the shape of the sums of weights of such a cache."""
+    (B, N, H, D), skv = cache.layout()
+    shape = q_slice.shape
+    if len(shape) != 4 or shape[0] != B or shape[3] != D:
+        raise SlimpipeError("q_slice and the cache must have the same batch and head_dim")
+    sq, so = q_slice.stride()[:3], out_like.stride()[:3]
+    return _pack_attn(B, shape[1], shape[2], H, D, 1 if causal else 0, N, q_offset, kv_begin, kv_end,
+                      scale if scale is not None else 1.0 / math.sqrt(D), out_dtype, *sq, *skv, *so, *so), (B, H, N)
 
 
 def _kv8_ws(p, block_len):
     n = ctypes.c_size_t(0)
-    _check(lib.slimpipe_attn_kv8_workspace_bytes(ctypes.byref(p), block_len, ctypes.byref(n)), "kv8_workspace_bytes")
+    _check(lib.slimpipe_attn_kv8_workspace_bytes(p, block_len, ctypes.byref(n)), "kv8_workspace_bytes")
     return n.value
 
 
 def slimpipe_attn_kv8_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
     """Bytes of workspace that slimpipe_attn_fwd_kv8 of these tensors needs (may be 0)."""
-    return _kv8_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16), cache.block_len)
+    return _kv8_ws(_kv8_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)[0], cache.block_len)
 
 
 def slimpipe_attn_fwd_kv8(q_slice, cache, q_offset, kv_begin, kv_end, causal=True, scale=None, out_dtype=BF16, out=None, lse=None, workspace=None):
@@ -787,12 +806,12 @@ def slimpipe_attn_fwd_kv8(q_slice, cache, q_offset, kv_begin, kv_end, causal=Tru
         out, lse = _outputs(q_slice, out_dtype, out, lse)
     _check_rows("out (its dtype is out_dtype's)", out, shape, _TORCH_DTYPE.get(out_dtype))
     _check_lse(lse, shape)
-    p = _cache_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
+    p, _ = _kv8_params(q_slice, cache, out, q_offset, kv_begin, kv_end, causal, scale, out_dtype)
     if workspace is None:
         workspace = torch.empty(_kv8_ws(p, cache.block_len), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
     _check_device(q_slice, out, lse, workspace, *cache[:4])
-    _check(lib.slimpipe_attn_fwd_kv8(ctypes.byref(p), cache.block_len, q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(),
+    _check(lib.slimpipe_attn_fwd_kv8(p, cache.block_len, q_slice.data_ptr(), *_cache_ptrs(cache), out.data_ptr(), lse.data_ptr(),
                                      *_ws(workspace), _stream()), "slimpipe_attn_fwd_kv8")
     return out, lse
 
@@ -804,13 +823,13 @@ def _check_weights(name, x, shape):
 
 def _weights_ws(p, block_len):
     n = ctypes.c_size_t(0)
-    _check(lib.slimpipe_attn_kv8_weights_workspace_bytes(ctypes.byref(p), block_len, ctypes.byref(n)), "kv8_weights_workspace_bytes")
+    _check(lib.slimpipe_attn_kv8_weights_workspace_bytes(p, block_len, ctypes.byref(n)), "kv8_weights_workspace_bytes")
     return n.value
 
 
 def slimpipe_attn_kv8_weights_workspace_bytes(q_slice, cache, q_offset, kv_begin, kv_end, causal=True):
     """Bytes of workspace that slimpipe_attn_kv8_weights of these tensors needs (may be 0)."""
-    return _weights_ws(_cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16), cache.block_len)
+    return _weights_ws(_kv8_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, None, BF16)[0], cache.block_len)
 
 
 def slimpipe_attn_kv8_weights(q_slice, cache, lse, q_offset, kv_begin, kv_end, causal=True, scale=None, weights=None, previous=None, decay=1.0,
@@ -820,8 +839,7 @@ def slimpipe_attn_kv8_weights(q_slice, cache, lse, q_offset, kv_begin, kv_end, c
     shape = q_slice.shape
     _check_rows("q_slice", q_slice, shape)
     _check_lse(lse, shape)
-    p = _cache_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, scale, BF16)
-    sums = (p.batch, p.n_kv_heads, p.kv_capacity)
+    p, sums = _kv8_params(q_slice, cache, q_slice, q_offset, kv_begin, kv_end, causal, scale, BF16)
     if weights is None:
         weights = torch.zeros(sums, device=q_slice.device, dtype=torch.float32)
     _check_weights("weights", weights, sums)
@@ -831,7 +849,7 @@ def slimpipe_attn_kv8_weights(q_slice, cache, lse, q_offset, kv_begin, kv_end, c
         workspace = torch.empty(_weights_ws(p, cache.block_len), device=q_slice.device, dtype=torch.uint8)
     _check_workspace(workspace)
     _check_device(q_slice, lse, weights, weights if previous is None else previous, workspace, cache.k_codes, cache.k_scales)
-    _check(lib.slimpipe_attn_kv8_weights(ctypes.byref(p), cache.block_len, q_slice.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(),
+    _check(lib.slimpipe_attn_kv8_weights(p, cache.block_len, q_slice.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(),
                                          lse.data_ptr(), _ptr(previous), decay, weights.data_ptr(), *_ws(workspace), _stream()), "slimpipe_attn_kv8_weights")
     return weights
 
@@ -880,36 +898,39 @@ def slimpipe_attn_kv8_gather(cache, index, kept, weights=None, kept_weights=None
         sums = [weights, kept_weights]
     _check_device(index, *sums, *cache[:4], *kept[:4])
     one = (H * D, H * D, D)
-    p = AttnParams(B, 1, H, H, D, 1, N, 0, 0, 0, 1.0, BF16, *one, *s_from, *one, *one)
-    to = AttnParams(B, 1, H, H, D, 1, N2, 0, 0, 0, 1.0, BF16, *one, *s_to, *one, *one)
-    _check(lib.slimpipe_attn_kv8_gather(ctypes.byref(p), cache.block_len, index.data_ptr() or None, index.shape[2], *_cache_ptrs(cache), _ptr(weights),
-                                        ctypes.byref(to), *_cache_ptrs(kept), _ptr(kept_weights), _stream())
+    p = _pack_attn(B, 1, H, H, D, 1, N, 0, 0, 0, 1.0, BF16, *one, *s_from, *one, *one)
+    to = _pack_attn(B, 1, H, H, D, 1, N2, 0, 0, 0, 1.0, BF16, *one, *s_to, *one, *one)
+    _check(lib.slimpipe_attn_kv8_gather(p, cache.block_len, index.data_ptr() or None, index.shape[2], *_cache_ptrs(cache), _ptr(weights),
+                                        to, *_cache_ptrs(kept), _ptr(kept_weights), _stream())
            if index.shape[2] > 0 else 0, "slimpipe_attn_kv8_gather")
     return kept
 
 
 def _rotate_params(q, k, weights, frequencies, position, eps, interleaved, q_out, k_out, q_out_dtype=torch.bfloat16, k_out_dtype=torch.bfloat16):
     """Checks of what the two directions share -> (parameters, device pointer of the positions or None)."""
-    shape, k_shape = q.shape, k.shape
-    _check_rows("q", q, shape)
-    _check_rows("k", k, (shape[0], shape[1], k_shape[2] if len(k_shape) == 4 else -1, shape[3]))
-    _check_rows("q_out", q_out, shape, q_out_dtype)
-    _check_rows("k_out", k_out, k_shape, k_out_dtype)
+    shape, k_shape, sq, sk, so, sk_out = q.shape, k.shape, q.stride(), k.stride(), q_out.stride(), k_out.stride()
+    if not (len(shape) == len(k_shape) == 4 and q_out.shape == shape and k_out.shape == k_shape and k_shape[0] == shape[0] and k_shape[1] == shape[1]
+            and k_shape[3] == shape[3] and sq[3] == sk[3] == so[3] == sk_out[3] == 1):
+        raise SlimpipeError("q and k must be [batch, rows, heads, head_dim] of the same batch, rows and head_dim, head_dim contiguous, their results of the same shapes")
+    if not (q.dtype is k.dtype is torch.bfloat16 and q_out.dtype is q_out_dtype and k_out.dtype is k_out_dtype):
+        raise SlimpipeError("q, k and their results must be torch.bfloat16")
     B, s, Hq, D = shape
+    tensors = [q, k, q_out, k_out, frequencies]
     for w in weights:
-        if w is not None and (w.dtype is not torch.float32 or w.shape != (D,) or not w.is_contiguous()):
-            raise SlimpipeError("weights and their gradients must be contiguous float32 tensors [head_dim]")
+        if w is not None:
+            if w.dtype is not torch.float32 or w.shape != (D,) or not w.is_contiguous():
+                raise SlimpipeError("weights and their gradients must be contiguous float32 tensors [head_dim]")
+            tensors.append(w)
     if frequencies.dtype is not torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
         raise SlimpipeError("frequencies must be a contiguous float64 tensor [rotate_dim / 2]")
     at = None
     if isinstance(position, torch.Tensor):
         if position.dtype is not torch.int64 or position.shape != (B, s) or not position.is_contiguous():
             raise SlimpipeError("positions must be a contiguous int64 tensor [batch, rows], or one number: that of row 0")
-        at, position = position, 0
-    _check_device(q, k, q_out, k_out, frequencies, *[w for w in weights if w is not None], *([at] if at is not None else []))
-    p = RotateParams(B, s, Hq, k_shape[2], D, 2 * frequencies.shape[0], 1 if interleaved else 0, eps, position,
-                     *q.stride()[:3], *k.stride()[:3], *q_out.stride()[:3], *k_out.stride()[:3])
-    return p, at.data_ptr() if at is not None else None
+        tensors.append(position)
+        at, position = position.data_ptr(), 0
+    _check_device(*tensors)
+    return _pack_rotate(B, s, Hq, k_shape[2], D, 2 * len(frequencies), 1 if interleaved else 0, eps, position, *sq[:3], *sk[:3], *so[:3], *sk_out[:3]), at
 
 
 def _ptr(x):
@@ -925,14 +946,14 @@ def slimpipe_attn_norm_rotate(q, k, q_weight, k_weight, frequencies, position, e
     if k_out is None:
         k_out = torch.empty(k.shape, device=k.device, dtype=torch.bfloat16)
     p, at = _rotate_params(q, k, (q_weight, k_weight), frequencies, position, eps, interleaved, q_out, k_out)
-    _check(lib.slimpipe_attn_norm_rotate(ctypes.byref(p), q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
+    _check(lib.slimpipe_attn_norm_rotate(p, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
                                          q_out.data_ptr(), k_out.data_ptr(), _stream()), "slimpipe_attn_norm_rotate")
     return q_out, k_out
 
 
 def _rotate_ws(p):
     n = ctypes.c_size_t(0)
-    _check(lib.slimpipe_attn_norm_rotate_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "norm_rotate_workspace_bytes")
+    _check(lib.slimpipe_attn_norm_rotate_workspace_bytes(p, ctypes.byref(n)), "norm_rotate_workspace_bytes")
     return n.value
 
 
@@ -942,7 +963,7 @@ def slimpipe_attn_norm_rotate_workspace_bytes(q, k):
     _check_rows("k", k, k.shape, k.dtype)
     B, s, Hq, D = q.shape
     strides = (D,) * 3
-    return _rotate_ws(RotateParams(B, s, Hq, k.shape[2], D, 0, 0, 1.0, 0, *strides, *strides, *strides, *strides))
+    return _rotate_ws(_pack_rotate(B, s, Hq, k.shape[2], D, 0, 0, 1.0, 0, *strides, *strides, *strides, *strides))
 
 
 def slimpipe_attn_norm_rotate_bwd(q, k, q_weight, k_weight, frequencies, position, dq_out, dk_out, eps=1e-6, interleaved=False, dq=None, dk=None,
@@ -972,7 +993,7 @@ def slimpipe_attn_norm_rotate_bwd(q, k, q_weight, k_weight, frequencies, positio
     _check_workspace(workspace)
     _check_device(dq, dk, workspace)
     codes = [F32 if t is torch.float32 else BF16 for t in dtypes]
-    _check(lib.slimpipe_attn_norm_rotate_bwd(ctypes.byref(p), q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
+    _check(lib.slimpipe_attn_norm_rotate_bwd(p, q.data_ptr(), k.data_ptr(), _ptr(q_weight), _ptr(k_weight), frequencies.data_ptr() or None, at,
                                              dq_out.data_ptr(), codes[0], dk_out.data_ptr(), codes[1], dq.data_ptr(), dk.data_ptr(), _ptr(dq_weight),
                                              _ptr(dk_weight), 1 if weight_accumulate else 0, *_ws(workspace), _stream()), "slimpipe_attn_norm_rotate_bwd")
     return dq, dk, dq_weight, dk_weight

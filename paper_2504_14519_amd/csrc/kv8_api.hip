@@ -55,6 +55,20 @@ int64_t few_parts(int64_t wgs, int64_t most, int64_t least_rounds, int64_t most_
   }
   return best;
 }
+// Key ranges of a slice: the fewest whose workgroups, two a compute unit at once, fill one to three rounds nearly, or those that fill them best (256
+// rows of 40 heads on 16640 keys, 80 workgroups a range: 6 ranges 137 us, 7 167).
+int64_t slice_parts(int64_t wgs, int64_t most) {
+  const int64_t places = 2 * (int64_t)compute_units();
+  int64_t best = 1;
+  double best_full = 0.;
+  for (int64_t parts = 1; parts <= most && (parts == 1 || parts * wgs <= 3 * places); ++parts) {
+    const int64_t n = parts * wgs;
+    const double full = (double)n / (double)((n + places - 1) / places * places);
+    if (full > best_full) { best = parts; best_full = full; }
+    if (full >= 0.9) break;
+  }
+  return best;
+}
 // Key ranges that a call is cut into, a workgroup for each and each block of rows, so that the chip is full.
 struct Kv8Plan {
   bool few;
@@ -69,9 +83,7 @@ Kv8Plan plan_of(const slimpipe_attn_params* p) {
   if (plan.few) {
     parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / least, 2, 6);
   } else {
-    const int64_t wgs = planes * ((rows + 127) / 128);
-    parts = (2 * (int64_t)compute_units() + wgs - 1) / wgs;
-    if (parts > keys / least) parts = keys / least;
+    parts = slice_parts(planes * ((rows + 127) / 128), keys / least);
   }
   if (parts > 1) {
     const int64_t unit = plan.few ? 32 : 64;      // keys of a step

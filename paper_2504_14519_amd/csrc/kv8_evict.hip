@@ -344,11 +344,13 @@ SP_DEV uint32_t weight_order(float w) {
 struct KeepScan { uint32_t upto, total; };
 SP_DEV KeepScan keep_scan(uint32_t v, uint32_t (&wave_sums)[kKeepWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int w = 1; w < 64; w <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_up((int)v, w, 64);
-    v += lane >= w ? o : 0u;
-  }
+  // (row_shr by 1, 2, 4 and 8 inside each sixteen, then the last lane of a sixteen to the next one, and of the first half to the second)
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
+  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
   __syncthreads();
   if (lane == 63) wave_sums[wave] = v;
   __syncthreads();
@@ -471,6 +473,13 @@ __global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8Ke
   const int64_t others = a.rows - a.recent, first = (int64_t)chunk * a.chunk, last = first + a.chunk < others ? first + a.chunk : others;
   const float* const w = a.weights + plane * a.capacity;
   const KeepWork work(a, plane);
+  // (the first rows are on their way while the last pass is added up)
+  float x[8];
+  auto load = [&](int64_t at) {
+#pragma unroll
+    for (int v = 0; v < 8; ++v) x[v] = at + v * kKeepThreads + tid < last ? w[at + v * kKeepThreads + tid] : 0.f;
+  };
+  load(first);
   KeepFound f{0u, (uint32_t)(a.keep - a.recent)};
   uint32_t above = 0, same = 0;                // PASS 3: rows before the chunk; else: those of it that the passes so far have put above
   const bool all = f.need >= (uint32_t)others, search = f.need > 0 && !all;
@@ -479,7 +488,7 @@ __global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8Ke
     if (PASS > 1) f = KeepFound{work.found[2 * PASS - 4], work.found[2 * PASS - 3]};
     const int top = kKeepBins[P] - 1 - tid * PER;
     uint32_t total[2] = {0, 0}, before[2] = {0, 0}, mine[2] = {0, 0};
-#pragma unroll 8
+#pragma unroll 16
     for (int c = 0; c < a.chunks; ++c)
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -513,9 +522,7 @@ __global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8Ke
     if (PASS > 0 && chunk == 0 && tid == 0) { work.found[2 * PASS - 2] = f.prefix; work.found[2 * PASS - 1] = f.need; }
     keep_clear(sh, PASS);
     for (int64_t at = first; at < last; at += kKeepSpan) {
-      float x[8];
-#pragma unroll
-      for (int v = 0; v < 8; ++v) x[v] = at + v * kKeepThreads + tid < last ? w[at + v * kKeepThreads + tid] : 0.f;
+      if (at > first) load(at);
 #pragma unroll
       for (int v = 0; v < 8; ++v)
         if (at + v * kKeepThreads + tid < last) keep_count(sh, PASS, weight_order(x[v]), f.prefix);
@@ -525,9 +532,10 @@ __global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8Ke
   } else {
     int32_t* const out = a.index + (int64_t)plane * a.keep;
     for (int64_t at = first; search && at < last; at += kKeepSpan) {
+      if (at > first) load(at);
       uint32_t u[8];
 #pragma unroll
-      for (int v = 0; v < 8; ++v) u[v] = at + v * kKeepThreads + tid < last ? weight_order(w[at + v * kKeepThreads + tid]) : 0u;
+      for (int v = 0; v < 8; ++v) u[v] = weight_order(x[v]);
       keep_write<8>(sh, u, at, last, f, above, same, out);
     }
     if (all)
@@ -540,8 +548,9 @@ hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
   const dim3 block(kKeepThreads);
   if (a.chunks == 0) {
     const dim3 grid((unsigned)a.planes);
-    if (a.rows <= 4 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<4>, grid, block, 0, st, a);
-    else if (a.rows <= 16 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<16>, grid, block, 0, st, a);
+    const int others = a.rows - a.recent;
+    if (others <= 4 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<4>, grid, block, 0, st, a);
+    else if (others <= 16 * kKeepThreads) hipLaunchKernelGGL(kv8_keep_kernel<16>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(kv8_keep_kernel<32>, grid, block, 0, st, a);
     return hipGetLastError();
   }
