@@ -125,7 +125,7 @@ size_t bytes_of(const slimpipe_attn_params* p, const Kv8Plan& plan) {
 // keep them from keys that are not finite.)
 bool copies(const slimpipe_attn_params* p) {
   return rows_of(p) >= kKv8CopyRows && seen_end(p, p->kv_begin, p->kv_end) > p->kv_begin && !(p->causal && p->kv_begin > p->q_offset) &&
-         rows_fit(p, p->kv_end - p->kv_begin);
+         rows_fit(p, p->kv_end - p->kv_begin) && (int64_t)p->n_kv_heads * p->head_dim < 1 << 22;      // (a row that slimpipe_attn_fwd takes)
 }
 size_t copy_bytes(const slimpipe_attn_params* p) {      // keys or values
   return up((size_t)p->batch * (size_t)(seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin) * p->n_kv_heads * p->head_dim * 2);
