@@ -59,6 +59,7 @@ int slimpipe::ensure_device_ready(void** scratch_ptr) {
     if (d.status == hipSuccess) d.status = opt_in_block_bwd_kernels();
     if (d.status == hipSuccess) d.status = opt_in_kv4_kernels();
     if (d.status == hipSuccess) d.status = opt_in_kv8_kernels();
+    if (d.status == hipSuccess) d.status = opt_in_kv8_evict_kernels();
     if (d.status == hipSuccess) d.status = hipGetSymbolAddress(&d.scratch, HIP_SYMBOL(scratch));
     if (d.status == hipSuccess && d.scratch == nullptr) d.status = hipErrorInvalidSymbol;
   });

@@ -89,5 +89,6 @@ hipError_t launch_kv8_gather(const Kv8GatherArgs& a, int head_dim, hipStream_t s
 inline __host__ __device__ constexpr int kv8_heads_wg(int n_kv_heads) { return n_kv_heads % 4 == 0 ? 4 : n_kv_heads % 2 == 0 ? 2 : 1; }
 constexpr int kv8_weight_keys() { return 256; }      // keys of a workgroup of the sums over a slice's rows
 hipError_t opt_in_kv8_kernels();
+hipError_t opt_in_kv8_evict_kernels();
 
 }  // namespace slimpipe

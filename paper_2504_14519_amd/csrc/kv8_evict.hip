@@ -115,17 +115,20 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
 }
 
 // Slices: a workgroup has 256 keys, 64 a wave, converted once and kept in registers, and walks the rows that see any of them (head by head, without the
-// rows before its first key), or one part of them, in tiles of 64 through a ring of three in LDS.
+// rows before its first key), or one part of them, in tiles of 128 through a ring of two in LDS.
 //   S^T = K Q^T        A = K in registers, B = rows of Q from LDS: a lane has one row and 32 keys of a block of 32 rows
 //   sums               p = exp2(c s - norm) added in place: the lane's sums over its rows, over the lanes at the end
-// The scores of a block of 32 rows are computed while the exponentials of the block before are taken, instruction by instruction.
-constexpr int kWeightKeys = kv8_weight_keys(), kWeightRows = 64;
+// A pair costs the vector unit three instructions, one of them an exponential, beside 2 D flop: both units have about the same to do at D = 128, twice
+// as much the vector unit at 64.  So the scores of a block of 32 rows are computed while the exponentials of the block before are taken, instruction by instruction.
+// 4096 rows of 8 heads on 32768 keys of 128: 245 us, 1.05 PFLOP/s (with the exponentials behind the matrix instructions of the same block 274; tiles of 64 rows
+// in a ring of three 244, but 368 and 318 us for 16384 rows of 4 heads of 64 on 32768 keys).
+constexpr int kWeightKeys = kv8_weight_keys(), kWeightRows = 128, kWeightRing = 2;
 template <int D>
-constexpr size_t kv8_weights_lds_bytes() { return (size_t)3 * kWeightRows * (D * 2 + 4); }
+constexpr size_t kv8_weights_lds_bytes() { return (size_t)kWeightRing * kWeightRows * (D * 2 + 4); }
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs a) {
-  constexpr int KS = D / 16, TILE = kWeightRows * D * 2, NC = D / 8, PASSES = kWeightRows / (4 * (64 / NC));      // copies of a wave a tile
+  constexpr int KS = D / 16, TILE = kWeightRows * D * 2, BLOCKS = kWeightRows / 32, NC = D / 8, PASSES = kWeightRows / (4 * (64 / NC));      // copies of a wave a tile
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const Kv8Cache& kv = a.cache;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -159,11 +162,13 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
     // The rows' lse come along, behind the ring.
     constexpr int RPP = 64 / NC;                                      // rows of a copy instruction
     auto copy_tile = [&](int t) {
-      const unsigned to = lds + (t % 3) * TILE, to_lse = lds + 3 * TILE + (t % 3) * kWeightRows * 4;
+      const unsigned to = lds + (t % kWeightRing) * TILE, to_lse = lds + kWeightRing * TILE + (t % kWeightRing) * kWeightRows * 4;
       const int rh0 = t * kWeightRows, h0 = __builtin_amdgcn_readfirstlane((int)((unsigned)rh0 / (unsigned)vis)), r0 = rh0 - h0 * vis;
       if (r0 + kWeightRows <= vis) {
         const bf16_t* src = q_base + (int64_t)h0 * a.q_stride_h + (int64_t)(r_min + r0) * a.q_stride_s;
-        dma4(uniform_ptr(lse + (int64_t)h0 * a.s_q + r_min + r0), (uint32_t)lane * 4, __builtin_amdgcn_readfirstlane(to_lse));
+#pragma unroll
+        for (int n = 0; n < kWeightRows; n += 64)
+          dma4(uniform_ptr(lse + (int64_t)h0 * a.s_q + r_min + r0 + n), (uint32_t)lane * 4, __builtin_amdgcn_readfirstlane(to_lse + n * 4));
 #pragma unroll
         for (int n = 0; n < PASSES; ++n) WaveDma<D, kWeightRows>::copy_pass(to, uniform_ptr(src), row_bytes, kWeightRows, lane, wave_u * PASSES + n);
         return;
@@ -174,8 +179,11 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
         return rh - hl * vis + r_min;
       };
       int hl;
-      const int rl = at(rh0 + lane, hl);
-      dma4_at(lse + (int64_t)hl * a.s_q + rl, to_lse);
+#pragma unroll
+      for (int n = 0; n < kWeightRows; n += 64) {
+        const int rl = at(rh0 + n + lane, hl);
+        dma4_at(lse + (int64_t)hl * a.s_q + rl, to_lse + n * 4);
+      }
 #pragma unroll
       for (int n = 0; n < PASSES; ++n) {
         const int pass = wave_u * PASSES + n, r = at(rh0 + pass * RPP + lane / NC, hl);
@@ -183,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       }
     };
     copy_tile(t0);
-    if (t0 + 1 < t1) copy_tile(t0 + 1);
+    if (kWeightRing == 3 && t0 + 1 < t1) copy_tile(t0 + 1);
     // K in registers.  The contraction may take head_dim in any order: lane group g has elements 32 j + 16 g .. + 15 in steps 2 j and 2 j + 1, one load.
     bf16x8 k[2][KS];
 #pragma unroll
@@ -204,92 +212,104 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
     // the rows of Q to go with it: step 2 j + e reads chunk 4 j + 2 g + e, which the swizzle puts at that of chunk 2 g with 4 j + e in bits 4 ..
     int lo_q = (int)lds + tile_off<D>(lane & 31, 2 * g);
     auto q_rows = [&](int ks) { return *lds_ptr<bf16x8>(lo_q ^ ((ks / 2 * 4 + ks % 2) << 4), 0); };
-    // Norm and last visible key (relative to the wave's first, less the lane's 4 g) of the lane's row in a block of 32.  Of most tiles every row sees every
-    // key of the wave.
+    // norm of the lane's row in a block of 32 (rows behind the last: one that takes all weight away)
+    auto norm_of = [&](int block) {
+      const float x = *lds_ptr<float>((int)lds + kWeightRing * TILE + (block / BLOCKS % kWeightRing) * kWeightRows * 4 + (block % BLOCKS) * 128 + (lane & 31) * 4, 0);
+      return block * 32 + (lane & 31) < rows ? row_norm(x) : INFINITY;
+    };
+    // Does every row of tile t see every key of the wave?  (Its first row decides, or, where it holds the end of a head, the first of the next.)
     const int64_t rel = a.q_offset - wave_key0 + r_min;
-    auto norm_of = [&](int block) { return row_norm(*lds_ptr<float>((int)lds + 3 * TILE + (block / 2 % 3) * kWeightRows * 4 + (block & 1) * 128 + (lane & 31) * 4, 0)); };
-    auto whole = [&](int t) {
+    auto unmasked = [&](int t) {
       const int rh0 = t * kWeightRows, r0 = rh0 - __builtin_amdgcn_readfirstlane((int)((unsigned)rh0 / (unsigned)vis)) * vis;
-      return r0 + kWeightRows <= vis && (!a.causal || rel + r0 >= 63);
+      return !a.causal || rel + (r0 + kWeightRows <= vis ? r0 : 0) >= 63;
     };
-    auto row_of = [&](int block, float& norm, int& see) {
-      const int rh = block * 32 + (lane & 31), rc = rh < rows ? rh : rows - 1;
-      if (rh >= rows) norm = INFINITY;
-      const int64_t far = rel + (int)((unsigned)rc % (unsigned)vis);
-      see = (!a.causal || far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
-    };
-    // Scores of block 0 or 1 of a tile, and of the block before (`Rows`: what its exponentials need), which are taken meanwhile.
-    struct Rows { float norm; int see; bool masked; };
+    // Scores of a block into s[x]; with `take_other` the exponentials of the scores s[1 - x], of rows with norm `other`, between the matrix instructions.
     f32x16 s[2][2];
-    auto scores = [&](auto x_, const Rows& other, bool with_other) {
+    auto scores = [&](auto x_, bool take_other, float other) {
       constexpr int x = decltype(x_)::value, LOOK = 6, NBUF = LOOK / 2 + 1, E = 32 / (2 * KS);      // two instructions a read
       const f32x16 zero = {0};
       bf16x8 buf[NBUF];
       auto read = [&](auto m) { if constexpr (m % 2 == 0) buf[m / 2 % NBUF] = q_rows(m / 2); };
-      if (with_other && !other.masked) {
-        // (an opaque norm: or the arithmetic that this way and the one below share would be done ahead of both)
-        float norm = other.norm, p[E];
-        asm volatile("" : "+v"(norm));
-        matrix_run<2 * KS, LOOK>(read, [&](auto m) {
-          s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]);
-          // an exponential is added one instruction later, when it is there
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            constexpr int at = m * E;
-            if constexpr (m > 0) acc[(at - E) / 16][(at - E) % 16 + e] += p[e];
-            p[e] = exp2_fast(__builtin_fmaf(s[1 - x][at / 16][at % 16 + e], a.scale_log2e, -norm));
-          }
-        });
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[1][16 - E + e] += p[e];
+      if (!take_other) {
+        matrix_run<2 * KS, LOOK>(read, [&](auto m) { s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]); });
         return;
       }
-      matrix_run<2 * KS, LOOK>(read, [&](auto m) { s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]); });
-      if (!with_other) return;
+      float p[E];
+      asm volatile("" : "+v"(other));              // (or the arithmetic below would be done ahead of the branch)
+      matrix_run<2 * KS, LOOK>(read, [&](auto m) {
+        s[x][m % 2] = mfma32(k[m % 2][m / 2], buf[m / 2 % NBUF], m < 2 ? zero : s[x][m % 2]);
+        // an exponential is added one instruction later, when it is there
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const float p = exp2_fast(__builtin_fmaf(s[1 - x][e / 16][e % 16], a.scale_log2e, -other.norm));
-        acc[e / 16][e % 16] += 32 * (e / 16) + 8 * (e % 16 >> 2) + (e & 3) <= other.see ? p : 0.f;
-      }
+        for (int e = 0; e < E; ++e) {
+          constexpr int at = m * E;
+          if constexpr (m > 0) acc[(at - E) / 16][(at - E) % 16 + e] += p[e];
+          p[e] = exp2_fast(__builtin_fmaf(s[1 - x][at / 16][at % 16 + e], a.scale_log2e, -other));
+        }
+      });
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[1][16 - E + e] += p[e];
     };
-    Rows r[2] = {{INFINITY, 63, false}, {INFINITY, 63, false}};
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 1> odd{};
+    bool left = false;                             // scores in s[1] whose exponentials have not been taken, and their rows' norm
+    float left_norm = 0.f;
+    auto take_left = [&] {
+      asm volatile("" : "+v"(left_norm));
+#pragma unroll
+      for (int e = 0; e < 32; ++e) acc[e / 16][e % 16] += exp2_fast(__builtin_fmaf(s[1][e / 16][e % 16], a.scale_log2e, -left_norm));
+    };
     for (int t = t0; t < t1; ++t) {
-      // this wave's copies of tile t have landed when at most those of tile t + 1 are under way
-      if (t + 1 < t1) wait_copies<PASSES + 1>();
+      // this wave's copies of tile t have landed; with a ring of three those of tile t + 1 may be under way
+      if (kWeightRing == 3 && t + 1 < t1) wait_copies<PASSES + kWeightRows / 64>();
       else wait_async();
       __syncthreads();
-      if (t + 2 < t1) copy_tile(t + 2);
-      Rows now[2] = {{norm_of(2 * t), 63, false}, {norm_of(2 * t + 1), 63, false}};
-      if (!whole(t)) {
+      if (t + kWeightRing - 1 < t1) copy_tile(t + kWeightRing - 1);
+      lo_q += (t % kWeightRing) * TILE;
+      if (unmasked(t)) {
+        float norm[BLOCKS];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          row_of(2 * t + x, now[x].norm, now[x].see);
-          now[x].masked = __builtin_amdgcn_ballot_w64(now[x].see < 63 - 4 * g) != 0;
+        for (int j = 0; j < BLOCKS; ++j) norm[j] = norm_of(t * BLOCKS + j);
+        scores(even, left, left_norm);
+#pragma unroll
+        for (int j = 1; j < BLOCKS; ++j) {
+          lo_q += 32 * D * 2;
+          if (j & 1) scores(odd, true, norm[j - 1]);
+          else scores(even, true, norm[j - 1]);
+        }
+        left = true;
+        left_norm = norm[BLOCKS - 1];
+      } else {
+        if (left) take_left();
+        left = false;
+        for (int j = 0; j < BLOCKS; ++j) {
+          if (j > 0) lo_q += 32 * D * 2;
+          scores(even, false, 0.f);
+          const int rh = (t * BLOCKS + j) * 32 + (lane & 31), rc = rh < rows ? rh : rows - 1;
+          const int64_t far = rel + (int)((unsigned)rc % (unsigned)vis);      // last key of the wave that the lane's row sees
+          const int see = (far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
+          const float norm = norm_of(t * BLOCKS + j);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float p = exp2_fast(__builtin_fmaf(s[0][e / 16][e % 16], a.scale_log2e, -norm));
+            acc[e / 16][e % 16] += 32 * (e / 16) + 8 * (e % 16 >> 2) + (e & 3) <= see ? p : 0.f;
+          }
         }
       }
-      lo_q += (t % 3) * TILE;
-      scores(std::integral_constant<int, 0>{}, r[1], t > t0);
-      lo_q += 32 * D * 2;
-      scores(std::integral_constant<int, 1>{}, now[0], true);
-      lo_q -= 32 * D * 2 + (t % 3) * TILE;
-      r[1] = now[1];
+      lo_q -= (BLOCKS - 1) * 32 * D * 2 + (t % kWeightRing) * TILE;
     }
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const float p = exp2_fast(__builtin_fmaf(s[1][e / 16][e % 16], a.scale_log2e, -r[1].norm));
-      acc[e / 16][e % 16] += 32 * (e / 16) + 8 * (e % 16 >> 2) + (e & 3) <= r[1].see ? p : 0.f;
-    }
+    if (left) take_left();
   }
-  // over the 32 rows of a half-wave
+  // over the 32 rows of a half-wave; lane n of it keeps element n
+  float mine = 0.f;
+  const int n = lane & 31;
+#pragma unroll
+  for (int e = 0; e < 32; ++e) {
+    const float v = half_sum(acc[e / 16][e % 16]);
+    mine = n == e ? v : mine;
+  }
   __syncthreads();
   float* const out = reinterpret_cast<float*>(smem) + 64 * wave_u;
-#pragma unroll
-  for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float v = half_sum(acc[kb][i]);
-      if ((lane & 31) == 0) out[32 * kb + 8 * (i >> 2) + 4 * g + (i & 3)] = v;
-    }
+  out[32 * (n / 16) + 8 * (n % 16 >> 2) + 4 * g + (n & 3)] = mine;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   const int64_t key = wave_key0 + lane;
@@ -321,6 +341,12 @@ static hipError_t launch_weights_t(const Kv8WeightArgs& a, bool few, hipStream_t
   hipLaunchKernelGGL(kv8_weights_kernel<D>, dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), kv8_weights_lds_bytes<D>(), st, a);
   if (a.n_parts > 1) hipLaunchKernelGGL(kv8_weights_sum_kernel, dim3((unsigned)((keys * planes + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError();
+}
+hipError_t opt_in_kv8_evict_kernels() {
+  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
+  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_weights_kernel<128>), attr, (int)kv8_weights_lds_bytes<128>());
+  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_weights_kernel<64>), attr, (int)kv8_weights_lds_bytes<64>());
+  return e;
 }
 hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hipStream_t st) {
   return head_dim == 128 ? launch_weights_t<128>(a, few, st) : launch_weights_t<64>(a, few, st);
