@@ -111,11 +111,13 @@ template <int D>
 __global__ __launch_bounds__(256) void kv8_load_kernel(const Kv8CopyArgs a) {
   constexpr int NC = D / 8;
   const Kv8Cache& k = a.cache;
-  const int64_t gid = (int64_t)blockIdx.x * 256 + threadIdx.x, rh = gid / NC;      // (batch index, row, head) flattened
-  const int c = (int)(gid - rh * NC);
-  if (rh >= a.batch * a.rows * k.n_kv_heads) return;
-  const int64_t br = rh / k.n_kv_heads, b = br / a.rows, r = br - b * a.rows;
-  const int h = (int)(rh - br * k.n_kv_heads);
+  // (less than 2^27 rows of all heads: 32 bits, in which a division is a fifth of the instructions)
+  const uint32_t gid = blockIdx.x * 256u + threadIdx.x, rh = gid / NC, rows = (uint32_t)a.rows;      // (batch index, row, head) flattened
+  const int c = (int)(gid % NC);
+  if (rh >= (uint32_t)a.batch * rows * (uint32_t)k.n_kv_heads) return;
+  const uint32_t br = rh / (uint32_t)k.n_kv_heads, bu = br / rows;
+  const int64_t b = bu, r = br - bu * rows;
+  const int h = (int)(rh - br * (uint32_t)k.n_kv_heads);
   const Kv8Operand from = blockIdx.y == 0 ? k.k : k.v;
   const u32x2 x = *reinterpret_cast<const u32x2*>(from.codes + b * k.stride_b + (a.position + r) * k.stride_s + h * k.stride_h + c * 8);
   const float unit = kv8_scale(from.scales[kv8_scale_at(k, b, a.position + r, h)]);

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
   const int64_t row = w.block * ROWS + lane / LANES;
   if (row >= a.total_rows) return;                                    // (whole heads' lanes leave together)
   const RotateSide& s = a.side[w.side];
-  const int64_t b = row / a.rows, r = row - b * a.rows;
+  const int64_t b = (uint32_t)row / (uint32_t)a.rows, r = row - b * a.rows;      // (less than 2^31 rows)
   Turn<D, INTERLEAVED> t;
   t.init(a, lane);
   const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;
@@ -157,7 +157,7 @@ SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, I
   for (int64_t block = w.block; block < a.row_blocks; block += a.wave_blocks) {
     const int64_t row = block * ROWS + lane / LANES;
     if (row >= a.total_rows) break;
-    const int64_t b = row / a.rows, r = row - b * a.rows;
+    const int64_t b = (uint32_t)row / (uint32_t)a.rows, r = row - b * a.rows;
     const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;
     const dout_t* d = static_cast<const dout_t*>(s.d_out) + b * s.out_stride_b + r * s.out_stride_s + w.first * s.out_stride_h;
     bf16x8 lo[N], hi[N];
