@@ -104,6 +104,7 @@ SP_DEV RotateWave rotate_wave(const RotateArgs& a, int wave_u) {
   return {side, first, left < a.heads_wave ? left : a.heads_wave, (int64_t)(blockIdx.x / (unsigned)sets) * 4 + wave_u};
 }
 
+// 4096 rows of 80 heads of 128: 37 us, 168 MB at 4.5 TB/s, where a copy has 4.9; vector units busy 39 % (2 heads a wave 41 us, 8 41).
 template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
   constexpr int LANES = D / 16, ROWS = 64 / LANES, N = kRotateFwdHeads;
@@ -145,7 +146,9 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
 }
 
 // The gradient.  The weights' gradients are summed in the lanes over the rows and heads of a wave, over the waves of a workgroup in LDS, and over the
-// workgroups by rotate_weights_kernel, all in a fixed order.
+// workgroups by rotate_weights_kernel, all in a fixed order.  16384 rows of 8 query heads and a key head of 128 (gradients in bf16 and float32): 27 us, 117 MB at
+// 4.4 TB/s, and 4 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
+// block ahead do not fit the registers).
 template <int D, bool INTERLEAVED, bool DOUT_F32>
 SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, INTERLEAVED>& t, int lane, float (&dw)[16]) {
   constexpr int LANES = D / 16, ROWS = 64 / LANES, N = kRotateBwdHeads;
