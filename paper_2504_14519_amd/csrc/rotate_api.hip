@@ -1,4 +1,5 @@
 // C ABI of the norm and rotation of queries and keys: argument checks, launches.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -14,7 +15,7 @@ int check(const slimpipe_rotate_params* p) {
   if (p->batch < 1 || p->rows < 1 || p->n_q_heads < 0 || p->n_kv_heads < 0 || p->n_q_heads > 65535 || p->n_kv_heads > 65535) return SLIMPIPE_EINVAL_SHAPE;
   if (p->n_q_heads + p->n_kv_heads < 1 || (p->head_dim != 64 && p->head_dim != 128)) return SLIMPIPE_EINVAL_SHAPE;
   if (p->rotate_dim < 0 || p->rotate_dim > p->head_dim || p->rotate_dim % 16 != 0) return SLIMPIPE_EINVAL_SHAPE;
-  if (!(p->eps > 0.f) || !isfinite(p->eps)) return SLIMPIPE_EINVAL_SHAPE;
+  if (!(p->eps >= FLT_MIN) || !isfinite(p->eps)) return SLIMPIPE_EINVAL_SHAPE;      // (1 / sqrt(eps) stays finite: rows of zeros stay zeros)
   const int64_t rows = (int64_t)p->batch * p->rows;
   if (rows >= (int64_t)1 << 31 || rows * (p->n_q_heads + p->n_kv_heads) >= (int64_t)1 << 31) return SLIMPIPE_EINVAL_SHAPE;
   const int64_t far = (int64_t)1 << 52;      // (a position is a double on its way to an angle)

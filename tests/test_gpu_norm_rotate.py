@@ -241,6 +241,18 @@ def test_zero_rows_and_values_that_are_not_finite(sp):
     assert torch.isfinite(dq[0, 3, 1].float()).all() and dq[0, 3, 1].abs().max() > 100
 
 
+def test_smallest_eps_and_rows_of_zeros(sp):
+    import torch
+    x, q, k, wq, wk = tensors(1, 8, 4, 2, 64, 25)
+    q[0, 2] = 0.0
+    f = torch.from_numpy(frequencies(64)).cuda()
+    eps = 2.0 ** -126
+    out = sp.slimpipe_attn_norm_rotate(q, k, wq, wk, f, 7, eps)
+    assert (out[0][0, 2] == 0).all() and all(torch.isfinite(t.float()).all() for t in out)
+    dq = sp.slimpipe_attn_norm_rotate_bwd(q, k, wq, wk, f, 7, torch.zeros_like(q), torch.zeros_like(k), eps)[0]
+    assert (dq == 0).all()
+
+
 def test_captured(sp):
     """Both directions in a captured graph, replayed on other inputs, against eager calls."""
     import torch
@@ -269,3 +281,48 @@ def test_captured(sp):
         got = [t.clone() for t in out + grads]
         calls()
         assert all(torch.equal(a, b) for a, b in zip(got, out + grads))
+
+
+def test_training_over_slices(sp):
+    """Norm, rotation and attention of a sequence cut into slices, forward and backward through the calls as a training step makes them, against 64-bit
+    automatic differentiation of the whole sequence.  Queries, keys, outputs, dq and dS are bf16 on the way: gradients within 2e-2 of their norm, the bar of the attention's
+    own gradients."""
+    import torch
+    say("norm_rotate, attention, two slices")
+    B, n, slices, Hq, Hkv, D = 2, 128, 2, 4, 2, 64
+    step = n // slices
+    x, q, k, wq, wk = tensors(B, n, Hq, Hkv, D, 41)
+    v = x[:, :, Hq + Hkv:].contiguous()
+    freq = torch.from_numpy(frequencies(D)).cuda()
+    do = torch.randn(q.shape, device="cuda").to(torch.bfloat16)
+    prefix = torch.zeros(k.shape, device="cuda", dtype=torch.bfloat16)
+    saved = []
+    for i in range(slices):
+        r = slice(i * step, (i + 1) * step)
+        turned, _ = sp.slimpipe_attn_norm_rotate(q[:, r], k[:, r], wq, wk, freq, r.start, EPS, k_out=prefix[:, r])
+        saved.append((r, turned) + sp.slimpipe_attn_fwd(turned, prefix, v, r.start, 0, r.stop))
+    dk, dv = torch.zeros((2,) + k.shape, device="cuda")
+    dx = torch.zeros_like(x)
+    dw = [torch.zeros(D, device="cuda") for _ in range(2)]
+    for r, turned, out, lse in reversed(saved):
+        dq = sp.slimpipe_attn_bwd(turned, prefix, v, out, do[:, r], lse, r.start, 0, r.stop, dk, dv)
+        sp.slimpipe_attn_norm_rotate_bwd(q[:, r], k[:, r], wq, wk, freq, r.start, dq, dk[:, r], EPS, dq=dx[:, r, :Hq], dk=dx[:, r, Hq:Hq + Hkv],
+                                         dq_weight=dw[0], dk_weight=dw[1], weight_accumulate=True)
+    leaf = [t.detach().cpu().double().requires_grad_() for t in (q, k, v, wq, wk)]
+    angle = torch.arange(n, dtype=torch.float64)[:, None] * freq.cpu()
+    c, s = angle.cos()[:, None], angle.sin()[:, None]
+
+    def turn(t, w):
+        y = t / torch.sqrt((t * t).mean(-1, keepdim=True) + EPS) * w
+        a, b = y[..., :D // 2], y[..., D // 2:]
+        return torch.cat((a * c - b * s, b * c + a * s), -1)
+    qq, kk = turn(leaf[0], leaf[3]), turn(leaf[1], leaf[4]).repeat_interleave(Hq // Hkv, 2)
+    vv = leaf[2].repeat_interleave(Hq // Hkv, 2)
+    score = (qq.transpose(1, 2) @ kk.permute(0, 2, 3, 1).contiguous()) / D ** 0.5
+    score = score.masked_fill(torch.ones(n, n).triu(1).bool(), float("-inf"))
+    out = (score.softmax(-1) @ vv.transpose(1, 2)).transpose(1, 2)
+    (out * do.cpu().double()).sum().backward()
+    got = [dx[:, :, :Hq], dx[:, :, Hq:Hq + Hkv], dv, dw[0], dw[1]]
+    for g, t in zip(got, leaf):
+        g = torch.from_numpy(host_f64(g))
+        assert float((g - t.grad).norm() / t.grad.norm()) <= 2e-2

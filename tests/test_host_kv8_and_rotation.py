@@ -173,7 +173,7 @@ def test_norm_rotate_refuses(sp, call):
     assert call(sp, None) == NULL
     for change, code in ((dict(batch=0), SHAPE), (dict(rows=0), SHAPE), (dict(n_q_heads=-1), SHAPE), (dict(n_q_heads=0, n_kv_heads=0), SHAPE),
                          (dict(n_q_heads=65536), SHAPE), (dict(head_dim=96), SHAPE), (dict(rotate_dim=8), SHAPE), (dict(rotate_dim=144), SHAPE),
-                         (dict(rotate_dim=-16), SHAPE), (dict(eps=0.0), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE),
+                         (dict(rotate_dim=-16), SHAPE), (dict(eps=0.0), SHAPE), (dict(eps=1e-40), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE),
                          (dict(batch=1 << 16, rows=1 << 15), SHAPE), (dict(batch=1 << 14, rows=1 << 14), SHAPE), (dict(position=-1), RANGE),
                          (dict(position=(1 << 52) - 99), RANGE), (dict(q_stride_s=4), STRIDE), (dict(ko_stride_h=64), STRIDE), (dict(qo_stride_b=0), STRIDE),
                          (dict(k_stride_h=-128), STRIDE)):
