@@ -149,32 +149,32 @@ hipError_t launch_kv8_load(const Kv8CopyArgs& a, int head_dim, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------------------------ attention
-template <int D>
+template <int D, int NW>
 constexpr size_t kv8_fwd_lds_bytes() {         // two slots of converted K and V tiles; then the output rows
-  constexpr size_t rings = (size_t)4 * 64 * D * 2, rows = (size_t)4 * 32 * kOutRow<D> * 4;
+  constexpr size_t rings = (size_t)4 * 64 * D * 2, rows = (size_t)NW * 32 * kOutRow<D> * 4;
   return rings > rows ? rings : rows;
 }
 
-// Slices of up to 1024 rows of a kv head (or where there is no room for a bf16 copy of the keys): 128 rows a workgroup, 32 a wave (row_tile.hpp).  Codes of a tile of
-// 64 keys are fetched one tile ahead into registers and converted into LDS for all four waves at once.  256 rows of 40 heads on 16640 keys: 137 us (630
-// TFLOP/s; the bf16 call 100).  Four waves share a converted tile where eight share one of the dense kernel, and their phases are not kept apart: 4096 rows of 8 heads
-// on 32768 keys 572 us, by the copy 444.
-template <int D>
-__global__ __launch_bounds__(256, 2) void kv8_fwd_kernel(const Kv8Args a) {
-  constexpr int BN = 64, TILE = BN * D * 2, NP = D / 16, PER = 2 * BN * NP / 256;      // pieces of 16 elements of a row; of a thread, K and V
+// Slices of less than 2048 rows of a kv head (or where there is no room for a bf16 copy of the keys): 256 or 128 rows a workgroup of NW waves, 32 a wave
+// (row_tile.hpp).  Codes of a tile of 64 keys are fetched one tile ahead into registers and converted into LDS for all waves at once.  256 rows of 40 heads on
+// 16640 keys: 104 us (830 TFLOP/s, the fold of three ranges included), and 102 on a bf16 cache; 4096 rows of 8 heads on 32768 keys 513 us, by the copy 455:
+// the waves' matrix and vector phases are not kept apart as in the dense kernel.
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void kv8_fwd_kernel(const Kv8Args a) {
+  constexpr int BN = 64, TILE = BN * D * 2, NP = D / 16, PER = 2 * BN * NP / (NW * 64), ROWS = NW * 32;      // pieces of 16 elements of a row; of a thread, K and V
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   const Kv8Cache& kv = a.cache;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave_u = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = a.group * a.s_q, blocks = (rows + 127) / 128;
+  const int rows = a.group * a.s_q, blocks = (rows + ROWS - 1) / ROWS;
   const int part_i = blockIdx.x / blocks, blk = blocks - 1 - (blockIdx.x - part_i * blocks);
   const int plane = blockIdx.y, b = plane / kv.n_kv_heads, hk = plane - b * kv.n_kv_heads;
-  const int rh = blk * 128 + wave_u * 32 + (lane & 31);
+  const int rh = blk * ROWS + wave_u * 32 + (lane & 31);
   const PlaneRow my = plane_row(a.s_q, a.group, hk, rh < rows ? rh : rows - 1);
   const int64_t lo = a.kv_begin + (int64_t)part_i * a.part_keys;
   int64_t hi = lo + a.part_keys < a.kv_end ? lo + a.part_keys : a.kv_end;
   // last row of the block: of its head, or of the head before where the block holds the end of one
   if (a.causal) {
-    const int r0 = blk * 128, r1 = r0 + 127 < rows ? r0 + 127 : rows - 1;
+    const int r0 = blk * ROWS, r1 = r0 + ROWS - 1 < rows ? r0 + ROWS - 1 : rows - 1;
     const int64_t last = r0 / a.s_q == r1 / a.s_q ? r1 % a.s_q : a.s_q - 1;
     if (a.q_offset + last + 1 < hi) hi = a.q_offset + last + 1;
   }
@@ -187,9 +187,9 @@ __global__ __launch_bounds__(256, 2) void kv8_fwd_kernel(const Kv8Args a) {
   // This thread's pieces: a wave takes 16 keys of K or V and four pieces of each at a time (sixteen rows in a column of chunks: no bank twice in the LDS
   // writes)
   constexpr int RUNS = BN / 16 * (NP / 4);
-  auto piece_kv = [&](int n) { return (n * 4 + wave_u) / RUNS; };
-  auto piece_key = [&](int n) { return (n * 4 + wave_u) % RUNS / (NP / 4) * 16 + (lane & 15); };
-  auto piece_at = [&](int n) { return (n * 4 + wave_u) % (NP / 4) * 4 + (lane >> 4); };
+  auto piece_kv = [&](int n) { return (n * NW + wave_u) / RUNS; };
+  auto piece_key = [&](int n) { return (n * NW + wave_u) % RUNS / (NP / 4) * 16 + (lane & 15); };
+  auto piece_at = [&](int n) { return (n * NW + wave_u) % (NP / 4) * 4 + (lane >> 4); };
   const int64_t base = (int64_t)b * kv.stride_b + (int64_t)hk * kv.stride_h + lo * kv.stride_s;
   u32x4 codes[PER];
   uint32_t scales[PER];
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256, 2) void kv8_fwd_kernel(const Kv8Args a) {
   float* const part = reinterpret_cast<float*>(smem) + wave_u * 32 * kOutRow<D>;
   put_rows<D>(part, st.o, norm, lane);
   const int64_t row = ((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r;
-  const int n_mine = rows - (blk * 128 + wave_u * 32);
+  const int n_mine = rows - (blk * ROWS + wave_u * 32);
   if (a.n_parts > 1) {
     const int64_t slot = row * a.n_parts + part_i;
     if (lane < 32 && lane < n_mine) a.part_lse[slot] = lse;
@@ -495,24 +495,37 @@ static void launch_few_t(const Kv8Args& a, hipStream_t st) {
   hipLaunchKernelGGL((kv8_few_kernel<D, SETS>), dim3(a.n_parts > 1 ? (unsigned)a.n_parts * planes : (planes + 7) / 8 * 8), dim3(256),
                      (kv8_few_lds_bytes<D, SETS>()), st, a);
 }
-template <int D>
-static void launch_fwd_t(const Kv8Args& a, bool few, hipStream_t st) {
-  const int rows = a.group * a.s_q;
-  if (few) rows <= 16 ? launch_few_t<D, 1>(a, st) : launch_few_t<D, 2>(a, st);
-  else hipLaunchKernelGGL(kv8_fwd_kernel<D>, dim3((unsigned)a.n_parts * (unsigned)((rows + 127) / 128), (unsigned)(a.batch * a.cache.n_kv_heads)), dim3(256),
-                          kv8_fwd_lds_bytes<D>(), st, a);
+template <int D, int NW>
+static void launch_slice_t(const Kv8Args& a, hipStream_t st) {
+  const unsigned blocks = (unsigned)((a.group * a.s_q + NW * 32 - 1) / (NW * 32));
+  hipLaunchKernelGGL((kv8_fwd_kernel<D, NW>), dim3((unsigned)a.n_parts * blocks, (unsigned)(a.batch * a.cache.n_kv_heads)), dim3(NW * 64),
+                     (kv8_fwd_lds_bytes<D, NW>()), st, a);
 }
-hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, bool few, hipStream_t st) {
-  if (head_dim == 128) launch_fwd_t<128>(a, few, st);
-  else launch_fwd_t<64>(a, few, st);
+template <int D>
+static void launch_fwd_t(const Kv8Args& a, Kv8Kernel kernel, hipStream_t st) {
+  switch (kernel) {
+    case Kv8Kernel::few: a.group * a.s_q <= 16 ? launch_few_t<D, 1>(a, st) : launch_few_t<D, 2>(a, st); break;
+    case Kv8Kernel::four_waves: launch_slice_t<D, 4>(a, st); break;
+    case Kv8Kernel::eight_waves: launch_slice_t<D, 8>(a, st);
+  }
+}
+hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, Kv8Kernel kernel, hipStream_t st) {
+  if (head_dim == 128) launch_fwd_t<128>(a, kernel, st);
+  else launch_fwd_t<64>(a, kernel, st);
   return hipGetLastError();
 }
 
+template <int D, int NW>
+static hipError_t opt_in_slice() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_fwd_kernel<D, NW>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kv8_fwd_lds_bytes<D, NW>());
+}
 hipError_t opt_in_kv8_kernels() {
-  const hipFuncAttribute attr = hipFuncAttributeMaxDynamicSharedMemorySize;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_fwd_kernel<128>), attr, (int)kv8_fwd_lds_bytes<128>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_fwd_kernel<64>), attr, (int)kv8_fwd_lds_bytes<64>());
-  if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_few_kernel<128, 2>), attr, (int)kv8_few_lds_bytes<128, 2>());
+  hipError_t e = opt_in_slice<128, 4>();
+  if (e == hipSuccess) e = opt_in_slice<64, 4>();
+  if (e == hipSuccess) e = opt_in_slice<128, 8>();
+  if (e == hipSuccess) e = opt_in_slice<64, 8>();
+  if (e == hipSuccess)
+    e = hipFuncSetAttribute(reinterpret_cast<const void*>(&kv8_few_kernel<128, 2>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)kv8_few_lds_bytes<128, 2>());
   return e;
 }
 

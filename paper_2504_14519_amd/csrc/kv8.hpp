@@ -77,11 +77,13 @@ struct Kv8GatherArgs {
 
 hipError_t launch_kv8_store(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
 hipError_t launch_kv8_load(const Kv8CopyArgs& a, int head_dim, hipStream_t st);
-hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, bool few, hipStream_t st);      // few: group * s_q <= kKv8FewRows
+enum class Kv8Kernel { few, four_waves, eight_waves };      // few: group * s_q <= kKv8FewRows; else 128 or 256 rows a workgroup
+hipError_t launch_kv8_fwd(const Kv8Args& a, int head_dim, Kv8Kernel kernel, hipStream_t st);
 constexpr int kKv8FewRows = 32;
-// Rows of a plane from which a bf16 copy of the keys and slimpipe_attn_fwd are faster than tiles converted in the kernel (us with the copy and without, 32K keys: 512
-// rows of 8 heads on one 39 and 29, 1024 43 and 41, 4096 77 and 92, 32768 444 and 572; 40 heads on 17K keys: 512 rows 254 and 250, 1024 423 and 490)
-constexpr int kKv8CopyRows = 1024;
+// Rows of a plane from which a bf16 copy of the keys and slimpipe_attn_fwd are faster than tiles converted in the kernel (us with the copy and without: 8 heads on one and
+// 32K keys, 512 rows 39 and 31, 1024 44 and 43, 2048 66 and 62, 4096 80 and 88, 32768 455 and 513; 40 heads on 17K keys, 512 rows 254 and 192, 1500 558 and 524,
+// 2048 762 and 842; 12 heads of 64 on four, 1800 rows 67 and 65, 4011 87 and 92)
+constexpr int kKv8CopyRows = 2048;
 hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hipStream_t st);
 hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st);
 hipError_t launch_kv8_gather(const Kv8GatherArgs& a, int head_dim, hipStream_t st);

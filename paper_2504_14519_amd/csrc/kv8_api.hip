@@ -55,10 +55,10 @@ int64_t few_parts(int64_t wgs, int64_t most, int64_t least_rounds, int64_t most_
   }
   return best;
 }
-// Key ranges of a slice: the fewest whose workgroups, two a compute unit at once, fill one to three rounds nearly, or those that fill them best (256
-// rows of 40 heads on 16640 keys, 80 workgroups a range: 6 ranges 137 us, 7 167).
-int64_t slice_parts(int64_t wgs, int64_t most) {
-  const int64_t places = 2 * (int64_t)compute_units();
+// Key ranges of a slice: the fewest whose workgroups, `a_unit` a compute unit at once, fill one to three rounds nearly, or those that fill them best (256
+// rows of 40 heads on 16640 keys, 80 workgroups of four waves a range: 6 ranges 137 us, 7 167).
+int64_t slice_parts(int64_t wgs, int64_t most, int64_t a_unit) {
+  const int64_t places = a_unit * compute_units();
   int64_t best = 1;
   double best_full = 0.;
   for (int64_t parts = 1; parts <= most && (parts == 1 || parts * wgs <= 3 * places); ++parts) {
@@ -69,27 +69,34 @@ int64_t slice_parts(int64_t wgs, int64_t most) {
   }
   return best;
 }
-// Key ranges that a call is cut into, a workgroup for each and each block of rows, so that the chip is full.
+// Which kernel, and key ranges that a call is cut into, a workgroup for each and each block of rows, so that the chip is full.  Eight waves share a converted tile
+// where four would convert it twice, but fill the chip later (us with eight and with four, 256 rows of 40 heads on 16640 keys 119 and 140, 800 rows of a kv head on
+// 32100 keys 38 and 39; 512 rows of one 33 and 29, 100 rows of 16 heads 51 and 47).
 struct Kv8Plan {
-  bool few;
+  Kv8Kernel kernel;
   int32_t parts;
   int64_t part_keys;
 };
+void cut_keys(Kv8Plan* plan, int64_t keys, int64_t parts) {
+  plan->parts = 1;
+  plan->part_keys = keys;
+  if (parts <= 1) return;
+  const int64_t unit = plan->kernel == Kv8Kernel::few ? 32 : 64;      // keys of a step
+  plan->part_keys = ((keys + parts - 1) / parts + unit - 1) / unit * unit;
+  plan->parts = (int32_t)((keys + plan->part_keys - 1) / plan->part_keys);
+}
 Kv8Plan plan_of(const slimpipe_attn_params* p) {
   const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin, rows = rows_of(p), planes = (int64_t)p->batch * p->n_kv_heads;
-  Kv8Plan plan{rows <= kKv8FewRows, 1, keys};
-  const int64_t least = plan.few ? 256 : 512;      // keys of a part
+  Kv8Plan plan{Kv8Kernel::few, 1, keys};
   int64_t parts;
-  if (plan.few) {
-    parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / least, 2, 6);
+  if (rows <= kKv8FewRows) {
+    parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / 256, 2, 6);
   } else {
-    parts = slice_parts(planes * ((rows + 127) / 128), keys / least);
+    const int64_t most = keys / 512, eight = planes * ((rows + 255) / 256);
+    plan.kernel = rows > 128 && eight * most >= compute_units() ? Kv8Kernel::eight_waves : Kv8Kernel::four_waves;
+    parts = plan.kernel == Kv8Kernel::eight_waves ? slice_parts(eight, most, 1) : slice_parts(planes * ((rows + 127) / 128), most, 2);
   }
-  if (parts > 1) {
-    const int64_t unit = plan.few ? 32 : 64;      // keys of a step
-    plan.part_keys = ((keys + parts - 1) / parts + unit - 1) / unit * unit;
-    plan.parts = (int32_t)((keys + plan.part_keys - 1) / plan.part_keys);
-  }
+  cut_keys(&plan, keys, parts);
   return plan;
 }
 // Sums of weights: key ranges of the kernel of few rows, or parts of a plane's rows, whose sums a second launch adds up.
@@ -264,11 +271,18 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
   if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
   if (rc != SLIMPIPE_OK) return rc;
   if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse)) return SLIMPIPE_EINVAL_ALIGN;
-  const Kv8Plan plan = plan_of(p);
-  if (workspace_bytes < bytes_of(p, plan) || (plan.parts > 1 && !workspace)) return SLIMPIPE_EWORKSPACE;
   if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
+  if (!workspace) workspace_bytes = 0;
+  Kv8Plan plan = plan_of(p);
+  const bool may_copy = copies(p), copy = may_copy && workspace_bytes >= 2 * copy_bytes(p);
+  if (!copy && workspace_bytes < bytes_of(p, plan)) {
+    if (!may_copy) return SLIMPIPE_EWORKSPACE;
+    // (a long slice without room for the copy: as many key ranges as there is room for)
+    const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin;
+    for (int64_t parts = plan.parts - 1; workspace_bytes < bytes_of(p, plan); --parts) cut_keys(&plan, keys, parts);
+  }
   const Kv8Cache cache = cache_of(p, block_len, k_codes, k_scales, v_codes, v_scales);
-  if (workspace && copies(p) && workspace_bytes >= 2 * copy_bytes(p)) {
+  if (copy) {
     if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
     return fwd_by_copy(p, cache, q_slice, out, lse, static_cast<char*>(workspace), workspace_bytes, hip_stream);
   }
@@ -292,7 +306,7 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
   }
   if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (launch_kv8_fwd(a, p->head_dim, plan.few, st) != hipSuccess) return SLIMPIPE_ELAUNCH;
+  if (launch_kv8_fwd(a, p->head_dim, plan.kernel, st) != hipSuccess) return SLIMPIPE_ELAUNCH;
   if (plan.parts <= 1) return SLIMPIPE_OK;
   PartMergeArgs m;
   m.part_out = a.part_out; m.part_f32 = 1; m.part_scale = nullptr; m.part_lse = a.part_lse; m.parts = plan.parts; m.s_q = p->s_q; m.n_q_heads = p->n_q_heads; m.out_f32 = a.out_f32;

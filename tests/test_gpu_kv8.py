@@ -136,6 +136,9 @@ SHAPES = [
     (1, 300, 3700, 3, 1, 128, True, None, 128),        # a slice, keys cut into parts
     (1, 700, 2900, 8, 2, 128, True, None, 64),
     (1, 200, 900, 2, 2, 128, False, None, 32),
+    (8, 150, 2100, 8, 8, 64, True, None, 32),          # enough of it for workgroups of eight waves, one part and several
+    (4, 300, 1000, 16, 16, 128, True, (500, 1300), 64),
+    (3, 400, 1300, 9, 3, 64, False, None, 128),
     (1, 2, 900, 4, 4, 64, False, (3, 890), 32),
     (2, 130, 400, 4, 1, 128, True, (100, 480), 16),
     (1, 130, 400, 4, 1, 64, True, (450, 500), 64),     # early rows see nothing
@@ -164,9 +167,9 @@ def test_forward(sp, case):
 
 
 def test_long_slice_with_and_without_room_for_a_copy(sp):
-    """1200 rows of a kv head, the whole range and a piece of it: by a bf16 copy of the keys, and tile by tile where the workspace has no room for one."""
+    """2200 rows of a kv head, the whole range and a piece of it: by a bf16 copy of the keys, and tile by tile where the workspace has no room for one."""
     import torch
-    B, s, off, Hq, Hkv, D, L = 2, 600, 333, 4, 2, 64, 32
+    B, s, off, Hq, Hkv, D, L = 1, 1100, 333, 4, 2, 64, 32
     N = off + s
     cache, k, v = random_cache(sp, B, N, Hkv, D, L)
     bits = normal_bf16((B, s, Hq, D), 43, "q", 1)
@@ -177,14 +180,14 @@ def test_long_slice_with_and_without_room_for_a_copy(sp):
         need = sp.slimpipe_attn_kv8_workspace_bytes(dev_bf16(bits), cache, off, begin, end)
         copy = 2 * B * (end - begin) * Hkv * D * 2
         assert need >= copy
-        for room in (need, copy - 256):
+        for room in (need, copy, copy - 256, 1 << 20, 0):
             ws = torch.empty(room, device="cuda", dtype=torch.uint8)
             out, lse = sp.slimpipe_attn_fwd_kv8(dev_bf16(bits), cache, off, begin, end, workspace=ws)
             bu.check("out", host_f64(out), r.out, r.out_tol)
             bu.check("lse", host_f64(lse), r.lse, r.lse_tol)
 
 
-@pytest.mark.parametrize("s", [2, 140, 520])
+@pytest.mark.parametrize("s", [2, 140, 520, 1100])
 def test_layouts_and_unseen_keys(sp, s):
     """Strided heads, a cache of another layout with NaN codes and scales behind the last seen key and before the first: the same bits."""
     import torch

@@ -135,6 +135,9 @@ def test_workspaces(sp):
     assert size(fwd, slice_) >= 2 * 1536 * 128 * 2
     # a piece of which early rows see nothing is converted tile by tile: no copy
     assert size(fwd, params(sp, kv_begin=1025)) < 2 * 511 * 128 * 2 + 512 * 8 * 129 * 4 * 2
+    early = params(sp, s_q=3000, kv_begin=1025, kv_end=4024)
+    need = size(fwd, early)
+    assert need > 0 and cached(sp, early, ws=None) == WORKSPACE and cached(sp, early, ws_bytes=need - 1) == WORKSPACE
     token = params(sp, s_q=1, q_offset=4095, kv_end=4096)
     need = size(fwd, token)
     assert 0 < need < 1 << 20 and size(fwd, params(sp, s_q=1, q_offset=100, kv_end=101)) == 0
