@@ -116,9 +116,15 @@ Kv8WeightPlan weight_plan_of(const slimpipe_attn_params* p) {
     }
     return plan;
   }
-  const int64_t wgs = planes * ((keys + kv8_weight_keys() - 1) / kv8_weight_keys()), want = 4 * (int64_t)compute_units();
-  int64_t parts = wgs > 0 ? (want + wgs - 1) / wgs : 1;
+  // Four workgroups a compute unit of 256 rows or more, or one a unit of 128 (a tile) where that leaves units idle (us of parts of 128 and of 256 rows: 652 rows of a kv
+  // head on 1547 keys 15.2 and 19.3, 948 on 3156 14.7 and 19.9; 3936 rows of two on 4660 27.9 and 25.6).
+  const int64_t wgs = planes * ((keys + kv8_weight_keys() - 1) / kv8_weight_keys()), units = compute_units();
+  int64_t parts = wgs > 0 ? (4 * units + wgs - 1) / wgs : 1;
   if (parts > rows / 256) parts = rows / 256;
+  if (parts * wgs < units && wgs > 0) {
+    parts = (units + wgs - 1) / wgs;
+    if (parts > (rows + 127) / 128) parts = (rows + 127) / 128;
+  }
   if (parts > 64) parts = 64;
   plan.parts = parts > 1 ? (int32_t)parts : 1;
   return plan;
