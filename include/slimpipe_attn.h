@@ -388,7 +388,7 @@ int slimpipe_attn_kv8_gather(const slimpipe_attn_params* p, int32_t block_len, c
  * and k (bf16, the q and k strides; dq may take the place of q or, with equal strides and bf16, of dq_out) and of the weights (float32 [head_dim],
  * overwritten, or added to when weight_accumulate; NULL: not wanted; only for weights that are given).  Sums run in a fixed order.
  *   workspace : slimpipe_attn_norm_rotate_workspace_bytes, needed when a weight's gradient is wanted (SLIMPIPE_EWORKSPACE).
- *   limits    : rotate_dim a multiple of 16, 0 .. head_dim; eps finite and at least 2^-126; heads 0 .. 65535, less than 2^31 rows of all heads
+ *   limits    : rotate_dim a multiple of 16, 0 .. head_dim; eps finite and at least 2^-126; heads 0 .. 65535, less than 2^28 rows of all heads
  *               (SLIMPIPE_EINVAL_SHAPE); position + rows <= 2^52 (SLIMPIPE_EINVAL_RANGE). */
 typedef struct slimpipe_rotate_params {
   int32_t batch;

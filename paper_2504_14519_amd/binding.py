@@ -50,11 +50,21 @@ class RotateParams(ctypes.Structure):
     ]
 
 
-# The parameter blocks as bytes, which the calls on the 8-bit cache and the norm and rotation pass (a Structure of as many fields takes twice as long to fill:
-# 0.5 us of a call)
-_pack_attn = struct.Struct("=6i4qfi12q").pack
-_pack_rotate = struct.Struct("=7if13q").pack
-assert len(_pack_attn(*[0] * 24)) == ctypes.sizeof(AttnParams) and len(_pack_rotate(*[0] * 21)) == ctypes.sizeof(RotateParams)
+def _packed(layout, structure):
+    """fields -> the bytes of a parameter block, which the calls on the 8-bit cache and the norm and rotation pass (a Structure of as many fields takes twice as
+    long to fill: 0.5 us of a call)."""
+    pack = struct.Struct(layout).pack
+
+    def packed(*fields):
+        try:
+            return pack(*fields)
+        except (struct.error, OverflowError) as e:
+            raise SlimpipeError("%s: %s" % (structure.__name__, e)) from None
+    assert len(packed(*[0] * len(structure._fields_))) == ctypes.sizeof(structure)
+    return packed
+
+
+_pack_attn, _pack_rotate = _packed("=6i4qfi12q", AttnParams), _packed("=7if13q", RotateParams)
 
 
 class BwdPlan(ctypes.Structure):

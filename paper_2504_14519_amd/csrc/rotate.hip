@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
   const int64_t row = w.block * ROWS + lane / LANES;
   if (row >= a.total_rows) return;                                    // (whole heads' lanes leave together)
   const RotateSide& s = a.side[w.side];
-  const int64_t b = (uint32_t)row / (uint32_t)a.rows, r = row - b * a.rows;      // (less than 2^31 rows)
+  const int64_t b = (uint32_t)row / (uint32_t)a.rows, r = row - b * a.rows;      // (less than 2^28 rows)
   Turn<D, INTERLEAVED> t;
   t.init(a, lane);
   const bf16_t* x = s.x + b * s.stride_b + r * s.stride_s + w.first * s.stride_h;

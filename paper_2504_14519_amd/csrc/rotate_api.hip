@@ -17,7 +17,7 @@ int check(const slimpipe_rotate_params* p) {
   if (p->rotate_dim < 0 || p->rotate_dim > p->head_dim || p->rotate_dim % 16 != 0) return SLIMPIPE_EINVAL_SHAPE;
   if (!(p->eps >= FLT_MIN) || !isfinite(p->eps)) return SLIMPIPE_EINVAL_SHAPE;      // (1 / sqrt(eps) stays finite: rows of zeros stay zeros)
   const int64_t rows = (int64_t)p->batch * p->rows;
-  if (rows >= (int64_t)1 << 31 || rows * (p->n_q_heads + p->n_kv_heads) >= (int64_t)1 << 31) return SLIMPIPE_EINVAL_SHAPE;
+  if (rows >= (int64_t)1 << 28 || rows * (p->n_q_heads + p->n_kv_heads) >= (int64_t)1 << 28) return SLIMPIPE_EINVAL_SHAPE;      // (less than 2^32 threads)
   const int64_t far = (int64_t)1 << 52;      // (a position is a double on its way to an angle)
   if (p->position < 0 || p->position > far - p->rows) return SLIMPIPE_EINVAL_RANGE;
   if (p->n_q_heads > 0 && !(stride_ok(p->q_stride_b) && stride_ok(p->q_stride_s) && stride_ok(p->q_stride_h) && stride_ok(p->qo_stride_b) &&

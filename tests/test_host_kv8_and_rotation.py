@@ -177,7 +177,8 @@ def test_norm_rotate_refuses(sp, call):
     for change, code in ((dict(batch=0), SHAPE), (dict(rows=0), SHAPE), (dict(n_q_heads=-1), SHAPE), (dict(n_q_heads=0, n_kv_heads=0), SHAPE),
                          (dict(n_q_heads=65536), SHAPE), (dict(head_dim=96), SHAPE), (dict(rotate_dim=8), SHAPE), (dict(rotate_dim=144), SHAPE),
                          (dict(rotate_dim=-16), SHAPE), (dict(eps=0.0), SHAPE), (dict(eps=1e-40), SHAPE), (dict(eps=float("nan")), SHAPE), (dict(eps=float("inf")), SHAPE),
-                         (dict(batch=1 << 16, rows=1 << 15), SHAPE), (dict(batch=1 << 14, rows=1 << 14), SHAPE), (dict(position=-1), RANGE),
+                         (dict(batch=1 << 16, rows=1 << 15), SHAPE), (dict(batch=1 << 14, rows=1 << 14), SHAPE),
+                         (dict(batch=1, rows=(1 << 28) // 10 + 1), SHAPE), (dict(batch=1, rows=1 << 28, n_q_heads=1, n_kv_heads=0), SHAPE), (dict(position=-1), RANGE),
                          (dict(position=(1 << 52) - 99), RANGE), (dict(q_stride_s=4), STRIDE), (dict(ko_stride_h=64), STRIDE), (dict(qo_stride_b=0), STRIDE),
                          (dict(k_stride_h=-128), STRIDE)):
         assert call(sp, rotation(sp, **change)) == code, change
@@ -314,6 +315,17 @@ def test_wrappers_beyond_single_tensors(wrapped):
     for block in (0, -32):
         with pytest.raises(sp.SlimpipeError):
             sp.slimpipe_attn_kv8_store(a["k"], a["v"], sp.KvCache8(*one(sp, a)[:4], block), 0)
+
+
+def test_wrappers_refuse_numbers_that_no_field_holds(wrapped):
+    sp, a = wrapped, right()
+    rotated = a["q"], a["k"], a["wq"], a["wk"], a["f"]
+    for call in (lambda: sp.slimpipe_attn_norm_rotate(*rotated, 0, eps=1e39), lambda: sp.slimpipe_attn_norm_rotate(*rotated, 1 << 63),
+                 lambda: sp.slimpipe_attn_norm_rotate(*rotated, 0.5), lambda: sp.slimpipe_attn_kv8_store(a["k"], a["v"], one(sp, a), 1 << 63),
+                 lambda: sp.slimpipe_attn_fwd_kv8(a["q"], one(sp, a), 0, 0, N, scale=1e39),
+                 lambda: sp.slimpipe_attn_kv8_weights(a["q"], one(sp, a), a["lse"], 0, -1 << 64, N)):
+        with pytest.raises(sp.SlimpipeError):
+            call()
 
 
 def test_a_load_of_no_rows(sp, monkeypatch):
