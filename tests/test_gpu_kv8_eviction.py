@@ -151,7 +151,8 @@ def spread(kind, shape, seed):
 @pytest.mark.parametrize("B,H,N,rows,keep,recent", [(1, 1, 1, 1, 1, 0), (1, 2, 70, 64, 1, 1), (2, 3, 1024, 1024, 1024, 7), (1, 1, 1025, 1025, 1, 0),
                                                     (2, 1, 5000, 4238, 2119, 337), (1, 4, 9000, 8193, 8000, 0), (1, 2, 20000, 20000, 500, 500),
                                                     (3, 2, 33333, 33331, 12345, 100), (1, 3, 140001, 140001, 33000, 1024), (1, 2, 40000, 40000, 40000, 7),
-                                                    (1, 2, 40000, 39999, 500, 500), (2, 1, 33000, 33000, 33000, 33000), (1, 1, 600000, 599999, 3, 1)])
+                                                    (1, 2, 40000, 39999, 500, 500), (2, 1, 33000, 33000, 33000, 33000), (1, 1, 600000, 599999, 3, 1),
+                                                    (2, 2, 16384, 16384, 9000, 50), (2, 2, 17000, 16385, 9000, 0), (1, 3, 30000, 28000, 27000, 900)])
 def test_keep(sp, kind, B, H, N, rows, keep, recent):
     import torch
     say("kv8 keep %s %r" % (kind, (B, H, N, rows, keep, recent)))

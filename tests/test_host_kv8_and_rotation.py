@@ -121,8 +121,8 @@ def test_keep(sp):
                          (dict(rows=40000, capacity=40000, ws=ODD), ALIGN)):
         assert keep(sp, **change) == code, change
     n = ctypes.c_size_t(7)
-    assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 32768, 100, ctypes.byref(n)) == 0 and n.value == 0
-    assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 32769, 100, ctypes.byref(n)) == 0 and n.value > 0
+    assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 16384, 100, ctypes.byref(n)) == 0 and n.value == 0
+    assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 16385, 100, ctypes.byref(n)) == 0 and n.value > 0
     assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 100, 101, ctypes.byref(n)) == RANGE
     assert sp.lib.slimpipe_attn_kv8_keep_workspace_bytes(4, 100, 50, None) == NULL
 
