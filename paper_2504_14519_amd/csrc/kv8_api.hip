@@ -55,7 +55,7 @@ int64_t few_parts(int64_t wgs, int64_t most, int64_t least_rounds, int64_t most_
   }
   return best;
 }
-// Key ranges of a slice: the fewest whose workgroups, `a_unit` a compute unit at once, fill one to three rounds nearly, or those that fill them best (256
+// Key ranges of a slice, or parts of its rows: the fewest whose workgroups, `a_unit` a compute unit at once, fill one to three rounds nearly, or those that fill them best (256
 // rows of 40 heads on 16640 keys, 80 workgroups of four waves a range: 6 ranges 137 us, 7 167).
 int64_t slice_parts(int64_t wgs, int64_t most, int64_t a_unit) {
   const int64_t places = a_unit * compute_units();
@@ -92,9 +92,18 @@ Kv8Plan plan_of(const slimpipe_attn_params* p) {
   if (rows <= kKv8FewRows) {
     parts = few_parts(planes / kv8_heads_wg(p->n_kv_heads), keys / 256, 2, 6);
   } else {
-    const int64_t most = keys / 512, eight = planes * ((rows + 255) / 256);
-    plan.kernel = rows > 128 && eight * most >= compute_units() ? Kv8Kernel::eight_waves : Kv8Kernel::four_waves;
-    parts = plan.kernel == Kv8Kernel::eight_waves ? slice_parts(eight, most, 1) : slice_parts(planes * ((rows + 127) / 128), most, 2);
+    const int64_t long_parts = keys / 512, eight = planes * ((rows + 255) / 256);
+    plan.kernel = rows > 128 && eight * long_parts >= compute_units() ? Kv8Kernel::eight_waves : Kv8Kernel::four_waves;
+    if (plan.kernel == Kv8Kernel::eight_waves) {
+      parts = slice_parts(eight, long_parts, 1);
+    } else {
+      // Ranges of 512 keys or more, or of 128 up to a workgroup a unit where that leaves units idle (us of 512 and of 128: 48 rows of 8 heads on 2 behind 1306 keys
+      // 24.8 and 15.8, 500 rows on 1000 keys 29.2 and 20.0).
+      const int64_t wgs = planes * ((rows + 127) / 128), units = compute_units();
+      int64_t most = long_parts;
+      if (most * wgs < units) most = keys / 128 < units / wgs ? keys / 128 : units / wgs;
+      parts = slice_parts(wgs, most, 2);
+    }
   }
   cut_keys(&plan, keys, parts);
   return plan;
@@ -116,11 +125,10 @@ Kv8WeightPlan weight_plan_of(const slimpipe_attn_params* p) {
     }
     return plan;
   }
-  // Four workgroups a compute unit of 256 rows or more, or one a unit of 128 (a tile) where that leaves units idle (us of parts of 128 and of 256 rows: 652 rows of a kv
+  // Parts of 256 rows or more that fill the chip, or one a unit of 128 (a tile) where that leaves units idle (us of parts of 128 and of 256 rows: 652 rows of a kv
   // head on 1547 keys 15.2 and 19.3, 948 on 3156 14.7 and 19.9; 3936 rows of two on 4660 27.9 and 25.6).
   const int64_t wgs = planes * ((keys + kv8_weight_keys() - 1) / kv8_weight_keys()), units = compute_units();
-  int64_t parts = wgs > 0 ? (4 * units + wgs - 1) / wgs : 1;
-  if (parts > rows / 256) parts = rows / 256;
+  int64_t parts = wgs > 0 ? slice_parts(wgs, rows / 256, 2) : 1;
   if (parts * wgs < units && wgs > 0) {
     parts = (units + wgs - 1) / wgs;
     if (parts > (rows + 127) / 128) parts = (rows + 127) / 128;
