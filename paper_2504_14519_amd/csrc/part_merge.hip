@@ -21,6 +21,37 @@ SP_DEV void put_result(const PartMergeArgs& a, int64_t row, int d, f32x4 x0, f32
   }
   if (d == 0) a.lse[row] = l == 0.f ? -INFINITY : m + __builtin_log2f(l) * kLn2;
 }
+// Adds N parts (s, s + step, ..) of 8 elements of a row, relative to the maximum m of all lse, their loads under way at once, also of those that add nothing
+// (calls of 1500 rows of 38 parts 73 us, one by one 81; of 1200 of 31 39 and 47; of 4000 of 8 26 and 28).
+template <int D, bool F32, int N>
+SP_DEV void add_parts(const PartMergeArgs& a, int64_t row, int d, int s, int step, f32x4& x0, f32x4& x1, float m, float& l) {
+  float lse[N], scale[N];
+  f32x4 y[N][2];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t part = row * a.parts + s + i * step;
+    lse[i] = a.part_lse[part];
+    if constexpr (F32) {
+      const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + part * D + d);
+      y[i][0] = src[0];
+      y[i][1] = src[1];
+    } else {
+      const f16x8 x = *reinterpret_cast<const f16x8*>(static_cast<const _Float16*>(a.part_out) + part * D + d);
+      scale[i] = a.part_scale[part];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { y[i][0][e] = (float)x[e]; y[i][1][e] = (float)x[4 + e]; }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (lse[i] == -INFINITY) continue;
+    float w = exp2_fast((lse[i] - m) * kLog2e);      // (m is -inf only where all are that or NaN, which gives NaN)
+    l += w;
+    if constexpr (!F32) w *= scale[i];
+    x0 += w * y[i][0];
+    x1 += w * y[i][1];
+  }
+}
 // Parts first, first + step, .. of 8 elements of a row: maximum of their lse, sum of weights, weighted sum.
 template <int D, bool F32>
 SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, int step, f32x4& x0, f32x4& x1, float& m, float& l) {
@@ -30,24 +61,11 @@ SP_DEV void fold_parts(const PartMergeArgs& a, int64_t row, int d, int first, in
   x0 = x1 = f32x4{0, 0, 0, 0};
 #pragma unroll 4
   for (int s = first; s < a.parts; s += step) m = fmaxf(m, lp[s]);
-#pragma unroll 4
-  for (int s = first; s < a.parts; s += step) {
-    const float ls = lp[s];
-    if (ls == -INFINITY) continue;
-    float w = exp2_fast((ls - m) * kLog2e);      // (m is -inf only where all are that or NaN, which gives NaN)
-    l += w;
-    const int64_t at = (row * a.parts + s) * D + d;
-    if constexpr (F32) {
-      const f32x4* src = reinterpret_cast<const f32x4*>(static_cast<const float*>(a.part_out) + at);
-      x0 += w * src[0];
-      x1 += w * src[1];
-    } else {
-      const f16x8 x = *reinterpret_cast<const f16x8*>(static_cast<const _Float16*>(a.part_out) + at);
-      w *= a.part_scale[row * a.parts + s];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) { x0[e] += w * (float)x[e]; x1[e] += w * (float)x[4 + e]; }
-    }
-  }
+  int s = first;
+  for (; s + 7 * step < a.parts; s += 8 * step) add_parts<D, F32, 8>(a, row, d, s, step, x0, x1, m, l);
+  if (s + 3 * step < a.parts) { add_parts<D, F32, 4>(a, row, d, s, step, x0, x1, m, l); s += 4 * step; }
+  if (s + step < a.parts) { add_parts<D, F32, 2>(a, row, d, s, step, x0, x1, m, l); s += 2 * step; }
+  if (s < a.parts) add_parts<D, F32, 1>(a, row, d, s, step, x0, x1, m, l);
 }
 
 // Many rows: D / 8 lanes a row.  Bound by the bytes: 65536 rows of 8 parts of 128 in 24 us (6.3 TB/s: they have just been written).
