@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
 //   sums               p = exp2(c s - norm) added in place: the lane's sums over its rows, over the lanes at the end
 // A pair costs the vector unit three instructions, one of them an exponential, beside 2 D flop: both units have about the same to do at D = 128, twice
 // as much the vector unit at 64.  So the scores of a block of 32 rows are computed while the exponentials of the block before are taken, instruction by instruction.
-// 4096 rows of 8 heads on 32768 keys of 128: 245 us, 1.05 PFLOP/s (with the exponentials behind the matrix instructions of the same block 274; tiles of 64 rows
+// 4096 rows of 8 heads on 32768 keys of 128: 247 us, 1.04 PFLOP/s (with the exponentials behind the matrix instructions of the same block 274; tiles of 64 rows
 // in a ring of three 244, but 368 and 318 us for 16384 rows of 4 heads of 64 on 32768 keys).
 constexpr int kWeightKeys = kv8_weight_keys(), kWeightRows = 128, kWeightRing = 2;
 template <int D>
@@ -355,7 +355,7 @@ hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hi
 // ------------------------------------------------------------------------------------ keep
 // The rows of a plane that are kept: the `recent` last ones and those of the others with the largest weights.  A radix selection (11, 11 and 10 bits) finds the
 // smallest weight that is taken and how many rows of exactly that weight are; a last walk writes the indices in order.  Counts alone cross threads, so
-// that the order in which they run shows nowhere.  4238 rows of 12 planes 7.5 us; 131072 rows of 8 planes 27 us in four launches (4.8, 6.3, 6.5 and 9.1: the first
+// that the order in which they run shows nowhere.  4238 rows of 12 planes 7.2 us; 131072 rows of 8 planes 28 us in four launches (4.9, 7.3, 6.5 and 9.0: the first
 // reads of each, and sums over the counts of 16 chunks), 230 with one workgroup a plane.
 constexpr int kKeepThreads = 1024, kKeepWaves = kKeepThreads / 64;
 constexpr int kKeepShift[3] = {21, 10, 0}, kKeepBins[3] = {2048, 2048, 1024};
