@@ -145,6 +145,10 @@ SHAPES = [
     (1, 3, 400, 4, 1, 64, True, (402, 403), 64),
     (1, 3, 400, 4, 1, 128, True, (200, 200), 64),
     (1, 50, 400, 4, 1, 128, True, (450, 450), 64),
+    (1, 48, 1306, 8, 2, 128, True, None, 64),          # few rows of a slice: ranges down to 128 keys
+    (1, 60, 6000, 3, 1, 64, True, None, 16),
+    (2, 500, 100, 4, 1, 128, True, None, 64),          # ranges that only late rows see
+    (1, 130, 200, 4, 1, 128, True, (150, 330), 32),    # and rows before any of them
 ]
 
 
