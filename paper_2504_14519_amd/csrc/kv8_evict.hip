@@ -600,8 +600,8 @@ hipError_t launch_kv8_keep(const Kv8KeepArgs& a, hipStream_t st) {
 
 // ------------------------------------------------------------------------------------ gather
 // A block of kept rows of a head, keys (blockIdx.y = 0) or values: its scale is the largest that its rows had, rows of smaller scales are rounded to it.  Bound
-// by the bytes, in rows of head_dim from anywhere: 32768 of 131072 rows of 8 heads of 128 in 37 us, 134 MB at 3.6 TB/s (codes under way while the scales are compared:
-// 38; neighbouring heads in neighbouring workgroups: 39).
+// by the bytes, in rows of head_dim from anywhere: 32768 of 131072 rows of 8 heads of 128 in 27 us, 134 MB at 5.0 TB/s (behind a kernel that leaves the caches full of
+// what it wrote 37; then codes under way while the scales are compared 38, neighbouring heads in neighbouring workgroups 39).
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(const Kv8GatherArgs a) {
   constexpr int NP = D / 16;

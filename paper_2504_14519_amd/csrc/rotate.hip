@@ -3,10 +3,10 @@
 //   n = x r, r = (mean x^2 + eps)^(-1/2);   y = n w;   (y_a, y_b) -> (y_a cos - y_b sin, y_b cos + y_a sin), angle = position * frequency
 //   backward: dy = the result's gradient turned back;  dw = sum over rows and heads of dy n;  g = dy w;  dx = r (g - n mean(g n))
 //
-// Bound by the bytes: x in, result out.  A lane has two chunks of 8 elements that hold whole pairs, so that nothing but the two sums over a head
-// crosses lanes, head_dim / 16 lanes have a head of a row, and a wave has a few heads of its 8 (head_dim 64: 16) rows: all of its loads are under way
-// before the angles are made, which serve all of its heads.  An angle is made in 64 bits as a fraction of a turn (position * frequency passes 2^20, where 32
-// bits leave an error of a sixteenth), its sine and cosine in 32.
+// Bound by the bytes: x in, result out (past the caches: a slice's results do not fit them).  A lane has two chunks of 8 elements that hold whole pairs, so that
+// nothing but the two sums over a head crosses lanes, head_dim / 16 lanes have a head of a row, and a wave has a few heads of its 8 (head_dim 64: 16) rows: all of
+// its loads are under way before the angles are made, which serve all of its heads.  An angle is made in 64 bits as a fraction of a turn (position * frequency
+// passes 2^20, where 32 bits leave an error of a sixteenth), its sine and cosine in 32.
 #include "rotate.hpp"
 #include "row_tile.hpp"
 
@@ -104,7 +104,8 @@ SP_DEV RotateWave rotate_wave(const RotateArgs& a, int wave_u) {
   return {side, first, left < a.heads_wave ? left : a.heads_wave, (int64_t)(blockIdx.x / (unsigned)sets) * 4 + wave_u};
 }
 
-// 4096 rows of 80 heads of 128: 37 us, 168 MB at 4.5 TB/s, where a copy has 4.9; vector units busy 39 % (2 heads a wave 41 us, 8 41).
+// 4096 rows of 80 heads of 128: 28 us, 168 MB at 6.1 TB/s; with results that stay in the caches 37, and the attention that reads them next
+// is as fast either way.  2 heads a wave 35, 8 27, but 16384 rows of 8 query heads and a key head 18.2 and 17.4 us (4 heads: 17.0).
 template <int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
   constexpr int LANES = D / 16, ROWS = 64 / LANES, N = kRotateFwdHeads;
@@ -140,14 +141,14 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
     for (int j = 0; j < 16; ++j) v[j] *= inv * wt[j];
     t.template apply<false>(v);
     bf16_t* p = out + (int64_t)u * s.out_stride_h;
-    *reinterpret_cast<bf16x8*>(p + 8 * t.ca) = narrow(v);
-    *reinterpret_cast<bf16x8*>(p + 8 * t.cb) = narrow(v + 8);
+    __builtin_nontemporal_store(narrow(v), reinterpret_cast<bf16x8*>(p + 8 * t.ca));
+    __builtin_nontemporal_store(narrow(v + 8), reinterpret_cast<bf16x8*>(p + 8 * t.cb));
   }
 }
 
 // The gradient.  The weights' gradients are summed in the lanes over the rows and heads of a wave, over the waves of a workgroup in LDS, and over the
-// workgroups by rotate_weights_kernel, all in a fixed order.  16384 rows of 8 query heads and a key head of 128 (gradients in bf16 and float32): 27 us, 117 MB at
-// 4.4 TB/s, and 4 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
+// workgroups by rotate_weights_kernel, all in a fixed order.  16384 rows of 8 query heads and a key head of 128 (gradients in bf16 and float32): 24 us, 117 MB at
+// 4.9 TB/s, and 4 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
 // block ahead do not fit the registers).
 template <int D, bool INTERLEAVED, bool DOUT_F32>
 SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, INTERLEAVED>& t, int lane, float (&dw)[16]) {
@@ -197,8 +198,8 @@ SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, I
         v[j] = (y[j] * wt[j] - v[j] * back) * inv;
       }
       bf16_t* p = dx + (int64_t)u * s.stride_h;
-      *reinterpret_cast<bf16x8*>(p + 8 * t.ca) = narrow(v);
-      *reinterpret_cast<bf16x8*>(p + 8 * t.cb) = narrow(v + 8);
+      __builtin_nontemporal_store(narrow(v), reinterpret_cast<bf16x8*>(p + 8 * t.ca));
+      __builtin_nontemporal_store(narrow(v + 8), reinterpret_cast<bf16x8*>(p + 8 * t.cb));
     }
   }
 }

@@ -63,8 +63,8 @@ void plan_fwd(RotateArgs* a) {
   plan(a, kRotateFwdHeads, (int64_t)compute_units() * 4);
   a->workgroups = (int32_t)((a->row_blocks + 3) / 4 * (a->sets[0] + a->sets[1]));
 }
-// Backward: beyond 2 workgroups a compute unit, what it holds at once, the waves take several blocks of rows (16384 rows of 9 heads: 29.7 us,
-// with up to 4 a unit 32.6, 8 34.3), which leaves few sums of the weights' gradients to add up.
+// Backward: beyond 2 workgroups a compute unit, what it holds at once, the waves take several blocks of rows (16384 rows of 9 heads: 28.2 us,
+// with up to 4 a unit 30.8), which leaves few sums of the weights' gradients to add up.
 void plan_bwd(RotateArgs* a) {
   plan(a, kRotateBwdHeads, (int64_t)compute_units() * 4);
   const int64_t sets = a->sets[0] + a->sets[1], groups = (a->row_blocks + 3) / 4, fit = (int64_t)compute_units() * 2 / sets;
