@@ -63,9 +63,9 @@ struct Kv8KeepArgs {
   uint32_t* work;                // [planes][chunks * kKeepChunkWords + kKeepPlaneWords]
 };
 
-constexpr int kKeepChunkWords = 2048 + 2048 + 1024 + 1, kKeepPlaneWords = 4;
-// most rows of a plane for one workgroup (8 planes of 18000 rows 24 us both ways, of 32000 30 us and 24.5 in four launches)
-constexpr int kKeepOneRows = 16 * 1024;
+constexpr int kKeepChunkWords = (2048 + 2048 + 1024) * 33 / 32 + 1, kKeepPlaneWords = 4;
+// most rows of a plane for one workgroup (8 planes of 16384 rows 16.7 us, of 18000 17.5 in four launches), and rows that a workgroup of several takes at a time
+constexpr int kKeepOneRows = 16 * 1024, kKeepSpan = 4 * 1024;
 
 struct Kv8GatherArgs {
   Kv8Cache from, to;

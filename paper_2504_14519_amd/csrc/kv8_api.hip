@@ -187,14 +187,14 @@ int check_keep(int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int
   if (planes < 1 || planes > 65535 || rows < 1 || rows > (int64_t)1 << 30 || capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;
   return rows <= capacity && keep >= 1 && keep <= rows && recent >= 0 && recent <= keep ? SLIMPIPE_OK : SLIMPIPE_EINVAL_RANGE;
 }
-// Workgroups of 8192 rows, more where there would be more than 64 of them (each adds up the counts of all of its plane).
+// Workgroups of kKeepSpan rows, of more where there would be more than 64 of them (each adds up the counts of all of its plane).
 struct KeepPlan {
   int32_t chunks;
   int64_t chunk;
 };
 KeepPlan keep_plan_of(int64_t rows) {
   if (rows <= kKeepOneRows) return {0, 0};
-  const int64_t span = 8192, chunk = (rows + 64 * span - 1) / (64 * span) * span;
+  const int64_t chunk = (rows + 64 * kKeepSpan - 1) / (64 * kKeepSpan) * kKeepSpan;
   return {(int32_t)((rows + chunk - 1) / chunk), chunk};
 }
 size_t keep_bytes_of(int32_t planes, const KeepPlan& plan) { return plan.chunks ? (size_t)planes * ((size_t)plan.chunks * kKeepChunkWords + kKeepPlaneWords) * 4 : 0; }

@@ -356,8 +356,8 @@ hipError_t launch_kv8_weights(const Kv8WeightArgs& a, int head_dim, bool few, hi
 // ------------------------------------------------------------------------------------ keep
 // The rows of a plane that are kept: the `recent` last ones and those of the others with the largest weights.  A radix selection (11, 11 and 10 bits) finds the
 // smallest weight that is taken and how many rows of exactly that weight are; a last walk writes the indices in order.  Counts alone cross threads, so
-// that the order in which they run shows nowhere.  4238 rows of 12 planes 7.2 us; 131072 rows of 8 planes 28 us in four launches (4.9, 7.3, 6.5 and 9.0: the first
-// reads of each, and sums over the counts of 16 chunks), 230 with one workgroup a plane.
+// that the order in which they run shows nowhere.  4238 rows of 12 planes 7.2 us; 131072 rows of 8 planes 21.5 us in four launches, 32000 18 (all bins of all chunks added
+// up by every workgroup 29 and 24.5; 8192 rows a chunk 22 and 21), and 230 with one workgroup a plane.
 constexpr int kKeepThreads = 1024, kKeepWaves = kKeepThreads / 64;
 constexpr int kKeepShift[3] = {21, 10, 0}, kKeepBins[3] = {2048, 2048, 1024};
 
@@ -368,17 +368,23 @@ SP_DEV uint32_t weight_order(float w) {
   if (u == 0x80000000u) u = 0u;
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-// Inclusive sum over the workgroup's threads, and the sum of all.  Two barriers.
-struct KeepScan { uint32_t upto, total; };
-SP_DEV KeepScan keep_scan(uint32_t v, uint32_t (&wave_sums)[kKeepWaves]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  // (row_shr by 1, 2, 4 and 8 inside each sixteen, then the last lane of a sixteen to the next one, and of the first half to the second)
+// Inclusive sum over the lanes of a half-wave, or of a wave (row_shr by 1, 2, 4 and 8 inside each sixteen, then the last lane of a sixteen to the next one, and of the
+// first half to the second).
+template <int LANES>
+SP_DEV uint32_t lane_scan(uint32_t v) {
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, true);
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, true);
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, true);
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, true);
   v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
-  v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+  if constexpr (LANES == 64) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+// Inclusive sum over the workgroup's threads, and the sum of all.  Two barriers.
+struct KeepScan { uint32_t upto, total; };
+SP_DEV KeepScan keep_scan(uint32_t v, uint32_t (&wave_sums)[kKeepWaves]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = lane_scan<64>(v);
   __syncthreads();
   if (lane == 63) wave_sums[wave] = v;
   __syncthreads();
@@ -390,7 +396,7 @@ SP_DEV KeepScan keep_scan(uint32_t v, uint32_t (&wave_sums)[kKeepWaves]) {
   }
   return s;
 }
-struct KeepShared { uint32_t hist[2048], wave_sums[kKeepWaves], found[2], entry[kKeepOneRows / 64]; };
+struct KeepShared { uint32_t hist[2048], wave_sums[kKeepWaves], found[4], entry[kKeepOneRows / 64]; };
 
 // What is known of the smallest weight that is taken: its leading bits, and how many rows that begin with them are wanted.
 struct KeepFound { uint32_t prefix, need; };
@@ -409,7 +415,7 @@ SP_DEV KeepFound keep_find(KeepShared& sh, int pass, uint32_t first, uint32_t se
   return f;
 }
 // Rows of a wave in the bin of its first one are counted there in one step: many weights may be equal (0 above all), or lie within one bin of a pass, and adds to one
-// counter wait for each other (131072 equal weights of 8 planes 30 us, one by one 46; uniform ones 29 and 28; 4238 of 12 planes 7.3 and 15.6, 7.2 and 6.8).
+// counter wait for each other (131072 equal weights of 8 planes 22 us, one by one 16 more; uniform ones a microsecond less; 4238 of 12 planes 7.3 and 15.6, 7.2 and 6.8).
 SP_DEV void keep_count(KeepShared& sh, int pass, uint32_t u, uint32_t prefix) {
   const int above = kKeepShift[pass] + (pass == 2 ? 10 : 11);
   if (pass > 0 && (u >> above) != (prefix >> above)) return;
@@ -485,93 +491,134 @@ __global__ __launch_bounds__(kKeepThreads) void kv8_keep_kernel(const Kv8KeepArg
   for (int i = tid; i < a.recent; i += kKeepThreads) out[a.keep - a.recent + i] = others + i;
 }
 
-// More rows: a workgroup for every a.chunk of them (a multiple of kKeepSpan), a launch a pass.  The counts of a pass stay in the workspace, [plane][chunk]
-// [2048]; every workgroup of the next pass adds its plane's up.  Behind them, for each chunk, how many of its rows are known to be above; and for each
-// plane what the passes found.
-constexpr int kKeepSpan = 8 * kKeepThreads;
+// More rows: a workgroup for every a.chunk of them (a multiple of kKeepSpan), a launch a pass.  The counts of a pass stay in the workspace, [plane][chunk], by bin and
+// by groups of 32 bins; the first wave of every workgroup of the next pass adds up its plane's counts of the groups, then those of the bins of one group.  Behind
+// them, for each chunk, how many of its rows are known to be above; and for each plane what the passes found.
+constexpr int kKeepGroup = 32;
 struct KeepWork {
-  uint32_t *hist[3], *above, *found;
+  uint32_t *hist[3], *groups[3], *above, *found;
   SP_DEV KeepWork(const Kv8KeepArgs& a, int plane) {
     uint32_t* p = a.work + (int64_t)plane * (a.chunks * (int64_t)kKeepChunkWords + kKeepPlaneWords);
-    for (int i = 0; i < 3; p += (int64_t)a.chunks * kKeepBins[i], ++i) hist[i] = p;
+    for (int i = 0; i < 3; ++i) {
+      hist[i] = p;
+      p += (int64_t)a.chunks * kKeepBins[i];
+      groups[i] = p;
+      p += a.chunks * (kKeepBins[i] / kKeepGroup);
+    }
     above = p;
     found = p + a.chunks;
   }
 };
-static_assert(kKeepChunkWords == 2048 + 2048 + 1024 + 1, "words of a chunk");
+static_assert(kKeepChunkWords == (2048 + 2048 + 1024) * 33 / 32 + 1, "words of a chunk");
+
+// What pass P found, by the counts of all chunks, in one wave; with it the rows of this chunk that the pass puts above (LAST: those of the chunks before, and in
+// `same` how many of them are in the bin).
+struct KeepStep { KeepFound found; uint32_t above, same; };
+template <int P, bool LAST>
+SP_DEV KeepStep keep_step(const KeepWork& work, int chunks, int chunk, KeepFound so_far) {
+  constexpr int BINS = kKeepBins[P], GROUPS = BINS / kKeepGroup;
+  static_assert(GROUPS <= 64 && kKeepGroup == 32, "a lane a group, half a wave the bins of one");
+  const int lane = threadIdx.x & 63;
+  auto at = [](uint32_t v, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+  // (loads of 16 or 8 chunks under way at once, those behind the last read once more)
+  auto add = [&](auto read, int first, int step, auto n_, uint32_t& total, uint32_t& part) {
+    constexpr int N = decltype(n_)::value;
+    for (int c0 = first; c0 < chunks; c0 += N * step) {
+      uint32_t n[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) n[i] = read(c0 + i * step < chunks ? c0 + i * step : chunks - 1);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = c0 + i * step;
+        total += c < chunks ? n[i] : 0u;
+        part += (LAST ? c < chunk : c == chunk) ? n[i] : 0u;      // (chunk < chunks)
+      }
+    }
+  };
+  // groups from the top on, a lane each
+  uint32_t total = 0, part = 0;
+  if (lane < GROUPS) add([&](int c) { return work.groups[P][c * GROUPS + GROUPS - 1 - lane]; }, 0, 1, std::integral_constant<int, 16>{}, total, part);
+  uint32_t upto = lane_scan<64>(total);
+  int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto - total < so_far.need && so_far.need <= upto));
+  uint32_t need = so_far.need - at(upto - total, l), above = at(lane_scan<64>(part) - part, l);
+  // its bins from the top on; the chunks shared out between the half-waves
+  const int group = GROUPS - 1 - l, bin = group * kKeepGroup + kKeepGroup - 1 - lane % 32;
+  total = part = 0;
+  add([&](int c) { return work.hist[P][(int64_t)c * BINS + bin]; }, lane / 32, 2, std::integral_constant<int, 8>{}, total, part);
+  total += (uint32_t)__shfl_xor((int)total, 32, 64);
+  part += (uint32_t)__shfl_xor((int)part, 32, 64);
+  upto = lane_scan<32>(total);
+  l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto - total < need && need <= upto));
+  need -= at(upto - total, l);
+  above += at(lane_scan<32>(part) - part, l);
+  return {{so_far.prefix | at((uint32_t)bin, l) << kKeepShift[P], need}, above, at(part, l)};
+}
 
 // PASS 0 .. 2: counts of a chunk; PASS 3: the indices.
 template <int PASS>
 __global__ __launch_bounds__(kKeepThreads) void kv8_keep_pass_kernel(const Kv8KeepArgs a) {
+  constexpr int V = kKeepSpan / kKeepThreads;      // rows of a thread at a time
   __shared__ KeepShared sh;
-  const int tid = threadIdx.x, chunk = blockIdx.x, plane = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, chunk = blockIdx.x, plane = blockIdx.y;
   const int64_t others = a.rows - a.recent, first = (int64_t)chunk * a.chunk, last = first + a.chunk < others ? first + a.chunk : others;
   const float* const w = a.weights + plane * a.capacity;
   const KeepWork work(a, plane);
   // (the first rows are on their way while the last pass is added up)
-  float x[8];
+  float x[V];
   auto load = [&](int64_t at) {
 #pragma unroll
-    for (int v = 0; v < 8; ++v) x[v] = at + v * kKeepThreads + tid < last ? w[at + v * kKeepThreads + tid] : 0.f;
+    for (int v = 0; v < V; ++v) x[v] = at + v * kKeepThreads + tid < last ? w[at + v * kKeepThreads + tid] : 0.f;
   };
   load(first);
   KeepFound f{0u, (uint32_t)(a.keep - a.recent)};
-  uint32_t above = 0, same = 0;                // PASS 3: rows before the chunk; else: those of it that the passes so far have put above
+  uint32_t above = 0, same = 0;                // PASS 3: rows before the chunk
   const bool all = f.need >= (uint32_t)others, search = f.need > 0 && !all;
-  if (PASS > 0 && search) {
-    constexpr int P = PASS > 0 ? PASS - 1 : 0, PER = kKeepBins[P] / kKeepThreads;
-    if (PASS > 1) f = KeepFound{work.found[2 * PASS - 4], work.found[2 * PASS - 3]};
-    const int top = kKeepBins[P] - 1 - tid * PER;
-    uint32_t total[2] = {0, 0}, before[2] = {0, 0}, mine[2] = {0, 0};
-#pragma unroll 16
-    for (int c = 0; c < a.chunks; ++c)
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const uint32_t n = work.hist[P][(int64_t)c * kKeepBins[P] + top - i];
-        total[i] += n;
-        before[i] += c < chunk ? n : 0u;
-        mine[i] += c == chunk ? n : 0u;
+  if constexpr (PASS > 0) {
+    if (search && tid < 64) {
+      if (PASS > 1) f = KeepFound{work.found[2 * PASS - 4], work.found[2 * PASS - 3]};
+      KeepStep step = keep_step<PASS - 1, PASS == 3>(work, a.chunks, chunk, f);
+      if (PASS == 3) step.above += (uint32_t)__builtin_amdgcn_readlane((int)lane_scan<64>(lane < chunk ? work.above[lane] : 0u), 63);
+      if (tid == 0) {
+        sh.found[0] = step.found.prefix;
+        sh.found[1] = step.found.need;
+        sh.found[2] = step.above;
+        sh.found[3] = step.same;
+        // rows of the chunk that the passes so far have put above; and the first workgroup of a plane writes down what all of them have found
+        if (PASS < 3) work.above[chunk] = step.above + (PASS > 1 ? work.above[chunk] : 0u);
+        if (PASS < 3 && chunk == 0) { work.found[2 * PASS - 2] = step.found.prefix; work.found[2 * PASS - 1] = step.found.need; }
       }
-    const KeepFound was = f;
-    f = keep_find(sh, P, total[0], total[1], f);
-    // of the bins above the one found: rows of this chunk, or (the last time) of the chunks before
-    const int bin = (int)((f.prefix ^ was.prefix) >> kKeepShift[P]);
-    uint32_t n = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) n += top - i > bin ? (PASS == 3 ? before[i] : mine[i]) : 0u;
-    above = keep_scan(n, sh.wave_sums).total;
-    if (PASS == 3) {
-      __syncthreads();
-      if (top == bin) sh.found[0] = before[0];
-      uint32_t known = 0;
-      for (int c = tid; c < chunk; c += kKeepThreads) known += work.above[c];
-      above += keep_scan(known, sh.wave_sums).total;
-      same = sh.found[0];
-    } else if (tid == 0) {
-      if (PASS > 1) above += work.above[chunk];
-      work.above[chunk] = above;
     }
   }
   if constexpr (PASS < 3) {
-    // (the first workgroup of a plane writes down what all of them have found, for the next launch)
-    if (PASS > 0 && chunk == 0 && tid == 0) { work.found[2 * PASS - 2] = f.prefix; work.found[2 * PASS - 1] = f.need; }
-    keep_clear(sh, PASS);
+    keep_clear(sh, PASS);                      // (and a barrier)
+    if (PASS > 0) f = KeepFound{sh.found[0], sh.found[1]};
     for (int64_t at = first; at < last; at += kKeepSpan) {
       if (at > first) load(at);
 #pragma unroll
-      for (int v = 0; v < 8; ++v)
+      for (int v = 0; v < V; ++v)
         if (at + v * kKeepThreads + tid < last) keep_count(sh, PASS, weight_order(x[v]), f.prefix);
     }
     __syncthreads();
-    for (int i = tid; i < kKeepBins[PASS]; i += kKeepThreads) work.hist[PASS][(int64_t)chunk * kKeepBins[PASS] + i] = sh.hist[i];
+#pragma unroll
+    for (int i = tid; i < kKeepBins[PASS]; i += kKeepThreads) {
+      const uint32_t n = sh.hist[i], sum = lane_scan<32>(n);
+      work.hist[PASS][(int64_t)chunk * kKeepBins[PASS] + i] = n;
+      if (lane % kKeepGroup == kKeepGroup - 1) work.groups[PASS][(chunk * kKeepBins[PASS] + i) / kKeepGroup] = sum;
+    }
   } else {
     int32_t* const out = a.index + (int64_t)plane * a.keep;
+    __syncthreads();
+    if (search) {
+      f = KeepFound{sh.found[0], sh.found[1]};
+      above = sh.found[2];
+      same = sh.found[3];
+    }
     for (int64_t at = first; search && at < last; at += kKeepSpan) {
       if (at > first) load(at);
-      uint32_t u[8];
+      uint32_t u[V];
 #pragma unroll
-      for (int v = 0; v < 8; ++v) u[v] = weight_order(x[v]);
-      keep_write<8>(sh, u, at, last, f, above, same, out);
+      for (int v = 0; v < V; ++v) u[v] = weight_order(x[v]);
+      keep_write<V>(sh, u, at, last, f, above, same, out);
     }
     if (all)
       for (int64_t i = first + tid; i < last; i += kKeepThreads) out[i] = (int32_t)i;
