@@ -324,8 +324,13 @@ __global__ __launch_bounds__(256) void kv8_weights_sum_kernel(const Kv8WeightArg
   const int64_t keys = a.kv_end - a.kv_begin, planes = (int64_t)a.batch * a.cache.n_kv_heads, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= keys * planes) return;
   float sum = 0.f;
-#pragma unroll 8
-  for (int p = 0; p < a.n_parts; ++p) sum += a.part[p * planes * keys + i];
+  for (int p0 = 0; p0 < a.n_parts; p0 += 8) {      // (eight loads under way at once, zeros behind the last)
+    float x[8];
+#pragma unroll
+    for (int p = 0; p < 8; ++p) x[p] = p0 + p < a.n_parts ? a.part[(p0 + p) * planes * keys + i] : 0.f;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) sum += x[p];
+  }
   put_weight(a, i / keys, a.kv_begin + i % keys, sum);
 }
 

@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
 
 // The gradient.  The weights' gradients are summed in the lanes over the rows and heads of a wave, over the waves of a workgroup in LDS, and over the
 // workgroups by rotate_weights_kernel, all in a fixed order.  16384 rows of 8 query heads and a key head of 128 (gradients in bf16 and float32): 24 us, 117 MB at
-// 4.9 TB/s, and 4 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
+// 4.9 TB/s, and 3 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
 // block ahead do not fit the registers).
 template <int D, bool INTERLEAVED, bool DOUT_F32>
 SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, INTERLEAVED>& t, int lane, float (&dw)[16]) {
@@ -239,8 +239,14 @@ __global__ __launch_bounds__(1024) void rotate_weights_kernel(const RotateArgs a
   const int groups = a.workgroups / (a.sets[0] + a.sets[1]), n = groups * a.sets[side];
   const float* p = a.part + (side ? (int64_t)groups * a.sets[0] * D : 0) + e;
   float v = 0.f;
-#pragma unroll 16
-  for (int i = k; i < n; i += 64) v += p[(int64_t)i * D];
+  // (eight loads under way at once, zeros behind the last)
+  for (int i0 = k; i0 < n; i0 += 8 * 64) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = i0 + 64 * i < n ? p[(int64_t)(i0 + 64 * i) * D] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += x[i];
+  }
   sums[k][c] = v;
   __syncthreads();
   if (k >= 4) return;                                     // (the first wave: 4 threads an element)
