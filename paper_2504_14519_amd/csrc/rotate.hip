@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void rotate_fwd_kernel(const RotateArgs a) {
 
 // The gradient.  The weights' gradients are summed in the lanes over the rows and heads of a wave, over the waves of a workgroup in LDS, and over the
 // workgroups by rotate_weights_kernel, all in a fixed order.  16384 rows of 8 query heads and a key head of 128 (gradients in bf16 and float32): 24 us, 117 MB at
-// 4.9 TB/s, and 3 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
+// 4.9 TB/s, and 3 to 4 for the last sums; what is left is the start of a block of rows, whose loads nothing hides but the other wave of the SIMD (loads of the next
 // block ahead do not fit the registers).
 template <int D, bool INTERLEAVED, bool DOUT_F32>
 SP_DEV void rotate_back_rows(const RotateArgs& a, const RotateWave& w, Turn<D, INTERLEAVED>& t, int lane, float (&dw)[16]) {
