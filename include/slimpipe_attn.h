@@ -350,7 +350,8 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
 
 /* weights[b, h, j] = decay * previous[b, h, j] + sum of exp(scale * q.k_j - lse) over the rows of the slice that see key j and the query heads of kv head h, for
  * the keys of [kv_begin, kv_end); others are untouched.  weights, previous: float32 [batch, n_kv_heads, kv_capacity], contiguous; previous may be NULL (for 0) or
- * weights itself.  lse: what the attention of these rows over all their keys returned; a row whose lse is -inf adds nothing.  Values are not read.
+ * weights itself.  lse: what the attention of these rows over all their keys returned; a row whose lse is -inf adds nothing, whatever
+ * its queries hold (rows of a padded batch, for instance).  Values are not read.
  * workspace: slimpipe_attn_kv8_weights_workspace_bytes (may be 0: NULL then).  Sums run in a fixed order, in 32 bits.
  *   limits : as for the cache's other calls; decay finite; ceil(keys / 256) * batch * n_kv_heads < 2^25 (SLIMPIPE_EINVAL_SHAPE otherwise). */
 int slimpipe_attn_kv8_weights_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);

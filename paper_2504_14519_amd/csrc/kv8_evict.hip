@@ -12,7 +12,8 @@ SP_DEV void put_weight(const Kv8WeightArgs& a, int64_t plane, int64_t key, float
   const int64_t at = plane * a.capacity + key;
   a.weights[at] = a.previous ? __builtin_fmaf(a.decay, a.previous[at], sum) : sum;
 }
-// lse of a row in log2 units, where exp2(score - that) is 0 for rows that saw nothing
+// lse of a row in log2 units, where exp2(score - that) is 0 for rows that saw nothing, if the score is finite.  Queries of such a row (a padded one, perhaps), or
+// keys that it alone sees, may not be: it is masked for every key as well.
 SP_DEV float row_norm(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
 
 // Tokens: at most 16 SETS rows of a plane.  S^T = K Q^T as in the attention of tokens (kv8.hip): codes go from memory to the matrix unit, a lane holds one row's
@@ -44,9 +45,10 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
     const bf16_t* qp = a.q + (int64_t)b * a.q_stride_b + (int64_t)my.r * a.q_stride_s + (int64_t)my.h * a.q_stride_h + 16 * h4;
 #pragma unroll
     for (int j = 0; j < W; ++j) q[r][j] = *reinterpret_cast<const bf16x8*>(qp + 64 * (j / 2) + 8 * (j % 2));
-    norm[r] = rh < rows ? row_norm(a.lse[((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r]) : INFINITY;
+    const float lse = a.lse[((int64_t)b * a.n_q_heads + my.h) * a.s_q + my.r];      // (behind the last row: that row once more, taken away by its norm)
+    norm[r] = rh < rows ? row_norm(lse) : INFINITY;
     const int64_t see = (a.causal && a.q_offset + my.r < hi - 1 ? a.q_offset + my.r : hi - 1) - lo;
-    see_rel[r] = see < -1 ? -1 : (int)see;
+    see_rel[r] = see < -1 || lse == -INFINITY ? -1 : (int)see;
   }
   int min_see = see_rel[0];
 #pragma unroll
@@ -160,7 +162,8 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
     const float* const lse = a.lse + ((int64_t)b * a.n_q_heads + (int64_t)hk * a.group) * a.s_q;
     const uint32_t row_bytes = (uint32_t)a.q_stride_s * 2;
     // Row rh of those that the workgroup walks is row r_min + rh % vis of head rh / vis.  A tile of one head, most of them, is copied from a uniform base.
-    // The rows' lse come along, behind the ring.
+    // The rows' lse come along, behind the ring, and into registers, where they are asked for rows that the tile's fast path would not leave out.
+    float ahead[kWeightRows / 64];
     constexpr int RPP = 64 / NC;                                      // rows of a copy instruction
     auto copy_tile = [&](int t) {
       const unsigned to = lds + (t % kWeightRing) * TILE, to_lse = lds + kWeightRing * TILE + (t % kWeightRing) * kWeightRows * 4;
@@ -168,8 +171,11 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       if (r0 + kWeightRows <= vis) {
         const bf16_t* src = q_base + (int64_t)h0 * a.q_stride_h + (int64_t)(r_min + r0) * a.q_stride_s;
 #pragma unroll
-        for (int n = 0; n < kWeightRows; n += 64)
-          dma4(uniform_ptr(lse + (int64_t)h0 * a.s_q + r_min + r0 + n), (uint32_t)lane * 4, __builtin_amdgcn_readfirstlane(to_lse + n * 4));
+        for (int n = 0; n < kWeightRows; n += 64) {
+          const float* from = uniform_ptr(lse + (int64_t)h0 * a.s_q + r_min + r0 + n);
+          dma4(from, (uint32_t)lane * 4, __builtin_amdgcn_readfirstlane(to_lse + n * 4));
+          ahead[n / 64] = from[lane];
+        }
 #pragma unroll
         for (int n = 0; n < PASSES; ++n) WaveDma<D, kWeightRows>::copy_pass(to, uniform_ptr(src), row_bytes, kWeightRows, lane, wave_u * PASSES + n);
         return;
@@ -184,6 +190,7 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       for (int n = 0; n < kWeightRows; n += 64) {
         const int rl = at(rh0 + n + lane, hl);
         dma4_at(lse + (int64_t)hl * a.s_q + rl, to_lse + n * 4);
+        ahead[n / 64] = lse[(int64_t)hl * a.s_q + rl];
       }
 #pragma unroll
       for (int n = 0; n < PASSES; ++n) {
@@ -264,9 +271,14 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       if (kWeightRing == 3 && t + 1 < t1) wait_copies<PASSES + kWeightRows / 64>();
       else wait_async();
       __syncthreads();
+      // Rows with lse -inf?  (256 us without the question, 259 with it; of the LDS copies, which the wave would wait for here, 265, and 11 % more at head_dim 64)
+      bool none = false;
+#pragma unroll
+      for (int n = 0; n < kWeightRows / 64; ++n) none |= ahead[n] == -INFINITY;
+      const bool whole = unmasked(t) && __builtin_amdgcn_ballot_w64(none) == 0;
       if (t + kWeightRing - 1 < t1) copy_tile(t + kWeightRing - 1);
       lo_q += (t % kWeightRing) * TILE;
-      if (unmasked(t)) {
+      if (whole) {
         float norm[BLOCKS];
 #pragma unroll
         for (int j = 0; j < BLOCKS; ++j) norm[j] = norm_of(t * BLOCKS + j);
@@ -286,9 +298,10 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
           if (j > 0) lo_q += 32 * D * 2;
           scores(even, false, 0.f);
           const int rh = (t * BLOCKS + j) * 32 + (lane & 31), rc = rh < rows ? rh : rows - 1;
-          const int64_t far = rel + (int)((unsigned)rc % (unsigned)vis);      // last key of the wave that the lane's row sees
-          const int see = (far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
           const float norm = norm_of(t * BLOCKS + j);
+          // last key of the wave that the lane's row sees
+          const int64_t far = norm == INFINITY ? -1 : a.causal ? rel + (int)((unsigned)rc % (unsigned)vis) : 63;
+          const int see = (far > 63 ? 63 : far < -1 ? -1 : (int)far) - 4 * g;
 #pragma unroll
           for (int e = 0; e < 32; ++e) {
             const float p = exp2_fast(__builtin_fmaf(s[0][e / 16][e % 16], a.scale_log2e, -norm));
