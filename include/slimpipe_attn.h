@@ -365,7 +365,7 @@ int slimpipe_attn_kv8_keep_workspace_bytes(int32_t planes, int64_t rows, int64_t
 int slimpipe_attn_kv8_keep(const float* weights, int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int64_t recent, int32_t* index,
                            void* workspace, size_t workspace_bytes, void* hip_stream);
 /* Rows index[b, h, 0 .. keep - 1] of every kv head of a cache (p) as rows 0 .. keep - 1 of another one (to: its kv_capacity and kv strides, the same batch, kv
- * heads and head_dim; the same block_len).  A block's scale is the largest that its rows had; rows of smaller scales are rounded to it (without an error
+ * heads and head_dim; the same block_len).  A block's scale is the largest that its rows had (2^-110 where none is a row); rows of smaller scales are rounded to it (without an error
  * but for elements that fall below 2^-6 of it).  Rows of `to` behind them keep their codes.  index: int32 [batch, n_kv_heads, keep]; any will do: a row may come
  * twice, an entry outside [0, kv_capacity) gives a row of zeros.  weights, kept_weights: the sums move along, [batch, n_kv_heads, kv_capacity] of either
  * cache; both or neither NULL.  The two caches, and the two sums, may not share memory (SLIMPIPE_EINVAL_RANGE). */

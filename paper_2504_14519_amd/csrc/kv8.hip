@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void kv8_store_kernel(const Kv8CopyArgs a) {
   }
   // largest = 1.m 2^(E - 127): 448 = 1.75 * 2^8, so e = E - 127 - 8, one more where 1.m > 1.75, and at least -110
   int byte = (int)(most >> 7) - 8 + ((most & 0x7fu) > 0x60u ? 1 : 0);
-  byte = byte < 17 ? 17 : byte;
+  byte = byte < (int)kKv8LeastScale ? (int)kKv8LeastScale : byte;
   byte = byte < (int)old ? (int)old : byte;
   const float unit = kv8_scale((uint32_t)byte);
 #pragma unroll

@@ -698,6 +698,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(const Kv8GatherArgs a) 
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < 4; ++w) byte = byte > most[w] ? byte : most[w];
+  byte = byte < kKv8LeastScale ? kKv8LeastScale : byte;      // (a block without a row)
   const float unit = kv8_scale(byte);
   for (int i = tid; i < n * NP; i += 256) {
     const int r = i / NP, c = i % NP;

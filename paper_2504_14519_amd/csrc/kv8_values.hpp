@@ -8,6 +8,7 @@ namespace slimpipe {
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
+constexpr uint32_t kKv8LeastScale = 17;      // 2^-110
 SP_DEV float kv8_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 SP_DEV int64_t kv8_scale_at(const Kv8Cache& c, int64_t b, int64_t row, int h) { return (b * c.blocks + (row >> c.shift)) * c.n_kv_heads + h; }
 
