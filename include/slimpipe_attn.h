@@ -353,7 +353,7 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
  * weights itself.  lse: what the attention of these rows over all their keys returned; a row whose lse is -inf adds nothing, whatever
  * its queries hold (rows of a padded batch, for instance).  Values are not read.
  * workspace: slimpipe_attn_kv8_weights_workspace_bytes (may be 0: NULL then).  Sums run in a fixed order, in 32 bits.
- *   limits : as for the cache's other calls; decay finite; ceil(keys / 256) * batch * n_kv_heads < 2^25 (SLIMPIPE_EINVAL_SHAPE otherwise). */
+ *   limits : as for the cache's other calls; decay finite; ceil(keys / 256) * batch * n_kv_heads <= 2^24 - 8 (SLIMPIPE_EINVAL_SHAPE otherwise). */
 int slimpipe_attn_kv8_weights_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);
 int slimpipe_attn_kv8_weights(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
                               const float* lse, const float* previous, float decay, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -178,10 +178,11 @@ int fwd_by_copy(const slimpipe_attn_params* p, const Kv8Cache& cache, const void
 size_t weight_bytes_of(const slimpipe_attn_params* p, const Kv8WeightPlan& plan) {
   return plan.few || plan.parts <= 1 ? 0 : up((size_t)plan.parts * p->batch * p->n_kv_heads * (size_t)(p->kv_end - p->kv_begin) * 4);
 }
-// What the sums check beyond check_cache: workgroups that a launch numbers in 31 bits.
+// What the sums check beyond check_cache: less than 2^32 threads, 256 for each of the workgroups, which are launched in eights.  (Parts of the rows are cut only where
+// there are few.)
 int check_weights(const slimpipe_attn_params* p) {
   const int64_t blocks = (p->kv_end - p->kv_begin + kv8_weight_keys() - 1) / kv8_weight_keys();
-  return blocks * p->batch * p->n_kv_heads * 64 < (int64_t)1 << 31 ? SLIMPIPE_OK : SLIMPIPE_EINVAL_SHAPE;
+  return blocks * p->batch * p->n_kv_heads <= ((int64_t)1 << 24) - 8 ? SLIMPIPE_OK : SLIMPIPE_EINVAL_SHAPE;
 }
 int check_keep(int32_t planes, int64_t capacity, int64_t rows, int64_t keep, int64_t recent) {
   if (planes < 1 || planes > 65535 || rows < 1 || rows > (int64_t)1 << 30 || capacity > (int64_t)1 << 36) return SLIMPIPE_EINVAL_SHAPE;
