@@ -338,8 +338,10 @@ int slimpipe_attn_kv8_load(const slimpipe_attn_params* p, int32_t block_len, con
 /* slimpipe_attn_fwd over such a cache, from one token to a slice: the same visibility, out, lse and rows without a key, and (out, lse) of key
  * ranges fold with those of bf16 and 4-bit calls.  workspace: slimpipe_attn_kv8_workspace_bytes (may be 0: NULL then; less is refused with
  * SLIMPIPE_EWORKSPACE).  For slices of 2048 and more rows of a kv head that includes room for a bf16 copy of the keys and values they see (4 * head_dim bytes a key and
- * kv head); such a call may be given less: it then converts tile by tile, in as many key ranges as there is room for, up to an eighth slower.  Results do not
- * depend on the order in which workgroups run, only on the room.  Codes are converted to bf16 exactly; roundings are otherwise those of slimpipe_attn_fwd. */
+ * kv head); such a call may be given less: it then converts tile by tile, in as many key ranges as there is room for, or copies all the same where that is
+ * faster.  A call whose blocks of 256 rows fill the chip is up to a third slower then; one of fewer blocks fills it with key ranges, and needs their room (256 rows
+ * of 8 heads on one behind 32512 keys, us with 29 MiB, what the query says, 73, with 16 74, 8 106, 2 372, none 722).  Results do not depend on the order in which workgroups
+ * run, only on the room.  Codes are converted to bf16 exactly; roundings are otherwise those of slimpipe_attn_fwd. */
 int slimpipe_attn_kv8_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);
 int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
                           const void* v_codes, const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -54,6 +54,14 @@ typedef struct slimpipe_call_path {
 } slimpipe_call_path;
 int slimpipe_attn_call_path(const slimpipe_attn_params* p, int is_bwd, int32_t n_chunks, size_t workspace_bytes, slimpipe_call_path* path);
 
+/* How slimpipe_attn_fwd_kv8 does a call with a workspace of workspace_bytes (SLIMPIPE_EWORKSPACE where it refuses that).  Host code only, nothing is launched. */
+typedef struct slimpipe_kv8_call_path {
+  int32_t copy;            /* the dense kernel over a bf16 copy of the keys */
+  int32_t ranges;          /* key ranges (of the dense call over the copy, or of the tiles) */
+  int32_t workgroup_rows;  /* rows of a workgroup that converts tiles (0 with a copy, 32 the kernel of few rows) */
+} slimpipe_kv8_call_path;
+int slimpipe_attn_kv8_call_path(const slimpipe_attn_params* p, int32_t block_len, size_t workspace_bytes, slimpipe_kv8_call_path* path);
+
 /* How the kernel of 32-row and 32-key items would do a backward call that takes it (slimpipe_attn_call_path: small), for gradients that do
  * not lie over out or lse (there own_statistics is 0).  All zero for other calls.  Host code only, nothing is launched. */
 typedef struct slimpipe_small_bwd_plan {

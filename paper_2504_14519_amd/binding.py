@@ -82,6 +82,10 @@ class SmallBwdPlan(ctypes.Structure):
     _fields_ = [("small", ctypes.c_int32), ("key_blocks", ctypes.c_int32), ("own_statistics", ctypes.c_int32), ("dq_first", ctypes.c_int32)]
 
 
+class Kv8CallPath(ctypes.Structure):
+    _fields_ = [("copy", ctypes.c_int32), ("ranges", ctypes.c_int32), ("workgroup_rows", ctypes.c_int32)]
+
+
 def library_path():
     return _LIB_PATH
 
@@ -179,6 +183,8 @@ def _load():
     L.slimpipe_attn_profile_read.restype = ctypes.c_int
     L.slimpipe_attn_bwd_plan.argtypes = [P, i32, ctypes.c_size_t, ctypes.POINTER(BwdPlan)]
     L.slimpipe_attn_bwd_plan.restype = ctypes.c_int
+    L.slimpipe_attn_kv8_call_path.argtypes = [vp, i32, ctypes.c_size_t, ctypes.POINTER(Kv8CallPath)]
+    L.slimpipe_attn_kv8_call_path.restype = ctypes.c_int
     L.slimpipe_attn_call_path.argtypes = [P, ctypes.c_int, i32, ctypes.c_size_t, ctypes.POINTER(CallPath)]
     L.slimpipe_attn_call_path.restype = ctypes.c_int
     L.slimpipe_attn_small_bwd_plan.argtypes = [P, i32, ctypes.c_size_t, ctypes.POINTER(SmallBwdPlan)]
@@ -1063,6 +1069,13 @@ def slimpipe_attn_call_path(params, is_bwd, n_chunks, workspace_bytes):
     """Which kernels a call with a workspace of that size takes (host code only; forward: 0 bytes = no workspace)."""
     path = CallPath()
     _check(lib.slimpipe_attn_call_path(ctypes.byref(params), 1 if is_bwd else 0, n_chunks, workspace_bytes, ctypes.byref(path)), "call_path")
+    return path
+
+
+def slimpipe_attn_kv8_call_path(params, block_len, workspace_bytes):
+    """How slimpipe_attn_fwd_kv8 does a call with a workspace of that size (host code only)."""
+    path = Kv8CallPath()
+    _check(lib.slimpipe_attn_kv8_call_path(ctypes.byref(params), block_len, workspace_bytes, ctypes.byref(path)), "kv8_call_path")
     return path
 
 

@@ -3,6 +3,7 @@
 #include <string.h>
 
 #include "host_common.hpp"
+#include "../../include/slimpipe_attn_bench.h"
 #include "kv8.hpp"
 
 using namespace slimpipe;
@@ -159,6 +160,40 @@ slimpipe_attn_params copy_params(const slimpipe_attn_params* p) {
   c.kv_stride_b = (c.kv_end - c.kv_begin) * c.kv_stride_s;
   return c;
 }
+// How a call goes with this much room: by a copy of the keys, or by this plan.  (plan.parts 0: it needs more.)
+struct Kv8Path {
+  bool copy;
+  Kv8Plan plan;
+};
+Kv8Path path_within(const slimpipe_attn_params* p, size_t room) {
+  Kv8Path path{false, plan_of(p)};
+  Kv8Plan& plan = path.plan;
+  const bool may_copy = copies(p);
+  const int64_t blocks = (int64_t)p->batch * p->n_kv_heads * ((rows_of(p) + 255) / 256), units = compute_units();
+  if (room < bytes_of(p, plan)) {
+    if (!may_copy) { plan.parts = 0; return path; }
+    // A long slice: as many key ranges as there is room for, and workgroups of four waves where the chip would be half empty with eight (256 rows of 8 heads on one and 32768
+    // keys, us with eight and with four, 1 range 834 and 723, 3 302 and 254, 12 90 and 79; 4096 rows of 4 heads on 16096 keys, 2 ranges, 128 workgroups of eight, 231 and
+    // 197, 3 163 and 189).
+    const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin;
+    for (int64_t parts = plan.parts - 1; room < bytes_of(p, plan); --parts) cut_keys(&plan, keys, parts);
+    if (plan.kernel == Kv8Kernel::eight_waves && 2 * blocks * plan.parts <= units) plan.kernel = Kv8Kernel::four_waves;
+  }
+  if (!may_copy || room < 2 * copy_bytes(p)) return path;
+  const slimpipe_attn_params c = copy_params(p);
+  const size_t rest = room - 2 * copy_bytes(p);
+  size_t wanted = 0;
+  slimpipe_call_path dense;
+  if (slimpipe_attn_workspace_bytes(&c, 0, &wanted) != SLIMPIPE_OK) return path;
+  path.copy = rest >= wanted;
+  if (path.copy || slimpipe_attn_call_path(&c, 0, 1, rest, &dense) != SLIMPIPE_OK) return path;
+  // With less beside the copy than the dense call asks for: what a compute unit has to do, in blocks of rows and all keys, tiles 1.22 times as long (us by the copy and by
+  // tiles in the same room: 2048 rows of 8 heads on 32768 keys, no range fits, 585 and 704; 4096 of 40 on 18688, as many blocks as fill the chip, 1288 and 1568; 4096 of 4
+  // on 16096 307 and 163).
+  auto load = [&](int64_t ranges) { return fmax(1.0 / (double)ranges, (double)blocks / (double)units); };
+  path.copy = load(dense.ranges) <= 1.22 * load(plan.parts);
+  return path;
+}
 int fwd_by_copy(const slimpipe_attn_params* p, const Kv8Cache& cache, const void* q, void* out, float* lse, char* ws, size_t bytes, void* stream) {
   const slimpipe_attn_params c = copy_params(p);
   const size_t each = copy_bytes(p);
@@ -277,6 +312,24 @@ int slimpipe_attn_kv8_workspace_bytes(const slimpipe_attn_params* p, int32_t blo
   return rc;
 }
 
+int slimpipe_attn_kv8_call_path(const slimpipe_attn_params* p, int32_t block_len, size_t workspace_bytes, slimpipe_kv8_call_path* out) {
+  if (!p || !out) return SLIMPIPE_EINVAL_NULL;
+  int rc = slimpipe_attn_validate(p, 0);
+  if (rc == SLIMPIPE_OK) rc = check_cache(p, block_len);
+  if (rc != SLIMPIPE_OK) return rc;
+  const Kv8Path path = path_within(p, workspace_bytes);
+  if (path.plan.parts < 1) return SLIMPIPE_EWORKSPACE;
+  if (path.copy) {
+    const slimpipe_attn_params c = copy_params(p);
+    slimpipe_call_path dense;
+    rc = slimpipe_attn_call_path(&c, 0, 1, workspace_bytes - 2 * copy_bytes(p), &dense);
+    if (rc == SLIMPIPE_OK) *out = {1, dense.ranges, 0};
+    return rc;
+  }
+  *out = {0, path.plan.parts, path.plan.kernel == Kv8Kernel::few ? kKv8FewRows : path.plan.kernel == Kv8Kernel::four_waves ? 128 : 256};
+  return SLIMPIPE_OK;
+}
+
 int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, const void* q_slice, const void* k_codes, const void* k_scales,
                           const void* v_codes, const void* v_scales, void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream) {
   int rc = slimpipe_attn_validate(p, 0);
@@ -288,16 +341,11 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
   if (!aligned16(q_slice) || !aligned16(out) || !aligned4(lse)) return SLIMPIPE_EINVAL_ALIGN;
   if (!aligned16(workspace)) return SLIMPIPE_EINVAL_ALIGN;
   if (!workspace) workspace_bytes = 0;
-  Kv8Plan plan = plan_of(p);
-  const bool may_copy = copies(p), copy = may_copy && workspace_bytes >= 2 * copy_bytes(p);
-  if (!copy && workspace_bytes < bytes_of(p, plan)) {
-    if (!may_copy) return SLIMPIPE_EWORKSPACE;
-    // (a long slice without room for the copy: as many key ranges as there is room for)
-    const int64_t keys = seen_end(p, p->kv_begin, p->kv_end) - p->kv_begin;
-    for (int64_t parts = plan.parts - 1; workspace_bytes < bytes_of(p, plan); --parts) cut_keys(&plan, keys, parts);
-  }
+  const Kv8Path path = path_within(p, workspace_bytes);
+  const Kv8Plan& plan = path.plan;
+  if (plan.parts < 1) return SLIMPIPE_EWORKSPACE;
   const Kv8Cache cache = cache_of(p, block_len, k_codes, k_scales, v_codes, v_scales);
-  if (copy) {
+  if (path.copy) {
     if (ensure_device_ready() != SLIMPIPE_OK) return SLIMPIPE_ELAUNCH;
     return fwd_by_copy(p, cache, q_slice, out, lse, static_cast<char*>(workspace), workspace_bytes, hip_stream);
   }
