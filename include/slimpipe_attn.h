@@ -352,8 +352,9 @@ int slimpipe_attn_fwd_kv8(const slimpipe_attn_params* p, int32_t block_len, cons
 
 /* weights[b, h, j] = decay * previous[b, h, j] + sum of exp(scale * q.k_j - lse) over the rows of the slice that see key j and the query heads of kv head h, for
  * the keys of [kv_begin, kv_end); others are untouched.  weights, previous: float32 [batch, n_kv_heads, kv_capacity], contiguous; previous may be NULL (for 0) or
- * weights itself.  lse: what the attention of these rows over all their keys returned; a row whose lse is -inf adds nothing, whatever
- * its queries hold (rows of a padded batch, for instance).  Values are not read.
+ * weights itself.  previous is read for all of these keys, those of the slice's own rows too: it has to hold 0 for rows that are new.  lse: what the attention
+ * of these rows over all their keys returned; a row whose lse is -inf adds nothing, whatever its queries hold (rows of a padded batch, for instance).  Values are
+ * not read.
  * workspace: slimpipe_attn_kv8_weights_workspace_bytes (may be 0: NULL then).  Sums run in a fixed order, in 32 bits.
  *   limits : as for the cache's other calls; decay finite; ceil(keys / 256) * batch * n_kv_heads <= 2^24 - 8 (SLIMPIPE_EINVAL_SHAPE otherwise). */
 int slimpipe_attn_kv8_weights_workspace_bytes(const slimpipe_attn_params* p, int32_t block_len, size_t* bytes);
@@ -370,7 +371,8 @@ int slimpipe_attn_kv8_keep(const float* weights, int32_t planes, int64_t capacit
  * heads and head_dim; the same block_len).  A block's scale is the largest that its rows had (2^-110 where none is a row); rows of smaller scales are rounded to it (without an error
  * but for elements that fall below 2^-6 of it).  Rows of `to` behind them keep their codes.  index: int32 [batch, n_kv_heads, keep]; any will do: a row may come
  * twice, an entry outside [0, kv_capacity) gives a row of zeros.  weights, kept_weights: the sums move along, [batch, n_kv_heads, kv_capacity] of either
- * cache; both or neither NULL.  The two caches, and the two sums, may not share memory (SLIMPIPE_EINVAL_RANGE). */
+ * cache; both or neither NULL.  kept_weights of the rows behind (from `keep` on) are left as they are: before slimpipe_attn_kv8_weights adds to them, rows that are
+ * appended there have to get 0, wherever the memory may hold anything else.  The two caches, and the two sums, may not share memory (SLIMPIPE_EINVAL_RANGE). */
 int slimpipe_attn_kv8_gather(const slimpipe_attn_params* p, int32_t block_len, const int32_t* index, int64_t keep, const void* k_codes,
                              const void* k_scales, const void* v_codes, const void* v_scales, const float* weights, const slimpipe_attn_params* to,
                              void* to_k_codes, void* to_k_scales, void* to_v_codes, void* to_v_scales, float* kept_weights, void* hip_stream);

@@ -851,7 +851,8 @@ def slimpipe_attn_kv8_weights_workspace_bytes(q_slice, cache, q_offset, kv_begin
 def slimpipe_attn_kv8_weights(q_slice, cache, lse, q_offset, kv_begin, kv_end, causal=True, scale=None, weights=None, previous=None, decay=1.0,
                               workspace=None):
     """-> weights [B, Hkv, capacity] fp32: for the keys of [kv_begin, kv_end) decay * previous (None: 0; may be weights itself) and the attention weights of the
-    slice's rows and their heads, by the lse that their attention returned; other entries stay as they are (zero where the call allocates)."""
+    slice's rows and their heads, by the lse that their attention returned; other entries stay as they are (zero where the call allocates).  previous is read
+    for the slice's own keys too: 0 for rows that are new."""
     shape = q_slice.shape
     _check_rows("q_slice", q_slice, shape)
     _check_lse(lse, shape)
@@ -898,7 +899,8 @@ def slimpipe_attn_kv8_keep(weights, rows, keep, recent=0, index=None, workspace=
 
 def slimpipe_attn_kv8_gather(cache, index, kept, weights=None, kept_weights=None):
     """Rows index [B, Hkv, keep] (int32) of every kv head of a KvCache8 become rows 0 .. keep - 1 of the KvCache8 `kept`; with them the sums weights [B, Hkv,
-    capacity of cache], where given, those of kept_weights [B, Hkv, capacity of kept].  -> kept"""
+    capacity of cache], where given, those of kept_weights [B, Hkv, capacity of kept]; kept_weights[..., keep:] stays as it is, and has to be 0 for rows
+    that are appended there before their weights are added up.  -> kept"""
     (B, N, H, D), s_from = cache.layout()
     (B2, N2, H2, D2), s_to = kept.layout()
     if (B2, H2, D2, kept.block_len) != (B, H, D, cache.block_len):
