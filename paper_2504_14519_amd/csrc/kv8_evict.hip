@@ -199,7 +199,6 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       }
     };
     copy_tile(t0);
-    if (kWeightRing == 3 && t0 + 1 < t1) copy_tile(t0 + 1);
     // K in registers.  The contraction may take head_dim in any order: lane group g has elements 32 j + 16 g .. + 15 in steps 2 j and 2 j + 1, one load.
     bf16x8 k[2][KS];
 #pragma unroll
@@ -267,16 +266,15 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_kernel(const Kv8WeightArgs
       for (int e = 0; e < 32; ++e) acc[e / 16][e % 16] += exp2_fast(__builtin_fmaf(s[1][e / 16][e % 16], a.scale_log2e, -left_norm));
     };
     for (int t = t0; t < t1; ++t) {
-      // this wave's copies of tile t have landed; with a ring of three those of tile t + 1 may be under way
-      if (kWeightRing == 3 && t + 1 < t1) wait_copies<PASSES + kWeightRows / 64>();
-      else wait_async();
+      // this wave's copies of tile t have landed, behind the barrier those of all waves; and all have read tile t - 1, whose place tile t + 1 takes
+      wait_async();
       __syncthreads();
       // Rows with lse -inf?  (256 us without the question, 259 with it; of the LDS copies, which the wave would wait for here, 265, and 11 % more at head_dim 64)
       bool none = false;
 #pragma unroll
       for (int n = 0; n < kWeightRows / 64; ++n) none |= ahead[n] == -INFINITY;
       const bool whole = unmasked(t) && __builtin_amdgcn_ballot_w64(none) == 0;
-      if (t + kWeightRing - 1 < t1) copy_tile(t + kWeightRing - 1);
+      if (t + 1 < t1) copy_tile(t + 1);
       lo_q += (t % kWeightRing) * TILE;
       if (whole) {
         float norm[BLOCKS];

@@ -1,9 +1,10 @@
-// Attention of 32 query rows a wave on tiles of keys in LDS: the inner loop that the forward kernels of four waves share (gathered
-// rows on key blocks, rows on a cache in 4 bits).
+// Attention of 32 query rows a wave on tiles of keys in LDS: the inner loop that the forward kernels without phases share (gathered
+// rows on key blocks, rows on a cache in 4 bits or in 8).
 //   S^T = K Q^T        A = K rows from LDS (row-packed), B = Q in registers
 //   online softmax     one query column a lane: in-lane maxima and sums, one exchange between the half-waves
 //   O^T += V^T P^T     A = V through the transposed LDS read, B = P straight from the C registers
-// Two workgroups of four waves share a compute unit, so that one's softmax runs beside the other's matrix instructions: no phases.
+// Two workgroups of four waves share a compute unit (on 8 bits also one of eight waves has it), so that one wave's softmax runs beside another's matrix
+// instructions: no phases.
 #pragma once
 #include "tile_common.hpp"
 
