@@ -13,8 +13,9 @@
 extern "C" {
 #endif
 
-/* Per-kernel timing.  While enabled, the kernels of every entry point but slimpipe_attn_bwd_noalloc, the slimpipe_attn_block_ calls and
- * those of the 4-bit cache (and but the one-workgroup kernel that clears the forward's counters) are bracketed by HIP events recorded on the caller's stream; the
+/* Per-kernel timing.  While enabled, the kernels of every entry point but slimpipe_attn_bwd_noalloc, the slimpipe_attn_block_ calls,
+ * those of the 4-bit and 8-bit caches (but for the dense kernel behind slimpipe_attn_fwd_kv8's copy) and the norm and rotation (and but the one-workgroup kernel that clears
+ * the forward's counters) are bracketed by HIP events recorded on the caller's stream; the
  * launches are the same as without it.  slimpipe_attn_profile_read waits for the recorded events, adds up the elapsed time per
  * kernel kind since the last read and clears the records.  The records are process-wide and guarded by a mutex:
  * enabling the switch serialises the launches of concurrent host threads.  Both arrays of slimpipe_attn_profile_read have
