@@ -381,7 +381,8 @@ int slimpipe_attn_kv8_gather(const slimpipe_attn_params* p, int32_t block_len, c
  * go through before the attention calls.  For a head x of a row at position t
  *     y = x / sqrt(mean(x^2) + eps) * weight;  of the first rotate_dim elements the pairs (i, i + rotate_dim / 2), or (2 i, 2 i + 1) when
  *     interleaved, become (y_a cos - y_b sin, y_b cos + y_a sin) at the angle t * frequencies[i]; the others stay.
- * Angles are computed in 64 bits, norms and products in 32, results rounded to bf16 once.
+ * Angles are computed in 64 bits, norms and products in 32, results rounded to bf16 once.  (A head whose sum of squares passes 2^128, with elements of 2^60
+ * and more, has results of 0, and a gradient that may be NaN.)
  *   q, k            : bf16 [batch, rows, heads, head_dim] with the q and k strides (parts of one projected row, for instance); a side with 0 heads is not part
  *                     of the call, its pointers may be NULL.
  *   q_weight, k_weight : float32 [head_dim], NULL for ones.

@@ -158,8 +158,9 @@ constexpr size_t kv8_fwd_lds_bytes() {         // two slots of converted K and V
 
 // Slices of less than 2048 rows of a kv head (or where there is no room for a bf16 copy of the keys): 256 or 128 rows a workgroup of NW waves, 32 a wave
 // (row_tile.hpp).  Codes of a tile of 64 keys are fetched one tile ahead into registers and converted into LDS for all waves at once.  256 rows of 40 heads on
-// 16640 keys: 104 us (830 TFLOP/s, the fold of three ranges included), and 102 on a bf16 cache; 4096 rows of 8 heads on 32768 keys 513 us, by the copy 455:
-// the waves' matrix and vector phases are not kept apart as in the dense kernel.
+// 16640 keys: 104 us (830 TFLOP/s, the fold of the ranges included), and 102 on a bf16 cache; 4096 rows of 8 heads on 32768 keys 513 us, by the copy 455:
+// the waves' matrix and vector phases are not kept apart as in the dense kernel.  (On a machine whose 8192^3 bf16 product runs at 1405 TFLOP/s; on one of 1245 119
+// and, by the copy, 516.)
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, 2) void kv8_fwd_kernel(const Kv8Args a) {
   constexpr int BN = 64, TILE = BN * D * 2, NP = D / 16, PER = 2 * BN * NP / (NW * 64), ROWS = NW * 32;      // pieces of 16 elements of a row; of a thread, K and V
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv8_fwd_kernel(const Kv8Args a) {
 //                    takes bytes 16 h .. 16 h + 15 of every 64 of a row, two steps, and 16 rows' codes are a load of whole lines
 //   O^T += V^T P^T   V passes through 32 rows of LDS of the wave's own for the transposed read (lane group h: keys 4 h .. 4 h + 3 of either 16)
 // Codes of the next DEPTH steps are under way in registers.  Neighbouring heads lie in a workgroup, and the workgroups that cover the same keys of a sequence
-// follow one another on one XCD.  Tokens of 4 sequences of 32768 keys, 40 heads of 128: 241 us, 1.34 GB at 5.6 TB/s; matrix units busy 8 %, vector units 23 %
+// follow one another on one XCD.  Tokens of 4 sequences of 32768 keys, 40 heads of 128: 241 us (with a profiler 250), 1.34 GB at 5.6 TB/s; matrix units busy 8 %, vector units 23 %
 // (one step under way 250 us, three or four 246; 128 registers for four workgroups a unit with two steps: spilled, 500).
 template <int D, int SETS>
 constexpr size_t kv8_few_lds_bytes() {

@@ -122,9 +122,10 @@ __global__ __launch_bounds__(256, 2) void kv8_weights_few_kernel(const Kv8Weight
 //   sums               p = exp2(c s - norm) added in place: the lane's sums over its rows, over the lanes at the end
 // A pair costs the vector unit three instructions, one of them an exponential, beside 2 D flop: both units have about the same to do at D = 128, twice
 // as much the vector unit at 64.  So the scores of a block of 32 rows are computed while the exponentials of the block before are taken, instruction by instruction.
-// 4096 rows of 8 heads on 32768 keys of 128: 247 us, 1.04 PFLOP/s (with the exponentials behind the matrix instructions of the same block 274; tiles of 64 rows
-// in a ring of three 244, but 368 and 318 us for 16384 rows of 4 heads of 64 on 32768 keys; one pipeline over the four blocks of a tile 262: spills).  All but the
-// matrix instructions takes 175 us, all but the exponentials 215; at head_dim 64 all but the matrix instructions 300 of 328.
+// 4096 rows of 8 heads on 32768 keys of 128: 247 to 259 us, 1.0 PFLOP/s, on machines whose 8192^3 bf16 product runs at 1405 TFLOP/s, 283 on one of 1245.  (On the former:
+// with the exponentials behind the matrix instructions of the same block 274; tiles of 64 rows in a ring of three 244, but 368 and 318 us for 16384 rows of 4 heads of 64 on
+// 32768 keys; one pipeline over the four blocks of a tile 262: spills.  All but the matrix instructions 175 us, all but the exponentials 215: the two do not overlap
+// enough.  At head_dim 64 all but the matrix instructions 300 of 328.)
 constexpr int kWeightKeys = kv8_weight_keys(), kWeightRows = 128, kWeightRing = 2;
 template <int D>
 constexpr size_t kv8_weights_lds_bytes() { return (size_t)kWeightRing * kWeightRows * (D * 2 + 4); }
