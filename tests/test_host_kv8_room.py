@@ -58,7 +58,7 @@ def test_calls_that_fill_the_chip_and_calls_without_a_range_copy(sp):
     p = params(sp, 1, 4096, 40, 40, 128, 14592)
     assert path(sp, p, copy_bytes(p) + 512)[:2] == (1, 1) and path(sp, p, copy_bytes(p) - 512)[0] == 0 and path(sp, p, 0) == (0, 1, 256)
     # 64 blocks, room for the copy or for one range, not for two
-    p = params(sp, 1, 2048, 8, 1, 128, 30720)
+    p = params(sp, 1, 2048, 8, 1, 128, 30700)
     assert 2 * range_bytes(p) > copy_bytes(p) + 512
     assert path(sp, p, copy_bytes(p) + 512)[:2] == (1, 1) and path(sp, p, 2 * range_bytes(p) + 1024) == (0, 2, 128)
     # three ranges of 64 blocks: more than half of the chip with eight waves
